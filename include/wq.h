@@ -65,7 +65,9 @@ typedef enum {
                                take the stack (1..8 tokens, every layer with the same bits, groups
                                and rank), also where the launch chain is the measured-faster route */
 
-/* Output element types of wq_down_w4. */
+#define WQ_HEAD_NORM 8u     /* wq_qkv_rope: unit-weight RMSNorm (eps 1e-6) of every query and key head */
+
+/* Element types (outputs of wq_down_w4, rows of wq_kv_append and wq_kv_read). */
 #define WQ_BF16 0
 #define WQ_F32 1
 
@@ -356,6 +358,117 @@ wq_status wq_decoder_layer_forward(const void *x, int batch, const int32_t *lens
                                    size_t ws_bytes, void *stream);
 
 /*
+ * A KV cache: rows [batch, n_kv, max_len, head_dim] of K and of V (device memory,
+ * caller-owned), head_dim 64 or 128.
+ *   bits 16: bf16 values (the caches of wq_attn_decode); k_meta, v_meta NULL.
+ *   bits 8:  one byte a value.  bits 4: 32-bit words of 8 values, value e at bits
+ *            4 (e / 2) + 16 (e % 2).
+ * A row of 8 or 4 bits has one binary16 scale s and one whole zero z
+ * (0 <= z <= qmax = 2^bits - 1) in k_meta, v_meta: uint32 [batch, n_kv, max_len],
+ * s in the low half, z (binary16) in the high one.  A value is s (code - z).
+ */
+typedef struct {
+    void *k, *v;
+    uint32_t *k_meta, *v_meta;
+    int32_t batch, n_kv, max_len, head_dim, bits;
+} wq_kv_cache;
+
+/*
+ * Writes K and V rows into the cache, quantized on the way:
+ *   mn = min(0, row), mx = max(0, row), s = fp16((mx - mn) / qmax) (1 if that is 0),
+ *   z = clamp(rint(-mn / s), 0, qmax), code = clamp(rint(value / s) + z, 0, qmax),
+ * every step in fp32, round to nearest; bits 16: one rounding to bf16 (none for
+ * bf16 rows).  A row with an infinity or NaN, or whose scale is beyond binary16,
+ * is held as s = NaN: it reads back as NaN and makes what attends to it NaN.
+ *   k, v:    rows of `dtype` (WQ_BF16, WQ_F32); token t, head g of sequence b starts at
+ *            element b stride[0] + t stride[1] + g stride[2] (strides in elements, multiples
+ *            of 16 bytes, so that the rows may be slices of a q/k/v buffer); n_src
+ *            tokens a sequence.
+ *   start:   int32 [batch] on the device: row i of sequence b goes to position start[b] + i.
+ *   counts:  int32 [batch] on the device or NULL: rows of sequence b, at most n (NULL: n).
+ *   index:   int32 [batch, n] on the device or NULL: row i is source token index[b][i]
+ *            (the accepted path of a drafted tree; NULL: token i).
+ *   A sequence whose count or last position is out of range, and a row whose index
+ *   is outside [0, n_src), are skipped and recorded as WQ_ERR_ARG in the device status.
+ *   batch n_kv n < 2^30.  n == 0 is a no-op.
+ */
+wq_status wq_kv_append(const wq_kv_cache *cache, const void *k, const void *v, int dtype, int n_src,
+                       const int64_t k_stride[3], const int64_t v_stride[3], const int32_t *start,
+                       const int32_t *counts, const int32_t *index, int n, void *stream);
+
+/*
+ * Reads positions start[b] .. start[b] + n - 1 back: k, v of `dtype`
+ * [batch, n, n_kv, head_dim], the values s (code - z) exactly (WQ_F32) or rounded
+ * once (WQ_BF16); zeros from counts[b] on (NULL: n).  Ranges as for wq_kv_append;
+ * a skipped sequence's rows are left unwritten.
+ */
+wq_status wq_kv_read(const wq_kv_cache *cache, const int32_t *start, const int32_t *counts, int n, void *k, void *v,
+                     int dtype, void *stream);
+
+/*
+ * Query, key and value rows of m tokens from their projections, each token at a
+ * position of its own (a drafted token's is its depth in the tree, not its slot):
+ *   u = rs qkv[t], rs = 1 / sqrt(mean(x[t]^2) + 1e-6) (x NULL: 1); q and k heads
+ *   normed (WQ_HEAD_NORM) and rotated, element i with i + head_dim/2 by the angle
+ *   whose cosine and sine are table[positions[t]][i]; every output rounded once.
+ *   qkv:       fp32 [m, (n_heads + 2 n_kv) head_dim]: q heads, k heads, v heads.
+ *   x:         bf16 [m, d] or NULL.
+ *   positions: int32 [m] on the device; outside [0, n_pos) the token is skipped and
+ *              WQ_ERR_ARG recorded in the device status.
+ *   table:     fp32 [n_pos, head_dim / 2, 2]: cosine, sine.
+ *   q: bf16 [m, n_heads, head_dim]; k, v: bf16 [m, n_kv, head_dim].
+ */
+wq_status wq_qkv_rope(const float *qkv, const void *x, int m, int d, const int32_t *positions, const float *table,
+                      int n_pos, int n_heads, int n_kv, int head_dim, unsigned flags, void *q, void *k, void *v,
+                      void *stream);
+
+/*
+ * Attention of a tree of drafted tokens over a cache (grouped-query heads, kv head
+ * g = h / (n_heads / n_kv)).  Draft i of sequence b attends to the cached positions
+ * 0 .. lens[b] - 1 and to the drafts j < counts[b] that its mask row names:
+ *   o[b, i, h] = bf16( softmax_j(scale q . K_j) V_j ),  0 for a row that sees nothing.
+ * The drafts' own K and V rows are given in bf16 and not yet in the cache: once the
+ * tree is verified, wq_kv_append writes the accepted path (its `index`).  One draft
+ * is a decode step.
+ *   q:       bf16 [batch, n_draft, n_heads, head_dim]; k_new, v_new: bf16
+ *            [batch, n_draft, n_kv, head_dim]; n_draft <= 128 (0: a no-op).
+ *   lens:    int32 [batch], positions cached, 0 <= lens[b] <= max_len.
+ *   counts:  int32 [batch] or NULL: drafts of sequence b (NULL: n_draft); the outputs of
+ *            the drafts from there on are 0 and their inputs are not read.
+ *   mask:    uint32 [batch, n_draft, ceil(n_draft / 32)] or NULL: bit j % 32 of word j / 32
+ *            of row i lets draft i see draft j (NULL: itself and the earlier ones).
+ *            What a masked draft's K and V hold, infinities and NaN too, does not
+ *            reach the row.
+ *   A length or count outside its range skips the sequence (o unwritten) and records
+ *   WQ_ERR_ARG in the device status.  n_heads / n_kv <= 16.
+ * Workspace: wq_attn_tree_workspace_bytes for up to `batch` sequences and n_draft
+ * drafts (no zeroing needed).
+ */
+size_t wq_attn_tree_workspace_bytes(int batch, int n_draft, int n_heads, int n_kv, int head_dim, int max_len);
+wq_status wq_attn_tree(const void *q, const void *k_new, const void *v_new, int n_draft, int n_heads,
+                       const wq_kv_cache *cache, const int32_t *lens, const int32_t *counts, const uint32_t *mask,
+                       float scale, void *o, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * The verify step of a decoder layer for n_draft drafted tokens of each of the cache's
+ * `batch` sequences (m = batch n_draft tokens, token b n_draft + i is draft i):
+ *   qkv = x deq(Wqkv)^T (fp32), (q, k_new, v_new) = wq_qkv_rope(qkv, x, ..., WQ_HEAD_NORM),
+ *   o = wq_attn_tree(q, k_new, v_new, ..., scale 1/sqrt(head_dim)), then the output
+ *   projection and the MLP block as in wq_decoder_layer_forward (flags likewise).
+ * The cache is not changed; k_new, v_new (bf16 [m, n_kv, head_dim], caller-owned, one pair
+ * a layer) hold the drafts' rows for wq_kv_append of the accepted path.  x: bf16 [m, d]
+ * and positions: int32 [m], both for padding drafts too (their y is that of o = 0).
+ * The layer's rope_theta is not used (the angles are the table's).  m <= 16384.
+ * Workspace: wq_decoder_tree_workspace_bytes, zero-filled before first use
+ * (wq_workspace_init).
+ */
+size_t wq_decoder_tree_workspace_bytes(int batch, int n_draft, const wq_decoder_layer *layer, int max_len);
+wq_status wq_decoder_tree_forward(const void *x, int n_draft, const int32_t *lens, const int32_t *positions,
+                                  const wq_decoder_layer *layer, const wq_kv_cache *cache, const float *table, int n_pos,
+                                  const int32_t *counts, const uint32_t *mask, unsigned flags, void *k_new, void *v_new,
+                                  void *y, void *ws, size_t ws_bytes, void *stream);
+
+/*
  * A mixture-of-experts MLP block (the MoE model of Sec. 5: a router picks a
  * few experts per token, so a decode step reads only those experts' weights,
  * which is how expert routing shrinks the realized gain of the 2-bit gate/up).
@@ -456,7 +569,8 @@ const char *wq_last_error(void);
 
 /* Reads and clears the device-side status words of the current device: WQ_OK,
  * WQ_ERR_TIMEOUT (a bounded wait ran out) or WQ_ERR_ARG (wq_attn_decode met a
- * sequence length outside its cache).  Synchronizes the device. */
+ * sequence length outside its cache, or one of the KV-cache calls a start, count,
+ * index, position or length outside its range).  Synchronizes the device. */
 wq_status wq_device_status(int *status);
 
 /* Library version string. */

@@ -15,6 +15,7 @@
 #include "wq.h"
 #include "wq_batch.h"
 #include "wq_internal.h"
+#include "wq_kv.h"
 #include "wq_launch.h"
 #include "wq_stack.h"
 
@@ -1298,18 +1299,19 @@ namespace {
 // projections', the attention partials and the intermediates qkv (fp32), o, x1
 // and h (bf16).
 struct DecoderWs {
-  size_t cnt_qkv, cnt_o, mlp, proj_qkv, proj_o, attn, qkv, o, x1, h, total;
+  size_t cnt_qkv, cnt_o, mlp, proj_qkv, proj_o, attn, qkv, o, x1, h, q, total;
   size_t b_qkv, b_o;  // sizes of the projections' counter blocks
   size_t n_mlp, n_attn;
 };
 
-bool decoder_ws(int batch, const wq_decoder_layer &Ly, int max_len, DecoderWs *W) {
+// n_attn bytes for the attention's partial results, n_q for query rows of their own.
+bool decoder_ws(int batch, const wq_decoder_layer &Ly, size_t n_attn, size_t n_q, DecoderWs *W) {
   const int d = Ly.mlp.gate.k, inter = Ly.mlp.gate.n;
   const int H = Ly.n_heads, Hkv = Ly.n_kv, hd = Ly.head_dim;
   const int nqkv = (H + 2 * Hkv) * hd;
   W->n_mlp = wq_workspace_bytes(batch, d, inter, Ly.mlp.r);
   const size_t n_qkv = wq_workspace_bytes(batch, nqkv, d, 0), n_o = wq_workspace_bytes(batch, d, H * hd, 0);
-  W->n_attn = wq_attn_workspace_bytes(batch, H, Hkv, hd, max_len);
+  W->n_attn = n_attn;
   if (!W->n_mlp || !n_qkv || !n_o || !W->n_attn) return false;
   WsLayout L;
   W->b_qkv = counter_block(nqkv, d, &L);
@@ -1325,6 +1327,7 @@ bool decoder_ws(int batch, const wq_decoder_layer &Ly, int max_len, DecoderWs *W
   W->o = off;        off = up256(off + (size_t)batch * H * hd * 2);
   W->x1 = off;       off = up256(off + (size_t)batch * d * 2);
   W->h = off;        off = up256(off + (size_t)batch * inter * 2);
+  W->q = off;        off = up256(off + n_q);
   W->total = off;
   return true;
 }
@@ -1340,21 +1343,7 @@ wq_status decoder_projection(const char *name, const void *h, int m, const wq_qw
   return st == WQ_OK ? st : fail(st, "%s projection: %s", name, g_last_error.c_str());
 }
 
-}  // namespace
-
-extern "C" {
-
-size_t wq_decoder_workspace_bytes(int batch, const wq_decoder_layer *layer, int max_len) {
-  if (!layer || batch <= 0 || max_len <= 0) return 0;
-  DecoderWs W;
-  return decoder_ws(batch, *layer, max_len, &W) ? W.total : 0;
-}
-
-wq_status wq_decoder_layer_forward(const void *x, int batch, const int32_t *lens, const wq_decoder_layer *layer,
-                                   void *k_cache, void *v_cache, int max_len, unsigned flags, void *y, void *ws,
-                                   size_t ws_bytes, void *stream) {
-  if (!layer) return fail(WQ_ERR_ARG, "null layer");
-  const wq_decoder_layer &Ly = *layer;
+wq_status check_decoder_layer(const wq_decoder_layer &Ly) {
   const int d = Ly.mlp.gate.k, inter = Ly.mlp.gate.n;
   const int H = Ly.n_heads, Hkv = Ly.n_kv, hd = Ly.head_dim;
   wq_status st;
@@ -1363,22 +1352,15 @@ wq_status wq_decoder_layer_forward(const void *x, int batch, const int32_t *lens
       Ly.o.k != H * hd || Ly.mlp.down.n != d || Ly.mlp.down.k != inter)
     return fail(WQ_ERR_SHAPE, "decoder layer shapes disagree (qkv [%d x %d], o [%d x %d], d %d, heads %d/%d x %d)",
                 Ly.qkv.n, Ly.qkv.k, Ly.o.n, Ly.o.k, d, H, Hkv, hd);
-  if (flags & ~WQ_PRENORM) return fail(WQ_ERR_ARG, "unknown flags 0x%x", flags);
-  if (batch < 0) return fail(WQ_ERR_ARG, "batch %d", batch);
-  if (batch == 0) return ok();
-  DecoderWs W;
-  if (!decoder_ws(batch, Ly, max_len, &W)) return fail(WQ_ERR_SHAPE, "no workspace layout for this layer");
-  if (!ws || ws_bytes < W.total)
-    return fail(WQ_ERR_WORKSPACE, "decoder workspace of %zu bytes, %zu needed", ws_bytes, W.total);
-  uint8_t *w8 = static_cast<uint8_t *>(ws);
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if ((st = decoder_projection("qkv", x, batch, &Ly.qkv, nullptr, w8 + W.qkv, WQ_F32, W.b_qkv, W.cnt_qkv, W.proj_qkv, w8,
-                               s)) != WQ_OK)
-    return st;
-  // x, lens and the caches come from before the projection, whose launches wait first
-  if ((st = attn_decode_impl(reinterpret_cast<const float *>(w8 + W.qkv), x, lens, batch, d, H, Hkv, hd, Ly.rope_theta,
-                           k_cache, v_cache, max_len, w8 + W.o, w8 + W.attn, W.n_attn, true, stream)) != WQ_OK)
-    return fail(st, "attention: %s", g_last_error.c_str());
+  return WQ_OK;
+}
+
+// The rest of a decoder layer for m tokens: x1 = x + o deq(Wo)^T and the MLP block
+// on x1, o in the workspace.
+wq_status decoder_after_attention(const void *x, int m, const wq_decoder_layer &Ly, unsigned flags, void *y,
+                                  const DecoderWs &W, uint8_t *w8, cudaStream_t s) {
+  const int d = Ly.mlp.gate.k, inter = Ly.mlp.gate.n, H = Ly.n_heads, hd = Ly.head_dim, batch = m;
+  wq_status st;
   const wq_mlp_layer &M = Ly.mlp;
   // Decode sizes: the output projection's epilogue also writes the MLP
   // input's tile partials (RMSNorm sums and LoRA-A products of x1, as the
@@ -1434,16 +1416,254 @@ wq_status wq_decoder_layer_forward(const void *x, int batch, const int32_t *lens
     return st;
   if (M.gate.bits == 3)
     st = wq_gateup_w3_lora(w8 + W.x1, batch, &M.gate, &M.up, M.lora_a, M.lora_b_gate, M.lora_b_up, M.r, M.lora_scale,
-                           flags, w8 + W.h, w8 + W.mlp, W.n_mlp, stream);
+                           flags, w8 + W.h, w8 + W.mlp, W.n_mlp, s);
   else if (M.gate.bits == 2)
     st = wq_gateup_w2_lora(w8 + W.x1, batch, &M.gate, &M.up, M.lora_a, M.lora_b_gate, M.lora_b_up, M.r, M.lora_scale,
-                           flags, w8 + W.h, w8 + W.mlp, W.n_mlp, stream);
+                           flags, w8 + W.h, w8 + W.mlp, W.n_mlp, s);
   else
-    st = wq_gateup_w4(w8 + W.x1, batch, &M.gate, &M.up, flags, w8 + W.h, w8 + W.mlp, W.n_mlp, stream);
+    st = wq_gateup_w4(w8 + W.x1, batch, &M.gate, &M.up, flags, w8 + W.h, w8 + W.mlp, W.n_mlp, s);
   if (st != WQ_OK) return fail(st, "gate/up: %s", g_last_error.c_str());
-  if ((st = wq_down_w4(w8 + W.h, batch, &M.down, w8 + W.x1, y, WQ_BF16, w8 + W.mlp, W.n_mlp, stream)) != WQ_OK)
+  if ((st = wq_down_w4(w8 + W.h, batch, &M.down, w8 + W.x1, y, WQ_BF16, w8 + W.mlp, W.n_mlp, s)) != WQ_OK)
     return fail(st, "down: %s", g_last_error.c_str());
   return ok();
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t wq_decoder_workspace_bytes(int batch, const wq_decoder_layer *layer, int max_len) {
+  if (!layer || batch <= 0 || max_len <= 0) return 0;
+  DecoderWs W;
+  return decoder_ws(batch, *layer,
+                    wq_attn_workspace_bytes(batch, layer->n_heads, layer->n_kv, layer->head_dim, max_len), 0, &W)
+             ? W.total
+             : 0;
+}
+
+wq_status wq_decoder_layer_forward(const void *x, int batch, const int32_t *lens, const wq_decoder_layer *layer,
+                                   void *k_cache, void *v_cache, int max_len, unsigned flags, void *y, void *ws,
+                                   size_t ws_bytes, void *stream) {
+  if (!layer) return fail(WQ_ERR_ARG, "null layer");
+  const wq_decoder_layer &Ly = *layer;
+  const int d = Ly.mlp.gate.k, H = Ly.n_heads, Hkv = Ly.n_kv, hd = Ly.head_dim;
+  wq_status st;
+  if ((st = check_decoder_layer(Ly)) != WQ_OK) return st;
+  if (flags & ~WQ_PRENORM) return fail(WQ_ERR_ARG, "unknown flags 0x%x", flags);
+  if (batch < 0) return fail(WQ_ERR_ARG, "batch %d", batch);
+  if (batch == 0) return ok();
+  DecoderWs W;
+  if (!decoder_ws(batch, Ly, wq_attn_workspace_bytes(batch, H, Hkv, hd, max_len), 0, &W))
+    return fail(WQ_ERR_SHAPE, "no workspace layout for this layer");
+  if (!ws || ws_bytes < W.total)
+    return fail(WQ_ERR_WORKSPACE, "decoder workspace of %zu bytes, %zu needed", ws_bytes, W.total);
+  uint8_t *w8 = static_cast<uint8_t *>(ws);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if ((st = decoder_projection("qkv", x, batch, &Ly.qkv, nullptr, w8 + W.qkv, WQ_F32, W.b_qkv, W.cnt_qkv, W.proj_qkv, w8,
+                               s)) != WQ_OK)
+    return st;
+  // x, lens and the caches come from before the projection, whose launches wait first
+  if ((st = attn_decode_impl(reinterpret_cast<const float *>(w8 + W.qkv), x, lens, batch, d, H, Hkv, hd, Ly.rope_theta,
+                           k_cache, v_cache, max_len, w8 + W.o, w8 + W.attn, W.n_attn, true, stream)) != WQ_OK)
+    return fail(st, "attention: %s", g_last_error.c_str());
+  return decoder_after_attention(x, batch, Ly, flags, y, W, w8, s);
+}
+
+}  // extern "C"
+
+namespace {
+
+constexpr int kMaxDrafts = 128;
+
+wq_status check_cache(const wq_kv_cache *c) {
+  if (!c) return fail(WQ_ERR_ARG, "null wq_kv_cache");
+  if (c->bits != 16 && c->bits != 8 && c->bits != 4) return fail(WQ_ERR_UNSUPPORTED, "cache bits %d not 16, 8 or 4", c->bits);
+  if (c->head_dim != 64 && c->head_dim != 128) return fail(WQ_ERR_UNSUPPORTED, "head_dim %d not 64 or 128", c->head_dim);
+  if (c->batch <= 0 || c->n_kv <= 0 || c->max_len <= 0)
+    return fail(WQ_ERR_SHAPE, "cache of %d sequences, %d heads, %d positions", c->batch, c->n_kv, c->max_len);
+  if ((long long)c->batch * c->n_kv > INT32_MAX) return fail(WQ_ERR_SHAPE, "cache of %d x %d heads", c->batch, c->n_kv);
+  if (!c->k || !c->v) return fail(WQ_ERR_ARG, "null cache pointer");
+  if (!aligned16(c->k) || !aligned16(c->v)) return fail(WQ_ERR_ALIGN, "cache not 16-byte aligned");
+  if (c->bits != 16) {
+    if (!c->k_meta || !c->v_meta) return fail(WQ_ERR_ARG, "null scales of a quantized cache");
+    if (!aligned16(c->k_meta) || !aligned16(c->v_meta)) return fail(WQ_ERR_ALIGN, "scales not 16-byte aligned");
+  }
+  return WQ_OK;
+}
+
+// Rows n a sequence of a cache: the launches number them in 31 bits.
+wq_status check_rows(const wq_kv_cache *c, int n) {
+  if (n < 0) return fail(WQ_ERR_ARG, "%d rows a sequence", n);
+  if ((long long)c->batch * c->n_kv * n >= 1ll << 30)
+    return fail(WQ_ERR_SHAPE, "%d x %d heads x %d rows in one call", c->batch, c->n_kv, n);
+  return WQ_OK;
+}
+
+wq_status check_dtype(int dtype) {
+  return dtype == WQ_BF16 || dtype == WQ_F32 ? WQ_OK : fail(WQ_ERR_ARG, "dtype %d", dtype);
+}
+
+wq_status attn_tree_impl(const void *q, const void *k_new, const void *v_new, int n_draft, int n_heads,
+                         const wq_kv_cache *c, const int32_t *lens, const int32_t *counts, const uint32_t *mask,
+                         float scale, void *o, void *ws, size_t ws_bytes, cudaStream_t s) {
+  wq_status st;
+  if ((st = check_cache(c)) != WQ_OK) return st;
+  if (n_draft < 0 || n_draft > kMaxDrafts) return fail(WQ_ERR_UNSUPPORTED, "%d drafts, at most %d", n_draft, kMaxDrafts);
+  if (n_heads <= 0 || n_heads % c->n_kv != 0 || n_heads / c->n_kv > 16)
+    return fail(WQ_ERR_UNSUPPORTED, "n_heads %d / n_kv %d: a multiple, at most 16 query heads a kv head", n_heads, c->n_kv);
+  if (!std::isfinite(scale)) return fail(WQ_ERR_ARG, "score scale not finite");
+  if (n_draft == 0) return ok();
+  if (!q || !k_new || !v_new || !lens || !o || !ws) return fail(WQ_ERR_ARG, "null pointer");
+  if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(o) || !aligned16(ws))
+    return fail(WQ_ERR_ALIGN, "q, k_new, v_new, o or workspace not 16-byte aligned");
+  const int sms = num_sms();
+  if (sms <= 0) return fail(WQ_ERR_CUDA, "cannot query the current device");
+  const size_t need = wq_attn_tree_workspace_bytes(c->batch, n_draft, n_heads, c->n_kv, c->head_dim, c->max_len);
+  if (ws_bytes < need) return fail(WQ_ERR_WORKSPACE, "attention workspace of %zu bytes, %zu needed", ws_bytes, need);
+  TreeArgs a{};
+  a.q = q, a.kn = k_new, a.vn = v_new;
+  a.kc = c->k, a.vc = c->v, a.km = c->k_meta, a.vm = c->v_meta;
+  a.lens = lens, a.counts = counts, a.mask = mask;
+  a.batch = c->batch, a.T = n_draft, a.H = n_heads, a.Hkv = c->n_kv, a.max_len = c->max_len, a.words = (n_draft + 31) / 32;
+  a.scale = scale * 1.4426950408889634f;  // scores in units of log 2
+  a.part = static_cast<float *>(ws);
+  a.o = o;
+  a.S = tree_splits(c->batch, n_draft, n_heads, c->n_kv, c->max_len, sms);
+  cudaError_t e = launch_attn_tree(a, c->head_dim, c->bits, s);
+  if (e != cudaSuccess) return cuda_fail(e, "tree attention launch");
+  return ok();
+}
+
+}  // namespace
+
+extern "C" {
+
+wq_status wq_kv_append(const wq_kv_cache *cache, const void *k, const void *v, int dtype, int n_src,
+                       const int64_t k_stride[3], const int64_t v_stride[3], const int32_t *start,
+                       const int32_t *counts, const int32_t *index, int n, void *stream) {
+  wq_status st;
+  if ((st = check_cache(cache)) != WQ_OK || (st = check_dtype(dtype)) != WQ_OK || (st = check_rows(cache, n)) != WQ_OK)
+    return st;
+  if (n_src < 0 || (!index && n > n_src)) return fail(WQ_ERR_SHAPE, "%d rows of %d source tokens", n, n_src);
+  if (n == 0) return ok();
+  if (!k || !v || !k_stride || !v_stride || !start) return fail(WQ_ERR_ARG, "null pointer");
+  if (!aligned16(k) || !aligned16(v)) return fail(WQ_ERR_ALIGN, "k or v not 16-byte aligned");
+  KvAppendArgs a{};
+  const int per16 = dtype == WQ_F32 ? 4 : 8;  // values in 16 bytes
+  for (int i = 0; i < 3; ++i) {
+    if (k_stride[i] % per16 != 0 || v_stride[i] % per16 != 0)
+      return fail(WQ_ERR_ALIGN, "a stride of k or v is not a multiple of 16 bytes");
+    a.k_stride[i] = k_stride[i];
+    a.v_stride[i] = v_stride[i];
+  }
+  a.k = k, a.v = v, a.kc = cache->k, a.vc = cache->v, a.km = cache->k_meta, a.vm = cache->v_meta;
+  a.start = start, a.counts = counts, a.index = index;
+  a.batch = cache->batch, a.n_kv = cache->n_kv, a.max_len = cache->max_len, a.n_src = n_src, a.n = n;
+  cudaError_t e = launch_kv_append(a, cache->head_dim, cache->bits, dtype == WQ_F32, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(e, "cache append launch");
+  return ok();
+}
+
+wq_status wq_kv_read(const wq_kv_cache *cache, const int32_t *start, const int32_t *counts, int n, void *k, void *v,
+                     int dtype, void *stream) {
+  wq_status st;
+  if ((st = check_cache(cache)) != WQ_OK || (st = check_dtype(dtype)) != WQ_OK || (st = check_rows(cache, n)) != WQ_OK)
+    return st;
+  if (n == 0) return ok();
+  if (!k || !v || !start) return fail(WQ_ERR_ARG, "null pointer");
+  if (!aligned16(k) || !aligned16(v)) return fail(WQ_ERR_ALIGN, "k or v not 16-byte aligned");
+  KvReadArgs a{};
+  a.kc = cache->k, a.vc = cache->v, a.km = cache->k_meta, a.vm = cache->v_meta, a.k = k, a.v = v;
+  a.start = start, a.counts = counts;
+  a.batch = cache->batch, a.n_kv = cache->n_kv, a.max_len = cache->max_len, a.n = n;
+  cudaError_t e = launch_kv_read(a, cache->head_dim, cache->bits, dtype == WQ_F32, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(e, "cache read launch");
+  return ok();
+}
+
+wq_status wq_qkv_rope(const float *qkv, const void *x, int m, int d, const int32_t *positions, const float *table,
+                      int n_pos, int n_heads, int n_kv, int head_dim, unsigned flags, void *q, void *k, void *v,
+                      void *stream) {
+  if (m < 0) return fail(WQ_ERR_ARG, "m %d", m);
+  if (flags & ~WQ_HEAD_NORM) return fail(WQ_ERR_ARG, "unknown flags 0x%x", flags);
+  if (head_dim != 64 && head_dim != 128) return fail(WQ_ERR_UNSUPPORTED, "head_dim %d not 64 or 128", head_dim);
+  if (n_heads <= 0 || n_kv <= 0 || (long long)n_heads + 2ll * n_kv > 1 << 16)
+    return fail(WQ_ERR_SHAPE, "heads %d/%d", n_heads, n_kv);
+  if (x && (d <= 0 || d % 8 != 0)) return fail(WQ_ERR_SHAPE, "d %d (a positive multiple of 8)", d);
+  if (n_pos <= 0) return fail(WQ_ERR_SHAPE, "a table of %d positions", n_pos);
+  if (m == 0) return ok();
+  if (!qkv || !positions || !table || !q || !k || !v) return fail(WQ_ERR_ARG, "null pointer");
+  if (!aligned16(qkv) || !aligned16(x) || !aligned16(table) || !aligned16(q) || !aligned16(k) || !aligned16(v))
+    return fail(WQ_ERR_ALIGN, "qkv, x, table, q, k or v not 16-byte aligned");
+  QkvRopeArgs a{};
+  a.qkv = qkv, a.x = x, a.positions = positions, a.table = table, a.q = q, a.k = k, a.v = v;
+  a.d = d, a.n_heads = n_heads, a.n_kv = n_kv, a.n_pos = n_pos, a.head_norm = (flags & WQ_HEAD_NORM) ? 1 : 0;
+  cudaError_t e = launch_qkv_rope(a, m, head_dim, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(e, "rotary launch");
+  return ok();
+}
+
+size_t wq_attn_tree_workspace_bytes(int batch, int n_draft, int n_heads, int n_kv, int head_dim, int max_len) {
+  const int sms = num_sms();
+  if (batch <= 0 || n_draft <= 0 || n_heads <= 0 || n_kv <= 0 || head_dim <= 0 || max_len <= 0 || sms <= 0) return 0;
+  return up256(4 * tree_part_floats(batch, n_draft, n_heads, n_kv, head_dim, max_len, sms));
+}
+
+wq_status wq_attn_tree(const void *q, const void *k_new, const void *v_new, int n_draft, int n_heads,
+                       const wq_kv_cache *cache, const int32_t *lens, const int32_t *counts, const uint32_t *mask,
+                       float scale, void *o, void *ws, size_t ws_bytes, void *stream) {
+  return attn_tree_impl(q, k_new, v_new, n_draft, n_heads, cache, lens, counts, mask, scale, o, ws, ws_bytes,
+                        static_cast<cudaStream_t>(stream));
+}
+
+size_t wq_decoder_tree_workspace_bytes(int batch, int n_draft, const wq_decoder_layer *layer, int max_len) {
+  if (!layer || batch <= 0 || n_draft <= 0 || n_draft > kMaxDrafts || max_len <= 0 ||
+      (long long)batch * n_draft > kMaxGemmTokens)
+    return 0;
+  const int m = batch * n_draft, H = layer->n_heads, hd = layer->head_dim;
+  DecoderWs W;
+  return decoder_ws(m, *layer, wq_attn_tree_workspace_bytes(batch, n_draft, H, layer->n_kv, hd, max_len),
+                    (size_t)m * H * hd * 2, &W)
+             ? W.total
+             : 0;
+}
+
+wq_status wq_decoder_tree_forward(const void *x, int n_draft, const int32_t *lens, const int32_t *positions,
+                                  const wq_decoder_layer *layer, const wq_kv_cache *cache, const float *table, int n_pos,
+                                  const int32_t *counts, const uint32_t *mask, unsigned flags, void *k_new, void *v_new,
+                                  void *y, void *ws, size_t ws_bytes, void *stream) {
+  if (!layer) return fail(WQ_ERR_ARG, "null layer");
+  const wq_decoder_layer &Ly = *layer;
+  const int d = Ly.mlp.gate.k, H = Ly.n_heads, Hkv = Ly.n_kv, hd = Ly.head_dim;
+  wq_status st;
+  if ((st = check_decoder_layer(Ly)) != WQ_OK || (st = check_cache(cache)) != WQ_OK) return st;
+  if (cache->n_kv != Hkv || cache->head_dim != hd)
+    return fail(WQ_ERR_SHAPE, "cache of %d heads of %d, layer of %d of %d", cache->n_kv, cache->head_dim, Hkv, hd);
+  if (flags & ~WQ_PRENORM) return fail(WQ_ERR_ARG, "unknown flags 0x%x", flags);
+  if (n_draft < 0 || n_draft > kMaxDrafts) return fail(WQ_ERR_UNSUPPORTED, "%d drafts, at most %d", n_draft, kMaxDrafts);
+  if ((long long)cache->batch * n_draft > kMaxGemmTokens)
+    return fail(WQ_ERR_SHAPE, "%d x %d tokens, at most %d", cache->batch, n_draft, kMaxGemmTokens);
+  if (n_draft == 0) return ok();
+  if (!x || !lens || !positions || !table || !k_new || !v_new || !y) return fail(WQ_ERR_ARG, "null pointer");
+  const int m = cache->batch * n_draft;
+  const size_t n_attn = wq_attn_tree_workspace_bytes(cache->batch, n_draft, H, Hkv, hd, cache->max_len);
+  DecoderWs W;
+  if (!decoder_ws(m, Ly, n_attn, (size_t)m * H * hd * 2, &W))
+    return fail(WQ_ERR_SHAPE, "no workspace layout for this layer");
+  if (!ws || ws_bytes < W.total)
+    return fail(WQ_ERR_WORKSPACE, "decoder workspace of %zu bytes, %zu needed", ws_bytes, W.total);
+  uint8_t *w8 = static_cast<uint8_t *>(ws);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if ((st = decoder_projection("qkv", x, m, &Ly.qkv, nullptr, w8 + W.qkv, WQ_F32, W.b_qkv, W.cnt_qkv, W.proj_qkv, w8,
+                               s)) != WQ_OK)
+    return st;
+  if ((st = wq_qkv_rope(reinterpret_cast<const float *>(w8 + W.qkv), x, m, d, positions, table, n_pos, H, Hkv, hd,
+                        WQ_HEAD_NORM, w8 + W.q, k_new, v_new, stream)) != WQ_OK)
+    return fail(st, "rotary positions: %s", g_last_error.c_str());
+  if ((st = attn_tree_impl(w8 + W.q, k_new, v_new, n_draft, H, cache, lens, counts, mask, 1.f / std::sqrt((float)hd),
+                           w8 + W.o, w8 + W.attn, n_attn, s)) != WQ_OK)
+    return fail(st, "attention: %s", g_last_error.c_str());
+  return decoder_after_attention(x, m, Ly, flags, y, W, w8, s);
 }
 
 }  // extern "C"
@@ -1775,6 +1995,12 @@ wq_status wq_device_status(int *status) {
   if (e != cudaSuccess) return cuda_fail(e, "device status read");
   if (*status == 0) *status = g;
   e = read_attn_status(&g);
+  if (e != cudaSuccess) return cuda_fail(e, "device status read");
+  if (*status == 0) *status = g;
+  e = read_kv_status(&g);
+  if (e != cudaSuccess) return cuda_fail(e, "device status read");
+  if (*status == 0) *status = g;
+  e = read_tree_status(&g);
   if (e != cudaSuccess) return cuda_fail(e, "device status read");
   if (*status == 0) *status = g;
   e = read_batch_status(&g);

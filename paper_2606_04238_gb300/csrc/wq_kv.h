@@ -1,0 +1,67 @@
+// wq_kv.h -- launchers of the KV-cache operators (wq_kv.cu) and of attention
+// over a tree of drafted tokens (wq_tree.cu).  Arguments have been validated by
+// the C ABI; every launcher returns the launch status.
+#pragma once
+
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+namespace wq {
+
+// Rows k, v [batch][n_src][n_kv][HD] (strides in values: sequence, token, head)
+// into the caches [batch][n_kv][max_len][HD] at start[b] + n, n < counts[b]
+// (null: n), row n taken from token index[b][n] (null: n).
+struct KvAppendArgs {
+  const void *k, *v;
+  long long k_stride[3], v_stride[3];
+  void *kc, *vc;
+  uint32_t *km, *vm;
+  const int *start, *counts, *index;
+  int batch, n_kv, max_len, n_src, n;
+};
+cudaError_t launch_kv_append(const KvAppendArgs &a, int hd, int bits, bool f32, cudaStream_t s);
+
+// Positions start[b] .. start[b] + n - 1 of the caches as rows [batch][n][n_kv][HD],
+// zeros from counts[b] (null: n) on.
+struct KvReadArgs {
+  const void *kc, *vc;
+  const uint32_t *km, *vm;
+  void *k, *v;
+  const int *start, *counts;
+  int batch, n_kv, max_len, n;
+};
+cudaError_t launch_kv_read(const KvReadArgs &a, int hd, int bits, bool f32, cudaStream_t s);
+
+struct QkvRopeArgs {
+  const float *qkv;   // [m][(n_heads + 2 n_kv) HD]
+  const void *x;      // bf16 [m][d] or null
+  const int *positions;
+  const float *table;  // [n_pos][HD / 2][2]
+  void *q, *k, *v;
+  int d, n_heads, n_kv, n_pos, head_norm;
+};
+cudaError_t launch_qkv_rope(const QkvRopeArgs &a, int m, int hd, cudaStream_t s);
+// Reads and clears the status word of the three kernels above.
+cudaError_t read_kv_status(int *status);
+
+struct TreeArgs {
+  const void *q;                // bf16 [batch][T][H][HD]
+  const void *kn, *vn;          // bf16 [batch][T][Hkv][HD]
+  const void *kc, *vc;          // caches
+  const uint32_t *km, *vm;      // scales and zeros of cached rows (8 and 4 bits)
+  const int *lens, *counts;     // [batch]; counts null: T
+  const uint32_t *mask;         // [batch][T][words] or null: each draft sees itself and the earlier ones
+  int batch, T, H, Hkv, max_len, words;
+  float scale;                  // of the scores, times log2(e)
+  float *part;                  // [batch Hkv][rows][S][HD + 2] (S > 1)
+  void *o;                      // bf16 [batch][T][H][HD]
+  int S;
+};
+// Splits of the context a launch takes, and its partial results in floats.
+int tree_splits(int batch, int T, int H, int Hkv, int max_len, int num_sms);
+size_t tree_part_floats(int batch, int T, int H, int Hkv, int hd, int max_len, int num_sms);
+cudaError_t launch_attn_tree(const TreeArgs &a, int hd, int bits, cudaStream_t s);
+cudaError_t read_tree_status(int *status);
+
+}  // namespace wq

@@ -19,6 +19,7 @@ from . import _build
 WQ_PRENORM = 1
 WQ_LAUNCH_CHAIN = 2
 WQ_LAUNCH_STACK = 4
+WQ_HEAD_NORM = 8
 WQ_BF16 = 0
 WQ_F32 = 1
 
@@ -52,6 +53,12 @@ class _MoELayer(ctypes.Structure):
     _fields_ = [("experts", _MLPLayer), ("n_experts", ctypes.c_int32), ("top_k", ctypes.c_int32)]
 
 
+class _KVCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_meta", ctypes.c_void_p),
+                ("v_meta", ctypes.c_void_p), ("batch", ctypes.c_int32), ("n_kv", ctypes.c_int32),
+                ("max_len", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("bits", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -70,6 +77,7 @@ def lib():
         L = ctypes.CDLL(path)
         P, I, S, F, U = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_float, ctypes.c_uint
         QP = ctypes.POINTER(_QWeight)
+        CP, L3 = ctypes.POINTER(_KVCache), ctypes.POINTER(ctypes.c_int64)
         sig = {
             "wq_packed_sizes": (I, [I, I, I, I, ctypes.POINTER(S), ctypes.POINTER(S)]),
             "wq_pack": (I, [P, I, I, I, I, QP, P, P]),
@@ -92,6 +100,14 @@ def lib():
             "wq_attn_decode": (I, [P, P, P, I, I, I, I, I, F, P, P, I, P, P, S, P]),
             "wq_decoder_workspace_bytes": (S, [I, ctypes.POINTER(_DecoderLayer), I]),
             "wq_decoder_layer_forward": (I, [P, I, P, ctypes.POINTER(_DecoderLayer), P, P, I, U, P, P, S, P]),
+            "wq_kv_append": (I, [CP, P, P, I, I, L3, L3, P, P, P, I, P]),
+            "wq_kv_read": (I, [CP, P, P, I, P, P, I, P]),
+            "wq_qkv_rope": (I, [P, P, I, I, P, P, I, I, I, I, U, P, P, P, P]),
+            "wq_attn_tree_workspace_bytes": (S, [I, I, I, I, I, I]),
+            "wq_attn_tree": (I, [P, P, P, I, I, CP, P, P, P, F, P, P, S, P]),
+            "wq_decoder_tree_workspace_bytes": (S, [I, I, ctypes.POINTER(_DecoderLayer), I]),
+            "wq_decoder_tree_forward": (I, [P, I, P, P, ctypes.POINTER(_DecoderLayer), CP, P, I, P, P, U, P, P, P, P,
+                                            S, P]),
             "wq_moe_workspace_bytes": (S, [I, ctypes.POINTER(_MoELayer), U]),
             "wq_moe_forward": (I, [P, I, P, ctypes.POINTER(_MoELayer), U, P, P, P, P, P, P, S, P]),
             "wq_wait_check": (I, [P]),
@@ -485,6 +501,203 @@ def decoder_layer_forward(x, lens, layer: DecoderLayer, k_cache, v_cache, prenor
                                           max_len, WQ_PRENORM if prenorm else 0, _ptr(y), _ptr(ws), ws.numel(),
                                           _stream()))
     return y
+
+
+@dataclass
+class KVCache:
+    """A KV cache [batch, n_kv, max_len, head_dim] of 16 (bf16), 8 or 4 bits (wq_kv_cache)."""
+    k: torch.Tensor                      # bf16, or uint8 [batch, n_kv, max_len, head_dim * bits / 8]
+    v: torch.Tensor
+    k_meta: torch.Tensor | None          # int32 [batch, n_kv, max_len]: scale and zero of a row
+    v_meta: torch.Tensor | None
+    head_dim: int
+    bits: int
+
+    @property
+    def batch(self) -> int:
+        return self.k.shape[0]
+
+    @property
+    def n_kv(self) -> int:
+        return self.k.shape[1]
+
+    @property
+    def max_len(self) -> int:
+        return self.k.shape[2]
+
+    def __post_init__(self):
+        want = torch.bfloat16 if self.bits == 16 else torch.uint8
+        for t in (self.k, self.v):
+            assert t.is_cuda and t.dtype == want and t.is_contiguous() and t.shape == self.k.shape
+            assert t.shape[3] == (self.head_dim if self.bits == 16 else self.head_dim * self.bits // 8)
+        for t in (self.k_meta, self.v_meta) if self.bits != 16 else ():
+            assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and t.shape == self.k.shape[:3]
+
+    def c(self) -> _KVCache:
+        meta = [None if t is None else t.data_ptr() for t in (self.k_meta, self.v_meta)]
+        return _KVCache(self.k.data_ptr(), self.v.data_ptr(), *meta, self.batch, self.n_kv, self.max_len, self.head_dim,
+                        self.bits)
+
+
+def kv_cache(batch: int, n_kv: int, max_len: int, head_dim: int, bits: int = 16, device="cuda") -> KVCache:
+    """An empty (zero) cache; ``bits`` 16 (bf16), 8 or 4."""
+    if bits == 16:
+        k, v = (torch.zeros((batch, n_kv, max_len, head_dim), dtype=torch.bfloat16, device=device) for _ in range(2))
+        return KVCache(k, v, None, None, head_dim, bits)
+    if bits not in (8, 4):
+        raise WQError(-4, f"cache bits {bits} not 16, 8 or 4")
+    k, v = (torch.zeros((batch, n_kv, max_len, head_dim * bits // 8), dtype=torch.uint8, device=device)
+            for _ in range(2))
+    km, vm = (torch.zeros((batch, n_kv, max_len), dtype=torch.int32, device=device) for _ in range(2))
+    return KVCache(k, v, km, vm, head_dim, bits)
+
+
+def _ints(t, shape, name):
+    assert t is None or (t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == shape), \
+        f"{name}: int32 {shape} on the device"
+
+
+def kv_append(cache: KVCache, k, v, start, counts=None, index=None):
+    """wq_kv_append: rows k, v (bf16 or fp32 [batch, T, n_kv, head_dim], any strides of the first
+    three dimensions that are multiples of 16 bytes) quantized into the cache at positions
+    start[b] + i; ``index`` [batch, n] picks the source token of row i, ``counts`` [batch] how many."""
+    b, t, hkv, hd = k.shape
+    assert k.is_cuda and v.is_cuda and k.shape == v.shape and k.dtype == v.dtype and k.dtype in (torch.bfloat16, torch.float32)
+    assert (b, hkv, hd) == (cache.batch, cache.n_kv, cache.head_dim) and k.stride(3) == 1 and v.stride(3) == 1
+    n = t if index is None else index.shape[1]
+    _ints(start, (b,), "start"), _ints(counts, (b,), "counts"), _ints(index, (b, n), "index")
+    cc = cache.c()
+    ks, vs = (ctypes.c_int64 * 3)(*k.stride()[:3]), (ctypes.c_int64 * 3)(*v.stride()[:3])
+    _check(lib().wq_kv_append(ctypes.byref(cc), _ptr(k), _ptr(v), WQ_F32 if k.dtype == torch.float32 else WQ_BF16, t,
+                              ks, vs, _ptr(start), _ptr(counts), _ptr(index), n, _stream()))
+
+
+def kv_read(cache: KVCache, start, n: int, counts=None, dtype=torch.bfloat16, k=None, v=None):
+    """wq_kv_read: (k, v) [batch, n, n_kv, head_dim] of positions start[b] .. start[b] + n - 1 in bf16 or fp32."""
+    assert dtype in (torch.bfloat16, torch.float32)
+    shape = (cache.batch, n, cache.n_kv, cache.head_dim)
+    _ints(start, (cache.batch,), "start"), _ints(counts, (cache.batch,), "counts")
+    if k is None:
+        k = torch.empty(shape, dtype=dtype, device=cache.k.device)
+    if v is None:
+        v = torch.empty(shape, dtype=dtype, device=cache.k.device)
+    assert k.is_cuda and v.is_cuda and k.dtype == dtype and v.dtype == dtype and k.is_contiguous() and v.is_contiguous()
+    assert tuple(k.shape) == shape and tuple(v.shape) == shape
+    cc = cache.c()
+    _check(lib().wq_kv_read(ctypes.byref(cc), _ptr(start), _ptr(counts), n, _ptr(k), _ptr(v),
+                            WQ_F32 if dtype == torch.float32 else WQ_BF16, _stream()))
+    return k, v
+
+
+def rope_table(n_pos: int, head_dim: int, theta: float = 1e6, device="cuda") -> torch.Tensor:
+    """fp32 [n_pos, head_dim / 2, 2]: cosine and sine of position * theta^(-2i / head_dim), from fp64 angles."""
+    f = theta ** (-2.0 * torch.arange(head_dim // 2, dtype=torch.float64, device=device) / head_dim)
+    a = torch.arange(n_pos, dtype=torch.float64, device=device)[:, None] * f
+    return torch.stack([torch.cos(a), torch.sin(a)], -1).to(torch.float32)
+
+
+def qkv_rope(qkv, positions, table, n_heads: int, n_kv: int, x=None, head_norm: bool = True, q=None, k=None, v=None):
+    """wq_qkv_rope: bf16 (q [m, n_heads, hd], k, v [m, n_kv, hd]) from fp32 projections [m, (n_heads + 2 n_kv) hd]."""
+    m, hd = qkv.shape[0], 2 * table.shape[1]
+    assert qkv.is_cuda and qkv.dtype == torch.float32 and qkv.is_contiguous() and qkv.shape[1] == (n_heads + 2 * n_kv) * hd
+    assert table.is_cuda and table.dtype == torch.float32 and table.is_contiguous() and table.shape[2] == 2
+    assert x is None or (x.is_cuda and x.dtype == torch.bfloat16 and x.is_contiguous() and x.shape[0] == m)
+    _ints(positions, (m,), "positions")
+    out = []
+    for t, h in ((q, n_heads), (k, n_kv), (v, n_kv)):
+        if t is None:
+            t = torch.empty((m, h, hd), dtype=torch.bfloat16, device=qkv.device)
+        assert t.is_cuda and t.dtype == torch.bfloat16 and t.is_contiguous() and t.numel() == m * h * hd
+        out.append(t)
+    _check(lib().wq_qkv_rope(_ptr(qkv), _ptr(x), m, 0 if x is None else x.shape[1], _ptr(positions), _ptr(table),
+                             table.shape[0], n_heads, n_kv, hd, WQ_HEAD_NORM if head_norm else 0, _ptr(out[0]),
+                             _ptr(out[1]), _ptr(out[2]), _stream()))
+    return tuple(out)
+
+
+def tree_mask(parents: torch.Tensor) -> torch.Tensor:
+    """The mask of wq_attn_tree for int32 parents [batch, T]: parents[b, i] < i is draft i's parent, -1 the
+    context's last token.  int32 [batch, T, ceil(T / 32)]; draft i sees its ancestors and itself."""
+    b, t = parents.shape
+    up = parents.cpu().tolist()
+    words = (t + 31) // 32
+    out = []
+    for row in up:
+        see = []
+        for i, p in enumerate(row):
+            assert -1 <= p < i, f"draft {i}: parent {p}"
+            see.append((see[p] if p >= 0 else 0) | 1 << i)
+        out.append([[(s >> (32 * w)) & 0xffffffff for w in range(words)] for s in see])
+    m = torch.tensor(out, dtype=torch.int64).view(b, t, words)
+    return torch.where(m >= 2 ** 31, m - 2 ** 32, m).to(torch.int32).to(parents.device)
+
+
+def attn_tree_workspace(batch: int, n_draft: int, n_heads: int, n_kv: int, head_dim: int, max_len: int,
+                        device="cuda") -> torch.Tensor:
+    nb = int(lib().wq_attn_tree_workspace_bytes(batch, n_draft, n_heads, n_kv, head_dim, max_len))
+    if nb == 0:
+        raise WQError(-2, "no attention workspace for these sizes")
+    return torch.empty(nb, dtype=torch.uint8, device=device)
+
+
+def attn_tree(q, k_new, v_new, cache: KVCache, lens, mask=None, counts=None, scale: float | None = None, o=None, ws=None):
+    """wq_attn_tree: attention of drafts q [batch, T, n_heads, hd] over the cache's first lens[b] positions
+    and the drafts k_new, v_new [batch, T, n_kv, hd] that ``mask`` (int32 [batch, T, ceil(T/32)], see
+    tree_mask; None: a chain) lets them see."""
+    b, t, h, hd = q.shape
+    assert (b, hd) == (cache.batch, cache.head_dim)
+    for x, heads in ((q, h), (k_new, cache.n_kv), (v_new, cache.n_kv)):
+        assert x.is_cuda and x.dtype == torch.bfloat16 and x.is_contiguous() and tuple(x.shape) == (b, t, heads, hd)
+    _ints(lens, (b,), "lens"), _ints(counts, (b,), "counts"), _ints(mask, (b, t, (t + 31) // 32), "mask")
+    if o is None:
+        o = torch.empty_like(q)
+    assert o.is_cuda and o.dtype == torch.bfloat16 and o.is_contiguous() and o.shape == q.shape
+    if ws is None:
+        ws = attn_tree_workspace(b, max(t, 1), h, cache.n_kv, hd, cache.max_len, device=q.device)
+    assert ws.is_cuda
+    cc = cache.c()
+    _check(lib().wq_attn_tree(_ptr(q), _ptr(k_new), _ptr(v_new), t, h, ctypes.byref(cc), _ptr(lens), _ptr(counts),
+                              _ptr(mask), hd ** -0.5 if scale is None else float(scale), _ptr(o), _ptr(ws), ws.numel(),
+                              _stream()))
+    return o
+
+
+def decoder_tree_workspace(batch: int, n_draft: int, layer: DecoderLayer, max_len: int, device="cuda") -> torch.Tensor:
+    cl = layer.c()
+    nb = int(lib().wq_decoder_tree_workspace_bytes(batch, n_draft, ctypes.byref(cl), max_len))
+    if nb == 0:
+        raise WQError(-2, "no decoder workspace for these sizes")
+    ws = torch.empty(nb, dtype=torch.uint8, device=device)
+    _check(lib().wq_workspace_init(_ptr(ws), nb, _stream()))
+    return ws
+
+
+def decoder_tree_forward(x, lens, positions, layer: DecoderLayer, cache: KVCache, table, mask=None, counts=None,
+                         prenorm: bool = True, k_new=None, v_new=None, y=None, ws=None, c_layer=None):
+    """wq_decoder_tree_forward: the verify step of a layer for x bf16 [batch, T, d].  Returns
+    (y, k_new, v_new); kv_append(cache, k_new, v_new, lens, counts=.., index=..) then keeps the accepted path."""
+    b, t, d = x.shape
+    assert x.is_cuda and x.dtype == torch.bfloat16 and x.is_contiguous() and b == cache.batch
+    assert table.is_cuda and table.dtype == torch.float32 and table.is_contiguous() and tuple(table.shape[1:]) == (cache.head_dim // 2, 2)
+    _ints(lens, (b,), "lens"), _ints(positions, (b, t), "positions"), _ints(counts, (b,), "counts")
+    _ints(mask, (b, t, (t + 31) // 32), "mask")
+    shape = (b, t, cache.n_kv, cache.head_dim)
+    k_new = torch.empty(shape, dtype=torch.bfloat16, device=x.device) if k_new is None else k_new
+    v_new = torch.empty(shape, dtype=torch.bfloat16, device=x.device) if v_new is None else v_new
+    for u in (k_new, v_new):
+        assert u.is_cuda and u.dtype == torch.bfloat16 and u.is_contiguous() and tuple(u.shape) == shape
+    if y is None:
+        y = torch.empty_like(x)
+    assert y.is_cuda and y.dtype == torch.bfloat16 and y.is_contiguous() and y.shape == x.shape
+    if ws is None:
+        ws = decoder_tree_workspace(b, max(t, 1), layer, cache.max_len, device=x.device)
+    cl = c_layer if c_layer is not None else layer.c()
+    cc = cache.c()
+    _check(lib().wq_decoder_tree_forward(_ptr(x), t, _ptr(lens), _ptr(positions), ctypes.byref(cl), ctypes.byref(cc),
+                                         _ptr(table), table.shape[0], _ptr(counts), _ptr(mask),
+                                         WQ_PRENORM if prenorm else 0, _ptr(k_new), _ptr(v_new), _ptr(y), _ptr(ws),
+                                         ws.numel(), _stream()))
+    return y, k_new, v_new
 
 
 @dataclass
