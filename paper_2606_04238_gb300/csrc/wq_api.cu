@@ -1474,6 +1474,7 @@ wq_status wq_decoder_layer_forward(const void *x, int batch, const int32_t *lens
 namespace {
 
 constexpr int kMaxDrafts = 128;
+constexpr int kTreeMmaRows = 16;  // rows (drafts x query heads of a kv head) of one m16 tile; above, tcgen05
 
 wq_status check_cache(const wq_kv_cache *c) {
   if (!c) return fail(WQ_ERR_ARG, "null wq_kv_cache");
@@ -1526,10 +1527,16 @@ wq_status attn_tree_impl(const void *q, const void *k_new, const void *v_new, in
   a.lens = lens, a.counts = counts, a.mask = mask;
   a.batch = c->batch, a.T = n_draft, a.H = n_heads, a.Hkv = c->n_kv, a.max_len = c->max_len, a.words = (n_draft + 31) / 32;
   a.scale = scale * 1.4426950408889634f;  // scores in units of log 2
-  a.part = static_cast<float *>(ws);
+  a.table = static_cast<int2 *>(ws);
+  a.part = reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + up256(sizeof(int2) * (size_t)c->batch));
   a.o = o;
-  a.S = tree_splits(c->batch, n_draft, n_heads, c->n_kv, c->max_len, sms);
-  cudaError_t e = launch_attn_tree(a, c->head_dim, c->bits, s);
+  cudaError_t e;
+  if (scale != 0.f && n_draft * (n_heads / c->n_kv) > kTreeMmaRows) {
+    e = launch_attn_tree_tc(a, c->head_dim, c->bits, sms, s);
+  } else {
+    a.S = tree_splits(c->batch, n_draft, n_heads, c->n_kv, c->max_len, sms);
+    e = launch_attn_tree(a, c->head_dim, c->bits, s);
+  }
   if (e != cudaSuccess) return cuda_fail(e, "tree attention launch");
   return ok();
 }
@@ -1606,7 +1613,10 @@ wq_status wq_qkv_rope(const float *qkv, const void *x, int m, int d, const int32
 size_t wq_attn_tree_workspace_bytes(int batch, int n_draft, int n_heads, int n_kv, int head_dim, int max_len) {
   const int sms = num_sms();
   if (batch <= 0 || n_draft <= 0 || n_heads <= 0 || n_kv <= 0 || head_dim <= 0 || max_len <= 0 || sms <= 0) return 0;
-  return up256(4 * tree_part_floats(batch, n_draft, n_heads, n_kv, head_dim, max_len, sms));
+  if (n_heads % n_kv != 0) return 0;
+  return up256(sizeof(int2) * (size_t)batch) +
+         up256(4 * std::max(tree_part_floats(batch, n_draft, n_heads, n_kv, head_dim, max_len, sms),
+                            tree_tc_part_floats(batch, n_draft, n_heads, n_kv, head_dim, max_len, sms)));
 }
 
 wq_status wq_attn_tree(const void *q, const void *k_new, const void *v_new, int n_draft, int n_heads,
@@ -1998,6 +2008,9 @@ wq_status wq_device_status(int *status) {
   if (e != cudaSuccess) return cuda_fail(e, "device status read");
   if (*status == 0) *status = g;
   e = read_kv_status(&g);
+  if (e != cudaSuccess) return cuda_fail(e, "device status read");
+  if (*status == 0) *status = g;
+  e = read_tree_tc_status(&g);
   if (e != cudaSuccess) return cuda_fail(e, "device status read");
   if (*status == 0) *status = g;
   e = read_tree_status(&g);

@@ -520,7 +520,7 @@ __global__ void __launch_bounds__(kTreeWarps * 32, 2) attn_tree_kernel(const Tre
     }
     if (a.S == 1) {
       const int t = row / rep, h = g * rep + row % rep;
-      const bool none = M == -INFINITY || t >= cnt;  // sees nothing, or is padding
+      const bool none = (M == -INFINITY && Ls == 0.f) || t >= cnt;  // sees nothing, or is padding
       *reinterpret_cast<uint32_t *>(reinterpret_cast<__nv_bfloat16 *>(a.o) + (((size_t)b * a.T + t) * a.H + h) * HD + e) =
           none ? 0u : pack_bf2(O0 / Ls, O1 / Ls);
     } else {
@@ -617,7 +617,7 @@ __global__ void __launch_bounds__(kCombineWarps * 32) attn_tree_combine_kernel(c
   __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(a.o) + (((size_t)b * a.T + t) * a.H + h) * HD + lane * E;
 #pragma unroll
   for (int e = 0; e < E / 2; ++e)
-    reinterpret_cast<uint32_t *>(dst)[e] = M == -INFINITY || t >= cnt ? 0u : pack_bf2(O[2 * e] / Ls, O[2 * e + 1] / Ls);
+    reinterpret_cast<uint32_t *>(dst)[e] = (M == -INFINITY && Ls == 0.f) || t >= cnt ? 0u : pack_bf2(O[2 * e] / Ls, O[2 * e + 1] / Ls);
 }
 
 int tree_splits(int batch, int T, int H, int Hkv, int max_len, int num_sms) {

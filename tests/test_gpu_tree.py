@@ -5,7 +5,10 @@ Bound, per output element, of what the kernel rounds (bf16 has 8 significant bit
 round to nearest is within 2^-8 of the value): each probability to bf16 (2^-11 over
 a quantized cache, whose drafts are bf16 too), so at most 2^-8 sum_j p_j |v_j|; the
 bf16 store, 2^-8 |o|; fp32 scores and exponents, some 2^-15 of sum_j p_j |v_j|; and
-binary16's smallest steps, 2^-25 of the largest term for each of the n terms.
+binary16's smallest steps: p_j times its row's scale s_j is within 2^-25 of the
+largest such product, and what it multiplies is at most the row's range r_j over s_j,
+so each of the n terms is within 2^-25 max_i p_i r_i (a row's scales differ from
+r / qmax by less than 2, a draft's by less than 4).
 """
 import math
 
@@ -77,7 +80,8 @@ def reference(q, kn, vn, k, v, lens, counts, vis, scale):
             out = torch.einsum("thj,thjd->thd", p, safe.expand(m, rep, n + m, hd)) if not torch.isfinite(vals).all() \
                 else torch.einsum("thj,jd->thd", p, vals)
             mag = torch.einsum("thj,jd->thd", p, vals.abs().nan_to_num(0, 0, 0))
-            big = (p[..., None] * vals.abs().nan_to_num(0, 0, 0)).amax(2) if (n + m) * m * rep * hd < 5e7 else mag
+            span = 2 * vals.abs().nan_to_num(0, 0, 0).amax(-1)  # a row's range, at most
+            big = 4 * (p * span).amax(-1, keepdim=True)
             o[s, :m, hs] = out
             tol[s, :m, hs] = (2.0 ** -8 + 2.0 ** -15) * mag + 2.0 ** -8 * 1.01 * out.abs().nan_to_num(0, 0, 0) + \
                 (n + m) * 2.0 ** -25 * big + 1e-30
@@ -113,7 +117,7 @@ def run(wq, b, t, H, kv, hd, bits, lens, counts=None, vis=None, parents=None, se
     o = wq.attn_tree(q.cuda(), kn.cuda(), vn.cuda(), cache, lens_t.cuda(), mask=dev(mask), counts=dev(counts_t), scale=scale)
     assert wq.device_status() == 0
     ref, tol = reference(q, kn, vn, kr.double().cpu().transpose(1, 2), vr.double().cpu().transpose(1, 2), lens,
-                         counts or [t] * b, vis, scale or hd ** -0.5)
+                         counts or [t] * b, vis, hd ** -0.5 if scale is None else scale)
     return o.cpu().double(), ref, tol
 
 
@@ -288,3 +292,20 @@ def test_small_workspace_is_refused(wq):
         wq.attn_tree(x, n, n, c, torch.zeros(1, dtype=torch.int32, device="cuda"),
                      ws=torch.empty(256, dtype=torch.uint8, device="cuda"))
     assert e.value.status == -7
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("t", [2, 30])
+def test_a_nan_query_gives_nan_rows(wq, bits, t):
+    """Also where every score of a row is NaN; the other rows are as without it."""
+    def spoil(q, kn, vn, k, v):
+        q[0, 1, 0, 3] = math.nan
+    o, ref, tol = run(wq, 1, t, 4, 1, 128, bits, [300], seed=17, spoil=spoil)
+    assert ref[0, 1, 0].isnan().all() and torch.isfinite(ref[0, 0]).all() and torch.isfinite(ref[0, 1, 1]).all()
+    close(o, ref, tol)
+
+
+def test_zero_scale_is_the_mean(wq):
+    close(*run(wq, 1, 24, 4, 1, 64, 8, [100], scale=0.0, seed=18))
+    close(*run(wq, 1, 24, 4, 1, 64, 16, [100], scale=-0.1, seed=19))
+    close(*run(wq, 1, 24, 4, 1, 64, 4, [100], scale=-0.1, seed=20))
