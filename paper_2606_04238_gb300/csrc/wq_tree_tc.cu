@@ -2,19 +2,19 @@
 // tcgen05 tensor cores (sm_103a): the mathematics of wq_tree.cu for calls with
 // more rows (drafts x query heads of a kv head) than one m16 tile.
 //
-// A CTA takes one (b, g), a block of 128 rows and a range of 64-position tiles:
-//   S = Q K^T   128 x 64, Q as the A operand in TMEM (written once), K in shared memory;
+// A CTA takes one (b, g), a block of 128 rows and a range of 128-position tiles:
+//   S = Q K^T   128 x 128 in TMEM, Q and K in shared memory (K-major);
 //   P           binary16 (bf16 cache: bf16) over S's own TMEM columns, rounded from
 //               the fp32 softmax of one thread a row;
-//   O += P V    128 x HD in TMEM, P as the A operand, V [position][HD] in shared
-//               memory as it lies in the cache (MN-major).
-// So of an MMA's operands only K and V are read from shared memory.  Nine warps:
-// 0-3 softmax (thread = row), 4-7 load a tile's codes into registers one tile
-// ahead, convert them (code - z, exact) and store them in the 128-byte swizzled
-// layout, 8 issues the MMAs.  Two CTAs an SM (256 TMEM columns each) fill each
-// other's waits.  A draft tile's rows are brought into binary16 by an exact power
-// of two a row.  The running maximum is raised, and O rescaled in TMEM, only when a
-// row's scores pass it by 2^8: p stays below 2^8.
+//   O += P V    128 x HD in TMEM, P as the A operand from TMEM, V [position][HD] in
+//               shared memory as it lies in the cache (MN-major).
+// Thirteen warps: 0-3 softmax (thread = row), 4-11 load a tile's codes into registers
+// one tile ahead, convert them (code - z, exact) and store them in the 128-byte
+// swizzled layout, 12 issues the MMAs.  Two CTAs an SM (256 TMEM columns and ~100 KB
+// each) fill each other's waits: a tile's products, softmax and products again are
+// one chain.  A draft tile's rows are brought into binary16 by an exact power of two
+// a row.  The running maximum is raised, and O rescaled in TMEM, only when a row's
+// scores pass it by 2^8: p stays below 2^8.
 //
 // The tiles of all (b, g, row block) are dealt to the CTAs in nearly equal
 // ranges: every CTA finds the tiles a range takes from the lengths themselves.
@@ -39,11 +39,15 @@ __device__ int g_tree_tc_status = 0;
 namespace {
 
 constexpr int kTcRows = 128;      // rows a CTA takes
-constexpr int kTile = 64;         // positions a tile
-constexpr int kTcThreads = 288;
-constexpr int kBlk = kTile * 128;  // bytes of a 64-value block of K or V: [position][128 bytes], swizzled
+constexpr int kTile = 128;        // positions a tile
+constexpr int kConv = 256;        // converting threads
+constexpr int kTcThreads = 128 + kConv + 32;
+constexpr int kMmaWarp = 4 + kConv / 32;
+constexpr int kBlk = kTile * 128;  // bytes of a 64-value block of Q, K or V: [row][128 bytes], swizzled
 constexpr float kRaise = 8.f;
-constexpr int kTmemCols = 256;    // S / P 0..63, Q 64.., O 128..
+constexpr int kTmemCols = 256;    // S / P 0..127, O 128..
+// registers a thread: the launch's 72 x 416 shared out as 88 x 128 + 64 x 256 + 72 x 32
+constexpr int kRegsSoftmax = 88, kRegsConv = 64;
 
 __device__ __forceinline__ float bf_lo(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
@@ -97,6 +101,13 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&v)[32
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(
           taddr),
       "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
+      "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
       : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -219,26 +230,26 @@ __device__ Work find_work(const TreeArgs &a, int rep, int cta) {
 
 template <int HD, int BITS>
 struct Cfg {
-  static constexpr int ST = BITS == 16 ? 3 : 2;  // stages of K and V
   static constexpr int NB = HD / 64;             // 64-value blocks
   static constexpr int KB = NB * kBlk;           // bytes of one operand tile
   static constexpr int CH = HD / 8;              // 16-byte chunks a row of 16-bit values
-  static constexpr int IT = kTile * CH / 128;    // chunks a converting thread takes
-  static constexpr int RS = 128 / CH;            // rows between them
-  static constexpr int SMEM = 1024 + ST * 2 * KB;
+  static constexpr int IT = kTile * CH / kConv;  // chunks a converting thread takes
+  static constexpr int RS = kConv / CH;          // rows between them
+  static constexpr int SMEM = 1024 + 3 * KB;     // Q, K, V
 };
 
 struct Shared {
-  uint64_t k_full[3], k_empty[3], v_full[3], v_empty[3], s_full, p_full;
+  uint64_t k_full, k_empty, v_full, v_empty, s_full, p_full;
   uint32_t tmem;
   int fail;
   uint32_t odd[4];  // drafts whose V has values that are not finite
   Work work;
-  // per stage: K's scale (times the score scale), log2 of V's scale, its reciprocal; 1024 + z twice
-  __align__(16) float sk[3][kTile];
-  __align__(16) float lg[3][kTile];
-  __align__(16) float rs[3][kTile];
-  uint32_t zk[3][kTile], zv[3][kTile];
+  // K's scale (times the score scale), log2 of V's scale, its reciprocal; 1024 + z twice.  Two tiles
+  // of each: the next tile's are written while this one's are read
+  __align__(16) float sk[2][kTile];
+  __align__(16) float lg[2][kTile];
+  __align__(16) float rs[2][kTile];
+  uint32_t zk[kTile], zv[kTile];
 };
 
 // 8 codes as 8 binary16 values code - z; z1024: 1024 + z in both halves.
@@ -271,9 +282,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
   constexpr int ROW = HD * BITS / 8;
   extern __shared__ uint8_t tree_dyn[];
   __shared__ Shared sh;
-  uint8_t *buf = tree_dyn + (1024 - (smem_addr(tree_dyn) & 1023)) % 1024;
-  auto kbuf = [&](int st) { return buf + st * 2 * C::KB; };
-  auto vbuf = [&](int st) { return buf + st * 2 * C::KB + C::KB; };
+  uint8_t *qbuf = tree_dyn + (1024 - (smem_addr(tree_dyn) & 1023)) % 1024, *kbuf = qbuf + C::KB, *vbuf = kbuf + C::KB;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rep = a.H / a.Hkv;
   pdl_wait();
@@ -281,17 +290,15 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
   if (warp == 0) {
     const Work w = find_work(a, rep, blockIdx.x);
     if (lane == 0) sh.work = w;
-  } else if (warp == 8) {
+  } else if (warp == kMmaWarp) {
     tmem_alloc(&sh.tmem, kTmemCols);
     if (lane == 0) {
-      for (int i = 0; i < C::ST; ++i) {
-        mbar_init(&sh.k_full[i], 128);
-        mbar_init(&sh.v_full[i], 128);
-        mbar_init(&sh.k_empty[i], 1);
-        mbar_init(&sh.v_empty[i], 1);
-      }
+      mbar_init(&sh.k_full, kConv / 32);
+      mbar_init(&sh.v_full, kConv / 32);
+      mbar_init(&sh.k_empty, 1);
+      mbar_init(&sh.v_empty, 1);
       mbar_init(&sh.s_full, 1);
-      mbar_init(&sh.p_full, 128);
+      mbar_init(&sh.p_full, 4);
       fence_barrier_init();
       sh.fail = 0;
     }
@@ -306,59 +313,64 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
   const int row0 = w.any ? w.rb * kTcRows : 0;
   const int R = a.T * rep, live = w.any ? min(w.cnt * rep - row0, kTcRows) : 0;  // rows of drafts that exist
   const int nt = live > 0 ? w.t1 - w.t0 : 0;
-  const int ndr = w.any ? (w.cnt + kTile - 1) / kTile : 0;
+  const int ndr = w.any && w.cnt > 0 ? 1 : 0;  // the drafts are one tile
+  // a warp's arrival, its shared-memory writes made visible to the tensor cores
+  auto hand_over = [&](uint64_t *bar) {
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar);
+  };
+  // all lanes alike: a warp leaves its loop as one after a timeout
+  auto wait = [&](uint64_t *bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity)) != 0; };
 
-  if (nt > 0 && warp == 8) {
+  if (nt > 0 && warp == kMmaWarp) {
     // ---- MMAs
     constexpr uint32_t idqk = tree_idesc(kTile, BF, false), idpv = tree_idesc(HD, BF, true);
-    bool ok = __all_sync(0xffffffffu, mbar_wait(&sh.p_full, 0));  // Q is in TMEM
-    tc_fence_after();
+    const uint64_t qd = umma_desc_kmajor_sw128(smem_addr(qbuf), 1024), kd = umma_desc_kmajor_sw128(smem_addr(kbuf), 1024);
+    const uint64_t vd = umma_desc_mnmajor_sw128(smem_addr(vbuf), kBlk);
+    bool ok = wait(&sh.p_full, 0);  // Q is in place
     for (int i = 0; i < nt && ok; ++i) {
-      const int st = i % C::ST;
-      ok = mbar_wait(&sh.k_full[st], (i / C::ST) & 1);
+      ok = wait(&sh.k_full, i & 1);
       // P V of the tile before has read P, which S overwrites
-      if (ok && i > 0) ok = mbar_wait(&sh.v_empty[(i - 1) % C::ST], ((i - 1) / C::ST) & 1);
-      ok = __all_sync(0xffffffffu, ok);
+      if (ok && i > 0) ok = wait(&sh.v_empty, (i - 1) & 1);
       if (!ok) break;
       tc_fence_after();
       if (elect_one()) {
-        const uint64_t kd = umma_desc_kmajor_sw128(smem_addr(kbuf(st)), 1024);
 #pragma unroll
-        for (int ks = 0; ks < HD / 16; ++ks)
-          umma_ts(tm, tm + 64 + 8 * ks, kd + (uint64_t)(((ks / 4) * kBlk + (ks % 4) * 32) >> 4), idqk, ks > 0);
+        for (int ks = 0; ks < HD / 16; ++ks) {
+          const uint64_t off = (uint64_t)(((ks / 4) * kBlk + (ks % 4) * 32) >> 4);
+          umma_f16(tm, qd + off, kd + off, idqk, ks > 0);
+        }
         umma_commit(&sh.s_full);
-        umma_commit(&sh.k_empty[st]);
+        umma_commit(&sh.k_empty);
       }
       __syncwarp();
-      ok = __all_sync(0xffffffffu, mbar_wait(&sh.p_full, (i + 1) & 1) && mbar_wait(&sh.v_full[st], (i / C::ST) & 1));
+      ok = wait(&sh.p_full, (i + 1) & 1) && wait(&sh.v_full, i & 1);
       if (!ok) break;
       tc_fence_after();
       if (elect_one()) {
-        const uint64_t vd = umma_desc_mnmajor_sw128(smem_addr(vbuf(st)), kBlk);
 #pragma unroll
         for (int ks = 0; ks < kTile / 16; ++ks)
           umma_ts(tm + 128, tm + 8 * ks, vd + (uint64_t)((ks * 2048) >> 4), idpv, i > 0 || ks > 0);
-        umma_commit(&sh.v_empty[st]);
+        umma_commit(&sh.v_empty);
       }
       __syncwarp();
     }
     if (!ok && lane == 0) sh.fail = 1;
   } else if (nt > 0 && warp >= 4) {
     // ---- loads and conversion: chunk c of rows r0 + it RS
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsConv));
     const int ct = tid - 128, c = ct % C::CH, r0 = ct / C::CH;
     const uint32_t dst0 = (c / 8) * kBlk + r0 * 128 + (((c & 7) ^ (r0 & 7)) << 4);
     const size_t base = ((size_t)w.b * a.Hkv + w.g) * a.max_len;
-    const uint8_t *kc = reinterpret_cast<const uint8_t *>(a.kc) + base * ROW;
-    const uint8_t *vc = reinterpret_cast<const uint8_t *>(a.vc) + base * ROW;
-    const size_t dstride = (size_t)a.Hkv * HD;
-    const __nv_bfloat16 *kd = reinterpret_cast<const __nv_bfloat16 *>(a.kn) + ((size_t)w.b * a.T * a.Hkv + w.g) * HD;
-    const __nv_bfloat16 *vd = reinterpret_cast<const __nv_bfloat16 *>(a.vn) + ((size_t)w.b * a.T * a.Hkv + w.g) * HD;
+    const uint8_t *kc = reinterpret_cast<const uint8_t *>(a.kc) + base * ROW + c * BITS;
+    const uint8_t *vc = reinterpret_cast<const uint8_t *>(a.vc) + base * ROW + c * BITS;
     uint2 kr[C::IT], vr[C::IT];
     uint32_t meta = 0;
     auto fetch = [&](const uint8_t *src, uint2 (&r)[C::IT], int p0) {
 #pragma unroll
       for (int it = 0; it < C::IT; ++it) {
-        const uint8_t *p = src + (size_t)min(p0 + r0 + it * C::RS, w.len - 1) * ROW + c * BITS;
+        const uint8_t *p = src + (size_t)(uint32_t)min(p0 + r0 + it * C::RS, w.len - 1) * ROW;
         if (BITS == 8)
           r[it] = __ldg(reinterpret_cast<const uint2 *>(p));
         else if (BITS == 4)
@@ -366,21 +378,25 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
       }
     };
     auto fetch_meta = [&](int p0) {
-      if (!BF) meta = __ldg((ct < 64 ? a.km : a.vm) + base + min(p0 + (ct & 63), w.len - 1));
+      if (!BF) meta = __ldg((ct < kTile ? a.km : a.vm) + base + min(p0 + (ct & (kTile - 1)), w.len - 1));
     };
     // copies of a bf16 tile, straight to its place; zeros past the length
     auto copy = [&](const uint8_t *src, uint8_t *to, int p0) {
 #pragma unroll
       for (int it = 0; it < C::IT; ++it) {
         const int p = p0 + r0 + it * C::RS;
-        cp_async16_zfill(to + dst0 + it * C::RS * 128, src + (size_t)min(p, w.len - 1) * ROW + c * 16, p < w.len ? 16u : 0u);
+        cp_async16_zfill(to + dst0 + it * C::RS * 128, src + (size_t)(uint32_t)min(p, w.len - 1) * ROW,
+                         p < w.len ? 16u : 0u);
       }
+      cp_async_commit();
     };
-    // a draft tile's K or V: in binary16 by a power of two a row, or as it is
-    auto draft = [&](const __nv_bfloat16 *src, uint8_t *to, int st, int j0, bool is_v) {
+    // the drafts' K or V: in binary16 by a power of two a row, or as it is
+    auto draft = [&](const void *rows, uint8_t *to, bool is_v) {
+      const __nv_bfloat16 *src = reinterpret_cast<const __nv_bfloat16 *>(rows) + ((size_t)w.b * a.T * a.Hkv + w.g) * HD + c * 8;
+#pragma unroll 1
       for (int it = 0; it < C::IT; ++it) {
-        const int r = r0 + it * C::RS, j = j0 + r;
-        uint4 v = j < w.cnt ? __ldg(reinterpret_cast<const uint4 *>(src + (size_t)j * dstride + c * 8)) : make_uint4(0, 0, 0, 0);
+        const int j = r0 + it * C::RS;
+        const uint4 v = j < w.cnt ? __ldg(reinterpret_cast<const uint4 *>(src + (size_t)j * a.Hkv * HD)) : make_uint4(0, 0, 0, 0);
         uint32_t x[4] = {v.x, v.y, v.z, v.w};
         if (is_v) {
           bool odd = false;
@@ -404,10 +420,10 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
           for (int e = 0; e < 4; ++e) x[e] = pack_h2(bf_lo(x[e]) * f, bf_hi(x[e]) * f);
           if (c == 0) {
             if (is_v) {
-              sh.lg[st][r] = (float)-e2;
-              sh.rs[st][r] = f;
+              sh.lg[0][j] = (float)-e2;
+              sh.rs[0][j] = f;
             } else {
-              sh.sk[st][r] = a.scale * pow2i(-e2);
+              sh.sk[0][j] = a.scale * pow2i(-e2);
             }
           }
         }
@@ -416,257 +432,248 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
     };
     auto pos_of = [&](int i) { return (w.t0 + i - ndr) * kTile; };
     const int i_ctx = max(0, ndr - w.t0);  // first tile of the context
-    if (!BF && i_ctx < nt) {
+    bool ok = true;
+    if (i_ctx < nt && !BF) {
       fetch_meta(pos_of(i_ctx));
       fetch(kc, kr, pos_of(i_ctx));
       fetch(vc, vr, pos_of(i_ctx));
     }
-    bool ok = true;
-    // stage of tile i, once the products of tile i - ST are done (all lanes alike)
-    auto stage_free = [&](int i) {
-      if (i < C::ST) return true;
-      const uint32_t par = ((i / C::ST) & 1) ^ 1;
-      const bool f = mbar_wait(&sh.k_empty[i % C::ST], par) && mbar_wait(&sh.v_empty[i % C::ST], par);
-      return __all_sync(0xffffffffu, f) != 0;
-    };
-    auto copy_tile = [&](int i) {
-      copy(kc, kbuf(i % C::ST), pos_of(i));
-      copy(vc, vbuf(i % C::ST), pos_of(i));
-      cp_async_commit();
-    };
-    for (int i = 0; i < nt; ++i) {
-      const int st = i % C::ST;
-      if (i < i_ctx) {
-        ok = stage_free(i);
+    if (i_ctx > 0) {
+      draft(a.kn, kbuf, false);
+      draft(a.vn, vbuf, true);
+      hand_over(&sh.k_full);
+      hand_over(&sh.v_full);
+    }
+    for (int i = i_ctx; i < nt; ++i) {
+      const int p0 = pos_of(i);
+      if constexpr (BF) {
+        // K's place is free once the scores of tile i - 1 are done, V's once its outputs are
+        if (i > 0) ok = wait(&sh.k_empty, (i - 1) & 1);
         if (!ok) break;
-        draft(kd, kbuf(st), st, (w.t0 + i) * kTile, false);
-        draft(vd, vbuf(st), st, (w.t0 + i) * kTile, true);
-        fence_proxy_async_smem();
-        mbar_arrive(&sh.k_full[st]);
-        mbar_arrive(&sh.v_full[st]);
-      } else if constexpr (BF) {
-        // copies run two tiles ahead: that of tile i + 2 waits for the products of tile i - 1,
-        // after tile i has been handed over
-        if (i == i_ctx)
-          for (int j = i; j < min(nt, i + 2) && ok; ++j) {
-            ok = stage_free(j);
-            if (ok) copy_tile(j);
-          }
-        if (!ok) break;
-        if (i + 1 < nt)
+        copy(kc, kbuf, p0);
+        if (i > i_ctx) {  // V of tile i - 1 has landed meanwhile
           cp_async_wait_group1();
-        else
-          cp_async_wait_all();
-        fence_proxy_async_smem();
-        mbar_arrive(&sh.k_full[st]);
-        mbar_arrive(&sh.v_full[st]);
-        if (i + 2 < nt) {
-          ok = stage_free(i + 2);
-          if (!ok) break;
-          copy_tile(i + 2);
+          hand_over(&sh.v_full);
         }
+        cp_async_wait_all();
+        hand_over(&sh.k_full);
+        if (i > 0) ok = wait(&sh.v_empty, (i - 1) & 1);
+        if (!ok) break;
+        copy(vc, vbuf, p0);
       } else {
-        ok = stage_free(i);
-        const int p0 = pos_of(i), pn = i + 1 < nt ? p0 + kTile : p0;
-        if (ok) {
+        const int par = i & 1, pn = i + 1 < nt ? p0 + kTile : p0;
+        if (i > 0) ok = wait(&sh.k_empty, (i - 1) & 1);
+        {
           const float s0 = __half2float(__ushort_as_half((unsigned short)(meta & 0xffffu)));
           const __half2 z = __hadd2(__half2half2(__ushort_as_half((unsigned short)(meta >> 16))), __float2half2_rn(1024.f));
           const uint32_t zz = *reinterpret_cast<const uint32_t *>(&z);
-          const int r = ct & 63;
-          if (ct < 64) {
-            sh.sk[st][r] = s0 * a.scale;
-            sh.zk[st][r] = zz;
+          const int r = ct & (kTile - 1);
+          if (ct < kTile) {
+            sh.sk[par][r] = s0 * a.scale;
+            sh.zk[r] = zz;
           } else {
             const float sv = s0 == 0.f ? 1.f : s0;  // a zero-filled cache's row: code - z is 0
             const bool in = p0 + r < w.len;
-            sh.lg[st][r] = in ? __log2f(sv) : -INFINITY;
-            sh.rs[st][r] = in ? __frcp_rn(sv) : 0.f;
-            sh.zv[st][r] = zz;
+            sh.lg[par][r] = in ? __log2f(sv) : -INFINITY;
+            sh.rs[par][r] = in ? __frcp_rn(sv) : 0.f;
+            sh.zv[r] = zz;
           }
         }
-        ok = barrier_and(1, 128, ok);  // the four warps leave together after a timeout
+        ok = barrier_and(1, kConv, ok);  // the warps leave together after a timeout
         if (!ok) break;
         fetch_meta(pn);
 #pragma unroll
         for (int it = 0; it < C::IT; ++it)
-          *reinterpret_cast<uint4 *>(kbuf(st) + dst0 + it * C::RS * 128) = convert8<BITS>(kr[it], sh.zk[st][r0 + it * C::RS]);
+          *reinterpret_cast<uint4 *>(kbuf + dst0 + it * C::RS * 128) = convert8<BITS>(kr[it], sh.zk[r0 + it * C::RS]);
+        hand_over(&sh.k_full);
         fetch(kc, kr, pn);
-        fence_proxy_async_smem();
-        mbar_arrive(&sh.k_full[st]);
+        if (i > 0) ok = wait(&sh.v_empty, (i - 1) & 1);
 #pragma unroll
         for (int it = 0; it < C::IT; ++it)
-          *reinterpret_cast<uint4 *>(vbuf(st) + dst0 + it * C::RS * 128) = convert8<BITS>(vr[it], sh.zv[st][r0 + it * C::RS]);
+          *reinterpret_cast<uint4 *>(vbuf + dst0 + it * C::RS * 128) = convert8<BITS>(vr[it], sh.zv[r0 + it * C::RS]);
+        hand_over(&sh.v_full);
         fetch(vc, vr, pn);
-        fence_proxy_async_smem();
-        mbar_arrive(&sh.v_full[st]);
+        // every warp has read this tile's zeros before the next one's are written
+        ok = barrier_and(1, kConv, ok);
+        if (!ok) break;
       }
     }
-    if constexpr (BF) cp_async_wait_all();
-    if (!ok) sh.fail = 1;
-  } else if (nt > 0 && warp < 4) {
+    if constexpr (BF) {
+      cp_async_wait_all();
+      if (ok && i_ctx < nt) hand_over(&sh.v_full);  // the last tile's V
+    }
+    if (!ok && lane == 0) sh.fail = 1;
+  } else if (nt > 0) {
     // ---- softmax: thread = row
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
     const int r = row0 + tid, t = r / rep;
     const bool in = tid < live;
     const bool busy = warp * 32 < live;  // warps without rows only keep the barriers going
     const uint32_t tw = tm + ((uint32_t)(warp * 32) << 16);
     float c1 = a.scale;  // of the raw products: bf16 the score scale (its sign in Q), else 2^-e of the row
     if (busy) {
-      const __nv_bfloat16 *q = reinterpret_cast<const __nv_bfloat16 *>(a.q) +
-                               (((size_t)w.b * a.T + (in ? t : 0)) * a.H + w.g * rep + (in ? r % rep : 0)) * HD;
-      uint32_t x[HD / 2];
-#pragma unroll
-      for (int i = 0; i < HD / 8; ++i) {
-        const uint4 v = in ? __ldg(reinterpret_cast<const uint4 *>(q) + i) : make_uint4(0, 0, 0, 0);
-        x[4 * i] = v.x, x[4 * i + 1] = v.y, x[4 * i + 2] = v.z, x[4 * i + 3] = v.w;
-      }
+      const uint4 *q = reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(a.q) +
+                                                       (((size_t)w.b * a.T + (in ? t : 0)) * a.H + w.g * rep + (in ? r % rep : 0)) * HD);
+      float f = 1.f;
       if constexpr (BF) {
-        if (a.scale < 0.f)
-#pragma unroll
-          for (int i = 0; i < HD / 2; ++i) x[i] ^= 0x80008000u;
         c1 = fabsf(a.scale);
       } else {
         float mx = 0.f;
-#pragma unroll
-        for (int i = 0; i < HD / 2; ++i) mx = fmaxf(mx, fmaxf(fabsf(bf_lo(x[i])), fabsf(bf_hi(x[i]))));
+#pragma unroll 4
+        for (int i = 0; i < HD / 8; ++i) {
+          const uint4 v = in ? __ldg(q + i) : make_uint4(0, 0, 0, 0);
+          mx = fmaxf(mx, fmaxf(fmaxf(fmaxf(fabsf(bf_lo(v.x)), fabsf(bf_hi(v.x))), fmaxf(fabsf(bf_lo(v.y)), fabsf(bf_hi(v.y)))),
+                               fmaxf(fmaxf(fabsf(bf_lo(v.z)), fabsf(bf_hi(v.z))), fmaxf(fabsf(bf_lo(v.w)), fabsf(bf_hi(v.w))))));
+        }
         const int e = f16_shift(mx, 14);
-        const float f = pow2i(e);
+        f = pow2i(e);
         c1 = pow2i(-e);
-#pragma unroll
-        for (int i = 0; i < HD / 2; ++i) x[i] = pack_h2(bf_lo(x[i]) * f, bf_hi(x[i]) * f);
       }
+#pragma unroll 4
+      for (int i = 0; i < HD / 8; ++i) {
+        const uint4 v = in ? __ldg(q + i) : make_uint4(0, 0, 0, 0);
+        uint32_t x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int h = 0; h < HD / 64; ++h) tmem_st32(tw + 64 + 32 * h, *reinterpret_cast<uint32_t(*)[32]>(&x[32 * h]));
-      tmem_st_wait();
+        for (int e = 0; e < 4; ++e) {
+          if (BF)
+            x[e] ^= a.scale < 0.f ? 0x80008000u : 0u;
+          else
+            x[e] = pack_h2(bf_lo(x[e]) * f, bf_hi(x[e]) * f);
+        }
+        *reinterpret_cast<uint4 *>(qbuf + (i / 8) * kBlk + tid * 128 + (((i & 7) ^ (tid & 7)) << 4)) =
+            make_uint4(x[0], x[1], x[2], x[3]);
+      }
     }
-    tc_fence_before();
-    mbar_arrive(&sh.p_full);  // phase 0: Q
+    hand_over(&sh.p_full);  // phase 0: Q
     float m = -INFINITY, l = 0.f;
     bool ok = true;
-    for (int i = 0; i < nt && ok; ++i) {
-      const int st = i % C::ST;
-      ok = __all_sync(0xffffffffu, mbar_wait(&sh.k_full[st], (i / C::ST) & 1) && mbar_wait(&sh.s_full, i & 1));
+    for (int i = 0; i < nt; ++i) {
+      const int par = i & 1, tile = w.t0 + i;
+      // (the scales were written before K was handed to the MMA warp, which issued S after that)
+      ok = wait(&sh.s_full, i & 1);
       if (!ok) break;
       tc_fence_after();
       if (busy) {
-        const int tile = w.t0 + i;
-        uint32_t s[64];
-        tmem_ld32(tw, *reinterpret_cast<uint32_t(*)[32]>(&s[0]));
-        tmem_ld32(tw + 32, *reinterpret_cast<uint32_t(*)[32]>(&s[32]));
-        tmem_ld_wait();
-        float *y = reinterpret_cast<float *>(s);
-        if constexpr (!BF) {
-          const uint64_t cc = pack_f32x2(c1, c1);
+        // which of the tile's positions count: the drafts the row sees, those before the length
+        const bool some = tile < ndr || w.len - (tile - ndr) * kTile < kTile;
+        uint32_t see[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
+        if (some)
 #pragma unroll
-          for (int j = 0; j < 64; j += 4) {
-            const float4 k4 = *reinterpret_cast<const float4 *>(&sh.sk[st][j]);
-            const float4 g4 = *reinterpret_cast<const float4 *>(&sh.lg[st][j]);
-            uint64_t u = fma_f32x2(mul_f32x2(pack_f32x2(y[j], y[j + 1]), cc), pack_f32x2(k4.x, k4.y), pack_f32x2(g4.x, g4.y));
-            unpack_f32x2(u, y[j], y[j + 1]);
-            u = fma_f32x2(mul_f32x2(pack_f32x2(y[j + 2], y[j + 3]), cc), pack_f32x2(k4.z, k4.w), pack_f32x2(g4.z, g4.w));
-            unpack_f32x2(u, y[j + 2], y[j + 3]);
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < 64; ++j) y[j] *= c1;
-        }
-        if (tile < ndr) {
-          // the drafts that the row sees
-          uint32_t see[2] = {0, 0};
-          if (in)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const int j0 = tile * kTile + 32 * h, n = w.cnt - j0;
-              if (n <= 0) continue;
-              const uint32_t have = n >= 32 ? 0xffffffffu : (1u << n) - 1u;
-              if (a.mask)
-                see[h] = a.mask[((size_t)w.b * a.T + t) * a.words + j0 / 32] & have;
+          for (int h = 0; h < 4; ++h) {
+            const int n = (tile < ndr ? w.cnt : w.len - (tile - ndr) * kTile) - 32 * h;
+            uint32_t have = n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u;
+            if (tile < ndr) {
+              if (!in || n <= 0)
+                have = 0;
+              else if (a.mask)
+                have &= a.mask[((size_t)w.b * a.T + t) * a.words + h];
               else
-                see[h] = t >= j0 + 31 ? have : t < j0 ? 0u : ((2u << (t - j0)) - 1u) & have;
+                have &= t >= 32 * h + 31 ? 0xffffffffu : t < 32 * h ? 0u : (2u << (t - 32 * h)) - 1u;
             }
-#pragma unroll
-          for (int j = 0; j < 64; ++j) y[j] = see[j / 32] >> (j % 32) & 1 ? y[j] : -INFINITY;
-        } else if (BF) {
-          const int n = w.len - (tile - ndr) * kTile;
-          if (n < kTile)
-#pragma unroll
-            for (int j = 0; j < 64; ++j) y[j] = j < n ? y[j] : -INFINITY;
-        } else if (w.len - (tile - ndr) * kTile < kTile) {
-          // lg is -inf there; a score that is NaN or +inf (a row repeated for the load) must not stand
-          const int n = w.len - (tile - ndr) * kTile;
-#pragma unroll
-          for (int j = 0; j < 64; ++j) y[j] = j < n ? y[j] : -INFINITY;
-        }
+            see[h] = have;
+          }
+        // 1. scores (over the raw products where they differ) and their maximum
         float mx = -INFINITY;
+        const uint64_t cc = pack_f32x2(c1, c1);
 #pragma unroll
-        for (int j = 0; j < 64; j += 2) mx = fmaxf(mx, fmaxf(y[j], y[j + 1]));
+        for (int h = 0; h < 4; ++h) {
+          uint32_t s[32];
+          tmem_ld32(tw + 32 * h, s);
+          tmem_ld_wait();
+          float *y = reinterpret_cast<float *>(s);
+          if constexpr (!BF) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {
+              const float4 k4 = *reinterpret_cast<const float4 *>(&sh.sk[par][32 * h + j]);
+              const float4 g4 = *reinterpret_cast<const float4 *>(&sh.lg[par][32 * h + j]);
+              uint64_t u = fma_f32x2(mul_f32x2(pack_f32x2(y[j], y[j + 1]), cc), pack_f32x2(k4.x, k4.y), pack_f32x2(g4.x, g4.y));
+              unpack_f32x2(u, y[j], y[j + 1]);
+              u = fma_f32x2(mul_f32x2(pack_f32x2(y[j + 2], y[j + 3]), cc), pack_f32x2(k4.z, k4.w), pack_f32x2(g4.z, g4.w));
+              unpack_f32x2(u, y[j + 2], y[j + 3]);
+            }
+          }
+          if (some)
+#pragma unroll
+            for (int j = 0; j < 32; ++j) y[j] = see[h] >> j & 1 ? y[j] : -INFINITY;
+#pragma unroll
+          for (int j = 0; j < 32; j += 2) mx = fmaxf(mx, fmaxf(y[j], y[j + 1]));
+          if (!BF || some) tmem_st32(tw + 32 * h, s);
+        }
+        if (BF) mx = mx == -INFINITY ? mx : mx * c1;
         if (__any_sync(0xffffffffu, mx > m + kRaise)) {
           const float mn = fmaxf(m, mx), al = mn == -INFINITY ? 1.f : ex2(m - mn);
           l *= al;
           m = mn;
-          if (i > 0) {  // P V of the tiles before is complete (S was issued after it)
-            for (int h = 0; h < HD / 16; ++h) {
-              uint32_t o[16];
-              tmem_ld16(tw + 128 + 16 * h, o);
+          if (i > 0)  // P V of the tiles before is complete (S was issued after it)
+#pragma unroll 1
+            for (int h = 0; h < HD / 32; ++h) {
+              uint32_t o[32];
+              tmem_ld32(tw + 128 + 32 * h, o);
               tmem_ld_wait();
 #pragma unroll
-              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * al);
-              asm volatile(
-                  "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(
-                      tw + 128 + 16 * h),
-                  "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]), "r"(o[8]),
-                  "r"(o[9]), "r"(o[10]), "r"(o[11]), "r"(o[12]), "r"(o[13]), "r"(o[14]), "r"(o[15])
-                  : "memory");
+              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * al);
+              tmem_st32(tw + 128 + 32 * h, o);
             }
-          }
         }
+        tmem_st_wait();
+        // 2. probabilities
         const float ms = m == -INFINITY ? 0.f : m;
-        uint32_t p[32];
         uint64_t sum = 0;
-        const uint64_t mm = pack_f32x2(-ms, -ms), one = pack_f32x2(1.f, 1.f);
+        const uint64_t mm = pack_f32x2(-ms, -ms), by = BF ? cc : pack_f32x2(1.f, 1.f);
 #pragma unroll
-        for (int j = 0; j < 64; j += 4) {
-          float4 r4 = make_float4(1.f, 1.f, 1.f, 1.f);
-          if (!BF) r4 = *reinterpret_cast<const float4 *>(&sh.rs[st][j]);
-          float e[4];
-          uint64_t u = fma_f32x2(pack_f32x2(y[j], y[j + 1]), one, mm);
-          unpack_f32x2(u, e[0], e[1]);
-          u = fma_f32x2(pack_f32x2(y[j + 2], y[j + 3]), one, mm);
-          unpack_f32x2(u, e[2], e[3]);
+        for (int h = 0; h < 4; ++h) {
+          uint32_t s[32], p[16];
+          tmem_ld32(tw + 32 * h, s);
+          tmem_ld_wait();
+          const float *y = reinterpret_cast<const float *>(s);
 #pragma unroll
-          for (int h = 0; h < 4; ++h) e[h] = ex2(e[h]);
-          sum = fma_f32x2(pack_f32x2(e[0], e[1]), pack_f32x2(r4.x, r4.y), sum);
-          sum = fma_f32x2(pack_f32x2(e[2], e[3]), pack_f32x2(r4.z, r4.w), sum);
-          p[j / 2] = BF ? pack_bf2(e[0], e[1]) : pack_h2(e[0], e[1]);
-          p[j / 2 + 1] = BF ? pack_bf2(e[2], e[3]) : pack_h2(e[2], e[3]);
+          for (int j = 0; j < 32; j += 4) {
+            float4 r4 = make_float4(1.f, 1.f, 1.f, 1.f);
+            if (!BF) r4 = *reinterpret_cast<const float4 *>(&sh.rs[par][32 * h + j]);
+            float e[4];
+            uint64_t u = fma_f32x2(pack_f32x2(y[j], y[j + 1]), by, mm);
+            unpack_f32x2(u, e[0], e[1]);
+            u = fma_f32x2(pack_f32x2(y[j + 2], y[j + 3]), by, mm);
+            unpack_f32x2(u, e[2], e[3]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) e[k] = ex2(e[k]);
+            sum = fma_f32x2(pack_f32x2(e[0], e[1]), pack_f32x2(r4.x, r4.y), sum);
+            sum = fma_f32x2(pack_f32x2(e[2], e[3]), pack_f32x2(r4.z, r4.w), sum);
+            p[j / 2] = BF ? pack_bf2(e[0], e[1]) : pack_h2(e[0], e[1]);
+            p[j / 2 + 1] = BF ? pack_bf2(e[2], e[3]) : pack_h2(e[2], e[3]);
+          }
+          // columns 16 h ..: S's there have been read
+          tmem_st16(tw + 16 * h, p);
         }
         float l0, l1;
         unpack_f32x2(sum, l0, l1);
         l += l0 + l1;
-        tmem_st32(tw, p);
         tmem_st_wait();
       }
       tc_fence_before();
-      mbar_arrive(&sh.p_full);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.p_full);
     }
-    if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sh.v_empty[(nt - 1) % C::ST], ((nt - 1) / C::ST) & 1));
-    if (!ok) sh.fail = 1;
+    if (ok) ok = wait(&sh.v_empty, (nt - 1) & 1);
+    if (!ok && lane == 0) sh.fail = 1;
     tc_fence_after();
     if (busy && ok) {
       // ---- the row's output, or its partial result
       const bool whole = w.n == 1, none = m == -INFINITY && l == 0.f;  // (all scores NaN: l is NaN)
       const float inv = whole ? (none ? 0.f : 1.f / l) : 1.f;
-      const bool drafts = w.t0 < ndr;
+      const bool odd = w.t0 < ndr && (sh.odd[0] | sh.odd[1] | sh.odd[2] | sh.odd[3]) != 0;
       float *pt = a.part + ((size_t)w.slot * a.part_rows + tid) * (HD + 2);
       __nv_bfloat16 *o = reinterpret_cast<__nv_bfloat16 *>(a.o) +
                          (((size_t)w.b * a.T + t) * a.H + w.g * rep + r % rep) * HD;
-#pragma unroll
+#pragma unroll 1
       for (int h = 0; h < HD / 32; ++h) {
         uint32_t v[32];
         tmem_ld32(tw + 128 + 32 * h, v);
         tmem_ld_wait();
         if (!in) continue;
-        if (drafts && (sh.odd[0] | sh.odd[1] | sh.odd[2] | sh.odd[3])) {
-          for (int j = w.t0 * kTile; j < min(w.cnt, w.t1 * kTile); ++j) {
+        if (odd) {
+#pragma unroll 1
+          for (int j = 0; j < w.cnt; ++j) {
             if (!(sh.odd[j / 32] >> (j % 32) & 1)) continue;
             const bool see = a.mask ? a.mask[((size_t)w.b * a.T + t) * a.words + j / 32] >> (j % 32) & 1 : j <= t;
             if (!see) continue;
@@ -685,8 +692,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
             uint32_t u[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              u[k] = none ? 0u
-                          : pack_bf2(__uint_as_float(v[e + 2 * k]) * inv, __uint_as_float(v[e + 2 * k + 1]) * inv);
+              u[k] = none ? 0u : pack_bf2(__uint_as_float(v[e + 2 * k]) * inv, __uint_as_float(v[e + 2 * k + 1]) * inv);
             *reinterpret_cast<uint4 *>(o + 32 * h + e) = make_uint4(u[0], u[1], u[2], u[3]);
           }
         } else {
@@ -717,7 +723,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
     for (int i = 0; i < (1 << 20) && global_timer_ns() - t0 < 2000000ull; ++i) __nanosleep(1000);
     __syncthreads();
   }
-  if (warp == 8) {
+  if (warp == kMmaWarp) {
     tc_fence_after();
     tmem_dealloc(tm, kTmemCols);
   }
@@ -788,6 +794,12 @@ cudaError_t launch_tree_tc_t(const TreeArgs &a, unsigned grid, bool merge, cudaS
   constexpr int sm = Cfg<HD, BITS>::SMEM;
   cudaError_t e = cudaFuncSetAttribute(attn_tree_tc_kernel<HD, BITS>, cudaFuncAttributeMaxDynamicSharedMemorySize, sm);
   if (e != cudaSuccess) return e;
+  // the warps' shares of registers have to fit into what the block is launched with, or their exchange would wait forever
+  static const int regs = [] {
+    cudaFuncAttributes f;
+    return cudaFuncGetAttributes(&f, attn_tree_tc_kernel<HD, BITS>) == cudaSuccess ? f.numRegs : 0;
+  }();
+  if (kRegsSoftmax * 128 + kRegsConv * kConv > regs * (128 + kConv)) return cudaErrorInvalidConfiguration;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
