@@ -24,6 +24,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cstdint>
 
 #include "wq_internal.h"
@@ -789,17 +790,31 @@ __global__ void __launch_bounds__(256) attn_tree_merge_kernel(const TreeArgs a) 
 
 namespace {
 
+// Once a device: the kernel's shared memory; and whether the warps' shares of
+// registers fit into what a block is launched with (their exchange would wait
+// forever otherwise).
+template <int HD, int BITS>
+cudaError_t prepare_tc() {
+  static std::atomic<bool> done[64];
+  auto k = attn_tree_tc_kernel<HD, BITS>;
+  constexpr int smem = Cfg<HD, BITS>::SMEM;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= 0 && dev < 64 && done[dev].load(std::memory_order_acquire)) return cudaSuccess;
+  cudaFuncAttributes f;
+  if ((e = cudaFuncGetAttributes(&f, k)) != cudaSuccess) return e;
+  if (kRegsSoftmax * 128 + kRegsConv * kConv > f.numRegs * (128 + kConv)) return cudaErrorInvalidConfiguration;
+  if ((e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return e;
+  if (dev >= 0 && dev < 64) done[dev].store(true, std::memory_order_release);
+  return cudaSuccess;
+}
+
 template <int HD, int BITS>
 cudaError_t launch_tree_tc_t(const TreeArgs &a, unsigned grid, bool merge, cudaStream_t s) {
   constexpr int sm = Cfg<HD, BITS>::SMEM;
-  cudaError_t e = cudaFuncSetAttribute(attn_tree_tc_kernel<HD, BITS>, cudaFuncAttributeMaxDynamicSharedMemorySize, sm);
+  cudaError_t e = prepare_tc<HD, BITS>();
   if (e != cudaSuccess) return e;
-  // the warps' shares of registers have to fit into what the block is launched with, or their exchange would wait forever
-  static const int regs = [] {
-    cudaFuncAttributes f;
-    return cudaFuncGetAttributes(&f, attn_tree_tc_kernel<HD, BITS>) == cudaSuccess ? f.numRegs : 0;
-  }();
-  if (kRegsSoftmax * 128 + kRegsConv * kConv > regs * (128 + kConv)) return cudaErrorInvalidConfiguration;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;

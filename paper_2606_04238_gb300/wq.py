@@ -134,7 +134,12 @@ def _ptr(t):
 
 
 def _stream():
-    return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
+    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+
+
+def _raw_stream() -> int:
+    """The current stream's handle, without the Stream object that torch.cuda.current_stream() makes."""
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 @dataclass
@@ -503,40 +508,30 @@ def decoder_layer_forward(x, lens, layer: DecoderLayer, k_cache, v_cache, prenor
     return y
 
 
-@dataclass
 class KVCache:
-    """A KV cache [batch, n_kv, max_len, head_dim] of 16 (bf16), 8 or 4 bits (wq_kv_cache)."""
-    k: torch.Tensor                      # bf16, or uint8 [batch, n_kv, max_len, head_dim * bits / 8]
-    v: torch.Tensor
-    k_meta: torch.Tensor | None          # int32 [batch, n_kv, max_len]: scale and zero of a row
-    v_meta: torch.Tensor | None
-    head_dim: int
-    bits: int
+    """A KV cache [batch, n_kv, max_len, head_dim] of 16 (bf16), 8 or 4 bits (wq_kv_cache): k, v are
+    bf16, or uint8 [batch, n_kv, max_len, head_dim * bits / 8] with int32 k_meta, v_meta
+    [batch, n_kv, max_len] (scale and zero of a row).  The tensors are held; the C struct is made once."""
+    __slots__ = ("_k", "_v", "_k_meta", "_v_meta", "batch", "n_kv", "max_len", "head_dim", "bits", "_c", "_ref")
 
-    @property
-    def batch(self) -> int:
-        return self.k.shape[0]
+    def __init__(self, k, v, k_meta, v_meta, head_dim: int, bits: int):
+        want = torch.bfloat16 if bits == 16 else torch.uint8
+        for t in (k, v):
+            assert t.is_cuda and t.dtype == want and t.dim() == 4 and t.is_contiguous() and t.shape == k.shape
+            assert t.shape[3] == (head_dim if bits == 16 else head_dim * bits // 8)
+        for t in (k_meta, v_meta) if bits != 16 else ():
+            assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and t.shape == k.shape[:3]
+        self._k, self._v, self._k_meta, self._v_meta = k, v, k_meta, v_meta
+        self.batch, self.n_kv, self.max_len = k.shape[:3]
+        self.head_dim, self.bits = head_dim, bits
+        meta = [None if t is None else t.data_ptr() for t in (k_meta, v_meta)]
+        self._c = _KVCache(k.data_ptr(), v.data_ptr(), *meta, self.batch, self.n_kv, self.max_len, head_dim, bits)
+        self._ref = ctypes.byref(self._c)
 
-    @property
-    def n_kv(self) -> int:
-        return self.k.shape[1]
-
-    @property
-    def max_len(self) -> int:
-        return self.k.shape[2]
-
-    def __post_init__(self):
-        want = torch.bfloat16 if self.bits == 16 else torch.uint8
-        for t in (self.k, self.v):
-            assert t.is_cuda and t.dtype == want and t.is_contiguous() and t.shape == self.k.shape
-            assert t.shape[3] == (self.head_dim if self.bits == 16 else self.head_dim * self.bits // 8)
-        for t in (self.k_meta, self.v_meta) if self.bits != 16 else ():
-            assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and t.shape == self.k.shape[:3]
-
-    def c(self) -> _KVCache:
-        meta = [None if t is None else t.data_ptr() for t in (self.k_meta, self.v_meta)]
-        return _KVCache(self.k.data_ptr(), self.v.data_ptr(), *meta, self.batch, self.n_kv, self.max_len, self.head_dim,
-                        self.bits)
+    k = property(lambda self: self._k)
+    v = property(lambda self: self._v)
+    k_meta = property(lambda self: self._k_meta)
+    v_meta = property(lambda self: self._v_meta)
 
 
 def kv_cache(batch: int, n_kv: int, max_len: int, head_dim: int, bits: int = 16, device="cuda") -> KVCache:
@@ -552,40 +547,48 @@ def kv_cache(batch: int, n_kv: int, max_len: int, head_dim: int, bits: int = 16,
     return KVCache(k, v, km, vm, head_dim, bits)
 
 
-def _ints(t, shape, name):
-    assert t is None or (t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == shape), \
-        f"{name}: int32 {shape} on the device"
+_Strides = ctypes.c_int64 * 3
+
+
+def _at(t, dtype, shape, name):
+    """The address of a contiguous device tensor of this type and shape (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+        raise AssertionError(f"{name}: contiguous {dtype} {shape} on the device, not {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
 
 
 def kv_append(cache: KVCache, k, v, start, counts=None, index=None):
     """wq_kv_append: rows k, v (bf16 or fp32 [batch, T, n_kv, head_dim], any strides of the first
     three dimensions that are multiples of 16 bytes) quantized into the cache at positions
     start[b] + i; ``index`` [batch, n] picks the source token of row i, ``counts`` [batch] how many."""
-    b, t, hkv, hd = k.shape
-    assert k.is_cuda and v.is_cuda and k.shape == v.shape and k.dtype == v.dtype and k.dtype in (torch.bfloat16, torch.float32)
-    assert (b, hkv, hd) == (cache.batch, cache.n_kv, cache.head_dim) and k.stride(3) == 1 and v.stride(3) == 1
+    b, t = cache.batch, k.shape[1]
+    dt = k.dtype
+    assert dt is torch.bfloat16 or dt is torch.float32
+    assert k.shape == (b, t, cache.n_kv, cache.head_dim) and v.shape == k.shape and v.dtype is dt
+    assert k.is_cuda and v.is_cuda
+    ks, vs = k.stride(), v.stride()
+    assert ks[3] == 1 and vs[3] == 1
     n = t if index is None else index.shape[1]
-    _ints(start, (b,), "start"), _ints(counts, (b,), "counts"), _ints(index, (b, n), "index")
-    cc = cache.c()
-    ks, vs = (ctypes.c_int64 * 3)(*k.stride()[:3]), (ctypes.c_int64 * 3)(*v.stride()[:3])
-    _check(lib().wq_kv_append(ctypes.byref(cc), _ptr(k), _ptr(v), WQ_F32 if k.dtype == torch.float32 else WQ_BF16, t,
-                              ks, vs, _ptr(start), _ptr(counts), _ptr(index), n, _stream()))
+    i32 = torch.int32
+    _check(lib().wq_kv_append(cache._ref, k.data_ptr(), v.data_ptr(), 1 if dt is torch.float32 else 0, t,
+                              _Strides(*ks[:3]), _Strides(*vs[:3]), _at(start, i32, (b,), "start"),
+                              _at(counts, i32, (b,), "counts"), _at(index, i32, (b, n), "index"), n, _raw_stream()))
 
 
 def kv_read(cache: KVCache, start, n: int, counts=None, dtype=torch.bfloat16, k=None, v=None):
     """wq_kv_read: (k, v) [batch, n, n_kv, head_dim] of positions start[b] .. start[b] + n - 1 in bf16 or fp32."""
-    assert dtype in (torch.bfloat16, torch.float32)
-    shape = (cache.batch, n, cache.n_kv, cache.head_dim)
-    _ints(start, (cache.batch,), "start"), _ints(counts, (cache.batch,), "counts")
+    assert dtype is torch.bfloat16 or dtype is torch.float32
+    b = cache.batch
+    shape = (b, n, cache.n_kv, cache.head_dim)
     if k is None:
-        k = torch.empty(shape, dtype=dtype, device=cache.k.device)
+        k = torch.empty(shape, dtype=dtype, device=cache._k.device)
     if v is None:
-        v = torch.empty(shape, dtype=dtype, device=cache.k.device)
-    assert k.is_cuda and v.is_cuda and k.dtype == dtype and v.dtype == dtype and k.is_contiguous() and v.is_contiguous()
-    assert tuple(k.shape) == shape and tuple(v.shape) == shape
-    cc = cache.c()
-    _check(lib().wq_kv_read(ctypes.byref(cc), _ptr(start), _ptr(counts), n, _ptr(k), _ptr(v),
-                            WQ_F32 if dtype == torch.float32 else WQ_BF16, _stream()))
+        v = torch.empty(shape, dtype=dtype, device=cache._k.device)
+    _check(lib().wq_kv_read(cache._ref, _at(start, torch.int32, (b,), "start"), _at(counts, torch.int32, (b,), "counts"),
+                            n, _at(k, dtype, shape, "k"), _at(v, dtype, shape, "v"), 1 if dtype is torch.float32 else 0,
+                            _raw_stream()))
     return k, v
 
 
@@ -598,21 +601,21 @@ def rope_table(n_pos: int, head_dim: int, theta: float = 1e6, device="cuda") -> 
 
 def qkv_rope(qkv, positions, table, n_heads: int, n_kv: int, x=None, head_norm: bool = True, q=None, k=None, v=None):
     """wq_qkv_rope: bf16 (q [m, n_heads, hd], k, v [m, n_kv, hd]) from fp32 projections [m, (n_heads + 2 n_kv) hd]."""
-    m, hd = qkv.shape[0], 2 * table.shape[1]
-    assert qkv.is_cuda and qkv.dtype == torch.float32 and qkv.is_contiguous() and qkv.shape[1] == (n_heads + 2 * n_kv) * hd
-    assert table.is_cuda and table.dtype == torch.float32 and table.is_contiguous() and table.shape[2] == 2
-    assert x is None or (x.is_cuda and x.dtype == torch.bfloat16 and x.is_contiguous() and x.shape[0] == m)
-    _ints(positions, (m,), "positions")
-    out = []
-    for t, h in ((q, n_heads), (k, n_kv), (v, n_kv)):
-        if t is None:
-            t = torch.empty((m, h, hd), dtype=torch.bfloat16, device=qkv.device)
-        assert t.is_cuda and t.dtype == torch.bfloat16 and t.is_contiguous() and t.numel() == m * h * hd
-        out.append(t)
-    _check(lib().wq_qkv_rope(_ptr(qkv), _ptr(x), m, 0 if x is None else x.shape[1], _ptr(positions), _ptr(table),
-                             table.shape[0], n_heads, n_kv, hd, WQ_HEAD_NORM if head_norm else 0, _ptr(out[0]),
-                             _ptr(out[1]), _ptr(out[2]), _stream()))
-    return tuple(out)
+    m, n_pos, hd = qkv.shape[0], table.shape[0], 2 * table.shape[1]
+    bf, f32, dev = torch.bfloat16, torch.float32, qkv.device
+    if q is None:
+        q = torch.empty((m, n_heads, hd), dtype=bf, device=dev)
+    if k is None:
+        k = torch.empty((m, n_kv, hd), dtype=bf, device=dev)
+    if v is None:
+        v = torch.empty((m, n_kv, hd), dtype=bf, device=dev)
+    d = 0 if x is None else x.shape[1]
+    _check(lib().wq_qkv_rope(_at(qkv, f32, (m, (n_heads + 2 * n_kv) * hd), "qkv"), _at(x, bf, (m, d), "x"), m, d,
+                             _at(positions, torch.int32, (m,), "positions"), _at(table, f32, (n_pos, hd // 2, 2), "table"),
+                             n_pos, n_heads, n_kv, hd, WQ_HEAD_NORM if head_norm else 0,
+                             _at(q, bf, (m, n_heads, hd), "q"), _at(k, bf, (m, n_kv, hd), "k"),
+                             _at(v, bf, (m, n_kv, hd), "v"), _raw_stream()))
+    return q, k, v
 
 
 def tree_mask(parents: torch.Tensor) -> torch.Tensor:
@@ -644,21 +647,19 @@ def attn_tree(q, k_new, v_new, cache: KVCache, lens, mask=None, counts=None, sca
     """wq_attn_tree: attention of drafts q [batch, T, n_heads, hd] over the cache's first lens[b] positions
     and the drafts k_new, v_new [batch, T, n_kv, hd] that ``mask`` (int32 [batch, T, ceil(T/32)], see
     tree_mask; None: a chain) lets them see."""
-    b, t, h, hd = q.shape
-    assert (b, hd) == (cache.batch, cache.head_dim)
-    for x, heads in ((q, h), (k_new, cache.n_kv), (v_new, cache.n_kv)):
-        assert x.is_cuda and x.dtype == torch.bfloat16 and x.is_contiguous() and tuple(x.shape) == (b, t, heads, hd)
-    _ints(lens, (b,), "lens"), _ints(counts, (b,), "counts"), _ints(mask, (b, t, (t + 31) // 32), "mask")
+    t, h = q.shape[1], q.shape[2]
+    b, hkv, hd = cache.batch, cache.n_kv, cache.head_dim
+    bf, i32 = torch.bfloat16, torch.int32
+    rows, kv = (b, t, h, hd), (b, t, hkv, hd)
     if o is None:
-        o = torch.empty_like(q)
-    assert o.is_cuda and o.dtype == torch.bfloat16 and o.is_contiguous() and o.shape == q.shape
+        o = torch.empty(rows, dtype=bf, device=q.device)
     if ws is None:
-        ws = attn_tree_workspace(b, max(t, 1), h, cache.n_kv, hd, cache.max_len, device=q.device)
+        ws = attn_tree_workspace(b, max(t, 1), h, hkv, hd, cache.max_len, device=q.device)
     assert ws.is_cuda
-    cc = cache.c()
-    _check(lib().wq_attn_tree(_ptr(q), _ptr(k_new), _ptr(v_new), t, h, ctypes.byref(cc), _ptr(lens), _ptr(counts),
-                              _ptr(mask), hd ** -0.5 if scale is None else float(scale), _ptr(o), _ptr(ws), ws.numel(),
-                              _stream()))
+    _check(lib().wq_attn_tree(_at(q, bf, rows, "q"), _at(k_new, bf, kv, "k_new"), _at(v_new, bf, kv, "v_new"), t, h,
+                              cache._ref, _at(lens, i32, (b,), "lens"), _at(counts, i32, (b,), "counts"),
+                              _at(mask, i32, (b, t, (t + 31) // 32), "mask"), hd ** -0.5 if scale is None else scale,
+                              _at(o, bf, rows, "o"), ws.data_ptr(), ws.numel(), _raw_stream()))
     return o
 
 
@@ -677,26 +678,24 @@ def decoder_tree_forward(x, lens, positions, layer: DecoderLayer, cache: KVCache
     """wq_decoder_tree_forward: the verify step of a layer for x bf16 [batch, T, d].  Returns
     (y, k_new, v_new); kv_append(cache, k_new, v_new, lens, counts=.., index=..) then keeps the accepted path."""
     b, t, d = x.shape
-    assert x.is_cuda and x.dtype == torch.bfloat16 and x.is_contiguous() and b == cache.batch
-    assert table.is_cuda and table.dtype == torch.float32 and table.is_contiguous() and tuple(table.shape[1:]) == (cache.head_dim // 2, 2)
-    _ints(lens, (b,), "lens"), _ints(positions, (b, t), "positions"), _ints(counts, (b,), "counts")
-    _ints(mask, (b, t, (t + 31) // 32), "mask")
-    shape = (b, t, cache.n_kv, cache.head_dim)
-    k_new = torch.empty(shape, dtype=torch.bfloat16, device=x.device) if k_new is None else k_new
-    v_new = torch.empty(shape, dtype=torch.bfloat16, device=x.device) if v_new is None else v_new
-    for u in (k_new, v_new):
-        assert u.is_cuda and u.dtype == torch.bfloat16 and u.is_contiguous() and tuple(u.shape) == shape
+    bf, i32 = torch.bfloat16, torch.int32
+    assert b == cache.batch and d == layer.qkv.k
+    kv = (b, t, cache.n_kv, cache.head_dim)
+    k_new = torch.empty(kv, dtype=bf, device=x.device) if k_new is None else k_new
+    v_new = torch.empty(kv, dtype=bf, device=x.device) if v_new is None else v_new
     if y is None:
         y = torch.empty_like(x)
-    assert y.is_cuda and y.dtype == torch.bfloat16 and y.is_contiguous() and y.shape == x.shape
     if ws is None:
         ws = decoder_tree_workspace(b, max(t, 1), layer, cache.max_len, device=x.device)
+    assert ws.is_cuda
+    n_pos = table.shape[0]
     cl = c_layer if c_layer is not None else layer.c()
-    cc = cache.c()
-    _check(lib().wq_decoder_tree_forward(_ptr(x), t, _ptr(lens), _ptr(positions), ctypes.byref(cl), ctypes.byref(cc),
-                                         _ptr(table), table.shape[0], _ptr(counts), _ptr(mask),
-                                         WQ_PRENORM if prenorm else 0, _ptr(k_new), _ptr(v_new), _ptr(y), _ptr(ws),
-                                         ws.numel(), _stream()))
+    _check(lib().wq_decoder_tree_forward(
+        _at(x, bf, (b, t, d), "x"), t, _at(lens, i32, (b,), "lens"), _at(positions, i32, (b, t), "positions"),
+        ctypes.byref(cl), cache._ref, _at(table, torch.float32, (n_pos, cache.head_dim // 2, 2), "table"), n_pos,
+        _at(counts, i32, (b,), "counts"), _at(mask, i32, (b, t, (t + 31) // 32), "mask"), WQ_PRENORM if prenorm else 0,
+        _at(k_new, bf, kv, "k_new"), _at(v_new, bf, kv, "v_new"), _at(y, bf, (b, t, d), "y"), ws.data_ptr(), ws.numel(),
+        _raw_stream()))
     return y, k_new, v_new
 
 
