@@ -1527,8 +1527,8 @@ wq_status attn_tree_impl(const void *q, const void *k_new, const void *v_new, in
   a.lens = lens, a.counts = counts, a.mask = mask;
   a.batch = c->batch, a.T = n_draft, a.H = n_heads, a.Hkv = c->n_kv, a.max_len = c->max_len, a.words = (n_draft + 31) / 32;
   a.scale = scale * 1.4426950408889634f;  // scores in units of log 2
-  a.table = static_cast<int2 *>(ws);
-  a.part = reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + up256(sizeof(int2) * (size_t)c->batch));
+  a.table = static_cast<int4 *>(ws);
+  a.part = reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + up256(sizeof(int4) * (size_t)c->batch));
   a.o = o;
   cudaError_t e;
   if (scale != 0.f && n_draft * (n_heads / c->n_kv) > kTreeMmaRows) {
@@ -1614,7 +1614,7 @@ size_t wq_attn_tree_workspace_bytes(int batch, int n_draft, int n_heads, int n_k
   const int sms = num_sms();
   if (batch <= 0 || n_draft <= 0 || n_heads <= 0 || n_kv <= 0 || head_dim <= 0 || max_len <= 0 || sms <= 0) return 0;
   if (n_heads % n_kv != 0) return 0;
-  return up256(sizeof(int2) * (size_t)batch) +
+  return up256(sizeof(int4) * (size_t)batch) +
          up256(4 * std::max(tree_part_floats(batch, n_draft, n_heads, n_kv, head_dim, max_len, sms),
                             tree_tc_part_floats(batch, n_draft, n_heads, n_kv, head_dim, max_len, sms)));
 }

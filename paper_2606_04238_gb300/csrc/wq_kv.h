@@ -58,16 +58,16 @@ struct TreeArgs {
   void *o;                      // bf16 [batch][T][H][HD]
   int S;
   // tcgen05 kernel: ranges of tiles wanted, least tiles a range, rows of a range's
-  // partial results, and per sequence its first range and its splits
-  int target, min_tiles, part_rows;
-  int2 *table;
+  // partial results, and per sequence its first range, splits, row blocks and drafts
+  int target, min_tiles, part_rows, rep_magic;
+  int4 *table;
 };
 // Splits of the context a launch takes, and its partial results in floats.
 int tree_splits(int batch, int T, int H, int Hkv, int max_len, int num_sms);
 size_t tree_part_floats(int batch, int T, int H, int Hkv, int hd, int max_len, int num_sms);
 cudaError_t launch_attn_tree(const TreeArgs &a, int hd, int bits, cudaStream_t s);
 cudaError_t read_tree_status(int *status);
-// The same on the tcgen05 tensor cores (wq_tree_tc.cu); part: [range][part_rows][HD + 2].
+// The same on the tcgen05 tensor cores (wq_tree_tc.cu); part: [range][part_rows][HD + 4].
 size_t tree_tc_part_floats(int batch, int T, int H, int Hkv, int hd, int max_len, int num_sms);
 cudaError_t launch_attn_tree_tc(TreeArgs a, int hd, int bits, int num_sms, cudaStream_t s);
 cudaError_t read_tree_tc_status(int *status);

@@ -13,8 +13,8 @@
 // swizzled layout, 12 issues the MMAs.  Two CTAs an SM (256 TMEM columns and ~100 KB
 // each) fill each other's waits: a tile's products, softmax and products again are
 // one chain.  A draft tile's rows are brought into binary16 by an exact power of two
-// a row.  The running maximum is raised, and O rescaled in TMEM, only when a row's
-// scores pass it by 2^8: p stays below 2^8.
+// a row.  The running maximum is raised, and O rescaled in TMEM, only when 32 of a
+// row's probabilities add up to 2^8: p stays below that, and no maximum is searched.
 //
 // The tiles of all (b, g, row block) are dealt to the CTAs in nearly equal
 // ranges: every CTA finds the tiles a range takes from the lengths themselves.
@@ -45,10 +45,12 @@ constexpr int kConv = 256;        // converting threads
 constexpr int kTcThreads = 128 + kConv + 32;
 constexpr int kMmaWarp = 4 + kConv / 32;
 constexpr int kBlk = kTile * 128;  // bytes of a 64-value block of Q, K or V: [row][128 bytes], swizzled
-constexpr float kRaise = 8.f;
 constexpr int kTmemCols = 256;    // S / P 0..127, O 128..
-// registers a thread: the launch's 72 x 416 shared out as 88 x 128 + 64 x 256 + 72 x 32
-constexpr int kRegsSoftmax = 88, kRegsConv = 64;
+// Queries enter binary16 times 2^7, which keeps a row with its largest |q| in [2^-4, 2^8) whole but for values
+// below 2^-27 of that; other rows by a power of two of their own.
+constexpr int kQueryShift = 7;
+// registers a thread: the launch's 72 x 416 shared out as 104 x 128 + 56 x 256 + 72 x 32
+constexpr int kRegsSoftmax = 104, kRegsConv = 56;
 
 __device__ __forceinline__ float bf_lo(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
@@ -64,12 +66,21 @@ __device__ __forceinline__ uint32_t hsub2_u(uint32_t a, uint32_t b) {
   const __half2 v = __hsub2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
   return *reinterpret_cast<const uint32_t *>(&v);
 }
+__device__ __forceinline__ uint32_t hmul2_u(uint32_t a, uint32_t b) {
+  const __half2 v = __hmul2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
+  return *reinterpret_cast<const uint32_t *>(&v);
+}
 // a / 16 - b
 __device__ __forceinline__ uint32_t hfma16_u(uint32_t a, uint32_t b) {
   const uint32_t k = 0x2c002c00u;  // 1/16, 1/16
   const __half2 v = __hfma2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&k),
                             __hneg2(*reinterpret_cast<const __half2 *>(&b)));
   return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
+  uint64_t v;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+  return v;
 }
 // Barrier `id` over `count` threads: whether `v` holds for all of them.
 __device__ __forceinline__ bool barrier_and(int id, int count, bool v) {
@@ -96,14 +107,7 @@ __device__ __forceinline__ int f16_shift(float mx, int top) {
   return mx == 0.f ? 0 : min(126, top - e);
 }
 
-// 32 lanes x 32 consecutive 32-bit TMEM columns, written.
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&v)[32]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(
-          taddr),
-      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
-      : "memory");
-}
+// 32 lanes x 16 consecutive 32-bit TMEM columns, written.
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
@@ -134,6 +138,36 @@ __host__ __device__ constexpr uint32_t tree_idesc(int N, bool bf16, bool b_mn) {
          ((uint32_t)(kTcRows >> 4) << 24);
 }
 
+// 2^(m - mn) for a maximum raised from m to mn (whole numbers, or infinite).
+__device__ __forceinline__ float raise_factor(float m, float mn) {
+  const float d = m - mn;
+  return mn == m ? 1.f : d < -126.f ? 0.f : pow2i((int)d);
+}
+// What a row has so far, times al: its probabilities of the tile's first 32 pc columns, and 16 oc columns of O.
+template <bool BF>
+__device__ __noinline__ void rescale(uint32_t tw, int pc, int oc, float al) {
+  tmem_st_wait();
+#pragma unroll 1
+  for (int c = 0; c < pc; ++c) {
+    uint32_t p[16];
+    tmem_ld16(tw + 16 * c, p);
+    tmem_ld_wait();
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      p[e] = BF ? pack_bf2(bf_lo(p[e]) * al, bf_hi(p[e]) * al) : hmul2_u(p[e], pack_h2(al, al));
+    tmem_st16(tw + 16 * c, p);
+  }
+#pragma unroll 1
+  for (int c = 0; c < oc; ++c) {
+    uint32_t o[16];
+    tmem_ld16(tw + 128 + 16 * c, o);
+    tmem_ld_wait();
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * al);
+    tmem_st16(tw + 128 + 16 * c, o);
+  }
+}
+
 // What a CTA takes: row block rb of (b, g), tiles t0 .. t1 - 1 (drafts' tiles
 // first); n splits of the row block, this is `split`, its partial results at `slot`.
 struct Work {
@@ -151,59 +185,77 @@ __device__ __forceinline__ void seq_tiles(const TreeArgs &a, int b, int rep, int
   blocks = bad ? 0 : max(1, (cnt * rep + kTcRows - 1) / kTcRows);
 }
 
-// One warp (every CTA the same sums): the least number W of tiles a range for which
-// the ranges are at most `target` (or the longest sequence's tiles), then this
-// CTA's range.  W >= a.min_tiles.
+// a / b rounded up, 0 <= a < 2^22, by the reciprocal: the product is within 1 of the quotient.
+__device__ __forceinline__ int ceil_div(int a, int b, float rb) {
+  int q = (int)(__int2float_rn(a) * rb);
+  q -= q * b > a;
+  q += (q + 1) * b <= a;
+  return q + (q * b < a);
+}
+
+// One warp, every CTA the same sums.  Ranges of W tiles: W the least of 32 candidates, from the tiles a CTA of an even
+// split would take up to what certainly gives no more than `target` ranges; then this CTA's range.
 __device__ Work find_work(const TreeArgs &a, int rep, int cta) {
   const int lane = threadIdx.x & 31;
-  int len, cnt, tiles, blocks;
-  auto ranges = [&](int W) {  // ranges of all sequences with W tiles each
-    long long s = 0;
-    for (int b = lane; b < a.batch; b += 32) {
-      seq_tiles(a, b, rep, len, cnt, tiles, blocks);
-      s += (long long)((tiles + W - 1) / W) * blocks;
-    }
-    for (int o = 16; o >= 1; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    return s * a.Hkv;
-  };
-  long long total = 0;
+  int len = 0, cnt = 0, tiles = 0, blocks = 0;
+  long long total = 0, many = 0;
   int most = 1;
   for (int b = lane; b < a.batch; b += 32) {
     seq_tiles(a, b, rep, len, cnt, tiles, blocks);
     total += (long long)tiles * blocks;
+    many += blocks;
     most = max(most, tiles);
   }
+#pragma unroll
   for (int o = 16; o >= 1; o >>= 1) {
     total += __shfl_xor_sync(0xffffffffu, total, o);
-    most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+    many += __shfl_xor_sync(0xffffffffu, many, o);
   }
+  most = __reduce_max_sync(0xffffffffu, most);
   total *= a.Hkv;
-  int lo = max(a.min_tiles, (int)min((long long)most, (total + a.target - 1) / a.target)), hi = max(most, lo);
-  while (lo < hi) {
-    const int mid = (lo + hi) / 2;
-    if (ranges(mid) <= a.target)
-      hi = mid;
-    else
-      lo = mid + 1;
+  many *= a.Hkv;
+  int W = most;
+  if (many < a.target && most > a.min_tiles) {
+    // sum ceil(tiles / W) <= total / W + many: no more than `target` at hi
+    const int lo = max(a.min_tiles, (int)((total + a.target - 1) / a.target));
+    const int hi = min(most, max(lo, (int)((total + (a.target - many) - 1) / (a.target - many))));
+    const int cand = lo + (int)((long long)(hi - lo) * lane / 31);
+    const float rc = __frcp_rn((float)cand);
+    long long n = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += 32) {
+      if (a.batch > 32) {
+        tiles = blocks = 0;
+        if (b0 + lane < a.batch) seq_tiles(a, b0 + lane, rep, len, cnt, tiles, blocks);
+      }
+      const int m = min(32, a.batch - b0);
+#pragma unroll 4
+      for (int j = 0; j < m; ++j)
+        n += ceil_div(__shfl_sync(0xffffffffu, tiles, j), cand, rc) * __shfl_sync(0xffffffffu, blocks, j);
+    }
+    const unsigned fits = __ballot_sync(0xffffffffu, n * a.Hkv <= a.target);
+    W = __shfl_sync(0xffffffffu, cand, fits ? __ffs(fits) - 1 : 31);
   }
-  const int W = lo;
+  const float rw = __frcp_rn((float)W);
   // the sequence this CTA falls into
   Work w;
   w.any = false;
   long long base = 0;
   for (int b0 = 0; b0 < a.batch; b0 += 32) {
     const int b = b0 + lane;
-    tiles = blocks = len = cnt = 0;
-    if (b < a.batch) seq_tiles(a, b, rep, len, cnt, tiles, blocks);
-    const int n = (tiles + W - 1) / W, mine = n * blocks * a.Hkv;
+    if (a.batch > 32) {
+      tiles = blocks = len = cnt = 0;
+      if (b < a.batch) seq_tiles(a, b, rep, len, cnt, tiles, blocks);
+    }
+    const int n = ceil_div(tiles, W, rw), mine = n * blocks * a.Hkv;
     int incl = mine;
+#pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int up = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += up;
     }
     const unsigned hit = __ballot_sync(0xffffffffu, cta < base + incl);
     if (cta == 0 && b < a.batch) {
-      if (a.table) a.table[b] = make_int2((int)(base + incl - mine), n);
+      a.table[b] = make_int4((int)(base + incl - mine), n, blocks, cnt);
       if (tiles == 0) atomicExch(&g_tree_tc_status, -1);
     }
     if (hit && !w.any) {
@@ -245,12 +297,14 @@ struct Shared {
   int fail;
   uint32_t odd[4];  // drafts whose V has values that are not finite
   Work work;
-  // K's scale (times the score scale), log2 of V's scale, its reciprocal; 1024 + z twice.  Two tiles
-  // of each: the next tile's are written while this one's are read
+  // of a tile: K's scales (times the score scale and the queries' 2^-kQueryShift) and the exponent t of V's operands, which are values
+  // times 2^-t.  Two tiles of each: the next tile's are written while this one's are read
   __align__(16) float sk[2][kTile];
-  __align__(16) float lg[2][kTile];
-  __align__(16) float rs[2][kTile];
-  uint32_t zk[kTile], zv[kTile];
+  float c1[kTcRows];                         // of a row's scores
+  int te[2];
+  uint32_t zk[kTile];                        // 1024 + z of K, twice
+  __align__(16) uint2 zsv[kTile];            // 1024 + z of V, twice; its scale times 2^-t, twice
+  __align__(16) uint32_t top[2][kConv / 32]; // warps' shares of the largest V scale of a tile (bits), of the drafts' |v|
 };
 
 // 8 codes as 8 binary16 values code - z; z1024: 1024 + z in both halves.
@@ -286,12 +340,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
   uint8_t *qbuf = tree_dyn + (1024 - (smem_addr(tree_dyn) & 1023)) % 1024, *kbuf = qbuf + C::KB, *vbuf = kbuf + C::KB;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rep = a.H / a.Hkv;
-  pdl_wait();
-  pdl_launch_dependents();
-  if (warp == 0) {
-    const Work w = find_work(a, rep, blockIdx.x);
-    if (lane == 0) sh.work = w;
-  } else if (warp == kMmaWarp) {
+  if (warp == kMmaWarp) {
     tmem_alloc(&sh.tmem, kTmemCols);
     if (lane == 0) {
       mbar_init(&sh.k_full, kConv / 32);
@@ -306,6 +355,12 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
   } else if (warp == 4 && lane < 4) {
     sh.odd[lane] = 0;
   }
+  pdl_wait();
+  pdl_launch_dependents();
+  if (warp == 0) {
+    const Work w = find_work(a, rep, blockIdx.x);
+    if (lane == 0) sh.work = w;
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -315,6 +370,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
   const int R = a.T * rep, live = w.any ? min(w.cnt * rep - row0, kTcRows) : 0;  // rows of drafts that exist
   const int nt = live > 0 ? w.t1 - w.t0 : 0;
   const int ndr = w.any && w.cnt > 0 ? 1 : 0;  // the drafts are one tile
+  auto draft_of = [&](int row) { return row * a.rep_magic >> 16; };  // row / rep
   // a warp's arrival, its shared-memory writes made visible to the tensor cores
   auto hand_over = [&](uint64_t *bar) {
     fence_proxy_async_smem();
@@ -329,14 +385,14 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
     constexpr uint32_t idqk = tree_idesc(kTile, BF, false), idpv = tree_idesc(HD, BF, true);
     const uint64_t qd = umma_desc_kmajor_sw128(smem_addr(qbuf), 1024), kd = umma_desc_kmajor_sw128(smem_addr(kbuf), 1024);
     const uint64_t vd = umma_desc_mnmajor_sw128(smem_addr(vbuf), kBlk);
-    bool ok = wait(&sh.p_full, 0);  // Q is in place
-    for (int i = 0; i < nt && ok; ++i) {
-      ok = wait(&sh.k_full, i & 1);
-      // P V of the tile before has read P, which S overwrites
-      if (ok && i > 0) ok = wait(&sh.v_empty, (i - 1) & 1);
-      if (!ok) break;
-      tc_fence_after();
-      if (elect_one()) {
+    if (elect_one()) {
+      bool ok = mbar_wait(&sh.p_full, 0);  // Q is in place
+      for (int i = 0; i < nt && ok; ++i) {
+        ok = mbar_wait(&sh.k_full, i & 1);
+        // P V of the tile before has read P, which S overwrites
+        if (ok && i > 0) ok = mbar_wait(&sh.v_empty, (i - 1) & 1);
+        if (!ok) break;
+        tc_fence_after();
 #pragma unroll
         for (int ks = 0; ks < HD / 16; ++ks) {
           const uint64_t off = (uint64_t)(((ks / 4) * kBlk + (ks % 4) * 32) >> 4);
@@ -344,20 +400,17 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
         }
         umma_commit(&sh.s_full);
         umma_commit(&sh.k_empty);
-      }
-      __syncwarp();
-      ok = wait(&sh.p_full, (i + 1) & 1) && wait(&sh.v_full, i & 1);
-      if (!ok) break;
-      tc_fence_after();
-      if (elect_one()) {
+        ok = mbar_wait(&sh.v_full, i & 1) && mbar_wait(&sh.p_full, (i + 1) & 1);
+        if (!ok) break;
+        tc_fence_after();
 #pragma unroll
         for (int ks = 0; ks < kTile / 16; ++ks)
           umma_ts(tm + 128, tm + 8 * ks, vd + (uint64_t)((ks * 2048) >> 4), idpv, i > 0 || ks > 0);
         umma_commit(&sh.v_empty);
       }
-      __syncwarp();
+      if (!ok) sh.fail = 1;
     }
-    if (!ok && lane == 0) sh.fail = 1;
+    __syncwarp();
   } else if (nt > 0 && warp >= 4) {
     // ---- loads and conversion: chunk c of rows r0 + it RS
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsConv));
@@ -391,45 +444,80 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
       }
       cp_async_commit();
     };
-    // the drafts' K or V: in binary16 by a power of two a row, or as it is
-    auto draft = [&](const void *rows, uint8_t *to, bool is_v) {
-      const __nv_bfloat16 *src = reinterpret_cast<const __nv_bfloat16 *>(rows) + ((size_t)w.b * a.T * a.Hkv + w.g) * HD + c * 8;
+    const __nv_bfloat16 *kd = reinterpret_cast<const __nv_bfloat16 *>(a.kn) + ((size_t)w.b * a.T * a.Hkv + w.g) * HD + c * 8;
+    const __nv_bfloat16 *vd = reinterpret_cast<const __nv_bfloat16 *>(a.vn) + ((size_t)w.b * a.T * a.Hkv + w.g) * HD + c * 8;
+    // chunk it of the drafts' rows; V's values that are not finite are noted and taken out
+    auto draft_chunk = [&](const __nv_bfloat16 *src, int it, bool is_v, uint32_t (&x)[4]) {
+      const int j = r0 + it * C::RS;
+      const uint4 v = j < w.cnt ? __ldg(reinterpret_cast<const uint4 *>(src + (size_t)j * a.Hkv * HD)) : make_uint4(0, 0, 0, 0);
+      x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+      if (!is_v) return;
+      bool odd = false;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if ((x[e] & 0x7f80u) == 0x7f80u) x[e] &= 0xffff0000u, odd = true;
+        if ((x[e] & 0x7f800000u) == 0x7f800000u) x[e] &= 0xffffu, odd = true;
+      }
+      if (odd) atomicOr(&sh.odd[j / 32], 1u << (j % 32));
+    };
+    auto largest = [&](const uint32_t (&x)[4]) {
+      float mx = 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) mx = fmaxf(mx, fmaxf(fabsf(bf_lo(x[e])), fabsf(bf_hi(x[e]))));
+      return mx;
+    };
+    auto scaled = [&](uint32_t (&x)[4], float f) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = pack_h2(bf_lo(x[e]) * f, bf_hi(x[e]) * f);
+    };
+    const float qscale = a.scale * pow2i(-kQueryShift);  // of K's scales
+    // The drafts' tile: K in binary16 by a power of two a row, V by one for all (bf16 cache: as they are).
+    auto draft_tile = [&]() {
+      const int its = min(C::IT, (w.cnt + C::RS - 1) / C::RS);  // chunks with drafts in them
+      float vmax = 0.f;
 #pragma unroll 1
-      for (int it = 0; it < C::IT; ++it) {
-        const int j = r0 + it * C::RS;
-        const uint4 v = j < w.cnt ? __ldg(reinterpret_cast<const uint4 *>(src + (size_t)j * a.Hkv * HD)) : make_uint4(0, 0, 0, 0);
-        uint32_t x[4] = {v.x, v.y, v.z, v.w};
-        if (is_v) {
-          bool odd = false;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if ((x[e] & 0x7f80u) == 0x7f80u) x[e] &= 0xffff0000u, odd = true;
-            if ((x[e] & 0x7f800000u) == 0x7f800000u) x[e] &= 0xffffu, odd = true;
-          }
-          if (odd) atomicOr(&sh.odd[j / 32], 1u << (j % 32));
-        }
+      for (int it = 0; it < its; ++it) {
+        uint32_t x[4], y[4];
+        draft_chunk(kd, it, false, x);
+        draft_chunk(vd, it, true, y);
+        vmax = fmaxf(vmax, largest(y));
         if constexpr (!BF) {
-          float mx = 0.f;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) mx = fmaxf(mx, fmaxf(fabsf(bf_lo(x[e])), fabsf(bf_hi(x[e]))));
+          float mx = largest(x);
 #pragma unroll
           for (int o = C::CH / 2; o >= 1; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-          // V as large as codes are, so that p times the row's scale is as large as theirs
-          const int e2 = f16_shift(mx, is_v ? BITS - 1 : 14);
-          const float f = pow2i(e2);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = pack_h2(bf_lo(x[e]) * f, bf_hi(x[e]) * f);
-          if (c == 0) {
-            if (is_v) {
-              sh.lg[0][j] = (float)-e2;
-              sh.rs[0][j] = f;
-            } else {
-              sh.sk[0][j] = a.scale * pow2i(-e2);
-            }
-          }
+          const int e2 = f16_shift(mx, 14);
+          scaled(x, pow2i(e2));
+          if (c == 0) sh.sk[0][r0 + it * C::RS] = qscale * pow2i(-e2);
+        } else {
+          *reinterpret_cast<uint4 *>(vbuf + dst0 + it * C::RS * 128) = make_uint4(y[0], y[1], y[2], y[3]);
         }
-        *reinterpret_cast<uint4 *>(to + dst0 + it * C::RS * 128) = make_uint4(x[0], x[1], x[2], x[3]);
+        *reinterpret_cast<uint4 *>(kbuf + dst0 + it * C::RS * 128) = make_uint4(x[0], x[1], x[2], x[3]);
       }
+      // (K's other rows hold what they held: their scores are not looked at)
+      if constexpr (!BF) {
+        const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(vmax));
+        if (lane == 0) sh.top[0][warp - 4] = top;
+        named_barrier_sync(1, kConv);
+        uint32_t all = 0;
+#pragma unroll
+        for (int i = 0; i < kConv / 32; ++i) all = max(all, sh.top[0][i]);
+        const int e2 = f16_shift(__uint_as_float(all), 13);
+        if (ct == 0) sh.te[0] = -e2;
+        hand_over(&sh.k_full);
+#pragma unroll 1
+        for (int it = 0; it < its; ++it) {
+          uint32_t y[4];
+          draft_chunk(vd, it, true, y);
+          scaled(y, pow2i(e2));
+          *reinterpret_cast<uint4 *>(vbuf + dst0 + it * C::RS * 128) = make_uint4(y[0], y[1], y[2], y[3]);
+        }
+      } else {
+        hand_over(&sh.k_full);
+      }
+#pragma unroll 1
+      for (int it = its; it < C::IT; ++it)
+        *reinterpret_cast<uint4 *>(vbuf + dst0 + it * C::RS * 128) = make_uint4(0, 0, 0, 0);
+      hand_over(&sh.v_full);
     };
     auto pos_of = [&](int i) { return (w.t0 + i - ndr) * kTile; };
     const int i_ctx = max(0, ndr - w.t0);  // first tile of the context
@@ -439,11 +527,18 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
       fetch(kc, kr, pos_of(i_ctx));
       fetch(vc, vr, pos_of(i_ctx));
     }
-    if (i_ctx > 0) {
-      draft(a.kn, kbuf, false);
-      draft(a.vn, vbuf, true);
-      hand_over(&sh.k_full);
-      hand_over(&sh.v_full);
+    if (i_ctx > 0) draft_tile();
+    // the warps' largest V scale of the tile whose scales this thread holds (bits; a NaN does not count)
+    auto note_top = [&](int which) {
+      if (ct < kTile) return;
+      uint32_t v = (meta & 0xffffu) > 0x7c00u ? 0u : meta & 0xffffu;
+      if (v == 0) v = 0x3c00u;  // a zero-filled cache's row counts as 1
+      v = __reduce_max_sync(0xffffffffu, v);
+      if (lane == 0) sh.top[which][warp - 4] = v;
+    };
+    if (!BF && i_ctx < nt) {
+      note_top(i_ctx & 1);
+      named_barrier_sync(1, kConv);
     }
     for (int i = i_ctx; i < nt; ++i) {
       const int p0 = pos_of(i);
@@ -464,20 +559,22 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
       } else {
         const int par = i & 1, pn = i + 1 < nt ? p0 + kTile : p0;
         if (i > 0) ok = wait(&sh.k_empty, (i - 1) & 1);
+        // V's operands (code - z) s 2^-t: t puts the tile's largest s in [2^5, 2^6)
+        const uint4 tops = *reinterpret_cast<const uint4 *>(&sh.top[par][4]);
+        const float stop = __half2float(__ushort_as_half((unsigned short)max(max(tops.x, tops.y), max(tops.z, tops.w))));
+        const int te = (int)(__float_as_uint(stop) >> 23) - 127 - 5;
         {
           const float s0 = __half2float(__ushort_as_half((unsigned short)(meta & 0xffffu)));
           const __half2 z = __hadd2(__half2half2(__ushort_as_half((unsigned short)(meta >> 16))), __float2half2_rn(1024.f));
           const uint32_t zz = *reinterpret_cast<const uint32_t *>(&z);
           const int r = ct & (kTile - 1);
           if (ct < kTile) {
-            sh.sk[par][r] = s0 * a.scale;
+            sh.sk[par][r] = s0 * qscale;
             sh.zk[r] = zz;
+            if (ct == 0) sh.te[par] = te;
           } else {
-            const float sv = s0 == 0.f ? 1.f : s0;  // a zero-filled cache's row: code - z is 0
-            const bool in = p0 + r < w.len;
-            sh.lg[par][r] = in ? __log2f(sv) : -INFINITY;
-            sh.rs[par][r] = in ? __frcp_rn(sv) : 0.f;
-            sh.zv[r] = zz;
+            const float sv = (s0 == 0.f ? 1.f : s0) * pow2i(-te);  // a zero-filled cache's row: code - z is 0
+            sh.zsv[r] = make_uint2(zz, pack_h2(sv, sv));
           }
         }
         ok = barrier_and(1, kConv, ok);  // the warps leave together after a timeout
@@ -490,10 +587,15 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
         fetch(kc, kr, pn);
         if (i > 0) ok = wait(&sh.v_empty, (i - 1) & 1);
 #pragma unroll
-        for (int it = 0; it < C::IT; ++it)
-          *reinterpret_cast<uint4 *>(vbuf + dst0 + it * C::RS * 128) = convert8<BITS>(vr[it], sh.zv[r0 + it * C::RS]);
+        for (int it = 0; it < C::IT; ++it) {
+          const uint2 zs = sh.zsv[r0 + it * C::RS];
+          uint4 v = convert8<BITS>(vr[it], zs.x);
+          v.x = hmul2_u(v.x, zs.y), v.y = hmul2_u(v.y, zs.y), v.z = hmul2_u(v.z, zs.y), v.w = hmul2_u(v.w, zs.y);
+          *reinterpret_cast<uint4 *>(vbuf + dst0 + it * C::RS * 128) = v;
+        }
         hand_over(&sh.v_full);
         fetch(vc, vr, pn);
+        note_top(par ^ 1);
         // every warp has read this tile's zeros before the next one's are written
         ok = barrier_and(1, kConv, ok);
         if (!ok) break;
@@ -505,44 +607,69 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
     }
     if (!ok && lane == 0) sh.fail = 1;
   } else if (nt > 0) {
-    // ---- softmax: thread = row
+    // ---- softmax: thread = row.  Up to 64 (32) rows stand twice (four times) in the 128, each copy with its own
+    // half (quarter) of a tile's positions, so that all four warps work on them; the copies are merged at the end.
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
-    const int r = row0 + tid, t = r / rep;
-    const bool in = tid < live;
-    const bool busy = warp * 32 < live;  // warps without rows only keep the barriers going
+    const int rpc = live <= 32 ? 32 : live <= 64 ? 64 : 128, copies = kTcRows / rpc, copy = tid / rpc;
+    const int lr = tid & (rpc - 1), t = draft_of(row0 + lr);
+    const bool in = lr < live;
+    const bool busy = (warp * 32 & (rpc - 1)) < live;  // warps without rows only keep the barriers going
     const uint32_t tw = tm + ((uint32_t)(warp * 32) << 16);
-    float c1 = a.scale;  // of the raw products: bf16 the score scale (its sign in Q), else 2^-e of the row
+    // c1, of the raw products: bf16 the score scale (its sign in Q); else what a row's own power of two differs from
+    // the common one, which K's scales take in
+    float c1 = BF ? fabsf(a.scale) : 1.f;
+    bool own = false;
+    uint32_t see[4] = {0, 0, 0, 0};
     if (busy) {
-      const uint4 *q = reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(a.q) +
-                                                       (((size_t)w.b * a.T + (in ? t : 0)) * a.H + w.g * rep + (in ? r % rep : 0)) * HD);
-      float f = 1.f;
-      if constexpr (BF) {
-        c1 = fabsf(a.scale);
-      } else {
-        float mx = 0.f;
-#pragma unroll 4
-        for (int i = 0; i < HD / 8; ++i) {
-          const uint4 v = in ? __ldg(q + i) : make_uint4(0, 0, 0, 0);
-          mx = fmaxf(mx, fmaxf(fmaxf(fmaxf(fabsf(bf_lo(v.x)), fabsf(bf_hi(v.x))), fmaxf(fabsf(bf_lo(v.y)), fabsf(bf_hi(v.y)))),
-                               fmaxf(fmaxf(fabsf(bf_lo(v.z)), fabsf(bf_hi(v.z))), fmaxf(fabsf(bf_lo(v.w)), fabsf(bf_hi(v.w))))));
-        }
-        const int e = f16_shift(mx, 14);
-        f = pow2i(e);
-        c1 = pow2i(-e);
+      // a warp's 32 rows, CH lanes a row: copied to their place, then worked on there
+      constexpr int RI = 32 / C::CH;  // rows an instruction
+      const int ch = lane % C::CH;
+      auto place = [&](int row) { return qbuf + (ch / 8) * kBlk + row * 128 + (((ch & 7) ^ (row & 7)) << 4); };
+      const __nv_bfloat16 *q0 = reinterpret_cast<const __nv_bfloat16 *>(a.q) + ((size_t)w.b * a.T * a.H + w.g * rep) * HD + ch * 8;
+#pragma unroll 1
+      for (int row = warp * 32 + lane / C::CH; row < warp * 32 + 32; row += RI) {
+        const int q = row & (rpc - 1), rq = row0 + min(q, live - 1), tq = draft_of(rq);
+        cp_async16_zfill(place(row), q0 + ((size_t)tq * a.H + rq - tq * rep) * HD, q < live ? 16u : 0u);
       }
-#pragma unroll 4
-      for (int i = 0; i < HD / 8; ++i) {
-        const uint4 v = in ? __ldg(q + i) : make_uint4(0, 0, 0, 0);
-        uint32_t x[4] = {v.x, v.y, v.z, v.w};
+      if (w.t0 < ndr && in) {  // the drafts that the row sees
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if (BF)
-            x[e] ^= a.scale < 0.f ? 0x80008000u : 0u;
-          else
-            x[e] = pack_h2(bf_lo(x[e]) * f, bf_hi(x[e]) * f);
+        for (int h = 0; h < 4; ++h)
+          if (32 * h < w.cnt)
+            see[h] = a.mask ? a.mask[((size_t)w.b * a.T + t) * a.words + h]
+                            : t >= 32 * h + 31 ? 0xffffffffu : t < 32 * h ? 0u : (2u << (t - 32 * h)) - 1u;
+      }
+      cp_async_wait_all();
+      __syncwarp();
+      if (!BF || a.scale < 0.f) {
+#pragma unroll 4
+        for (int row = warp * 32 + lane / C::CH; row < warp * 32 + 32; row += RI) {
+          uint4 *at = reinterpret_cast<uint4 *>(place(row));
+          uint4 v = *at;
+          if constexpr (BF) {
+            v.x ^= 0x80008000u, v.y ^= 0x80008000u, v.z ^= 0x80008000u, v.w ^= 0x80008000u;
+          } else {
+            // the largest |q| of the row, as bf16 bits
+            uint32_t mx = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+            mx = max(mx & 0xffffu, mx >> 16);
+#pragma unroll
+            for (int o = C::CH / 2; o >= 1; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            const int e = (int)(mx >> 7) - 127;
+            int mine = kQueryShift;
+            if (mx != 0 && (e < -4 || e >= 8)) mine = max(min(min(126, 14 - e), kQueryShift + 126), -114);
+            const float f = pow2i(mine);
+            v.x = pack_h2(bf_lo(v.x) * f, bf_hi(v.x) * f);
+            v.y = pack_h2(bf_lo(v.y) * f, bf_hi(v.y) * f);
+            v.z = pack_h2(bf_lo(v.z) * f, bf_hi(v.z) * f);
+            v.w = pack_h2(bf_lo(v.w) * f, bf_hi(v.w) * f);
+            if (ch == 0) sh.c1[row] = pow2i(kQueryShift - mine);
+          }
+          *at = v;
         }
-        *reinterpret_cast<uint4 *>(qbuf + (i / 8) * kBlk + tid * 128 + (((i & 7) ^ (tid & 7)) << 4)) =
-            make_uint4(x[0], x[1], x[2], x[3]);
+      }
+      if constexpr (!BF) {
+        __syncwarp();
+        c1 = sh.c1[tid];
+        own = __any_sync(0xffffffffu, c1 != 1.f);
       }
     }
     hand_over(&sh.p_full);  // phase 0: Q
@@ -556,99 +683,123 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
       tc_fence_after();
       if (busy) {
         // which of the tile's positions count: the drafts the row sees, those before the length
-        const bool some = tile < ndr || w.len - (tile - ndr) * kTile < kTile;
-        uint32_t see[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
-        if (some)
+        const bool drafts = tile < ndr;
+        const int left = drafts ? w.cnt : w.len - (tile - ndr) * kTile;
+        const bool some = drafts || left < kTile;
+        auto seen = [&](int h) {
+          const int n = left - 32 * h;
+          const uint32_t have = n >= 32 ? 0xffffffffu : (1u << n) - 1u;  // (n > 0: works(h))
+          return drafts ? have & (h == 0 ? see[0] : h == 1 ? see[1] : h == 2 ? see[2] : see[3]) : have;
+        };
+        const int ti = BF ? 0 : sh.te[par];
+        const float te = (float)ti;
+        // the 32 columns that this copy works on, where any count
+        auto works = [&](int h) { return (h * copies) / 4 == copy && 32 * h < left; };
+        // u = the scores of 32 columns less m, from their raw products, where they count
+        auto exponents = [&](float (&u)[32], int h, float ms, bool masks) {
+          float4 k4[BF ? 1 : 8];
+          tmem_ld32(tw + 32 * h, *reinterpret_cast<uint32_t(*)[32]>(&u));
+          if constexpr (!BF)
 #pragma unroll
-          for (int h = 0; h < 4; ++h) {
-            const int n = (tile < ndr ? w.cnt : w.len - (tile - ndr) * kTile) - 32 * h;
-            uint32_t have = n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u;
-            if (tile < ndr) {
-              if (!in || n <= 0)
-                have = 0;
-              else if (a.mask)
-                have &= a.mask[((size_t)w.b * a.T + t) * a.words + h];
-              else
-                have &= t >= 32 * h + 31 ? 0xffffffffu : t < 32 * h ? 0u : (2u << (t - 32 * h)) - 1u;
-            }
-            see[h] = have;
-          }
-        // 1. scores (over the raw products where they differ) and their maximum
-        float mx = -INFINITY;
-        const uint64_t cc = pack_f32x2(c1, c1);
-#pragma unroll
-        for (int h = 0; h < 4; ++h) {
-          uint32_t s[32];
-          tmem_ld32(tw + 32 * h, s);
+            for (int j = 0; j < 8; ++j) k4[j] = *reinterpret_cast<const float4 *>(&sh.sk[par][32 * h + 4 * j]);
           tmem_ld_wait();
-          float *y = reinterpret_cast<float *>(s);
-          if constexpr (!BF) {
+          if (!BF && own)
 #pragma unroll
-            for (int j = 0; j < 32; j += 4) {
-              const float4 k4 = *reinterpret_cast<const float4 *>(&sh.sk[par][32 * h + j]);
-              const float4 g4 = *reinterpret_cast<const float4 *>(&sh.lg[par][32 * h + j]);
-              uint64_t u = fma_f32x2(mul_f32x2(pack_f32x2(y[j], y[j + 1]), cc), pack_f32x2(k4.x, k4.y), pack_f32x2(g4.x, g4.y));
-              unpack_f32x2(u, y[j], y[j + 1]);
-              u = fma_f32x2(mul_f32x2(pack_f32x2(y[j + 2], y[j + 3]), cc), pack_f32x2(k4.z, k4.w), pack_f32x2(g4.z, g4.w));
-              unpack_f32x2(u, y[j + 2], y[j + 3]);
-            }
-          }
-          if (some)
-#pragma unroll
-            for (int j = 0; j < 32; ++j) y[j] = see[h] >> j & 1 ? y[j] : -INFINITY;
-#pragma unroll
-          for (int j = 0; j < 32; j += 2) mx = fmaxf(mx, fmaxf(y[j], y[j + 1]));
-          if (!BF || some) tmem_st32(tw + 32 * h, s);
-        }
-        if (BF) mx = mx == -INFINITY ? mx : mx * c1;
-        if (__any_sync(0xffffffffu, mx > m + kRaise)) {
-          const float mn = fmaxf(m, mx), al = mn == -INFINITY ? 1.f : ex2(m - mn);
-          l *= al;
-          m = mn;
-          if (i > 0)  // P V of the tiles before is complete (S was issued after it)
-#pragma unroll 1
-            for (int h = 0; h < HD / 32; ++h) {
-              uint32_t o[32];
-              tmem_ld32(tw + 128 + 32 * h, o);
-              tmem_ld_wait();
-#pragma unroll
-              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * al);
-              tmem_st32(tw + 128 + 32 * h, o);
-            }
-        }
-        tmem_st_wait();
-        // 2. probabilities
-        const float ms = m == -INFINITY ? 0.f : m;
-        uint64_t sum = 0;
-        const uint64_t mm = pack_f32x2(-ms, -ms), by = BF ? cc : pack_f32x2(1.f, 1.f);
-#pragma unroll
-        for (int h = 0; h < 4; ++h) {
-          uint32_t s[32], p[16];
-          tmem_ld32(tw + 32 * h, s);
-          tmem_ld_wait();
-          const float *y = reinterpret_cast<const float *>(s);
+            for (int j = 0; j < 32; ++j) u[j] *= c1;
+          const uint64_t mm = pack_f32x2(ms, ms), cc = pack_f32x2(c1, c1);
 #pragma unroll
           for (int j = 0; j < 32; j += 4) {
-            float4 r4 = make_float4(1.f, 1.f, 1.f, 1.f);
-            if (!BF) r4 = *reinterpret_cast<const float4 *>(&sh.rs[par][32 * h + j]);
-            float e[4];
-            uint64_t u = fma_f32x2(pack_f32x2(y[j], y[j + 1]), by, mm);
-            unpack_f32x2(u, e[0], e[1]);
-            u = fma_f32x2(pack_f32x2(y[j + 2], y[j + 3]), by, mm);
-            unpack_f32x2(u, e[2], e[3]);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) e[k] = ex2(e[k]);
-            sum = fma_f32x2(pack_f32x2(e[0], e[1]), pack_f32x2(r4.x, r4.y), sum);
-            sum = fma_f32x2(pack_f32x2(e[2], e[3]), pack_f32x2(r4.z, r4.w), sum);
-            p[j / 2] = BF ? pack_bf2(e[0], e[1]) : pack_h2(e[0], e[1]);
-            p[j / 2 + 1] = BF ? pack_bf2(e[2], e[3]) : pack_h2(e[2], e[3]);
+            uint64_t k0 = cc, k1 = cc;
+            if constexpr (!BF) k0 = pack_f32x2(k4[j / 4].x, k4[j / 4].y), k1 = pack_f32x2(k4[j / 4].z, k4[j / 4].w);
+            unpack_f32x2(fma_f32x2(pack_f32x2(u[j], u[j + 1]), k0, mm), u[j], u[j + 1]);
+            unpack_f32x2(fma_f32x2(pack_f32x2(u[j + 2], u[j + 3]), k1, mm), u[j + 2], u[j + 3]);
           }
+          if (masks && some) {
+            const uint32_t bits = seen(h);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) u[j] = bits >> j & 1 ? u[j] : -INFINITY;
+          }
+        };
+        auto largest = [&](const float (&u)[32]) {
+          float top[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            top[j] = fmaxf(u[j], u[j + 4]);
+#pragma unroll
+            for (int e = 8; e < 32; e += 8) top[j] = fmaxf(fmaxf(top[j], u[j + e]), u[j + e + 4]);
+          }
+          return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        };
+        // 32 columns at a time: probabilities with the row's maximum so far.  Where a row's 32 add up to 2^8 (or it
+        // has no maximum yet), the maximum is raised first, to a whole number, so that what was computed with the
+        // old one is rescaled by exact powers of two.
+        float total = 0.f;
+        auto probabilities = [&](int h, bool masks) {
+          float u[32], part = 0.f;
+          uint32_t p[16];
+          const float ms = m == -INFINITY ? 0.f : te - m;
+          exponents(u, h, ms, masks);
+#pragma unroll 1
+          for (int again = 0; again < 2; ++again) {
+            uint64_t sum[2] = {0, 0};
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+              const float e0 = ex2(u[j]), e1 = ex2(u[j + 1]);
+              sum[j / 2 % 2] = add_f32x2(sum[j / 2 % 2], pack_f32x2(e0, e1));
+              p[j / 2] = BF ? pack_bf2(e0, e1) : pack_h2(e0, e1);
+            }
+            float s0, s1;
+            unpack_f32x2(add_f32x2(sum[0], sum[1]), s0, s1);
+            part = s0 + s1;
+            const bool up = part >= 256.f || (m == -INFINITY && part > 0.f);
+            if (again || !__any_sync(0xffffffffu, up)) break;
+            const float mn = up ? ceilf(largest(u) - ms + te) : m;
+            const float al = raise_factor(m, mn);
+            rescale<BF>(tw, h, i > 0 ? HD / 16 : 0, al);
+            m = mn;
+            l *= al;
+            total *= al;
+            const float now = m == -INFINITY ? 0.f : te - m;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) u[j] += now - ms;
+          }
+          total += part;
           // columns 16 h ..: S's there have been read
           tmem_st16(tw + 16 * h, p);
+        };
+        if (i >= 2 && copies == 1 && !some) {
+          // four times in a row: a row's work is bound by latency, which the next columns' loads then overlap
+#pragma unroll
+          for (int h = 0; h < 4; ++h) probabilities(h, false);
+        } else {
+          // A range's first two tiles (the drafts', the context's first) set the maximum from all their scores.
+          if (i < 2) {
+            float mx = -INFINITY;
+#pragma unroll 1
+            for (int h = 0; h < 4; ++h) {
+              if (!works(h)) continue;
+              float u[32];
+              exponents(u, h, te, true);
+              mx = fmaxf(mx, largest(u));
+            }
+            if (__any_sync(0xffffffffu, mx > m)) {
+              const float mn = fmaxf(m, ceilf(mx)), al = raise_factor(m, mn);
+              if (i > 0 && __any_sync(0xffffffffu, al != 1.f && m > -INFINITY)) rescale<BF>(tw, 0, HD / 16, al);
+              m = mn;
+              l *= al;
+            }
+          }
+#pragma unroll 1
+          for (int h = 0; h < 4; ++h) {
+            if (works(h)) {
+              probabilities(h, true);
+            } else {
+              const uint32_t none[16] = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
+              tmem_st16(tw + 16 * h, none);
+            }
+          }
         }
-        float l0, l1;
-        unpack_f32x2(sum, l0, l1);
-        l += l0 + l1;
+        l = fmaf(total, BF ? 1.f : pow2i(-ti), l);  // p stands for 2^-t of itself
         tmem_st_wait();
       }
       tc_fence_before();
@@ -657,61 +808,92 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
     }
     if (ok) ok = wait(&sh.v_empty, (nt - 1) & 1);
     if (!ok && lane == 0) sh.fail = 1;
+    ok = barrier_and(2, 128, ok);
     tc_fence_after();
-    if (busy && ok) {
-      // ---- the row's output, or its partial result
-      const bool whole = w.n == 1, none = m == -INFINITY && l == 0.f;  // (all scores NaN: l is NaN)
-      const float inv = whole ? (none ? 0.f : 1.f / l) : 1.f;
-      const bool odd = w.t0 < ndr && (sh.odd[0] | sh.odd[1] | sh.odd[2] | sh.odd[3]) != 0;
-      float *pt = a.part + ((size_t)w.slot * a.part_rows + tid) * (HD + 2);
-      __nv_bfloat16 *o = reinterpret_cast<__nv_bfloat16 *>(a.o) +
-                         (((size_t)w.b * a.T + t) * a.H + w.g * rep + r % rep) * HD;
+    if (ok) {
+      // ---- the rows' outputs, or their partial results, over shared memory (Q's and K's place): row tid's 16-byte
+      // chunk c at c ^ (tid % chunks), so that neither rows nor chunks meet in a bank
+      constexpr int CK = HD / 4;
+      float4 *stage = reinterpret_cast<float4 *>(qbuf);
+      if (busy) {
 #pragma unroll 1
-      for (int h = 0; h < HD / 32; ++h) {
-        uint32_t v[32];
-        tmem_ld32(tw + 128 + 32 * h, v);
-        tmem_ld_wait();
-        if (!in) continue;
+        for (int h = 0; h < HD / 32; ++h) {
+          uint32_t v[32];
+          tmem_ld32(tw + 128 + 32 * h, v);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            stage[tid * CK + ((8 * h + j) ^ (tid & (CK - 1)))] =
+                make_float4(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1]), __uint_as_float(v[4 * j + 2]),
+                            __uint_as_float(v[4 * j + 3]));
+        }
+      }
+      float *sm = sh.sk[0], *sl = sh.sk[1];
+      sm[tid] = m;
+      sl[tid] = l;
+      named_barrier_sync(2, 128);
+      const bool whole = w.n == 1;
+      const bool odd = w.t0 < ndr && (sh.odd[0] | sh.odd[1] | sh.odd[2] | sh.odd[3]) != 0;
+      // CK lanes a row
+      const int c = tid % CK;
+#pragma unroll 4
+      for (int lrow = tid / CK; lrow < live; lrow += 128 / CK) {
+        float M = sm[lrow], L = sl[lrow];
+        float4 o = stage[lrow * CK + (c ^ (lrow & (CK - 1)))];
+        if (copies > 1) {
+#pragma unroll 1
+          for (int k = 1; k < copies; ++k) M = fmaxf(M, sm[k * rpc + lrow]);
+          float f = sm[lrow] == -INFINITY ? 0.f : ex2(sm[lrow] - M);  // (a NaN of a copy stays NaN)
+          L *= f;
+          o.x *= f, o.y *= f, o.z *= f, o.w *= f;
+#pragma unroll 1
+          for (int k = 1; k < copies; ++k) {
+            const int row = k * rpc + lrow;
+            f = sm[row] == -INFINITY ? 0.f : ex2(sm[row] - M);
+            const float4 x = stage[row * CK + (c ^ (row & (CK - 1)))];
+            L = fmaf(sl[row], f, L);
+            o.x = fmaf(x.x, f, o.x), o.y = fmaf(x.y, f, o.y), o.z = fmaf(x.z, f, o.z), o.w = fmaf(x.w, f, o.w);
+          }
+        }
+        const int ro = row0 + lrow, to = draft_of(ro);
         if (odd) {
 #pragma unroll 1
           for (int j = 0; j < w.cnt; ++j) {
             if (!(sh.odd[j / 32] >> (j % 32) & 1)) continue;
-            const bool see = a.mask ? a.mask[((size_t)w.b * a.T + t) * a.words + j / 32] >> (j % 32) & 1 : j <= t;
-            if (!see) continue;
+            if (!(a.mask ? a.mask[((size_t)w.b * a.T + to) * a.words + j / 32] >> (j % 32) & 1 : j <= to)) continue;
             const __nv_bfloat16 *vj = reinterpret_cast<const __nv_bfloat16 *>(a.vn) +
-                                      (((size_t)w.b * a.T + j) * a.Hkv + w.g) * HD + 32 * h;
+                                      (((size_t)w.b * a.T + j) * a.Hkv + w.g) * HD + 4 * c;
+            float f[4];
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const float f = __bfloat162float(vj[e]);
-              if (!isfinite(f)) v[e] = __float_as_uint(__uint_as_float(v[e]) + f);
+            for (int e = 0; e < 4; ++e) {
+              f[e] = __bfloat162float(vj[e]);
+              f[e] = isfinite(f[e]) ? 0.f : f[e];
             }
+            o.x += f[0], o.y += f[1], o.z += f[2], o.w += f[3];
           }
         }
         if (whole) {
-#pragma unroll
-          for (int e = 0; e < 32; e += 8) {
-            uint32_t u[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              u[k] = none ? 0u : pack_bf2(__uint_as_float(v[e + 2 * k]) * inv, __uint_as_float(v[e + 2 * k + 1]) * inv);
-            *reinterpret_cast<uint4 *>(o + 32 * h + e) = make_uint4(u[0], u[1], u[2], u[3]);
-          }
+          const bool none = M == -INFINITY && L == 0.f;  // (all scores NaN: L is NaN)
+          const float inv = none ? 0.f : 1.f / L;
+          *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(a.o) +
+                                     (((size_t)w.b * a.T + to) * a.H + w.g * rep + ro - to * rep) * HD + 4 * c) =
+              none ? make_uint2(0, 0) : make_uint2(pack_bf2(o.x * inv, o.y * inv), pack_bf2(o.z * inv, o.w * inv));
         } else {
-#pragma unroll
-          for (int e = 0; e < 32; e += 2)
-            *reinterpret_cast<float2 *>(pt + 32 * h + e) = make_float2(__uint_as_float(v[e]), __uint_as_float(v[e + 1]));
+          float *pt = a.part + ((size_t)w.slot * a.part_rows + lrow) * (HD + 4);
+          *reinterpret_cast<float4 *>(pt + 4 * c) = o;
+          if (c == 0) *reinterpret_cast<float2 *>(pt + HD) = make_float2(M, L);
         }
       }
-      if (in && !whole) *reinterpret_cast<float2 *>(pt + HD) = make_float2(m, l);
     }
   }
   // rows of drafts that do not exist: 0, by the last row block's first split
   if (w.any && w.split == 0 && w.cnt * rep - row0 <= kTcRows) {
     const int z0 = max(row0, w.cnt * rep);
+#pragma unroll 1
     for (int i = z0 * (HD / 8) + tid; i < R * (HD / 8); i += kTcThreads) {
-      const int row = i / (HD / 8), e = i % (HD / 8);
+      const int row = i / (HD / 8), e = i % (HD / 8), to = draft_of(row);
       *reinterpret_cast<uint4 *>(reinterpret_cast<__nv_bfloat16 *>(a.o) +
-                                 (((size_t)w.b * a.T + row / rep) * a.H + w.g * rep + row % rep) * HD + 8 * e) =
+                                 (((size_t)w.b * a.T + to) * a.H + w.g * rep + row - to * rep) * HD + 8 * e) =
           make_uint4(0, 0, 0, 0);
     }
   }
@@ -730,62 +912,51 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
   }
 }
 
-// o of the rows whose block was split: a warp a row, its parts in split order.
+// o of the rows whose block was split: HD / 4 lanes a row, its parts in split order.
 template <int HD>
 __global__ void __launch_bounds__(256) attn_tree_merge_kernel(const TreeArgs a) {
-  constexpr int E = HD / 32, CU = 4;
+  constexpr int LPR = HD / 4, CU = 8;  // splits loaded in one round trip
+  const int rep = a.H / a.Hkv, R = a.T * rep;
+  const long long row = (long long)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+  const int c = threadIdx.x % LPR;
+  const int bg = (int)(row / R), r = (int)(row - (long long)bg * R), b = bg / a.Hkv, g = bg % a.Hkv;
   pdl_wait();
   pdl_launch_dependents();
-  const int lane = threadIdx.x & 31, rep = a.H / a.Hkv, R = a.T * rep;
-  const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
   if (row >= (long long)a.batch * a.Hkv * R) return;
-  const int bg = (int)(row / R), r = (int)(row - (long long)bg * R), b = bg / a.Hkv, g = bg % a.Hkv;
-  const int2 tab = a.table[b];
-  int len, cnt, tiles, blocks;
-  seq_tiles(a, b, rep, len, cnt, tiles, blocks);
-  if (tab.y <= 1 || r >= cnt * rep) return;  // written by the first kernel, or skipped
-  const size_t step = (size_t)a.Hkv * blocks * a.part_rows * (HD + 2);
-  const float *pt = a.part + ((size_t)(tab.x + g * blocks + r / kTcRows) * a.part_rows + r % kTcRows) * (HD + 2);
-  float M = -INFINITY, L = 0.f, O[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) O[e] = 0.f;
+  const int4 tab = a.table[b];  // first range, splits, row blocks, drafts
+  if (tab.y <= 1 || r >= tab.w * rep) return;  // written by the first kernel, or skipped
+  const size_t step = (size_t)a.Hkv * tab.z * a.part_rows * (HD + 4);
+  const float *pt = a.part + ((size_t)(tab.x + g * tab.z + r / kTcRows) * a.part_rows + r % kTcRows) * (HD + 4);
+  float M = -INFINITY, L = 0.f;
+  float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int s0 = 0; s0 < tab.y; s0 += CU) {
-    float2 ml[CU], ov[CU][E / 2];
+    float2 ml[CU];
+    float4 ov[CU];
     float mn = M;
 #pragma unroll
-    for (int c = 0; c < CU; ++c) {
-      const float *ps = pt + (size_t)(s0 + c) * step;
-      const bool in = s0 + c < tab.y;
-      ml[c] = in ? *reinterpret_cast<const float2 *>(ps + HD) : make_float2(-INFINITY, 0.f);
-#pragma unroll
-      for (int e = 0; e < E / 2; ++e)
-        ov[c][e] = in ? *reinterpret_cast<const float2 *>(ps + lane * E + 2 * e) : make_float2(0.f, 0.f);
+    for (int j = 0; j < CU; ++j) {
+      const float *ps = pt + (size_t)(s0 + j) * step;
+      const bool in = s0 + j < tab.y;
+      ml[j] = in ? *reinterpret_cast<const float2 *>(ps + HD) : make_float2(-INFINITY, 0.f);
+      ov[j] = in ? *reinterpret_cast<const float4 *>(ps + 4 * c) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
 #pragma unroll
-    for (int c = 0; c < CU; ++c) mn = fmaxf(mn, ml[c].x);
+    for (int j = 0; j < CU; ++j) mn = fmaxf(mn, ml[j].x);
     const float f0 = M == -INFINITY ? 0.f : ex2(M - mn);
     M = mn;
     L *= f0;
+    O.x *= f0, O.y *= f0, O.z *= f0, O.w *= f0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) O[e] *= f0;
-#pragma unroll
-    for (int c = 0; c < CU; ++c) {
-      if (s0 + c >= tab.y) break;
-      const float f = ml[c].x == -INFINITY ? 0.f : ex2(ml[c].x - M);  // (a NaN of a part stays NaN)
-      L = fmaf(ml[c].y, f, L);
-#pragma unroll
-      for (int e = 0; e < E / 2; ++e) {
-        O[2 * e] = fmaf(ov[c][e].x, f, O[2 * e]);
-        O[2 * e + 1] = fmaf(ov[c][e].y, f, O[2 * e + 1]);
-      }
+    for (int j = 0; j < CU; ++j) {
+      const float f = ml[j].x == -INFINITY ? 0.f : ex2(ml[j].x - M);  // (a NaN of a part stays NaN)
+      L = fmaf(ml[j].y, f, L);
+      O.x = fmaf(ov[j].x, f, O.x), O.y = fmaf(ov[j].y, f, O.y), O.z = fmaf(ov[j].z, f, O.z), O.w = fmaf(ov[j].w, f, O.w);
     }
   }
   const bool none = M == -INFINITY && L == 0.f;
-  __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(a.o) +
-                       (((size_t)b * a.T + r / rep) * a.H + g * rep + r % rep) * HD + lane * E;
-#pragma unroll
-  for (int e = 0; e < E / 2; ++e)
-    reinterpret_cast<uint32_t *>(dst)[e] = none ? 0u : pack_bf2(O[2 * e] / L, O[2 * e + 1] / L);
+  *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(a.o) +
+                             (((size_t)b * a.T + r / rep) * a.H + g * rep + r % rep) * HD + 4 * c) =
+      none ? make_uint2(0, 0) : make_uint2(pack_bf2(O.x / L, O.y / L), pack_bf2(O.z / L, O.w / L));
 }
 
 namespace {
@@ -828,7 +999,7 @@ cudaError_t launch_tree_tc_t(const TreeArgs &a, unsigned grid, bool merge, cudaS
   e = cudaLaunchKernelEx(&cfg, attn_tree_tc_kernel<HD, BITS>, a);
   if (e != cudaSuccess || !merge) return e;
   const long long rows = (long long)a.batch * a.H * a.T;
-  cfg.gridDim = dim3((unsigned)((rows + 7) / 8));
+  cfg.gridDim = dim3((unsigned)((rows * (HD / 4) + 255) / 256));
   cfg.blockDim = dim3(256);
   cfg.dynamicSmemBytes = 0;
   return cudaLaunchKernelEx(&cfg, attn_tree_merge_kernel<HD>, a);
@@ -844,7 +1015,7 @@ size_t tree_tc_part_floats(int batch, int T, int H, int Hkv, int hd, int max_len
   const long long rows = std::min((long long)T * (H / Hkv), (long long)kTcRows);
   const long long tiles = ((long long)max_len + kTile - 1) / kTile + (T + kTile - 1) / kTile;
   const long long blocks = ((long long)T * (H / Hkv) + kTcRows - 1) / kTcRows;
-  return (size_t)(std::min((long long)tree_tc_target(num_sms), (long long)batch * Hkv * blocks * tiles) * rows * (hd + 2));
+  return (size_t)(std::min((long long)tree_tc_target(num_sms), (long long)batch * Hkv * blocks * tiles) * rows * (hd + 4));
 }
 
 cudaError_t launch_attn_tree_tc(TreeArgs a, int hd, int bits, int num_sms, cudaStream_t s) {
@@ -854,6 +1025,7 @@ cudaError_t launch_attn_tree_tc(TreeArgs a, int hd, int bits, int num_sms, cudaS
   a.target = tree_tc_target(num_sms);
   a.min_tiles = 1;
   a.part_rows = std::min(a.T * rep, kTcRows);
+  a.rep_magic = (65536 + rep - 1) / rep;  // row / rep = row rep_magic >> 16 for row < 65536 / (rep - 1)
   const long long tiles = ((long long)a.max_len + kTile - 1) / kTile + (a.T + kTile - 1) / kTile;
   const unsigned grid = (unsigned)std::max(blocks, std::min((long long)a.target, blocks * tiles));
   const bool merge = blocks < a.target && tiles > a.min_tiles;  // else every row block is one range
