@@ -300,7 +300,6 @@ struct Shared {
   // of a tile: K's scales (times the score scale and the queries' 2^-kQueryShift) and the exponent t of V's operands, which are values
   // times 2^-t.  Two tiles of each: the next tile's are written while this one's are read
   __align__(16) float sk[2][kTile];
-  float c1[kTcRows];                         // of a row's scores
   int te[2];
   uint32_t zk[kTile];                        // 1024 + z of K, twice
   __align__(16) uint2 zsv[kTile];            // 1024 + z of V, twice; its scale times 2^-t, twice
@@ -640,36 +639,35 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
       }
       cp_async_wait_all();
       __syncwarp();
-      if (!BF || a.scale < 0.f) {
+      // thread = row
+      auto chunk = [&](int c) { return reinterpret_cast<uint4 *>(qbuf + (c / 8) * kBlk + tid * 128 + (((c & 7) ^ (tid & 7)) << 4)); };
+      if constexpr (BF) {
+        if (a.scale < 0.f)
 #pragma unroll 4
-        for (int row = warp * 32 + lane / C::CH; row < warp * 32 + 32; row += RI) {
-          uint4 *at = reinterpret_cast<uint4 *>(place(row));
-          uint4 v = *at;
-          if constexpr (BF) {
-            v.x ^= 0x80008000u, v.y ^= 0x80008000u, v.z ^= 0x80008000u, v.w ^= 0x80008000u;
-          } else {
-            // the largest |q| of the row, as bf16 bits
-            uint32_t mx = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
-            mx = max(mx & 0xffffu, mx >> 16);
-#pragma unroll
-            for (int o = C::CH / 2; o >= 1; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-            const int e = (int)(mx >> 7) - 127;
-            int mine = kQueryShift;
-            if (mx != 0 && (e < -4 || e >= 8)) mine = max(min(min(126, 14 - e), kQueryShift + 126), -114);
-            const float f = pow2i(mine);
-            v.x = pack_h2(bf_lo(v.x) * f, bf_hi(v.x) * f);
-            v.y = pack_h2(bf_lo(v.y) * f, bf_hi(v.y) * f);
-            v.z = pack_h2(bf_lo(v.z) * f, bf_hi(v.z) * f);
-            v.w = pack_h2(bf_lo(v.w) * f, bf_hi(v.w) * f);
-            if (ch == 0) sh.c1[row] = pow2i(kQueryShift - mine);
+          for (int c = 0; c < C::CH; ++c) {
+            uint4 v = *chunk(c);
+            *chunk(c) = make_uint4(v.x ^ 0x80008000u, v.y ^ 0x80008000u, v.z ^ 0x80008000u, v.w ^ 0x80008000u);
           }
-          *at = v;
+      } else {
+        uint32_t big = 0;  // the row's largest |q|, as bf16 bits
+#pragma unroll
+        for (int c = 0; c < C::CH; ++c) {
+          const uint4 v = *chunk(c);
+          big = __vmaxu2(big, __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu)));
         }
-      }
-      if constexpr (!BF) {
-        __syncwarp();
-        c1 = sh.c1[tid];
+        big = max(big & 0xffffu, big >> 16);
+        const int e = (int)(big >> 7) - 127;
+        int mine = kQueryShift;
+        if (big != 0 && (e < -4 || e >= 8)) mine = max(min(min(126, 14 - e), kQueryShift + 126), -114);
+        c1 = pow2i(kQueryShift - mine);
+        const float f = pow2i(mine);
         own = __any_sync(0xffffffffu, c1 != 1.f);
+#pragma unroll 4
+        for (int c = 0; c < C::CH; ++c) {
+          const uint4 v = *chunk(c);
+          *chunk(c) = make_uint4(pack_h2(bf_lo(v.x) * f, bf_hi(v.x) * f), pack_h2(bf_lo(v.y) * f, bf_hi(v.y) * f),
+                                 pack_h2(bf_lo(v.z) * f, bf_hi(v.z) * f), pack_h2(bf_lo(v.w) * f, bf_hi(v.w) * f));
+        }
       }
     }
     hand_over(&sh.p_full);  // phase 0: Q
