@@ -1474,7 +1474,22 @@ wq_status wq_decoder_layer_forward(const void *x, int batch, const int32_t *lens
 namespace {
 
 constexpr int kMaxDrafts = 128;
-constexpr int kTreeMmaRows = 16;  // rows (drafts x query heads of a kv head) of one m16 tile; above, tcgen05
+
+// Which of the two tree-attention kernels a call takes.  The mma.sync kernel starts in 6 to 10 us and takes 16 rows
+// (drafts x query heads of a kv head) at a time, so its time grows with positions x 16-row tiles; the tcgen05 kernel
+// takes 11 to 15 us for one tile a CTA, and its 128 rows cost what one costs.  Both measured over 1 to 16 sequences of
+// 256 to 32768 positions, 4 to 512 rows, heads of 128 and 64 (us, mma.sync / tcgen05): the lengths being known on the
+// device alone, the bound is on the cache's positions.
+//   heads of 128, bf16:   131k (32 rows, 1 x 8192) 19.0 / 25.3, 262k (32 rows, 16 x 1024) 33.5 / 23.1, 262k (16 rows,
+//                         1 x 32768) 32.4 / 39.8, 524k (16 rows, 16 x 4096) 48.9 / 41.3
+//   heads of 128, 8 bits: 262k (64 rows, 1 x 8192) 25.9 / 30.7, 524k (32 rows, 4 x 8192) 36.9 / 33.0, 524k (16 rows,
+//                         16 x 4096) 41.4 / 46.3
+//   heads of 64, bf16:    262k (64 rows, 4 x 2048) 14.3 / 16.1, 524k (128 rows, 4 x 2048) 26.0 / 17.6
+bool tree_on_tcgen05(int batch, int T, int H, int Hkv, int hd, int bits, int max_len) {
+  const long long tiles = ((long long)T * (H / Hkv) + 15) / 16;
+  const double work = (double)tiles * batch * Hkv * max_len;
+  return work > (tiles == 1 ? 400e3 : 250e3) * (bits == 16 ? 1.0 : 1.25) * (hd == 64 ? 1.5 : 1.0);
+}
 
 wq_status check_cache(const wq_kv_cache *c) {
   if (!c) return fail(WQ_ERR_ARG, "null wq_kv_cache");
@@ -1531,10 +1546,11 @@ wq_status attn_tree_impl(const void *q, const void *k_new, const void *v_new, in
   a.part = reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + up256(sizeof(int4) * (size_t)c->batch));
   a.o = o;
   cudaError_t e;
-  if (scale != 0.f && n_draft * (n_heads / c->n_kv) > kTreeMmaRows) {
+  if (scale != 0.f && tree_on_tcgen05(c->batch, n_draft, n_heads, c->n_kv, c->head_dim, c->bits, c->max_len)) {
     e = launch_attn_tree_tc(a, c->head_dim, c->bits, sms, s);
   } else {
     a.S = tree_splits(c->batch, n_draft, n_heads, c->n_kv, c->max_len, sms);
+    a.cluster = tree_cluster(c->batch, n_draft, n_heads, c->n_kv, a.S, sms);
     e = launch_attn_tree(a, c->head_dim, c->bits, s);
   }
   if (e != cudaSuccess) return cuda_fail(e, "tree attention launch");

@@ -56,7 +56,7 @@ struct TreeArgs {
   float scale;                  // of the scores, times log2(e)
   float *part;                  // [batch Hkv][rows][S][HD + 2] (S > 1)
   void *o;                      // bf16 [batch][T][H][HD]
-  int S;
+  int S, cluster;               // splits of the context; whether they are a cluster
   // tcgen05 kernel: ranges of tiles wanted, least tiles a range, rows of a range's
   // partial results, and per sequence its first range, splits, row blocks and drafts
   int target, min_tiles, part_rows, rep_magic;
@@ -64,6 +64,7 @@ struct TreeArgs {
 };
 // Splits of the context a launch takes, and its partial results in floats.
 int tree_splits(int batch, int T, int H, int Hkv, int max_len, int num_sms);
+bool tree_cluster(int batch, int T, int H, int Hkv, int S, int num_sms);
 size_t tree_part_floats(int batch, int T, int H, int Hkv, int hd, int max_len, int num_sms);
 cudaError_t launch_attn_tree(const TreeArgs &a, int hd, int bits, cudaStream_t s);
 cudaError_t read_tree_status(int *status);

@@ -18,20 +18,24 @@
 // (binary16) or 2^-8 (bf16) of each term at most, of either sign; the bf16 store of
 // o costs as much of their sum.
 //
-// A CTA of 4 warps takes one (b, g), 16 rows and one split of the context; each
-// warp takes chunks of 16 (4 bits: 32) positions with mma.sync m16n8k16, rows as
-// M.  Codes go from global memory to the MMA fragments through registers alone:
-// the contraction over HD and the order of V's columns are free, so a lane takes
-// 16 consecutive bytes of its position's row, and two prmt or and-or build the
-// binary16 value 1024 + code, from which 1024 + z is subtracted (exact).  The
-// next chunk's K is loaded when the current one's has been converted, V likewise.
-// The drafts' chunks run first, in bf16.  The splits' partial results are merged
-// in a fixed order by a second kernel (none with one split).
+// A CTA of 4 warps takes one (b, g), 16 rows and one split of the context, in tiles
+// of 64 positions that bulk copies bring into a ring of 64 KB of shared memory; a
+// warp takes 16 positions of a tile with mma.sync m16n8k16, rows as M.  Codes go
+// from there to the MMA fragments through registers alone: the contraction over HD
+// and the order of V's columns are free, so a lane takes 16 consecutive bytes of its
+// position's row, and two prmt or and-or build the binary16 value 1024 + code, from
+// which 1024 + z is subtracted (exact).  The drafts' chunks run first, in bf16,
+// straight from global memory, while the first tiles are on their way.  Few
+// splits are a cluster, whose CTAs add up the splits' results (each a share of the
+// rows) from one another's shared memory; else a second kernel does.  Both add in a
+// fixed order.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
+#include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cstdint>
 
 #include "wq_internal.h"
@@ -40,14 +44,20 @@
 
 namespace wq {
 
-// Status word: WQ_OK (0), or WQ_ERR_ARG (-1) after a length outside [0,
-// max_len] or a count outside [0, T] was met (that sequence is skipped).
+namespace cg = cooperative_groups;
+
+// Status word: WQ_OK (0), WQ_ERR_ARG (-1) after a length outside [0, max_len] or a
+// count outside [0, T] was met (that sequence is skipped), WQ_ERR_TIMEOUT (-6)
+// after a wait ran out.
 __device__ int g_tree_status = 0;
 
 namespace {
 
 constexpr int kTreeWarps = 4;
-constexpr int kRows = 16;  // rows a CTA takes
+constexpr int kRows = 16;     // rows a CTA takes
+constexpr int kTreeTile = 64;  // positions a tile
+constexpr int kRing = 65536;   // bytes of the ring at most
+constexpr int kTreeCluster = 8;  // splits that a cluster can be
 
 __device__ __forceinline__ uint32_t pack_bf2(float a, float b) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
@@ -74,13 +84,13 @@ template <int N>
 __device__ __forceinline__ void load_words(uint32_t (&w)[N], const void *p) {
   static_assert(N == 1 || N == 2 || N == 4, "");
   if constexpr (N == 4) {
-    const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p));
+    const uint4 v = *reinterpret_cast<const uint4 *>(p);
     w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
   } else if constexpr (N == 2) {
-    const uint2 v = __ldg(reinterpret_cast<const uint2 *>(p));
+    const uint2 v = *reinterpret_cast<const uint2 *>(p);
     w[0] = v.x, w[1] = v.y;
   } else {
-    w[0] = __ldg(reinterpret_cast<const uint32_t *>(p));
+    w[0] = *reinterpret_cast<const uint32_t *>(p);
   }
 }
 
@@ -94,6 +104,10 @@ struct Lay {
   static constexpr int VW = ROW / 8 >= 16 ? 4 : ROW / 32, VI = ROW / (32 * VW);
   static constexpr int KS = HD / 16;                            // MMA steps along HD
   static constexpr int NJ = HD / 8;                             // 8-column tiles of the output
+  static constexpr int STAGE = 2 * kTreeTile * ROW;             // bytes of a tile
+  static constexpr int NS = kRing / STAGE < 8 ? kRing / STAGE : 8;
+  static constexpr int OUT = kTreeWarps * kRows * (HD + 4) * 4; // the warps' results, over the ring
+  static constexpr int SMEM = NS * STAGE > OUT ? NS * STAGE : OUT;
   // first of the four values that lane t gives MMA step ks
   static __device__ __forceinline__ int q_at(int ks, int t) {
     constexpr int PER = KW * 4 * 8 / BITS;                      // values a piece
@@ -144,6 +158,23 @@ __device__ __forceinline__ uint32_t v_frag(const uint32_t (&wa)[Lay<HD, BITS>::V
   }
 }
 
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ float lg2(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rcp(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // What a warp accumulates: rows gr and gr + 8 of its 16, columns v_at(j, 2 tc),
 // v_at(j, 2 tc + 1); m the rows' maximum of y, l this lane's part of their sums.
 template <int HD>
@@ -161,28 +192,28 @@ __device__ __forceinline__ void softmax_step(Acc<HD> &acc, float (&y)[NT][4]) {
   for (int u = 0; u < NT; ++u)
 #pragma unroll
     for (int e = 0; e < 4; ++e) mc[e / 2] = fmaxf(mc[e / 2], y[u][e]);
-  float ms[2], al[2];
+  // Nothing is rescaled until a score passes its row's maximum so far by 2^8 (p stays below that)
+  if (__any_sync(0xffffffffu, mc[0] > acc.m[0] + 8.f || mc[1] > acc.m[1] + 8.f)) {
+    float al[2];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    mc[i] = fmaxf(mc[i], __shfl_xor_sync(0xffffffffu, mc[i], 1));
-    mc[i] = fmaxf(mc[i], __shfl_xor_sync(0xffffffffu, mc[i], 2));
-    const float mn = fmaxf(acc.m[i], mc[i]);
-    ms[i] = mn == -INFINITY ? 0.f : mn;
-    al[i] = exp2f(acc.m[i] - ms[i]);  // 0 at first (m = -inf)
-    acc.m[i] = mn;
-  }
-  if (__any_sync(0xffffffffu, al[0] != 1.f || al[1] != 1.f)) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) acc.l[i] *= al[i];
+    for (int i = 0; i < 2; ++i) {
+      mc[i] = fmaxf(mc[i], __shfl_xor_sync(0xffffffffu, mc[i], 1));
+      mc[i] = fmaxf(mc[i], __shfl_xor_sync(0xffffffffu, mc[i], 2));
+      const float mn = fmaxf(acc.m[i], mc[i]);
+      al[i] = mn == -INFINITY ? 1.f : ex2(acc.m[i] - mn);  // 0 at first (m = -inf)
+      acc.m[i] = mn;
+      acc.l[i] *= al[i];
+    }
 #pragma unroll
     for (int j = 0; j < HD / 8; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc.o[j][e] *= al[e / 2];
   }
+  const float ms[2] = {acc.m[0] == -INFINITY ? 0.f : acc.m[0], acc.m[1] == -INFINITY ? 0.f : acc.m[1]};
 #pragma unroll
   for (int u = 0; u < NT; ++u)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[u][e] = exp2f(y[u][e] - ms[e / 2]);
+    for (int e = 0; e < 4; ++e) y[u][e] = ex2(y[u][e] - ms[e / 2]);
 }
 
 // q's fragments: rows gr, gr + 8 of the CTA's 16; -1: a row of zeros.
@@ -190,34 +221,30 @@ template <int HD, int BITS>
 __device__ __forceinline__ void load_q(uint32_t (&qa)[HD / 16][4], float (&qf)[2], const __nv_bfloat16 *q0,
                                        const __nv_bfloat16 *q1, int tc, float scale) {
   using L = Lay<HD, BITS>;
-  float mx[2] = {0.f, 0.f};
+  uint32_t big[2] = {0, 0};  // the rows' largest |q|, as bf16 bits
 #pragma unroll
   for (int ks = 0; ks < L::KS; ++ks) {
     const int at = L::q_at(ks, tc);
     const uint2 a = q0 ? __ldg(reinterpret_cast<const uint2 *>(q0 + at)) : make_uint2(0, 0);
     const uint2 b = q1 ? __ldg(reinterpret_cast<const uint2 *>(q1 + at)) : make_uint2(0, 0);
     qa[ks][0] = a.x, qa[ks][1] = b.x, qa[ks][2] = a.y, qa[ks][3] = b.y;
+    if constexpr (BITS != 16)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      mx[i % 2] = fmaxf(mx[i % 2], fabsf(bf_lo(qa[ks][i])));
-      mx[i % 2] = fmaxf(mx[i % 2], fabsf(bf_hi(qa[ks][i])));
-    }
+      for (int i = 0; i < 4; ++i) big[i % 2] = __vmaxu2(big[i % 2], qa[ks][i] & 0x7fff7fffu);
   }
   qf[0] = qf[1] = scale;
   if constexpr (BITS != 16) {
     // an exact power of two puts the row's largest value in [2^14, 2^15): what
     // binary16 then loses is below 2^-38 of it
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 1));
-      mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 2));
-    }
     float f[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      // exponent of mx, kept where 2^e and 2^-e are normal; 0 and inf: 1
-      const int e = (int)(__float_as_uint(mx[i]) >> 23) - 127;
-      const int sh = e == 128 || mx[i] == 0.f ? 0 : min(126, max(-100, 14 - e));
+      big[i] = max(big[i] & 0xffffu, big[i] >> 16);
+      big[i] = max(big[i], __shfl_xor_sync(0xffffffffu, big[i], 1));
+      big[i] = max(big[i], __shfl_xor_sync(0xffffffffu, big[i], 2));
+      // its exponent, kept where 2^e and 2^-e are normal; 0 and inf: 1
+      const int e = (int)(big[i] >> 7) - 127;
+      const int sh = e == 128 || big[i] == 0 ? 0 : min(126, max(-100, 14 - e));
       f[i] = __uint_as_float((uint32_t)(127 + sh) << 23);
       qf[i] = scale * __uint_as_float((uint32_t)(127 - sh) << 23);
     }
@@ -230,37 +257,64 @@ __device__ __forceinline__ void load_q(uint32_t (&qa)[HD / 16][4], float (&qf)[2
 
 }  // namespace
 
-// Where lane tc's output columns go: Lay<HD, BITS> of the context's V for the
-// cache's chunks, Lay<HD, 16> for the drafts'.  Both orders differ for a
-// quantized cache, so a draft's V is fetched in the cache's order (value by
-// value: at most T rows).
 template <int HD, int BITS>
-__global__ void __launch_bounds__(kTreeWarps * 32, 2) attn_tree_kernel(const TreeArgs a) {
+__global__ void __launch_bounds__(kTreeWarps * 32, 3) attn_tree_kernel(const TreeArgs a) {
   using L = Lay<HD, BITS>;
   using L16 = Lay<HD, 16>;
-  constexpr int NC = BITS == 4 ? 2 : 1, CHP = 16 * NC;  // 16-position groups a chunk
   constexpr int OS = HD + 4;
-  __shared__ __align__(16) float so[kTreeWarps][kRows][OS];
+  extern __shared__ __align__(128) uint8_t tree_ring[];
+  __shared__ uint64_t full[L::NS], empty[L::NS];
   __shared__ float sm[kTreeWarps][kRows], sl[kTreeWarps][kRows];
+  __shared__ int late;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gr = lane >> 2, tc = lane & 3;
+  if (tid == 0) {
+    for (int i = 0; i < L::NS; ++i) {
+      mbar_init(&full[i], 1);
+      mbar_init(&empty[i], kTreeWarps);
+    }
+    fence_barrier_init();
+    late = 0;
+  }
+  __syncthreads();
   pdl_wait();
   pdl_launch_dependents();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gr = lane >> 2, tc = lane & 3;
   const int b = blockIdx.x / a.Hkv, g = blockIdx.x % a.Hkv, split = blockIdx.y, r0 = blockIdx.z * kRows;
   const int rep = a.H / a.Hkv, R = a.T * rep;
   const int len = a.lens[b], cnt = a.counts ? a.counts[b] : a.T;
-  if (len < 0 || len > a.max_len || cnt < 0 || cnt > a.T) {
+  if (len < 0 || len > a.max_len || cnt < 0 || cnt > a.T) {  // the whole cluster alike
     if (tid == 0 && g == 0 && split == 0 && r0 == 0) atomicExch(&g_tree_status, -1);
     return;
   }
-  // units of this split: chunks of drafts, then of the context
-  const int ndr = (cnt + 15) / 16, U = ndr + (len + CHP - 1) / CHP;
+  // what this split takes, in units of 16: drafts, then the context
+  const int ndr = (cnt + 15) / 16, U = ndr + (len + 15) / 16;
   const int u0 = (int)((long long)U * split / a.S), u1 = (int)((long long)U * (split + 1) / a.S);
+  const bool rows = r0 < cnt * rep;  // rows of drafts that exist
+  const int c0 = rows ? (max(u0, ndr) - ndr) * 16 : 0, c1 = rows ? min(len, (u1 - ndr) * 16) : 0;  // positions
+  const int nt = c1 > c0 ? (c1 - c0 + kTreeTile - 1) / kTreeTile : 0;
+  const size_t base = ((size_t)b * a.Hkv + g) * a.max_len;
+  const uint8_t *kc = reinterpret_cast<const uint8_t *>(a.kc) + base * L::ROW;
+  const uint8_t *vc = reinterpret_cast<const uint8_t *>(a.vc) + base * L::ROW;
+  auto copy_tile = [&](int i) {  // one thread
+    const int p = c0 + i * kTreeTile, st = i % L::NS;
+    const uint32_t bytes = (uint32_t)min(kTreeTile, c1 - p) * L::ROW;
+    mbar_arrive_expect_tx(&full[st], 2 * bytes);
+    bulk_g2s(tree_ring + st * L::STAGE, kc + (size_t)p * L::ROW, bytes, &full[st]);
+    bulk_g2s(tree_ring + st * L::STAGE + L::STAGE / 2, vc + (size_t)p * L::ROW, bytes, &full[st]);
+  };
+  if (tid == 0)
+    for (int i = 0; i < min(nt, L::NS); ++i) copy_tile(i);
   const int ra = r0 + gr, rb = ra + 8;
   const int ta = ra / rep, tb = rb / rep;  // the rows' drafts
   const bool ina = ra < R && ta < cnt, inb = rb < R && tb < cnt;
   const __nv_bfloat16 *qbase = reinterpret_cast<const __nv_bfloat16 *>(a.q);
   const __nv_bfloat16 *qa_p = ina ? qbase + (((size_t)b * a.T + ta) * a.H + g * rep + ra % rep) * HD : nullptr;
   const __nv_bfloat16 *qb_p = inb ? qbase + (((size_t)b * a.T + tb) * a.H + g * rep + rb % rep) * HD : nullptr;
+  uint32_t meta = 0;
+  auto load_meta = [&](int i) {  // lanes 0-15: K's, 16-31: V's of the warp's 16 positions of tile i
+    if constexpr (BITS != 16)
+      meta = __ldg((lane < 16 ? a.km : a.vm) + base + min(c0 + i * kTreeTile + warp * 16 + (lane & 15), len - 1));
+  };
+  if (nt > 0) load_meta(0);
 
   Acc<HD> acc;
 #pragma unroll
@@ -277,7 +331,7 @@ __global__ void __launch_bounds__(kTreeWarps * 32, 2) attn_tree_kernel(const Tre
   const size_t dstride = (size_t)a.Hkv * HD;
   const __nv_bfloat16 *kd = reinterpret_cast<const __nv_bfloat16 *>(a.kn) + ((size_t)b * a.T * a.Hkv + g) * HD;
   const __nv_bfloat16 *vd = reinterpret_cast<const __nv_bfloat16 *>(a.vn) + ((size_t)b * a.T * a.Hkv + g) * HD;
-  if (u < min(u1, ndr)) {
+  if (rows && u < min(u1, ndr)) {
     load_q<HD, 16>(qa, qf, qa_p, qb_p, tc, a.scale);
     for (; u < min(u1, ndr); u += kTreeWarps) {
       const int j0 = u * 16, n = min(16, cnt - j0);
@@ -316,23 +370,29 @@ __global__ void __launch_bounds__(kTreeWarps * 32, 2) attn_tree_kernel(const Tre
       for (int i = 0; i < 4; ++i) pf[i] = pack_bf2(y[i / 2][2 * (i % 2)], y[i / 2][2 * (i % 2) + 1]);
 #pragma unroll
       for (int i = 0; i < 2; ++i) acc.l[i] += (y[0][2 * i] + y[0][2 * i + 1]) + (y[1][2 * i] + y[1][2 * i + 1]);
+      // V's rows in the order of the cache's columns (8 in a row lie together in all of them)
       bool odd = false;
+      uint32_t vw[4][HD / 16];
 #pragma unroll
-      for (int j = 0; j < L::NJ; ++j) {
-        uint32_t h[4];
+      for (int i = 0; i < 4; ++i) {
+        const int p = 8 * (i / 2) + 2 * tc + i % 2;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int p = 8 * (i / 2) + 2 * tc + i % 2;
-          uint32_t x = 0;
-          if (p < n) x = __bfloat16_as_ushort(vd[(size_t)(j0 + p) * dstride + L::v_at(j, gr)]);
-          if ((x & 0x7f80u) == 0x7f80u) {
-            x = 0;
-            odd = true;
-          }
-          h[i] = x;
+        for (int k = 0; k < HD / 64; ++k) {
+          const uint4 x = p < n ? __ldg(reinterpret_cast<const uint4 *>(vd + (size_t)(j0 + p) * dstride + L::v_at(8 * k, gr)))
+                                : make_uint4(0, 0, 0, 0);
+          vw[i][4 * k] = x.x, vw[i][4 * k + 1] = x.y, vw[i][4 * k + 2] = x.z, vw[i][4 * k + 3] = x.w;
         }
-        mma_bf16_16816(acc.o[j], pf, h[0] | h[1] << 16, h[2] | h[3] << 16);
+#pragma unroll
+        for (int k = 0; k < HD / 16; ++k) {
+          uint32_t &x = vw[i][k];
+          if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u, odd = true;
+          if ((x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu, odd = true;
+        }
       }
+#pragma unroll
+      for (int j = 0; j < L::NJ; ++j)
+        mma_bf16_16816(acc.o[j], pf, __byte_perm(vw[0][j / 2], vw[1][j / 2], j % 2 ? 0x7632 : 0x5410),
+                       __byte_perm(vw[2][j / 2], vw[3][j / 2], j % 2 ? 0x7632 : 0x5410));
       if (__any_sync(0xffffffffu, odd)) {
         for (int p = 0; p < n; ++p)
 #pragma unroll
@@ -349,145 +409,140 @@ __global__ void __launch_bounds__(kTreeWarps * 32, 2) attn_tree_kernel(const Tre
   }
 
   // ---- context
-  if (u < u1) {
+  bool ok = true;
+  if (nt > 0) {
     load_q<HD, BITS>(qa, qf, qa_p, qb_p, tc, a.scale);
-    const size_t base = ((size_t)b * a.Hkv + g) * a.max_len;
-    const uint8_t *kc = reinterpret_cast<const uint8_t *>(a.kc) + base * L::ROW;
-    const uint8_t *vc = reinterpret_cast<const uint8_t *>(a.vc) + base * L::ROW;
-    uint32_t kw[NC][2][L::KI * L::KW], vw[NC][4][L::VI * L::VW], meta[NC];
-    auto load_k = [&](int p0) {
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int v = 0; v < 2; ++v) {
-          const int p = min(p0 + 16 * c + 8 * v + gr, len - 1);
-#pragma unroll
-          for (int i = 0; i < L::KI; ++i)
-            load_words(*reinterpret_cast<uint32_t(*)[L::KW]>(&kw[c][v][L::KW * i]),
-                       kc + (size_t)p * L::ROW + i * 64 + tc * 4 * L::KW);
-        }
-    };
-    auto load_v = [&](int p0) {
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          const int p = min(p0 + 16 * c + 8 * (v / 2) + 2 * tc + v % 2, len - 1);
-#pragma unroll
-          for (int i = 0; i < L::VI; ++i)
-            load_words(*reinterpret_cast<uint32_t(*)[L::VW]>(&vw[c][v][L::VW * i]),
-                       vc + (size_t)p * L::ROW + i * 128 + gr * 4 * L::VW);
-        }
-    };
-    auto load_meta = [&](int p0) {  // lanes 0-15: K's, 16-31: V's
-      if constexpr (BITS != 16)
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-          meta[c] = __ldg((lane < 16 ? a.km : a.vm) + base + min(p0 + 16 * c + (lane & 15), len - 1));
-    };
-    int p0 = (u - ndr) * CHP;
-    load_k(p0);
-    load_meta(p0);
-    load_v(p0);
-    for (; u < u1; u += kTreeWarps, p0 += kTreeWarps * CHP) {
-      const int pn = u + kTreeWarps < u1 ? p0 + kTreeWarps * CHP : p0;  // past the end: the same rows again
-      float y[2 * NC][4];
-      uint32_t mk[NC], mv[NC];
-#pragma unroll
-      for (int c = 0; c < NC; ++c) mk[c] = mv[c] = meta[c];
-#pragma unroll
-      for (int c = 0; c < NC; ++c)
+    for (int i = 0; i < nt && ok; ++i) {
+      const int st = i % L::NS, p0 = c0 + i * kTreeTile + warp * 16, n = c1 - p0;  // n: positions of the warp's 16
+      ok = __all_sync(0xffffffffu, mbar_wait(&full[st], (i / L::NS) & 1));
+      if (!ok) break;
+      const uint32_t mw = meta;
+      if (i + 1 < nt) load_meta(i + 1);
+      if (n > 0) {
+        const uint8_t *kt = tree_ring + st * L::STAGE + warp * 16 * L::ROW, *vt = kt + L::STAGE / 2;
+        float y[2][4];
 #pragma unroll
         for (int v = 0; v < 2; ++v) {
-          uint32_t z1 = 0, z6 = 0;
+          uint32_t kw[L::KI * L::KW], z1 = 0, z6 = 0;
+#pragma unroll
+          for (int k = 0; k < L::KI; ++k)
+            load_words(*reinterpret_cast<uint32_t(*)[L::KW]>(&kw[L::KW * k]), kt + (8 * v + gr) * L::ROW + k * 64 + tc * 4 * L::KW);
           if constexpr (BITS != 16) {
-            const uint32_t m = __shfl_sync(0xffffffffu, mk[c], 8 * v + gr);
-            const __half z = __ushort_as_half((unsigned short)(m >> 16));
-            const __half2 zz = __half2half2(z);
+            const uint32_t m = __shfl_sync(0xffffffffu, mw, 8 * v + gr);
+            const __half2 zz = __half2half2(__ushort_as_half((unsigned short)(m >> 16)));
             const __half2 k1 = __hadd2(zz, __float2half2_rn(1024.f)), k6 = __hadd2(zz, __float2half2_rn(64.f));
             z1 = *reinterpret_cast<const uint32_t *>(&k1);
             z6 = *reinterpret_cast<const uint32_t *>(&k6);
           }
-          float *yy = y[2 * c + v];
+          // two chains of MMAs
+          float y2[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) yy[e] = 0.f;
+          for (int e = 0; e < 4; ++e) y[v][e] = 0.f;
 #pragma unroll
           for (int ks = 0; ks < L::KS; ++ks) {
             uint32_t b0, b1;
-            k_frag<HD, BITS>(kw[c][v], ks, z1, z6, b0, b1);
+            k_frag<HD, BITS>(kw, ks, z1, z6, b0, b1);
             if constexpr (BITS == 16)
-              mma_bf16_16816(y[2 * c + v], qa[ks], b0, b1);
+              mma_bf16_16816(ks % 2 ? y2 : y[v], qa[ks], b0, b1);
             else
-              mma_f16_16816(y[2 * c + v], qa[ks], b0, b1);
+              mma_f16_16816(ks % 2 ? y2 : y[v], qa[ks], b0, b1);
           }
-        }
-      load_k(pn);
-      float rs[NC][4];
-      uint32_t zv[NC][2][2];  // [.][positions 2 tc, + 1 of 8 v ..][1024 + z, 64 + z]
 #pragma unroll
-      for (int c = 0; c < NC; ++c)
+          for (int e = 0; e < 4; ++e) y[v][e] += y2[e];
+        }
+        float rs[4];
+        uint32_t zv[2][2];  // [positions 2 tc, + 1 of 8 v ..][1024 + z, 64 + z]
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          const int at = 8 * (v / 2) + 2 * tc + v % 2;  // of the group's 16 positions
-          const bool in = p0 + 16 * c + at < len;
-          float *yy = y[2 * c + v / 2];
+          float *yy = y[v / 2];
           if constexpr (BITS == 16) {
-            yy[v % 2] = in ? yy[v % 2] * qf[0] : -INFINITY;
-            yy[2 + v % 2] = in ? yy[2 + v % 2] * qf[1] : -INFINITY;
+            yy[v % 2] *= qf[0];
+            yy[2 + v % 2] *= qf[1];
           } else {
-            const uint32_t m = __shfl_sync(0xffffffffu, mk[c], at), mm = __shfl_sync(0xffffffffu, mv[c], 16 + at);
+            const int at = 8 * (v / 2) + 2 * tc + v % 2;  // of the 16 positions
+            const uint32_t m = __shfl_sync(0xffffffffu, mw, at), mm = __shfl_sync(0xffffffffu, mw, 16 + at);
             const float sk = __half2float(__ushort_as_half((unsigned short)(m & 0xffffu)));
             float sv = __half2float(__ushort_as_half((unsigned short)(mm & 0xffffu)));
             if (sv == 0.f) sv = 1.f;  // a zero-filled cache's row: code - z is 0
-            const float lg = in ? __log2f(sv) : -INFINITY;
-            rs[c][v] = __frcp_rn(sv);
+            const float lg = lg2(sv);
+            rs[v] = rcp(sv);
             yy[v % 2] = fmaf(yy[v % 2] * qf[0], sk, lg);
             yy[2 + v % 2] = fmaf(yy[2 + v % 2] * qf[1], sk, lg);
-            if (!in) yy[v % 2] = yy[2 + v % 2] = -INFINITY, rs[c][v] = 0.f;
-            const uint32_t zh = mm >> 16;
             if (v % 2 == 0)
-              zv[c][v / 2][0] = zh;
+              zv[v / 2][0] = mm >> 16;
             else
-              zv[c][v / 2][0] |= zh << 16;
+              zv[v / 2][0] |= mm & 0xffff0000u;
           }
         }
-      if constexpr (BITS != 16)
+        if (n < 16)
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
+          for (int v = 0; v < 4; ++v)
+            if (8 * (v / 2) + 2 * tc + v % 2 >= n) {
+              y[v / 2][v % 2] = y[v / 2][2 + v % 2] = -INFINITY;
+              rs[v] = 0.f;
+            }
+        if constexpr (BITS != 16)
 #pragma unroll
           for (int v = 0; v < 2; ++v) {
-            const __half2 zz = *reinterpret_cast<const __half2 *>(&zv[c][v][0]);
+            const __half2 zz = *reinterpret_cast<const __half2 *>(&zv[v][0]);
             const __half2 k1 = __hadd2(zz, __float2half2_rn(1024.f)), k6 = __hadd2(zz, __float2half2_rn(64.f));
-            zv[c][v][0] = *reinterpret_cast<const uint32_t *>(&k1);
-            zv[c][v][1] = *reinterpret_cast<const uint32_t *>(&k6);
+            zv[v][0] = *reinterpret_cast<const uint32_t *>(&k1);
+            zv[v][1] = *reinterpret_cast<const uint32_t *>(&k6);
           }
-      load_meta(pn);
-      softmax_step<HD, 2 * NC>(acc, y);
+        uint32_t vw[4][L::VI * L::VW];
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
+        for (int v = 0; v < 4; ++v) {
+          const int at = 8 * (v / 2) + 2 * tc + v % 2;
+#pragma unroll
+          for (int k = 0; k < L::VI; ++k)
+            load_words(*reinterpret_cast<uint32_t(*)[L::VW]>(&vw[v][L::VW * k]), vt + at * L::ROW + k * 128 + gr * 4 * L::VW);
+        }
+        if (BITS == 16 && n < 16)  // what the ring held before may not be finite
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+            if (8 * (v / 2) + 2 * tc + v % 2 >= n)
+#pragma unroll
+              for (int k = 0; k < L::VI * L::VW; ++k) vw[v][k] = 0;
+        softmax_step<HD, 2>(acc, y);
         uint32_t pf[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float p = y[2 * c + i / 2][2 * (i % 2)], q = y[2 * c + i / 2][2 * (i % 2) + 1];
-          pf[i] = BITS == 16 ? pack_bf2(p, q) : pack_h2(p, q);
+        for (int k = 0; k < 4; ++k) {
+          const float p = y[k / 2][2 * (k % 2)], q = y[k / 2][2 * (k % 2) + 1];
+          pf[k] = BITS == 16 ? pack_bf2(p, q) : pack_h2(p, q);
           if constexpr (BITS == 16)
-            acc.l[i % 2] += p + q;
+            acc.l[k % 2] += p + q;
           else
-            acc.l[i % 2] += fmaf(p, rs[c][2 * (i / 2)], q * rs[c][2 * (i / 2) + 1]);
+            acc.l[k % 2] += fmaf(p, rs[2 * (k / 2)], q * rs[2 * (k / 2) + 1]);
         }
 #pragma unroll
         for (int j = 0; j < L::NJ; ++j) {
-          uint32_t b0 = v_frag<HD, BITS>(vw[c][0], vw[c][1], j, zv[c][0][0], zv[c][0][1]);
-          uint32_t b1 = v_frag<HD, BITS>(vw[c][2], vw[c][3], j, zv[c][1][0], zv[c][1][1]);
+          const uint32_t b0 = v_frag<HD, BITS>(vw[0], vw[1], j, zv[0][0], zv[0][1]);
+          const uint32_t b1 = v_frag<HD, BITS>(vw[2], vw[3], j, zv[1][0], zv[1][1]);
           if constexpr (BITS == 16)
             mma_bf16_16816(acc.o[j], pf, b0, b1);
           else
             mma_f16_16816(acc.o[j], pf, b0, b1);
         }
       }
-      load_v(pn);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&empty[st]);
+      // the tile NS after the one before this, whose warps have had a tile's time
+      if (warp == 0 && i > 0 && i - 1 + L::NS < nt) {
+        const int e = (i - 1) % L::NS;
+        ok = __all_sync(0xffffffffu, mbar_wait(&empty[e], ((i - 1) / L::NS) & 1));
+        if (ok && lane == 0) copy_tile(i - 1 + L::NS);
+      }
     }
+    if (!ok && lane == 0) late = 1;
   }
+  __syncthreads();
+  if (late) {  // copies in flight are given time to land
+    if (tid == 0) atomicExch(&g_tree_status, -6);
+    const unsigned long long t0 = global_timer_ns();
+    for (int i = 0; i < (1 << 20) && global_timer_ns() - t0 < 2000000ull; ++i) __nanosleep(1000);
+    __syncthreads();
+  }
+  float(*so)[kRows][OS] = reinterpret_cast<float(*)[kRows][OS]>(tree_ring);
 
   // ---- the warps' results merged in warp order
 #pragma unroll
@@ -513,7 +568,7 @@ __global__ void __launch_bounds__(kTreeWarps * 32, 2) attn_tree_kernel(const Tre
     float Ls = 0.f, O0 = 0.f, O1 = 0.f;
 #pragma unroll
     for (int w = 0; w < kTreeWarps; ++w) {
-      const float f = sm[w][r] == -INFINITY ? 0.f : exp2f(sm[w][r] - M);
+      const float f = sm[w][r] == -INFINITY ? 0.f : ex2(sm[w][r] - M);
       Ls = fmaf(sl[w][r], f, Ls);
       O0 = fmaf(so[w][r][e], f, O0);
       O1 = fmaf(so[w][r][e + 1], f, O1);
@@ -523,140 +578,196 @@ __global__ void __launch_bounds__(kTreeWarps * 32, 2) attn_tree_kernel(const Tre
       const bool none = (M == -INFINITY && Ls == 0.f) || t >= cnt;  // sees nothing, or is padding
       *reinterpret_cast<uint32_t *>(reinterpret_cast<__nv_bfloat16 *>(a.o) + (((size_t)b * a.T + t) * a.H + h) * HD + e) =
           none ? 0u : pack_bf2(O0 / Ls, O1 / Ls);
+    } else if (a.cluster) {
+      // (this thread alone reads these places: the warps' results, whose first takes the CTA's)
+      so[0][r][e] = O0;
+      so[0][r][e + 1] = O1;
+      if (e == 0) {
+        so[0][r][HD] = M;
+        so[0][r][HD + 1] = Ls;
+      }
     } else {
       float *pt = a.part + (((size_t)blockIdx.x * R + row) * a.S + split) * (HD + 2);
       *reinterpret_cast<float2 *>(pt + e) = make_float2(O0, O1);
       if (e == 0) *reinterpret_cast<float2 *>(pt + HD) = make_float2(M, Ls);
     }
   }
+  if (a.cluster) {
+    // the cluster's CTAs are the splits: CTA `split` adds up its share of the outputs
+    cg::cluster_group cl = cg::this_cluster();
+    cl.sync();
+    const float *of[kTreeCluster];
+#pragma unroll
+    for (int k = 0; k < kTreeCluster; ++k) of[k] = k < a.S ? cl.map_shared_rank(&so[0][0][0], k) : nullptr;
+    for (int i = split * kTreeWarps * 32 + tid; i < kRows * HD / 2; i += a.S * kTreeWarps * 32) {
+      const int r = i / (HD / 2), e = 2 * (i % (HD / 2)), row = r0 + r;
+      if (row >= R) break;
+      float2 ml[kTreeCluster], ov[kTreeCluster];
+      float M = -INFINITY, Ls = 0.f, O0 = 0.f, O1 = 0.f;
+#pragma unroll
+      for (int k = 0; k < kTreeCluster; ++k) {
+        ml[k] = k < a.S ? *reinterpret_cast<const float2 *>(of[k] + r * OS + HD) : make_float2(-INFINITY, 0.f);
+        ov[k] = k < a.S ? *reinterpret_cast<const float2 *>(of[k] + r * OS + e) : make_float2(0.f, 0.f);
+      }
+#pragma unroll
+      for (int k = 0; k < kTreeCluster; ++k) M = fmaxf(M, ml[k].x);
+#pragma unroll
+      for (int k = 0; k < kTreeCluster; ++k) {
+        const float f = ml[k].x == -INFINITY ? 0.f : ex2(ml[k].x - M);
+        Ls = fmaf(ml[k].y, f, Ls);
+        O0 = fmaf(ov[k].x, f, O0);
+        O1 = fmaf(ov[k].y, f, O1);
+      }
+      const int t = row / rep, h = g * rep + row % rep;
+      const bool none = (M == -INFINITY && Ls == 0.f) || t >= cnt;
+      *reinterpret_cast<uint32_t *>(reinterpret_cast<__nv_bfloat16 *>(a.o) + (((size_t)b * a.T + t) * a.H + h) * HD + e) =
+          none ? 0u : pack_bf2(O0 / Ls, O1 / Ls);
+    }
+    cl.sync();  // no CTA leaves while another reads from it
+  }
 }
 
-// o of one row: its splits' parts added in a fixed order by WPR warps (warp w:
-// splits w, w + WPR, .. in order, then the warps in order).  grid: rows / (8 / WPR).
+// o of one row: its splits' parts added in a fixed order (warp w: splits w, w + 8, .. in order, then the warps in
+// order).  grid: rows.
 constexpr int kCombineWarps = 8;
 
-template <int HD, int WPR>
+template <int HD>
 __global__ void __launch_bounds__(kCombineWarps * 32) attn_tree_combine_kernel(const TreeArgs a) {
-  constexpr int E = HD / 32, CU = WPR == 1 ? 4 : 8;  // splits loaded in one round trip
+  constexpr int E = HD / 32, CU = 8;  // splits loaded in one round trip
   __shared__ float wm[kCombineWarps], wl[kCombineWarps], wo[kCombineWarps][HD];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rep = a.H / a.Hkv, R = a.T * rep;
-  const long long rows = (long long)a.batch * a.Hkv * R;
-  const long long row = (long long)blockIdx.x * (kCombineWarps / WPR) + warp / WPR;
-  const int sub = warp % WPR;
+  const size_t row = blockIdx.x;
+  const int bg = (int)(row / R), r = (int)(row - (size_t)bg * R), b = bg / a.Hkv, g = bg % a.Hkv;
   pdl_wait();
   pdl_launch_dependents();
-  const bool in = row < rows;
-  const int bg = (int)(row / R), r = (int)(row - (long long)bg * R), b = bg / a.Hkv, g = bg % a.Hkv;
-  bool skip = !in;
-  int cnt = a.T;
-  if (in) {
-    const int len = a.lens[b];
-    if (a.counts) cnt = a.counts[b];
-    skip = len < 0 || len > a.max_len || cnt < 0 || cnt > a.T;
-  }
+  const int len = a.lens[b], cnt = a.counts ? a.counts[b] : a.T;
   float M = -INFINITY, Ls = 0.f, O[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) O[e] = 0.f;
-  if (!skip) {
-    const float *pt = a.part + (size_t)row * a.S * (HD + 2);
-    for (int s0 = sub; s0 < a.S; s0 += CU * WPR) {
-      float2 ml[CU], ov[CU][E / 2];
-      float mn = M;
+  const float *pt = a.part + row * a.S * (HD + 2);
+  for (int s0 = warp; s0 < a.S; s0 += CU * kCombineWarps) {
+    float2 ml[CU], ov[CU][E / 2];
+    float mn = M;
 #pragma unroll
-      for (int c = 0; c < CU; ++c) {
-        const int s = s0 + c * WPR;
-        const float *ps = pt + (size_t)s * (HD + 2);
-        ml[c] = s < a.S ? *reinterpret_cast<const float2 *>(ps + HD) : make_float2(-INFINITY, 0.f);
+    for (int c = 0; c < CU; ++c) {
+      const int s = s0 + c * kCombineWarps;
+      const float *ps = pt + (size_t)s * (HD + 2);
+      ml[c] = s < a.S ? *reinterpret_cast<const float2 *>(ps + HD) : make_float2(-INFINITY, 0.f);
 #pragma unroll
-        for (int e = 0; e < E / 2; ++e)
-          ov[c][e] = s < a.S ? *reinterpret_cast<const float2 *>(ps + lane * E + 2 * e) : make_float2(0.f, 0.f);
-      }
+      for (int e = 0; e < E / 2; ++e)
+        ov[c][e] = s < a.S ? *reinterpret_cast<const float2 *>(ps + lane * E + 2 * e) : make_float2(0.f, 0.f);
+    }
 #pragma unroll
-      for (int c = 0; c < CU; ++c) mn = fmaxf(mn, ml[c].x);
-      const float f0 = M == -INFINITY ? 0.f : exp2f(M - mn);
-      M = mn;
-      Ls *= f0;
+    for (int c = 0; c < CU; ++c) mn = fmaxf(mn, ml[c].x);
+    const float f0 = M == -INFINITY ? 0.f : ex2(M - mn);
+    M = mn;
+    Ls *= f0;
 #pragma unroll
-      for (int e = 0; e < E; ++e) O[e] *= f0;
+    for (int e = 0; e < E; ++e) O[e] *= f0;
 #pragma unroll
-      for (int c = 0; c < CU; ++c) {
-        const float f = ml[c].x == -INFINITY ? 0.f : exp2f(ml[c].x - M);
-        Ls = fmaf(ml[c].y, f, Ls);
+    for (int c = 0; c < CU; ++c) {
+      const float f = ml[c].x == -INFINITY ? 0.f : ex2(ml[c].x - M);  // (a NaN of a part stays NaN)
+      Ls = fmaf(ml[c].y, f, Ls);
 #pragma unroll
-        for (int e = 0; e < E / 2; ++e) {
-          O[2 * e] = fmaf(ov[c][e].x, f, O[2 * e]);
-          O[2 * e + 1] = fmaf(ov[c][e].y, f, O[2 * e + 1]);
-        }
+      for (int e = 0; e < E / 2; ++e) {
+        O[2 * e] = fmaf(ov[c][e].x, f, O[2 * e]);
+        O[2 * e + 1] = fmaf(ov[c][e].y, f, O[2 * e + 1]);
       }
     }
   }
-  if constexpr (WPR > 1) {
-    if (lane == 0) {
-      wm[warp] = M;
-      wl[warp] = Ls;
-    }
-#pragma unroll
-    for (int e = 0; e < E; ++e) wo[warp][lane * E + e] = O[e];
-    __syncthreads();
-    if (sub != 0) return;
-    M = -INFINITY;
-    Ls = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) O[e] = 0.f;
-    for (int w = warp; w < warp + WPR; ++w) M = fmaxf(M, wm[w]);
-    for (int w = warp; w < warp + WPR; ++w) {
-      const float f = wm[w] == -INFINITY ? 0.f : exp2f(wm[w] - M);
-      Ls = fmaf(wl[w], f, Ls);
-#pragma unroll
-      for (int e = 0; e < E; ++e) O[e] = fmaf(wo[w][lane * E + e], f, O[e]);
-    }
+  if (len < 0 || len > a.max_len || cnt < 0 || cnt > a.T) return;  // skipped (the whole CTA alike)
+  if (lane == 0) {
+    wm[warp] = M;
+    wl[warp] = Ls;
   }
-  if (skip) return;
+#pragma unroll
+  for (int e = 0; e < E; ++e) wo[warp][lane * E + e] = O[e];
+  __syncthreads();
+  if (threadIdx.x >= HD / 2) return;
+  const int e = 2 * threadIdx.x;
+  M = -INFINITY;
+  Ls = 0.f;
+  float O0 = 0.f, O1 = 0.f;
+#pragma unroll
+  for (int w = 0; w < kCombineWarps; ++w) M = fmaxf(M, wm[w]);
+#pragma unroll
+  for (int w = 0; w < kCombineWarps; ++w) {
+    const float f = wm[w] == -INFINITY ? 0.f : ex2(wm[w] - M);
+    Ls = fmaf(wl[w], f, Ls);
+    O0 = fmaf(wo[w][e], f, O0);
+    O1 = fmaf(wo[w][e + 1], f, O1);
+  }
   const int t = r / rep, h = g * rep + r % rep;
-  __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(a.o) + (((size_t)b * a.T + t) * a.H + h) * HD + lane * E;
-#pragma unroll
-  for (int e = 0; e < E / 2; ++e)
-    reinterpret_cast<uint32_t *>(dst)[e] = (M == -INFINITY && Ls == 0.f) || t >= cnt ? 0u : pack_bf2(O[2 * e] / Ls, O[2 * e + 1] / Ls);
+  const bool none = (M == -INFINITY && Ls == 0.f) || t >= cnt;
+  *reinterpret_cast<uint32_t *>(reinterpret_cast<__nv_bfloat16 *>(a.o) + (((size_t)b * a.T + t) * a.H + h) * HD + e) =
+      none ? 0u : pack_bf2(O0 / Ls, O1 / Ls);
 }
 
 int tree_splits(int batch, int T, int H, int Hkv, int max_len, int num_sms) {
-  // as many CTAs as the SMs hold at once (2 each), at least 64 positions a split
+  // as many CTAs as the SMs hold at once (3 each), at least 64 positions a split
   const long long row_tiles = ((long long)T * (H / Hkv) + kRows - 1) / kRows;
-  const long long want = std::max(1ll, 2ll * num_sms / (batch * (long long)Hkv * row_tiles));
+  const long long want = std::max(1ll, 3ll * num_sms / (batch * (long long)Hkv * row_tiles));
   return (int)std::max(1ll, std::min(want, ((long long)max_len + T + 63) / 64));
 }
 
+// Whether the splits are a cluster each.  Three at most always are (32 rows over 512 positions, 16 sequences: 13.7 us
+// against 16.1 with a second kernel); more only where every CTA has an SM of its own, since clusters of several CTAs that
+// share SMs wait for places together (4 sequences, 8 drafts, 1024 positions, 7 splits: 19.0 against 16.3; one sequence,
+// one draft, 500 positions, 8 splits: the same time on the GPU, one launch less for the host).
+bool tree_cluster(int batch, int T, int H, int Hkv, int S, int num_sms) {
+  const long long row_tiles = ((long long)T * (H / Hkv) + kRows - 1) / kRows;
+  return S > 1 && (S <= 3 || (S <= kTreeCluster && batch * (long long)Hkv * row_tiles * S <= num_sms));
+}
+
 size_t tree_part_floats(int batch, int T, int H, int Hkv, int hd, int max_len, int num_sms) {
-  // more than one split only where the CTAs are at most two an SM, of 16 rows each
+  // more than one split only where the CTAs are at most three an SM, of 16 rows each
   const long long most = (long long)batch * T * H * (((long long)max_len + T + 63) / 64);
-  return (size_t)std::min(most, 2ll * kRows * num_sms) * (hd + 2);
+  return (size_t)std::min(most, 3ll * kRows * num_sms) * (hd + 2);
 }
 
 namespace {
 
+// Once a device: the kernel's shared memory.
+template <int HD, int BITS>
+cudaError_t prepare_tree() {
+  static std::atomic<bool> done[64];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= 0 && dev < 64 && done[dev].load(std::memory_order_acquire)) return cudaSuccess;
+  e = cudaFuncSetAttribute(attn_tree_kernel<HD, BITS>, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay<HD, BITS>::SMEM);
+  if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev].store(true, std::memory_order_release);
+  return e;
+}
+
 template <int HD, int BITS>
 cudaError_t launch_tree_t(const TreeArgs &a, cudaStream_t s) {
   const int R = a.T * (a.H / a.Hkv);
-  cudaLaunchAttribute attr[1];
+  cudaError_t e = prepare_tree<HD, BITS>();
+  if (e != cudaSuccess) return e;
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 1;
+  attr[1].val.clusterDim.y = a.S;
+  attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.stream = s;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = a.cluster ? 2 : 1;
   cfg.gridDim = dim3(a.batch * a.Hkv, a.S, (R + kRows - 1) / kRows);
   cfg.blockDim = dim3(kTreeWarps * 32);
-  cudaError_t e = cudaLaunchKernelEx(&cfg, attn_tree_kernel<HD, BITS>, a);
-  if (e != cudaSuccess || a.S == 1) return e;
+  cfg.dynamicSmemBytes = Lay<HD, BITS>::SMEM;
+  e = cudaLaunchKernelEx(&cfg, attn_tree_kernel<HD, BITS>, a);
+  if (e != cudaSuccess || a.S == 1 || a.cluster) return e;
   const long long rows = (long long)a.batch * a.Hkv * R;
+  cfg.numAttrs = 1;
   cfg.blockDim = dim3(kCombineWarps * 32);
-  if (a.S <= 8) {
-    cfg.gridDim = dim3((unsigned)((rows + kCombineWarps - 1) / kCombineWarps));
-    return cudaLaunchKernelEx(&cfg, attn_tree_combine_kernel<HD, 1>, a);
-  }
+  cfg.dynamicSmemBytes = 0;
   cfg.gridDim = dim3((unsigned)rows);
-  return cudaLaunchKernelEx(&cfg, attn_tree_combine_kernel<HD, kCombineWarps>, a);
+  return cudaLaunchKernelEx(&cfg, attn_tree_combine_kernel<HD>, a);
 }
 
 }  // namespace

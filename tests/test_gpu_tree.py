@@ -88,8 +88,21 @@ def reference(q, kn, vn, k, v, lens, counts, vis, scale):
     return o, tol
 
 
-def run(wq, b, t, H, kv, hd, bits, lens, counts=None, vis=None, parents=None, seed=0, max_len=None, scale=None,
-        vscale=1.0, spoil=None, pack=True):
+# Short caches run on the mma.sync kernel, roomy ones on the tcgen05 kernel: every test takes both.
+ROOMY = 800_000
+
+
+@pytest.fixture(params=["short", "roomy"])
+def room(request):
+    """Positions of a cache beyond the filled ones, so that the call takes the other kernel."""
+    def capacity(b, kv, t, H, filled):
+        tiles = (t * (H // kv) + 15) // 16
+        return filled if request.param == "short" else max(filled, ROOMY // (b * kv * tiles) + 1)
+    return capacity
+
+
+def run(wq, room, b, t, H, kv, hd, bits, lens, counts=None, vis=None, parents=None, seed=0, max_len=None, scale=None,
+        vscale=1.0, spoil=None):
     g = torch.Generator().manual_seed(seed)
     L = max_len or max(1, max(lens))
     bf = lambda *s: torch.randn(s, generator=g).to(torch.bfloat16)
@@ -109,7 +122,7 @@ def run(wq, b, t, H, kv, hd, bits, lens, counts=None, vis=None, parents=None, se
         vis = torch.ones((t, t), dtype=torch.bool).tril().expand(b, t, t)
     if spoil:
         spoil(q, kn, vn, k, v)
-    cache = wq.kv_cache(b, kv, L, hd, bits)
+    cache = wq.kv_cache(b, kv, room(b, kv, t, H, L), hd, bits)
     zero = torch.zeros(b, dtype=torch.int32, device="cuda")
     wq.kv_append(cache, k.cuda(), v.cuda(), zero)
     kr, vr = wq.kv_read(cache, zero, L, dtype=torch.float32)
@@ -133,43 +146,43 @@ def close(o, ref, tol):
 @pytest.mark.parametrize("bits", [16, 8, 4])
 @pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("H,kv,t", [(4, 1, 1), (8, 2, 5), (5, 1, 3), (2, 2, 33), (32, 2, 7), (8, 1, 61)])
-def test_trees(wq, bits, hd, H, kv, t):
+def test_trees(wq, room, bits, hd, H, kv, t):
     lens = [0, 1, 15, 16, 17, 31, 33, 127, 129, 300]
     b = len(lens)
     counts = [max(1, t - i % 3) for i in range(b)]
-    close(*run(wq, b, t, H, kv, hd, bits, lens, counts, parents=tree(b, t, t), seed=t + hd + bits, max_len=301))
+    close(*run(wq, room, b, t, H, kv, hd, bits, lens, counts, parents=tree(b, t, t), seed=t + hd + bits, max_len=301))
 
 
 @pytest.mark.parametrize("bits", [16, 8, 4])
-def test_one_token_long_contexts(wq, bits):
-    close(*run(wq, 2, 1, 8, 2, 128, bits, [4097, 9001], seed=1))
-    close(*run(wq, 1, 1, 8, 1, 64, bits, [20000], seed=2))
+def test_one_token_long_contexts(wq, room, bits):
+    close(*run(wq, room, 2, 1, 8, 2, 128, bits, [4097, 9001], seed=1))
+    close(*run(wq, room, 1, 1, 8, 1, 64, bits, [20000], seed=2))
 
 
 @pytest.mark.parametrize("bits,hd,H,kv", [(16, 128, 8, 2), (8, 128, 10, 2), (4, 128, 8, 1), (8, 64, 16, 2), (4, 64, 8, 2),
                                           (16, 64, 8, 1)])
-def test_many_drafts(wq, bits, hd, H, kv):
-    close(*run(wq, 2, 128, H, kv, hd, bits, [777, 1500], [128, 101], parents=tree(2, 128, 3), seed=3))
-    close(*run(wq, 1, 64, H, kv, hd, bits, [2048], seed=4))  # a chain: mask None
+def test_many_drafts(wq, room, bits, hd, H, kv):
+    close(*run(wq, room, 2, 128, H, kv, hd, bits, [777, 1500], [128, 101], parents=tree(2, 128, 3), seed=3))
+    close(*run(wq, room, 1, 64, H, kv, hd, bits, [2048], seed=4))  # a chain: mask None
 
 
 @pytest.mark.parametrize("bits", [16, 8, 4])
-def test_rows_that_see_nothing(wq, bits):
+def test_rows_that_see_nothing(wq, room, bits):
     b, t = 3, 20
     vis = torch.rand((b, t, t), generator=torch.Generator().manual_seed(5)) < 0.2
     vis[:, 4] = False
     vis[1] = False
-    o, ref, tol = run(wq, b, t, 8, 2, 128, bits, [0, 0, 40], vis=vis, seed=5)
+    o, ref, tol = run(wq, room, b, t, 8, 2, 128, bits, [0, 0, 40], vis=vis, seed=5)
     close(o, ref, tol)
     assert (o[0, 4] == 0).all() and (o[1] == 0).all() and (o[2, 4] != 0).any()
-    o, ref, tol = run(wq, b, t, 8, 2, 128, bits, [7, 0, 40], [0, 20, 3], vis=vis, seed=6)  # no drafts, padding drafts
+    o, ref, tol = run(wq, room, b, t, 8, 2, 128, bits, [7, 0, 40], [0, 20, 3], vis=vis, seed=6)  # no drafts, padding drafts
     close(o, ref, tol)
     assert (o[0] == 0).all() and (o[2, 3:] == 0).all()
 
 
 @pytest.mark.parametrize("bits", [16, 8, 4])
 @pytest.mark.parametrize("t,H", [(12, 4), (40, 8)])
-def test_masked_and_unused_places_hold_anything(wq, bits, t, H):
+def test_masked_and_unused_places_hold_anything(wq, room, bits, t, H):
     """NaN and infinities in drafts a row does not see, in padding drafts and behind the length."""
     def spoil(q, kn, vn, k, v):
         for x in (k, v):
@@ -183,13 +196,13 @@ def test_masked_and_unused_places_hold_anything(wq, bits, t, H):
     vis[0, :, 5] = False
     vis[1, :, 3] = False
     vis[1, :, 7] = False
-    o, ref, tol = run(wq, 2, t, H, 1, 128, bits, [200, 90], [t - 2, t], vis=vis, seed=7, spoil=spoil, max_len=210)
+    o, ref, tol = run(wq, room, 2, t, H, 1, 128, bits, [200, 90], [t - 2, t], vis=vis, seed=7, spoil=spoil, max_len=210)
     assert torch.isfinite(ref).all()
     close(o, ref, tol)
 
 
 @pytest.mark.parametrize("bits", [16, 8])
-def test_seen_infinities_reach_only_their_rows(wq, bits):
+def test_seen_infinities_reach_only_their_rows(wq, room, bits):
     t = 20
     def spoil(q, kn, vn, k, v):
         vn[0, 5, 0, 17] = math.inf
@@ -198,56 +211,58 @@ def test_seen_infinities_reach_only_their_rows(wq, bits):
     vis = torch.ones((1, t, t), dtype=torch.bool).tril()
     vis[0, 12:15, 5] = False
     vis[0, 13:, 9] = False
-    o, ref, tol = run(wq, 1, t, 4, 1, 128, bits, [50], vis=vis, seed=8, spoil=spoil)
+    o, ref, tol = run(wq, room, 1, t, 4, 1, 128, bits, [50], vis=vis, seed=8, spoil=spoil)
     assert torch.isinf(ref[0, 6, :, 17]).all() and torch.isnan(ref[0, 10, :, 64]).all() and torch.isfinite(ref[0, 13]).all()
     close(o, ref, tol)
 
 
 @pytest.mark.parametrize("bits", [8, 4])
-def test_rows_of_very_different_scales(wq, bits):
-    close(*run(wq, 2, 6, 8, 2, 128, bits, [500, 77], vscale=100.0, seed=9))
-    close(*run(wq, 1, 40, 8, 1, 64, bits, [500], vscale=100.0, seed=10))
+def test_rows_of_very_different_scales(wq, room, bits):
+    close(*run(wq, room, 2, 6, 8, 2, 128, bits, [500, 77], vscale=100.0, seed=9))
+    close(*run(wq, room, 1, 40, 8, 1, 64, bits, [500], vscale=100.0, seed=10))
 
 
-def test_nan_row_of_a_quantized_cache(wq):
+def test_nan_row_of_a_quantized_cache(wq, room):
     def spoil(q, kn, vn, k, v):
         k[0, 30, 0, 4] = math.nan
-    o, ref, _ = run(wq, 2, 4, 4, 1, 64, 8, [60, 30], seed=11, spoil=spoil)
+    o, ref, _ = run(wq, room, 2, 4, 4, 1, 64, 8, [60, 30], seed=11, spoil=spoil)
     assert o[0].isnan().all() and torch.isfinite(o[1]).all()
 
 
 @pytest.mark.parametrize("scale", [1.0, 0.02])
-def test_scale_and_peaked_scores(wq, scale):
-    close(*run(wq, 1, 9, 8, 2, 128, 16, [333], scale=scale, seed=12))
-    close(*run(wq, 1, 30, 8, 2, 128, 8, [333], scale=scale, seed=13))
+def test_scale_and_peaked_scores(wq, room, scale):
+    close(*run(wq, room, 1, 9, 8, 2, 128, 16, [333], scale=scale, seed=12))
+    close(*run(wq, room, 1, 30, 8, 2, 128, 8, [333], scale=scale, seed=13))
 
 
-def test_query_rows_of_any_size(wq):
+def test_query_rows_of_any_size(wq, room):
     """Rows of q from 2^-60 to 2^60: scores far below and (clipped to one key) far above 1."""
     def spoil(q, kn, vn, k, v):
         for i in range(q.shape[1]):
             q[0, i] = (q[0, i].float() * 2.0 ** (-60 + 20 * (i % 4))).to(torch.bfloat16)
     for bits in (16, 8, 4):
-        close(*run(wq, 1, 8, 4, 1, 128, bits, [100], seed=14, spoil=spoil))
+        close(*run(wq, room, 1, 8, 4, 1, 128, bits, [100], seed=14, spoil=spoil))
 
 
 def test_lengths_out_of_range(wq):
-    c = wq.kv_cache(3, 1, 8, 64, 8)
     x = torch.zeros((3, 2, 1, 64), dtype=torch.bfloat16, device="cuda")
     i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
-    for lens, counts in ((i32(-1, 9, 8), None), (i32(0, 0, 0), i32(-1, 3, 2))):
+    for cap, lens, counts in ((8, i32(-1, 9, 8), None), (8, i32(0, 0, 0), i32(-1, 3, 2)),
+                              (300_000, i32(-1, 300_001, 8), None), (300_000, i32(0, 0, 0), i32(-1, 3, 2))):
+        c = wq.kv_cache(3, 1, cap, 64, 8)
         o = torch.full_like(x, 3.0)
         wq.attn_tree(x, x, x, c, lens, counts=counts, o=o)
         assert wq.device_status() == -1 and wq.device_status() == 0
         assert (o[:2] == 3).all() and (o[2] == 0).all()
 
 
-def test_workspace_of_a_larger_call_other_stream_and_repeats(wq):
+@pytest.mark.parametrize("L", [5000, 90_000])
+def test_workspace_of_a_larger_call_other_stream_and_repeats(wq, L):
     b, t, H, kv, hd = 2, 9, 8, 2, 128
-    ws = wq.attn_tree_workspace(8, 64, H, kv, hd, 5000)
+    ws = wq.attn_tree_workspace(8, 64, H, kv, hd, L)
     g = torch.Generator(device="cuda").manual_seed(15)
     bf = lambda *s: torch.randn(s, generator=g, device="cuda").to(torch.bfloat16)
-    c = wq.kv_cache(b, kv, 5000, hd, 8)
+    c = wq.kv_cache(b, kv, L, hd, 8)
     wq.kv_append(c, bf(b, 5000, kv, hd), bf(b, 5000, kv, hd), torch.zeros(b, dtype=torch.int32, device="cuda"))
     q, kn, vn = bf(b, t, H, hd), bf(b, t, kv, hd), bf(b, t, kv, hd)
     lens = torch.tensor([4999, 3000], dtype=torch.int32, device="cuda")
@@ -296,16 +311,16 @@ def test_small_workspace_is_refused(wq):
 
 @pytest.mark.parametrize("bits", [16, 8])
 @pytest.mark.parametrize("t", [2, 30])
-def test_a_nan_query_gives_nan_rows(wq, bits, t):
+def test_a_nan_query_gives_nan_rows(wq, room, bits, t):
     """Also where every score of a row is NaN; the other rows are as without it."""
     def spoil(q, kn, vn, k, v):
         q[0, 1, 0, 3] = math.nan
-    o, ref, tol = run(wq, 1, t, 4, 1, 128, bits, [300], seed=17, spoil=spoil)
+    o, ref, tol = run(wq, room, 1, t, 4, 1, 128, bits, [300], seed=17, spoil=spoil)
     assert ref[0, 1, 0].isnan().all() and torch.isfinite(ref[0, 0]).all() and torch.isfinite(ref[0, 1, 1]).all()
     close(o, ref, tol)
 
 
-def test_zero_scale_is_the_mean(wq):
-    close(*run(wq, 1, 24, 4, 1, 64, 8, [100], scale=0.0, seed=18))
-    close(*run(wq, 1, 24, 4, 1, 64, 16, [100], scale=-0.1, seed=19))
-    close(*run(wq, 1, 24, 4, 1, 64, 4, [100], scale=-0.1, seed=20))
+def test_zero_scale_is_the_mean(wq, room):
+    close(*run(wq, room, 1, 24, 4, 1, 64, 8, [100], scale=0.0, seed=18))
+    close(*run(wq, room, 1, 24, 4, 1, 64, 16, [100], scale=-0.1, seed=19))
+    close(*run(wq, room, 1, 24, 4, 1, 64, 4, [100], scale=-0.1, seed=20))
