@@ -13,8 +13,14 @@
 //
 // A row is taken by 8 lanes (HD 128) or 4 (HD 64), 16 values a lane: 3 or 2
 // shuffles for the row's range, and the lane's codes are one 16-byte (8 bits)
-// or 8-byte (4 bits) store.  Bound by HBM for prompts, by launch latency for
-// decode steps.
+// or 8-byte (4 bits) store.  A lane takes a K row and the V row beside it (one row
+// a lane: less in flight, 28.8 us for 26.6 below).  The row of 8191 tokens of 8 kv
+// heads is written to 4 bits and read back to bf16 in 21.3 us, 3.5 TB/s: the
+// quantizing is bound by issue slots (17 instructions a value where the quotient
+// was a division and codes were clamped one by one 24, 31.5 us).  Reads are bound
+// by HBM: 12,000 tokens of 8 bits 11.0 us, 6.8 TB/s; 32,768 of 4 bits to fp32 49.5
+// us, 6.1 TB/s.  Decode steps are bound by launches: 16 tokens written and read
+// back 4.4 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -24,7 +30,6 @@
 #include "wq_internal.h"
 #include "wq_kv.h"
 #include "wq_ptx.cuh"
-#include "wq_quant.cuh"
 
 namespace wq {
 
@@ -35,7 +40,7 @@ __device__ int g_kv_status = 0;
 
 namespace {
 
-constexpr int kKvThreads = 256;
+constexpr int kAppendThreads = 128, kReadThreads = 256;
 
 __device__ __forceinline__ float bf_lo(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
@@ -44,145 +49,216 @@ __device__ __forceinline__ uint32_t pack_bf2(float a, float b) {
   return *reinterpret_cast<const uint32_t *>(&v);
 }
 
+
+// Quotients by a divisor of the whole launch: x d' >> (31 + l), l = ceil(log2 d), d' the
+// whole number above 2^(31 + l) / d, too large by at most 1: exact for x below 2^31.
+struct Divisor {
+  unsigned d, mul;
+  int shift;
+  explicit Divisor(int by) : d((unsigned)by), shift(31) {
+    while ((1u << (shift - 31)) < d) ++shift;
+    mul = (unsigned)((1ull << shift) / d + 1);
+  }
+  __device__ __forceinline__ unsigned divide(unsigned x) const { return (unsigned)((unsigned long long)x * mul >> shift); }
+};
+
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  unsigned long long d;
+  asm("{\n.reg .b64 x, y, z;\nmov.b64 x, {%1, %2};\nmov.b64 y, {%3, %4};\nmov.b64 z, {%5, %6};\nfma.rn.f32x2 %0, x, y, z;\n}"
+      : "=l"(d)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return make_float2(__uint_as_float((uint32_t)d), __uint_as_float((uint32_t)(d >> 32)));
+}
+
 }  // namespace
 
-// Slot i of the launch: cache (K, V), sequence, head and step n, the step
-// fastest, so that neighbouring rows of the cache are written together.  Lane l
-// of a row holds its values 16 l .. 16 l + 15.
+// 16 values of a row whose range around 0 is mn .. mx: the row's scale and zero as a
+// cache holds them, the values' codes, two a word.
+//   With M = 1.5 2^23, v r + M rounded is M + a whole number, held in its low bits.
+// r is 1 / sf made 2^-22 larger and 2^-22 smaller: v / sf and its rounding to fp32 lie
+// between the two products, so that where both give the same whole number it is the
+// quotient's; else (a half, or within 2^-21 of its size of one: in 5% of rows of normal
+// bf16 values in 4 bits, for 8 bits 0.2%) the pair is divided.
+// A product is below 2^9, since sf is at least two thirds of range / qmax.
+template <int BITS>
+__device__ __forceinline__ uint32_t quantize16(const float (&v)[16], float mn, float mx, uint32_t (&c)[8]) {
+  constexpr float qmax = (float)((1 << BITS) - 1), M = 12582912.f;
+  __half sh = __float2half_rn(__fdiv_rn(__fsub_rn(mx, mn), qmax));
+  if (__half2float(sh) == 0.f) sh = __float2half_rn(1.f);
+  const float sf = __half2float(sh);
+  if (!isfinite(sf)) {  // also infinite or NaN values: mx - mn is then too
+#pragma unroll
+    for (int k = 0; k < 8; ++k) c[k] = 0;
+    return 0x7fffu;
+  }
+  const float zf = __fadd_rn(fminf(fmaxf(rintf(__fdiv_rn(-mn, sf)), 0.f), qmax), 0.f);
+  const float rcp = __frcp_rn(sf), up = __fmul_rn(rcp, 1.f + 0x1p-22f), dn = __fmul_rn(rcp, 1.f - 0x1p-22f);
+  const float2 up2 = make_float2(up, up), dn2 = make_float2(dn, dn), M2 = make_float2(M, M);
+  const uint32_t z2 = (uint32_t)zf * 0x10001u, q2 = (uint32_t)qmax * 0x10001u;
+  uint32_t differ = 0;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const float2 x = make_float2(v[2 * k], v[2 * k + 1]);
+    const float2 t = fma2(x, up2, M2), u = fma2(x, dn2, M2);
+    const uint32_t t0 = __float_as_uint(t.x), t1 = __float_as_uint(t.y);
+    differ |= t0 ^ __float_as_uint(u.x);
+    differ |= t1 ^ __float_as_uint(u.y);
+    c[k] = __viaddmin_s16x2_relu(__byte_perm(t0, t1, 0x5410), z2, q2);  // max(min(t + z, qmax), 0)
+  }
+  if (differ != 0) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float2 x = make_float2(v[2 * k], v[2 * k + 1]);
+      const float2 t = fma2(x, up2, M2), u = fma2(x, dn2, M2);
+      if (t.x != u.x || t.y != u.y) {
+        const float t0 = __fadd_rn(rintf(__fdiv_rn(x.x, sf)), zf), t1 = __fadd_rn(rintf(__fdiv_rn(x.y, sf)), zf);
+        c[k] = (uint32_t)fminf(fmaxf(t0, 0.f), qmax) | (uint32_t)fminf(fmaxf(t1, 0.f), qmax) << 16;
+      }
+    }
+  }
+  return (uint32_t)__half_as_ushort(sh) | (uint32_t)__half_as_ushort(__float2half_rn(zf)) << 16;
+}
+
+// Slot i of the launch: sequence, head and step n, the step fastest, so that
+// neighbouring rows of the cache are written together (tokens in groups with their
+// other heads beside them took the same time).
+// Lane l of a slot holds values 16 l .. 16 l + 15 of its K row and of its V row.
 template <int HD, int BITS, bool F32>
-__global__ void __launch_bounds__(kKvThreads) kv_append_kernel(const KvAppendArgs a) {
+__global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const KvAppendArgs a, const Divisor by_n, const Divisor by_kv) {
   constexpr int LPR = HD / 16;  // lanes a row
   pdl_wait();
   pdl_launch_dependents();
-  const long long slot = (long long)blockIdx.x * (kKvThreads / LPR) + threadIdx.x / LPR;
+  const unsigned slot = blockIdx.x * (kAppendThreads / LPR) + threadIdx.x / LPR;
   const int lane = threadIdx.x % LPR;
-  const long long per_cache = (long long)a.batch * a.n_kv * a.n;
-  const bool in = slot < 2 * per_cache;
-  const bool is_v = slot >= per_cache;
-  const unsigned rest = (unsigned)(is_v ? slot - per_cache : slot);  // below 2^31 (host check)
-  const unsigned bh = rest / (unsigned)a.n;
-  const int n = (int)(rest - bh * (unsigned)a.n);
-  const int b = (int)(bh / (unsigned)a.n_kv), h = (int)(bh - (unsigned)b * (unsigned)a.n_kv);
-  bool put = in;
+  bool put = slot < (unsigned)a.batch * a.n_kv * a.n;  // below 2^30 (host check)
+  const unsigned bh = by_n.divide(slot);
+  const int n = (int)(slot - bh * (unsigned)a.n);
+  const int b = (int)by_kv.divide(bh), h = (int)(bh - (unsigned)b * (unsigned)a.n_kv);
   int t = n;
   long long pos = 0;
-  if (in) {
+  if (put) {
     const int start = a.start[b], cnt = a.counts ? a.counts[b] : a.n;
+    if (a.index) t = a.index[(size_t)b * a.n + n];
     if (cnt < 0 || cnt > a.n || start < 0 || (long long)start + cnt > a.max_len) {
       if (lane == 0) atomicExch(&g_kv_status, -1);
       put = false;
     } else if (n >= cnt) {
       put = false;
-    } else {
-      pos = (long long)start + n;
-      if (a.index) t = a.index[(size_t)b * a.n + n];
-      if (t < 0 || t >= a.n_src) {
-        if (lane == 0) atomicExch(&g_kv_status, -1);
-        put = false;
-      }
+    } else if (t < 0 || t >= a.n_src) {
+      if (lane == 0) atomicExch(&g_kv_status, -1);
+      put = false;
     }
+    pos = (long long)start + n;
   }
-  float v[16];
-  uint4 raw[2];
+  float v[2][16];
+  uint4 raw[2][2];
 #pragma unroll
-  for (int e = 0; e < 16; ++e) v[e] = 0.f;
-  raw[0] = raw[1] = make_uint4(0, 0, 0, 0);
-  if (put) {
-    const long long *st = is_v ? a.v_stride : a.k_stride;
-    const long long off = (long long)b * st[0] + (long long)t * st[1] + (long long)h * st[2] + lane * 16;
+  for (int i = 0; i < 2; ++i) {
+    const long long *st = i ? a.v_stride : a.k_stride;
+    const long long off = put ? (long long)b * st[0] + (long long)t * st[1] + (long long)h * st[2] + lane * 16 : 0;
     if (F32) {
-      const float4 *src = reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(is_v ? a.v : a.k) + off);
+      const float4 *src = reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(i ? a.v : a.k) + off);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float4 f = __ldcs(src + i);
-        v[4 * i] = f.x, v[4 * i + 1] = f.y, v[4 * i + 2] = f.z, v[4 * i + 3] = f.w;
+      for (int k = 0; k < 4; ++k) {
+        const float4 f = put ? __ldcs(src + k) : make_float4(0.f, 0.f, 0.f, 0.f);
+        v[i][4 * k] = f.x, v[i][4 * k + 1] = f.y, v[i][4 * k + 2] = f.z, v[i][4 * k + 3] = f.w;
       }
     } else {
-      const uint4 *src = reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(is_v ? a.v : a.k) + off);
-      raw[0] = __ldcs(src);
-      raw[1] = __ldcs(src + 1);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[8 * i + 2 * j] = bf_lo(w[j]), v[8 * i + 2 * j + 1] = bf_hi(w[j]);
-      }
+      const uint4 *src = reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(i ? a.v : a.k) + off);
+      raw[i][0] = put ? __ldcs(src) : make_uint4(0, 0, 0, 0);
+      raw[i][1] = put ? __ldcs(src + 1) : make_uint4(0, 0, 0, 0);
     }
   }
   const size_t row = ((size_t)b * a.n_kv + h) * a.max_len + pos;
-  if constexpr (BITS == 16) {
-    if (!put) return;
-    uint4 *dst = reinterpret_cast<uint4 *>(reinterpret_cast<__nv_bfloat16 *>(is_v ? a.vc : a.kc) + row * HD + lane * 16);
-    if (F32) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-        raw[i] = make_uint4(pack_bf2(v[8 * i], v[8 * i + 1]), pack_bf2(v[8 * i + 2], v[8 * i + 3]),
-                            pack_bf2(v[8 * i + 4], v[8 * i + 5]), pack_bf2(v[8 * i + 6], v[8 * i + 7]));
-    }
-    dst[0] = raw[0];
-    dst[1] = raw[1];
-  } else {
-    constexpr float qmax = (float)((1 << BITS) - 1);
-    float mn = 0.f, mx = 0.f;
-    bool bad = false;
+  for (int i = 0; i < 2; ++i) {
+    if constexpr (BITS == 16) {
+      if (!put) continue;
+      uint4 *dst = reinterpret_cast<uint4 *>(reinterpret_cast<__nv_bfloat16 *>(i ? a.vc : a.kc) + row * HD + lane * 16);
+      if (F32) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      mn = fminf(mn, v[e]);
-      mx = fmaxf(mx, v[e]);
-      bad |= !isfinite(v[e]);
-    }
-#pragma unroll
-    for (int o = LPR / 2; o >= 1; o >>= 1) {
-      mn = fminf(mn, __shfl_xor_sync(0xffffffffu, mn, o));
-      mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-      bad |= __shfl_xor_sync(0xffffffffu, (int)bad, o) != 0;
-    }
-    __half sh = __float2half_rn(__fdiv_rn(__fsub_rn(mx, mn), qmax));
-    if (__half2float(sh) == 0.f) sh = __float2half_rn(1.f);
-    const float sf = __half2float(sh);
-    bad |= !isfinite(sf);
-    const float zf = bad ? 0.f : __fadd_rn(fminf(fmaxf(rintf(__fdiv_rn(-mn, sf)), 0.f), qmax), 0.f);
-    const float rcp = __frcp_rn(sf);
-    uint32_t c[16];
-#pragma unroll
-    for (int e = 0; e < 16; ++e)
-      c[e] = bad ? 0u : (uint32_t)fminf(fmaxf(__fadd_rn(rint_div(v[e], sf, rcp), zf), 0.f), qmax);
-    if (!put) return;
-    uint8_t *dst = reinterpret_cast<uint8_t *>(is_v ? a.vc : a.kc) + row * (HD * BITS / 8) + lane * (2 * BITS);
-    if (BITS == 8) {
-      uint32_t w[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = c[4 * i] | c[4 * i + 1] << 8 | c[4 * i + 2] << 16 | c[4 * i + 3] << 24;
-      *reinterpret_cast<uint4 *>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+        for (int k = 0; k < 2; ++k)
+          raw[i][k] = make_uint4(pack_bf2(v[i][8 * k], v[i][8 * k + 1]), pack_bf2(v[i][8 * k + 2], v[i][8 * k + 3]),
+                                 pack_bf2(v[i][8 * k + 4], v[i][8 * k + 5]), pack_bf2(v[i][8 * k + 6], v[i][8 * k + 7]));
+      }
+      dst[0] = raw[i][0];
+      dst[1] = raw[i][1];
     } else {
-      // value e of a word of 8 at bits 4 (e / 2) + 16 (e % 2)
-      uint32_t w[2] = {0, 0};
+      // the row's range around 0 (a NaN is kept in mx)
+      float mn = 0.f, mx = 0.f;
+      if (F32) {
+        bool nan = false;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) w[e / 8] |= c[e] << (4 * (e % 8 / 2) + 16 * (e % 2));
-      *reinterpret_cast<uint2 *>(dst) = make_uint2(w[0], w[1]);
+        for (int e = 0; e < 16; ++e) {
+          mn = fminf(mn, v[i][e]);
+          mx = fmaxf(mx, v[i][e]);
+          nan |= v[i][e] != v[i][e];
+        }
+        if (nan) mx = __int_as_float(0x7fffffff);
+#pragma unroll
+        for (int o = LPR / 2; o >= 1; o >>= 1) {
+          const float x = __shfl_xor_sync(0xffffffffu, mn, o), y = __shfl_xor_sync(0xffffffffu, mx, o);
+          mn = fminf(mn, x);
+          mx = y > mx || y != y ? y : mx;
+        }
+      } else {
+        __nv_bfloat162 lo = __float2bfloat162_rn(0.f), hi = lo;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const uint32_t w[4] = {raw[i][k].x, raw[i][k].y, raw[i][k].z, raw[i][k].w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162 *>(&w[j]);
+            lo = __hmin2_nan(lo, x);
+            hi = __hmax2_nan(hi, x);
+            v[i][8 * k + 2 * j] = bf_lo(w[j]), v[i][8 * k + 2 * j + 1] = bf_hi(w[j]);
+          }
+        }
+        // (the most, minus the least) go through the lanes together
+        __nv_bfloat162 r = __halves2bfloat162(__hmax_nan(__low2bfloat16(hi), __high2bfloat16(hi)),
+                                              __hneg(__hmin_nan(__low2bfloat16(lo), __high2bfloat16(lo))));
+#pragma unroll
+        for (int o = LPR / 2; o >= 1; o >>= 1) r = __hmax2_nan(r, __shfl_xor_sync(0xffffffffu, r, o));
+        mx = __low2float(r);
+        mn = -__high2float(r);
+      }
+      uint32_t c[8];
+      const uint32_t meta = quantize16<BITS>(v[i], mn, mx, c);
+      if (!put) continue;
+      uint8_t *dst = reinterpret_cast<uint8_t *>(i ? a.vc : a.kc) + row * (HD * BITS / 8) + lane * (2 * BITS);
+      if (BITS == 8) {
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = __byte_perm(c[2 * k], c[2 * k + 1], 0x6420);
+        *reinterpret_cast<uint4 *>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+      } else {
+        // value e of a word of 8 at bits 4 (e / 2) + 16 (e % 2)
+        uint32_t w[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) w[k] = (c[4 * k] + (c[4 * k + 1] << 4)) + ((c[4 * k + 2] + (c[4 * k + 3] << 4)) << 8);
+        *reinterpret_cast<uint2 *>(dst) = make_uint2(w[0], w[1]);
+      }
+      if (lane == 0) (i ? a.vm : a.km)[row] = meta;
     }
-    if (lane == 0)
-      (is_v ? a.vm : a.km)[row] = (bad ? 0x7fffu : (uint32_t)__half_as_ushort(sh)) |
-                                  (uint32_t)__half_as_ushort(__float2half_rn(zf)) << 16;
   }
 }
 
-// A lane takes 8 values at a time, chunks l and l + LPR of its row, so that a
-// row's stores are whole 128-byte lines.
+// A lane takes the values of one 16-byte store at a time (8 of bf16, 4 of fp32),
+// chunks l, l + LPR, .. of its row, so that a row's stores are whole lines.
 template <int HD, int BITS, bool F32>
-__global__ void __launch_bounds__(kKvThreads) kv_read_kernel(const KvReadArgs a) {
-  constexpr int LPR = HD / 16;
+__global__ void __launch_bounds__(kReadThreads) kv_read_kernel(const KvReadArgs a, const Divisor by_n, const Divisor by_kv) {
+  constexpr int LPR = HD / 16, N = F32 ? 4 : 8, CH = 16 / N;  // lanes a row, values a chunk, chunks a lane
   pdl_wait();
   pdl_launch_dependents();
-  const long long slot = (long long)blockIdx.x * (kKvThreads / LPR) + threadIdx.x / LPR;
+  const unsigned slot = blockIdx.x * (kReadThreads / LPR) + threadIdx.x / LPR;
   const int lane = threadIdx.x % LPR;
-  const long long per_cache = (long long)a.batch * a.n_kv * a.n;
+  const unsigned per_cache = (unsigned)a.batch * a.n_kv * a.n;  // below 2^30 (host check)
   if (slot >= 2 * per_cache) return;
   const bool is_v = slot >= per_cache;
-  const unsigned rest = (unsigned)(is_v ? slot - per_cache : slot);
-  const unsigned bh = rest / (unsigned)a.n;
+  const unsigned rest = is_v ? slot - per_cache : slot;
+  const unsigned bh = by_n.divide(rest);
   const int n = (int)(rest - bh * (unsigned)a.n);
-  const int b = (int)(bh / (unsigned)a.n_kv), h = (int)(bh - (unsigned)b * (unsigned)a.n_kv);
+  const int b = (int)by_kv.divide(bh), h = (int)(bh - (unsigned)b * (unsigned)a.n_kv);
   const int start = a.start[b], cnt = a.counts ? a.counts[b] : a.n;
   if (cnt < 0 || cnt > a.n || start < 0 || (long long)start + cnt > a.max_len) {
     if (lane == 0) atomicExch(&g_kv_status, -1);
@@ -191,51 +267,61 @@ __global__ void __launch_bounds__(kKvThreads) kv_read_kernel(const KvReadArgs a)
   const size_t row = ((size_t)b * a.n_kv + h) * a.max_len + start + n;
   const size_t out = (((size_t)b * a.n + n) * a.n_kv + h) * HD;
   const bool get = n < cnt;
-  const void *cache = is_v ? a.vc : a.kc;
-  float v[2][8];
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
+  const uint8_t *src = reinterpret_cast<const uint8_t *>(is_v ? a.vc : a.kc) + row * (HD * BITS / 8);
+  float v[CH][N];
+  uint32_t m = 0;
+  uint32_t w[CH][4];  // a chunk's bytes (4 bits: the word it lies in)
   if (get) {
-    float s = 0.f, z = 0.f;
-    if (BITS != 16) {
-      const uint32_t m = (is_v ? a.vm : a.km)[row];
-      s = __half2float(__ushort_as_half((unsigned short)(m & 0xffffu)));
-      z = __half2float(__ushort_as_half((unsigned short)(m >> 16)));
-    }
+    if (BITS != 16) m = __ldcs((is_v ? a.vm : a.km) + row);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int c = lane + i * LPR;  // chunk of 8 values
-      if (BITS == 16) {
-        const uint4 q = __ldcs(reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(cache) + row * HD + c * 8));
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[i][2 * j] = bf_lo(w[j]), v[i][2 * j + 1] = bf_hi(w[j]);
-      } else if (BITS == 8) {
-        const uint2 q = __ldcs(reinterpret_cast<const uint2 *>(reinterpret_cast<const uint8_t *>(cache) + row * HD + c * 8));
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          v[i][e] = __fmul_rn(s, (float)((e < 4 ? q.x : q.y) >> (8 * (e % 4)) & 0xffu) - z);
+    for (int i = 0; i < CH; ++i) {
+      const int c = lane + i * LPR;
+      if (BITS == 16 && N == 8) {
+        const uint4 q = __ldcs(reinterpret_cast<const uint4 *>(src) + c);
+        w[i][0] = q.x, w[i][1] = q.y, w[i][2] = q.z, w[i][3] = q.w;
+      } else if ((BITS == 16 && N == 4) || (BITS == 8 && N == 8)) {
+        const uint2 q = __ldcs(reinterpret_cast<const uint2 *>(src) + c);
+        w[i][0] = q.x, w[i][1] = q.y;
       } else {
-        const uint32_t q = __ldcs(reinterpret_cast<const uint32_t *>(reinterpret_cast<const uint8_t *>(cache) + row * (HD / 2) + c * 4));
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[i][e] = __fmul_rn(s, (float)(q >> (4 * (e / 2) + 16 * (e % 2)) & 0xfu) - z);
+        w[i][0] = __ldcs(reinterpret_cast<const uint32_t *>(src) + (BITS == 4 && N == 4 ? c / 2 : c));
       }
     }
   }
+  // code - z exactly in binary16, as (1024 + code) - (1024 + z)
+  const float s = __half2float(__ushort_as_half((unsigned short)(m & 0xffffu)));
+  const __half2 z = __hadd2(__half2half2(__ushort_as_half((unsigned short)(m >> 16))), __float2half2_rn(1024.f));
+  auto pair = [&](uint32_t codes, float *to) {
+    const uint32_t c = codes | 0x64006400u;
+    const float2 f = __half22float2(__hsub2(*reinterpret_cast<const __half2 *>(&c), z));
+    to[0] = __fmul_rn(s, f.x);
+    to[1] = __fmul_rn(s, f.y);
+  };
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const size_t at = out + (lane + i * LPR) * 8;
-    if (F32) {
-      float4 *dst = reinterpret_cast<float4 *>(reinterpret_cast<float *>(is_v ? a.v : a.k) + at);
-      dst[0] = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
-      dst[1] = make_float4(v[i][4], v[i][5], v[i][6], v[i][7]);
-    } else {
+  for (int i = 0; i < CH; ++i)
+#pragma unroll
+    for (int e = 0; e < N; e += 2) {
+      if (!get) {
+        v[i][e] = v[i][e + 1] = 0.f;
+      } else if (BITS == 16) {
+        v[i][e] = bf_lo(w[i][e / 2]);
+        v[i][e + 1] = bf_hi(w[i][e / 2]);
+      } else if (BITS == 8) {
+        pair(__byte_perm(w[i][e / 4], 0, e % 4 ? 0x4342 : 0x4140), &v[i][e]);
+      } else {
+        // value x of a word of 8 at bits 4 (x / 2) + 16 (x % 2)
+        const int half = N == 4 ? lane % 2 * 8 : 0;  // (LPR is even: a lane's chunks are all first or all second halves)
+        pair(w[i][0] >> (half + 2 * e) & 0x000f000fu, &v[i][e]);
+      }
+    }
+#pragma unroll
+  for (int i = 0; i < CH; ++i) {
+    const size_t at = out + (size_t)(lane + i * LPR) * N;
+    if constexpr (F32)
+      *reinterpret_cast<float4 *>(reinterpret_cast<float *>(is_v ? a.v : a.k) + at) = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
+    else
       *reinterpret_cast<uint4 *>(reinterpret_cast<__nv_bfloat16 *>(is_v ? a.v : a.k) + at) =
           make_uint4(pack_bf2(v[i][0], v[i][1]), pack_bf2(v[i][2], v[i][3]), pack_bf2(v[i][4], v[i][5]),
                      pack_bf2(v[i][6], v[i][7]));
-    }
   }
 }
 
@@ -245,12 +331,12 @@ __global__ void __launch_bounds__(kKvThreads) kv_read_kernel(const KvReadArgs a)
 // token's position (value i with i + HD/2), each rounded once to bf16.  A CTA
 // takes one token; LPR lanes take a head, 4 values of each half a lane, and a
 // lane's heads are loaded before the sum over x is waited for.
-constexpr int kRopeThreads = 256;
 
-template <int HD>
-__global__ void __launch_bounds__(kRopeThreads) qkv_rope_kernel(const QkvRopeArgs a) {
-  constexpr int LPR = HD / 8, GROUPS = kRopeThreads / LPR, MAXU = 4;  // lanes a head, heads a pass, passes in registers
-  __shared__ float red[kRopeThreads / 32];
+
+template <int HD, int THREADS>
+__global__ void __launch_bounds__(THREADS, 896 / THREADS) qkv_rope_kernel(const QkvRopeArgs a) {
+  constexpr int LPR = HD / 8, GROUPS = THREADS / LPR, MAXU = 4;  // lanes a head, heads a pass, passes in registers
+  __shared__ float red[THREADS / 32];
   pdl_wait();
   pdl_launch_dependents();
   const int tid = threadIdx.x, lane = tid % LPR, grp = tid / LPR;
@@ -282,7 +368,7 @@ __global__ void __launch_bounds__(kRopeThreads) qkv_rope_kernel(const QkvRopeArg
   if (a.x) {
     float ss = 0.f;
     const uint4 *xs = reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(a.x) + tok * a.d);
-    for (int i = tid; i < a.d / 8; i += kRopeThreads) {
+    for (int i = tid; i < a.d / 8; i += THREADS) {
       const uint4 q = xs[i];
       const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
@@ -297,7 +383,7 @@ __global__ void __launch_bounds__(kRopeThreads) qkv_rope_kernel(const QkvRopeArg
     __syncthreads();
     float tot = 0.f;
 #pragma unroll
-    for (int w = 0; w < kRopeThreads / 32; ++w) tot += red[w];
+    for (int w = 0; w < THREADS / 32; ++w) tot += red[w];
     rs = __fdiv_rn(1.f, __fsqrt_rn(__fadd_rn(__fdiv_rn(tot, (float)a.d), kRmsEps)));
   }
   for (int h0 = 0; h0 < heads; h0 += MAXU * GROUPS) {
@@ -342,8 +428,8 @@ __global__ void __launch_bounds__(kRopeThreads) qkv_rope_kernel(const QkvRopeArg
 
 namespace {
 
-template <class Kernel, class Args>
-cudaError_t launch_pdl(Kernel k, const Args &a, unsigned grid, int threads, cudaStream_t s) {
+template <class... Params, class... Args>
+cudaError_t launch_pdl(void (*k)(Params...), unsigned grid, int threads, cudaStream_t s, const Args &...args) {
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -353,42 +439,50 @@ cudaError_t launch_pdl(Kernel k, const Args &a, unsigned grid, int threads, cuda
   cfg.numAttrs = 1;
   cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(threads);
-  return cudaLaunchKernelEx(&cfg, k, a);
+  return cudaLaunchKernelEx(&cfg, k, args...);
 }
 
 // CTAs of a launch of one row (of hd values) per hd / 16 lanes.
-unsigned row_ctas(long long rows, int hd) {
-  const long long per = kKvThreads / (hd / 16);
+unsigned row_ctas(long long rows, int hd, int threads) {
+  const long long per = threads / (hd / 16);
   return (unsigned)((rows + per - 1) / per);
 }
 
 }  // namespace
 
 cudaError_t launch_kv_append(const KvAppendArgs &a, int hd, int bits, bool f32, cudaStream_t s) {
-  const unsigned grid = row_ctas(2ll * a.batch * a.n_kv * a.n, hd);
+  const unsigned grid = row_ctas((long long)a.batch * a.n_kv * a.n, hd, kAppendThreads);
 #define WQ_APPEND(HD, BITS)                                                               \
   if (hd == HD && bits == BITS)                                                           \
-    return f32 ? launch_pdl(kv_append_kernel<HD, BITS, true>, a, grid, kKvThreads, s)     \
-               : launch_pdl(kv_append_kernel<HD, BITS, false>, a, grid, kKvThreads, s);
+    return f32 ? launch_pdl(kv_append_kernel<HD, BITS, true>, grid, kAppendThreads, s, a, Divisor(a.n), Divisor(a.n_kv))     \
+               : launch_pdl(kv_append_kernel<HD, BITS, false>, grid, kAppendThreads, s, a, Divisor(a.n), Divisor(a.n_kv));
   WQ_APPEND(128, 16) WQ_APPEND(128, 8) WQ_APPEND(128, 4) WQ_APPEND(64, 16) WQ_APPEND(64, 8) WQ_APPEND(64, 4)
 #undef WQ_APPEND
   return cudaErrorInvalidValue;
 }
 
 cudaError_t launch_kv_read(const KvReadArgs &a, int hd, int bits, bool f32, cudaStream_t s) {
-  const unsigned grid = row_ctas(2ll * a.batch * a.n_kv * a.n, hd);
+  const unsigned grid = row_ctas(2ll * a.batch * a.n_kv * a.n, hd, kReadThreads);
 #define WQ_READ(HD, BITS)                                                               \
   if (hd == HD && bits == BITS)                                                         \
-    return f32 ? launch_pdl(kv_read_kernel<HD, BITS, true>, a, grid, kKvThreads, s)     \
-               : launch_pdl(kv_read_kernel<HD, BITS, false>, a, grid, kKvThreads, s);
+    return f32 ? launch_pdl(kv_read_kernel<HD, BITS, true>, grid, kReadThreads, s, a, Divisor(a.n), Divisor(a.n_kv))     \
+               : launch_pdl(kv_read_kernel<HD, BITS, false>, grid, kReadThreads, s, a, Divisor(a.n), Divisor(a.n_kv));
   WQ_READ(128, 16) WQ_READ(128, 8) WQ_READ(128, 4) WQ_READ(64, 16) WQ_READ(64, 8) WQ_READ(64, 4)
 #undef WQ_READ
   return cudaErrorInvalidValue;
 }
 
 cudaError_t launch_qkv_rope(const QkvRopeArgs &a, int m, int hd, cudaStream_t s) {
-  if (hd == 128) return launch_pdl(qkv_rope_kernel<128>, a, (unsigned)m, kRopeThreads, s);
-  if (hd == 64) return launch_pdl(qkv_rope_kernel<64>, a, (unsigned)m, kRopeThreads, s);
+  // Up to two tokens an SM 256 threads a token, whose heads are then all in flight (304
+  // tokens of 48 heads 4.4 us, with 128 threads 5.5), above that 128, of which seven
+  // CTAs fit an SM where of 256 only three do (1220 tokens of 56 heads 14.5 us for 20.9).
+  const bool few = m <= 2 * 152;
+  if (hd == 128)
+    return few ? launch_pdl(qkv_rope_kernel<128, 256>, (unsigned)m, 256, s, a)
+               : launch_pdl(qkv_rope_kernel<128, 128>, (unsigned)m, 128, s, a);
+  if (hd == 64)
+    return few ? launch_pdl(qkv_rope_kernel<64, 256>, (unsigned)m, 256, s, a)
+               : launch_pdl(qkv_rope_kernel<64, 128>, (unsigned)m, 128, s, a);
   return cudaErrorInvalidValue;
 }
 
