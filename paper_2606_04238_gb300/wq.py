@@ -550,6 +550,14 @@ def kv_cache(batch: int, n_kv: int, max_len: int, head_dim: int, bits: int = 16,
 _Strides = ctypes.c_int64 * 3
 
 
+def _out(t, dtype, shape, device, name):
+    """An output tensor and its address: ``t`` checked, or a new one."""
+    if t is not None:
+        return t, _at(t, dtype, shape, name)
+    t = torch.empty(shape, dtype=dtype, device=device)
+    return t, t.data_ptr()
+
+
 def _at(t, dtype, shape, name):
     """The address of a contiguous device tensor of this type and shape (None: NULL)."""
     if t is None:
@@ -582,13 +590,11 @@ def kv_read(cache: KVCache, start, n: int, counts=None, dtype=torch.bfloat16, k=
     assert dtype is torch.bfloat16 or dtype is torch.float32
     b = cache.batch
     shape = (b, n, cache.n_kv, cache.head_dim)
-    if k is None:
-        k = torch.empty(shape, dtype=dtype, device=cache._k.device)
-    if v is None:
-        v = torch.empty(shape, dtype=dtype, device=cache._k.device)
+    dev = cache._k.device
+    k, kp = _out(k, dtype, shape, dev, "k")
+    v, vp = _out(v, dtype, shape, dev, "v")
     _check(lib().wq_kv_read(cache._ref, _at(start, torch.int32, (b,), "start"), _at(counts, torch.int32, (b,), "counts"),
-                            n, _at(k, dtype, shape, "k"), _at(v, dtype, shape, "v"), 1 if dtype is torch.float32 else 0,
-                            _raw_stream()))
+                            n, kp, vp, 1 if dtype is torch.float32 else 0, _raw_stream()))
     return k, v
 
 
@@ -603,18 +609,13 @@ def qkv_rope(qkv, positions, table, n_heads: int, n_kv: int, x=None, head_norm: 
     """wq_qkv_rope: bf16 (q [m, n_heads, hd], k, v [m, n_kv, hd]) from fp32 projections [m, (n_heads + 2 n_kv) hd]."""
     m, n_pos, hd = qkv.shape[0], table.shape[0], 2 * table.shape[1]
     bf, f32, dev = torch.bfloat16, torch.float32, qkv.device
-    if q is None:
-        q = torch.empty((m, n_heads, hd), dtype=bf, device=dev)
-    if k is None:
-        k = torch.empty((m, n_kv, hd), dtype=bf, device=dev)
-    if v is None:
-        v = torch.empty((m, n_kv, hd), dtype=bf, device=dev)
+    q, qp = _out(q, bf, (m, n_heads, hd), dev, "q")
+    k, kp = _out(k, bf, (m, n_kv, hd), dev, "k")
+    v, vp = _out(v, bf, (m, n_kv, hd), dev, "v")
     d = 0 if x is None else x.shape[1]
     _check(lib().wq_qkv_rope(_at(qkv, f32, (m, (n_heads + 2 * n_kv) * hd), "qkv"), _at(x, bf, (m, d), "x"), m, d,
                              _at(positions, torch.int32, (m,), "positions"), _at(table, f32, (n_pos, hd // 2, 2), "table"),
-                             n_pos, n_heads, n_kv, hd, WQ_HEAD_NORM if head_norm else 0,
-                             _at(q, bf, (m, n_heads, hd), "q"), _at(k, bf, (m, n_kv, hd), "k"),
-                             _at(v, bf, (m, n_kv, hd), "v"), _raw_stream()))
+                             n_pos, n_heads, n_kv, hd, WQ_HEAD_NORM if head_norm else 0, qp, kp, vp, _raw_stream()))
     return q, k, v
 
 

@@ -128,6 +128,34 @@ def test_rows_at_the_edges_of_the_scale(wq, bits):
     assert torch.isnan(kr[0, 3:7]).all() and torch.isfinite(kr[0, :3]).all() and torch.isfinite(kr[0, 7:]).all()
 
 
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_quotients_at_and_beside_halves(wq, bits, hd):
+    """Values (j + 1/2) s, where v / s is rounded to even, and the fp32 values next to them: codes as the
+    fp32 quotient's, scales of binary16 from the smallest on.  A row holds -z s and (top - z) s, exactly in
+    fp32 and 19 bits, so that its scale is s and its zero z."""
+    top, n = 2 ** bits - 1, 96
+    g = torch.Generator().manual_seed(9)
+    s = torch.cat([torch.tensor([1.0, 3.0, 1023.0]) * 2.0 ** -24, torch.tensor([1.0, 0.1, 31.0]),
+                   2.0 ** (torch.rand(n - 6, generator=g) * 14 - 10)]).to(torch.float16).to(torch.float32)
+    z = torch.randint(0, top + 1, (n,), generator=g).float()
+    j = torch.floor(torch.rand((n, hd), generator=g) * top) - z[:, None]
+    v = (j + 0.5) * s[:, None]
+    bits_of = v.view(torch.int32) + torch.randint(-2, 3, (n, hd), generator=g, dtype=torch.int32) * (v != 0)
+    v = torch.minimum(torch.maximum(bits_of.view(torch.float32), -(z * s)[:, None]), ((top - z) * s)[:, None])
+    v[:, 0], v[:, 1] = -z * s, (top - z) * s
+    for dtype in (torch.float32, torch.bfloat16):
+        rows = v.to(dtype)[None, :, None]
+        c = wq.kv_cache(1, 1, n, hd, bits)
+        wq.kv_append(c, rows.cuda(), rows.cuda(), torch.zeros(1, dtype=torch.int32, device="cuda"))
+        _, q, sc, zc = stored(rows, bits)
+        if dtype is torch.float32:
+            assert torch.equal(sc.flatten(), s.double()) and torch.equal(zc.flatten(), z.double())
+        for which in "kv":
+            assert torch.equal(_codes(c, which)[0, 0], q[0, :, 0].to(torch.int64))
+            assert _same(_meta(c, which)[0][0, 0], sc[0, :, 0]) and _same(_meta(c, which)[1][0, 0], zc[0, :, 0])
+
+
 @pytest.mark.parametrize("bits", [16, 8, 4])
 def test_accepted_path_and_counts(wq, bits):
     b, t, h, hd, n, L = 4, 37, 3, 64, 9, 50
