@@ -913,7 +913,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
 // o of the rows whose block was split: HD / 4 lanes a row, its parts in split order.
 template <int HD>
 __global__ void __launch_bounds__(256) attn_tree_merge_kernel(const TreeArgs a) {
-  constexpr int LPR = HD / 4, CU = 8;  // splits loaded in one round trip
+  constexpr int LPR = HD / 4, CU = 2;  // splits loaded in one round trip (8: half as many warps fit, 1.2 us more)
   const int rep = a.H / a.Hkv, R = a.T * rep;
   const long long row = (long long)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
   const int c = threadIdx.x % LPR;

@@ -9,6 +9,7 @@ calls raise.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 
@@ -547,7 +548,10 @@ def kv_cache(batch: int, n_kv: int, max_len: int, head_dim: int, bits: int = 16,
     return KVCache(k, v, km, vm, head_dim, bits)
 
 
-_Strides = ctypes.c_int64 * 3
+@functools.lru_cache(maxsize=256)
+def _strides(s):
+    """The first three strides as the C ABI takes them."""
+    return (ctypes.c_int64 * 3)(*s[:3])
 
 
 def _out(t, dtype, shape, device, name):
@@ -571,17 +575,16 @@ def kv_append(cache: KVCache, k, v, start, counts=None, index=None):
     """wq_kv_append: rows k, v (bf16 or fp32 [batch, T, n_kv, head_dim], any strides of the first
     three dimensions that are multiples of 16 bytes) quantized into the cache at positions
     start[b] + i; ``index`` [batch, n] picks the source token of row i, ``counts`` [batch] how many."""
-    b, t = cache.batch, k.shape[1]
-    dt = k.dtype
+    b, dt, shape = cache.batch, k.dtype, k.shape
+    t = shape[1]
     assert dt is torch.bfloat16 or dt is torch.float32
-    assert k.shape == (b, t, cache.n_kv, cache.head_dim) and v.shape == k.shape and v.dtype is dt
-    assert k.is_cuda and v.is_cuda
+    assert shape == (b, t, cache.n_kv, cache.head_dim) and v.shape == shape and v.dtype is dt
     ks, vs = k.stride(), v.stride()
-    assert ks[3] == 1 and vs[3] == 1
+    assert ks[3] == 1 and vs[3] == 1 and k.is_cuda and v.is_cuda
     n = t if index is None else index.shape[1]
     i32 = torch.int32
     _check(lib().wq_kv_append(cache._ref, k.data_ptr(), v.data_ptr(), 1 if dt is torch.float32 else 0, t,
-                              _Strides(*ks[:3]), _Strides(*vs[:3]), _at(start, i32, (b,), "start"),
+                              _strides(ks), _strides(vs), _at(start, i32, (b,), "start"),
                               _at(counts, i32, (b,), "counts"), _at(index, i32, (b, n), "index"), n, _raw_stream()))
 
 

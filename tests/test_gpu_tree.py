@@ -166,6 +166,24 @@ def test_many_drafts(wq, room, bits, hd, H, kv):
     close(*run(wq, room, 1, 64, H, kv, hd, bits, [2048], seed=4))  # a chain: mask None
 
 
+@pytest.mark.parametrize("bits,hd", [(16, 128), (8, 64), (4, 128)])
+def test_more_row_blocks_than_ctas(wq, room, bits, hd):
+    """45 x 8 heads of up to three drafts, lengths and counts of zero among them: a CTA takes several."""
+    g = torch.Generator().manual_seed(3)
+    lens = [int(x) for x in torch.randint(0, 700, (45,), generator=g)]
+    counts = [int(x) for x in torch.randint(0, 4, (45,), generator=g)]
+    lens[0], lens[7], lens[8], lens[44], counts[44], counts[5], counts[6] = 0, 0, 0, 640, 0, 0, 0
+    close(*run(wq, room, 45, 3, 16, 8, hd, bits, lens, counts=counts, parents=tree(45, 3, 1), seed=21))
+
+
+@pytest.mark.parametrize("bits,hd", [(16, 64), (8, 128), (4, 64)])
+def test_uneven_row_blocks(wq, room, bits, hd):
+    """Two to four row blocks a head, 2 to 32 tiles each: the ends of some and the begins of the next go to one CTA."""
+    lens = [3832, 2316, 1272, 1492, 3947, 2660, 1, 2751]
+    counts = [33, 42, 50, 50, 48, 60, 46, 41]
+    close(*run(wq, room, 8, 61, 64, 8, hd, bits, lens, counts=counts, parents=tree(8, 61, 2), seed=22))
+
+
 @pytest.mark.parametrize("bits", [16, 8, 4])
 def test_rows_that_see_nothing(wq, room, bits):
     b, t = 3, 20
