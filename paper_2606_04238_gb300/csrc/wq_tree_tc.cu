@@ -23,7 +23,7 @@
 // Measured (device time): 4 sequences of 9,400 to 15,600 positions in 4 bits, 47 to 61
 // drafts, 40 query heads over 8 kv heads of 128: 91 us, 440 TFLOP/s of products that
 // count.  8 sequences of 1,300 to 3,900 positions in bf16, 33 to 60 drafts, 64 heads over
-// 8 of 64: 56 us.  16 sequences of 580 to 1,950 positions in 8 bits, 4 to 8 drafts: 33 us,
+// 8 of 64: 55 us.  16 sequences of 580 to 1,950 positions in 8 bits, 4 to 8 drafts: 34 us,
 // of which 7 until the queries are in place and 8 from the last tile to the merged rows.
 // A tile of 128 positions takes a CTA 1.8 us (bf16, 64) to 2.9 us (4 bits, 128) with two
 // CTAs an SM, 1.6 and 2.3 alone.  No one part bounds it: half the issue slots, 55% of the
@@ -213,11 +213,12 @@ __device__ __forceinline__ int ceil_div(int a, int b, float rb) {
 __device__ Work find_work(const TreeArgs &a, int rep, int cta) {
   const int lane = threadIdx.x & 31;
   int len = 0, cnt = 0, tiles = 0, blocks = 0;
-  long long total = 0, many = 0;
+  unsigned total = 0, many = 0;  // (32 bits: tiles x kv heads x row blocks of what fits in memory)
+  const unsigned target = (unsigned)a.target;
   int most = 1;
   for (int b = lane; b < a.batch; b += 32) {
     seq_tiles(a, b, rep, len, cnt, tiles, blocks);
-    total += (long long)tiles * blocks;
+    total += tiles * blocks;
     many += blocks;
     most = max(most, tiles);
   }
@@ -230,13 +231,13 @@ __device__ Work find_work(const TreeArgs &a, int rep, int cta) {
   total *= a.Hkv;
   many *= a.Hkv;
   int W = most;
-  if (many < a.target && most > a.min_tiles) {
+  if (many < target && most > a.min_tiles) {
     // sum ceil(tiles / W) <= total / W + many: no more than `target` at hi
-    const int lo = max(a.min_tiles, (int)((total + a.target - 1) / a.target));
-    const int hi = min(most, max(lo, (int)((total + (a.target - many) - 1) / (a.target - many))));
-    const int cand = lo + (int)((long long)(hi - lo) * lane / 31);
+    const int lo = max(a.min_tiles, (int)((total + target - 1) / target));
+    const int hi = min(most, max(lo, (int)((total + (target - many) - 1) / (target - many))));
+    const int cand = lo + (hi - lo) / 31 * lane + (hi - lo) % 31 * lane / 31;
     const float rc = __frcp_rn((float)cand);
-    long long n = 0;
+    unsigned n = 0;
     for (int b0 = 0; b0 < a.batch; b0 += 32) {
       if (a.batch > 32) {
         tiles = blocks = 0;
@@ -247,14 +248,14 @@ __device__ Work find_work(const TreeArgs &a, int rep, int cta) {
       for (int j = 0; j < m; ++j)
         n += ceil_div(__shfl_sync(0xffffffffu, tiles, j), cand, rc) * __shfl_sync(0xffffffffu, blocks, j);
     }
-    const unsigned fits = __ballot_sync(0xffffffffu, n * a.Hkv <= a.target);
+    const unsigned fits = __ballot_sync(0xffffffffu, n * a.Hkv <= target);
     W = __shfl_sync(0xffffffffu, cand, fits ? __ffs(fits) - 1 : 31);
   }
   const float rw = __frcp_rn((float)W);
   // the sequence this CTA falls into
   Work w;
   w.any = false;
-  long long base = 0;
+  unsigned base = 0;
   for (int b0 = 0; b0 < a.batch; b0 += 32) {
     const int b = b0 + lane;
     if (a.batch > 32) {
@@ -268,7 +269,7 @@ __device__ Work find_work(const TreeArgs &a, int rep, int cta) {
       const int up = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += up;
     }
-    const unsigned hit = __ballot_sync(0xffffffffu, cta < base + incl);
+    const unsigned hit = __ballot_sync(0xffffffffu, cta < (int)(base + incl));
     if (cta == 0 && b < a.batch) {
       a.table[b] = make_int4((int)(base + incl - mine), n, blocks, cnt);
       if (tiles == 0) atomicExch(&g_tree_tc_status, -1);
@@ -286,8 +287,9 @@ __device__ Work find_work(const TreeArgs &a, int rep, int cta) {
       w.rb = i % rbs;
       w.g = i / rbs % a.Hkv;
       w.split = i / (rbs * a.Hkv);
-      w.t0 = (int)((long long)nt * w.split / w.n);
-      w.t1 = (int)((long long)nt * (w.split + 1) / w.n);
+      const int each = nt / w.n, more = nt - each * w.n;  // nt split / n = each split + more split / n
+      w.t0 = each * w.split + more * w.split / w.n;
+      w.t1 = each * (w.split + 1) + more * (w.split + 1) / w.n;
       w.slot = cta;
       if (cta != 0) break;
     }
