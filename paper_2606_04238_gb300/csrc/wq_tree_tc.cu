@@ -21,14 +21,14 @@
 // Ranges of one row block that is split are merged by a second kernel.
 //
 // Measured (device time): 4 sequences of 9,400 to 15,600 positions in 4 bits, 47 to 61
-// drafts, 40 query heads over 8 kv heads of 128: 91 us, 440 TFLOP/s of products that
+// drafts, 40 query heads over 8 kv heads of 128: 88 us, 460 TFLOP/s of products that
 // count.  8 sequences of 1,300 to 3,900 positions in bf16, 33 to 60 drafts, 64 heads over
 // 8 of 64: 55 us.  16 sequences of 580 to 1,950 positions in 8 bits, 4 to 8 drafts: 34 us,
 // of which 7 until the queries are in place and 8 from the last tile to the merged rows.
 // A tile of 128 positions takes a CTA 1.8 us (bf16, 64) to 2.9 us (4 bits, 128) with two
-// CTAs an SM, 1.6 and 2.3 alone.  No one part bounds it: half the issue slots, 55% of the
-// tensor pipe's cycles and 60% of shared memory's bandwidth are in use, and copies that
-// leave out the exponentials, the conversion or either product are at most 8% faster.
+// CTAs an SM, 1.6 and 2.3 alone.  No one part bounds it: about half the issue slots, half
+// the tensor rate (whole tiles) and 60% of shared memory's bandwidth are in use, and copies
+// that leave out the exponentials, the conversion or either product are at most 8% faster.
 // Scores and outputs in halves of 64 positions, so that a half's softmax runs beside the
 // other's products, gained nothing (57 -> 56 and 92 -> 96 us): a row's thread then never
 // waits, and its own instructions, ~4 clocks each, are the chain.  64 columns a thread at
@@ -849,9 +849,9 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
       named_barrier_sync(2, 128);
       const bool whole = w.n == 1;
       const bool odd = w.t0 < ndr && (sh.odd[0] | sh.odd[1] | sh.odd[2] | sh.odd[3]) != 0;
-      // CK lanes a row
+      // CK lanes a row (one row a turn: four took 2.5 us more at 64 drafts, code that every CTA fetches once)
       const int c = tid % CK;
-#pragma unroll 4
+#pragma unroll 1
       for (int lrow = tid / CK; lrow < live; lrow += 128 / CK) {
         float M = sm[lrow], L = sl[lrow];
         float4 o = stage[lrow * CK + (c ^ (lrow & (CK - 1)))];
