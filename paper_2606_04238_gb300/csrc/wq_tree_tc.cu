@@ -698,7 +698,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
       tc_fence_after();
       if (busy) {
         // which of the tile's positions count: the drafts the row sees, those before the length
-        const bool drafts = tile < ndr;
+        const bool drafts = tile < ndr, search = i == 0 || (i == 1 && w.t0 < ndr);
         const int left = drafts ? w.cnt : w.len - (tile - ndr) * kTile;
         const bool some = drafts || left < kTile;
         auto seen = [&](int h) {
@@ -782,13 +782,14 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
           // columns 16 h ..: S's there have been read
           tmem_st16(tw + 16 * h, p);
         };
-        if (i >= 2 && copies == 1 && !some) {
+        if (!search && copies == 1 && !some) {
           // four times in a row: a row's work is bound by latency, which the next columns' loads then overlap
 #pragma unroll
           for (int h = 0; h < 4; ++h) probabilities(h, false);
         } else {
-          // A range's first two tiles (the drafts', the context's first) set the maximum from all their scores.
-          if (i < 2) {
+          // A range's first tile, the drafts' and the first of the context set the maximum from all their scores (with
+          // the drafts' alone to go by, raises in the tiles after it took 6 us of 61).
+          if (search) {
             float mx = -INFINITY;
 #pragma unroll 1
             for (int h = 0; h < 4; ++h) {
