@@ -1482,12 +1482,14 @@ constexpr int kMaxDrafts = 128;
 // device alone, the bound is on the cache's positions.
 //   heads of 128, bf16:   131k (32 rows, 1 x 8192) 19.0 / 25.3, 262k (32 rows, 16 x 1024) 33.5 / 23.1, 262k (16 rows,
 //                         1 x 32768) 32.4 / 39.8, 524k (16 rows, 16 x 4096) 48.9 / 41.3
-//   heads of 128, 8 bits: 262k (64 rows, 1 x 8192) 25.9 / 30.7, 524k (32 rows, 4 x 8192) 36.9 / 33.0, 524k (16 rows,
-//                         16 x 4096) 41.4 / 46.3
+//   heads of 128, 8 bits: 262k (64 rows, 1 x 8192) 24.0 / 27.8, 524k (64 rows, 2 x 8192) 30.4 / 26.9
+//   16 rows, 8 and 4 bits: 262k (1 x 32768) 23.7 / 39.0, 524k (4 x 16384) 32.0 / 43.2, 786k (4 x 24576) 42.3 / 58.7, heads
+//                         of 64 262k (8 x 4096) 16.8 / 22.0: a row costs mma.sync less at any length
 //   heads of 64, bf16:    262k (64 rows, 4 x 2048) 14.3 / 16.1, 524k (128 rows, 4 x 2048) 26.0 / 17.6
 bool tree_on_tcgen05(int batch, int T, int H, int Hkv, int hd, int bits, int max_len) {
   const long long tiles = ((long long)T * (H / Hkv) + 15) / 16;
   const double work = (double)tiles * batch * Hkv * max_len;
+  if (tiles == 1 && bits != 16) return false;
   return work > (tiles == 1 ? 400e3 : 250e3) * (bits == 16 ? 1.0 : 1.25) * (hd == 64 ? 1.5 : 1.0);
 }
 

@@ -31,14 +31,12 @@
 // fixed order.
 //
 // Measured (device time): one token over 500 positions of 8 bits, 32 query heads over
-// 8 kv heads of 128, 7.0 us, all latency: launch, the lengths, one round of loads, the
-// cluster's exchange.  Four drafts over 32,767 positions of 4 bits 27 us, 1.3 TB/s: 7
-// until queries and first tile are there (all CTAs' rings are asked for at once), 1.5 a
-// tile after that, 2.5 for a CTA's results and 3.5 for the second kernel.  A warp's 16
-// positions of a tile take 545 instructions, of which 200 make fragments and products;
-// three warps a scheduler issue 0.6 a clock.  Scales fetched three tiles ahead and V
-// rows that meet in fewer banks changed nothing, queries before the rings' other tiles
-// cost 1 us (spilled registers).
+// 8 kv heads of 128, 6.6 us, all latency: launch, the lengths, one round of loads, the
+// cluster's exchange.  Four drafts over 32,767 positions of 4 bits 23.6 us, 1.5 TB/s: 3
+// until queries and first tile are there, 1.5 a tile after that, 2.5 for a CTA's results
+// and 3.5 for the second kernel.  A warp's 16 positions of a tile take 545 instructions,
+// of which 200 make fragments and products; three warps a scheduler issue 0.6 a clock.
+// Scales fetched three tiles ahead and V rows that meet in fewer banks changed nothing.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cooperative_groups.h>

@@ -928,10 +928,11 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
   }
 }
 
-// o of the rows whose block was split: HD / 4 lanes a row, its parts in split order.
-template <int HD>
+// o of the rows whose block was split: HD / 4 lanes a row, its parts in split order,
+// CU of them loaded in one round trip.
+template <int HD, int CU>
 __global__ void __launch_bounds__(256) attn_tree_merge_kernel(const TreeArgs a) {
-  constexpr int LPR = HD / 4, CU = 2;  // splits loaded in one round trip (8: half as many warps fit, 1.2 us more)
+  constexpr int LPR = HD / 4;
   const int rep = a.H / a.Hkv, R = a.T * rep;
   const long long row = (long long)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
   const int c = threadIdx.x % LPR;
@@ -998,7 +999,7 @@ cudaError_t prepare_tc() {
 }
 
 template <int HD, int BITS>
-cudaError_t launch_tree_tc_t(const TreeArgs &a, unsigned grid, bool merge, cudaStream_t s) {
+cudaError_t launch_tree_tc_t(const TreeArgs &a, unsigned grid, bool merge, bool many, cudaStream_t s) {
   constexpr int sm = Cfg<HD, BITS>::SMEM;
   cudaError_t e = prepare_tc<HD, BITS>();
   if (e != cudaSuccess) return e;
@@ -1018,7 +1019,7 @@ cudaError_t launch_tree_tc_t(const TreeArgs &a, unsigned grid, bool merge, cudaS
   cfg.gridDim = dim3((unsigned)((rows * (HD / 4) + 255) / 256));
   cfg.blockDim = dim3(256);
   cfg.dynamicSmemBytes = 0;
-  return cudaLaunchKernelEx(&cfg, attn_tree_merge_kernel<HD>, a);
+  return cudaLaunchKernelEx(&cfg, many ? attn_tree_merge_kernel<HD, 8> : attn_tree_merge_kernel<HD, 2>, a);
 }
 
 }  // namespace
@@ -1044,9 +1045,12 @@ cudaError_t launch_attn_tree_tc(TreeArgs a, int hd, int bits, int num_sms, cudaS
   a.rep_magic = (65536 + rep - 1) / rep;  // row / rep = row rep_magic >> 16 for row < 65536 / (rep - 1)
   const long long tiles = ((long long)a.max_len + kTile - 1) / kTile + (a.T + kTile - 1) / kTile;
   const unsigned grid = (unsigned)std::max(blocks, std::min((long long)a.target, blocks * tiles));
+  // Few row blocks are split often and are few rows: eight parts in one round trip (38 parts a block: a call 39.0 us
+  // for 45.3); else two, as more warps then fit (2 parts of 488 rows, 64 heads: 1.2 us less).
+  const bool many = blocks * 8 <= a.target;
   const bool merge = blocks < a.target && tiles > a.min_tiles;  // else every row block is one range
 #define WQ_TREE(HD, BITS) \
-  if (hd == HD && bits == BITS) return launch_tree_tc_t<HD, BITS>(a, grid, merge, s);
+  if (hd == HD && bits == BITS) return launch_tree_tc_t<HD, BITS>(a, grid, merge, many, s);
   WQ_TREE(128, 16) WQ_TREE(128, 8) WQ_TREE(128, 4) WQ_TREE(64, 16) WQ_TREE(64, 8) WQ_TREE(64, 4)
 #undef WQ_TREE
   return cudaErrorInvalidValue;
