@@ -21,7 +21,7 @@
 // Ranges of one row block that is split are merged by a second kernel.
 //
 // Measured (device time): 4 sequences of 9,400 to 15,600 positions in 4 bits, 47 to 61
-// drafts, 40 query heads over 8 kv heads of 128: 88 us, 460 TFLOP/s of products that
+// drafts, 40 query heads over 8 kv heads of 128: 87 us, 465 TFLOP/s of products that
 // count.  8 sequences of 1,300 to 3,900 positions in bf16, 33 to 60 drafts, 64 heads over
 // 8 of 64: 55 us.  16 sequences of 580 to 1,950 positions in 8 bits, 4 to 8 drafts: 34 us,
 // of which 7 until the queries are in place and 8 from the last tile to the merged rows.
