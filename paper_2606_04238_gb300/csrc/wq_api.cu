@@ -1521,6 +1521,9 @@ wq_status check_dtype(int dtype) {
   return dtype == WQ_BF16 || dtype == WQ_F32 ? WQ_OK : fail(WQ_ERR_ARG, "dtype %d", dtype);
 }
 
+// The tcgen05 kernel's plan at the workspace's start: an int4 a sequence and one more.
+size_t tree_table_bytes(int batch) { return up256(sizeof(int4) * ((size_t)batch + 1)); }
+
 wq_status attn_tree_impl(const void *q, const void *k_new, const void *v_new, int n_draft, int n_heads,
                          const wq_kv_cache *c, const int32_t *lens, const int32_t *counts, const uint32_t *mask,
                          float scale, void *o, void *ws, size_t ws_bytes, cudaStream_t s) {
@@ -1545,7 +1548,7 @@ wq_status attn_tree_impl(const void *q, const void *k_new, const void *v_new, in
   a.batch = c->batch, a.T = n_draft, a.H = n_heads, a.Hkv = c->n_kv, a.max_len = c->max_len, a.words = (n_draft + 31) / 32;
   a.scale = scale * 1.4426950408889634f;  // scores in units of log 2
   a.table = static_cast<int4 *>(ws);
-  a.part = reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + up256(sizeof(int4) * (size_t)c->batch));
+  a.part = reinterpret_cast<float *>(static_cast<uint8_t *>(ws) + tree_table_bytes(c->batch));
   a.o = o;
   cudaError_t e;
   if (scale != 0.f && tree_on_tcgen05(c->batch, n_draft, n_heads, c->n_kv, c->head_dim, c->bits, c->max_len)) {
@@ -1632,7 +1635,7 @@ size_t wq_attn_tree_workspace_bytes(int batch, int n_draft, int n_heads, int n_k
   const int sms = num_sms();
   if (batch <= 0 || n_draft <= 0 || n_heads <= 0 || n_kv <= 0 || head_dim <= 0 || max_len <= 0 || sms <= 0) return 0;
   if (n_heads % n_kv != 0) return 0;
-  return up256(sizeof(int4) * (size_t)batch) +
+  return tree_table_bytes(batch) +
          up256(4 * std::max(tree_part_floats(batch, n_draft, n_heads, n_kv, head_dim, max_len, sms),
                             tree_tc_part_floats(batch, n_draft, n_heads, n_kv, head_dim, max_len, sms)));
 }

@@ -40,6 +40,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <climits>
 #include <cstdint>
 
 #include "wq_internal.h"
@@ -210,6 +211,7 @@ __device__ __forceinline__ int ceil_div(int a, int b, float rb) {
 
 // One warp, every CTA the same sums.  Ranges of W tiles: W the least of 32 candidates, from the tiles a CTA of an even
 // split would take up to what certainly gives no more than `target` ranges; then this CTA's range.
+// Whole row blocks, W the most tiles, where they are `target` already or the host launches no merge.
 __device__ Work find_work(const TreeArgs &a, int rep, int cta) {
   const int lane = threadIdx.x & 31;
   int len = 0, cnt = 0, tiles = 0, blocks = 0;
@@ -231,7 +233,7 @@ __device__ Work find_work(const TreeArgs &a, int rep, int cta) {
   total *= a.Hkv;
   many *= a.Hkv;
   int W = most;
-  if (many < target && most > a.min_tiles) {
+  if (a.split && many < target && most > a.min_tiles) {
     // sum ceil(tiles / W) <= total / W + many: no more than `target` at hi
     const int lo = max(a.min_tiles, (int)((total + target - 1) / target));
     const int hi = min(most, max(lo, (int)((total + (target - many) - 1) / (target - many))));
@@ -251,6 +253,7 @@ __device__ Work find_work(const TreeArgs &a, int rep, int cta) {
     const unsigned fits = __ballot_sync(0xffffffffu, n * a.Hkv <= target);
     W = __shfl_sync(0xffffffffu, cand, fits ? __ffs(fits) - 1 : 31);
   }
+  if (cta == 0 && lane == 0) a.table[a.batch] = make_int4(W < most, 0, 0, 0);
   const float rw = __frcp_rn((float)W);
   // the sequence this CTA falls into
   Work w;
@@ -929,51 +932,55 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
 }
 
 // o of the rows whose block was split: HD / 4 lanes a row, its parts in split order,
-// CU of them loaded in one round trip.
+// CU of them loaded in one round trip.  A launch that most likely has nothing to merge has
+// few CTAs, which take the rows in turn.
 template <int HD, int CU>
 __global__ void __launch_bounds__(256) attn_tree_merge_kernel(const TreeArgs a) {
   constexpr int LPR = HD / 4;
   const int rep = a.H / a.Hkv, R = a.T * rep;
-  const long long row = (long long)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
   const int c = threadIdx.x % LPR;
-  const int bg = (int)(row / R), r = (int)(row - (long long)bg * R), b = bg / a.Hkv, g = bg % a.Hkv;
   pdl_wait();
   pdl_launch_dependents();
-  if (row >= (long long)a.batch * a.Hkv * R) return;
-  const int4 tab = a.table[b];  // first range, splits, row blocks, drafts
-  if (tab.y <= 1 || r >= tab.w * rep) return;  // written by the first kernel, or skipped
-  const size_t step = (size_t)a.Hkv * tab.z * a.part_rows * (HD + 4);
-  const float *pt = a.part + ((size_t)(tab.x + g * tab.z + r / kTcRows) * a.part_rows + r % kTcRows) * (HD + 4);
-  float M = -INFINITY, L = 0.f;
-  float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int s0 = 0; s0 < tab.y; s0 += CU) {
-    float2 ml[CU];
-    float4 ov[CU];
-    float mn = M;
+  if (a.table[a.batch].x == 0) return;
+#pragma unroll 1
+  for (long long row = (long long)blockIdx.x * (256 / LPR) + threadIdx.x / LPR; row < (long long)a.batch * a.Hkv * R;
+       row += (long long)gridDim.x * (256 / LPR)) {
+    const int bg = (int)(row / R), r = (int)(row - (long long)bg * R), b = bg / a.Hkv, g = bg % a.Hkv;
+    const int4 tab = a.table[b];  // first range, splits, row blocks, drafts
+    if (tab.y <= 1 || r >= tab.w * rep) continue;  // written by the first kernel, or skipped
+    const size_t step = (size_t)a.Hkv * tab.z * a.part_rows * (HD + 4);
+    const float *pt = a.part + ((size_t)(tab.x + g * tab.z + r / kTcRows) * a.part_rows + r % kTcRows) * (HD + 4);
+    float M = -INFINITY, L = 0.f;
+    float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s0 = 0; s0 < tab.y; s0 += CU) {
+      float2 ml[CU];
+      float4 ov[CU];
+      float mn = M;
 #pragma unroll
-    for (int j = 0; j < CU; ++j) {
-      const float *ps = pt + (size_t)(s0 + j) * step;
-      const bool in = s0 + j < tab.y;
-      ml[j] = in ? *reinterpret_cast<const float2 *>(ps + HD) : make_float2(-INFINITY, 0.f);
-      ov[j] = in ? *reinterpret_cast<const float4 *>(ps + 4 * c) : make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int j = 0; j < CU; ++j) {
+        const float *ps = pt + (size_t)(s0 + j) * step;
+        const bool in = s0 + j < tab.y;
+        ml[j] = in ? *reinterpret_cast<const float2 *>(ps + HD) : make_float2(-INFINITY, 0.f);
+        ov[j] = in ? *reinterpret_cast<const float4 *>(ps + 4 * c) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+#pragma unroll
+      for (int j = 0; j < CU; ++j) mn = fmaxf(mn, ml[j].x);
+      const float f0 = M == -INFINITY ? 0.f : ex2(M - mn);
+      M = mn;
+      L *= f0;
+      O.x *= f0, O.y *= f0, O.z *= f0, O.w *= f0;
+#pragma unroll
+      for (int j = 0; j < CU; ++j) {
+        const float f = ml[j].x == -INFINITY ? 0.f : ex2(ml[j].x - M);  // (a NaN of a part stays NaN)
+        L = fmaf(ml[j].y, f, L);
+        O.x = fmaf(ov[j].x, f, O.x), O.y = fmaf(ov[j].y, f, O.y), O.z = fmaf(ov[j].z, f, O.z), O.w = fmaf(ov[j].w, f, O.w);
+      }
     }
-#pragma unroll
-    for (int j = 0; j < CU; ++j) mn = fmaxf(mn, ml[j].x);
-    const float f0 = M == -INFINITY ? 0.f : ex2(M - mn);
-    M = mn;
-    L *= f0;
-    O.x *= f0, O.y *= f0, O.z *= f0, O.w *= f0;
-#pragma unroll
-    for (int j = 0; j < CU; ++j) {
-      const float f = ml[j].x == -INFINITY ? 0.f : ex2(ml[j].x - M);  // (a NaN of a part stays NaN)
-      L = fmaf(ml[j].y, f, L);
-      O.x = fmaf(ov[j].x, f, O.x), O.y = fmaf(ov[j].y, f, O.y), O.z = fmaf(ov[j].z, f, O.z), O.w = fmaf(ov[j].w, f, O.w);
-    }
+    const bool none = M == -INFINITY && L == 0.f;
+    *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(a.o) +
+                               (((size_t)b * a.T + r / rep) * a.H + g * rep + r % rep) * HD + 4 * c) =
+        none ? make_uint2(0, 0) : make_uint2(pack_bf2(O.x / L, O.y / L), pack_bf2(O.z / L, O.w / L));
   }
-  const bool none = M == -INFINITY && L == 0.f;
-  *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(a.o) +
-                             (((size_t)b * a.T + r / rep) * a.H + g * rep + r % rep) * HD + 4 * c) =
-      none ? make_uint2(0, 0) : make_uint2(pack_bf2(O.x / L, O.y / L), pack_bf2(O.z / L, O.w / L));
 }
 
 namespace {
@@ -999,7 +1006,7 @@ cudaError_t prepare_tc() {
 }
 
 template <int HD, int BITS>
-cudaError_t launch_tree_tc_t(const TreeArgs &a, unsigned grid, bool merge, bool many, cudaStream_t s) {
+cudaError_t launch_tree_tc_t(const TreeArgs &a, unsigned grid, int merge_ctas, bool many, cudaStream_t s) {
   constexpr int sm = Cfg<HD, BITS>::SMEM;
   cudaError_t e = prepare_tc<HD, BITS>();
   if (e != cudaSuccess) return e;
@@ -1014,9 +1021,9 @@ cudaError_t launch_tree_tc_t(const TreeArgs &a, unsigned grid, bool merge, bool 
   cfg.blockDim = dim3(kTcThreads);
   cfg.dynamicSmemBytes = sm;
   e = cudaLaunchKernelEx(&cfg, attn_tree_tc_kernel<HD, BITS>, a);
-  if (e != cudaSuccess || !merge) return e;
+  if (e != cudaSuccess || !a.split) return e;
   const long long rows = (long long)a.batch * a.H * a.T;
-  cfg.gridDim = dim3((unsigned)((rows * (HD / 4) + 255) / 256));
+  cfg.gridDim = dim3((unsigned)std::min((rows * (HD / 4) + 255) / 256, (long long)merge_ctas));
   cfg.blockDim = dim3(256);
   cfg.dynamicSmemBytes = 0;
   return cudaLaunchKernelEx(&cfg, many ? attn_tree_merge_kernel<HD, 8> : attn_tree_merge_kernel<HD, 2>, a);
@@ -1048,9 +1055,13 @@ cudaError_t launch_attn_tree_tc(TreeArgs a, int hd, int bits, int num_sms, cudaS
   // Few row blocks are split often and are few rows: eight parts in one round trip (38 parts a block: a call 39.0 us
   // for 45.3); else two, as more warps then fit (2 parts of 488 rows, 64 heads: 1.2 us less).
   const bool many = blocks * 8 <= a.target;
-  const bool merge = blocks < a.target && tiles > a.min_tiles;  // else every row block is one range
+  // Row blocks are split where those of the drafts that exist are fewer than `target`: the device knows the counts, the
+  // host only whether there are any.  Without them a call of `target` row blocks is never split and has no merge
+  // to launch.  With them it may be, and where the counts are full the merge finds nothing to do (1.3 us: 20 sequences
+  // of 61 drafts over 500 positions 53.4 for 52.1; of 15 in the same places 22.2).
+  a.split = tiles > a.min_tiles && (blocks < a.target || a.counts != nullptr);
 #define WQ_TREE(HD, BITS) \
-  if (hd == HD && bits == BITS) return launch_tree_tc_t<HD, BITS>(a, grid, merge, many, s);
+  if (hd == HD && bits == BITS) return launch_tree_tc_t<HD, BITS>(a, grid, blocks < a.target ? INT_MAX : 2 * a.target, many, s);
   WQ_TREE(128, 16) WQ_TREE(128, 8) WQ_TREE(128, 4) WQ_TREE(64, 16) WQ_TREE(64, 8) WQ_TREE(64, 4)
 #undef WQ_TREE
   return cudaErrorInvalidValue;
