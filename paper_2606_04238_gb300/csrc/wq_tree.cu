@@ -11,10 +11,12 @@
 // point (wq_kv.cu), and code - z is exact in binary16.  So K's scale multiplies
 // the score, and V's scale is taken into the exponent:
 //   y_j = x_j + log2 s_j,  p_j = 2^(y_j - m),  o = sum_j p_j (code - z)_j / sum_j p_j / s_j,
-// with m the running maximum of y.  p_j then fills binary16's range whatever V's
-// scales are; p_j (bf16 for a bf16 cache) and q (bf16 given; for a quantized
-// cache binary16 with an exact power of two a row) are the products' only other
-// 16-bit operands, all sums and softmax statistics fp32.  Rounding p costs 2^-11
+// with m the running maximum of y.  The terms being p_j times a whole number, p_j then
+// fills binary16's range whatever V's scales are.  The drafts' terms come first, V as it
+// is, and their sum's size is taken into m before the context's.  p_j (bf16 for a bf16
+// cache and for drafts) and q (bf16 given; for a quantized cache binary16 with an
+// exact power of two a row) are the products' only other 16-bit operands, all sums and
+// softmax statistics fp32.  Rounding p costs 2^-11
 // (binary16) or 2^-8 (bf16) of each term at most, of either sign; the bf16 store of
 // o costs as much of their sum.
 //
@@ -66,6 +68,9 @@ constexpr int kRows = 16;     // rows a CTA takes
 constexpr int kTreeTile = 64;  // positions a tile
 constexpr int kRing = 65536;   // bytes of the ring at most
 constexpr int kTreeCluster = 8;  // splits that a cluster can be
+// Exponents that the drafts' sums can bring into a row's maximum.  The least is that of zeros, below what the smallest
+// scale (2^-24) gives; with the most, probabilities of the context are still normal numbers in l.
+constexpr int kLeastSize = -40, kMostSize = 64;
 
 __device__ __forceinline__ uint32_t pack_bf2(float a, float b) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
@@ -193,22 +198,38 @@ struct Acc {
 
 // y[u][e]: scores of positions 8 u + 2 tc + e % 2 and row gr + 8 (e / 2), -inf
 // where masked.  Leaves p (fp32) in y and the accumulators rescaled.
-template <int HD, int NT>
-__device__ __forceinline__ void softmax_step(Acc<HD> &acc, float (&y)[NT][4]) {
+//   TOP > 0, the first step after the drafts': what those gave a row is o 2^m and l 2^m with V as it is, and y has log2 s in
+// it from here on.  So m takes in the exponent of the row's largest |o| over 2^TOP, a code's size, and o and l the inverse:
+// o is then what a p of about 1 gives over codes, whatever V's unit.
+template <int HD, int NT, int TOP = 0>
+__device__ __forceinline__ void softmax_step(Acc<HD> &acc, float (&y)[NT][4], bool after_drafts = false) {
   float mc[2] = {-INFINITY, -INFINITY};
 #pragma unroll
   for (int u = 0; u < NT; ++u)
 #pragma unroll
     for (int e = 0; e < 4; ++e) mc[e / 2] = fmaxf(mc[e / 2], y[u][e]);
   // Nothing is rescaled until a score passes its row's maximum so far by 2^8 (p stays below that)
-  if (__any_sync(0xffffffffu, mc[0] > acc.m[0] + 8.f || mc[1] > acc.m[1] + 8.f)) {
-    float al[2];
+  if (__any_sync(0xffffffffu, mc[0] > acc.m[0] + 8.f || mc[1] > acc.m[1] + 8.f || (TOP > 0 && after_drafts))) {
+    float al[2], f[2] = {1.f, 1.f};
+    if (TOP > 0 && after_drafts) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float big = 0.f;
+#pragma unroll
+        for (int j = 0; j < HD / 8; ++j) big = fmaxf(fmaxf(big, fabsf(acc.o[j][2 * i])), fabsf(acc.o[j][2 * i + 1]));
+        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+        const int e = min(max((int)(__float_as_uint(big) >> 23) - 127 - TOP, kLeastSize), isinf(big) ? 0 : kMostSize);
+        acc.m[i] += (float)e;
+        f[i] = __uint_as_float((uint32_t)(127 - e) << 23);
+      }
+    }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       mc[i] = fmaxf(mc[i], __shfl_xor_sync(0xffffffffu, mc[i], 1));
       mc[i] = fmaxf(mc[i], __shfl_xor_sync(0xffffffffu, mc[i], 2));
       const float mn = fmaxf(acc.m[i], mc[i]);
-      al[i] = mn == -INFINITY ? 1.f : ex2(acc.m[i] - mn);  // 0 at first (m = -inf)
+      al[i] = mn == -INFINITY ? 1.f : ex2(acc.m[i] - mn) * f[i];  // 0 at first (m = -inf)
       acc.m[i] = mn;
       acc.l[i] *= al[i];
     }
@@ -514,7 +535,7 @@ __global__ void __launch_bounds__(kTreeWarps * 32, 3) attn_tree_kernel(const Tre
             if (8 * (v / 2) + 2 * tc + v % 2 >= n)
 #pragma unroll
               for (int k = 0; k < L::VI * L::VW; ++k) vw[v][k] = 0;
-        softmax_step<HD, 2>(acc, y);
+        softmax_step<HD, 2, BITS == 16 ? 0 : BITS - 1>(acc, y, i == 0 && u0 + warp < min(u1, ndr));
         uint32_t pf[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
