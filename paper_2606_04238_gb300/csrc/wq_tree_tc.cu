@@ -932,22 +932,16 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
 }
 
 // o of the rows whose block was split: HD / 4 lanes a row, its parts in split order,
-// CU of them loaded in one round trip.  A launch that most likely has nothing to merge has
-// few CTAs, which take the rows in turn.
-template <int HD, int CU>
+// CU of them loaded in one round trip.  TURNS: a launch that most likely has nothing to
+// merge, of few CTAs that take the rows in turn.
+template <int HD, int CU, bool TURNS>
 __global__ void __launch_bounds__(256) attn_tree_merge_kernel(const TreeArgs a) {
   constexpr int LPR = HD / 4;
   const int rep = a.H / a.Hkv, R = a.T * rep;
   const int c = threadIdx.x % LPR;
-  pdl_wait();
-  pdl_launch_dependents();
-  if (a.table[a.batch].x == 0) return;
-#pragma unroll 1
-  for (long long row = (long long)blockIdx.x * (256 / LPR) + threadIdx.x / LPR; row < (long long)a.batch * a.Hkv * R;
-       row += (long long)gridDim.x * (256 / LPR)) {
-    const int bg = (int)(row / R), r = (int)(row - (long long)bg * R), b = bg / a.Hkv, g = bg % a.Hkv;
+  auto merge = [&](int bg, int r, int b, int g) {
     const int4 tab = a.table[b];  // first range, splits, row blocks, drafts
-    if (tab.y <= 1 || r >= tab.w * rep) continue;  // written by the first kernel, or skipped
+    if (tab.y <= 1 || r >= tab.w * rep) return;  // written by the first kernel, or skipped
     const size_t step = (size_t)a.Hkv * tab.z * a.part_rows * (HD + 4);
     const float *pt = a.part + ((size_t)(tab.x + g * tab.z + r / kTcRows) * a.part_rows + r % kTcRows) * (HD + 4);
     float M = -INFINITY, L = 0.f;
@@ -980,6 +974,17 @@ __global__ void __launch_bounds__(256) attn_tree_merge_kernel(const TreeArgs a) 
     *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(a.o) +
                                (((size_t)b * a.T + r / rep) * a.H + g * rep + r % rep) * HD + 4 * c) =
         none ? make_uint2(0, 0) : make_uint2(pack_bf2(O.x / L, O.y / L), pack_bf2(O.z / L, O.w / L));
+  };
+  long long row = (long long)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+  int bg = (int)(row / R), r = (int)(row - (long long)bg * R), b = bg / a.Hkv, g = bg % a.Hkv;
+  pdl_wait();
+  pdl_launch_dependents();
+  if (TURNS && a.table[a.batch].x == 0) return;  // nothing was split
+  while (row < (long long)a.batch * a.Hkv * R) {
+    merge(bg, r, b, g);
+    if (!TURNS) return;
+    row += (long long)gridDim.x * (256 / LPR);
+    bg = (int)(row / R), r = (int)(row - (long long)bg * R), b = bg / a.Hkv, g = bg % a.Hkv;
   }
 }
 
@@ -1006,7 +1011,7 @@ cudaError_t prepare_tc() {
 }
 
 template <int HD, int BITS>
-cudaError_t launch_tree_tc_t(const TreeArgs &a, unsigned grid, int merge_ctas, bool many, cudaStream_t s) {
+cudaError_t launch_tree_tc_t(const TreeArgs &a, unsigned grid, bool turns, bool many, cudaStream_t s) {
   constexpr int sm = Cfg<HD, BITS>::SMEM;
   cudaError_t e = prepare_tc<HD, BITS>();
   if (e != cudaSuccess) return e;
@@ -1023,10 +1028,14 @@ cudaError_t launch_tree_tc_t(const TreeArgs &a, unsigned grid, int merge_ctas, b
   e = cudaLaunchKernelEx(&cfg, attn_tree_tc_kernel<HD, BITS>, a);
   if (e != cudaSuccess || !a.split) return e;
   const long long rows = (long long)a.batch * a.H * a.T;
-  cfg.gridDim = dim3((unsigned)std::min((rows * (HD / 4) + 255) / 256, (long long)merge_ctas));
+  cfg.gridDim = dim3((unsigned)std::min((rows * (HD / 4) + 255) / 256, turns ? 2ll * a.target : LLONG_MAX));
   cfg.blockDim = dim3(256);
   cfg.dynamicSmemBytes = 0;
-  return cudaLaunchKernelEx(&cfg, many ? attn_tree_merge_kernel<HD, 8> : attn_tree_merge_kernel<HD, 2>, a);
+  return cudaLaunchKernelEx(&cfg,
+                            turns  ? attn_tree_merge_kernel<HD, 2, true>
+                            : many ? attn_tree_merge_kernel<HD, 8, false>
+                                   : attn_tree_merge_kernel<HD, 2, false>,
+                            a);
 }
 
 }  // namespace
@@ -1061,7 +1070,7 @@ cudaError_t launch_attn_tree_tc(TreeArgs a, int hd, int bits, int num_sms, cudaS
   // of 61 drafts over 500 positions 53.4 for 52.1; of 15 in the same places 22.2).
   a.split = tiles > a.min_tiles && (blocks < a.target || a.counts != nullptr);
 #define WQ_TREE(HD, BITS) \
-  if (hd == HD && bits == BITS) return launch_tree_tc_t<HD, BITS>(a, grid, blocks < a.target ? INT_MAX : 2 * a.target, many, s);
+  if (hd == HD && bits == BITS) return launch_tree_tc_t<HD, BITS>(a, grid, blocks >= a.target, many, s);
   WQ_TREE(128, 16) WQ_TREE(128, 8) WQ_TREE(128, 4) WQ_TREE(64, 16) WQ_TREE(64, 8) WQ_TREE(64, 4)
 #undef WQ_TREE
   return cudaErrorInvalidValue;
