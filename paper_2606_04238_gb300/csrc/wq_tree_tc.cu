@@ -13,7 +13,8 @@
 // swizzled layout, 12 issues the MMAs.  Two CTAs an SM (256 TMEM columns and ~100 KB
 // each) fill each other's waits: a tile's products, softmax and products again are
 // one chain.  A draft tile's rows are brought into binary16 by an exact power of two
-// a row.  The running maximum is raised, and O rescaled in TMEM, only when 32 of a
+// a row, of V's taken into the exponent of the row's p (a masked draft then has no say in
+// the others' steps, whatever it holds).  The running maximum is raised, and O rescaled in TMEM, only when 32 of a
 // row's probabilities add up to 2^8: p stays below that, and no maximum is searched.
 //
 // The tiles of all (b, g, row block) are dealt to the CTAs in nearly equal
@@ -65,6 +66,9 @@ constexpr int kTmemCols = 256;    // S / P 0..127, O 128..
 // Queries enter binary16 times 2^7, which keeps a row with its largest |q| in [2^-4, 2^8) whole but for values
 // below 2^-27 of that; other rows by a power of two of their own.
 constexpr int kQueryShift = 7;
+// Exponents that a draft's V can bring into its score over a quantized cache.  The least is that of zeros, below what the
+// smallest scale gives; with the most, the context's probabilities are still normal numbers in the sums.
+constexpr int kLeastSize = -40, kMostSize = 64;
 // registers a thread: the launch's 72 x 416 shared out as 104 x 128 + 56 x 256 + 72 x 32
 constexpr int kRegsSoftmax = 104, kRegsConv = 56;
 
@@ -316,6 +320,7 @@ struct Shared {
   uint32_t tmem;
   int fail;
   uint32_t odd[4];  // drafts whose V has values that are not finite
+  int wide;         // a draft's V is beyond binary16 with its exponent at kMostSize: V of the tile is bf16, and p too
   Work work;
   // of a tile: K's scales (times the score scale and the queries' 2^-kQueryShift) and the exponent t of V's operands, which are values
   // times 2^-t.  Two tiles of each: the next tile's are written while this one's are read
@@ -323,7 +328,8 @@ struct Shared {
   int te[2];
   uint32_t zk[kTile];                        // 1024 + z of K, twice
   __align__(16) uint2 zsv[kTile];            // 1024 + z of V, twice; its scale times 2^-t, twice
-  __align__(16) uint32_t top[2][kConv / 32]; // warps' shares of the largest V scale of a tile (bits), of the drafts' |v|
+  __align__(16) uint32_t top[2][kConv / 32]; // warps' shares of the largest V scale of a tile (bits)
+  __align__(16) float td[kTile], tw[kTile];  // exponents t of the drafts' V, 2^-t
 };
 
 // 8 codes as 8 binary16 values code - z; z1024: 1024 + z in both halves.
@@ -373,6 +379,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
     }
   } else if (warp == 4 && lane < 4) {
     sh.odd[lane] = 0;
+    sh.wide = 0;
   }
   pdl_wait();
   pdl_launch_dependents();
@@ -422,9 +429,10 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
         ok = mbar_wait(&sh.v_full, i & 1) && mbar_wait(&sh.p_full, (i + 1) & 1);
         if (!ok) break;
         tc_fence_after();
+        const uint32_t id = !BF && i == 0 && w.t0 < ndr && sh.wide ? tree_idesc(HD, true, true) : idpv;
 #pragma unroll
         for (int ks = 0; ks < kTile / 16; ++ks)
-          umma_ts(tm + 128, tm + 8 * ks, vd + (uint64_t)((ks * 2048) >> 4), idpv, i > 0 || ks > 0);
+          umma_ts(tm + 128, tm + 8 * ks, vd + (uint64_t)((ks * 2048) >> 4), id, i > 0 || ks > 0);
         umma_commit(&sh.v_empty);
       }
       if (!ok) sh.fail = 1;
@@ -490,23 +498,32 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
       for (int e = 0; e < 4; ++e) x[e] = pack_h2(bf_lo(x[e]) * f, bf_hi(x[e]) * f);
     };
     const float qscale = a.scale * pow2i(-kQueryShift);  // of K's scales
-    // The drafts' tile: K in binary16 by a power of two a row, V by one for all (bf16 cache: as they are).
+    // The drafts' tile: K and V in binary16 by a power of two a row (bf16 cache: as they are).  V's brings its largest
+    // value to [2^(BITS + 5), 2^(BITS + 6)), where a code times a scale is at most.
     auto draft_tile = [&]() {
       const int its = min(C::IT, (w.cnt + C::RS - 1) / C::RS);  // chunks with drafts in them
-      float vmax = 0.f;
 #pragma unroll 1
       for (int it = 0; it < its; ++it) {
         uint32_t x[4], y[4];
         draft_chunk(kd, it, false, x);
         draft_chunk(vd, it, true, y);
-        vmax = fmaxf(vmax, largest(y));
         if constexpr (!BF) {
-          float mx = largest(x);
+          float mx = largest(x), mv = largest(y);
 #pragma unroll
-          for (int o = C::CH / 2; o >= 1; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+          for (int o = C::CH / 2; o >= 1; o >>= 1) {
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            mv = fmaxf(mv, __shfl_xor_sync(0xffffffffu, mv, o));
+          }
           const int e2 = f16_shift(mx, 14);
           scaled(x, pow2i(e2));
-          if (c == 0) sh.sk[0][r0 + it * C::RS] = qscale * pow2i(-e2);
+          if (c == 0) {
+            const int r = r0 + it * C::RS, ev = (int)(__float_as_uint(mv) >> 23) - 127 - (BITS + 5);
+            const int t = min(max(ev, kLeastSize), kMostSize);
+            sh.sk[0][r] = qscale * pow2i(-e2);
+            sh.td[r] = (float)t;
+            sh.tw[r] = pow2i(-t);
+            if (ev > kMostSize) sh.wide = 1;
+          }
         } else {
           *reinterpret_cast<uint4 *>(vbuf + dst0 + it * C::RS * 128) = make_uint4(y[0], y[1], y[2], y[3]);
         }
@@ -514,20 +531,18 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
       }
       // (K's other rows hold what they held: their scores are not looked at)
       if constexpr (!BF) {
-        const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(vmax));
-        if (lane == 0) sh.top[0][warp - 4] = top;
-        named_barrier_sync(1, kConv);
-        uint32_t all = 0;
-#pragma unroll
-        for (int i = 0; i < kConv / 32; ++i) all = max(all, sh.top[0][i]);
-        const int e2 = f16_shift(__uint_as_float(all), 13);
-        if (ct == 0) sh.te[0] = -e2;
+        if (c == 0)
+#pragma unroll 1
+          for (int it = its; it < C::IT; ++it) sh.td[r0 + it * C::RS] = sh.tw[r0 + it * C::RS] = 0.f;
+        if (ct == 0) sh.te[0] = 0;
         hand_over(&sh.k_full);
+        named_barrier_sync(1, kConv);
+        const bool wide = sh.wide != 0;
 #pragma unroll 1
         for (int it = 0; it < its; ++it) {
           uint32_t y[4];
           draft_chunk(vd, it, true, y);
-          scaled(y, pow2i(e2));
+          if (!wide) scaled(y, sh.tw[r0 + it * C::RS]);
           *reinterpret_cast<uint4 *>(vbuf + dst0 + it * C::RS * 128) = make_uint4(y[0], y[1], y[2], y[3]);
         }
       } else {
@@ -732,6 +747,9 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
             unpack_f32x2(fma_f32x2(pack_f32x2(u[j], u[j + 1]), k0, mm), u[j], u[j + 1]);
             unpack_f32x2(fma_f32x2(pack_f32x2(u[j + 2], u[j + 3]), k1, mm), u[j + 2], u[j + 3]);
           }
+          if (masks && !BF && drafts)
+#pragma unroll
+            for (int j = 0; j < 32; ++j) u[j] += sh.td[32 * h + j];
           if (masks && some) {
             const uint32_t bits = seen(h);
 #pragma unroll
@@ -780,6 +798,16 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
             const float now = m == -INFINITY ? 0.f : te - m;
 #pragma unroll
             for (int j = 0; j < 32; ++j) u[j] += now - ms;
+          }
+          if (masks && !BF && drafts) {  // each p stands for 2^-t of itself with a t of its own
+            const bool wide = sh.wide != 0;
+            part = 0.f;
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+              const float e0 = ex2(u[j]) * sh.tw[32 * h + j], e1 = ex2(u[j + 1]) * sh.tw[32 * h + j + 1];
+              part += e0 + e1;
+              if (wide) p[j / 2] = pack_bf2(e0, e1);
+            }
           }
           total += part;
           // columns 16 h ..: S's there have been read

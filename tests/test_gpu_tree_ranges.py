@@ -1,7 +1,7 @@
 """Tree attention with values far from 1: small V rows, in the cache and among the
-drafts, beside drafts with high scores.  The result scales with V, so its error has
-to as well.  Bound: that of test_gpu_tree.py, in which every term is relative to V's
-size.
+drafts, beside drafts with high scores; masked drafts of any finite size.  The result
+scales with V, so its error has to as well.  Bound: that of test_gpu_tree.py, in which
+every term is relative to V's size.
 """
 import math
 
@@ -52,3 +52,22 @@ def test_drafts_of_another_size_than_the_context(wq, room, bits, ratio, t):
             towards(q, kn, j, -8.0 if ratio > 1 else 8.0, 64 ** -0.5)
         vn.copy_((vn.float() * ratio).to(torch.bfloat16))
     close(*run(wq, room, 2, t, 4, 4, 64, bits, [300, 1200], seed=44, spoil=spoil))
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("t,H", [(12, 2), (40, 8)])
+@pytest.mark.parametrize("size", [3e38, 1e20, 1e9])
+def test_masked_drafts_of_any_size(wq, room, bits, t, H, size):
+    """Drafts that only themselves see, or no one, with finite K and V of any size."""
+    def spoil(q, kn, vn, k, v):
+        vn[0, 5], vn[1, 7] = size, -size
+        kn[0, 6], kn[1, 7] = -size, size
+        vn[1, 0] = (vn[1, 0].float() / size).to(torch.bfloat16)
+
+    vis = torch.ones((2, t, t), dtype=torch.bool).tril()
+    vis[0, :, 5:7] = False
+    vis[0, 5, 5] = True
+    vis[1, :, 7] = False
+    o, ref, tol = run(wq, room, 2, t, H, 1, 128, bits, [200, 90], vis=vis, seed=45, spoil=spoil)
+    assert float(ref[0, 5].abs().max()) > 1e6 and float(ref[0, 7:].abs().max()) < 100 and float(ref[1].abs().max()) < 100
+    close(o, ref, tol)
