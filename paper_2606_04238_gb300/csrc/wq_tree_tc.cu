@@ -188,6 +188,25 @@ __device__ __noinline__ void rescale(uint32_t tw, int pc, int oc, float al) {
   }
 }
 
+// Infinities and NaN among four columns of a bf16 cache's V, n positions from vp on: every row sees them, so a column that
+// has any is their sum; a copy's p of 0 for the others' positions made it NaN.  (A quantized cache has NaN rows only.)
+template <int HD>
+__device__ __noinline__ float4 column_infinities(const __nv_bfloat16 *vp, int n, float4 o) {
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int p = 0; p < n; ++p) {
+    const uint2 x = __ldg(reinterpret_cast<const uint2 *>(vp + (size_t)p * HD));
+    const float f[4] = {bf_lo(x.x), bf_hi(x.x), bf_lo(x.y), bf_hi(x.y)};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[e] += isfinite(f[e]) ? 0.f : f[e];
+  }
+  if (s[0] != 0.f) o.x = s[0];
+  if (s[1] != 0.f) o.y = s[1];
+  if (s[2] != 0.f) o.z = s[2];
+  if (s[3] != 0.f) o.w = s[3];
+  return o;
+}
+
 // What a CTA takes: row block rb of (b, g), tiles t0 .. t1 - 1 (drafts' tiles
 // first); n splits of the row block, this is `split`, its partial results at `slot`.
 struct Work {
@@ -900,6 +919,12 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
             const float4 x = stage[row * CK + (c ^ (row & (CK - 1)))];
             L = fmaf(sl[row], f, L);
             o.x = fmaf(x.x, f, o.x), o.y = fmaf(x.y, f, o.y), o.z = fmaf(x.z, f, o.z), o.w = fmaf(x.w, f, o.w);
+          }
+          if (BF && !(fabsf((o.x + o.y) + (o.z + o.w)) < INFINITY)) {
+            const int p0 = max(0, w.t0 - ndr) * kTile;
+            o = column_infinities<HD>(reinterpret_cast<const __nv_bfloat16 *>(a.vc) +
+                                          (((size_t)w.b * a.Hkv + w.g) * a.max_len + p0) * HD + 4 * c,
+                                      min(w.len, (w.t1 - ndr) * kTile) - p0, o);
           }
         }
         const int ro = row0 + lrow, to = draft_of(ro);
