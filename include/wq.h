@@ -440,7 +440,7 @@ wq_status wq_qkv_rope(const float *qkv, const void *x, int m, int d, const int32
  *            What a masked draft's K and V hold, infinities and NaN too, does not
  *            reach the row.
  *   A length or count outside its range skips the sequence (o unwritten) and records
- *   WQ_ERR_ARG in the device status.  n_heads / n_kv <= 16.
+ *   WQ_ERR_ARG in the device status.  n_heads / n_kv <= 16, max_len < 2^31 - 1024.
  * Workspace: wq_attn_tree_workspace_bytes for up to `batch` sequences and n_draft
  * drafts (no zeroing needed).
  */

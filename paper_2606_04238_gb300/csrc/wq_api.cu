@@ -1533,6 +1533,8 @@ wq_status attn_tree_impl(const void *q, const void *k_new, const void *v_new, in
   if (n_heads <= 0 || n_heads % c->n_kv != 0 || n_heads / c->n_kv > 16)
     return fail(WQ_ERR_UNSUPPORTED, "n_heads %d / n_kv %d: a multiple, at most 16 query heads a kv head", n_heads, c->n_kv);
   if (!std::isfinite(scale)) return fail(WQ_ERR_ARG, "score scale not finite");
+  // the kernels round positions up to whole tiles, and look past a tile's end, in 32 bits
+  if (c->max_len > INT32_MAX - 1024) return fail(WQ_ERR_SHAPE, "a cache of %d positions, at most 2^31 - 1025", c->max_len);
   if (n_draft == 0) return ok();
   if (!q || !k_new || !v_new || !lens || !o || !ws) return fail(WQ_ERR_ARG, "null pointer");
   if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(o) || !aligned16(ws))
