@@ -365,7 +365,8 @@ wq_status wq_decoder_layer_forward(const void *x, int batch, const int32_t *lens
  *            4 (e / 2) + 16 (e % 2).
  * A row of 8 or 4 bits has one binary16 scale s and one whole zero z
  * (0 <= z <= qmax = 2^bits - 1) in k_meta, v_meta: uint32 [batch, n_kv, max_len],
- * s in the low half, z (binary16) in the high one.  A value is s (code - z).
+ * s in the low half, z (binary16) in the high one.  A value is s (code - z).  A row of
+ * zeros has s 1, z -0 and codes 0 (0x80003c00); wq_attn_tree knows V rows of zeros by that.
  */
 typedef struct {
     void *k, *v;
@@ -375,7 +376,7 @@ typedef struct {
 
 /*
  * Writes K and V rows into the cache, quantized on the way:
- *   mn = min(0, row), mx = max(0, row), s = fp16((mx - mn) / qmax) (1 if that is 0),
+ *   mn = min(0, row), mx = max(0, row), s = fp16((mx - mn) / qmax) (1 if that is 0: a row of zeros),
  *   z = clamp(rint(-mn / s), 0, qmax), code = clamp(rint(value / s) + z, 0, qmax),
  * every step in fp32, round to nearest; bits 16: one rounding to bf16 (none for
  * bf16 rows).  A row with an infinity or NaN, or whose scale is beyond binary16,

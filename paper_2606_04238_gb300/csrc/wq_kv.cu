@@ -3,7 +3,7 @@
 // rotary positions of drafted tokens' projections.
 //
 // A cached row is one position's K or V of one kv head (HD values):
-//   s = fp16((mx - mn) / qmax), mn = min(0, row), mx = max(0, row)  (1 if zero),
+//   s = fp16((mx - mn) / qmax), mn = min(0, row), mx = max(0, row)  (1 if zero, z then -0),
 //   z = clamp(rint(-mn / s), 0, qmax), code = clamp(rint(v / s) + z, 0, qmax),
 // value s (code - z), in fp32 with explicit round-to-nearest.  0 lies in the
 // range, so z needs no sign and code - z is a whole number of 9 bits: an exact
@@ -84,7 +84,11 @@ template <int BITS>
 __device__ __forceinline__ uint32_t quantize16(const float (&v)[16], float mn, float mx, uint32_t (&c)[8]) {
   constexpr float qmax = (float)((1 << BITS) - 1), M = 12582912.f;
   __half sh = __float2half_rn(__fdiv_rn(__fsub_rn(mx, mn), qmax));
-  if (__half2float(sh) == 0.f) sh = __float2half_rn(1.f);
+  if (__half2float(sh) == 0.f) {  // no value is above 2^-25 qmax: codes and zero point 0
+#pragma unroll
+    for (int k = 0; k < 8; ++k) c[k] = 0;
+    return kZeroRow;
+  }
   const float sf = __half2float(sh);
   if (!isfinite(sf)) {  // also infinite or NaN values: mx - mn is then too
 #pragma unroll

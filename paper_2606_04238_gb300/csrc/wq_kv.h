@@ -9,6 +9,12 @@
 
 namespace wq {
 
+// Scale and zero of a cached row of zeros: 1 and -0 (the zero point of any other row is +0 or above).  Attention takes such
+// a V row, like one of a zero-filled cache (scale 0), for one of the least scale: its codes are its zero point, so any
+// scale gives its values, and 1 would make small rows beside it look small.
+constexpr uint32_t kZeroRow = 0x80003c00u;
+constexpr float kLeastScale = 0x1p-24f;  // of binary16, bits 0x0001
+
 // Rows k, v [batch][n_src][n_kv][HD] (strides in values: sequence, token, head)
 // into the caches [batch][n_kv][max_len][HD] at start[b] + n, n < counts[b]
 // (null: n), row n taken from token index[b][n] (null: n).

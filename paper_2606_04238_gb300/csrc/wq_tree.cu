@@ -495,7 +495,7 @@ __global__ void __launch_bounds__(kTreeWarps * 32, 3) attn_tree_kernel(const Tre
             const uint32_t m = __shfl_sync(0xffffffffu, mw, at), mm = __shfl_sync(0xffffffffu, mw, 16 + at);
             const float sk = __half2float(__ushort_as_half((unsigned short)(m & 0xffffu)));
             float sv = __half2float(__ushort_as_half((unsigned short)(mm & 0xffffu)));
-            if (sv == 0.f) sv = 1.f;  // a zero-filled cache's row: code - z is 0
+            if (sv == 0.f || mm == kZeroRow) sv = kLeastScale;  // code - z is 0
             const float lg = lg2(sv);
             rs[v] = rcp(sv);
             yy[v % 2] = fmaf(yy[v % 2] * qf[0], sk, lg);

@@ -585,7 +585,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
     auto note_top = [&](int which) {
       if (ct < kTile) return;
       uint32_t v = (meta & 0xffffu) > 0x7c00u ? 0u : meta & 0xffffu;
-      if (v == 0) v = 0x3c00u;  // a zero-filled cache's row counts as 1
+      if (v == 0 || meta == kZeroRow) v = 1;  // kLeastScale
       v = __reduce_max_sync(0xffffffffu, v);
       if (lane == 0) sh.top[which][warp - 4] = v;
     };
@@ -626,7 +626,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
             sh.zk[r] = zz;
             if (ct == 0) sh.te[par] = te;
           } else {
-            const float sv = (s0 == 0.f ? 1.f : s0) * pow2i(-te);  // a zero-filled cache's row: code - z is 0
+            const float sv = (s0 == 0.f || meta == kZeroRow ? kLeastScale : s0) * pow2i(-te);  // (then code - z is 0)
             sh.zsv[r] = make_uint2(zz, pack_h2(sv, sv));
           }
         }

@@ -1,6 +1,6 @@
 """Tree attention with values far from 1: small V rows, in the cache and among the
-drafts, beside drafts with high scores; masked drafts of any finite size.  The result
-scales with V, so its error has to as well.  Bound: that of test_gpu_tree.py, in which
+drafts, beside drafts with high scores; masked drafts of any finite size; V rows of
+zeros.  The result scales with V, so its error has to as well.  Bound: that of test_gpu_tree.py, in which
 every term is relative to V's size.
 """
 import math
@@ -71,3 +71,48 @@ def test_masked_drafts_of_any_size(wq, room, bits, t, H, size):
     o, ref, tol = run(wq, room, 2, t, H, 1, 128, bits, [200, 90], vis=vis, seed=45, spoil=spoil)
     assert float(ref[0, 5].abs().max()) > 1e6 and float(ref[0, 7:].abs().max()) < 100 and float(ref[1].abs().max()) < 100
     close(o, ref, tol)
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("size", [1.0, 1e-3, 2.0 ** -13])
+@pytest.mark.parametrize("t,H", [(1, 2), (30, 2)])
+def test_zero_rows_beside_small_values(wq, room, bits, size, t, H):
+    """Rows of zeros among the cached V (attended to more than the others) and among the drafts'."""
+    def spoil(q, kn, vn, k, v):
+        for x in (v, vn):
+            x.copy_(((x.float() + 0.5) * size).to(torch.bfloat16))
+        for j in range(t):
+            towards(q, kn, j, 7.0 if j % 3 else -3.0, 64 ** -0.5)
+        k[:, 5], k[:, 700] = kn[:, 0], kn[:, t // 2]
+        v[:, 5], v[:, 700], v[:, 300:310], vn[:, t // 2] = 0, 0, 0, 0
+    close(*run(wq, room, 2, t, H, H, 64, bits, [1500, 600], seed=46, spoil=spoil))
+    # one split a sequence, a row of zeros in every 16 positions of a tile
+    def sixteenths(q, kn, vn, k, v):
+        spoil(q, kn, vn, k, v)
+        for p in range(5, 128, 16):
+            k[:, p], v[:, p] = kn[:, 1 % t], 0
+    close(*run(wq, room, 29, t, 12 * H, 12 * H, 64, bits, [800] * 28 + [701], seed=48, spoil=sixteenths))
+    # every V row of the cache, or of the drafts, is zeros
+    def empty(which):
+        def f(q, kn, vn, k, v):
+            (v if which else vn).zero_()
+            (vn if which else v).copy_(((vn if which else v).float() * size).to(torch.bfloat16))
+        return f
+    for which in (0, 1):
+        close(*run(wq, room, 1, t, H, H, 64, bits, [400], seed=47, spoil=empty(which)))
+
+
+def test_a_row_of_zeros_is_marked(wq):
+    """Scale 1 and zero -0 (any other row's is +0): what attention knows it by."""
+    rows = torch.randn((1, 4, 1, 64)).to(torch.bfloat16)
+    rows[0, 1] = 0
+    rows[0, 2] = rows[0, 2].abs()  # zero point 0
+    rows[0, 3] = 1e-9              # below the smallest scale: held as zeros
+    for bits in (8, 4):
+        c = wq.kv_cache(1, 1, 4, 64, bits)
+        wq.kv_append(c, rows.cuda(), rows.cuda(), torch.zeros(1, dtype=torch.int32, device="cuda"))
+        for m in (c.k_meta, c.v_meta):
+            m = (m.cpu().flatten().long() & 0xffffffff).tolist()
+            assert m[1] == m[3] == 0x80003c00 and m[0] >> 31 == 0 and m[2] >> 16 == 0
+        k, v = wq.kv_read(c, torch.zeros(1, dtype=torch.int32, device="cuda"), 4, dtype=torch.float32)
+        assert (k[0, 1] == 0).all() and (v[0, 3] == 0).all() and not torch.signbit(k[0, 1]).any()
