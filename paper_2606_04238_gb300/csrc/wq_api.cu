@@ -1628,7 +1628,9 @@ wq_status wq_qkv_rope(const float *qkv, const void *x, int m, int d, const int32
   QkvRopeArgs a{};
   a.qkv = qkv, a.x = x, a.positions = positions, a.table = table, a.q = q, a.k = k, a.v = v;
   a.d = d, a.n_heads = n_heads, a.n_kv = n_kv, a.n_pos = n_pos, a.head_norm = (flags & WQ_HEAD_NORM) ? 1 : 0;
-  cudaError_t e = launch_qkv_rope(a, m, head_dim, static_cast<cudaStream_t>(stream));
+  const int sms = num_sms();
+  if (sms <= 0) return fail(WQ_ERR_CUDA, "cannot query the current device");
+  cudaError_t e = launch_qkv_rope(a, m, head_dim, sms, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return cuda_fail(e, "rotary launch");
   return ok();
 }

@@ -478,11 +478,11 @@ cudaError_t launch_kv_read(const KvReadArgs &a, int hd, int bits, bool f32, cuda
   return cudaErrorInvalidValue;
 }
 
-cudaError_t launch_qkv_rope(const QkvRopeArgs &a, int m, int hd, cudaStream_t s) {
+cudaError_t launch_qkv_rope(const QkvRopeArgs &a, int m, int hd, int num_sms, cudaStream_t s) {
   // Up to two tokens an SM 256 threads a token, whose heads are then all in flight (304
   // tokens of 48 heads 4.4 us, with 128 threads 5.5), above that 128, of which seven
   // CTAs fit an SM where of 256 only three do (1220 tokens of 56 heads 14.5 us for 20.9).
-  const bool few = m <= 2 * 152;
+  const bool few = m <= 2 * num_sms;
   if (hd == 128)
     return few ? launch_pdl(qkv_rope_kernel<128, 256>, (unsigned)m, 256, s, a)
                : launch_pdl(qkv_rope_kernel<128, 128>, (unsigned)m, 128, s, a);

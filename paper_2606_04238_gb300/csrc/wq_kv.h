@@ -47,7 +47,7 @@ struct QkvRopeArgs {
   void *q, *k, *v;
   int d, n_heads, n_kv, n_pos, head_norm;
 };
-cudaError_t launch_qkv_rope(const QkvRopeArgs &a, int m, int hd, cudaStream_t s);
+cudaError_t launch_qkv_rope(const QkvRopeArgs &a, int m, int hd, int num_sms, cudaStream_t s);
 // Reads and clears the status word of the three kernels above.
 cudaError_t read_kv_status(int *status);
 
