@@ -63,10 +63,10 @@ struct TreeArgs {
   float *part;                  // [batch Hkv][rows][S][HD + 2] (S > 1)
   void *o;                      // bf16 [batch][T][H][HD]
   int S, cluster;               // splits of the context; whether they are a cluster
-  // tcgen05 kernel: ranges of tiles wanted, least tiles a range, whether row blocks may be split
-  // (only then the merge is launched), rows of a range's partial results, and per sequence its
-  // first range, splits, row blocks and drafts; after the sequences whether any was split (.x)
-  int target, min_tiles, split, part_rows, rep_magic;
+  // tcgen05 kernel: ranges of tiles wanted, whether row blocks may be split (only then the merge is
+  // launched), rows of a range's partial results, and per sequence its first range, splits, row
+  // blocks and drafts; after the sequences whether any was split (.x)
+  int target, split, part_rows, rep_magic;
   int4 *table;
 };
 // Splits of the context a launch takes, and its partial results in floats.

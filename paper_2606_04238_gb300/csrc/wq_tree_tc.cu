@@ -256,9 +256,9 @@ __device__ Work find_work(const TreeArgs &a, int rep, int cta) {
   total *= a.Hkv;
   many *= a.Hkv;
   int W = most;
-  if (a.split && many < target && most > a.min_tiles) {
+  if (a.split && many < target && most > 1) {
     // sum ceil(tiles / W) <= total / W + many: no more than `target` at hi
-    const int lo = max(a.min_tiles, (int)((total + target - 1) / target));
+    const int lo = max(1, (int)((total + target - 1) / target));
     const int hi = min(most, max(lo, (int)((total + (target - many) - 1) / (target - many))));
     const int cand = lo + (hi - lo) / 31 * lane + (hi - lo) % 31 * lane / 31;
     const float rc = __frcp_rn((float)cand);
@@ -1109,7 +1109,6 @@ cudaError_t launch_attn_tree_tc(TreeArgs a, int hd, int bits, int num_sms, cudaS
   if (a.scale == 0.f) return cudaErrorInvalidValue;
   const long long blocks = (long long)a.batch * a.Hkv * (((long long)a.T * rep + kTcRows - 1) / kTcRows);
   a.target = tree_tc_target(num_sms);
-  a.min_tiles = 1;
   a.part_rows = std::min(a.T * rep, kTcRows);
   a.rep_magic = (65536 + rep - 1) / rep;  // row / rep = row rep_magic >> 16 for row < 65536 / (rep - 1)
   const long long tiles = ((long long)a.max_len + kTile - 1) / kTile + (a.T + kTile - 1) / kTile;
@@ -1121,7 +1120,7 @@ cudaError_t launch_attn_tree_tc(TreeArgs a, int hd, int bits, int num_sms, cudaS
   // host only whether there are any.  Without them a call of `target` row blocks is never split and has no merge
   // to launch.  With them it may be, and where the counts are full the merge finds nothing to do (1.3 us: 20 sequences
   // of 61 drafts over 500 positions 53.4 for 52.1; of 15 in the same places 22.2).
-  a.split = tiles > a.min_tiles && (blocks < a.target || a.counts != nullptr);
+  a.split = tiles > 1 && (blocks < a.target || a.counts != nullptr);
 #define WQ_TREE(HD, BITS) \
   if (hd == HD && bits == BITS) return launch_tree_tc_t<HD, BITS>(a, grid, blocks >= a.target, many, s);
   WQ_TREE(128, 16) WQ_TREE(128, 8) WQ_TREE(128, 4) WQ_TREE(64, 16) WQ_TREE(64, 8) WQ_TREE(64, 4)
