@@ -24,12 +24,20 @@
 
 #include "wq_internal.h"
 #include "wq_launch.h"
-#include "wq_quant.cuh"
 
 namespace wq {
 namespace {
 
 constexpr int kPackWarps = 8;  // blocks a CTA
+
+// rint(v / sf) as the IEEE division gives it.  p = v * rcp is within |p| 2^-22
+// of the quotient (two roundings), as is the division's own result, so both
+// round to the same integer unless p is that near to a half.
+__device__ __forceinline__ float rint_div(float v, float sf, float rcp) {
+  const float p = __fmul_rn(v, rcp), r = rintf(p);
+  if (fabsf(p - r) < 0.5f - fabsf(p) * 0x1p-21f) return r;
+  return rintf(__fdiv_rn(v, sf));  // also nan and infinite quotients
+}
 
 template <int BITS, int GROUP>
 __global__ void __launch_bounds__(kPackWarps * 32) pack_kernel(const float *__restrict__ w, int n, int k, int RT, int KB,
