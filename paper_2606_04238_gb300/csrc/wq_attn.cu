@@ -51,6 +51,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include "wq_cvt.cuh"
 #include "wq_internal.h"
 #include "wq_ptx.cuh"
 
@@ -69,18 +70,11 @@ constexpr int kCombWarps = 8;
 constexpr int kHG = 4;        // query heads a pass takes (padded with zero heads)
 constexpr int kPos = 16;      // positions a chunk takes
 
-__device__ __forceinline__ float bf_lo(uint32_t v) { return __uint_as_float(v << 16); }
-__device__ __forceinline__ float bf_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
-
 // x = hi + mid + lo with bf16 parts (exact to 24 bits).
 __device__ __forceinline__ void split3(float x, float (&p)[3]) {
   p[0] = __bfloat162float(__float2bfloat16_rn(x));
   p[1] = __bfloat162float(__float2bfloat16_rn(x - p[0]));
   p[2] = x - p[0] - p[1];
-}
-__device__ __forceinline__ uint32_t pack_bf2(float a, float b) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const uint32_t *>(&v);
 }
 
 }  // namespace

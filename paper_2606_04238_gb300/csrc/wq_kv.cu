@@ -27,6 +27,7 @@
 
 #include <cstdint>
 
+#include "wq_cvt.cuh"
 #include "wq_internal.h"
 #include "wq_kv.h"
 #include "wq_ptx.cuh"
@@ -42,14 +43,6 @@ namespace {
 
 constexpr int kAppendThreads = 128, kReadThreads = 256;
 
-__device__ __forceinline__ float bf_lo(uint32_t v) { return __uint_as_float(v << 16); }
-__device__ __forceinline__ float bf_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
-__device__ __forceinline__ uint32_t pack_bf2(float a, float b) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const uint32_t *>(&v);
-}
-
-
 // Quotients by a divisor of the whole launch: x d' >> (31 + l), l = ceil(log2 d), d' the
 // whole number above 2^(31 + l) / d, too large by at most 1: exact for x below 2^31.
 struct Divisor {
@@ -61,14 +54,6 @@ struct Divisor {
   }
   __device__ __forceinline__ unsigned divide(unsigned x) const { return (unsigned)((unsigned long long)x * mul >> shift); }
 };
-
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  unsigned long long d;
-  asm("{\n.reg .b64 x, y, z;\nmov.b64 x, {%1, %2};\nmov.b64 y, {%3, %4};\nmov.b64 z, {%5, %6};\nfma.rn.f32x2 %0, x, y, z;\n}"
-      : "=l"(d)
-      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-  return make_float2(__uint_as_float((uint32_t)d), __uint_as_float((uint32_t)(d >> 32)));
-}
 
 }  // namespace
 
@@ -97,25 +82,24 @@ __device__ __forceinline__ uint32_t quantize16(const float (&v)[16], float mn, f
   }
   const float zf = __fadd_rn(fminf(fmaxf(rintf(__fdiv_rn(-mn, sf)), 0.f), qmax), 0.f);
   const float rcp = __frcp_rn(sf), up = __fmul_rn(rcp, 1.f + 0x1p-22f), dn = __fmul_rn(rcp, 1.f - 0x1p-22f);
-  const float2 up2 = make_float2(up, up), dn2 = make_float2(dn, dn), M2 = make_float2(M, M);
+  const uint64_t up2 = pack_f32x2(up, up), dn2 = pack_f32x2(dn, dn), M2 = pack_f32x2(M, M);
   const uint32_t z2 = (uint32_t)zf * 0x10001u, q2 = (uint32_t)qmax * 0x10001u;
   uint32_t differ = 0;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-    const float2 x = make_float2(v[2 * k], v[2 * k + 1]);
-    const float2 t = fma2(x, up2, M2), u = fma2(x, dn2, M2);
-    const uint32_t t0 = __float_as_uint(t.x), t1 = __float_as_uint(t.y);
-    differ |= t0 ^ __float_as_uint(u.x);
-    differ |= t1 ^ __float_as_uint(u.y);
+    const uint64_t x = pack_f32x2(v[2 * k], v[2 * k + 1]), t = fma_f32x2(x, up2, M2), u = fma_f32x2(x, dn2, M2);
+    const uint32_t t0 = (uint32_t)t, t1 = (uint32_t)(t >> 32);
+    differ |= t0 ^ (uint32_t)u;
+    differ |= t1 ^ (uint32_t)(u >> 32);
     c[k] = __viaddmin_s16x2_relu(__byte_perm(t0, t1, 0x5410), z2, q2);  // max(min(t + z, qmax), 0)
   }
   if (differ != 0) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const float2 x = make_float2(v[2 * k], v[2 * k + 1]);
-      const float2 t = fma2(x, up2, M2), u = fma2(x, dn2, M2);
-      if (t.x != u.x || t.y != u.y) {
-        const float t0 = __fadd_rn(rintf(__fdiv_rn(x.x, sf)), zf), t1 = __fadd_rn(rintf(__fdiv_rn(x.y, sf)), zf);
+      const uint64_t x = pack_f32x2(v[2 * k], v[2 * k + 1]);
+      if (fma_f32x2(x, up2, M2) != fma_f32x2(x, dn2, M2)) {  // (both are near 1.5 2^23: equal as numbers if as bits)
+        const float t0 = __fadd_rn(rintf(__fdiv_rn(v[2 * k], sf)), zf);
+        const float t1 = __fadd_rn(rintf(__fdiv_rn(v[2 * k + 1], sf)), zf);
         c[k] = (uint32_t)fminf(fmaxf(t0, 0.f), qmax) | (uint32_t)fminf(fmaxf(t1, 0.f), qmax) << 16;
       }
     }
@@ -337,7 +321,6 @@ __global__ void __launch_bounds__(kReadThreads) kv_read_kernel(const KvReadArgs 
 // lane's heads are loaded before the sum over x is waited for.  10 tokens of 48 heads
 // of 128 take 2.8 us, launch latency; 1220 tokens of 56 heads 14.4 us, 4.6 TB/s: loads
 // in flight bound it (72 registers a thread leave 7 CTAs of 128 threads an SM).
-
 
 template <int HD, int THREADS>
 __global__ void __launch_bounds__(THREADS, 896 / THREADS) qkv_rope_kernel(const QkvRopeArgs a) {

@@ -48,6 +48,7 @@
 #include <atomic>
 #include <cstdint>
 
+#include "wq_cvt.cuh"
 #include "wq_internal.h"
 #include "wq_kv.h"
 #include "wq_ptx.cuh"
@@ -72,27 +73,6 @@ constexpr int kTreeCluster = 8;  // splits that a cluster can be
 // scale (2^-24) gives; with the most, probabilities of the context are still normal numbers in l.
 constexpr int kLeastSize = -40, kMostSize = 64;
 
-__device__ __forceinline__ uint32_t pack_bf2(float a, float b) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const uint32_t *>(&v);
-}
-__device__ __forceinline__ uint32_t pack_h2(float a, float b) {
-  const __half2 v = __floats2half2_rn(a, b);
-  return *reinterpret_cast<const uint32_t *>(&v);
-}
-__device__ __forceinline__ float bf_lo(uint32_t v) { return __uint_as_float(v << 16); }
-__device__ __forceinline__ float bf_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
-__device__ __forceinline__ uint32_t hsub2_u(uint32_t a, uint32_t b) {
-  const __half2 v = __hsub2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
-  return *reinterpret_cast<const uint32_t *>(&v);
-}
-// a / 16 - b
-__device__ __forceinline__ uint32_t hfma16_u(uint32_t a, uint32_t b) {
-  const uint32_t k = 0x2c002c00u;  // 1/16, 1/16
-  const __half2 v = __hfma2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&k),
-                            __hneg2(*reinterpret_cast<const __half2 *>(&b)));
-  return *reinterpret_cast<const uint32_t *>(&v);
-}
 template <int N>
 __device__ __forceinline__ void load_words(uint32_t (&w)[N], const void *p) {
   static_assert(N == 1 || N == 2 || N == 4, "");
@@ -169,12 +149,6 @@ __device__ __forceinline__ uint32_t v_frag(const uint32_t (&wa)[Lay<HD, BITS>::V
     if (nib >= 2) x >>= 8;
     return nib % 2 ? hfma16_u((x & 0x00f000f0u) | 0x64006400u, z64) : hsub2_u((x & 0x000f000fu) | 0x64006400u, z1024);
   }
-}
-
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
 }
 
 __device__ __forceinline__ float lg2(float x) {

@@ -44,6 +44,7 @@
 #include <climits>
 #include <cstdint>
 
+#include "wq_cvt.cuh"
 #include "wq_internal.h"
 #include "wq_kv.h"
 #include "wq_ptx.cuh"
@@ -72,31 +73,6 @@ constexpr int kLeastSize = -40, kMostSize = 64;
 // registers a thread: the launch's 72 x 416 shared out as 104 x 128 + 56 x 256 + 72 x 32
 constexpr int kRegsSoftmax = 104, kRegsConv = 56;
 
-__device__ __forceinline__ float bf_lo(uint32_t v) { return __uint_as_float(v << 16); }
-__device__ __forceinline__ float bf_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
-__device__ __forceinline__ uint32_t pack_bf2(float a, float b) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const uint32_t *>(&v);
-}
-__device__ __forceinline__ uint32_t pack_h2(float a, float b) {
-  const __half2 v = __floats2half2_rn(a, b);
-  return *reinterpret_cast<const uint32_t *>(&v);
-}
-__device__ __forceinline__ uint32_t hsub2_u(uint32_t a, uint32_t b) {
-  const __half2 v = __hsub2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
-  return *reinterpret_cast<const uint32_t *>(&v);
-}
-__device__ __forceinline__ uint32_t hmul2_u(uint32_t a, uint32_t b) {
-  const __half2 v = __hmul2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
-  return *reinterpret_cast<const uint32_t *>(&v);
-}
-// a / 16 - b
-__device__ __forceinline__ uint32_t hfma16_u(uint32_t a, uint32_t b) {
-  const uint32_t k = 0x2c002c00u;  // 1/16, 1/16
-  const __half2 v = __hfma2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&k),
-                            __hneg2(*reinterpret_cast<const __half2 *>(&b)));
-  return *reinterpret_cast<const uint32_t *>(&v);
-}
 __device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
   uint64_t v;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
@@ -111,11 +87,6 @@ __device__ __forceinline__ bool barrier_and(int id, int count, bool v) {
       : "r"(id), "r"(count), "r"((uint32_t)v)
       : "memory");
   return r != 0;
-}
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
 }
 // 2^e, -126 <= e <= 127
 __device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
