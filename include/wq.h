@@ -383,8 +383,8 @@ typedef struct {
  * is held as s = NaN: it reads back as NaN and makes what attends to it NaN.
  *   k, v:    rows of `dtype` (WQ_BF16, WQ_F32); token t, head g of sequence b starts at
  *            element b stride[0] + t stride[1] + g stride[2] (strides in elements, multiples
- *            of 16 bytes, so that the rows may be slices of a q/k/v buffer); n_src
- *            tokens a sequence.
+ *            of 16 bytes where the dimension is longer than 1, so that the rows may be slices of
+ *            a q/k/v buffer); n_src tokens a sequence.
  *   start:   int32 [batch] on the device: row i of sequence b goes to position start[b] + i.
  *   counts:  int32 [batch] on the device or NULL: rows of sequence b, at most n (NULL: n).
  *   index:   int32 [batch, n] on the device or NULL: row i is source token index[b][i]

@@ -1580,8 +1580,9 @@ wq_status wq_kv_append(const wq_kv_cache *cache, const void *k, const void *v, i
   if (!aligned16(k) || !aligned16(v)) return fail(WQ_ERR_ALIGN, "k or v not 16-byte aligned");
   KvAppendArgs a{};
   const int per16 = dtype == WQ_F32 ? 4 : 8;  // values in 16 bytes
+  const int extent[3] = {cache->batch, n_src, cache->n_kv};
   for (int i = 0; i < 3; ++i) {
-    if (k_stride[i] % per16 != 0 || v_stride[i] % per16 != 0)
+    if (extent[i] > 1 && (k_stride[i] % per16 != 0 || v_stride[i] % per16 != 0))
       return fail(WQ_ERR_ALIGN, "a stride of k or v is not a multiple of 16 bytes");
     a.k_stride[i] = k_stride[i];
     a.v_stride[i] = v_stride[i];
