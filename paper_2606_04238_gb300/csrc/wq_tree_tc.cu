@@ -13,8 +13,9 @@
 // swizzled layout, 12 issues the MMAs.  Two CTAs an SM (256 TMEM columns and ~100 KB
 // each) fill each other's waits: a tile's products, softmax and products again are
 // one chain.  A draft tile's rows are brought into binary16 by an exact power of two
-// a row, of V's taken into the exponent of the row's p (a masked draft then has no say in
-// the others' steps, whatever it holds).  The running maximum is raised, and O rescaled in TMEM, only when 32 of a
+// a row, V's taken into the exponent of the row's p (a masked draft then has no say in the
+// others' steps, whatever it holds); so are V's rows of a context tile whose scales are far
+// apart.  The running maximum is raised, and O rescaled in TMEM, only when 32 of a
 // row's probabilities add up to 2^8: p stays below that, and no maximum is searched.
 //
 // The tiles of all (b, g, row block) are dealt to the CTAs in nearly equal
@@ -70,6 +71,10 @@ constexpr int kQueryShift = 7;
 // Exponents that a draft's V can bring into its score over a quantized cache.  The least is that of zeros, below what the
 // smallest scale gives; with the most, the context's probabilities are still normal numbers in the sums.
 constexpr int kLeastSize = -40, kMostSize = 64;
+// Exponents that V's scales of a tile may span with one power of two for all: a small row's terms then have steps of up to
+// 2^8 times 2^-25 of the largest.  Beyond it each row has its own, as drafts have (4 x 64 drafts over 13,000 positions of
+// 4 bits: 124 us with no such tile, 170 with such tiles alone).
+constexpr int kSpread = 8;
 // registers a thread: the launch's 72 x 416 shared out as 104 x 128 + 56 x 256 + 72 x 32
 constexpr int kRegsSoftmax = 104, kRegsConv = 56;
 
@@ -315,11 +320,11 @@ struct Shared {
   // of a tile: K's scales (times the score scale and the queries' 2^-kQueryShift) and the exponent t of V's operands, which are values
   // times 2^-t.  Two tiles of each: the next tile's are written while this one's are read
   __align__(16) float sk[2][kTile];
-  int te[2];
+  int te[2], spread[2];  // spread: V's scales span more than kSpread exponents, and each row has a t of its own
   uint32_t zk[kTile];                        // 1024 + z of K, twice
   __align__(16) uint2 zsv[kTile];            // 1024 + z of V, twice; its scale times 2^-t, twice
-  __align__(16) uint32_t top[2][kConv / 32]; // warps' shares of the largest V scale of a tile (bits)
-  __align__(16) float td[kTile], tw[kTile];  // exponents t of the drafts' V, 2^-t
+  __align__(16) uint32_t top[2][8];          // four warps' shares of the least and of the largest V scale of a tile (bits)
+  __align__(16) float td[2][kTile], tw[2][kTile];  // rows' own exponents t of V (drafts, spread), 2^-t
 };
 
 // 8 codes as 8 binary16 values code - z; z1024: 1024 + z in both halves.
@@ -510,8 +515,8 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
             const int r = r0 + it * C::RS, ev = (int)(__float_as_uint(mv) >> 23) - 127 - (BITS + 5);
             const int t = min(max(ev, kLeastSize), kMostSize);
             sh.sk[0][r] = qscale * pow2i(-e2);
-            sh.td[r] = (float)t;
-            sh.tw[r] = pow2i(-t);
+            sh.td[0][r] = (float)t;
+            sh.tw[0][r] = pow2i(-t);
             if (ev > kMostSize) sh.wide = 1;
           }
         } else {
@@ -523,7 +528,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
       if constexpr (!BF) {
         if (c == 0)
 #pragma unroll 1
-          for (int it = its; it < C::IT; ++it) sh.td[r0 + it * C::RS] = sh.tw[r0 + it * C::RS] = 0.f;
+          for (int it = its; it < C::IT; ++it) sh.td[0][r0 + it * C::RS] = sh.tw[0][r0 + it * C::RS] = 0.f;
         if (ct == 0) sh.te[0] = 0;
         hand_over(&sh.k_full);
         named_barrier_sync(1, kConv);
@@ -532,7 +537,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
         for (int it = 0; it < its; ++it) {
           uint32_t y[4];
           draft_chunk(vd, it, true, y);
-          if (!wide) scaled(y, sh.tw[r0 + it * C::RS]);
+          if (!wide) scaled(y, sh.tw[0][r0 + it * C::RS]);
           *reinterpret_cast<uint4 *>(vbuf + dst0 + it * C::RS * 128) = make_uint4(y[0], y[1], y[2], y[3]);
         }
       } else {
@@ -552,13 +557,14 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
       fetch(vc, vr, pos_of(i_ctx));
     }
     if (i_ctx > 0) draft_tile();
-    // the warps' largest V scale of the tile whose scales this thread holds (bits; a NaN does not count)
+    // the warps' least and largest V scale of the tile whose scales this thread holds (bits; a NaN counts as the least)
     auto note_top = [&](int which) {
       if (ct < kTile) return;
       uint32_t v = (meta & 0xffffu) > 0x7c00u ? 0u : meta & 0xffffu;
       if (v == 0 || meta == kZeroRow) v = 1;  // kLeastScale
+      const uint32_t lo = __reduce_min_sync(0xffffffffu, v);
       v = __reduce_max_sync(0xffffffffu, v);
-      if (lane == 0) sh.top[which][warp - 4] = v;
+      if (lane == 0) sh.top[which][warp - 8] = lo, sh.top[which][warp - 4] = v;
     };
     if (!BF && i_ctx < nt) {
       note_top(i_ctx & 1);
@@ -583,10 +589,14 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
       } else {
         const int par = i & 1, pn = i + 1 < nt ? p0 + kTile : p0;
         if (i > 0) ok = wait(&sh.k_empty, (i - 1) & 1);
-        // V's operands (code - z) s 2^-t: t puts the tile's largest s in [2^5, 2^6)
-        const uint4 tops = *reinterpret_cast<const uint4 *>(&sh.top[par][4]);
-        const float stop = __half2float(__ushort_as_half((unsigned short)max(max(tops.x, tops.y), max(tops.z, tops.w))));
-        const int te = (int)(__float_as_uint(stop) >> 23) - 127 - 5;
+        // V's operands (code - z) s 2^-t: t puts the tile's largest s in [2^5, 2^6), or where they span too much each
+        // row's own, which then counts in the row's score
+        const uint4 tops = *reinterpret_cast<const uint4 *>(&sh.top[par][4]), lows = *reinterpret_cast<const uint4 *>(&sh.top[par][0]);
+        auto exponent = [](uint32_t h) {
+          return (int)(__float_as_uint(__half2float(__ushort_as_half((unsigned short)h))) >> 23) - 127 - 5;
+        };
+        const int te = exponent(max(max(tops.x, tops.y), max(tops.z, tops.w)));
+        const bool spread = te - exponent(min(min(lows.x, lows.y), min(lows.z, lows.w))) > kSpread;
         {
           const float s0 = __half2float(__ushort_as_half((unsigned short)(meta & 0xffffu)));
           const __half2 z = __hadd2(__half2half2(__ushort_as_half((unsigned short)(meta >> 16))), __float2half2_rn(1024.f));
@@ -595,9 +605,12 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
           if (ct < kTile) {
             sh.sk[par][r] = s0 * qscale;
             sh.zk[r] = zz;
-            if (ct == 0) sh.te[par] = te;
+            if (ct == 0) sh.te[par] = spread ? 0 : te, sh.spread[par] = spread;
           } else {
-            const float sv = (s0 == 0.f || meta == kZeroRow ? kLeastScale : s0) * pow2i(-te);  // (then code - z is 0)
+            float sv = s0 == 0.f || meta == kZeroRow ? kLeastScale : s0;  // (then code - z is 0)
+            const int t = spread ? min((int)(__float_as_uint(sv) >> 23) - 127 - 5, te) : te;  // (a NaN scale's: te)
+            if (spread) sh.td[par][r] = (float)t, sh.tw[par][r] = pow2i(-t);
+            sv *= pow2i(-t);
             sh.zsv[r] = make_uint2(zz, pack_h2(sv, sv));
           }
         }
@@ -714,6 +727,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
           const uint32_t have = n >= 32 ? 0xffffffffu : (1u << n) - 1u;  // (n > 0: works(h))
           return drafts ? have & (h == 0 ? see[0] : h == 1 ? see[1] : h == 2 ? see[2] : see[3]) : have;
         };
+        const bool own_t = !BF && (drafts || sh.spread[par]);  // V's rows have exponents of their own
         const int ti = BF ? 0 : sh.te[par];
         const float te = (float)ti;
         // the 32 columns that this copy works on, where any count
@@ -737,9 +751,9 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
             unpack_f32x2(fma_f32x2(pack_f32x2(u[j], u[j + 1]), k0, mm), u[j], u[j + 1]);
             unpack_f32x2(fma_f32x2(pack_f32x2(u[j + 2], u[j + 3]), k1, mm), u[j + 2], u[j + 3]);
           }
-          if (masks && !BF && drafts)
+          if (masks && own_t)
 #pragma unroll
-            for (int j = 0; j < 32; ++j) u[j] += sh.td[32 * h + j];
+            for (int j = 0; j < 32; ++j) u[j] += sh.td[par][32 * h + j];
           if (masks && some) {
             const uint32_t bits = seen(h);
 #pragma unroll
@@ -789,12 +803,12 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
 #pragma unroll
             for (int j = 0; j < 32; ++j) u[j] += now - ms;
           }
-          if (masks && !BF && drafts) {  // each p stands for 2^-t of itself with a t of its own
-            const bool wide = sh.wide != 0;
+          if (masks && own_t) {  // each p stands for 2^-t of itself with a t of its own
+            const bool wide = drafts && sh.wide != 0;
             part = 0.f;
 #pragma unroll
             for (int j = 0; j < 32; j += 2) {
-              const float e0 = ex2(u[j]) * sh.tw[32 * h + j], e1 = ex2(u[j + 1]) * sh.tw[32 * h + j + 1];
+              const float e0 = ex2(u[j]) * sh.tw[par][32 * h + j], e1 = ex2(u[j + 1]) * sh.tw[par][32 * h + j + 1];
               part += e0 + e1;
               if (wide) p[j / 2] = pack_bf2(e0, e1);
             }
@@ -803,7 +817,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
           // columns 16 h ..: S's there have been read
           tmem_st16(tw + 16 * h, p);
         };
-        if (!search && copies == 1 && !some) {
+        if (!search && copies == 1 && !some && !own_t) {
           // four times in a row: a row's work is bound by latency, which the next columns' loads then overlap
 #pragma unroll
           for (int h = 0; h < 4; ++h) probabilities(h, false);

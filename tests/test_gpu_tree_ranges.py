@@ -116,3 +116,24 @@ def test_a_row_of_zeros_is_marked(wq):
             assert m[1] == m[3] == 0x80003c00 and m[0] >> 31 == 0 and m[2] >> 16 == 0
         k, v = wq.kv_read(c, torch.zeros(1, dtype=torch.int32, device="cuda"), 4, dtype=torch.float32)
         assert (k[0, 1] == 0).all() and (v[0, 3] == 0).all() and not torch.signbit(k[0, 1]).any()
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("ratio", [2.0 ** 7, 2.0 ** 10, 2.0 ** 16, 2.0 ** 20])
+@pytest.mark.parametrize("t", [1, 30])
+def test_large_rows_that_hardly_count(wq, room, bits, ratio, t):
+    """One V row far larger than the others and hardly attended to, and a row of zeros attended to more than all others:
+    in whole tiles and in ragged ones, alone and with other tiles in a range."""
+    def spoil(q, kn, vn, k, v):
+        for j in range(t):
+            q[:, j] = q[:, 0]
+        for x in (v, vn):
+            x.copy_(((x.float() + 0.5) * 2.0 ** -5).to(torch.bfloat16))
+        d = q[:, 0].float()
+        for p, score in ((70, -25.0), (v.shape[1] - 3, -25.0), (300, 9.0)):
+            k[:, p] = (d * (score * 8 / d.pow(2).sum(-1, keepdim=True))).to(torch.bfloat16)
+        v[:, 70], v[:, -3] = (v[:, 70].float() * ratio).to(torch.bfloat16), (v[:, -3].float() * -ratio).to(torch.bfloat16)
+        v[:, 300] = 0
+    close(*run(wq, room, 20, t, 24, 24, 64, bits, [800] * 19 + [701], seed=49, spoil=spoil))
+    close(*run(wq, room, 1, t, 2, 2, 64, bits, [1000], seed=50, spoil=spoil))
+    close(*run(wq, room, 1, t, 8, 8, 64, bits, [333], seed=51, spoil=spoil))
