@@ -422,7 +422,8 @@ __global__ void __launch_bounds__(kTreeWarps * 32, 3) attn_tree_kernel(const Tre
       const int st = i % L::NS, p0 = c0 + i * kTreeTile + warp * 16, n = c1 - p0;  // n: positions of the warp's 16
       ok = __all_sync(0xffffffffu, mbar_wait(&full[st], (i / L::NS) & 1));
       if (!ok) break;
-      const uint32_t mw = meta;
+      // rows of zeros, those of a zero-filled cache too: code - z is 0, and the least scale (kLeastScale) does as well
+      const uint32_t mw = (meta & 0xffffu) == 0 || meta == kZeroRow ? (meta & 0xffff0000u) | 1u : meta;
       if (i + 1 < nt) load_meta(i + 1);
       if (n > 0) {
         const uint8_t *kt = tree_ring + st * L::STAGE + warp * 16 * L::ROW, *vt = kt + L::STAGE / 2;
@@ -468,8 +469,7 @@ __global__ void __launch_bounds__(kTreeWarps * 32, 3) attn_tree_kernel(const Tre
             const int at = 8 * (v / 2) + 2 * tc + v % 2;  // of the 16 positions
             const uint32_t m = __shfl_sync(0xffffffffu, mw, at), mm = __shfl_sync(0xffffffffu, mw, 16 + at);
             const float sk = __half2float(__ushort_as_half((unsigned short)(m & 0xffffu)));
-            float sv = __half2float(__ushort_as_half((unsigned short)(mm & 0xffffu)));
-            if (sv == 0.f || mm == kZeroRow) sv = kLeastScale;  // code - z is 0
+            const float sv = __half2float(__ushort_as_half((unsigned short)(mm & 0xffffu)));
             const float lg = lg2(sv);
             rs[v] = rcp(sv);
             yy[v % 2] = fmaf(yy[v % 2] * qf[0], sk, lg);
