@@ -442,6 +442,10 @@ wq_status wq_qkv_rope(const float *qkv, const void *x, int m, int d, const int32
  *            reach the row.
  *   A length or count outside its range skips the sequence (o unwritten) and records
  *   WQ_ERR_ARG in the device status.  n_heads / n_kv <= 16, max_len < 2^31 - 1024.
+ *   Roundings: each probability once to 16 bits (binary16 over a quantized cache, 2^-11 of
+ *   its term at most; bf16 over a bf16 cache, 2^-8), on long calls over a quantized cache
+ *   each cached V value once to binary16, and o.  Everything else is fp32.  wq_attn_decode,
+ *   one token over a bf16 cache, keeps its probabilities to 24 bits.
  * Workspace: wq_attn_tree_workspace_bytes for up to `batch` sequences and n_draft
  * drafts (no zeroing needed).
  */

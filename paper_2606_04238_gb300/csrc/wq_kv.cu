@@ -14,13 +14,15 @@
 // A row is taken by 8 lanes (HD 128) or 4 (HD 64), 16 values a lane: 3 or 2
 // shuffles for the row's range, and the lane's codes are one 16-byte (8 bits)
 // or 8-byte (4 bits) store.  A lane takes a K row and the V row beside it (one row
-// a lane: less in flight, 28.8 us for 26.6 below).  The row of 8191 tokens of 8 kv
-// heads is written to 4 bits and read back to bf16 in 21.3 us, 3.5 TB/s: the
-// quantizing is bound by issue slots (17 instructions a value where the quotient
-// was a division and codes were clamped one by one 24, 31.5 us).  Reads are bound
-// by HBM: 12,000 tokens of 8 bits 11.0 us, 6.8 TB/s; 32,768 of 4 bits to fp32 49.5
-// us, 6.1 TB/s.  Decode steps are bound by launches: 16 tokens written and read
-// back 4.4 us.
+// a lane: less in flight, 28.8 us for 26.6 below).  8191 tokens of 8 kv heads are
+// written to 4 bits and read back to bf16 in 21.6 us, 3.5 TB/s; written alone, in 14.1
+// us, to 8 bits 13.6, to a bf16 cache 13.1 (5.1 TB/s), and from fp32 17.7, 17.3 and
+// 18.7.  Neither issue slots (55% of them at 4 bits, 17 instructions a value; with a
+// division a value and codes clamped one by one 24, 31.5 us the pair) nor memory is full:
+// a CTA loads its rows once and then works on them, and at 80 registers a thread 20 of
+// an SM's warps cannot hide that.  Reads are bound by HBM: 12,000 tokens of 8 bits 11.0
+// us, 6.8 TB/s; 32,768 of 4 bits to fp32 49.8 us, 6.1 TB/s.  Decode steps are bound by
+// launches: 16 tokens written and read back 4.4 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -320,7 +322,8 @@ __global__ void __launch_bounds__(kReadThreads) kv_read_kernel(const KvReadArgs 
 // takes one token; LPR lanes take a head, 4 values of each half a lane, and a
 // lane's heads are loaded before the sum over x is waited for.  10 tokens of 48 heads
 // of 128 take 2.8 us, launch latency; 1220 tokens of 56 heads 14.4 us, 4.6 TB/s: loads
-// in flight bound it (72 registers a thread leave 7 CTAs of 128 threads an SM).
+// in flight bound it (72 registers a thread leave 7 CTAs of 128 threads an SM, and a CTA's
+// loads start when one before it has left).
 
 template <int HD, int THREADS>
 __global__ void __launch_bounds__(THREADS, 896 / THREADS) qkv_rope_kernel(const QkvRopeArgs a) {

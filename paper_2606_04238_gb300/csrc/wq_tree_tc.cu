@@ -9,8 +9,11 @@
 //   O += P V    128 x HD in TMEM, P as the A operand from TMEM, V [position][HD] in
 //               shared memory as it lies in the cache (MN-major).
 // Thirteen warps: 0-3 softmax (thread = row), 4-11 load a tile's codes into registers
-// one tile ahead, convert them (code - z, exact) and store them in the 128-byte
-// swizzled layout, 12 issues the MMAs.  Two CTAs an SM (256 TMEM columns and ~100 KB
+// one tile ahead, convert them and store them in the 128-byte swizzled layout, 12 issues
+// the MMAs.  K's operands are code - z, exact, its scales factors of the scores.  V's are
+// (code - z) s 2^-t rounded to binary16, t one for a tile: 2^-11 of each term at most, for
+// which the rows' threads, the longest chain, need no factor a position.  P rounds like
+// wq_tree.cu's.  Two CTAs an SM (256 TMEM columns and ~100 KB
 // each) fill each other's waits: a tile's products, softmax and products again are
 // one chain.  A draft tile's rows are brought into binary16 by an exact power of two
 // a row, V's taken into the exponent of the row's p (a masked draft then has no say in the
@@ -23,7 +26,7 @@
 // Ranges of one row block that is split are merged by a second kernel.
 //
 // Measured (device time): 4 sequences of 9,400 to 15,600 positions in 4 bits, 47 to 61
-// drafts, 40 query heads over 8 kv heads of 128: 87 us, 465 TFLOP/s of products that
+// drafts, 40 query heads over 8 kv heads of 128: 89 us, 450 TFLOP/s of products that
 // count.  8 sequences of 1,300 to 3,900 positions in bf16, 33 to 60 drafts, 64 heads over
 // 8 of 64: 55 us.  16 sequences of 580 to 1,950 positions in 8 bits, 4 to 8 drafts: 34 us,
 // of which 7 until the queries are in place and 8 from the last tile to the merged rows.

@@ -1,8 +1,9 @@
-"""Python binding of libwq.so (include/wq.h): argument marshalling only.
+"""Python binding of libwq.so (include/wq.h): argument marshalling, and two helpers that
+prepare arguments (rope_table, tree_mask).
 
 Every function here converts torch tensors to device pointers and sizes,
 calls the C ABI of the same name on the current CUDA stream, and raises
-``WQError`` on a non-zero status.  All arithmetic runs in the CUDA kernels;
+``WQError`` on a non-zero status.  All other arithmetic runs in the CUDA kernels;
 there is no fallback: if the library is missing or no GPU is present the
 calls raise.
 """
@@ -624,7 +625,10 @@ def qkv_rope(qkv, positions, table, n_heads: int, n_kv: int, x=None, head_norm: 
 
 def tree_mask(parents: torch.Tensor) -> torch.Tensor:
     """The mask of wq_attn_tree for int32 parents [batch, T]: parents[b, i] < i is draft i's parent, -1 the
-    context's last token.  int32 [batch, T, ceil(T / 32)]; draft i sees its ancestors and itself."""
+    context's last token.  int32 [batch, T, ceil(T / 32)]; draft i sees its ancestors and itself.
+    Made on the host: parents on the device are copied there (a synchronisation, not for stream capture), and 32 x 128
+    drafts take milliseconds.  A loop whose trees keep their shape makes it once; one that draws a tree a step is better
+    served by a mask that it writes itself."""
     b, t = parents.shape
     up = parents.cpu().tolist()
     words = (t + 31) // 32
