@@ -222,7 +222,8 @@ def prepare(case, seed):
         s["pool"] = [_pack(s.pop(n), c["bits"]) for n in "kv"]
     if own:
         (k, km), (v, vm) = s["pool"]
-        s["pool"] = wq.KVCache(k, v, km, vm, c["hd"], c["bits"])
+        s["pool"] = wq.KVCache(k, v, km, vm, c["hd"], c["bits"]) if c["kind"] != "write" else \
+            wq.kv_pool(s["n_pages"], c["kv"], c["page"], c["hd"], c["bits"])
         if c["kind"] == "attn":
             s.update(ws=wq.attn_paged_workspace(s["lens"].numel(), s["q"].shape[0], c["heads"], c["kv"], c["hd"]),
                      o=torch.empty_like(s["q"]))
