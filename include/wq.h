@@ -65,9 +65,10 @@ typedef enum {
                                take the stack (1..8 tokens, every layer with the same bits, groups
                                and rank), also where the launch chain is the measured-faster route */
 
-#define WQ_HEAD_NORM 8u     /* wq_qkv_rope: unit-weight RMSNorm (eps 1e-6) of every query and key head */
+#define WQ_HEAD_NORM 8u     /* wq_qkv_rope, wq_qkv_paged: RMSNorm (eps 1e-6) of every query and key head */
 
-/* Element types (outputs of wq_down_w4, rows of wq_kv_append and wq_kv_read). */
+/* Element types (outputs of wq_down_w4, rows of wq_kv_append and wq_kv_read, projections of
+ * wq_qkv_paged, rows of wq_paged_read). */
 #define WQ_BF16 0
 #define WQ_F32 1
 
@@ -474,6 +475,114 @@ wq_status wq_decoder_tree_forward(const void *x, int n_draft, const int32_t *len
                                   void *y, void *ws, size_t ws_bytes, void *stream);
 
 /*
+ * Pages.  A pool of pages is a wq_kv_cache whose `batch` is the number of pages and whose
+ * `max_len` is the positions of a page: 16, 32, 64, 128 or 256, the pool's positions below
+ * 2^31.  Position p of a request is place p % page of the page that entry p / page of its row
+ * of a block table names (int32 [batch, max_pages]); slot s of the pool is place s % page of
+ * page s / page.  Requests may share pages that none of them writes to.
+ */
+
+/*
+ * The plan of one step of a continuous batch.  Request b holds lens[b] positions in the
+ * first ceil(lens[b] / page) pages of its table row, keeps the first keep[b] of them (fewer:
+ * rejected drafts; 0: the request has ended and another takes its place) and adds n_new[b]
+ * tokens.  Pages that it no longer needs go back on the stack of free pages, in request
+ * order; then, in request order, pages that it needs beyond those it holds are taken from the
+ * top and entered in its row.
+ *   lens:       int32 [batch].  keep: int32 [batch] or NULL (lens).  n_new: int32 [batch].
+ *   tables:     int32 [batch, max_pages], in place: only entries from ceil(lens[b] / page)
+ *               on are written (what a request gives back stays in its row, out of use).
+ *   free_pages: int32 [n_pages], in place: a stack of n_free[0] pages; written from there on.
+ *   n_free, n_free_out: int32 [1], and what is left.  n_free_out may be n_free.
+ *   cu:         int32 [batch + 1]: request b's tokens are rows cu[b] .. cu[b + 1] - 1 of the
+ *               step (at most m).
+ *   kv_lens:    int32 [batch]: keep[b] + n_new[b], the next step's lens; may be lens.  -1:
+ *               the request is not served (below), holds what it held, and its lens is to
+ *               be put back.
+ *   positions, slots: int32 [m]: where each row's token stands and the slot that its K and V
+ *               go to; 0 and -1 for rows of requests that are not served and rows behind
+ *               the last request.
+ *   Not served: requests that take pages where they and those before them want more than
+ *   there are; and, recorded as WQ_ERR_ARG in the device status, requests whose numbers are
+ *   out of range (0 <= keep <= lens <= max_pages page, 0 <= n_new, keep + n_new <= max_pages
+ *   page) or whose tokens do not all fit into m rows.  A page number outside the pool that a
+ *   row or the stack holds is recorded too; its slots are -1.
+ *   page as above; batch <= 2048, m <= 2^18, max_pages page <= 2^31 - 1024.  batch == 0 is a no-op.
+ */
+wq_status wq_page_plan(const int32_t *lens, const int32_t *keep, const int32_t *n_new, int batch, int page, int32_t *tables,
+                       int max_pages, int32_t *free_pages, int n_pages, const int32_t *n_free, int32_t *n_free_out, int m,
+                       int32_t *cu, int32_t *kv_lens, int32_t *positions, int32_t *slots, void *stream);
+
+/*
+ * Query, key and value rows of m tokens from their projections, K and V written to the
+ * tokens' slots, quantized as wq_kv_append does:
+ *   u = rs qkv[t], rs = 1 / sqrt(mean(x[t]^2) + 1e-6) (x NULL: 1); q and k heads normed
+ *   (WQ_HEAD_NORM) and multiplied by q_norm, k_norm, then rotated as in wq_qkv_rope.  Every
+ *   step is fp32; q (and K, V of a bf16 pool) are rounded once to bf16, codes are those
+ *   of the fp32 rows.
+ *   qkv:       [m, (n_heads + 2 n_kv) head_dim] of qkv_dtype (WQ_BF16, WQ_F32): q, k, v heads.
+ *   positions: int32 [m] or NULL (no rotation; table and n_pos are then not looked at).  Outside
+ *              [0, n_pos) the token is skipped and WQ_ERR_ARG recorded in the device status.
+ *   q_norm, k_norm: bf16 [head_dim] or NULL (ones).
+ *   slots:     int32 [m], different from one another; -1: the token's K and V are not kept.
+ *              Outside the pool: the same, recorded as WQ_ERR_ARG.
+ *   q:         bf16 [m, n_heads, head_dim].
+ */
+wq_status wq_qkv_paged(const void *qkv, int qkv_dtype, const void *x, int m, int d, const int32_t *positions,
+                       const float *table, int n_pos, const void *q_norm, const void *k_norm, int n_heads, unsigned flags,
+                       const wq_kv_cache *pool, const int32_t *slots, void *q, void *stream);
+
+/*
+ * Reads the rows at m slots back: k, v of `dtype` [m, n_kv, head_dim], exact (WQ_F32) or
+ * rounded once (WQ_BF16); zeros where a slot is -1.  A slot outside the pool is recorded as
+ * WQ_ERR_ARG and its rows are left unwritten.  m n_kv < 2^29.
+ */
+wq_status wq_paged_read(const wq_kv_cache *pool, const int32_t *slots, int m, void *k, void *v, int dtype, void *stream);
+
+/*
+ * Causal attention of a ragged batch over its pages (grouped-query heads, kv head
+ * g = h / (n_heads / n_kv)): decode steps, chunks of prompts, whole prompts, and all of them
+ * in one call.  Sequence b has rows cu[b] .. cu[b + 1] - 1 (nq of them) and kv_lens[b]
+ * positions, its new tokens' among them (wq_qkv_paged has written them).  Its row i sees the
+ * first kv_lens[b] - nq + i + 1:
+ *   o = bf16( softmax_j(scale q . K_j) V_j ).
+ *   q, o:    bf16 [m, n_heads, head_dim].  Rows behind cu[batch] are left as they were.
+ *   cu:      int32 [batch + 1], kv_lens: int32 [batch], tables: int32 [batch, max_pages], all
+ *            on the device (wq_page_plan makes them).
+ *   max_q:   the most rows of a sequence, 1 <= max_q <= m: a hint for which kernels run, and a bound.
+ *   What positions hold that a row does not see, infinities and NaN too, does not reach it.
+ *   kv_lens[b] == -1: the sequence's rows are zeros.  Offsets that do not ascend within m, more
+ *   than max_q rows, or a length below nq or above max_pages page skip the sequence (o
+ *   unwritten); a page outside the pool is read as page 0.  All are recorded as WQ_ERR_ARG
+ *   in the device status.
+ *   n_heads / n_kv <= 16, batch <= 2048, m <= 2^18, max_pages page <= 2^31 - 1024.
+ *   Roundings: each probability once to 16 bits (binary16 over a quantized pool, 2^-11 of
+ *   its term at most; bf16 over a bf16 pool, 2^-8), and o.  Everything else is fp32.
+ * Workspace: wq_attn_paged_workspace_bytes for up to `batch` sequences and m rows, zero-filled
+ * before first use (wq_workspace_init).
+ */
+size_t wq_attn_paged_workspace_bytes(int batch, int m, int n_heads, int n_kv, int head_dim);
+wq_status wq_attn_paged(const void *q, int m, int max_q, int n_heads, const wq_kv_cache *pool, int batch, const int32_t *cu,
+                        const int32_t *kv_lens, const int32_t *tables, int max_pages, float scale, void *o, void *ws,
+                        size_t ws_bytes, void *stream);
+
+/*
+ * One step of a decoder layer for the m rows of a ragged batch over its pages:
+ *   qkv = x deq(Wqkv)^T (fp32), q and the pages' rows by wq_qkv_paged(..., WQ_HEAD_NORM),
+ *   o = wq_attn_paged(..., scale 1/sqrt(head_dim)), then the output projection and the MLP block as in
+ *   wq_decoder_layer_forward (flags likewise).
+ * x, y: bf16 [m, d].  The y of rows behind cu[batch] means nothing.  The layer's rope_theta
+ * is not used (the angles are the table's).  m <= 16384.
+ * Workspace: wq_decoder_paged_workspace_bytes, zero-filled before first use (wq_workspace_init).
+ */
+size_t wq_decoder_paged_workspace_bytes(int batch, int m, const wq_decoder_layer *layer);
+wq_status wq_decoder_paged_forward(const void *x, int m, int max_q, int batch, const int32_t *cu, const int32_t *kv_lens,
+                                   const int32_t *positions, const int32_t *slots, const wq_decoder_layer *layer,
+                                   const void *q_norm, const void *k_norm, const wq_kv_cache *pool, const int32_t *tables,
+                                   int max_pages, const float *table, int n_pos, unsigned flags, void *y, void *ws,
+                                   size_t ws_bytes, void *stream);
+
+/*
  * A mixture-of-experts MLP block (the MoE model of Sec. 5: a router picks a
  * few experts per token, so a decode step reads only those experts' weights,
  * which is how expert routing shrinks the realized gain of the 2-bit gate/up).
@@ -574,8 +683,8 @@ const char *wq_last_error(void);
 
 /* Reads and clears the device-side status words of the current device: WQ_OK,
  * WQ_ERR_TIMEOUT (a bounded wait ran out) or WQ_ERR_ARG (wq_attn_decode met a
- * sequence length outside its cache, or one of the KV-cache calls a start, count,
- * index, position or length outside its range).  Synchronizes the device. */
+ * sequence length outside its cache, or one of the KV-cache and page calls a start, count,
+ * index, position, length, slot or page outside its range).  Synchronizes the device. */
 wq_status wq_device_status(int *status);
 
 /* Library version string. */

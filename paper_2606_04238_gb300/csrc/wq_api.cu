@@ -16,6 +16,7 @@
 #include "wq_batch.h"
 #include "wq_internal.h"
 #include "wq_kv.h"
+#include "wq_paged.h"
 #include "wq_launch.h"
 #include "wq_stack.h"
 
@@ -1299,13 +1300,14 @@ namespace {
 // projections', the attention partials and the intermediates qkv (fp32), o, x1
 // and h (bf16).
 struct DecoderWs {
-  size_t cnt_qkv, cnt_o, mlp, proj_qkv, proj_o, attn, qkv, o, x1, h, q, total;
+  size_t cnt_qkv, cnt_o, cnt_attn, mlp, proj_qkv, proj_o, attn, qkv, o, x1, h, q, total;
   size_t b_qkv, b_o;  // sizes of the projections' counter blocks
   size_t n_mlp, n_attn;
 };
 
-// n_attn bytes for the attention's partial results, n_q for query rows of their own.
-bool decoder_ws(int batch, const wq_decoder_layer &Ly, size_t n_attn, size_t n_q, DecoderWs *W) {
+// n_attn bytes for the attention's partial results, n_q for query rows of their own, n_cnt for the attention's arrival
+// counters (counters are where calls of every batch that share a workspace find them).
+bool decoder_ws(int batch, const wq_decoder_layer &Ly, size_t n_attn, size_t n_q, DecoderWs *W, size_t n_cnt = 0) {
   const int d = Ly.mlp.gate.k, inter = Ly.mlp.gate.n;
   const int H = Ly.n_heads, Hkv = Ly.n_kv, hd = Ly.head_dim;
   const int nqkv = (H + 2 * Hkv) * hd;
@@ -1319,6 +1321,7 @@ bool decoder_ws(int batch, const wq_decoder_layer &Ly, size_t n_attn, size_t n_q
   size_t off = 0;
   W->cnt_qkv = off;  off = up256(off + W->b_qkv);
   W->cnt_o = off;    off = up256(off + W->b_o);
+  W->cnt_attn = off; off = up256(off + n_cnt);
   W->mlp = off;      off = up256(off + W->n_mlp);
   W->proj_qkv = off; off = up256(off + n_qkv - W->b_qkv);
   W->proj_o = off;   off = up256(off + n_o - W->b_o);
@@ -1706,6 +1709,205 @@ wq_status wq_decoder_tree_forward(const void *x, int n_draft, const int32_t *len
 
 namespace {
 
+// A pool: a cache of pages of 16 to 256 positions, a power of two; log2 of it in *shift.
+wq_status check_page(int page, int *shift) {
+  int s = 4;
+  while (s < 8 && 1 << s != page) ++s;
+  if (1 << s != page) return fail(WQ_ERR_UNSUPPORTED, "pages of %d positions: 16, 32, 64, 128 or 256", page);
+  *shift = s;
+  return WQ_OK;
+}
+wq_status check_pool(const wq_kv_cache *c, int *shift) {
+  wq_status st;
+  if ((st = check_cache(c)) != WQ_OK || (st = check_page(c->max_len, shift)) != WQ_OK) return st;
+  if ((long long)c->batch * c->max_len > INT32_MAX) return fail(WQ_ERR_SHAPE, "a pool of %d pages of %d", c->batch, c->max_len);
+  return WQ_OK;
+}
+// A ragged batch: its sequences, rows and the width of its tables.
+wq_status check_ragged(int batch, int m, int max_pages, int page) {
+  if (batch < 0 || batch > kMaxRequests) return fail(batch < 0 ? WQ_ERR_ARG : WQ_ERR_SHAPE, "%d requests, at most %d", batch, kMaxRequests);
+  if (m < 0 || m > kMaxPlanRows) return fail(m < 0 ? WQ_ERR_ARG : WQ_ERR_SHAPE, "%d rows, at most %d", m, kMaxPlanRows);
+  if (max_pages <= 0 || (long long)max_pages * page > INT32_MAX - 1023)
+    return fail(WQ_ERR_SHAPE, "tables of %d pages of %d positions", max_pages, page);
+  return WQ_OK;
+}
+wq_status check_group(int n_heads, int n_kv) {
+  if (n_heads <= 0 || n_heads % n_kv != 0 || n_heads / n_kv > 16)
+    return fail(WQ_ERR_UNSUPPORTED, "n_heads %d / n_kv %d: a multiple, at most 16 query heads a kv head", n_heads, n_kv);
+  return WQ_OK;
+}
+
+// The arrival counters, at the workspace's start, and the partial results behind them.
+size_t paged_counter_bytes(int sms) { return up256(sizeof(int) * (size_t)attn_paged_ctas(sms)); }
+size_t paged_part_bytes(int hd, int sms) { return up256(4 * attn_paged_part_floats(hd, sms)); }
+
+wq_status attn_paged_impl(const void *q, int m, int max_q, int n_heads, const wq_kv_cache *pool, int batch, const int32_t *cu,
+                          const int32_t *kv_lens, const int32_t *tables, int max_pages, float scale, void *o, void *counters,
+                          void *part, cudaStream_t s) {
+  wq_status st;
+  AttnPagedArgs a{};
+  if ((st = check_pool(pool, &a.shift)) != WQ_OK || (st = check_ragged(batch, m, max_pages, pool->max_len)) != WQ_OK ||
+      (st = check_group(n_heads, pool->n_kv)) != WQ_OK)
+    return st;
+  if (!std::isfinite(scale)) return fail(WQ_ERR_ARG, "score scale not finite");
+  if (batch == 0 || m == 0) return ok();
+  if (max_q < 1 || max_q > m) return fail(WQ_ERR_ARG, "max_q %d of %d rows", max_q, m);
+  if (!q || !cu || !kv_lens || !tables || !o || !counters) return fail(WQ_ERR_ARG, "null pointer");
+  if (!aligned16(q) || !aligned16(o) || !aligned16(counters)) return fail(WQ_ERR_ALIGN, "q, o or workspace not 16-byte aligned");
+  const int sms = num_sms();
+  if (sms <= 0) return fail(WQ_ERR_CUDA, "cannot query the current device");
+  a.q = q, a.kc = pool->k, a.vc = pool->v, a.km = pool->k_meta, a.vm = pool->v_meta;
+  a.cu = cu, a.kv_lens = kv_lens, a.tables = tables;
+  a.m = m, a.max_q = max_q, a.batch = batch, a.H = n_heads, a.Hkv = pool->n_kv, a.n_pages = pool->batch, a.max_pages = max_pages;
+  a.scale = scale * 1.4426950408889634f;  // scores in units of log 2
+  a.counters = static_cast<int *>(counters);
+  a.part = static_cast<float *>(part);
+  a.o = o;
+  cudaError_t e = launch_attn_paged(a, pool->head_dim, pool->bits, sms, s);
+  if (e != cudaSuccess) return cuda_fail(e, "paged attention launch");
+  return ok();
+}
+
+}  // namespace
+
+extern "C" {
+
+wq_status wq_page_plan(const int32_t *lens, const int32_t *keep, const int32_t *n_new, int batch, int page, int32_t *tables,
+                       int max_pages, int32_t *free_pages, int n_pages, const int32_t *n_free, int32_t *n_free_out, int m,
+                       int32_t *cu, int32_t *kv_lens, int32_t *positions, int32_t *slots, void *stream) {
+  wq_status st;
+  PagePlanArgs a{};
+  if ((st = check_page(page, &a.shift)) != WQ_OK || (st = check_ragged(batch, m, max_pages, page)) != WQ_OK) return st;
+  if (n_pages <= 0 || (long long)n_pages * page > INT32_MAX) return fail(WQ_ERR_SHAPE, "a pool of %d pages of %d", n_pages, page);
+  if ((long long)batch * max_pages > INT32_MAX) return fail(WQ_ERR_SHAPE, "tables of %d x %d pages", batch, max_pages);
+  if (batch == 0) return ok();
+  if (!lens || !n_new || !tables || !free_pages || !n_free || !n_free_out || !cu || !kv_lens || (m > 0 && (!positions || !slots)))
+    return fail(WQ_ERR_ARG, "null pointer");
+  a.lens = lens, a.keep = keep, a.n_new = n_new, a.tables = tables, a.free_pages = free_pages;
+  a.n_free = n_free, a.n_free_out = n_free_out;
+  a.batch = batch, a.max_pages = max_pages, a.n_pages = n_pages, a.m = m;
+  a.cu = cu, a.kv_lens = kv_lens, a.positions = positions, a.slots = slots;
+  cudaError_t e = launch_page_plan(a, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(e, "page plan launch");
+  return ok();
+}
+
+wq_status wq_qkv_paged(const void *qkv, int qkv_dtype, const void *x, int m, int d, const int32_t *positions,
+                       const float *table, int n_pos, const void *q_norm, const void *k_norm, int n_heads, unsigned flags,
+                       const wq_kv_cache *pool, const int32_t *slots, void *q, void *stream) {
+  wq_status st;
+  QkvPagedArgs a{};
+  if ((st = check_pool(pool, &a.shift)) != WQ_OK || (st = check_dtype(qkv_dtype)) != WQ_OK) return st;
+  if (m < 0) return fail(WQ_ERR_ARG, "m %d", m);
+  if (flags & ~WQ_HEAD_NORM) return fail(WQ_ERR_ARG, "unknown flags 0x%x", flags);
+  if ((q_norm || k_norm) && !(flags & WQ_HEAD_NORM)) return fail(WQ_ERR_ARG, "weights of a head norm without WQ_HEAD_NORM");
+  if (n_heads <= 0 || (long long)n_heads + 2ll * pool->n_kv > 1 << 16) return fail(WQ_ERR_SHAPE, "heads %d/%d", n_heads, pool->n_kv);
+  if (x && (d <= 0 || d % 8 != 0)) return fail(WQ_ERR_SHAPE, "d %d (a positive multiple of 8)", d);
+  if (positions && n_pos <= 0) return fail(WQ_ERR_SHAPE, "a table of %d positions", n_pos);
+  if (m == 0) return ok();
+  if (!qkv || !slots || !q || (positions && !table)) return fail(WQ_ERR_ARG, "null pointer");
+  const void *all[] = {qkv, x, positions ? table : nullptr, q_norm, k_norm, q};
+  for (const void *p : all)
+    if (!aligned16(p)) return fail(WQ_ERR_ALIGN, "qkv, x, table, q_norm, k_norm or q not 16-byte aligned");
+  a.qkv = qkv, a.x = x, a.positions = positions, a.table = table, a.q_norm = q_norm, a.k_norm = k_norm, a.slots = slots;
+  a.kc = pool->k, a.vc = pool->v, a.km = pool->k_meta, a.vm = pool->v_meta, a.q = q;
+  a.d = d, a.n_heads = n_heads, a.n_kv = pool->n_kv, a.n_pos = n_pos, a.head_norm = (flags & WQ_HEAD_NORM) ? 1 : 0;
+  a.n_pages = pool->batch;
+  cudaError_t e = launch_qkv_paged(a, m, pool->head_dim, pool->bits, qkv_dtype == WQ_F32, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(e, "paged projection launch");
+  return ok();
+}
+
+wq_status wq_paged_read(const wq_kv_cache *pool, const int32_t *slots, int m, void *k, void *v, int dtype, void *stream) {
+  wq_status st;
+  PagedReadArgs a{};
+  if ((st = check_pool(pool, &a.shift)) != WQ_OK || (st = check_dtype(dtype)) != WQ_OK) return st;
+  if (m < 0) return fail(WQ_ERR_ARG, "m %d", m);
+  if ((long long)m * pool->n_kv >= 1ll << 29) return fail(WQ_ERR_SHAPE, "%d rows x %d heads in one call", m, pool->n_kv);
+  if (m == 0) return ok();
+  if (!slots || !k || !v) return fail(WQ_ERR_ARG, "null pointer");
+  if (!aligned16(k) || !aligned16(v)) return fail(WQ_ERR_ALIGN, "k or v not 16-byte aligned");
+  a.kc = pool->k, a.vc = pool->v, a.km = pool->k_meta, a.vm = pool->v_meta, a.slots = slots, a.k = k, a.v = v;
+  a.m = m, a.n_kv = pool->n_kv, a.n_pages = pool->batch;
+  cudaError_t e = launch_paged_read(a, pool->head_dim, pool->bits, dtype == WQ_F32, static_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return cuda_fail(e, "paged read launch");
+  return ok();
+}
+
+size_t wq_attn_paged_workspace_bytes(int batch, int m, int n_heads, int n_kv, int head_dim) {
+  const int sms = num_sms();
+  if (batch <= 0 || m <= 0 || n_heads <= 0 || n_kv <= 0 || head_dim <= 0 || n_heads % n_kv != 0 || sms <= 0) return 0;
+  return paged_counter_bytes(sms) + paged_part_bytes(head_dim, sms);
+}
+
+wq_status wq_attn_paged(const void *q, int m, int max_q, int n_heads, const wq_kv_cache *pool, int batch, const int32_t *cu,
+                        const int32_t *kv_lens, const int32_t *tables, int max_pages, float scale, void *o, void *ws,
+                        size_t ws_bytes, void *stream) {
+  size_t at = 0;
+  if (pool && batch > 0 && m > 0 && ws) {
+    const int sms = num_sms();
+    const size_t need = wq_attn_paged_workspace_bytes(batch, m, n_heads, pool->n_kv, pool->head_dim);
+    // (sizes without a workspace are refused below)
+    if (need && ws_bytes < need) return fail(WQ_ERR_WORKSPACE, "attention workspace of %zu bytes, %zu needed", ws_bytes, need);
+    if (need) at = paged_counter_bytes(sms);
+  }
+  return attn_paged_impl(q, m, max_q, n_heads, pool, batch, cu, kv_lens, tables, max_pages, scale, o, ws,
+                         static_cast<uint8_t *>(ws) + at, static_cast<cudaStream_t>(stream));
+}
+
+size_t wq_decoder_paged_workspace_bytes(int batch, int m, const wq_decoder_layer *layer) {
+  const int sms = num_sms();
+  if (!layer || batch <= 0 || m <= 0 || m > kMaxGemmTokens || sms <= 0) return 0;
+  DecoderWs W;
+  return decoder_ws(m, *layer, paged_part_bytes(layer->head_dim, sms), (size_t)m * layer->n_heads * layer->head_dim * 2, &W,
+                    paged_counter_bytes(sms))
+             ? W.total
+             : 0;
+}
+
+wq_status wq_decoder_paged_forward(const void *x, int m, int max_q, int batch, const int32_t *cu, const int32_t *kv_lens,
+                                   const int32_t *positions, const int32_t *slots, const wq_decoder_layer *layer,
+                                   const void *q_norm, const void *k_norm, const wq_kv_cache *pool, const int32_t *tables,
+                                   int max_pages, const float *table, int n_pos, unsigned flags, void *y, void *ws,
+                                   size_t ws_bytes, void *stream) {
+  if (!layer) return fail(WQ_ERR_ARG, "null layer");
+  const wq_decoder_layer &Ly = *layer;
+  const int d = Ly.mlp.gate.k, H = Ly.n_heads, Hkv = Ly.n_kv, hd = Ly.head_dim;
+  wq_status st;
+  int shift;
+  if ((st = check_decoder_layer(Ly)) != WQ_OK || (st = check_pool(pool, &shift)) != WQ_OK ||
+      (st = check_ragged(batch, m, max_pages, pool->max_len)) != WQ_OK)
+    return st;
+  if (pool->n_kv != Hkv || pool->head_dim != hd)
+    return fail(WQ_ERR_SHAPE, "pool of %d heads of %d, layer of %d of %d", pool->n_kv, pool->head_dim, Hkv, hd);
+  if (flags & ~WQ_PRENORM) return fail(WQ_ERR_ARG, "unknown flags 0x%x", flags);
+  if (m > kMaxGemmTokens) return fail(WQ_ERR_SHAPE, "%d rows, at most %d", m, kMaxGemmTokens);
+  if (batch == 0 || m == 0) return ok();
+  if (max_q < 1 || max_q > m) return fail(WQ_ERR_ARG, "max_q %d of %d rows", max_q, m);
+  if (!x || !cu || !kv_lens || !positions || !slots || !tables || !table || !y) return fail(WQ_ERR_ARG, "null pointer");
+  const int sms = num_sms();
+  if (sms <= 0) return fail(WQ_ERR_CUDA, "cannot query the current device");
+  DecoderWs W;
+  if (!decoder_ws(m, Ly, paged_part_bytes(hd, sms), (size_t)m * H * hd * 2, &W, paged_counter_bytes(sms)))
+    return fail(WQ_ERR_SHAPE, "no workspace layout for this layer");
+  if (!ws || ws_bytes < W.total) return fail(WQ_ERR_WORKSPACE, "decoder workspace of %zu bytes, %zu needed", ws_bytes, W.total);
+  uint8_t *w8 = static_cast<uint8_t *>(ws);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if ((st = decoder_projection("qkv", x, m, &Ly.qkv, nullptr, w8 + W.qkv, WQ_F32, W.b_qkv, W.cnt_qkv, W.proj_qkv, w8, s)) != WQ_OK)
+    return st;
+  if ((st = wq_qkv_paged(w8 + W.qkv, WQ_F32, x, m, d, positions, table, n_pos, q_norm, k_norm, H, WQ_HEAD_NORM, pool, slots,
+                         w8 + W.q, stream)) != WQ_OK)
+    return fail(st, "projections to pages: %s", g_last_error.c_str());
+  if ((st = attn_paged_impl(w8 + W.q, m, max_q, H, pool, batch, cu, kv_lens, tables, max_pages, 1.f / std::sqrt((float)hd),
+                            w8 + W.o, w8 + W.cnt_attn, w8 + W.attn, s)) != WQ_OK)
+    return fail(st, "attention: %s", g_last_error.c_str());
+  return decoder_after_attention(x, m, Ly, flags, y, W, w8, s);
+}
+
+}  // extern "C"
+
+namespace {
+
 // Plans and workspace regions of a mixture-of-experts block for m tokens:
 // the slots' arrival counters first (zero between calls), then the routing
 // outputs, tile partials, h and the experts' fp32 outputs of every slot, then
@@ -2043,6 +2245,12 @@ wq_status wq_device_status(int *status) {
   if (e != cudaSuccess) return cuda_fail(e, "device status read");
   if (*status == 0) *status = g;
   e = read_batch_status(&g);
+  if (e != cudaSuccess) return cuda_fail(e, "device status read");
+  if (*status == 0) *status = g;
+  e = read_pages_status(&g);
+  if (e != cudaSuccess) return cuda_fail(e, "device status read");
+  if (*status == 0) *status = g;
+  e = read_attn_paged_status(&g);
   if (e != cudaSuccess) return cuda_fail(e, "device status read");
   if (*status == 0) *status = g;
   return ok();

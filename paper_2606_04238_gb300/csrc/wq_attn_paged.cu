@@ -1,0 +1,598 @@
+// wq_attn_paged.cu -- causal attention of a ragged batch over a paged KV cache of 16, 8 or 4
+// bits (sm_103a) on mma.sync, for sequences of few query rows: decode steps and short runs
+// of drafts.
+//
+// Query i of a sequence of nq stands at position kv_len - nq + i and sees the positions up to
+// its own.  Row r = i rep + h stands for token i and query head g rep + h of kv head g:
+//   x_j = scale log2(e) (q . k_j),  o = sum_j 2^(x_j - m) v_j / sum_j 2^(x_j - m).
+// Positions are the products' M and rows their N: S^T = K Q^T and O^T = V^T P^T, so that
+// 8 rows take what 16 would as M, and a lane's softmax values are half as many.  A cached row
+// of 8 or 4 bits is s (code - z), and code - z is exact in binary16: K's scale multiplies the
+// score, V's is taken into the exponent,
+//   p_j = 2^(x_j + log2 s_j - m),  o = sum_j p_j (code - z)_j / sum_j p_j / s_j,
+// with m the running maximum of x_j + log2 s_j.  (Codes as they lie there are binary16 too,
+// subnormal numbers code 2^-24, and the zero points could come off the sums: a third of the
+// instructions less.  But the tensor cores add products of subnormal numbers with 2^-14 of
+// their size lost, a 4-bit column's error then 2^-14 of its codes and not of their difference.)
+// p_j is rounded to binary16 (2^-11 of its term at most; 2^6 larger than above, so that small
+// ones are normal numbers) or over a bf16 cache to bf16 (2^-8); everything else is fp32.
+//
+// The blocks of 64 positions of all (sequence, row tile, kv head) are laid end to end and
+// every CTA takes an equal run of them, found from the lengths themselves; what it has of an
+// (item) that other CTAs share is left in the workspace, and the last of them to arrive adds
+// up all parts in their order.  A warp takes 16 positions at a time, which always lie in one
+// page, through a ring of its own that cp.async fills: no warp waits for another.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <atomic>
+#include <cstdint>
+
+#include "wq_cvt.cuh"
+#include "wq_frag.cuh"
+#include "wq_internal.h"
+#include "wq_kv.h"
+#include "wq_paged.h"
+#include "wq_ptx.cuh"
+
+namespace wq {
+
+// Status word: WQ_OK (0), or WQ_ERR_ARG (-1) after a row offset, length or page outside its
+// range was met (that sequence is skipped; a page outside the pool is read as page 0).
+__device__ int g_attn_paged_status = 0;
+
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kUnit = 16;            // positions a warp takes at a time
+constexpr int kBlock = kWarps * kUnit;
+constexpr int kCtasPerSm = 4;        // at most
+constexpr int kMostRows = 16;        // rows of an item at most
+
+// An 8 x 8 matrix of 16-bit values (row lane / 4, columns 2 (lane % 4) ..) transposed.
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+__device__ __forceinline__ void cp_async4(void *dst, const void *src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_addr(dst)), "l"(src) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// How a warp holds 16 positions.  K: lane (gr, tc) takes 16-byte pieces tc, tc + 4, .. of the
+// row in place gr and of that in place gr + 8 (KW words each: half or a quarter of a piece
+// where rows are shorter than 128 bytes).  V: lane (gr, tc) takes pieces gr, gr + 8, .. of the
+// rows tc, tc + 4, tc + 8 and tc + 12.  Row p lies in place 2 (p % 4) + p / 4 % 2 of its eight
+// for K, so that place j of the product's order is row j / 2 + 4 (j % 2) for both.  Pieces are
+// permuted within a row by what keeps a quarter warp's lanes in different banks.
+template <int HD, int BITS>
+struct Lay : RowLay<HD, BITS> {
+  static constexpr int ROW = RowLay<HD, BITS>::ROW;
+  static constexpr int CHR = ROW / 16, COPIES = kUnit * CHR / 32;  // pieces a row; copies a lane of K, and of V
+  static constexpr int STAGE = 2 * kUnit * ROW + (BITS == 16 ? 0 : 128);
+  static constexpr int NS = BITS == 16 && HD == 128 ? 3 : 16 * 1024 / STAGE < 6 ? 16 * 1024 / STAGE : 6;
+  static constexpr int RING = kWarps * NS * STAGE;
+  static __device__ __forceinline__ int k_swz(int place) { return ROW >= 128 ? 4 * (place & 1) : 0; }
+  static __device__ __forceinline__ int v_swz(int row) { return ROW >= 128 ? 2 * (row & 3) : ROW == 64 ? 2 * (row / 2 & 1) : 0; }
+};
+
+// CTAs an SM holds: 128 registers a thread for 8 rows, 168 for 16; a bf16 ring of heads of 128 takes 96 KB.
+constexpr int occupancy(int hd, int bits, int nt) { return bits == 16 && hd == 128 ? 2 : nt == 1 ? kCtasPerSm : 3; }
+
+// A sequence: its first row and rows, positions; blocks of 64 positions of each of its items.
+struct Seq {
+  int q0, nq, len, blocks, tiles;  // tiles of rows
+};
+// items of no blocks where a row offset or length is out of range, or there are no rows.
+__device__ __forceinline__ Seq get_seq(const AttnPagedArgs &a, int b, int rep, int rows, bool &bad) {
+  Seq s;
+  s.q0 = a.cu[b];
+  const int q1 = a.cu[b + 1];
+  s.len = a.kv_lens[b];
+  s.nq = q1 - s.q0;
+  const bool none = s.len == -1;  // not served: rows of zeros
+  const bool ok = s.q0 >= 0 && q1 >= s.q0 && q1 <= a.m && s.nq <= a.max_q && (none || (s.len >= s.nq && s.len <= a.max_pages << a.shift));
+  bad |= !ok;
+  if (none) s.len = 0;
+  s.tiles = ok ? (s.nq * rep + rows - 1) / rows : 0;
+  s.blocks = max(1, (s.len + kBlock - 1) / kBlock);
+  return s;
+}
+
+}  // namespace
+
+template <int HD, int BITS, int NT>
+__global__ void __launch_bounds__(kWarps * 32, occupancy(HD, BITS, NT)) attn_paged_kernel(const AttnPagedArgs a) {
+  using L = Lay<HD, BITS>;
+  constexpr int ROWS = 8 * NT, OS = HD + 4;
+  extern __shared__ __align__(128) uint8_t paged_ring[];
+  __shared__ float sm[kWarps][ROWS], sl[kWarps][ROWS];
+  __shared__ int last;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gr = lane >> 2, tc = lane & 3;
+  uint8_t *const ring = paged_ring + warp * (L::NS * L::STAGE);
+  const int rep = a.H / a.Hkv, page = 1 << a.shift;
+  pdl_wait();
+  pdl_launch_dependents();
+
+  // ---- this CTA's run of blocks: every warp the same sums
+  bool bad = false;
+  long long total = 0;
+  for (int b = lane; b < a.batch; b += 32) {
+    const Seq s = get_seq(a, b, rep, ROWS, bad);
+    total += (long long)s.blocks * s.tiles;
+  }
+#pragma unroll
+  for (int o = 16; o >= 1; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+  total *= a.Hkv;
+  if (bad && blockIdx.x == 0) atomicExch(&g_attn_paged_status, -1);
+  const long long N = min((long long)gridDim.x, total), c = blockIdx.x;
+  if (c >= N) return;
+  const long long x0 = total * c / N, x1 = total * (c + 1) / N;
+  // the sequence that x0 falls into
+  int b = 0;
+  long long base = 0;
+  Seq s{};
+  for (int b0 = 0;; b0 += 32) {
+    long long mine = 0;
+    if (b0 + lane < a.batch) {
+      s = get_seq(a, b0 + lane, rep, ROWS, bad);
+      mine = (long long)s.blocks * s.tiles * a.Hkv;
+    }
+    long long incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long up = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += up;
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, x0 < base + incl);
+    if (hit) {
+      const int src = __ffs(hit) - 1;
+      b = b0 + src;
+      base += __shfl_sync(0xffffffffu, incl - mine, src);
+      break;
+    }
+    base += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  s = get_seq(a, b, rep, ROWS, bad);
+
+  for (long long x = x0; x < x1;) {
+    while (x >= base + (long long)s.blocks * s.tiles * a.Hkv) {
+      base += (long long)s.blocks * s.tiles * a.Hkv;
+      s = get_seq(a, ++b, rep, ROWS, bad);
+    }
+    const int local = (int)((x - base) / s.blocks), blk0 = (int)((x - base) - (long long)local * s.blocks);
+    const int g = local % a.Hkv, r0 = local / a.Hkv * ROWS;
+    const int blk1 = (int)min((long long)s.blocks, blk0 + (x1 - x));
+    const long long item = x - blk0;  // the item's first block
+    x += blk1 - blk0;
+    const int R = s.nq * rep, before = s.len - s.nq;  // positions that every row sees, less its own
+    const int most = s.len == 0 ? 0 : before + min(R - 1, r0 + ROWS - 1) / rep + 1;  // positions that the tile's last row sees
+    const int least = s.len == 0 ? 0 : before + r0 / rep + 1;                       // ... and its first
+    const int u0 = blk0 * kWarps + warp, c1 = min(most, blk1 * kBlock);
+    const int nu = u0 * kUnit < c1 ? ((c1 - u0 * kUnit + kUnit - 1) / kUnit + kWarps - 1) / kWarps : 0;  // this warp's units
+
+    // pages of 32 units: lane k has unit k's
+    int ids = 0;
+    auto load_ids = [&](int k) {
+      const int p = (u0 + kWarps * (k + lane)) * kUnit;
+      int id = p < c1 ? a.tables[(size_t)b * a.max_pages + (p >> a.shift)] : 0;
+      if (id < 0 || id >= a.n_pages) {
+        id = 0;
+        atomicExch(&g_attn_paged_status, -1);
+      }
+      ids = id;
+    };
+    auto copy_unit = [&](int k, int stage) {
+      if (k % 32 == 0) load_ids(k);
+      const int id = __shfl_sync(0xffffffffu, ids, k % 32);
+      if (k < nu) {
+        const size_t row = (((size_t)id * a.Hkv + g) << a.shift) + ((u0 + kWarps * k) * kUnit & (page - 1));
+        uint8_t *st = ring + stage * L::STAGE;
+        const uint8_t *ks = reinterpret_cast<const uint8_t *>(a.kc) + row * L::ROW + lane * 16;
+        const uint8_t *vs = reinterpret_cast<const uint8_t *>(a.vc) + row * L::ROW + lane * 16;
+#pragma unroll
+        for (int i = 0; i < L::COPIES; ++i) {
+          const int p = (lane + 32 * i) / L::CHR, ch = (lane + 32 * i) % L::CHR;
+          const int place = (p & 8) + 2 * (p & 3) + (p >> 2 & 1);
+          cp_async16(st + place * L::ROW + ((ch ^ L::k_swz(place)) << 4), ks + 512 * i);
+          cp_async16(st + (kUnit + p) * L::ROW + ((ch ^ L::v_swz(p)) << 4), vs + 512 * i);
+        }
+        if constexpr (BITS != 16)
+          cp_async4(st + 2 * kUnit * L::ROW + lane * 4, (lane < 16 ? a.km : a.vm) + row + (lane & 15));
+      }
+      cp_async_commit();
+    };
+#pragma unroll 1
+    for (int k = 0; k < L::NS - 1; ++k) copy_unit(k, k);
+
+    // ---- the rows' queries: lane (gr, tc) has row gr's operands, rows 2 tc and 2 tc + 1 its scores
+    uint32_t qb[NT][L::KS][2];
+    float A[NT][2];            // x = s A acc
+    int limit[NT][2];          // positions that the rows see
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int r = r0 + 8 * n + gr;
+      const bool in = r < R;
+      const __nv_bfloat16 *qp = reinterpret_cast<const __nv_bfloat16 *>(a.q) +
+                                ((size_t)(s.q0 + (in ? r / rep : 0)) * a.H + g * rep + (in ? r % rep : 0)) * HD;
+      uint32_t big = 0;
+#pragma unroll
+      for (int ks = 0; ks < L::KS; ++ks) {
+        const uint2 v = in ? __ldg(reinterpret_cast<const uint2 *>(qp + L::q_at(ks, tc))) : make_uint2(0, 0);
+        qb[n][ks][0] = v.x, qb[n][ks][1] = v.y;
+        big = __vmaxu2(big, __vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu));
+      }
+      float qf = a.scale;
+      if constexpr (BITS != 16) {
+        // an exact power of two puts the row's largest value in [2^14, 2^15): what binary16 then
+        // loses is below 2^-38 of it
+        big = max(big & 0xffffu, big >> 16);
+        big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
+        big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
+        const int e = (int)(big >> 7) - 127;
+        const int sh = e == 128 || big == 0 ? 0 : min(126, max(-100, 14 - e));
+        const float f = __uint_as_float((uint32_t)(127 + sh) << 23);
+        qf = a.scale * __uint_as_float((uint32_t)(127 - sh) << 23);
+#pragma unroll
+        for (int ks = 0; ks < L::KS; ++ks)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) qb[n][ks][i] = pack_h2(bf_lo(qb[n][ks][i]) * f, bf_hi(qb[n][ks][i]) * f);
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int rr = r0 + 8 * n + 2 * tc + e;
+        A[n][e] = __shfl_sync(0xffffffffu, qf, 8 * tc + 4 * e);
+        limit[n][e] = rr < R && s.len > 0 ? before + rr / rep + 1 : 0;
+      }
+    }
+
+    float o[NT][L::NJ / 2][4], m[NT][2], l[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int j = 0; j < L::NJ / 2; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[n][j][e] = 0.f;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) m[n][e] = -INFINITY, l[n][e] = 0.f;
+    }
+
+    int stage = 0, into = L::NS - 1;
+    for (int k = 0; k < nu; ++k) {
+      cp_async_wait<L::NS - 2>();
+      __syncwarp();
+      // (every lane has read what this stage held, the one before)
+      copy_unit(k + L::NS - 1, into);
+      into = into + 1 == L::NS ? 0 : into + 1;
+      const uint8_t *st = ring + stage * L::STAGE, *sv = st + kUnit * L::ROW;
+      stage = stage + 1 == L::NS ? 0 : stage + 1;
+      const int p0 = (u0 + kWarps * k) * kUnit;
+      const int pa = (gr >> 1) + 4 * (gr & 1);  // the lane's positions of the scores: pa and pa + 8
+
+      const uint32_t *meta = reinterpret_cast<const uint32_t *>(sv + kUnit * L::ROW);
+      float y[NT][4], y2[NT][4], sk[2];
+      {
+        uint32_t ka[L::KI * L::KW], kb[L::KI * L::KW];
+#pragma unroll
+        for (int i = 0; i < L::KI; ++i) {
+          const int off = L::ROW >= 64 ? (((tc + 4 * i) ^ L::k_swz(gr)) << 4) : tc * 4 * L::KW;
+          load_words(*reinterpret_cast<uint32_t(*)[L::KW]>(&ka[L::KW * i]), st + gr * L::ROW + off);
+          load_words(*reinterpret_cast<uint32_t(*)[L::KW]>(&kb[L::KW * i]), st + (gr + 8) * L::ROW + off);
+        }
+        uint32_t za = 0, zb = 0;
+        if constexpr (BITS != 16) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const __half2 mk = *reinterpret_cast<const __half2 *>(meta + pa + 8 * i);
+            sk[i] = __low2float(mk);
+            const __half2 z = __hadd2(__high2half2(mk), __float2half2_rn(1024.f));
+            (i ? zb : za) = *reinterpret_cast<const uint32_t *>(&z);
+          }
+        }
+        const uint32_t za6 = hsub2_u(za, 0x63806380u), zb6 = hsub2_u(zb, 0x63806380u);  // less 960: 64 + z, exact
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[n][e] = y2[n][e] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < L::KS; ++ks) {
+          uint32_t f[4];
+          k_frag<HD, BITS>(ka, ks, za, za6, f[0], f[2]);
+          k_frag<HD, BITS>(kb, ks, zb, zb6, f[1], f[3]);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            if constexpr (BITS == 16)
+              mma_bf16_16816(ks % 2 ? y2[n] : y[n], f, qb[n][ks][0], qb[n][ks][1]);
+            else
+              mma_f16_16816(ks % 2 ? y2[n] : y[n], f, qb[n][ks][0], qb[n][ks][1]);
+          }
+        }
+      }
+      // places that some row does not see: behind the last position they may hold anything
+      const bool some = p0 + kUnit > least;
+      float rs[2] = {1.f, 1.f};
+      uint32_t zv[2] = {0, 0};  // 1024 + z of rows tc and tc + 4, tc + 8 and tc + 12
+      if constexpr (BITS == 16) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[n][e] = (y[n][e] + y2[n][e]) * A[n][e % 2];
+      } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          uint32_t mv = meta[16 + pa + 8 * i];
+          // rows of zeros, those of a zero-filled cache too: code - z is 0, and the least scale does as well
+          if ((mv & 0xffffu) == 0 || mv == kZeroRow) mv = 1u;
+          const float s = __half2float(__ushort_as_half((unsigned short)(mv & 0xffffu)));
+          const float lg = lg2(s);
+          rs[i] = rcp(s);
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              y[n][2 * i + e] = fmaf((y[n][2 * i + e] + y2[n][2 * i + e]) * A[n][e], sk[i], lg);
+          uint32_t z = __byte_perm(meta[16 + tc + 8 * i], meta[20 + tc + 8 * i], 0x7632);
+          if (some) z &= (p0 + tc + 8 * i < most ? 0xffffu : 0u) | (p0 + tc + 4 + 8 * i < most ? 0xffff0000u : 0u);
+          const __half2 zz = __hadd2(*reinterpret_cast<const __half2 *>(&z), __float2half2_rn(1024.f));
+          zv[i] = *reinterpret_cast<const uint32_t *>(&zz);
+        }
+      }
+      uint32_t vw[4][L::VI * L::VW];
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+#pragma unroll
+        for (int i = 0; i < L::VI; ++i) {
+          const int off = L::ROW >= 128 ? (((gr + 8 * i) ^ L::v_swz(tc)) << 4)
+                                        : (((gr * 4 * L::VW >> 4) ^ L::v_swz(tc)) << 4) + (gr * 4 * L::VW & 15);
+          load_words(*reinterpret_cast<uint32_t(*)[L::VW]>(&vw[v][L::VW * i]), sv + (tc + 4 * v) * L::ROW + off);
+        }
+      bool odd = false;
+      if (some) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int p = p0 + pa + 8 * i;
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              if (p >= limit[n][e]) y[n][2 * i + e] = -INFINITY;
+        }
+        if constexpr (BITS == 16)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const bool behind = p0 + tc + 4 * v >= most;
+#pragma unroll
+            for (int i = 0; i < L::VI * L::VW; ++i) {
+              uint32_t &w = vw[v][i];
+              if (behind) w = 0;
+              // values that are not finite are taken out, and added to the rows that see them
+              if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u, odd = true;
+              if ((w & 0x7f800000u) == 0x7f800000u) w &= 0xffffu, odd = true;
+            }
+          }
+      }
+      // ---- softmax: the maximum is raised when a score passes it by 2^8 (p stays below that times 2^kLift)
+      constexpr float kLift = BITS == 16 ? 0.f : 6.f;
+      bool up = false;
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) up |= fmaxf(y[n][e], y[n][2 + e]) > m[n][e] + 8.f;
+      if (__any_sync(0xffffffffu, up)) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          float al[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float t = fmaxf(y[n][e], y[n][2 + e]);
+#pragma unroll
+            for (int d = 4; d <= 16; d <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
+            t = fmaxf(t, m[n][e]);
+            al[e] = t == -INFINITY ? 1.f : ex2(m[n][e] - t);
+            m[n][e] = t;
+            l[n][e] *= al[e];
+          }
+#pragma unroll
+          for (int j = 0; j < L::NJ / 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[n][j][e] *= al[e % 2];
+        }
+      }
+      uint32_t pb[NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float p[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) p[e] = ex2(y[n][2 * i + e] - (m[n][e] == -INFINITY ? 0.f : m[n][e] - kLift));
+          const uint32_t w = BITS == 16 ? pack_bf2(p[0], p[1]) : pack_h2(p[0], p[1]);
+          if constexpr (BITS != 16) {
+            // (a masked row's scale may be NaN)
+            l[n][0] = some && p[0] == 0.f ? l[n][0] : fmaf(p[0], rs[i], l[n][0]);
+            l[n][1] = some && p[1] == 0.f ? l[n][1] : fmaf(p[1], rs[i], l[n][1]);
+          } else {
+            l[n][0] += p[0];
+            l[n][1] += p[1];
+          }
+          pb[n][i] = transpose8(w);
+        }
+      const uint32_t z6[2] = {hsub2_u(zv[0], 0x63806380u), hsub2_u(zv[1], 0x63806380u)};
+#pragma unroll
+      for (int j = 0; j < L::NJ / 2; ++j) {
+        uint32_t f[4];
+        f[0] = v_frag<HD, BITS>(vw[0], vw[1], 2 * j, zv[0], z6[0]);
+        f[1] = v_frag<HD, BITS>(vw[0], vw[1], 2 * j + 1, zv[0], z6[0]);
+        f[2] = v_frag<HD, BITS>(vw[2], vw[3], 2 * j, zv[1], z6[1]);
+        f[3] = v_frag<HD, BITS>(vw[2], vw[3], 2 * j + 1, zv[1], z6[1]);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          if constexpr (BITS == 16)
+            mma_bf16_16816(o[n][j], f, pb[n][0], pb[n][1]);
+          else
+            mma_f16_16816(o[n][j], f, pb[n][0], pb[n][1]);
+        }
+      }
+      if (BITS == 16 && __any_sync(0xffffffffu, odd)) {
+        for (int p = 0; p < kUnit && p0 + p < most; ++p)
+#pragma unroll
+          for (int j = 0; j < L::NJ; ++j) {
+            const int at = L::v_at(j, gr) * 2;
+            const float f = __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(
+                sv + p * L::ROW + (((at >> 4) ^ L::v_swz(p)) << 4) + (at & 15)));
+            if (isfinite(f)) continue;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int e = 0; e < 2; ++e)
+                if (p0 + p < limit[n][e]) o[n][j / 2][2 * (j % 2) + e] += f;
+          }
+      }
+    }
+    cp_async_wait_all();
+    __syncthreads();  // the rings are read to their end
+
+    // ---- the warps' results, over the rings
+    float(*so)[ROWS][OS] = reinterpret_cast<float(*)[ROWS][OS]>(paged_ring);
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+#pragma unroll
+        for (int d = 4; d <= 16; d <<= 1) l[n][e] += __shfl_xor_sync(0xffffffffu, l[n][e], d);
+        const int r = 8 * n + 2 * tc + e;
+        if (gr == 0) {
+          sm[warp][r] = m[n][e];
+          sl[warp][r] = l[n][e];
+        }
+#pragma unroll
+        for (int j = 0; j < L::NJ; ++j) so[warp][r][L::v_at(j, gr)] = o[n][j / 2][2 * (j % 2) + e];
+      }
+    __syncthreads();
+    const bool whole = blk0 == 0 && blk1 == s.blocks;
+    // the CTAs that share the item: c0 has its begin (in its place 1), the others their first blocks (0)
+    const long long c0 = ((item + 1) * N - 1) / total, cl = ((item + s.blocks) * N - 1) / total;
+    for (int i = tid; i < ROWS * HD / 2; i += kWarps * 32) {
+      const int r = i / (HD / 2), e = 2 * (i % (HD / 2)), row = r0 + r;
+      if (row >= R) break;
+      float M = -INFINITY, Ls = 0.f, O0 = 0.f, O1 = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) M = fmaxf(M, sm[w][r]);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float f = sm[w][r] == -INFINITY ? 0.f : ex2(sm[w][r] - M);
+        Ls = fmaf(sl[w][r], f, Ls);
+        O0 = fmaf(so[w][r][e], f, O0);
+        O1 = fmaf(so[w][r][e + 1], f, O1);
+      }
+      if (whole) {
+        const bool none = M == -INFINITY && Ls == 0.f;
+        *reinterpret_cast<uint32_t *>(reinterpret_cast<__nv_bfloat16 *>(a.o) +
+                                      ((size_t)(s.q0 + row / rep) * a.H + g * rep + row % rep) * HD + e) =
+            none ? 0u : pack_bf2(O0 / Ls, O1 / Ls);
+      } else {
+        float *pt = a.part + (((size_t)c * 2 + (blk0 == 0)) * kMostRows + r) * (HD + 2);
+        *reinterpret_cast<float2 *>(pt + e) = make_float2(O0, O1);
+        if (e == 0) *reinterpret_cast<float2 *>(pt + HD) = make_float2(M, Ls);
+      }
+    }
+    if (!whole) {
+      __threadfence();
+      __syncthreads();
+      if (tid == 0) {
+        const int all = (int)(cl - c0 + 1);
+        last = atomicAdd(&a.counters[c0], 1) == all - 1;
+        if (last) a.counters[c0] = 0;
+      }
+      __syncthreads();
+      if (last) {
+        __threadfence();
+        for (int i = tid; i < ROWS * HD / 2; i += kWarps * 32) {
+          const int r = i / (HD / 2), e = 2 * (i % (HD / 2)), row = r0 + r;
+          if (row >= R) break;
+          float M = -INFINITY, Ls = 0.f, O0 = 0.f, O1 = 0.f;
+          for (long long k = c0; k <= cl; ++k) {
+            const float *pt = a.part + (((size_t)k * 2 + (k == c0)) * kMostRows + r) * (HD + 2);
+            const float2 ov = __ldcg(reinterpret_cast<const float2 *>(pt + e)), ml = __ldcg(reinterpret_cast<const float2 *>(pt + HD));
+            const float mn = fmaxf(M, ml.x);
+            const float f0 = M == -INFINITY ? 0.f : ex2(M - mn), f1 = ml.x == -INFINITY ? 0.f : ex2(ml.x - mn);
+            M = mn;
+            Ls = fmaf(ml.y, f1, Ls * f0);
+            O0 = fmaf(ov.x, f1, O0 * f0);
+            O1 = fmaf(ov.y, f1, O1 * f0);
+          }
+          const bool none = M == -INFINITY && Ls == 0.f;
+          *reinterpret_cast<uint32_t *>(reinterpret_cast<__nv_bfloat16 *>(a.o) +
+                                        ((size_t)(s.q0 + row / rep) * a.H + g * rep + row % rep) * HD + e) =
+              none ? 0u : pack_bf2(O0 / Ls, O1 / Ls);
+        }
+      }
+    }
+    __syncthreads();  // the rings take the next item's positions
+  }
+}
+
+int attn_paged_ctas(int num_sms) { return kCtasPerSm * num_sms; }
+
+size_t attn_paged_part_floats(int hd, int num_sms) {
+  return (size_t)attn_paged_ctas(num_sms) * 2 * kMostRows * (hd + 2);
+}
+
+namespace {
+
+template <int HD, int BITS, int NT>
+cudaError_t launch_t(const AttnPagedArgs &a, int num_sms, cudaStream_t s) {
+  using L = Lay<HD, BITS>;
+  constexpr int out = kWarps * 8 * NT * (HD + 4) * 4, smem = L::RING > out ? L::RING : out;
+  static std::atomic<bool> done[64];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  auto k = attn_paged_kernel<HD, BITS, NT>;
+  if (dev < 0 || dev >= 64 || !done[dev].load(std::memory_order_acquire)) {
+    if ((e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64) done[dev].store(true, std::memory_order_release);
+  }
+  // as many CTAs as the SMs hold at once, and no more than blocks there can be
+  const long long tiles = ((long long)a.m * (a.H / a.Hkv) + 8 * NT - 1) / (8 * NT) + a.batch;
+  const long long blocks = (((long long)a.max_pages << a.shift) + kBlock - 1) / kBlock;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  cfg.gridDim = dim3((unsigned)std::min((long long)occupancy(HD, BITS, NT) * num_sms, std::min(tiles, (long long)1 << 30) * blocks * a.Hkv));
+  cfg.blockDim = dim3(kWarps * 32);
+  cfg.dynamicSmemBytes = smem;
+  return cudaLaunchKernelEx(&cfg, k, a);
+}
+
+}  // namespace
+
+cudaError_t launch_attn_paged(const AttnPagedArgs &a, int hd, int bits, int num_sms, cudaStream_t s) {
+  const bool one = (long long)a.max_q * (a.H / a.Hkv) <= 8;
+#define WQ_PAGED(HD, BITS) \
+  if (hd == HD && bits == BITS) return one ? launch_t<HD, BITS, 1>(a, num_sms, s) : launch_t<HD, BITS, 2>(a, num_sms, s);
+  WQ_PAGED(128, 16) WQ_PAGED(128, 8) WQ_PAGED(128, 4) WQ_PAGED(64, 16) WQ_PAGED(64, 8) WQ_PAGED(64, 4)
+#undef WQ_PAGED
+  return cudaErrorInvalidValue;
+}
+
+cudaError_t read_attn_paged_status(int *status) {
+  cudaError_t e = cudaDeviceSynchronize();
+  if (e != cudaSuccess) return e;
+  e = cudaMemcpyFromSymbol(status, g_attn_paged_status, sizeof(int));
+  if (e != cudaSuccess) return e;
+  const int zero = 0;
+  return cudaMemcpyToSymbol(g_attn_paged_status, &zero, sizeof(int));
+}
+
+}  // namespace wq

@@ -110,6 +110,14 @@ def lib():
             "wq_decoder_tree_workspace_bytes": (S, [I, I, ctypes.POINTER(_DecoderLayer), I]),
             "wq_decoder_tree_forward": (I, [P, I, P, P, ctypes.POINTER(_DecoderLayer), CP, P, I, P, P, U, P, P, P, P,
                                             S, P]),
+            "wq_page_plan": (I, [P, P, P, I, I, P, I, P, I, P, P, I, P, P, P, P, P]),
+            "wq_qkv_paged": (I, [P, I, P, I, I, P, P, I, P, P, I, U, CP, P, P, P]),
+            "wq_paged_read": (I, [CP, P, I, P, P, I, P]),
+            "wq_attn_paged_workspace_bytes": (S, [I, I, I, I, I]),
+            "wq_attn_paged": (I, [P, I, I, I, CP, I, P, P, P, I, F, P, P, S, P]),
+            "wq_decoder_paged_workspace_bytes": (S, [I, I, ctypes.POINTER(_DecoderLayer)]),
+            "wq_decoder_paged_forward": (I, [P, I, I, I, P, P, P, P, ctypes.POINTER(_DecoderLayer), P, P, CP, P, I, P, I, U,
+                                             P, P, S, P]),
             "wq_moe_workspace_bytes": (S, [I, ctypes.POINTER(_MoELayer), U]),
             "wq_moe_forward": (I, [P, I, P, ctypes.POINTER(_MoELayer), U, P, P, P, P, P, P, S, P]),
             "wq_wait_check": (I, [P]),
@@ -705,6 +713,123 @@ def decoder_tree_forward(x, lens, positions, layer: DecoderLayer, cache: KVCache
         _at(k_new, bf, kv, "k_new"), _at(v_new, bf, kv, "v_new"), _at(y, bf, (b, t, d), "y"), ws.data_ptr(), ws.numel(),
         _raw_stream()))
     return y, k_new, v_new
+
+
+def kv_pool(n_pages: int, n_kv: int, page: int, head_dim: int, bits: int = 16, device="cuda") -> KVCache:
+    """An empty (zero) pool of pages of ``page`` positions (16, 32, 64, 128 or 256): a cache whose batch is the pages."""
+    return kv_cache(n_pages, n_kv, page, head_dim, bits, device)
+
+
+def page_plan(lens, n_new, tables, free_pages, n_free, page: int, m: int, keep=None, n_free_out=None, cu=None, kv_lens=None,
+              positions=None, slots=None):
+    """wq_page_plan: (cu [batch + 1], kv_lens [batch], positions [m], slots [m]) of one step of requests that hold lens,
+    keep ``keep`` of it (None: all) and add n_new tokens.  tables [batch, max_pages] and the stack free_pages [n_pages] of
+    n_free [1] pages are changed in place, the pages left go to n_free_out (None: n_free); all int32 on the device.
+    kv_lens may be lens."""
+    i32, dev, b = torch.int32, lens.device, lens.shape[0]
+    cu, cup = _out(cu, i32, (b + 1,), dev, "cu")
+    kv_lens, lp = _out(kv_lens, i32, (b,), dev, "kv_lens")
+    positions, pp = _out(positions, i32, (m,), dev, "positions")
+    slots, sp = _out(slots, i32, (m,), dev, "slots")
+    max_pages, n_pages = tables.shape[1], free_pages.shape[0]
+    _check(lib().wq_page_plan(_at(lens, i32, (b,), "lens"), _at(keep, i32, (b,), "keep"), _at(n_new, i32, (b,), "n_new"), b,
+                              page, _at(tables, i32, (b, max_pages), "tables"), max_pages,
+                              _at(free_pages, i32, (n_pages,), "free_pages"), n_pages, _at(n_free, i32, (1,), "n_free"),
+                              _at(n_free if n_free_out is None else n_free_out, i32, (1,), "n_free_out"), m, cup, lp, pp, sp,
+                              _raw_stream()))
+    return cu, kv_lens, positions, slots
+
+
+def qkv_paged(qkv, slots, pool: KVCache, n_heads: int, positions=None, table=None, x=None, q_norm=None, k_norm=None,
+              head_norm: bool = True, q=None):
+    """wq_qkv_paged: bf16 q [m, n_heads, hd] from projections [m, (n_heads + 2 n_kv) hd] (bf16 or fp32), whose K and V are
+    normed, rotated (``positions`` and ``table``; None: not) and written to the pool's slots."""
+    m, hd, dt = qkv.shape[0], pool.head_dim, qkv.dtype
+    assert dt is torch.bfloat16 or dt is torch.float32
+    bf, i32 = torch.bfloat16, torch.int32
+    q, qp = _out(q, bf, (m, n_heads, hd), qkv.device, "q")
+    d = 0 if x is None else x.shape[1]
+    n_pos = 0 if table is None else table.shape[0]
+    _check(lib().wq_qkv_paged(_at(qkv, dt, (m, (n_heads + 2 * pool.n_kv) * hd), "qkv"), 1 if dt is torch.float32 else 0,
+                              _at(x, bf, (m, d), "x"), m, d, _at(positions, i32, (m,), "positions"),
+                              _at(table, torch.float32, (n_pos, hd // 2, 2), "table"), n_pos, _at(q_norm, bf, (hd,), "q_norm"),
+                              _at(k_norm, bf, (hd,), "k_norm"), n_heads, WQ_HEAD_NORM if head_norm else 0, pool._ref,
+                              _at(slots, i32, (m,), "slots"), qp, _raw_stream()))
+    return q
+
+
+def paged_read(pool: KVCache, slots, dtype=torch.bfloat16, k=None, v=None):
+    """wq_paged_read: (k, v) [m, n_kv, head_dim] of the pool's rows at ``slots`` (int32 [m]; -1: zeros) in bf16 or fp32."""
+    assert dtype is torch.bfloat16 or dtype is torch.float32
+    m = slots.shape[0]
+    shape = (m, pool.n_kv, pool.head_dim)
+    k, kp = _out(k, dtype, shape, slots.device, "k")
+    v, vp = _out(v, dtype, shape, slots.device, "v")
+    _check(lib().wq_paged_read(pool._ref, _at(slots, torch.int32, (m,), "slots"), m, kp, vp, 1 if dtype is torch.float32 else 0,
+                               _raw_stream()))
+    return k, v
+
+
+def attn_paged_workspace(batch: int, m: int, n_heads: int, n_kv: int, head_dim: int, device="cuda") -> torch.Tensor:
+    """A zero-initialised workspace of attn_paged for up to ``batch`` sequences and m rows."""
+    nb = int(lib().wq_attn_paged_workspace_bytes(batch, m, n_heads, n_kv, head_dim))
+    if nb == 0:
+        raise WQError(-2, "no attention workspace for these sizes")
+    ws = torch.empty(nb, dtype=torch.uint8, device=device)
+    _check(lib().wq_workspace_init(_ptr(ws), nb, _stream()))
+    return ws
+
+
+def attn_paged(q, cu, kv_lens, tables, pool: KVCache, max_q: int | None = None, scale: float | None = None, o=None, ws=None):
+    """wq_attn_paged: causal attention of q [m, n_heads, hd], rows cu[b] .. cu[b + 1] - 1 of sequence b being its last
+    positions, over kv_lens[b] positions in the pages that tables [batch, max_pages] names.  max_q: the most rows of a
+    sequence (None: m)."""
+    m, h, hd = q.shape
+    b, max_pages = tables.shape
+    bf, i32 = torch.bfloat16, torch.int32
+    if o is None:
+        o = torch.empty((m, h, hd), dtype=bf, device=q.device)
+    if ws is None:
+        ws = attn_paged_workspace(max(b, 1), max(m, 1), h, pool.n_kv, hd, device=q.device)
+    assert ws.is_cuda and hd == pool.head_dim
+    _check(lib().wq_attn_paged(_at(q, bf, (m, h, hd), "q"), m, m if max_q is None else max_q, h, pool._ref, b,
+                               _at(cu, i32, (b + 1,), "cu"), _at(kv_lens, i32, (b,), "kv_lens"),
+                               _at(tables, i32, (b, max_pages), "tables"), max_pages, hd ** -0.5 if scale is None else scale,
+                               _at(o, bf, (m, h, hd), "o"), ws.data_ptr(), ws.numel(), _raw_stream()))
+    return o
+
+
+def decoder_paged_workspace(batch: int, m: int, layer: DecoderLayer, device="cuda") -> torch.Tensor:
+    cl = layer.c()
+    nb = int(lib().wq_decoder_paged_workspace_bytes(batch, m, ctypes.byref(cl)))
+    if nb == 0:
+        raise WQError(-2, "no decoder workspace for these sizes")
+    ws = torch.empty(nb, dtype=torch.uint8, device=device)
+    _check(lib().wq_workspace_init(_ptr(ws), nb, _stream()))
+    return ws
+
+
+def decoder_paged_forward(x, cu, kv_lens, positions, slots, layer: DecoderLayer, pool: KVCache, tables, table,
+                          max_q: int | None = None, q_norm=None, k_norm=None, prenorm: bool = True, y=None, ws=None, c_layer=None):
+    """wq_decoder_paged_forward: one step of the layer for x bf16 [m, d], the rows of a ragged batch as page_plan lays
+    them out; the layer's K and V go to the pool's slots."""
+    m, d = x.shape
+    b, max_pages = tables.shape
+    bf, i32, n_pos, hd = torch.bfloat16, torch.int32, table.shape[0], pool.head_dim
+    if y is None:
+        y = torch.empty_like(x)
+    if ws is None:
+        ws = decoder_paged_workspace(max(b, 1), max(m, 1), layer, device=x.device)
+    cl = c_layer if c_layer is not None else layer.c()
+    assert ws.is_cuda
+    _check(lib().wq_decoder_paged_forward(_at(x, bf, (m, d), "x"), m, m if max_q is None else max_q, b, _at(cu, i32, (b + 1,), "cu"),
+                                          _at(kv_lens, i32, (b,), "kv_lens"), _at(positions, i32, (m,), "positions"),
+                                          _at(slots, i32, (m,), "slots"), ctypes.byref(cl), _at(q_norm, bf, (hd,), "q_norm"),
+                                          _at(k_norm, bf, (hd,), "k_norm"), pool._ref, _at(tables, i32, (b, max_pages), "tables"),
+                                          max_pages, _at(table, torch.float32, (n_pos, hd // 2, 2), "table"), n_pos,
+                                          WQ_PRENORM if prenorm else 0, _at(y, bf, (m, d), "y"), ws.data_ptr(), ws.numel(),
+                                          _raw_stream()))
+    return y
 
 
 @dataclass
