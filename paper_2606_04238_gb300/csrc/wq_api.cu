@@ -1739,7 +1739,9 @@ wq_status check_group(int n_heads, int n_kv) {
 
 // The arrival counters, at the workspace's start, and the partial results behind them.
 size_t paged_counter_bytes(int sms) { return up256(sizeof(int) * (size_t)attn_paged_ctas(sms)); }
-size_t paged_part_bytes(int hd, int sms) { return up256(4 * attn_paged_part_floats(hd, sms)); }
+size_t paged_part_bytes(int hd, int sms) {
+  return up256(4 * std::max(attn_paged_part_floats(hd, sms), attn_paged_tc_part_floats(hd, sms)));
+}
 
 wq_status attn_paged_impl(const void *q, int m, int max_q, int n_heads, const wq_kv_cache *pool, int batch, const int32_t *cu,
                           const int32_t *kv_lens, const int32_t *tables, int max_pages, float scale, void *o, void *counters,
@@ -1763,7 +1765,8 @@ wq_status attn_paged_impl(const void *q, int m, int max_q, int n_heads, const wq
   a.counters = static_cast<int *>(counters);
   a.part = static_cast<float *>(part);
   a.o = o;
-  cudaError_t e = launch_attn_paged(a, pool->head_dim, pool->bits, sms, s);
+  const bool tc = (long long)max_q * (n_heads / pool->n_kv) > 16;
+  cudaError_t e = tc ? launch_attn_paged_tc(a, pool->head_dim, pool->bits, sms, s) : launch_attn_paged(a, pool->head_dim, pool->bits, sms, s);
   if (e != cudaSuccess) return cuda_fail(e, "paged attention launch");
   return ok();
 }
@@ -2251,6 +2254,9 @@ wq_status wq_device_status(int *status) {
   if (e != cudaSuccess) return cuda_fail(e, "device status read");
   if (*status == 0) *status = g;
   e = read_attn_paged_status(&g);
+  if (e != cudaSuccess) return cuda_fail(e, "device status read");
+  if (*status == 0) *status = g;
+  e = read_attn_paged_tc_status(&g);
   if (e != cudaSuccess) return cuda_fail(e, "device status read");
   if (*status == 0) *status = g;
   return ok();

@@ -36,6 +36,7 @@
 #include "wq_kv.h"
 #include "wq_paged.h"
 #include "wq_ptx.cuh"
+#include "wq_ragged.cuh"
 
 namespace wq {
 
@@ -85,22 +86,14 @@ struct Lay : RowLay<HD, BITS> {
 // CTAs an SM holds: 128 registers a thread for 8 rows, 168 for 16; a bf16 ring of heads of 128 takes 96 KB.
 constexpr int occupancy(int hd, int bits, int nt) { return bits == 16 && hd == 128 ? 2 : nt == 1 ? kCtasPerSm : 3; }
 
-// A sequence: its first row and rows, positions; blocks of 64 positions of each of its items.
-struct Seq {
-  int q0, nq, len, blocks, tiles;  // tiles of rows
+// A sequence; the blocks of 64 positions of each of its items, and its tiles of rows.
+struct Item : Seq {
+  int blocks, tiles;
 };
-// items of no blocks where a row offset or length is out of range, or there are no rows.
-__device__ __forceinline__ Seq get_seq(const AttnPagedArgs &a, int b, int rep, int rows, bool &bad) {
-  Seq s;
-  s.q0 = a.cu[b];
-  const int q1 = a.cu[b + 1];
-  s.len = a.kv_lens[b];
-  s.nq = q1 - s.q0;
-  const bool none = s.len == -1;  // not served: rows of zeros
-  const bool ok = s.q0 >= 0 && q1 >= s.q0 && q1 <= a.m && s.nq <= a.max_q && (none || (s.len >= s.nq && s.len <= a.max_pages << a.shift));
-  bad |= !ok;
-  if (none) s.len = 0;
-  s.tiles = ok ? (s.nq * rep + rows - 1) / rows : 0;
+__device__ __forceinline__ Item get_item(const AttnPagedArgs &a, int b, int rep, int rows, bool &bad) {
+  Item s;
+  static_cast<Seq &>(s) = get_seq(a, b, bad);
+  s.tiles = (s.nq * rep + rows - 1) / rows;
   s.blocks = max(1, (s.len + kBlock - 1) / kBlock);
   return s;
 }
@@ -124,7 +117,7 @@ __global__ void __launch_bounds__(kWarps * 32, occupancy(HD, BITS, NT)) attn_pag
   bool bad = false;
   long long total = 0;
   for (int b = lane; b < a.batch; b += 32) {
-    const Seq s = get_seq(a, b, rep, ROWS, bad);
+    const Item s = get_item(a, b, rep, ROWS, bad);
     total += (long long)s.blocks * s.tiles;
   }
 #pragma unroll
@@ -137,11 +130,11 @@ __global__ void __launch_bounds__(kWarps * 32, occupancy(HD, BITS, NT)) attn_pag
   // the sequence that x0 falls into
   int b = 0;
   long long base = 0;
-  Seq s{};
+  Item s{};
   for (int b0 = 0;; b0 += 32) {
     long long mine = 0;
     if (b0 + lane < a.batch) {
-      s = get_seq(a, b0 + lane, rep, ROWS, bad);
+      s = get_item(a, b0 + lane, rep, ROWS, bad);
       mine = (long long)s.blocks * s.tiles * a.Hkv;
     }
     long long incl = mine;
@@ -159,12 +152,12 @@ __global__ void __launch_bounds__(kWarps * 32, occupancy(HD, BITS, NT)) attn_pag
     }
     base += __shfl_sync(0xffffffffu, incl, 31);
   }
-  s = get_seq(a, b, rep, ROWS, bad);
+  s = get_item(a, b, rep, ROWS, bad);
 
   for (long long x = x0; x < x1;) {
     while (x >= base + (long long)s.blocks * s.tiles * a.Hkv) {
       base += (long long)s.blocks * s.tiles * a.Hkv;
-      s = get_seq(a, ++b, rep, ROWS, bad);
+      s = get_item(a, ++b, rep, ROWS, bad);
     }
     const int local = (int)((x - base) / s.blocks), blk0 = (int)((x - base) - (long long)local * s.blocks);
     const int g = local % a.Hkv, r0 = local / a.Hkv * ROWS;

@@ -1,0 +1,899 @@
+// wq_attn_paged_tc.cu -- causal attention of a ragged batch over a paged KV cache on the
+// tcgen05 tensor cores (sm_103a): the mathematics of wq_attn_paged.cu for sequences of more
+// query rows (tokens x query heads of a kv head), chunks of prompts above all.
+//
+// A CTA (one an SM) takes a block of 256 rows of a sequence and kv head, as two streams of
+// 128, and tiles of 128 positions:
+//   S = Q K^T   128 x 128 a stream in TMEM, Q and K in shared memory (K-major);
+//   P           binary16 (bf16 pool: bf16) over S's own columns, from the fp32 softmax of two
+//               threads a row, half the tile's positions each;
+//   O += P V    128 x HD a stream in TMEM, P as the A operand from TMEM, V [position][HD]
+//               in shared memory as it lies in a page (MN-major).
+// The MMA warp issues P V of one stream and its next S while the other's softmax runs.  Up to
+// 128 rows (a block's rest, short chunks) both streams have the same rows and take the tiles
+// in turn; their results are added up at the end.  21 warps: 0-15 softmax, 16-17 K and
+// 18-19 V (codes through registers to binary16 in the 128-byte swizzled layout; a bf16 pool by
+// cp.async; all four the queries of the next block), 20 the MMAs.
+//
+// K's operands are code - z, exact, its scales factors of the scores; V's are (code - z) s 2^-t
+// rounded to binary16, t one for a tile, or, where a tile's scales span more than 2^8, one
+// for each row, taken into its score.  The maximum is not searched in every tile: p is taken
+// with the maximum that the row has, which is raised, and O rescaled in TMEM by a power of two,
+// only where half a row's p add up to 2^15 (p is 2^6 at most where it is raised).
+//
+// The tiles of all blocks are laid end to end and every CTA takes an equal run, found from the
+// lengths themselves; blocks are paired, the first with the last and so on inward, so that
+// a causal prompt's pairs are about equally long.  What a CTA has of a block that others
+// share is left in the workspace, and the last of them to arrive adds up all parts in their order.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <atomic>
+#include <cstdint>
+#include <type_traits>
+
+#include "wq_cvt.cuh"
+#include "wq_internal.h"
+#include "wq_kv.h"
+#include "wq_paged.h"
+#include "wq_ptx.cuh"
+#include "wq_ragged.cuh"
+#include "wq_rows.cuh"
+#include "wq_tc.cuh"
+
+namespace wq {
+
+// Status word: WQ_OK (0), WQ_ERR_ARG (-1) after a row offset, length or page outside its range
+// (that sequence is skipped; such a page is read as page 0), WQ_ERR_TIMEOUT (-6) after
+// a wait ran out.
+__device__ int g_attn_paged_tc_status = 0;
+
+namespace {
+
+constexpr int kStream = 128;               // rows of a stream
+constexpr int kBlockRows = 2 * kStream;
+constexpr int kTile = 128;                 // positions a tile
+constexpr int kSoft = 512;                 // softmax threads
+constexpr int kConvWarp = kSoft / 32, kMmaWarp = kConvWarp + 4;
+constexpr int kThreads = 768;               // registers are given to whole groups of 4 warps: 3 of the last are idle
+// registers a thread: the launch's 80 x 768 shared out as 88 x 512 + 88 x 128 + 40 x 128
+constexpr int kRegsSoftmax = 88, kRegsConv = 88, kRegsMma = 40;
+constexpr int kBlk = kTile * 128;          // bytes of a 64-value block of Q, K or V: [row][128 bytes], swizzled
+constexpr int kTmemCols = 512;             // S / P of the streams 0.., 128..; O 256.., 256 + HD..
+// Queries enter binary16 times 2^7, which keeps a row with its largest |q| in [2^-4, 2^8) whole
+// but for values below 2^-27 of that; other rows by a power of two of their own.
+constexpr int kQueryShift = 7;
+constexpr int kSpread = 8;                 // exponents that V's scales of a tile may span with one power of two for all
+constexpr float kMostSum = 32768.f;        // of half a row's p in a tile; binary16 ends at 65504
+
+template <int HD, int BITS>
+struct Cfg {
+  static constexpr int NB = HD / 64;             // 64-value blocks
+  static constexpr int KB = NB * kBlk;           // bytes of one operand tile
+  static constexpr int CH = HD / 8;              // 16-byte chunks a row of 16-bit values
+  static constexpr int ROW = HD * BITS / 8;
+  static constexpr int SMEM = 1024 + 6 * KB;     // Q of both streams, two stages of K and of V
+  // codes: 16-byte pieces a row, pieces of a row in one load of a warp, rows of it; loads of a tile's 64 rows, those in flight
+  static constexpr int PPR = ROW / 16, PP = PPR < 4 ? PPR : 4, RPI = 32 / PP, NI = 64 * PPR / 32, NR = NI < 8 ? NI : 8;
+  static_assert(PPR > 0 && RPI > 0 && NI >= NR, "");
+  static constexpr float LIFT = BITS == 16 ? 0.f : 6.f;  // of p: small ones are then normal numbers
+};
+
+struct Shared {
+  uint64_t q_full, q_empty, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2];
+  uint32_t tmem;
+  int fail, sfail[2], last;
+  // of a tile, four tiles deep (a tile's are written when S of the one two before is done, whose softmax has then
+  // ended for the tile four before): K's scales times the score scale and 2^-kQueryShift, V's exponent t, whether its
+  // rows have their own, and those
+  __align__(16) float sk[4][kTile];
+  int te[4], spread[4];
+  __align__(16) float td[4][kTile], tw[4][kTile];
+  float qf[4][kBlockRows];         // what a row's own power of two differs from 2^kQueryShift
+  uint32_t odd[4][2][16];          // of a block, by either V warp: positions from its first masked tile on whose V is not finite
+  float pm[2][2][kStream], pl[2][2][kStream];  // the halves' maxima and sums
+};
+
+// A run of tiles of one block of rows.
+struct Run {
+  int b, g, q0, len, before, r0, live, t0, n;  // live: rows of the block; tiles t0 .. t0 + n - 1
+  int least;                                   // positions that its first row sees
+  int c0, cl;                                  // the first and last CTA that have tiles of the block
+  bool any, split, whole;
+};
+
+// The line of tiles: sequences in order, in a sequence pairs of blocks, the kv head fastest.  A pair has C places, as many
+// as any has tiles; those behind its two blocks are empty.  Held in shared memory, one a role.
+struct Walk {
+  long long x, x1, base, T, N, total;
+  int b, R, nb, before, C;
+  Seq s;
+
+  __device__ __forceinline__ int tiles(const Divisor &by_rep, int k, bool full) const {
+    if (s.len == 0) return 1;
+    const int r = k * kBlockRows + kBlockRows - 1;
+    return (before + (int)by_rep.divide(full ? r : min(r, R - 1)) + 1 + kTile - 1) / kTile;
+  }
+  __device__ __forceinline__ void load(const AttnPagedArgs &a, const Divisor &by_rep, int to, bool &bad) {
+    b = to;
+    s = get_seq(a, b, bad);
+    R = s.nq * (int)by_rep.d;
+    nb = (R + kBlockRows - 1) / kBlockRows;
+    before = s.len - s.nq;
+    // (tiles(k) + tiles(nb - 1 - k) is at most this: quotients and their rounding up differ by one at most)
+    C = nb == 0 ? 0 : nb == 1 ? tiles(by_rep, 0, false) : tiles(by_rep, 0, false) + tiles(by_rep, nb - 1, true) + 1;
+    total = (long long)a.Hkv * ((nb + 1) / 2) * C;
+  }
+  // One warp, all lanes alike: this CTA's part of the line.
+  __device__ __forceinline__ void start(const AttnPagedArgs &a, const Divisor &by_rep, bool &bad) {
+    const int lane = threadIdx.x & 31;
+    T = 0;
+    for (int i = lane; i < a.batch; i += 32) {
+      load(a, by_rep, i, bad);
+      T += total;
+    }
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) T += __shfl_xor_sync(0xffffffffu, T, o);
+    N = min((long long)gridDim.x, T);
+    const long long c = blockIdx.x;
+    x = x1 = base = 0;
+    if (c >= N) return;
+    x = T * c / N;
+    x1 = T * (c + 1) / N;
+    for (int b0 = 0;; b0 += 32) {
+      long long mine = 0;
+      if (b0 + lane < a.batch) {
+        load(a, by_rep, b0 + lane, bad);
+        mine = total;
+      }
+      long long incl = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long up = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += up;
+      }
+      const unsigned hit = __ballot_sync(0xffffffffu, x < base + incl);
+      if (hit) {
+        const int src = __ffs(hit) - 1;
+        base += __shfl_sync(0xffffffffu, incl - mine, src);
+        load(a, by_rep, b0 + src, bad);
+        return;
+      }
+      base += __shfl_sync(0xffffffffu, incl, 31);
+    }
+  }
+  // One thread: the next run; false at the end.
+  __device__ __forceinline__ bool next(const AttnPagedArgs &a, const Divisor &by_rep, Run &o) {
+    bool bad = false;
+    while (x < x1) {
+      while (x >= base + total) {
+        base += total;
+        load(a, by_rep, b + 1, bad);
+      }
+      const long long local = x - base, item = local / C;
+      const int y = (int)(local - item * C), p = (int)(item / a.Hkv), p2 = nb - 1 - p;
+      const int t1 = tiles(by_rep, p, false), t2 = p2 != p ? tiles(by_rep, p2, false) : 0;
+      if (y >= t1 + t2) {  // an empty place
+        x += C - y;
+        continue;
+      }
+      const int k = y < t1 ? p : p2, off = y < t1 ? y : y - t1, all = y < t1 ? t1 : t2;
+      const int n = (int)min((long long)(all - off), x1 - x);
+      o.b = b, o.g = (int)(item % a.Hkv), o.q0 = s.q0, o.len = s.len, o.before = before;
+      o.r0 = k * kBlockRows, o.live = min(kBlockRows, R - o.r0);
+      o.t0 = off, o.n = s.len == 0 ? 0 : n;
+      o.split = o.live <= kStream;
+      o.whole = n == all;
+      o.least = before + (int)by_rep.divide(o.r0) + 1;
+      o.c0 = (int)(((x - off + 1) * N - 1) / T);
+      o.cl = (int)(((x - off + all) * N - 1) / T);
+      x += n;
+      return o.any = true;
+    }
+    return o.any = false;
+  }
+};
+
+// The roles' runs and where they are in the line: four converting warps, the MMA warp, softmax (two, in turn).
+struct Roles {
+  Run run[7];
+  Walk walk[6];
+};
+
+__device__ __forceinline__ float half_lo(uint32_t m) { return __half2float(__ushort_as_half((unsigned short)(m & 0xffffu))); }
+
+}  // namespace
+
+template <int HD, int BITS>
+__global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPagedArgs a, const Divisor by_rep) {
+  using C = Cfg<HD, BITS>;
+  constexpr bool BF = BITS == 16;
+  extern __shared__ uint8_t paged_dyn[];
+  __shared__ Shared sh;
+  __shared__ Roles roles;
+  uint8_t *qbuf = paged_dyn + (1024 - (smem_addr(paged_dyn) & 1023)) % 1024, *kbuf = qbuf + 2 * C::KB, *vbuf = kbuf + 2 * C::KB;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int page = 1 << a.shift;
+  if (warp == kMmaWarp) {
+    tmem_alloc(&sh.tmem, kTmemCols);
+    if (lane == 0) {
+      mbar_init(&sh.q_full, 4);
+      mbar_init(&sh.q_empty, 1);
+      for (int i = 0; i < 2; ++i) {
+        mbar_init(&sh.k_full[i], 2);
+        mbar_init(&sh.v_full[i], 2);
+        mbar_init(&sh.k_empty[i], 1);
+        mbar_init(&sh.v_empty[i], 1);
+        mbar_init(&sh.s_full[i], 1);
+        mbar_init(&sh.p_full[i], 8);
+        mbar_init(&sh.o_full[i], 1);
+        sh.sfail[i] = 0;
+      }
+      fence_barrier_init();
+      sh.fail = 0;
+    }
+  }
+  pdl_wait();
+  pdl_launch_dependents();
+  if (warp == 0) {
+    bool bad = false;
+    Walk walk;
+    walk.start(a, by_rep, bad);
+    if (bad && blockIdx.x == 0) atomicExch(&g_attn_paged_tc_status, -1);
+    if (lane < 6) roles.walk[lane] = walk;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tm = sh.tmem;
+  const int rep = (int)by_rep.d;
+  // all lanes alike: a warp leaves its loop as one after a timeout
+  auto wait = [&](uint64_t *bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity)) != 0; };
+  // a warp's arrival, its shared-memory writes made visible to the tensor cores
+  auto hand_over = [&](uint64_t *bar) {
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar);
+  };
+
+  if (warp >= kMmaWarp) {
+    // ---- MMAs.  T: tiles so far, cs: tiles of a stream so far
+    constexpr uint32_t idqk = attn_idesc(kTile, BF, false), idpv = attn_idesc(HD, BF, true);
+    const uint64_t qd = umma_desc_kmajor_sw128(smem_addr(qbuf), 1024), kd = umma_desc_kmajor_sw128(smem_addr(kbuf), 1024);
+    const uint64_t vd = umma_desc_mnmajor_sw128(smem_addr(vbuf), kBlk);
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsMma));
+    Run &w = roles.run[4];
+    if (warp == kMmaWarp && elect_one()) {
+      bool ok = true;
+      int T = 0, seg = 0, cs[2] = {0, 0};
+      auto scores = [&](int s, int t, bool last) {  // S of stream s and tile t
+        ok = mbar_wait(&sh.k_full[(T + t) & 1], (T + t) >> 1 & 1);
+        if (!ok) return;
+        tc_fence_after();
+        const uint64_t q = qd + (uint64_t)(((w.split ? 0 : s) * C::KB) >> 4), k = kd + (uint64_t)((((T + t) & 1) * C::KB) >> 4);
+#pragma unroll
+        for (int ks = 0; ks < HD / 16; ++ks) {
+          const uint64_t off = (uint64_t)(((ks / 4) * kBlk + (ks % 4) * 32) >> 4);
+          umma_f16(tm + s * 128, q + off, k + off, idqk, ks > 0);
+        }
+        umma_commit(&sh.s_full[s]);
+        if (w.split || s == 1) umma_commit(&sh.k_empty[(T + t) & 1]);
+        if (last) umma_commit(&sh.q_empty);
+      };
+      while (ok && roles.walk[4].next(a, by_rep, w)) {
+        if (w.n == 0) continue;
+        const int step = w.split ? 2 : 1;
+        ok = mbar_wait(&sh.q_full, seg & 1);
+        for (int s = 0; s < 2 && ok; ++s) {
+          const int t = w.split ? s : 0;
+          if (t < w.n) scores(s, t, w.split ? t == w.n - 1 : s == 1 && w.n == 1);
+        }
+        for (int t = 0; t < w.n && ok; t += step)
+          for (int s = 0; s < 2 && ok; ++s) {
+            const int mine = w.split ? t + s : t;
+            if (mine >= w.n) break;
+            const int st = (T + mine) & 1;
+            ok = mbar_wait(&sh.v_full[st], (T + mine) >> 1 & 1) && mbar_wait(&sh.p_full[s], cs[s] & 1);
+            if (!ok) break;
+            ++cs[s];
+            tc_fence_after();
+            const uint64_t v = vd + (uint64_t)((st * C::KB) >> 4);
+#pragma unroll
+            for (int ks = 0; ks < kTile / 16; ++ks)
+              umma_ts(tm + 256 + s * HD, tm + s * 128 + 8 * ks, v + (uint64_t)((ks * 2048) >> 4), idpv, t > 0 || ks > 0);
+            if (w.split || s == 1) umma_commit(&sh.v_empty[st]);
+            const int nx = mine + step;
+            if (nx < w.n)
+              scores(s, nx, nx == w.n - 1 && (w.split || s == 1));
+            else
+              umma_commit(&sh.o_full[s]);
+          }
+        T += w.n;
+        ++seg;
+      }
+      if (!ok) sh.fail = 1;
+    }
+    __syncwarp();
+  } else if (warp >= kConvWarp) {
+    // ---- queries, K and V
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsConv));
+    Run &w = roles.run[warp - kConvWarp];
+    auto next = [&]() {
+      __syncwarp();  // (all lanes are done with the run before)
+      if (lane == 0) roles.walk[warp - kConvWarp].next(a, by_rep, w);
+      __syncwarp();
+      return w.any;
+    };
+    const bool is_v = warp >= kConvWarp + 2;
+    const int ct = tid - 32 * kConvWarp, half = warp & 1;  // a warp has rows 64 half .. of every tile
+    uint8_t *const buf = is_v ? vbuf : kbuf;
+    uint64_t *const full = is_v ? sh.v_full : sh.k_full, *const empty = is_v ? sh.v_empty : sh.k_empty;
+    const uint8_t *const src = reinterpret_cast<const uint8_t *>(is_v ? a.vc : a.kc);
+    const uint32_t *const meta = is_v ? a.vm : a.km;
+    const float qscale = a.scale * pow2i(-kQueryShift);  // of K's scales
+    bool ok = true;
+    int T = 0, seg = 0;
+    while (ok && next()) {
+      if (w.n == 0) continue;
+      const int least = w.least, first_odd = least / kTile * kTile;  // positions from `least` on are not seen by all rows
+      // pages of tile ti: lane l < 8 has that of positions 16 l ..
+      auto load_ids = [&](int ti) {
+        int id = 0;
+        if (lane < 8 && ti < w.n) {
+          id = a.tables[(size_t)w.b * a.max_pages + (min((w.t0 + ti) * kTile + 16 * lane, w.len - 1) >> a.shift)];
+          if (id < 0 || id >= a.n_pages) {
+            id = 0;
+            atomicExch(&g_attn_paged_tc_status, -1);
+          }
+        }
+        return id;
+      };
+      // the pool's row of place r of tile ti
+      auto row_at = [&](int ids, int ti, int r) {
+        const int p0 = (w.t0 + ti) * kTile, p = min(p0 + r, w.len - 1);
+        const int id = __shfl_sync(0xffffffffu, ids, (p - p0) >> 4);
+        return (((size_t)id * a.Hkv + w.g) << a.shift) + (p & (page - 1));
+      };
+      int ids = load_ids(0), ids_next = load_ids(1);
+      if (is_v && lane < 16) sh.odd[seg & 3][half][lane] = 0;
+
+      // the block's queries
+      if (seg > 0) ok = wait(&sh.q_empty, (seg - 1) & 1);
+      if (!ok) break;
+      {
+        const int c = ct % C::CH;
+        const __nv_bfloat16 *q0 = reinterpret_cast<const __nv_bfloat16 *>(a.q) + ((size_t)w.q0 * a.H + w.g * rep) * HD + c * 8;
+#pragma unroll 2
+        for (int r = ct / C::CH; r < (w.live + 31) / 32 * 32; r += 128 / C::CH) {
+          const int row = w.r0 + min(r, w.live - 1), tok = (int)by_rep.divide(row);
+          const uint4 v = __ldg(reinterpret_cast<const uint4 *>(q0 + ((size_t)tok * a.H + row - tok * rep) * HD));
+          uint4 *dst = reinterpret_cast<uint4 *>(qbuf + (r / kStream) * C::KB + (c / 8) * kBlk + r % kStream * 128 + (((c & 7) ^ (r & 7)) << 4));
+          if constexpr (BF) {
+            *dst = v;
+          } else {
+            uint32_t big = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+            big = max(big & 0xffffu, big >> 16);  // the row's largest |q|, as bf16 bits
+#pragma unroll
+            for (int o = C::CH / 2; o >= 1; o >>= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, o));
+            const int e = (int)(big >> 7) - 127;
+            int mine = kQueryShift;
+            if (big != 0 && (e < -4 || e >= 8)) mine = max(min(min(126, 14 - e), kQueryShift + 126), -114);
+            const float f = pow2i(mine);
+            if (c == 0) sh.qf[seg & 3][r] = pow2i(kQueryShift - mine);
+            *dst = make_uint4(pack_h2(bf_lo(v.x) * f, bf_hi(v.x) * f), pack_h2(bf_lo(v.y) * f, bf_hi(v.y) * f),
+                              pack_h2(bf_lo(v.z) * f, bf_hi(v.z) * f), pack_h2(bf_lo(v.w) * f, bf_hi(v.w) * f));
+          }
+        }
+      }
+      hand_over(&sh.q_full);
+
+      if constexpr (BF) {
+        const int lt = ct & 63, c = lt % C::CH, r0 = lt / C::CH;  // 64 threads a tile
+        auto copy = [&](int ti, int st, int id) {
+          const int p0 = (w.t0 + ti) * kTile;
+#pragma unroll 4
+          for (int r = r0; r < kTile; r += 64 / C::CH) {
+            const size_t at = row_at(id, ti, r);
+            cp_async16_zfill(buf + st * C::KB + (c / 8) * kBlk + r * 128 + (((c & 7) ^ (r & 7)) << 4), src + at * C::ROW + c * 16,
+                             p0 + r < w.len ? 16u : 0u);
+          }
+          cp_async_commit();
+        };
+        auto landed = [&](int ti) {  // this thread's copies of tile ti have landed
+          const int st = (T + ti) & 1, p0 = (w.t0 + ti) * kTile;
+          if (is_v && p0 + kTile > least) {
+            // V's values that are not finite are taken out and noted: what does not see them must not meet them
+            for (int r = r0; r < kTile; r += 64 / C::CH) {
+              uint4 *p = reinterpret_cast<uint4 *>(buf + st * C::KB + (c / 8) * kBlk + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+              const uint4 v = *p;
+              uint32_t x[4] = {v.x, v.y, v.z, v.w};
+              bool odd = false;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                if ((x[e] & 0x7f80u) == 0x7f80u) x[e] &= 0xffff0000u, odd = true;
+                if ((x[e] & 0x7f800000u) == 0x7f800000u) x[e] &= 0xffffu, odd = true;
+              }
+              if (odd) {
+                *p = make_uint4(x[0], x[1], x[2], x[3]);
+                const int at = p0 + r - first_odd;
+                atomicOr(&sh.odd[seg & 3][half][at / 32], 1u << (at % 32));
+              }
+            }
+          }
+          hand_over(&full[st]);
+        };
+        for (int ti = 0; ti < w.n; ++ti) {
+          const int st = (T + ti) & 1;
+          if (T + ti >= 2) ok = wait(&empty[st], ((T + ti) >> 1) + 1 & 1);
+          if (!ok) break;
+          copy(ti, st, ids);
+          ids = ids_next;
+          ids_next = load_ids(ti + 2);
+          if (ti > 0) {
+            cp_async_wait_group1();
+            landed(ti - 1);
+          }
+        }
+        cp_async_wait_all();
+        if (ok) landed(w.n - 1);
+      } else {
+        const int lr = lane % 8 + 8 * (lane / 8 / C::PP), lp = lane / 8 % C::PP;  // a lane's row and piece of a load
+        uint4 r[C::NR];
+        size_t at[C::RPI == 8 ? 8 : 4];  // pool rows of a lane's places 64 half + RPI j + lr
+        uint32_t own[2], vm4[4];
+        auto place = [&](int k) { return 64 * half + C::RPI * (k / (C::PPR / C::PP)) + lr; };
+        auto fetch_rows = [&](int ti, int id) {
+#pragma unroll
+          for (int j = 0; j < 64 / C::RPI; ++j) at[j] = row_at(id, ti, 64 * half + C::RPI * j + lr);
+        };
+        auto fetch = [&](int k) {
+          return __ldg(reinterpret_cast<const uint4 *>(src + at[k / (C::PPR / C::PP)] * C::ROW + 16 * (lp + C::PP * (k % (C::PPR / C::PP)))));
+        };
+        auto fetch_meta = [&](int ti, int id) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const size_t x = row_at(id, ti, 32 * j + lane);
+            vm4[j] = __ldg(a.vm + x);
+            if (j / 2 == half) own[j % 2] = is_v ? vm4[j] : __ldg(meta + x);
+          }
+        };
+        fetch_rows(0, ids);
+        fetch_meta(0, ids);
+#pragma unroll
+        for (int k = 0; k < C::NR; ++k) r[k] = fetch(k);
+        for (int ti = 0; ti < w.n; ++ti) {
+          const int st = (T + ti) & 1, ring = (T + ti) & 3, p0 = (w.t0 + ti) * kTile;
+          if (T + ti >= 2) ok = wait(&empty[st], ((T + ti) >> 1) + 1 & 1);
+          if (!ok) break;
+          // V's exponent: the largest scale at 2^5 .., or each row's own where they span too much (a NaN counts as the least)
+          uint32_t lo = 0x7fffu, hi = 0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            uint32_t v = (vm4[j] & 0xffffu) > 0x7c00u ? 0u : vm4[j] & 0xffffu;
+            if (v == 0 || vm4[j] == kZeroRow) v = 1;  // kLeastScale
+            if (p0 + 32 * j + lane < w.len) lo = min(lo, v), hi = max(hi, v);
+          }
+          lo = __reduce_min_sync(0xffffffffu, lo);
+          hi = __reduce_max_sync(0xffffffffu, hi);
+          auto exponent = [](uint32_t h) { return (int)(__float_as_uint(half_lo(h)) >> 23) - 127 - 5; };
+          const int te = exponent(hi);
+          const bool spread = te - exponent(lo) > kSpread;
+          uint32_t zz[2], sv[2];  // of places 64 half + 32 j + lane: 1024 + z twice; V's scale times 2^-t twice
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int pl = 64 * half + 32 * j + lane;
+            const bool in = p0 + pl < w.len;
+            const float s0 = half_lo(own[j]);
+            const __half2 z = __hadd2(__half2half2(__ushort_as_half((unsigned short)(in ? own[j] >> 16 : 0u))), __float2half2_rn(1024.f));
+            zz[j] = *reinterpret_cast<const uint32_t *>(&z);
+            sv[j] = 0;
+            if (!is_v) {
+              sh.sk[ring][pl] = s0 * qscale;
+              if (spread) {
+                // (K's warps know V's scales of their rows too)
+                const uint32_t vmj = half ? vm4[2 + j] : vm4[j];
+                float v = half_lo(vmj);
+                if (v == 0.f || vmj == kZeroRow) v = kLeastScale;
+                const int t = min((int)(__float_as_uint(v) >> 23) - 127 - 5, te);
+                sh.td[ring][pl] = (float)t;
+                sh.tw[ring][pl] = pow2i(-t);
+              }
+            } else {
+              float v = s0 == 0.f || own[j] == kZeroRow ? kLeastScale : s0;
+              const int t = spread ? min((int)(__float_as_uint(v) >> 23) - 127 - 5, te) : te;
+              v *= pow2i(-t);
+              if (p0 + kTile > least && in && v != v) {  // a NaN row that not all rows see
+                const int x = p0 + pl - first_odd;
+                atomicOr(&sh.odd[seg & 3][half][x / 32], 1u << (x % 32));
+                v = 0.f;
+              }
+              if (in) sv[j] = pack_h2(v, v);
+            }
+          }
+          if (!is_v && half == 0 && lane == 0) sh.te[ring] = spread ? 0 : te, sh.spread[ring] = spread;
+          if (ti + 1 < w.n) fetch_meta(ti + 1, ids_next);
+          uint8_t *const to = buf + st * C::KB;
+#pragma unroll
+          for (int k = 0; k < C::NI; ++k) {
+            if (k == C::NI - C::NR) fetch_rows(min(ti + 1, w.n - 1), ti + 1 < w.n ? ids_next : ids);
+            const int pl = place(k);
+            const uint32_t z = C::RPI * (k / (C::PPR / C::PP)) < 32 ? __shfl_sync(0xffffffffu, zz[0], pl & 31) : __shfl_sync(0xffffffffu, zz[1], pl & 31);
+            uint32_t s2 = 0;
+            if (is_v)
+              s2 = C::RPI * (k / (C::PPR / C::PP)) < 32 ? __shfl_sync(0xffffffffu, sv[0], pl & 31) : __shfl_sync(0xffffffffu, sv[1], pl & 31);
+            const uint32_t words[4] = {r[k % C::NR].x, r[k % C::NR].y, r[k % C::NR].z, r[k % C::NR].w};
+            r[k % C::NR] = fetch((k + C::NR) % C::NI);
+            constexpr int CPP = BITS == 4 ? 4 : 2;  // chunks a piece
+#pragma unroll
+            for (int i = 0; i < CPP; ++i) {
+              uint4 o = convert8<BITS>(BITS == 4 ? make_uint2(words[i], 0) : make_uint2(words[2 * i % 4], words[(2 * i + 1) % 4]), z);
+              if (is_v) o.x = hmul2_u(o.x, s2), o.y = hmul2_u(o.y, s2), o.z = hmul2_u(o.z, s2), o.w = hmul2_u(o.w, s2);
+              const int c = CPP * (lp + C::PP * (k % (C::PPR / C::PP))) + i;
+              *reinterpret_cast<uint4 *>(to + (c / 8) * kBlk + pl * 128 + (((c & 7) ^ (pl & 7)) << 4)) = o;
+            }
+          }
+          hand_over(&full[st]);
+          ids = ids_next;
+          ids_next = load_ids(ti + 2);
+        }
+      }
+      T += w.n;
+      ++seg;
+    }
+    if (!ok && lane == 0) sh.fail = 1;
+  } else {
+    // ---- softmax: stream s, half h of a tile's positions, thread = row
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+    const int s = warp / 8, h = warp / 4 % 2, row = tid % kStream;
+    const uint32_t tw = tm + ((uint32_t)(warp % 4 * 32) << 16), ts = tw + s * 128, to = tw + 256 + s * HD;
+    bool ok = true;
+    int T = 0, seg = 0, cs = 0, os = 0;
+    auto sync_stream = [&](bool v) { return barrier_and(1 + s, 256, v); };
+    for (int turn = 0; ok; ++turn) {
+      Run &w = roles.run[5 + (turn & 1)];
+      if (tid == 0) roles.walk[5].next(a, by_rep, w);
+      named_barrier_sync(3, kSoft);
+      if (!w.any) break;
+      const int lr = w.split ? row : s * kStream + row;  // the block's row
+      const bool in = lr < w.live, busy = lr - lane < w.live;
+      const int tok = (int)by_rep.divide(w.r0 + min(lr, w.live - 1));
+      const int limit = in && w.len > 0 ? w.before + tok + 1 : 0;  // positions that the row sees
+      const int first = w.split ? s : 0, step = w.split ? 2 : 1;
+      const int seen_by_all = w.least, n_tiles = w.n, t0 = w.t0;
+      auto out_row = [&](int tok) {
+        return reinterpret_cast<__nv_bfloat16 *>(a.o) + ((size_t)(w.q0 + tok) * a.H + w.g * rep + w.r0 + lr - tok * rep) * HD;
+      };
+      float m = -INFINITY, l = 0.f, c1 = 1.f;
+      bool own = false;
+      for (int ti = first; ti < n_tiles; ti += step) {
+        const int ring = (T + ti) & 3, p0 = (t0 + ti) * kTile + 64 * h;
+        ok = wait(&sh.s_full[s], cs & 1);
+        ++cs;
+        if (!ok && lane == 0) sh.sfail[s] = 1;
+        tc_fence_after();
+        if (ti == first) {
+          c1 = BF ? a.scale : in ? sh.qf[seg & 3][lr] : 1.f;
+          own = !BF && __any_sync(0xffffffffu, c1 != 1.f);
+        }
+        const bool spread = !BF && sh.spread[ring] != 0;
+        const int ti2 = BF ? 0 : sh.te[ring];
+        const float te = (float)ti2;
+        const bool some = p0 + 64 > seen_by_all;
+        const bool plain = !some && !spread && !own;
+        // u = the scores of columns 16 c .. (raw in u) plus ms (and V's exponents), -inf where they are not seen
+        auto exponents = [&](float (&u)[16], int c, float ms, bool plain) {
+          const uint64_t mm = pack_f32x2(ms, ms), cc = pack_f32x2(c1, c1);
+          if (!BF && !plain && own)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) u[j] *= c1;
+#pragma unroll
+          for (int j = 0; j < 16; j += 4) {
+            uint64_t k0 = cc, k1 = cc;
+            if constexpr (!BF) {
+              const float4 k4 = *reinterpret_cast<const float4 *>(&sh.sk[ring][64 * h + 16 * c + j]);
+              k0 = pack_f32x2(k4.x, k4.y), k1 = pack_f32x2(k4.z, k4.w);
+            }
+            unpack_f32x2(fma_f32x2(pack_f32x2(u[j], u[j + 1]), k0, mm), u[j], u[j + 1]);
+            unpack_f32x2(fma_f32x2(pack_f32x2(u[j + 2], u[j + 3]), k1, mm), u[j + 2], u[j + 3]);
+          }
+          if (plain) return;
+          if (spread)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) u[j] += sh.td[ring][64 * h + 16 * c + j];
+          if (some) {
+            const int n = limit - p0 - 16 * c;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) u[j] = j < n ? u[j] : -INFINITY;
+          }
+        };
+        // p of the half row with maximum m, packed; their sum in units of 2^-te
+        uint32_t p[4][8];
+        auto probabilities = [&](auto is_plain) {
+          constexpr bool PLAIN = decltype(is_plain)::value;
+          const float ms = m == -INFINITY ? 0.f : te - m;
+          uint64_t sum[2] = {0, 0};
+          float u[2][16];
+          tmem_ld16(ts + 64 * h, *reinterpret_cast<uint32_t(*)[16]>(&u[0]));
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            float(&v)[16] = u[c % 2];
+            tmem_ld_wait16(v);
+            if (c < 3) tmem_ld16(ts + 64 * h + 16 * (c + 1), *reinterpret_cast<uint32_t(*)[16]>(&u[(c + 1) % 2]));
+            exponents(v, c, ms, PLAIN);
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) {
+              float e0 = ex2(v[j]), e1 = ex2(v[j + 1]);
+              p[c][j / 2] = BF ? pack_bf2(e0, e1) : pack_h2(e0, e1);
+              if (!PLAIN && spread) e0 *= sh.tw[ring][64 * h + 16 * c + j], e1 *= sh.tw[ring][64 * h + 16 * c + j + 1];
+              sum[j / 2 % 2] = add_f32x2(sum[j / 2 % 2], pack_f32x2(e0, e1));
+            }
+          }
+          float s0, s1;
+          unpack_f32x2(add_f32x2(sum[0], sum[1]), s0, s1);
+          return s0 + s1;
+        };
+        auto biggest = [&]() {  // p's largest, of what is packed
+          uint32_t b = 0;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) b = __vmaxu2(b, p[j / 8][j % 8] & 0x7fff7fffu);
+          return max(b & 0xffffu, b >> 16);
+        };
+        float part = 0.f;
+        bool fine = ok;
+        if (busy && ok && ti != first) {
+          part = plain ? probabilities(std::true_type()) : probabilities(std::false_type());
+          // (with exponents of their own the sum does not bound p)
+          fine = spread ? biggest() < (BF ? 0x7f80u : 0x7800u) && (m > -INFINITY || part == 0.f)
+                        : !(part >= kMostSum) && (m > -INFINITY || part == 0.f);
+        }
+        tc_fence_before();
+        if (!sync_stream(fine && ti != first)) {
+          if (sh.sfail[s]) {
+            ok = false;
+            break;
+          }
+          // the maxima of the rows' halves, whole numbers above them, and what was summed with the old ones
+          float mx = -INFINITY;
+          if (busy) {
+#pragma unroll 1
+            for (int c = 0; c < 4; ++c) {
+              float u[16];
+              tmem_ld16(ts + 64 * h + 16 * c, *reinterpret_cast<uint32_t(*)[16]>(&u));
+              tmem_ld_wait16(u);
+              exponents(u, c, te, false);
+#pragma unroll
+              for (int j = 0; j < 16; ++j) mx = fmaxf(mx, u[j]);
+            }
+          }
+          sh.pm[s][h][row] = mx;
+          sync_stream(true);
+          if (busy) {
+            mx = fmaxf(mx, sh.pm[s][h ^ 1][row]);
+            const float mn = fmaxf(m, ceilf(mx) - C::LIFT), al = raise_factor(m, mn);
+            if (ti != first && __any_sync(0xffffffffu, al != 1.f)) {
+#pragma unroll 1
+              for (int c = 0; c < HD / 32; ++c) {
+                uint32_t o[16];
+                tmem_ld16(to + h * (HD / 2) + 16 * c, o);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * al);
+                tmem_st16(to + h * (HD / 2) + 16 * c, o);
+              }
+            }
+            m = mn;
+            l *= al;
+            part = probabilities(std::false_type());
+          }
+          tc_fence_before();
+          sync_stream(true);  // S is read before P takes its place
+        }
+        tc_fence_after();
+        if (busy) {
+          l = fmaf(part, BF ? 1.f : pow2i(-ti2), l);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_st8(ts + 32 * h + 8 * c, p[c]);
+          tmem_st_wait();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.p_full[s]);
+      }
+      if (!ok) break;
+
+      // ---- the rows' outputs, or their parts
+      if (w.n == 0) {  // not served
+        if (in && (s == 0 || !w.split))
+#pragma unroll 1
+          for (int e = 0; e < HD / 16; ++e)
+            *reinterpret_cast<uint4 *>(out_row(tok) + h * (HD / 2) + 8 * e) = make_uint4(0, 0, 0, 0);
+        continue;
+      }
+      const bool has = first < w.n;
+      if (has && ok) {
+        ok = wait(&sh.o_full[s], os & 1);
+        ++os;
+        sh.pl[s][h][row] = l;
+      }
+      ok = barrier_and(3, kSoft, ok);  // (both streams leave together after a timeout)
+      if (!ok) break;
+      tc_fence_after();
+      const float L = has ? sh.pl[s][0][row] + sh.pl[s][1][row] : 0.f;
+      const bool alone = w.whole && !w.split;
+      const bool none = m == -INFINITY && L == 0.f;  // (all scores NaN: L is NaN)
+      const float inv = alone ? (none ? 0.f : 1.f / L) : 1.f;
+      const int c0 = w.c0, cl = w.cl;
+      float *pt = a.part + (((size_t)blockIdx.x * 2 + (w.t0 == 0)) * kBlockRows + s * kStream + row) * (HD + 4);
+      if (has && busy) {
+        const int least = seen_by_all, first_odd = least / kTile * kTile;
+        uint32_t odd = 0;
+        if ((w.t0 + w.n) * kTile > least)
+#pragma unroll 1
+          for (int i = 0; i < 32; ++i) odd |= sh.odd[seg & 3][i / 16][i % 16];
+#pragma unroll 1
+        for (int c = 0; c < HD / 64; ++c) {
+          float o[32];
+          tmem_ld32(to + h * (HD / 2) + 32 * c, *reinterpret_cast<uint32_t(*)[32]>(&o));
+          tmem_ld_wait();
+          if (odd != 0) {  // V rows that are not finite, added where they are seen
+#pragma unroll 1
+            for (int x = 0; x < 512 && first_odd + x < limit; ++x) {
+              if (((sh.odd[seg & 3][0][x / 32] | sh.odd[seg & 3][1][x / 32]) >> (x % 32) & 1) == 0) continue;
+              // (in split blocks the other stream's tiles are the other stream's to add)
+              if (w.split && ((first_odd + x) / kTile - w.t0 - first) % 2 != 0) continue;
+              const int p = first_odd + x, id = min(max(a.tables[(size_t)w.b * a.max_pages + (p >> a.shift)], 0), a.n_pages - 1);
+              const size_t at = (((size_t)id * a.Hkv + w.g) << a.shift) + (p & (page - 1));
+#pragma unroll
+              for (int e = 0; e < 32; ++e) {
+                const float f = BF ? __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(a.vc)[at * HD + h * (HD / 2) + 32 * c + e])
+                                   : __int_as_float(0x7fffffff);
+                if (!isfinite(f)) o[e] += f;
+              }
+            }
+          }
+          if (!in) continue;
+          if (alone) {
+            __nv_bfloat16 *dst = out_row(tok) + h * (HD / 2) + 32 * c;
+#pragma unroll
+            for (int e = 0; e < 32; e += 8)
+              *reinterpret_cast<uint4 *>(dst + e) =
+                  none ? make_uint4(0, 0, 0, 0)
+                       : make_uint4(pack_bf2(o[e] * inv, o[e + 1] * inv), pack_bf2(o[e + 2] * inv, o[e + 3] * inv),
+                                    pack_bf2(o[e + 4] * inv, o[e + 5] * inv), pack_bf2(o[e + 6] * inv, o[e + 7] * inv));
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4)
+              *reinterpret_cast<float4 *>(pt + h * (HD / 2) + 32 * c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+          }
+        }
+      }
+      tc_fence_before();
+      if (!alone) {
+        if (in && h == 0) *reinterpret_cast<float2 *>(pt + HD) = make_float2(m, L);
+        __threadfence();
+        named_barrier_sync(3, kSoft);
+        if (!w.whole) {
+          if (tid == 0) {
+            sh.last = atomicAdd(&a.counters[c0], 1) == cl - c0;
+            if (sh.last) a.counters[c0] = 0;
+          }
+          named_barrier_sync(3, kSoft);
+        }
+        if (w.whole || sh.last) {
+          // all parts of the block in their order: CTA c0 has its begin (in its place 1), the others their first blocks
+          // (0); a split block's streams one after the other
+          __threadfence();
+          constexpr int LPR = HD / 4, CU = 4;
+          const int e = 4 * (tid % LPR), subs = w.split ? 2 : 1, parts = (cl - c0 + 1) * subs;
+          for (int r = tid / LPR; r < w.live; r += kSoft / LPR) {
+            float M = -INFINITY, S = 0.f;
+            float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int k0 = 0; k0 < parts; k0 += CU) {
+              float2 ml[CU];
+              float4 ov[CU];
+              float mn = M;
+#pragma unroll
+              for (int j = 0; j < CU; ++j) {
+                const int k = k0 + j, cta = k / subs, sub = k % subs;
+                const float *ps = a.part + (((size_t)(c0 + cta) * 2 + (cta == 0)) * kBlockRows + sub * kStream + r) * (HD + 4);
+                const bool there = k < parts;
+                ml[j] = there ? __ldcg(reinterpret_cast<const float2 *>(ps + HD)) : make_float2(-INFINITY, 0.f);
+                ov[j] = there ? __ldcg(reinterpret_cast<const float4 *>(ps + e)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                mn = fmaxf(mn, ml[j].x);
+              }
+              const float f0 = M == -INFINITY ? 0.f : ex2(M - mn);
+              M = mn;
+              S *= f0;
+              O.x *= f0, O.y *= f0, O.z *= f0, O.w *= f0;
+#pragma unroll
+              for (int j = 0; j < CU; ++j) {
+                if (ml[j].x == -INFINITY && ml[j].y == 0.f) continue;  // (its values were not written)
+                const float f = ml[j].x == -INFINITY ? 0.f : ex2(ml[j].x - M);  // (a NaN of a part stays NaN)
+                S = fmaf(ml[j].y, f, S);
+                O.x = fmaf(ov[j].x, f, O.x), O.y = fmaf(ov[j].y, f, O.y), O.z = fmaf(ov[j].z, f, O.z), O.w = fmaf(ov[j].w, f, O.w);
+              }
+            }
+            const bool nothing = M == -INFINITY && S == 0.f;
+            const int rr = w.r0 + r, t = (int)by_rep.divide(rr);
+            *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(a.o) + ((size_t)(w.q0 + t) * a.H + w.g * rep + rr - t * rep) * HD + e) =
+                nothing ? make_uint2(0, 0) : make_uint2(pack_bf2(O.x / S, O.y / S), pack_bf2(O.z / S, O.w / S));
+          }
+        }
+      }
+      T += w.n;
+      ++seg;
+    }
+    if (!ok && lane == 0) sh.fail = 1;
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (sh.fail) {
+    // what the MMA warp issued last is given time to end before its memory goes
+    if (tid == 0) atomicExch(&g_attn_paged_tc_status, -6);
+    const unsigned long long t0 = global_timer_ns();
+    for (int i = 0; i < (1 << 20) && global_timer_ns() - t0 < 2000000ull; ++i) __nanosleep(1000);
+    __syncthreads();
+  }
+  if (warp == kMmaWarp) {
+    tc_fence_after();
+    tmem_dealloc(tm, kTmemCols);
+  }
+}
+
+size_t attn_paged_tc_part_floats(int hd, int num_sms) { return (size_t)num_sms * 2 * kBlockRows * (hd + 4); }
+
+namespace {
+
+template <int HD, int BITS>
+cudaError_t launch_t(const AttnPagedArgs &a, int num_sms, cudaStream_t s) {
+  constexpr int smem = Cfg<HD, BITS>::SMEM;
+  static std::atomic<bool> done[64];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  auto k = attn_paged_tc_kernel<HD, BITS>;
+  if (dev < 0 || dev >= 64 || !done[dev].load(std::memory_order_acquire)) {
+    // whether the warps' shares of registers fit into what a block is launched with (their exchange would wait forever)
+    cudaFuncAttributes f;
+    if ((e = cudaFuncGetAttributes(&f, k)) != cudaSuccess) return e;
+    if (kRegsSoftmax * 512 + (kRegsConv + kRegsMma) * 128 > f.numRegs * kThreads) return cudaErrorInvalidConfiguration;
+    if ((e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64) done[dev].store(true, std::memory_order_release);
+  }
+  const long long blocks = ((long long)a.m * (a.H / a.Hkv) + kBlockRows - 1) / kBlockRows + a.batch;
+  const long long tiles = (((long long)a.max_pages << a.shift) + kTile - 1) / kTile;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  cfg.gridDim = dim3((unsigned)std::min((long long)num_sms, blocks * tiles * a.Hkv));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  return cudaLaunchKernelEx(&cfg, k, a, Divisor(a.H / a.Hkv));
+}
+
+}  // namespace
+
+cudaError_t launch_attn_paged_tc(const AttnPagedArgs &a, int hd, int bits, int num_sms, cudaStream_t s) {
+#define WQ_PAGED(HD, BITS) \
+  if (hd == HD && bits == BITS) return launch_t<HD, BITS>(a, num_sms, s);
+  WQ_PAGED(128, 16) WQ_PAGED(128, 8) WQ_PAGED(128, 4) WQ_PAGED(64, 16) WQ_PAGED(64, 8) WQ_PAGED(64, 4)
+#undef WQ_PAGED
+  return cudaErrorInvalidValue;
+}
+
+cudaError_t read_attn_paged_tc_status(int *status) {
+  cudaError_t e = cudaDeviceSynchronize();
+  if (e != cudaSuccess) return e;
+  e = cudaMemcpyFromSymbol(status, g_attn_paged_tc_status, sizeof(int));
+  if (e != cudaSuccess) return e;
+  const int zero = 0;
+  return cudaMemcpyToSymbol(g_attn_paged_tc_status, &zero, sizeof(int));
+}
+
+}  // namespace wq

@@ -67,5 +67,9 @@ int attn_paged_ctas(int num_sms);
 size_t attn_paged_part_floats(int hd, int num_sms);
 cudaError_t launch_attn_paged(const AttnPagedArgs &a, int hd, int bits, int num_sms, cudaStream_t s);
 cudaError_t read_attn_paged_status(int *status);
+// The same on the tcgen05 tensor cores (wq_attn_paged_tc.cu); part: [CTA][2][256][HD + 4].
+size_t attn_paged_tc_part_floats(int hd, int num_sms);
+cudaError_t launch_attn_paged_tc(const AttnPagedArgs &a, int hd, int bits, int num_sms, cudaStream_t s);
+cudaError_t read_attn_paged_tc_status(int *status);
 
 }  // namespace wq

@@ -49,6 +49,7 @@
 #include <cstdint>
 
 #include "wq_cvt.cuh"
+#include "wq_tc.cuh"
 #include "wq_internal.h"
 #include "wq_kv.h"
 #include "wq_ptx.cuh"
@@ -81,23 +82,6 @@ constexpr int kSpread = 8;
 // registers a thread: the launch's 72 x 416 shared out as 104 x 128 + 56 x 256 + 72 x 32
 constexpr int kRegsSoftmax = 104, kRegsConv = 56;
 
-__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
-  uint64_t v;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
-  return v;
-}
-// Barrier `id` over `count` threads: whether `v` holds for all of them.
-__device__ __forceinline__ bool barrier_and(int id, int count, bool v) {
-  uint32_t r;
-  asm volatile(
-      "{\n .reg .pred p, q;\n setp.ne.u32 p, %3, 0;\n barrier.cta.red.and.pred q, %1, %2, p;\n selp.u32 %0, 1, 0, q;\n}\n"
-      : "=r"(r)
-      : "r"(id), "r"(count), "r"((uint32_t)v)
-      : "memory");
-  return r != 0;
-}
-// 2^e, -126 <= e <= 127
-__device__ __forceinline__ float pow2i(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
 // The exact power of two 2^e that puts a row's largest value mx (not 0) in [2^top,
 // 2^(top + 1)); kept where 2^e and 2^-e are normal.  An infinite mx: 2^(top - 128),
 // which keeps every finite value in range.
@@ -106,42 +90,6 @@ __device__ __forceinline__ int f16_shift(float mx, int top) {
   return mx == 0.f ? 0 : min(126, top - e);
 }
 
-// 32 lanes x 16 consecutive 32-bit TMEM columns, written.
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
-      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
-      "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
-      : "memory");
-}
-__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
-// D (TMEM) = A (TMEM) * B (+ D when `accumulate`), issued by one thread.
-__device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
-                                        uint32_t accumulate) {
-  asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-// B operand [k][n] with n contiguous (MN-major), 128-byte swizzle: blocks of 64 n
-// `lbo` bytes apart, groups of 8 k 1024 bytes apart.
-__device__ __forceinline__ uint64_t umma_desc_mnmajor_sw128(uint32_t saddr, uint32_t lbo) {
-  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)((lbo >> 4) & 0x3FFFu) << 16) | ((uint64_t)(1024 >> 4) << 32) |
-         ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
-}
-// fp32 accumulator, A and B binary16 or bf16, A K-major, B K-major or MN-major.
-__host__ __device__ constexpr uint32_t tree_idesc(int N, bool bf16, bool b_mn) {
-  return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (b_mn ? 1u << 16 : 0u) | ((uint32_t)(N >> 3) << 17) |
-         ((uint32_t)(kTcRows >> 4) << 24);
-}
-
-// 2^(m - mn) for a maximum raised from m to mn (whole numbers, or infinite).
-__device__ __forceinline__ float raise_factor(float m, float mn) {
-  const float d = m - mn;
-  return mn == m ? 1.f : d < -126.f ? 0.f : pow2i((int)d);
-}
 // What a row has so far, times al: its probabilities of the tile's first 32 pc columns, and 16 oc columns of O.
 template <bool BF>
 __device__ __noinline__ void rescale(uint32_t tw, int pc, int oc, float al) {
@@ -330,27 +278,6 @@ struct Shared {
   __align__(16) float td[2][kTile], tw[2][kTile];  // rows' own exponents t of V (drafts, spread), 2^-t
 };
 
-// 8 codes as 8 binary16 values code - z; z1024: 1024 + z in both halves.
-template <int BITS>
-__device__ __forceinline__ uint4 convert8(const uint2 &c, uint32_t z1024) {
-  uint4 o;
-  if constexpr (BITS == 8) {
-    o.x = hsub2_u(__byte_perm(c.x, 0x64646464u, 0x4140), z1024);
-    o.y = hsub2_u(__byte_perm(c.x, 0x64646464u, 0x4342), z1024);
-    o.z = hsub2_u(__byte_perm(c.y, 0x64646464u, 0x4140), z1024);
-    o.w = hsub2_u(__byte_perm(c.y, 0x64646464u, 0x4342), z1024);
-  } else {
-    // 64 + z from 1024 + z: exact (z <= 15)
-    const uint32_t z64 = hsub2_u(z1024, 0x63806380u);  // 960
-    const uint32_t x = c.x >> 8;
-    o.x = hsub2_u((c.x & 0x000f000fu) | 0x64006400u, z1024);
-    o.y = hfma16_u((c.x & 0x00f000f0u) | 0x64006400u, z64);
-    o.z = hsub2_u((x & 0x000f000fu) | 0x64006400u, z1024);
-    o.w = hfma16_u((x & 0x00f000f0u) | 0x64006400u, z64);
-  }
-  return o;
-}
-
 }  // namespace
 
 template <int HD, int BITS>
@@ -406,7 +333,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
 
   if (nt > 0 && warp == kMmaWarp) {
     // ---- MMAs
-    constexpr uint32_t idqk = tree_idesc(kTile, BF, false), idpv = tree_idesc(HD, BF, true);
+    constexpr uint32_t idqk = attn_idesc(kTile, BF, false), idpv = attn_idesc(HD, BF, true);
     const uint64_t qd = umma_desc_kmajor_sw128(smem_addr(qbuf), 1024), kd = umma_desc_kmajor_sw128(smem_addr(kbuf), 1024);
     const uint64_t vd = umma_desc_mnmajor_sw128(smem_addr(vbuf), kBlk);
     if (elect_one()) {
@@ -427,7 +354,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) attn_tree_tc_kernel(const TreeA
         ok = mbar_wait(&sh.v_full, i & 1) && mbar_wait(&sh.p_full, (i + 1) & 1);
         if (!ok) break;
         tc_fence_after();
-        const uint32_t id = !BF && i == 0 && w.t0 < ndr && sh.wide ? tree_idesc(HD, true, true) : idpv;
+        const uint32_t id = !BF && i == 0 && w.t0 < ndr && sh.wide ? attn_idesc(HD, true, true) : idpv;
 #pragma unroll
         for (int ks = 0; ks < kTile / 16; ++ks)
           umma_ts(tm + 128, tm + 8 * ks, vd + (uint64_t)((ks * 2048) >> 4), id, i > 0 || ks > 0);

@@ -81,14 +81,15 @@ def pool_values(pool):
 
 def attn_ref(q, cu, kv_lens, tables, pool, scale, own=None):
     """fp64 (o, bound) of wq_attn_paged.  The bound of |got - o|, element by element: each probability off by u of itself
-    (its rounding to 16 bits, 2^-11 over a quantized pool and 2^-8 over a bf16 one) and by the error of its score, each fp32 sum
+    (its rounding to 16 bits, 2^-11 over a quantized pool, where a kernel may round V once to binary16 too, and 2^-8 over a bf16
+    one) and by the error of its score, each fp32 sum
     by n 2^-24 of its terms' magnitudes (codes and zero points are summed apart, so those of code + z), 2^x by 2^-21, and the
     bf16 store by 2^-8.  Over a quantized pool the largest p times V's scale is at least 2^6 where binary16's least step is
     2^-24: what is left of any other code is off by 2^-31 of the largest scale more."""
     kd, vd, ka, va, sv = pool_values(pool)
     m, h, hd = q.shape
     rep = h // pool.n_kv
-    u = 2.0 ** -8 if pool.bits == 16 else 2.0 ** -11
+    u = 2.0 ** -8 if pool.bits == 16 else 2.0 ** -10
     o = torch.zeros((m, h, hd), dtype=torch.float64, device="cuda")
     bound = torch.zeros_like(o)
     for b, n in enumerate(kv_lens):
