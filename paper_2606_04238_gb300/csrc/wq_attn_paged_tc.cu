@@ -6,7 +6,7 @@
 // 128, and tiles of 128 positions:
 //   S = Q K^T   128 x 128 a stream in TMEM, Q and K in shared memory (K-major);
 //   P           binary16 (bf16 pool: bf16) over S's own columns, from the fp32 softmax of two
-//               threads a row, half the tile's positions each;
+//               threads a row, half the tile's positions each (a half's p over its own scores);
 //   O += P V    128 x HD a stream in TMEM, P as the A operand from TMEM, V [position][HD]
 //               in shared memory as it lies in a page (MN-major).
 // The MMA warp issues P V of one stream and its next S while the other's softmax runs.  Up to
@@ -18,8 +18,8 @@
 // K's operands are code - z, exact, its scales factors of the scores; V's are (code - z) s 2^-t
 // rounded to binary16, t one for a tile, or, where a tile's scales span more than 2^8, one
 // for each row, taken into its score.  The maximum is not searched in every tile: p is taken
-// with the maximum that the row has, which is raised, and O rescaled in TMEM by a power of two,
-// only where half a row's p add up to 2^15 (p is 2^6 at most where it is raised).
+// with the maximum that the row has, which is raised, and what was computed with it rescaled in
+// TMEM by a power of two, only where 16 p add up to 2^15 (p is 2^6 at most where it is raised).
 //
 // The tiles of all blocks are laid end to end and every CTA takes an equal run, found from the
 // lengths themselves; blocks are paired, the first with the last and so on inward, so that
@@ -58,15 +58,15 @@ constexpr int kTile = 128;                 // positions a tile
 constexpr int kSoft = 512;                 // softmax threads
 constexpr int kConvWarp = kSoft / 32, kMmaWarp = kConvWarp + 4;
 constexpr int kThreads = 768;               // registers are given to whole groups of 4 warps: 3 of the last are idle
-// registers a thread: the launch's 80 x 768 shared out as 88 x 512 + 88 x 128 + 40 x 128
-constexpr int kRegsSoftmax = 88, kRegsConv = 88, kRegsMma = 40;
+// registers a thread: the launch's 80 x 768 shared out as 80 x 512 + 96 x 128 + 64 x 128
+constexpr int kRegsSoftmax = 80, kRegsConv = 96, kRegsMma = 64;
 constexpr int kBlk = kTile * 128;          // bytes of a 64-value block of Q, K or V: [row][128 bytes], swizzled
 constexpr int kTmemCols = 512;             // S / P of the streams 0.., 128..; O 256.., 256 + HD..
 // Queries enter binary16 times 2^7, which keeps a row with its largest |q| in [2^-4, 2^8) whole
 // but for values below 2^-27 of that; other rows by a power of two of their own.
 constexpr int kQueryShift = 7;
 constexpr int kSpread = 8;                 // exponents that V's scales of a tile may span with one power of two for all
-constexpr float kMostSum = 32768.f;        // of half a row's p in a tile; binary16 ends at 65504
+constexpr float kMostSum = 32768.f;        // of 16 p; binary16 ends at 65504
 
 template <int HD, int BITS>
 struct Cfg {
@@ -81,8 +81,19 @@ struct Cfg {
   static constexpr float LIFT = BITS == 16 ? 0.f : 6.f;  // of p: small ones are then normal numbers
 };
 
+
+// A run of tiles of one block of rows.
+struct Run {
+  int b, g, q0, len, before, r0, live, t0, n;  // live: rows of the block; tiles t0 .. t0 + n - 1
+  int least;                                   // positions that its first row sees
+  int c0, cl;                                  // the first and last CTA that have tiles of the block
+  bool any, split, whole;
+};
+
 struct Shared {
   uint64_t q_full, q_empty, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2];
+  uint64_t run_full[4], run_empty[4];
+  Run run[4];
   uint32_t tmem;
   int fail, sfail[2], last;
   // of a tile, four tiles deep (a tile's are written when S of the one two before is done, whose softmax has then
@@ -96,16 +107,8 @@ struct Shared {
   float pm[2][2][kStream], pl[2][2][kStream];  // the halves' maxima and sums
 };
 
-// A run of tiles of one block of rows.
-struct Run {
-  int b, g, q0, len, before, r0, live, t0, n;  // live: rows of the block; tiles t0 .. t0 + n - 1
-  int least;                                   // positions that its first row sees
-  int c0, cl;                                  // the first and last CTA that have tiles of the block
-  bool any, split, whole;
-};
-
 // The line of tiles: sequences in order, in a sequence pairs of blocks, the kv head fastest.  A pair has C places, as many
-// as any has tiles; those behind its two blocks are empty.  Held in shared memory, one a role.
+// as any has tiles; those behind its two blocks are empty.
 struct Walk {
   long long x, x1, base, T, N, total;
   int b, R, nb, before, C;
@@ -196,11 +199,34 @@ struct Walk {
   }
 };
 
-// The roles' runs and where they are in the line: four converting warps, the MMA warp, softmax (two, in turn).
-struct Roles {
-  Run run[7];
-  Walk walk[6];
-};
+// A half row's p of 16 c columns, and 16 c columns of O, times al.
+template <bool BF>
+__device__ __noinline__ void rescale_p(uint32_t at, int c, float al) {
+  tmem_st_wait();
+#pragma unroll 1
+  for (int i = 0; i < (c + 1) / 2; ++i) {  // (a place behind the last may hold scores that are not read yet: put back as they are)
+    uint32_t p[16];
+    tmem_ld16(at + 16 * i, p);
+    tmem_ld_wait();
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (e < 8 || 2 * i + 1 < c) p[e] = BF ? pack_bf2(bf_lo(p[e]) * al, bf_hi(p[e]) * al) : hmul2_u(p[e], pack_h2(al, al));
+    tmem_st16(at + 16 * i, p);
+  }
+  tmem_st_wait();
+}
+template <int N>
+__device__ __noinline__ void rescale_o(uint32_t at, float al) {
+#pragma unroll 1
+  for (int c = 0; c < N; ++c) {
+    uint32_t o[16];
+    tmem_ld16(at + 16 * c, o);
+    tmem_ld_wait();
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * al);
+    tmem_st16(at + 16 * c, o);
+  }
+}
 
 __device__ __forceinline__ float half_lo(uint32_t m) { return __half2float(__ushort_as_half((unsigned short)(m & 0xffffu))); }
 
@@ -212,7 +238,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
   constexpr bool BF = BITS == 16;
   extern __shared__ uint8_t paged_dyn[];
   __shared__ Shared sh;
-  __shared__ Roles roles;
   uint8_t *qbuf = paged_dyn + (1024 - (smem_addr(paged_dyn) & 1023)) % 1024, *kbuf = qbuf + 2 * C::KB, *vbuf = kbuf + 2 * C::KB;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int page = 1 << a.shift;
@@ -231,19 +256,16 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
         mbar_init(&sh.o_full[i], 1);
         sh.sfail[i] = 0;
       }
+      for (int i = 0; i < 4; ++i) {
+        mbar_init(&sh.run_full[i], 1);
+        mbar_init(&sh.run_empty[i], kMmaWarp + 1);
+      }
       fence_barrier_init();
       sh.fail = 0;
     }
   }
   pdl_wait();
   pdl_launch_dependents();
-  if (warp == 0) {
-    bool bad = false;
-    Walk walk;
-    walk.start(a, by_rep, bad);
-    if (bad && blockIdx.x == 0) atomicExch(&g_attn_paged_tc_status, -1);
-    if (lane < 6) roles.walk[lane] = walk;
-  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -251,6 +273,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
   const int rep = (int)by_rep.d;
   // all lanes alike: a warp leaves its loop as one after a timeout
   auto wait = [&](uint64_t *bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity)) != 0; };
+  // a warp is done with a run
+  auto done = [&](int turn) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&sh.run_empty[turn & 3]);
+  };
   // a warp's arrival, its shared-memory writes made visible to the tensor cores
   auto hand_over = [&](uint64_t *bar) {
     fence_proxy_async_smem();
@@ -264,11 +291,25 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
     const uint64_t qd = umma_desc_kmajor_sw128(smem_addr(qbuf), 1024), kd = umma_desc_kmajor_sw128(smem_addr(kbuf), 1024);
     const uint64_t vd = umma_desc_mnmajor_sw128(smem_addr(vbuf), kBlk);
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsMma));
-    Run &w = roles.run[4];
-    if (warp == kMmaWarp && elect_one()) {
+    if (warp == kMmaWarp + 1) {
+      // the runs, for all warps
+      bool bad = false, ok = true;
+      Walk walk;
+      walk.start(a, by_rep, bad);
+      if (bad && blockIdx.x == 0) atomicExch(&g_attn_paged_tc_status, -1);
+      if (lane == 0)
+        for (int turn = 0; ok; ++turn) {
+          if (turn >= 4) ok = mbar_wait(&sh.run_empty[turn & 3], (turn >> 2) + 1 & 1);
+          if (!ok) break;
+          const bool any = walk.next(a, by_rep, sh.run[turn & 3]);
+          mbar_arrive(&sh.run_full[turn & 3]);
+          if (!any) break;
+        }
+      if (!ok) sh.fail = 1;
+    } else if (warp == kMmaWarp && elect_one()) {
       bool ok = true;
       int T = 0, seg = 0, cs[2] = {0, 0};
-      auto scores = [&](int s, int t, bool last) {  // S of stream s and tile t
+      auto scores = [&](const Run &w, int s, int t, bool last) {  // S of stream s and tile t
         ok = mbar_wait(&sh.k_full[(T + t) & 1], (T + t) >> 1 & 1);
         if (!ok) return;
         tc_fence_after();
@@ -282,13 +323,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
         if (w.split || s == 1) umma_commit(&sh.k_empty[(T + t) & 1]);
         if (last) umma_commit(&sh.q_empty);
       };
-      while (ok && roles.walk[4].next(a, by_rep, w)) {
-        if (w.n == 0) continue;
+      for (int turn = 0; ok; ++turn) {
+        const Run &w = sh.run[turn & 3];
+        ok = mbar_wait(&sh.run_full[turn & 3], turn >> 2 & 1);
+        if (!ok || !w.any) break;
         const int step = w.split ? 2 : 1;
-        ok = mbar_wait(&sh.q_full, seg & 1);
+        if (w.n > 0) ok = mbar_wait(&sh.q_full, seg & 1);
         for (int s = 0; s < 2 && ok; ++s) {
           const int t = w.split ? s : 0;
-          if (t < w.n) scores(s, t, w.split ? t == w.n - 1 : s == 1 && w.n == 1);
+          if (t < w.n) scores(w, s, t, w.split ? t == w.n - 1 : s == 1 && w.n == 1);
         }
         for (int t = 0; t < w.n && ok; t += step)
           for (int s = 0; s < 2 && ok; ++s) {
@@ -302,16 +345,17 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
             const uint64_t v = vd + (uint64_t)((st * C::KB) >> 4);
 #pragma unroll
             for (int ks = 0; ks < kTile / 16; ++ks)
-              umma_ts(tm + 256 + s * HD, tm + s * 128 + 8 * ks, v + (uint64_t)((ks * 2048) >> 4), idpv, t > 0 || ks > 0);
+              umma_ts(tm + 256 + s * HD, tm + s * 128 + 8 * ks + (ks < 4 ? 0 : 32), v + (uint64_t)((ks * 2048) >> 4), idpv, t > 0 || ks > 0);
             if (w.split || s == 1) umma_commit(&sh.v_empty[st]);
             const int nx = mine + step;
             if (nx < w.n)
-              scores(s, nx, nx == w.n - 1 && (w.split || s == 1));
+              scores(w, s, nx, nx == w.n - 1 && (w.split || s == 1));
             else
               umma_commit(&sh.o_full[s]);
           }
         T += w.n;
-        ++seg;
+        seg += w.n > 0;
+        mbar_arrive(&sh.run_empty[turn & 3]);
       }
       if (!ok) sh.fail = 1;
     }
@@ -319,13 +363,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
   } else if (warp >= kConvWarp) {
     // ---- queries, K and V
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsConv));
-    Run &w = roles.run[warp - kConvWarp];
-    auto next = [&]() {
-      __syncwarp();  // (all lanes are done with the run before)
-      if (lane == 0) roles.walk[warp - kConvWarp].next(a, by_rep, w);
-      __syncwarp();
-      return w.any;
-    };
     const bool is_v = warp >= kConvWarp + 2;
     const int ct = tid - 32 * kConvWarp, half = warp & 1;  // a warp has rows 64 half .. of every tile
     uint8_t *const buf = is_v ? vbuf : kbuf;
@@ -335,8 +372,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
     const float qscale = a.scale * pow2i(-kQueryShift);  // of K's scales
     bool ok = true;
     int T = 0, seg = 0;
-    while (ok && next()) {
-      if (w.n == 0) continue;
+    for (int turn = 0; ok; ++turn) {
+      const Run &w = sh.run[turn & 3];
+      ok = wait(&sh.run_full[turn & 3], turn >> 2 & 1);
+      if (!ok || !w.any) break;
+      if (w.n == 0) {
+        done(turn);
+        continue;
+      }
       const int least = w.least, first_odd = least / kTile * kTile;  // positions from `least` on are not seen by all rows
       // pages of tile ti: lane l < 8 has that of positions 16 l ..
       auto load_ids = [&](int ti) {
@@ -350,11 +393,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
         }
         return id;
       };
-      // the pool's row of place r of tile ti
+      // the pool's row of place r of tile ti (a pool has fewer than 2^32: host check)
       auto row_at = [&](int ids, int ti, int r) {
         const int p0 = (w.t0 + ti) * kTile, p = min(p0 + r, w.len - 1);
         const int id = __shfl_sync(0xffffffffu, ids, (p - p0) >> 4);
-        return (((size_t)id * a.Hkv + w.g) << a.shift) + (p & (page - 1));
+        return (((uint32_t)id * a.Hkv + w.g) << a.shift) + (p & (page - 1));
       };
       int ids = load_ids(0), ids_next = load_ids(1);
       if (is_v && lane < 16) sh.odd[seg & 3][half][lane] = 0;
@@ -395,8 +438,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
           const int p0 = (w.t0 + ti) * kTile;
 #pragma unroll 4
           for (int r = r0; r < kTile; r += 64 / C::CH) {
-            const size_t at = row_at(id, ti, r);
-            cp_async16_zfill(buf + st * C::KB + (c / 8) * kBlk + r * 128 + (((c & 7) ^ (r & 7)) << 4), src + at * C::ROW + c * 16,
+            const uint32_t at = row_at(id, ti, r);
+            cp_async16_zfill(buf + st * C::KB + (c / 8) * kBlk + r * 128 + (((c & 7) ^ (r & 7)) << 4), src + (size_t)at * C::ROW + c * 16,
                              p0 + r < w.len ? 16u : 0u);
           }
           cp_async_commit();
@@ -441,7 +484,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
       } else {
         const int lr = lane % 8 + 8 * (lane / 8 / C::PP), lp = lane / 8 % C::PP;  // a lane's row and piece of a load
         uint4 r[C::NR];
-        size_t at[C::RPI == 8 ? 8 : 4];  // pool rows of a lane's places 64 half + RPI j + lr
+        uint32_t at[C::RPI == 8 ? 8 : 4];  // pool rows of a lane's places 64 half + RPI j + lr
         uint32_t own[2], vm4[4];
         auto place = [&](int k) { return 64 * half + C::RPI * (k / (C::PPR / C::PP)) + lr; };
         auto fetch_rows = [&](int ti, int id) {
@@ -449,12 +492,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
           for (int j = 0; j < 64 / C::RPI; ++j) at[j] = row_at(id, ti, 64 * half + C::RPI * j + lr);
         };
         auto fetch = [&](int k) {
-          return __ldg(reinterpret_cast<const uint4 *>(src + at[k / (C::PPR / C::PP)] * C::ROW + 16 * (lp + C::PP * (k % (C::PPR / C::PP)))));
+          return __ldg(reinterpret_cast<const uint4 *>(src + (size_t)at[k / (C::PPR / C::PP)] * C::ROW + 16 * (lp + C::PP * (k % (C::PPR / C::PP)))));
         };
         auto fetch_meta = [&](int ti, int id) {
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const size_t x = row_at(id, ti, 32 * j + lane);
+            const uint32_t x = row_at(id, ti, 32 * j + lane);
             vm4[j] = __ldg(a.vm + x);
             if (j / 2 == half) own[j % 2] = is_v ? vm4[j] : __ldg(meta + x);
           }
@@ -541,6 +584,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
       }
       T += w.n;
       ++seg;
+      done(turn);
     }
     if (!ok && lane == 0) sh.fail = 1;
   } else {
@@ -552,10 +596,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
     int T = 0, seg = 0, cs = 0, os = 0;
     auto sync_stream = [&](bool v) { return barrier_and(1 + s, 256, v); };
     for (int turn = 0; ok; ++turn) {
-      Run &w = roles.run[5 + (turn & 1)];
-      if (tid == 0) roles.walk[5].next(a, by_rep, w);
-      named_barrier_sync(3, kSoft);
-      if (!w.any) break;
+      const Run &w = sh.run[turn & 3];
+      ok = wait(&sh.run_full[turn & 3], turn >> 2 & 1);
+      if (!ok) sh.sfail[0] = sh.sfail[1] = 1;
+      ok = barrier_and(3, kSoft, ok);
+      if (!ok || !w.any) break;
       const int lr = w.split ? row : s * kStream + row;  // the block's row
       const bool in = lr < w.live, busy = lr - lane < w.live;
       const int tok = (int)by_rep.divide(w.r0 + min(lr, w.live - 1));
@@ -608,100 +653,89 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
             for (int j = 0; j < 16; ++j) u[j] = j < n ? u[j] : -INFINITY;
           }
         };
-        // p of the half row with maximum m, packed; their sum in units of 2^-te
-        uint32_t p[4][8];
+        // The half row's p with maximum m, into the columns whose scores have been read; their sum, in units of 2^-te.
+        // 16 columns at a time: where those add up to kMostSum (or there is no maximum yet) m is raised first, to a whole
+        // number, so that what has been computed with the old one is rescaled by an exact power of two.
+        const float m0 = m;
+        float part = 0.f;
         auto probabilities = [&](auto is_plain) {
           constexpr bool PLAIN = decltype(is_plain)::value;
-          const float ms = m == -INFINITY ? 0.f : te - m;
-          uint64_t sum[2] = {0, 0};
-          float u[2][16];
-          tmem_ld16(ts + 64 * h, *reinterpret_cast<uint32_t(*)[16]>(&u[0]));
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
-            float(&v)[16] = u[c % 2];
-            tmem_ld_wait16(v);
-            if (c < 3) tmem_ld16(ts + 64 * h + 16 * (c + 1), *reinterpret_cast<uint32_t(*)[16]>(&u[(c + 1) % 2]));
-            exponents(v, c, ms, PLAIN);
+            float u[16], sum = 0.f, sum_l = 0.f;
+            uint32_t p[8];
+            tmem_ld16(ts + 64 * h + 16 * c, *reinterpret_cast<uint32_t(*)[16]>(&u));
+            tmem_ld_wait16(u);
+            const float ms = m == -INFINITY ? 0.f : te - m;
+            exponents(u, c, ms, PLAIN);
+#pragma unroll 1
+            for (int again = 0; again < 2; ++again) {
+              uint64_t s2[2] = {0, 0};
+              sum_l = 0.f;
 #pragma unroll
-            for (int j = 0; j < 16; j += 2) {
-              float e0 = ex2(v[j]), e1 = ex2(v[j + 1]);
-              p[c][j / 2] = BF ? pack_bf2(e0, e1) : pack_h2(e0, e1);
-              if (!PLAIN && spread) e0 *= sh.tw[ring][64 * h + 16 * c + j], e1 *= sh.tw[ring][64 * h + 16 * c + j + 1];
-              sum[j / 2 % 2] = add_f32x2(sum[j / 2 % 2], pack_f32x2(e0, e1));
+              for (int j = 0; j < 16; j += 2) {
+                const float e0 = ex2(u[j]), e1 = ex2(u[j + 1]);
+                p[j / 2] = BF ? pack_bf2(e0, e1) : pack_h2(e0, e1);
+                s2[j / 2 % 2] = add_f32x2(s2[j / 2 % 2], pack_f32x2(e0, e1));
+                if (!PLAIN && spread)
+                  sum_l += fmaf(e0, sh.tw[ring][64 * h + 16 * c + j], e1 * sh.tw[ring][64 * h + 16 * c + j + 1]);
+              }
+              float x, y;
+              unpack_f32x2(add_f32x2(s2[0], s2[1]), x, y);
+              sum = x + y;
+              const bool up = sum >= kMostSum || (m == -INFINITY && sum > 0.f);
+              if (again || !__any_sync(0xffffffffu, up)) break;
+              float mx = -INFINITY;
+#pragma unroll
+              for (int j = 0; j < 16; ++j) mx = fmaxf(mx, u[j]);
+              const float was = m == -INFINITY ? 0.f : te - m;
+              const float mn = up ? ceilf(mx - was + te) - C::LIFT : m, al = raise_factor(m, mn);
+              if (c > 0) rescale_p<BF>(ts + 64 * h, c, al);
+              part *= al;
+              m = mn;
+              const float now = m == -INFINITY ? 0.f : te - m;
+#pragma unroll
+              for (int j = 0; j < 16; ++j) u[j] += now - was;
             }
+            part += !PLAIN && spread ? sum_l : sum;
+            tmem_st8(ts + 64 * h + 8 * c, p);
           }
-          float s0, s1;
-          unpack_f32x2(add_f32x2(sum[0], sum[1]), s0, s1);
-          return s0 + s1;
         };
-        auto biggest = [&]() {  // p's largest, of what is packed
-          uint32_t b = 0;
-#pragma unroll
-          for (int j = 0; j < 32; ++j) b = __vmaxu2(b, p[j / 8][j % 8] & 0x7fff7fffu);
-          return max(b & 0xffffu, b >> 16);
-        };
-        float part = 0.f;
-        bool fine = ok;
-        if (busy && ok && ti != first) {
-          part = plain ? probabilities(std::true_type()) : probabilities(std::false_type());
-          // (with exponents of their own the sum does not bound p)
-          fine = spread ? biggest() < (BF ? 0x7f80u : 0x7800u) && (m > -INFINITY || part == 0.f)
-                        : !(part >= kMostSum) && (m > -INFINITY || part == 0.f);
+        if (busy && ok) {
+          if (plain)
+            probabilities(std::true_type());
+          else
+            probabilities(std::false_type());
         }
-        tc_fence_before();
-        if (!sync_stream(fine && ti != first)) {
+        // the halves of a row go by the larger maximum
+        if (!sync_stream(ok && m == m0)) {
           if (sh.sfail[s]) {
             ok = false;
             break;
           }
-          // the maxima of the rows' halves, whole numbers above them, and what was summed with the old ones
-          float mx = -INFINITY;
-          if (busy) {
-#pragma unroll 1
-            for (int c = 0; c < 4; ++c) {
-              float u[16];
-              tmem_ld16(ts + 64 * h + 16 * c, *reinterpret_cast<uint32_t(*)[16]>(&u));
-              tmem_ld_wait16(u);
-              exponents(u, c, te, false);
-#pragma unroll
-              for (int j = 0; j < 16; ++j) mx = fmaxf(mx, u[j]);
-            }
-          }
-          sh.pm[s][h][row] = mx;
+          sh.pm[s][h][row] = m;
           sync_stream(true);
           if (busy) {
-            mx = fmaxf(mx, sh.pm[s][h ^ 1][row]);
-            const float mn = fmaxf(m, ceilf(mx) - C::LIFT), al = raise_factor(m, mn);
-            if (ti != first && __any_sync(0xffffffffu, al != 1.f)) {
-#pragma unroll 1
-              for (int c = 0; c < HD / 32; ++c) {
-                uint32_t o[16];
-                tmem_ld16(to + h * (HD / 2) + 16 * c, o);
-                tmem_ld_wait();
-#pragma unroll
-                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * al);
-                tmem_st16(to + h * (HD / 2) + 16 * c, o);
-              }
+            const float mn = fmaxf(m, sh.pm[s][h ^ 1][row]), al = raise_factor(m, mn), old = raise_factor(m0, mn);
+            if (__any_sync(0xffffffffu, al != 1.f)) {
+              tmem_st_wait();
+              rescale_p<BF>(ts + 64 * h, 4, al);
+              part *= al;
             }
+            if (ti != first && __any_sync(0xffffffffu, old != 1.f)) rescale_o<HD / 32>(to + h * (HD / 2), old);
             m = mn;
-            l *= al;
-            part = probabilities(std::false_type());
+            l *= old;
           }
-          tc_fence_before();
-          sync_stream(true);  // S is read before P takes its place
+          sync_stream(true);  // pm is read
         }
-        tc_fence_after();
         if (busy) {
           l = fmaf(part, BF ? 1.f : pow2i(-ti2), l);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_st8(ts + 32 * h + 8 * c, p[c]);
           tmem_st_wait();
         }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.p_full[s]);
       }
-      if (!ok) break;
 
       // ---- the rows' outputs, or their parts
       if (w.n == 0) {  // not served
@@ -709,6 +743,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
 #pragma unroll 1
           for (int e = 0; e < HD / 16; ++e)
             *reinterpret_cast<uint4 *>(out_row(tok) + h * (HD / 2) + 8 * e) = make_uint4(0, 0, 0, 0);
+        done(turn);
         continue;
       }
       const bool has = first < w.n;
@@ -824,6 +859,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
       }
       T += w.n;
       ++seg;
+      done(turn);
     }
     if (!ok && lane == 0) sh.fail = 1;
   }
