@@ -61,11 +61,6 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
 __device__ __forceinline__ void cp_async4(void *dst, const void *src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_addr(dst)), "l"(src) : "memory");
 }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-
 // How a warp holds 16 positions.  K: lane (gr, tc) takes 16-byte pieces tc, tc + 4, .. of the
 // row in place gr and of that in place gr + 8 (KW words each: half or a quarter of a piece
 // where rows are shorter than 128 bytes).  V: lane (gr, tc) takes pieces gr, gr + 8, .. of the
@@ -258,7 +253,7 @@ __global__ void __launch_bounds__(kWarps * 32, occupancy(HD, BITS, NT)) attn_pag
 
     int stage = 0, into = L::NS - 1;
     for (int k = 0; k < nu; ++k) {
-      cp_async_wait<L::NS - 2>();
+      cp_async_wait_group<L::NS - 2>();
       __syncwarp();
       // (every lane has read what this stage held, the one before)
       copy_unit(k + L::NS - 1, into);

@@ -56,10 +56,11 @@ constexpr int kStream = 128;               // rows of a stream
 constexpr int kBlockRows = 2 * kStream;
 constexpr int kTile = 128;                 // positions a tile
 constexpr int kSoft = 512;                 // softmax threads
-constexpr int kConvWarp = kSoft / 32, kMmaWarp = kConvWarp + 4;
-constexpr int kThreads = 768;               // registers are given to whole groups of 4 warps: 3 of the last are idle
-// registers a thread: the launch's 80 x 768 shared out as 80 x 512 + 96 x 128 + 64 x 128
-constexpr int kRegsSoftmax = 80, kRegsConv = 96, kRegsMma = 64;
+constexpr int kConv = 256;                 // converting threads
+constexpr int kConvWarp = kSoft / 32, kMmaWarp = kConvWarp + kConv / 32;
+constexpr int kThreads = kSoft + kConv + 128;  // the MMA warp, one that plans, and two that registers are allotted with
+// registers a thread: the launch's 72 x 896 shared out as 80 x 512 + 64 x 256 + 56 x 128
+constexpr int kRegsSoftmax = 80, kRegsConv = 64, kRegsMma = 56;
 constexpr int kBlk = kTile * 128;          // bytes of a 64-value block of Q, K or V: [row][128 bytes], swizzled
 constexpr int kTmemCols = 512;             // S / P of the streams 0.., 128..; O 256.., 256 + HD..
 // Queries enter binary16 times 2^7, which keeps a row with its largest |q| in [2^-4, 2^8) whole
@@ -75,9 +76,9 @@ struct Cfg {
   static constexpr int CH = HD / 8;              // 16-byte chunks a row of 16-bit values
   static constexpr int ROW = HD * BITS / 8;
   static constexpr int SMEM = 1024 + 6 * KB;     // Q of both streams, two stages of K and of V
-  // codes: 16-byte pieces a row, pieces of a row in one load of a warp, rows of it; loads of a tile's 64 rows, those in flight
-  static constexpr int PPR = ROW / 16, PP = PPR < 4 ? PPR : 4, RPI = 32 / PP, NI = 64 * PPR / 32, NR = NI < 8 ? NI : 8;
-  static_assert(PPR > 0 && RPI > 0 && NI >= NR, "");
+  // codes: 16-byte pieces a row, pieces of a row in one load of a warp, rows of it, loads a row, loads of a warp's 16 rows
+  static constexpr int PPR = ROW / 16, PP = PPR < 4 ? PPR : 4, RPI = 32 / PP, SPR = PPR / PP, NI = 16 * PPR / 32;
+  static_assert(RPI > 0 && SPR > 0 && NI > 0, "");
   static constexpr float LIFT = BITS == 16 ? 0.f : 6.f;  // of p: small ones are then normal numbers
 };
 
@@ -91,7 +92,7 @@ struct Run {
 };
 
 struct Shared {
-  uint64_t q_full, q_empty, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2];
+  uint64_t q_full, q_empty, top_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2];
   uint64_t run_full[4], run_empty[4];
   Run run[4];
   uint32_t tmem;
@@ -102,8 +103,9 @@ struct Shared {
   __align__(16) float sk[4][kTile];
   int te[4], spread[4];
   __align__(16) float td[4][kTile], tw[4][kTile];
+  __align__(16) uint32_t top[4][8];  // by converting warp: the largest of V's scales (bits), and of 0xffff less them
   float qf[4][kBlockRows];         // what a row's own power of two differs from 2^kQueryShift
-  uint32_t odd[4][2][16];          // of a block, by either V warp: positions from its first masked tile on whose V is not finite
+  uint32_t odd[4][8][16];          // of a block, by converting warp: positions from its first masked tile on whose V is not finite
   float pm[2][2][kStream], pl[2][2][kStream];  // the halves' maxima and sums
 };
 
@@ -244,11 +246,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
   if (warp == kMmaWarp) {
     tmem_alloc(&sh.tmem, kTmemCols);
     if (lane == 0) {
-      mbar_init(&sh.q_full, 4);
+      mbar_init(&sh.q_full, kConv / 32);
       mbar_init(&sh.q_empty, 1);
+      mbar_init(&sh.top_full, kConv / 32);
       for (int i = 0; i < 2; ++i) {
-        mbar_init(&sh.k_full[i], 2);
-        mbar_init(&sh.v_full[i], 2);
+        mbar_init(&sh.k_full[i], kConv / 32);
+        mbar_init(&sh.v_full[i], kConv / 32);
         mbar_init(&sh.k_empty[i], 1);
         mbar_init(&sh.v_empty[i], 1);
         mbar_init(&sh.s_full[i], 1);
@@ -361,15 +364,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
     }
     __syncwarp();
   } else if (warp >= kConvWarp) {
-    // ---- queries, K and V
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsConv));
-    const bool is_v = warp >= kConvWarp + 2;
-    const int ct = tid - 32 * kConvWarp, half = warp & 1;  // a warp has rows 64 half .. of every tile
-    uint8_t *const buf = is_v ? vbuf : kbuf;
-    uint64_t *const full = is_v ? sh.v_full : sh.k_full, *const empty = is_v ? sh.v_empty : sh.k_empty;
-    const uint8_t *const src = reinterpret_cast<const uint8_t *>(is_v ? a.vc : a.kc);
-    const uint32_t *const meta = is_v ? a.vm : a.km;
-    const float qscale = a.scale * pow2i(-kQueryShift);  // of K's scales
+    // ---- queries, K and V: warp cw has rows 16 cw .. of every tile, which lie in one page
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsConv));
+    const int ct = tid - 32 * kConvWarp, cw = ct >> 5;
+    const uint8_t *const kc = reinterpret_cast<const uint8_t *>(a.kc), *const vc = reinterpret_cast<const uint8_t *>(a.vc);
     bool ok = true;
     int T = 0, seg = 0;
     for (int turn = 0; ok; ++turn) {
@@ -380,27 +378,21 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
         done(turn);
         continue;
       }
+      const int n = w.n, len = w.len, p1 = w.t0 * kTile + 16 * cw;  // the warp's first position of the first tile
       const int least = w.least, first_odd = least / kTile * kTile;  // positions from `least` on are not seen by all rows
-      // pages of tile ti: lane l < 8 has that of positions 16 l ..
-      auto load_ids = [&](int ti) {
-        int id = 0;
-        if (lane < 8 && ti < w.n) {
-          id = a.tables[(size_t)w.b * a.max_pages + (min((w.t0 + ti) * kTile + 16 * lane, w.len - 1) >> a.shift)];
-          if (id < 0 || id >= a.n_pages) {
-            id = 0;
-            atomicExch(&g_attn_paged_tc_status, -1);
-          }
+      const int *const table = a.tables + (size_t)w.b * a.max_pages;
+      // the page of the warp's rows of tile ti, and the pool's row of the first (a pool has fewer than 2^32: host check);
+      // rows behind the length are some row of the pool
+      auto load_id = [&](int ti) { return table[min(p1 + ti * kTile, len - 1) >> a.shift]; };
+      auto base_of = [&](int id, int ti) {
+        if ((unsigned)id >= (unsigned)a.n_pages) {
+          id = 0;
+          if (lane == 0) atomicExch(&g_attn_paged_tc_status, -1);
         }
-        return id;
+        return (((uint32_t)id * a.Hkv + w.g) << a.shift) + ((p1 + ti * kTile) & (page - 1));
       };
-      // the pool's row of place r of tile ti (a pool has fewer than 2^32: host check)
-      auto row_at = [&](int ids, int ti, int r) {
-        const int p0 = (w.t0 + ti) * kTile, p = min(p0 + r, w.len - 1);
-        const int id = __shfl_sync(0xffffffffu, ids, (p - p0) >> 4);
-        return (((uint32_t)id * a.Hkv + w.g) << a.shift) + (p & (page - 1));
-      };
-      int ids = load_ids(0), ids_next = load_ids(1);
-      if (is_v && lane < 16) sh.odd[seg & 3][half][lane] = 0;
+      int id0 = load_id(0), id1 = load_id(1), id2 = load_id(2), id3 = load_id(3);
+      if (lane < 16) sh.odd[seg & 3][cw][lane] = 0;
 
       // the block's queries
       if (seg > 0) ok = wait(&sh.q_empty, (seg - 1) & 1);
@@ -409,7 +401,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
         const int c = ct % C::CH;
         const __nv_bfloat16 *q0 = reinterpret_cast<const __nv_bfloat16 *>(a.q) + ((size_t)w.q0 * a.H + w.g * rep) * HD + c * 8;
 #pragma unroll 2
-        for (int r = ct / C::CH; r < (w.live + 31) / 32 * 32; r += 128 / C::CH) {
+        for (int r = ct / C::CH; r < (w.live + 31) / 32 * 32; r += kConv / C::CH) {
           const int row = w.r0 + min(r, w.live - 1), tok = (int)by_rep.divide(row);
           const uint4 v = __ldg(reinterpret_cast<const uint4 *>(q0 + ((size_t)tok * a.H + row - tok * rep) * HD));
           uint4 *dst = reinterpret_cast<uint4 *>(qbuf + (r / kStream) * C::KB + (c / 8) * kBlk + r % kStream * 128 + (((c & 7) ^ (r & 7)) << 4));
@@ -433,156 +425,176 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
       hand_over(&sh.q_full);
 
       if constexpr (BF) {
-        const int lt = ct & 63, c = lt % C::CH, r0 = lt / C::CH;  // 64 threads a tile
-        auto copy = [&](int ti, int st, int id) {
-          const int p0 = (w.t0 + ti) * kTile;
-#pragma unroll 4
-          for (int r = r0; r < kTile; r += 64 / C::CH) {
-            const uint32_t at = row_at(id, ti, r);
-            cp_async16_zfill(buf + st * C::KB + (c / 8) * kBlk + r * 128 + (((c & 7) ^ (r & 7)) << 4), src + (size_t)at * C::ROW + c * 16,
-                             p0 + r < w.len ? 16u : 0u);
-          }
+        // a lane's 16-byte chunks lane, lane + 32, .. of the 16 rows
+        constexpr int NC = 16 * C::CH / 32;
+        auto place = [&](uint8_t *tile, int i) {
+          const int r = (lane + 32 * i) / C::CH, c = lane % C::CH;
+          return tile + (c / 8) * kBlk + (16 * cw + r) * 128 + (((c & 7) ^ (r & 7)) << 4);
+        };
+        auto copy = [&](const uint8_t *src, uint8_t *tile, uint32_t base, int ti) {
+          const uint8_t *p = src + (size_t)base * C::ROW + lane * 16;
+          const int left = len - p1 - ti * kTile;  // rows before the length
+#pragma unroll
+          for (int i = 0; i < NC; ++i) cp_async16_zfill(place(tile, i), p + 512 * i, (lane + 32 * i) / C::CH < left ? 16u : 0u);
           cp_async_commit();
         };
-        auto landed = [&](int ti) {  // this thread's copies of tile ti have landed
-          const int st = (T + ti) & 1, p0 = (w.t0 + ti) * kTile;
-          if (is_v && p0 + kTile > least) {
-            // V's values that are not finite are taken out and noted: what does not see them must not meet them
-            for (int r = r0; r < kTile; r += 64 / C::CH) {
-              uint4 *p = reinterpret_cast<uint4 *>(buf + st * C::KB + (c / 8) * kBlk + r * 128 + (((c & 7) ^ (r & 7)) << 4));
-              const uint4 v = *p;
-              uint32_t x[4] = {v.x, v.y, v.z, v.w};
-              bool odd = false;
+        auto clean = [&](uint8_t *tile, int ti) {
+          // V's values that are not finite are taken out and noted: rows that do not see them must not meet them
+          if ((w.t0 + ti + 1) * kTile <= least) return;
+#pragma unroll 1
+          for (int i = 0; i < NC; ++i) {
+            uint4 *p = reinterpret_cast<uint4 *>(place(tile, i));
+            const uint4 v = *p;
+            uint32_t x[4] = {v.x, v.y, v.z, v.w};
+            bool odd = false;
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                if ((x[e] & 0x7f80u) == 0x7f80u) x[e] &= 0xffff0000u, odd = true;
-                if ((x[e] & 0x7f800000u) == 0x7f800000u) x[e] &= 0xffffu, odd = true;
-              }
-              if (odd) {
-                *p = make_uint4(x[0], x[1], x[2], x[3]);
-                const int at = p0 + r - first_odd;
-                atomicOr(&sh.odd[seg & 3][half][at / 32], 1u << (at % 32));
-              }
+            for (int e = 0; e < 4; ++e) {
+              if ((x[e] & 0x7f80u) == 0x7f80u) x[e] &= 0xffff0000u, odd = true;
+              if ((x[e] & 0x7f800000u) == 0x7f800000u) x[e] &= 0xffffu, odd = true;
+            }
+            if (odd) {
+              *p = make_uint4(x[0], x[1], x[2], x[3]);
+              const int at = p1 + ti * kTile + (lane + 32 * i) / C::CH - first_odd;
+              atomicOr(&sh.odd[seg & 3][cw][at / 32], 1u << (at % 32));
             }
           }
-          hand_over(&full[st]);
         };
-        for (int ti = 0; ti < w.n; ++ti) {
+        for (int ti = 0; ti < n; ++ti) {
           const int st = (T + ti) & 1;
-          if (T + ti >= 2) ok = wait(&empty[st], ((T + ti) >> 1) + 1 & 1);
+          const uint32_t base = base_of(id0, ti);
+          id0 = id1, id1 = id2, id2 = id3;
+          id3 = load_id(ti + 4);
+          if (T + ti >= 2) ok = wait(&sh.k_empty[st], ((T + ti) >> 1) + 1 & 1);
           if (!ok) break;
-          copy(ti, st, ids);
-          ids = ids_next;
-          ids_next = load_ids(ti + 2);
-          if (ti > 0) {
-            cp_async_wait_group1();
-            landed(ti - 1);
+          copy(kc, kbuf + st * C::KB, base, ti);
+          if (ti > 0) {  // K of the tile before has landed, all but the last two groups have
+            cp_async_wait_group<2>();
+            hand_over(&sh.k_full[st ^ 1]);
           }
+          if (T + ti >= 2) ok = wait(&sh.v_empty[st], ((T + ti) >> 1) + 1 & 1);
+          if (!ok) break;
+          copy(vc, vbuf + st * C::KB, base, ti);
+          if (ti > 0) {
+            cp_async_wait_group<2>();
+            clean(vbuf + (st ^ 1) * C::KB, ti - 1);
+            hand_over(&sh.v_full[st ^ 1]);
+          }
+        }
+        const int st = (T + n - 1) & 1;
+        if (ok) {
+          cp_async_wait_group<1>();
+          hand_over(&sh.k_full[st]);
         }
         cp_async_wait_all();
-        if (ok) landed(w.n - 1);
+        if (ok) {
+          clean(vbuf + st * C::KB, n - 1);
+          hand_over(&sh.v_full[st]);
+        }
       } else {
+        const float qscale = a.scale * pow2i(-kQueryShift);  // of K's scales
         const int lr = lane % 8 + 8 * (lane / 8 / C::PP), lp = lane / 8 % C::PP;  // a lane's row and piece of a load
-        uint4 r[C::NR];
-        uint32_t at[C::RPI == 8 ? 8 : 4];  // pool rows of a lane's places 64 half + RPI j + lr
-        uint32_t own[2], vm4[4];
-        auto place = [&](int k) { return 64 * half + C::RPI * (k / (C::PPR / C::PP)) + lr; };
-        auto fetch_rows = [&](int ti, int id) {
+        // where chunk i of the lane's first piece goes (rows 8 further lie 1024 bytes further, and are swizzled alike)
+        constexpr int CPP = BITS == 4 ? 4 : 2;  // 8-value chunks a piece
+        uint32_t to[CPP];
 #pragma unroll
-          for (int j = 0; j < 64 / C::RPI; ++j) at[j] = row_at(id, ti, 64 * half + C::RPI * j + lr);
-        };
-        auto fetch = [&](int k) {
-          return __ldg(reinterpret_cast<const uint4 *>(src + (size_t)at[k / (C::PPR / C::PP)] * C::ROW + 16 * (lp + C::PP * (k % (C::PPR / C::PP)))));
-        };
-        auto fetch_meta = [&](int ti, int id) {
+        for (int i = 0; i < CPP; ++i) {
+          const int c = CPP * lp + i;
+          to[i] = (c / 8) * kBlk + (16 * cw + lr) * 128 + (((c & 7) ^ (lr & 7)) << 4);
+        }
+        uint4 rk[C::NI], rv[C::NI];
+        auto fetch = [&](const uint8_t *src, uint4 (&r)[C::NI], uint32_t base) {
+          const uint8_t *p = src + (size_t)base * C::ROW + lr * C::ROW + lp * 16;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t x = row_at(id, ti, 32 * j + lane);
-            vm4[j] = __ldg(a.vm + x);
-            if (j / 2 == half) own[j % 2] = is_v ? vm4[j] : __ldg(meta + x);
-          }
+          for (int k = 0; k < C::NI; ++k)
+            r[k] = __ldg(reinterpret_cast<const uint4 *>(p + (k / C::SPR) * C::RPI * C::ROW + (k % C::SPR) * C::PP * 16));
         };
-        fetch_rows(0, ids);
-        fetch_meta(0, ids);
-#pragma unroll
-        for (int k = 0; k < C::NR; ++k) r[k] = fetch(k);
-        for (int ti = 0; ti < w.n; ++ti) {
-          const int st = (T + ti) & 1, ring = (T + ti) & 3, p0 = (w.t0 + ti) * kTile;
-          if (T + ti >= 2) ok = wait(&empty[st], ((T + ti) >> 1) + 1 & 1);
+        // lanes 0-15: K's, 16-31: V's scale and zero point of the warp's rows
+        auto fetch_meta = [&](uint32_t base) { return __ldg((lane < 16 ? a.km : a.vm) + base + (lane & 15)); };
+        // the largest and the least of V's scales that the warp has of a tile, for all (a NaN counts as the least)
+        auto publish = [&](uint32_t mv, int ti) {
+          uint32_t v = (mv & 0xffffu) > 0x7c00u ? 0u : mv & 0xffffu;
+          if (v == 0 || mv == kZeroRow) v = 1;  // kLeastScale
+          const bool in = lane >= 16 && p1 + ti * kTile + (lane & 15) < len;
+          const uint32_t hi = __reduce_max_sync(0xffffffffu, in ? v : 0u), lo = __reduce_max_sync(0xffffffffu, in ? 0xffffu - v : 0u);
+          if (lane == 0) sh.top[(T + ti) & 3][cw] = hi << 16 | lo;
+        };
+        uint32_t b0 = base_of(id0, 0), b1 = base_of(id1, 1), b2 = base_of(id2, 2);
+        uint32_t m0 = fetch_meta(b0), m1 = fetch_meta(b1), m2 = fetch_meta(b2), m3 = 0;
+        fetch(kc, rk, b0);
+        fetch(vc, rv, b0);
+        publish(m0, 0);
+        if (n > 1) publish(m1, 1);
+        hand_over(&sh.top_full);
+        ok = wait(&sh.top_full, seg & 1);
+        for (int ti = 0; ti < n && ok; ++ti) {
+          const int st = (T + ti) & 1, ring = (T + ti) & 3, p0 = p1 + ti * kTile;
+          const uint32_t b3 = base_of(id3, ti + 3);
+          m3 = fetch_meta(b3);
+          id3 = load_id(ti + 4);
+          if (T + ti >= 2) ok = wait(&sh.k_empty[st], ((T + ti) >> 1) + 1 & 1);
           if (!ok) break;
-          // V's exponent: the largest scale at 2^5 .., or each row's own where they span too much (a NaN counts as the least)
-          uint32_t lo = 0x7fffu, hi = 0;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            uint32_t v = (vm4[j] & 0xffffu) > 0x7c00u ? 0u : vm4[j] & 0xffffu;
-            if (v == 0 || vm4[j] == kZeroRow) v = 1;  // kLeastScale
-            if (p0 + 32 * j + lane < w.len) lo = min(lo, v), hi = max(hi, v);
-          }
-          lo = __reduce_min_sync(0xffffffffu, lo);
-          hi = __reduce_max_sync(0xffffffffu, hi);
-          auto exponent = [](uint32_t h) { return (int)(__float_as_uint(half_lo(h)) >> 23) - 127 - 5; };
-          const int te = exponent(hi);
-          const bool spread = te - exponent(lo) > kSpread;
-          uint32_t zz[2], sv[2];  // of places 64 half + 32 j + lane: 1024 + z twice; V's scale times 2^-t twice
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const int pl = 64 * half + 32 * j + lane;
-            const bool in = p0 + pl < w.len;
-            const float s0 = half_lo(own[j]);
-            const __half2 z = __hadd2(__half2half2(__ushort_as_half((unsigned short)(in ? own[j] >> 16 : 0u))), __float2half2_rn(1024.f));
-            zz[j] = *reinterpret_cast<const uint32_t *>(&z);
-            sv[j] = 0;
-            if (!is_v) {
-              sh.sk[ring][pl] = s0 * qscale;
-              if (spread) {
-                // (K's warps know V's scales of their rows too)
-                const uint32_t vmj = half ? vm4[2 + j] : vm4[j];
-                float v = half_lo(vmj);
-                if (v == 0.f || vmj == kZeroRow) v = kLeastScale;
-                const int t = min((int)(__float_as_uint(v) >> 23) - 127 - 5, te);
-                sh.td[ring][pl] = (float)t;
-                sh.tw[ring][pl] = pow2i(-t);
-              }
-            } else {
-              float v = s0 == 0.f || own[j] == kZeroRow ? kLeastScale : s0;
-              const int t = spread ? min((int)(__float_as_uint(v) >> 23) - 127 - 5, te) : te;
-              v *= pow2i(-t);
-              if (p0 + kTile > least && in && v != v) {  // a NaN row that not all rows see
-                const int x = p0 + pl - first_odd;
-                atomicOr(&sh.odd[seg & 3][half][x / 32], 1u << (x % 32));
-                v = 0.f;
-              }
-              if (in) sv[j] = pack_h2(v, v);
+          // (every warp has handed over K of the tile two before, and published this one's scales before that)
+          const uint4 t0 = *reinterpret_cast<const uint4 *>(&sh.top[ring][0]), t1 = *reinterpret_cast<const uint4 *>(&sh.top[ring][4]);
+          const uint32_t top = __vmaxu2(__vmaxu2(__vmaxu2(t0.x, t0.y), __vmaxu2(t0.z, t0.w)), __vmaxu2(__vmaxu2(t1.x, t1.y), __vmaxu2(t1.z, t1.w)));
+          auto exponent = [](float s) { return (int)(__float_as_uint(s) >> 23) - 127 - 5; };
+          // V's exponent: the largest scale at 2^5 .., or each row's own where they span too much
+          const int te = exponent(half_lo(top >> 16));
+          const bool spread = te - exponent(half_lo(0xffffu - (top & 0xffffu))) > kSpread;
+          // of the lane's row: 1024 + z; V: its scale times 2^-t too
+          const int pl = lane & 15;
+          const bool in = p0 + pl < len;
+          const float s0 = half_lo(m0);
+          const __half2 z = __hadd2(__half2half2(__ushort_as_half((unsigned short)(in ? m0 >> 16 : 0u))), __float2half2_rn(1024.f));
+          uint32_t zs = *reinterpret_cast<const uint32_t *>(&z);
+          if (lane < 16) {
+            sh.sk[ring][16 * cw + pl] = s0 * qscale;
+          } else {
+            float v = s0 == 0.f || m0 == kZeroRow ? kLeastScale : s0;
+            const int t = spread ? min(exponent(v), te) : te;  // (a NaN's: te)
+            if (spread) sh.td[ring][16 * cw + pl] = (float)t, sh.tw[ring][16 * cw + pl] = pow2i(-t);
+            v *= pow2i(-t);
+            if (p0 - 16 * cw + kTile > least && in && v != v) {  // a NaN row that not all rows see
+              const int x = p0 + pl - first_odd;
+              atomicOr(&sh.odd[seg & 3][cw][x / 32], 1u << (x % 32));
+              v = 0.f;
             }
+            zs = __byte_perm(zs, in ? (uint32_t)__half_as_ushort(__float2half_rn(v)) : 0u, 0x5410);
           }
-          if (!is_v && half == 0 && lane == 0) sh.te[ring] = spread ? 0 : te, sh.spread[ring] = spread;
-          if (ti + 1 < w.n) fetch_meta(ti + 1, ids_next);
-          uint8_t *const to = buf + st * C::KB;
+          if (ct == 0) sh.te[ring] = spread ? 0 : te, sh.spread[ring] = spread;
+          uint8_t *const tk = kbuf + st * C::KB, *const tv = vbuf + st * C::KB;
 #pragma unroll
           for (int k = 0; k < C::NI; ++k) {
-            if (k == C::NI - C::NR) fetch_rows(min(ti + 1, w.n - 1), ti + 1 < w.n ? ids_next : ids);
-            const int pl = place(k);
-            const uint32_t z = C::RPI * (k / (C::PPR / C::PP)) < 32 ? __shfl_sync(0xffffffffu, zz[0], pl & 31) : __shfl_sync(0xffffffffu, zz[1], pl & 31);
-            uint32_t s2 = 0;
-            if (is_v)
-              s2 = C::RPI * (k / (C::PPR / C::PP)) < 32 ? __shfl_sync(0xffffffffu, sv[0], pl & 31) : __shfl_sync(0xffffffffu, sv[1], pl & 31);
-            const uint32_t words[4] = {r[k % C::NR].x, r[k % C::NR].y, r[k % C::NR].z, r[k % C::NR].w};
-            r[k % C::NR] = fetch((k + C::NR) % C::NI);
-            constexpr int CPP = BITS == 4 ? 4 : 2;  // chunks a piece
+            const uint32_t z = __shfl_sync(0xffffffffu, zs, lr + C::RPI * (k / C::SPR));
+            const uint32_t x[4] = {rk[k].x, rk[k].y, rk[k].z, rk[k].w};
+#pragma unroll
+            for (int i = 0; i < CPP; ++i)
+              *reinterpret_cast<uint4 *>(tk + to[i] + (k / C::SPR) * C::RPI * 128 + (k % C::SPR) * (CPP * C::PP / 8) * kBlk) =
+                  convert8<BITS>(BITS == 4 ? make_uint2(x[i], 0) : make_uint2(x[2 * i % 4], x[(2 * i + 1) % 4]), z);
+          }
+          if (ti + 2 < n) publish(m2, ti + 2);
+          hand_over(&sh.k_full[st]);
+          fetch(kc, rk, b1);
+          if (T + ti >= 2) ok = wait(&sh.v_empty[st], ((T + ti) >> 1) + 1 & 1);
+          if (!ok) break;
+#pragma unroll
+          for (int k = 0; k < C::NI; ++k) {
+            const uint32_t both = __shfl_sync(0xffffffffu, zs, 16 + lr + C::RPI * (k / C::SPR));
+            const uint32_t z = __byte_perm(both, 0, 0x1010), s2 = __byte_perm(both, 0, 0x3232);
+            const uint32_t x[4] = {rv[k].x, rv[k].y, rv[k].z, rv[k].w};
 #pragma unroll
             for (int i = 0; i < CPP; ++i) {
-              uint4 o = convert8<BITS>(BITS == 4 ? make_uint2(words[i], 0) : make_uint2(words[2 * i % 4], words[(2 * i + 1) % 4]), z);
-              if (is_v) o.x = hmul2_u(o.x, s2), o.y = hmul2_u(o.y, s2), o.z = hmul2_u(o.z, s2), o.w = hmul2_u(o.w, s2);
-              const int c = CPP * (lp + C::PP * (k % (C::PPR / C::PP))) + i;
-              *reinterpret_cast<uint4 *>(to + (c / 8) * kBlk + pl * 128 + (((c & 7) ^ (pl & 7)) << 4)) = o;
+              uint4 o = convert8<BITS>(BITS == 4 ? make_uint2(x[i], 0) : make_uint2(x[2 * i % 4], x[(2 * i + 1) % 4]), z);
+              o.x = hmul2_u(o.x, s2), o.y = hmul2_u(o.y, s2), o.z = hmul2_u(o.z, s2), o.w = hmul2_u(o.w, s2);
+              *reinterpret_cast<uint4 *>(tv + to[i] + (k / C::SPR) * C::RPI * 128 + (k % C::SPR) * (CPP * C::PP / 8) * kBlk) = o;
             }
           }
-          hand_over(&full[st]);
-          ids = ids_next;
-          ids_next = load_ids(ti + 2);
+          hand_over(&sh.v_full[st]);
+          fetch(vc, rv, b1);
+          m0 = m1, m1 = m2, m2 = m3;
+          b1 = b2, b2 = b3;
         }
       }
-      T += w.n;
+      T += n;
       ++seg;
       done(turn);
     }
@@ -766,7 +778,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
         uint32_t odd = 0;
         if ((w.t0 + w.n) * kTile > least)
 #pragma unroll 1
-          for (int i = 0; i < 32; ++i) odd |= sh.odd[seg & 3][i / 16][i % 16];
+          for (int i = 0; i < 128; ++i) odd |= sh.odd[seg & 3][i / 16][i % 16];
 #pragma unroll 1
         for (int c = 0; c < HD / 64; ++c) {
           float o[32];
@@ -775,7 +787,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
           if (odd != 0) {  // V rows that are not finite, added where they are seen
 #pragma unroll 1
             for (int x = 0; x < 512 && first_odd + x < limit; ++x) {
-              if (((sh.odd[seg & 3][0][x / 32] | sh.odd[seg & 3][1][x / 32]) >> (x % 32) & 1) == 0) continue;
+              if ((sh.odd[seg & 3][x % kTile / 16][x / 32] >> (x % 32) & 1) == 0) continue;
               // (in split blocks the other stream's tiles are the other stream's to add)
               if (w.split && ((first_odd + x) / kTile - w.t0 - first) % 2 != 0) continue;
               const int p = first_odd + x, id = min(max(a.tables[(size_t)w.b * a.max_pages + (p >> a.shift)], 0), a.n_pages - 1);
@@ -894,7 +906,7 @@ cudaError_t launch_t(const AttnPagedArgs &a, int num_sms, cudaStream_t s) {
     // whether the warps' shares of registers fit into what a block is launched with (their exchange would wait forever)
     cudaFuncAttributes f;
     if ((e = cudaFuncGetAttributes(&f, k)) != cudaSuccess) return e;
-    if (kRegsSoftmax * 512 + (kRegsConv + kRegsMma) * 128 > f.numRegs * kThreads) return cudaErrorInvalidConfiguration;
+    if (kRegsSoftmax * kSoft + kRegsConv * kConv + kRegsMma * 128 > f.numRegs * kThreads) return cudaErrorInvalidConfiguration;
     if ((e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) done[dev].store(true, std::memory_order_release);
   }
