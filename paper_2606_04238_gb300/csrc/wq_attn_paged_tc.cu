@@ -16,8 +16,8 @@
 // cp.async; all four the queries of the next block), 20 the MMAs.
 //
 // K's operands are code - z, exact, its scales factors of the scores; V's are (code - z) s 2^-t
-// rounded to binary16, t one for a tile, or, where a tile's scales span more than 2^8, one
-// for each row, taken into its score.  The maximum is not searched in every tile: p is taken
+// rounded to binary16, t one for 16 positions, or, where their scales span more than 2^8, one for
+// each, taken into the score.  The maximum is not searched in every tile: p is taken
 // with the maximum that the row has, which is raised, and what was computed with it rescaled in
 // TMEM by a power of two, only where 16 p add up to 2^15 (p is 2^6 at most where it is raised).
 //
@@ -66,7 +66,8 @@ constexpr int kTmemCols = 512;             // S / P of the streams 0.., 128..; O
 // Queries enter binary16 times 2^7, which keeps a row with its largest |q| in [2^-4, 2^8) whole
 // but for values below 2^-27 of that; other rows by a power of two of their own.
 constexpr int kQueryShift = 7;
-constexpr int kSpread = 8;                 // exponents that V's scales of a tile may span with one power of two for all
+constexpr int kSpread = 8;                 // exponents that V's scales of 16 positions may span with one power of two for all
+constexpr int kOwn = 1 << 16;
 constexpr float kMostSum = 32768.f;        // of 16 p; binary16 ends at 65504
 
 template <int HD, int BITS>
@@ -92,20 +93,20 @@ struct Run {
 };
 
 struct Shared {
-  uint64_t q_full, q_empty, top_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2];
+  uint64_t q_full, q_empty, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2];
   uint64_t run_full[4], run_empty[4];
   Run run[4];
   uint32_t tmem;
   int fail, sfail[2], last;
   // of a tile, four tiles deep (a tile's are written when S of the one two before is done, whose softmax has then
-  // ended for the tile four before): K's scales times the score scale and 2^-kQueryShift, V's exponent t, whether its
-  // rows have their own, and those
+  // ended for the tile four before): K's scales times the score scale and 2^-kQueryShift, V's exponents t
   __align__(16) float sk[4][kTile];
-  int te[4], spread[4];
+  __align__(16) int te[4][8];  // by 16 positions; kOwn: their rows have their own
   __align__(16) float td[4][kTile], tw[4][kTile];
-  __align__(16) uint32_t top[4][8];  // by converting warp: the largest of V's scales (bits), and of 0xffff less them
   float qf[4][kBlockRows];         // what a row's own power of two differs from 2^kQueryShift
-  uint32_t odd[4][8][16];          // of a block, by converting warp: positions from its first masked tile on whose V is not finite
+  // of a block, by converting warp: positions from its first masked tile on (384 at most) whose V is not finite, and whether
+  // there are any
+  uint32_t odd[4][8][16];
   float pm[2][2][kStream], pl[2][2][kStream];  // the halves' maxima and sums
 };
 
@@ -230,6 +231,24 @@ __device__ __noinline__ void rescale_o(uint32_t at, float al) {
   }
 }
 
+// Lane `at` of four has v[i], 16 bytes i of its row: after, 16 bytes `at` of the rows of lane i.
+__device__ __forceinline__ void transpose4(uint4 (&v)[4], int at) {
+  auto swap = [](uint4 &a, uint4 &b, bool up, int by) {  // a of the upper lane for b of the lower one
+    const uint4 give = up ? a : b;
+    uint4 got;
+    got.x = __shfl_xor_sync(0xffffffffu, give.x, by), got.y = __shfl_xor_sync(0xffffffffu, give.y, by);
+    got.z = __shfl_xor_sync(0xffffffffu, give.z, by), got.w = __shfl_xor_sync(0xffffffffu, give.w, by);
+    if (up)
+      a = got;
+    else
+      b = got;
+  };
+  swap(v[0], v[1], at & 1, 1);
+  swap(v[2], v[3], at & 1, 1);
+  swap(v[0], v[2], at & 2, 2);
+  swap(v[1], v[3], at & 2, 2);
+}
+
 __device__ __forceinline__ float half_lo(uint32_t m) { return __half2float(__ushort_as_half((unsigned short)(m & 0xffffu))); }
 
 }  // namespace
@@ -248,7 +267,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
     if (lane == 0) {
       mbar_init(&sh.q_full, kConv / 32);
       mbar_init(&sh.q_empty, 1);
-      mbar_init(&sh.top_full, kConv / 32);
       for (int i = 0; i < 2; ++i) {
         mbar_init(&sh.k_full[i], kConv / 32);
         mbar_init(&sh.v_full[i], kConv / 32);
@@ -379,7 +397,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
         continue;
       }
       const int n = w.n, len = w.len, p1 = w.t0 * kTile + 16 * cw;  // the warp's first position of the first tile
-      const int least = w.least, first_odd = least / kTile * kTile;  // positions from `least` on are not seen by all rows
+      const int first_odd = w.least / kTile * kTile;  // positions from w.least on are not seen by all rows
       const int *const table = a.tables + (size_t)w.b * a.max_pages;
       // the page of the warp's rows of tile ti, and the pool's row of the first (a pool has fewer than 2^32: host check);
       // rows behind the length are some row of the pool
@@ -391,7 +409,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
         }
         return (((uint32_t)id * a.Hkv + w.g) << a.shift) + ((p1 + ti * kTile) & (page - 1));
       };
-      int id0 = load_id(0), id1 = load_id(1), id2 = load_id(2), id3 = load_id(3);
+      int id0 = load_id(0), id1 = load_id(1);
       if (lane < 16) sh.odd[seg & 3][cw][lane] = 0;
 
       // the block's queries
@@ -440,7 +458,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
         };
         auto clean = [&](uint8_t *tile, int ti) {
           // V's values that are not finite are taken out and noted: rows that do not see them must not meet them
-          if ((w.t0 + ti + 1) * kTile <= least) return;
+          if ((w.t0 + ti + 1) * kTile <= w.least) return;
 #pragma unroll 1
           for (int i = 0; i < NC; ++i) {
             uint4 *p = reinterpret_cast<uint4 *>(place(tile, i));
@@ -456,14 +474,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
               *p = make_uint4(x[0], x[1], x[2], x[3]);
               const int at = p1 + ti * kTile + (lane + 32 * i) / C::CH - first_odd;
               atomicOr(&sh.odd[seg & 3][cw][at / 32], 1u << (at % 32));
+              sh.odd[seg & 3][cw][15] = 1;
             }
           }
         };
         for (int ti = 0; ti < n; ++ti) {
           const int st = (T + ti) & 1;
           const uint32_t base = base_of(id0, ti);
-          id0 = id1, id1 = id2, id2 = id3;
-          id3 = load_id(ti + 4);
+          id0 = id1;
+          id1 = load_id(ti + 2);
           if (T + ti >= 2) ok = wait(&sh.k_empty[st], ((T + ti) >> 1) + 1 & 1);
           if (!ok) break;
           copy(kc, kbuf + st * C::KB, base, ti);
@@ -510,42 +529,31 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
         };
         // lanes 0-15: K's, 16-31: V's scale and zero point of the warp's rows
         auto fetch_meta = [&](uint32_t base) { return __ldg((lane < 16 ? a.km : a.vm) + base + (lane & 15)); };
-        // the largest and the least of V's scales that the warp has of a tile, for all (a NaN counts as the least)
-        auto publish = [&](uint32_t mv, int ti) {
-          uint32_t v = (mv & 0xffffu) > 0x7c00u ? 0u : mv & 0xffffu;
-          if (v == 0 || mv == kZeroRow) v = 1;  // kLeastScale
-          const bool in = lane >= 16 && p1 + ti * kTile + (lane & 15) < len;
-          const uint32_t hi = __reduce_max_sync(0xffffffffu, in ? v : 0u), lo = __reduce_max_sync(0xffffffffu, in ? 0xffffu - v : 0u);
-          if (lane == 0) sh.top[(T + ti) & 3][cw] = hi << 16 | lo;
-        };
-        uint32_t b0 = base_of(id0, 0), b1 = base_of(id1, 1), b2 = base_of(id2, 2);
-        uint32_t m0 = fetch_meta(b0), m1 = fetch_meta(b1), m2 = fetch_meta(b2), m3 = 0;
-        fetch(kc, rk, b0);
-        fetch(vc, rv, b0);
-        publish(m0, 0);
-        if (n > 1) publish(m1, 1);
-        hand_over(&sh.top_full);
-        ok = wait(&sh.top_full, seg & 1);
-        for (int ti = 0; ti < n && ok; ++ti) {
+        uint32_t m0, b1 = base_of(id0, 0);
+        m0 = fetch_meta(b1);
+        fetch(kc, rk, b1);
+        fetch(vc, rv, b1);
+        for (int ti = 0; ti < n; ++ti) {
           const int st = (T + ti) & 1, ring = (T + ti) & 3, p0 = p1 + ti * kTile;
-          const uint32_t b3 = base_of(id3, ti + 3);
-          m3 = fetch_meta(b3);
-          id3 = load_id(ti + 4);
-          if (T + ti >= 2) ok = wait(&sh.k_empty[st], ((T + ti) >> 1) + 1 & 1);
-          if (!ok) break;
-          // (every warp has handed over K of the tile two before, and published this one's scales before that)
-          const uint4 t0 = *reinterpret_cast<const uint4 *>(&sh.top[ring][0]), t1 = *reinterpret_cast<const uint4 *>(&sh.top[ring][4]);
-          const uint32_t top = __vmaxu2(__vmaxu2(__vmaxu2(t0.x, t0.y), __vmaxu2(t0.z, t0.w)), __vmaxu2(__vmaxu2(t1.x, t1.y), __vmaxu2(t1.z, t1.w)));
+          b1 = base_of(id1, ti + 1);
+          const uint32_t m1 = fetch_meta(b1);
+          id1 = load_id(ti + 2);
+          // V's exponent: the largest scale at 2^5 .., or each row's own where they span too much (a NaN counts as the least)
+          uint32_t v = (m0 & 0xffffu) > 0x7c00u ? 0u : m0 & 0xffffu;
+          if (v == 0 || m0 == kZeroRow) v = 1;  // kLeastScale
+          const bool in = p0 + (lane & 15) < len;
+          const uint32_t hi = __reduce_max_sync(0xffffffffu, lane >= 16 && in ? v : 1u);
+          const uint32_t lo = __reduce_min_sync(0xffffffffu, lane >= 16 && in ? v : 0x7c00u);
           auto exponent = [](float s) { return (int)(__float_as_uint(s) >> 23) - 127 - 5; };
-          // V's exponent: the largest scale at 2^5 .., or each row's own where they span too much
-          const int te = exponent(half_lo(top >> 16));
-          const bool spread = te - exponent(half_lo(0xffffu - (top & 0xffffu))) > kSpread;
+          const int te = exponent(half_lo(hi));
+          const bool spread = te - exponent(half_lo(lo)) > kSpread;
           // of the lane's row: 1024 + z; V: its scale times 2^-t too
           const int pl = lane & 15;
-          const bool in = p0 + pl < len;
           const float s0 = half_lo(m0);
           const __half2 z = __hadd2(__half2half2(__ushort_as_half((unsigned short)(in ? m0 >> 16 : 0u))), __float2half2_rn(1024.f));
           uint32_t zs = *reinterpret_cast<const uint32_t *>(&z);
+          if (T + ti >= 2) ok = wait(&sh.k_empty[st], ((T + ti) >> 1) + 1 & 1);
+          if (!ok) break;
           if (lane < 16) {
             sh.sk[ring][16 * cw + pl] = s0 * qscale;
           } else {
@@ -553,14 +561,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
             const int t = spread ? min(exponent(v), te) : te;  // (a NaN's: te)
             if (spread) sh.td[ring][16 * cw + pl] = (float)t, sh.tw[ring][16 * cw + pl] = pow2i(-t);
             v *= pow2i(-t);
-            if (p0 - 16 * cw + kTile > least && in && v != v) {  // a NaN row that not all rows see
+            if (in && v != v && p0 - 16 * cw + kTile > w.least) {  // a NaN row that not all rows see
               const int x = p0 + pl - first_odd;
               atomicOr(&sh.odd[seg & 3][cw][x / 32], 1u << (x % 32));
+              sh.odd[seg & 3][cw][15] = 1;
               v = 0.f;
             }
             zs = __byte_perm(zs, in ? (uint32_t)__half_as_ushort(__float2half_rn(v)) : 0u, 0x5410);
           }
-          if (ct == 0) sh.te[ring] = spread ? 0 : te, sh.spread[ring] = spread;
+          if (lane == 0) sh.te[ring][cw] = spread ? kOwn : te;
           uint8_t *const tk = kbuf + st * C::KB, *const tv = vbuf + st * C::KB;
 #pragma unroll
           for (int k = 0; k < C::NI; ++k) {
@@ -571,7 +580,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
               *reinterpret_cast<uint4 *>(tk + to[i] + (k / C::SPR) * C::RPI * 128 + (k % C::SPR) * (CPP * C::PP / 8) * kBlk) =
                   convert8<BITS>(BITS == 4 ? make_uint2(x[i], 0) : make_uint2(x[2 * i % 4], x[(2 * i + 1) % 4]), z);
           }
-          if (ti + 2 < n) publish(m2, ti + 2);
           hand_over(&sh.k_full[st]);
           fetch(kc, rk, b1);
           if (T + ti >= 2) ok = wait(&sh.v_empty[st], ((T + ti) >> 1) + 1 & 1);
@@ -590,8 +598,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
           }
           hand_over(&sh.v_full[st]);
           fetch(vc, rv, b1);
-          m0 = m1, m1 = m2, m2 = m3;
-          b1 = b2, b2 = b3;
+          m0 = m1;
         }
       }
       T += n;
@@ -634,13 +641,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
           c1 = BF ? a.scale : in ? sh.qf[seg & 3][lr] : 1.f;
           own = !BF && __any_sync(0xffffffffu, c1 != 1.f);
         }
-        const bool spread = !BF && sh.spread[ring] != 0;
-        const int ti2 = BF ? 0 : sh.te[ring];
-        const float te = (float)ti2;
+        // V's exponents of the half's four times 16 positions
         const bool some = p0 + 64 > seen_by_all;
-        const bool plain = !some && !spread && !own;
+        bool plain = !some && !own;
+        if constexpr (!BF) {
+          const int4 te4 = *reinterpret_cast<const int4 *>(&sh.te[ring][4 * h]);
+          plain = plain && max(max(te4.x, te4.y), max(te4.z, te4.w)) < kOwn;
+        }
         // u = the scores of columns 16 c .. (raw in u) plus ms (and V's exponents), -inf where they are not seen
-        auto exponents = [&](float (&u)[16], int c, float ms, bool plain) {
+        auto exponents = [&](float (&u)[16], int c, float ms, bool spread, bool plain) {
           const uint64_t mm = pack_f32x2(ms, ms), cc = pack_f32x2(c1, c1);
           if (!BF && !plain && own)
 #pragma unroll
@@ -665,7 +674,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
             for (int j = 0; j < 16; ++j) u[j] = j < n ? u[j] : -INFINITY;
           }
         };
-        // The half row's p with maximum m, into the columns whose scores have been read; their sum, in units of 2^-te.
+        // The half row's p with maximum m, into the columns whose scores have been read, and their sum (p stands for 2^-t).
         // 16 columns at a time: where those add up to kMostSum (or there is no maximum yet) m is raised first, to a whole
         // number, so that what has been computed with the old one is rescaled by an exact power of two.
         const float m0 = m;
@@ -674,12 +683,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
           constexpr bool PLAIN = decltype(is_plain)::value;
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
-            float u[16], sum = 0.f, sum_l = 0.f;
+            float u[16];
+            float sum = 0.f, sum_l = 0.f;
             uint32_t p[8];
             tmem_ld16(ts + 64 * h + 16 * c, *reinterpret_cast<uint32_t(*)[16]>(&u));
             tmem_ld_wait16(u);
-            const float ms = m == -INFINITY ? 0.f : te - m;
-            exponents(u, c, ms, PLAIN);
+            const int t = BF ? 0 : sh.te[ring][4 * h + c];
+            const bool spread = !PLAIN && t == kOwn;
+            const float te = spread ? 0.f : (float)t, ms = m == -INFINITY ? 0.f : te - m;
+            exponents(u, c, ms, spread, PLAIN);
 #pragma unroll 1
             for (int again = 0; again < 2; ++again) {
               uint64_t s2[2] = {0, 0};
@@ -689,7 +701,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
                 const float e0 = ex2(u[j]), e1 = ex2(u[j + 1]);
                 p[j / 2] = BF ? pack_bf2(e0, e1) : pack_h2(e0, e1);
                 s2[j / 2 % 2] = add_f32x2(s2[j / 2 % 2], pack_f32x2(e0, e1));
-                if (!PLAIN && spread)
+                if (spread)
                   sum_l += fmaf(e0, sh.tw[ring][64 * h + 16 * c + j], e1 * sh.tw[ring][64 * h + 16 * c + j + 1]);
               }
               float x, y;
@@ -709,7 +721,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
 #pragma unroll
               for (int j = 0; j < 16; ++j) u[j] += now - was;
             }
-            part += !PLAIN && spread ? sum_l : sum;
+            part = spread ? part + sum_l : BF ? part + sum : fmaf(sum, pow2i(-t), part);
             tmem_st8(ts + 64 * h + 8 * c, p);
           }
         };
@@ -741,7 +753,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
           sync_stream(true);  // pm is read
         }
         if (busy) {
-          l = fmaf(part, BF ? 1.f : pow2i(-ti2), l);
+          l += part;
           tmem_st_wait();
         }
         tc_fence_before();
@@ -778,7 +790,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
         uint32_t odd = 0;
         if ((w.t0 + w.n) * kTile > least)
 #pragma unroll 1
-          for (int i = 0; i < 128; ++i) odd |= sh.odd[seg & 3][i / 16][i % 16];
+          for (int i = 0; i < 8; ++i) odd |= sh.odd[seg & 3][i][15];
 #pragma unroll 1
         for (int c = 0; c < HD / 64; ++c) {
           float o[32];
@@ -786,7 +798,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
           tmem_ld_wait();
           if (odd != 0) {  // V rows that are not finite, added where they are seen
 #pragma unroll 1
-            for (int x = 0; x < 512 && first_odd + x < limit; ++x) {
+            for (int x = 0; x < 384 && first_odd + x < limit; ++x) {
               if ((sh.odd[seg & 3][x % kTile / 16][x / 32] >> (x % 32) & 1) == 0) continue;
               // (in split blocks the other stream's tiles are the other stream's to add)
               if (w.split && ((first_odd + x) / kTile - w.t0 - first) % 2 != 0) continue;
@@ -800,19 +812,36 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
               }
             }
           }
-          if (!in) continue;
+          // four lanes write 64 bytes of a row together: lane i of four has rows i' = 0 .. 3's 16 bytes i
+          const int quad = lane & ~3, at = lane & 3;
           if (alone) {
-            __nv_bfloat16 *dst = out_row(tok) + h * (HD / 2) + 32 * c;
+            uint4 v[4];
 #pragma unroll
             for (int e = 0; e < 32; e += 8)
-              *reinterpret_cast<uint4 *>(dst + e) =
-                  none ? make_uint4(0, 0, 0, 0)
-                       : make_uint4(pack_bf2(o[e] * inv, o[e + 1] * inv), pack_bf2(o[e + 2] * inv, o[e + 3] * inv),
-                                    pack_bf2(o[e + 4] * inv, o[e + 5] * inv), pack_bf2(o[e + 6] * inv, o[e + 7] * inv));
+              v[e / 8] = none ? make_uint4(0, 0, 0, 0)
+                              : make_uint4(pack_bf2(o[e] * inv, o[e + 1] * inv), pack_bf2(o[e + 2] * inv, o[e + 3] * inv),
+                                           pack_bf2(o[e + 4] * inv, o[e + 5] * inv), pack_bf2(o[e + 6] * inv, o[e + 7] * inv));
+            transpose4(v, at);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int other = lr - at + i, ot = __shfl_sync(0xffffffffu, tok, quad + i);
+              if (other < w.live)
+                *reinterpret_cast<uint4 *>(out_row(ot) + (ptrdiff_t)(other - lr) * HD + h * (HD / 2) + 32 * c + 8 * at) = v[i];
+            }
           } else {
 #pragma unroll
-            for (int e = 0; e < 32; e += 4)
-              *reinterpret_cast<float4 *>(pt + h * (HD / 2) + 32 * c + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+            for (int k = 0; k < 2; ++k) {
+              uint4 v[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                v[e] = make_uint4(__float_as_uint(o[16 * k + 4 * e]), __float_as_uint(o[16 * k + 4 * e + 1]),
+                                  __float_as_uint(o[16 * k + 4 * e + 2]), __float_as_uint(o[16 * k + 4 * e + 3]));
+              transpose4(v, at);
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (lr - at + i < w.live)
+                  *reinterpret_cast<uint4 *>(pt + (i - at) * (HD + 4) + h * (HD / 2) + 32 * c + 16 * k + 4 * at) = v[i];
+            }
           }
         }
       }
@@ -832,40 +861,46 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
           // all parts of the block in their order: CTA c0 has its begin (in its place 1), the others their first blocks
           // (0); a split block's streams one after the other
           __threadfence();
-          constexpr int LPR = HD / 4, CU = 4;
+          constexpr int LPR = HD / 4, RU = 4, STEP = kSoft / LPR;  // lanes a row, rows of a thread in flight
           const int e = 4 * (tid % LPR), subs = w.split ? 2 : 1, parts = (cl - c0 + 1) * subs;
-          for (int r = tid / LPR; r < w.live; r += kSoft / LPR) {
-            float M = -INFINITY, S = 0.f;
-            float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int k0 = 0; k0 < parts; k0 += CU) {
-              float2 ml[CU];
-              float4 ov[CU];
-              float mn = M;
+#pragma unroll 1
+          for (int r = tid / LPR; r < w.live; r += RU * STEP) {
+            float M[RU], S[RU];
+            float4 O[RU];
 #pragma unroll
-              for (int j = 0; j < CU; ++j) {
-                const int k = k0 + j, cta = k / subs, sub = k % subs;
-                const float *ps = a.part + (((size_t)(c0 + cta) * 2 + (cta == 0)) * kBlockRows + sub * kStream + r) * (HD + 4);
-                const bool there = k < parts;
-                ml[j] = there ? __ldcg(reinterpret_cast<const float2 *>(ps + HD)) : make_float2(-INFINITY, 0.f);
-                ov[j] = there ? __ldcg(reinterpret_cast<const float4 *>(ps + e)) : make_float4(0.f, 0.f, 0.f, 0.f);
-                mn = fmaxf(mn, ml[j].x);
+            for (int j = 0; j < RU; ++j) M[j] = -INFINITY, S[j] = 0.f, O[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+            for (int k = 0; k < parts; ++k) {
+              const int cta = k / subs, sub = k % subs;
+              const float *ps = a.part + (((size_t)(c0 + cta) * 2 + (cta == 0)) * kBlockRows + sub * kStream + r) * (HD + 4);
+              float2 ml[RU];
+              float4 ov[RU];
+#pragma unroll
+              for (int j = 0; j < RU; ++j) {
+                const bool there = r + j * STEP < w.live;
+                ml[j] = there ? __ldcg(reinterpret_cast<const float2 *>(ps + (size_t)j * STEP * (HD + 4) + HD)) : make_float2(-INFINITY, 0.f);
+                ov[j] = there ? __ldcg(reinterpret_cast<const float4 *>(ps + (size_t)j * STEP * (HD + 4) + e)) : make_float4(0.f, 0.f, 0.f, 0.f);
               }
-              const float f0 = M == -INFINITY ? 0.f : ex2(M - mn);
-              M = mn;
-              S *= f0;
-              O.x *= f0, O.y *= f0, O.z *= f0, O.w *= f0;
 #pragma unroll
-              for (int j = 0; j < CU; ++j) {
+              for (int j = 0; j < RU; ++j) {
                 if (ml[j].x == -INFINITY && ml[j].y == 0.f) continue;  // (its values were not written)
-                const float f = ml[j].x == -INFINITY ? 0.f : ex2(ml[j].x - M);  // (a NaN of a part stays NaN)
-                S = fmaf(ml[j].y, f, S);
-                O.x = fmaf(ov[j].x, f, O.x), O.y = fmaf(ov[j].y, f, O.y), O.z = fmaf(ov[j].z, f, O.z), O.w = fmaf(ov[j].w, f, O.w);
+                const float mn = fmaxf(M[j], ml[j].x);
+                const float f0 = M[j] == -INFINITY ? 0.f : ex2(M[j] - mn);
+                const float f = ml[j].x == -INFINITY ? 0.f : ex2(ml[j].x - mn);  // (a NaN of a part stays NaN)
+                M[j] = mn;
+                S[j] = fmaf(ml[j].y, f, S[j] * f0);
+                O[j].x = fmaf(ov[j].x, f, O[j].x * f0), O[j].y = fmaf(ov[j].y, f, O[j].y * f0);
+                O[j].z = fmaf(ov[j].z, f, O[j].z * f0), O[j].w = fmaf(ov[j].w, f, O[j].w * f0);
               }
             }
-            const bool nothing = M == -INFINITY && S == 0.f;
-            const int rr = w.r0 + r, t = (int)by_rep.divide(rr);
-            *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(a.o) + ((size_t)(w.q0 + t) * a.H + w.g * rep + rr - t * rep) * HD + e) =
-                nothing ? make_uint2(0, 0) : make_uint2(pack_bf2(O.x / S, O.y / S), pack_bf2(O.z / S, O.w / S));
+#pragma unroll
+            for (int j = 0; j < RU; ++j) {
+              const int rr = w.r0 + r + j * STEP, t = (int)by_rep.divide(rr);
+              if (r + j * STEP >= w.live) break;
+              const bool nothing = M[j] == -INFINITY && S[j] == 0.f;
+              *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(a.o) + ((size_t)(w.q0 + t) * a.H + w.g * rep + rr - t * rep) * HD + e) =
+                  nothing ? make_uint2(0, 0) : make_uint2(pack_bf2(O[j].x / S[j], O[j].y / S[j]), pack_bf2(O[j].z / S[j], O[j].w / S[j]));
+            }
           }
         }
       }
