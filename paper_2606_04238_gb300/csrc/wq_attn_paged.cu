@@ -98,7 +98,7 @@ __device__ __forceinline__ Item get_item(const AttnPagedArgs &a, int b, int rep,
 template <int HD, int BITS, int NT>
 __global__ void __launch_bounds__(kWarps * 32, occupancy(HD, BITS, NT)) attn_paged_kernel(const AttnPagedArgs a) {
   using L = Lay<HD, BITS>;
-  constexpr int ROWS = 8 * NT, OS = HD + 4;
+  constexpr int ROWS = 8 * NT, OS = HD + 4, PS = HD + 4;  // (a part's row: its sums, maximum and sum of p)
   extern __shared__ __align__(128) uint8_t paged_ring[];
   __shared__ float sm[kWarps][ROWS], sl[kWarps][ROWS];
   __shared__ int last;
@@ -464,62 +464,83 @@ __global__ void __launch_bounds__(kWarps * 32, occupancy(HD, BITS, NT)) attn_pag
       }
     __syncthreads();
     const bool whole = blk0 == 0 && blk1 == s.blocks;
-    // the CTAs that share the item: c0 has its begin (in its place 1), the others their first blocks (0)
-    const long long c0 = ((item + 1) * N - 1) / total, cl = ((item + s.blocks) * N - 1) / total;
-    for (int i = tid; i < ROWS * HD / 2; i += kWarps * 32) {
-      const int r = i / (HD / 2), e = 2 * (i % (HD / 2)), row = r0 + r;
-      if (row >= R) break;
-      float M = -INFINITY, Ls = 0.f, O0 = 0.f, O1 = 0.f;
+    // the warps' results added up in their order: the rows' outputs, or this CTA's part of them
+    auto add_up = [&](bool all, float *part) {
+      for (int i = tid; i < ROWS * HD / 2; i += kWarps * 32) {
+        const int r = i / (HD / 2), e = 2 * (i % (HD / 2)), row = r0 + r;
+        if (row >= R) break;
+        float M = -INFINITY, Ls = 0.f, O0 = 0.f, O1 = 0.f;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) M = fmaxf(M, sm[w][r]);
+        for (int w = 0; w < kWarps; ++w) M = fmaxf(M, sm[w][r]);
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const float f = sm[w][r] == -INFINITY ? 0.f : ex2(sm[w][r] - M);
-        Ls = fmaf(sl[w][r], f, Ls);
-        O0 = fmaf(so[w][r][e], f, O0);
-        O1 = fmaf(so[w][r][e + 1], f, O1);
-      }
-      if (whole) {
-        const bool none = M == -INFINITY && Ls == 0.f;
-        *reinterpret_cast<uint32_t *>(reinterpret_cast<__nv_bfloat16 *>(a.o) +
-                                      ((size_t)(s.q0 + row / rep) * a.H + g * rep + row % rep) * HD + e) =
-            none ? 0u : pack_bf2(O0 / Ls, O1 / Ls);
-      } else {
-        float *pt = a.part + (((size_t)c * 2 + (blk0 == 0)) * kMostRows + r) * (HD + 2);
-        *reinterpret_cast<float2 *>(pt + e) = make_float2(O0, O1);
-        if (e == 0) *reinterpret_cast<float2 *>(pt + HD) = make_float2(M, Ls);
-      }
-    }
-    if (!whole) {
-      __threadfence();
-      __syncthreads();
-      if (tid == 0) {
-        const int all = (int)(cl - c0 + 1);
-        last = atomicAdd(&a.counters[c0], 1) == all - 1;
-        if (last) a.counters[c0] = 0;
-      }
-      __syncthreads();
-      if (last) {
-        __threadfence();
-        for (int i = tid; i < ROWS * HD / 2; i += kWarps * 32) {
-          const int r = i / (HD / 2), e = 2 * (i % (HD / 2)), row = r0 + r;
-          if (row >= R) break;
-          float M = -INFINITY, Ls = 0.f, O0 = 0.f, O1 = 0.f;
-          for (long long k = c0; k <= cl; ++k) {
-            const float *pt = a.part + (((size_t)k * 2 + (k == c0)) * kMostRows + r) * (HD + 2);
-            const float2 ov = __ldcg(reinterpret_cast<const float2 *>(pt + e)), ml = __ldcg(reinterpret_cast<const float2 *>(pt + HD));
-            const float mn = fmaxf(M, ml.x);
-            const float f0 = M == -INFINITY ? 0.f : ex2(M - mn), f1 = ml.x == -INFINITY ? 0.f : ex2(ml.x - mn);
-            M = mn;
-            Ls = fmaf(ml.y, f1, Ls * f0);
-            O0 = fmaf(ov.x, f1, O0 * f0);
-            O1 = fmaf(ov.y, f1, O1 * f0);
-          }
+        for (int w = 0; w < kWarps; ++w) {
+          const float f = sm[w][r] == -INFINITY ? 0.f : ex2(sm[w][r] - M);
+          Ls = fmaf(sl[w][r], f, Ls);
+          O0 = fmaf(so[w][r][e], f, O0);
+          O1 = fmaf(so[w][r][e + 1], f, O1);
+        }
+        if (all) {
           const bool none = M == -INFINITY && Ls == 0.f;
           *reinterpret_cast<uint32_t *>(reinterpret_cast<__nv_bfloat16 *>(a.o) +
                                         ((size_t)(s.q0 + row / rep) * a.H + g * rep + row % rep) * HD + e) =
               none ? 0u : pack_bf2(O0 / Ls, O1 / Ls);
+        } else {
+          float *pt = part + (size_t)r * PS;
+          *reinterpret_cast<float2 *>(pt + e) = make_float2(O0, O1);
+          if (e == 0) *reinterpret_cast<float2 *>(pt + HD) = make_float2(M, Ls);
         }
+      }
+    };
+    // of the CTAs that share the item, c0 has its begin (in its place 1), the others their first blocks (0)
+    auto part_of = [&](long long cta, bool begin) { return a.part + ((size_t)cta * 2 + begin) * kMostRows * PS; };
+    add_up(whole, part_of(c, blk0 == 0));
+    if (!whole) {
+      const int c0 = (int)(((item + 1) * N - 1) / total), parts = (int)(((item + s.blocks) * N - 1) / total) - c0 + 1;
+      __threadfence();
+      __syncthreads();
+      if (tid == 0) {
+        last = atomicAdd(&a.counters[c0], 1) == parts - 1;
+        if (last) a.counters[c0] = 0;
+      }
+      __syncthreads();
+      if (last) {
+        // all parts: warp w adds up w, w + 4, .. in order, a row's HD / 4 lanes 16 bytes each, then the warps in order
+        __threadfence();
+        constexpr int LPR = HD / 4, RPW = 32 / LPR, CU = 8;
+        const int e = 4 * (lane % LPR);
+        for (int rr = 0; rr < min(ROWS, R - r0); rr += RPW) {
+          const int r = min(rr + lane / LPR, ROWS - 1);
+          float M = -INFINITY, Ls = 0.f;
+          float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int k0 = warp; k0 < parts; k0 += CU * kWarps) {
+            float2 ml[CU];
+            float4 ov[CU];
+            float mn = M;
+#pragma unroll
+            for (int j = 0; j < CU; ++j) {
+              const int k = k0 + j * kWarps;
+              const float *pt = part_of(c0 + min(k, parts - 1), k == 0) + (size_t)r * PS;
+              ml[j] = k < parts ? __ldcg(reinterpret_cast<const float2 *>(pt + HD)) : make_float2(-INFINITY, 0.f);
+              ov[j] = k < parts ? __ldcg(reinterpret_cast<const float4 *>(pt + e)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int j = 0; j < CU; ++j) mn = fmaxf(mn, ml[j].x);
+            const float f0 = M == -INFINITY ? 0.f : ex2(M - mn);
+            M = mn;
+            Ls *= f0;
+            O.x *= f0, O.y *= f0, O.z *= f0, O.w *= f0;
+#pragma unroll
+            for (int j = 0; j < CU; ++j) {
+              const float f = ml[j].x == -INFINITY ? 0.f : ex2(ml[j].x - M);  // (a NaN of a part stays NaN)
+              Ls = fmaf(ml[j].y, f, Ls);
+              O.x = fmaf(ov[j].x, f, O.x), O.y = fmaf(ov[j].y, f, O.y), O.z = fmaf(ov[j].z, f, O.z), O.w = fmaf(ov[j].w, f, O.w);
+            }
+          }
+          if (lane % LPR == 0) sm[warp][r] = M, sl[warp][r] = Ls;
+          so[warp][r][e] = O.x, so[warp][r][e + 1] = O.y, so[warp][r][e + 2] = O.z, so[warp][r][e + 3] = O.w;
+        }
+        __syncthreads();
+        add_up(true, nullptr);
       }
     }
     __syncthreads();  // the rings take the next item's positions
@@ -529,7 +550,7 @@ __global__ void __launch_bounds__(kWarps * 32, occupancy(HD, BITS, NT)) attn_pag
 int attn_paged_ctas(int num_sms) { return kCtasPerSm * num_sms; }
 
 size_t attn_paged_part_floats(int hd, int num_sms) {
-  return (size_t)attn_paged_ctas(num_sms) * 2 * kMostRows * (hd + 2);
+  return (size_t)attn_paged_ctas(num_sms) * 2 * kMostRows * (hd + 4);
 }
 
 namespace {

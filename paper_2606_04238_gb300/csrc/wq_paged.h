@@ -58,7 +58,7 @@ struct AttnPagedArgs {
   const int *tables;        // [batch][max_pages]
   int m, max_q, batch, H, Hkv, n_pages, shift, max_pages;
   float scale;              // of the scores, times log2(e)
-  float *part;              // [CTA][2][rows][HD + 2]
+  float *part;              // [CTA][2][16][HD + 4]
   int *counters;            // [CTA], zero between calls
   void *o;                  // bf16 [m][H][HD]
 };
