@@ -1721,6 +1721,9 @@ wq_status check_pool(const wq_kv_cache *c, int *shift) {
   wq_status st;
   if ((st = check_cache(c)) != WQ_OK || (st = check_page(c->max_len, shift)) != WQ_OK) return st;
   if ((long long)c->batch * c->max_len > INT32_MAX) return fail(WQ_ERR_SHAPE, "a pool of %d pages of %d", c->batch, c->max_len);
+  // the attention kernels number a pool's rows in 32 bits (the least rows, of 36 bytes in K and in V, of more would be 309 GB)
+  if ((long long)c->batch * c->max_len * c->n_kv >= 1ll << 32)
+    return fail(WQ_ERR_SHAPE, "a pool of %d pages of %d positions of %d heads", c->batch, c->max_len, c->n_kv);
   return WQ_OK;
 }
 // A ragged batch: its sequences, rows and the width of its tables.

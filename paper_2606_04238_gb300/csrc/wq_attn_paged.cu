@@ -17,11 +17,11 @@
 // p_j is rounded to binary16 (2^-11 of its term at most; 2^6 larger than above, so that small
 // ones are normal numbers) or over a bf16 cache to bf16 (2^-8); everything else is fp32.
 //
-// The blocks of 64 positions of all (sequence, row tile, kv head) are laid end to end and
+// The blocks of 64 positions (128 of 4 bits) of all (sequence, row tile, kv head) are laid end to end and
 // every CTA takes an equal run of them, found from the lengths themselves; what it has of an
 // (item) that other CTAs share is left in the workspace, and the last of them to arrive adds
-// up all parts in their order.  A warp takes 16 positions at a time, which always lie in one
-// page, through a ring of its own that cp.async fills: no warp waits for another.
+// up all parts in their order.  A warp takes 16 positions (32 of 4 bits) at a time, 16 of which
+// always lie in one page, through a ring of its own that cp.async fills: no warp waits for another.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -29,6 +29,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cstdint>
+#include <type_traits>
 
 #include "wq_cvt.cuh"
 #include "wq_frag.cuh"
@@ -47,19 +48,42 @@ __device__ int g_attn_paged_status = 0;
 namespace {
 
 constexpr int kWarps = 4;
-constexpr int kUnit = 16;            // positions a warp takes at a time
-constexpr int kBlock = kWarps * kUnit;
-constexpr int kCtasPerSm = 4;        // at most
+constexpr int kSub = 16;             // positions of an MMA step, always of one page
+constexpr int kCtasPerSm = 3;        // at most
 constexpr int kMostRows = 16;        // rows of an item at most
 
+__device__ __forceinline__ uint32_t hadd2_u(uint32_t a, uint32_t b) {
+  const __half2 v = __hadd2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
+  return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float v;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(v) : "f"(a), "f"(b));
+  return v;
+}
+__device__ __forceinline__ float half_of(uint32_t m) { return __half2float(__ushort_as_half((unsigned short)(m & 0xffffu))); }
 // An 8 x 8 matrix of 16-bit values (row lane / 4, columns 2 (lane % 4) ..) transposed.
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
   uint32_t r;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
-__device__ __forceinline__ void cp_async4(void *dst, const void *src) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_addr(dst)), "l"(src) : "memory");
+// cp.async of 16 and of 4 bytes, and loads, at a shared-memory address.
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void *src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void lds_words(uint32_t (&w)[N], uint32_t at) {
+  static_assert(N == 1 || N == 2 || N == 4, "");
+  if constexpr (N == 4)
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at));
+  else if constexpr (N == 2)
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
+  else
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(at));
 }
 // How a warp holds 16 positions.  K: lane (gr, tc) takes 16-byte pieces tc, tc + 4, .. of the
 // row in place gr and of that in place gr + 8 (KW words each: half or a quarter of a piece
@@ -70,26 +94,31 @@ __device__ __forceinline__ void cp_async4(void *dst, const void *src) {
 template <int HD, int BITS>
 struct Lay : RowLay<HD, BITS> {
   static constexpr int ROW = RowLay<HD, BITS>::ROW;
-  static constexpr int CHR = ROW / 16, COPIES = kUnit * CHR / 32;  // pieces a row; copies a lane of K, and of V
-  static constexpr int STAGE = 2 * kUnit * ROW + (BITS == 16 ? 0 : 128);
-  static constexpr int NS = BITS == 16 && HD == 128 ? 3 : 16 * 1024 / STAGE < 6 ? 16 * 1024 / STAGE : 6;
+  static constexpr int CHR = ROW / 16, COPIES = kSub * CHR / 32;  // pieces a row; copies a lane of K, and of V, of 16 positions
+  // positions a warp takes in one step: 32 of 4 bits, whose bytes are few for a step's fixed instructions
+  static constexpr int SUBS = BITS == 4 ? 2 : 1, UNIT = kSub * SUBS, BLOCK = kWarps * UNIT;
+  static constexpr int SUB = 2 * kSub * ROW + (BITS == 16 ? 0 : 128), STAGE = SUBS * SUB;
+  static constexpr int NS = BITS == 16 && HD == 128 ? 3 : BITS == 4 ? 3 : 16 * 1024 / STAGE < 6 ? 16 * 1024 / STAGE : 6;
+  static_assert(NS >= 2, "a stage in flight beside the one that is read");
   static constexpr int RING = kWarps * NS * STAGE;
   static __device__ __forceinline__ int k_swz(int place) { return ROW >= 128 ? 4 * (place & 1) : 0; }
   static __device__ __forceinline__ int v_swz(int row) { return ROW >= 128 ? 2 * (row & 3) : ROW == 64 ? 2 * (row / 2 & 1) : 0; }
 };
 
-// CTAs an SM holds: 128 registers a thread for 8 rows, 168 for 16; a bf16 ring of heads of 128 takes 96 KB.
-constexpr int occupancy(int hd, int bits, int nt) { return bits == 16 && hd == 128 ? 2 : nt == 1 ? kCtasPerSm : 3; }
+// CTAs an SM holds: 168 registers a thread (with 128 and four CTAs 64 tokens over 4k to 8k positions of 4 bits take 117 us
+// for 110, over 2k to 4k of a bf16 pool 82 for 72); a bf16 ring of heads of 128 takes 96 KB.
+constexpr int occupancy(int hd, int bits, int nt) { return bits == 16 && hd == 128 ? 2 : kCtasPerSm; }
 
-// A sequence; the blocks of 64 positions of each of its items, and its tiles of rows.
+// A sequence; the blocks of positions of each of its items, and its tiles of rows.
 struct Item : Seq {
   int blocks, tiles;
 };
+template <int BLOCK>
 __device__ __forceinline__ Item get_item(const AttnPagedArgs &a, int b, int rep, int rows, bool &bad) {
   Item s;
   static_cast<Seq &>(s) = get_seq(a, b, bad);
   s.tiles = (s.nq * rep + rows - 1) / rows;
-  s.blocks = max(1, (s.len + kBlock - 1) / kBlock);
+  s.blocks = max(1, (s.len + BLOCK - 1) / BLOCK);
   return s;
 }
 
@@ -103,7 +132,7 @@ __global__ void __launch_bounds__(kWarps * 32, occupancy(HD, BITS, NT)) attn_pag
   __shared__ float sm[kWarps][ROWS], sl[kWarps][ROWS];
   __shared__ int last;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gr = lane >> 2, tc = lane & 3;
-  uint8_t *const ring = paged_ring + warp * (L::NS * L::STAGE);
+  const uint32_t ring_at = smem_addr(paged_ring) + warp * (L::NS * L::STAGE);
   const int rep = a.H / a.Hkv, page = 1 << a.shift;
   pdl_wait();
   pdl_launch_dependents();
@@ -112,7 +141,7 @@ __global__ void __launch_bounds__(kWarps * 32, occupancy(HD, BITS, NT)) attn_pag
   bool bad = false;
   long long total = 0;
   for (int b = lane; b < a.batch; b += 32) {
-    const Item s = get_item(a, b, rep, ROWS, bad);
+    const Item s = get_item<L::BLOCK>(a, b, rep, ROWS, bad);
     total += (long long)s.blocks * s.tiles;
   }
 #pragma unroll
@@ -129,7 +158,7 @@ __global__ void __launch_bounds__(kWarps * 32, occupancy(HD, BITS, NT)) attn_pag
   for (int b0 = 0;; b0 += 32) {
     long long mine = 0;
     if (b0 + lane < a.batch) {
-      s = get_item(a, b0 + lane, rep, ROWS, bad);
+      s = get_item<L::BLOCK>(a, b0 + lane, rep, ROWS, bad);
       mine = (long long)s.blocks * s.tiles * a.Hkv;
     }
     long long incl = mine;
@@ -147,12 +176,12 @@ __global__ void __launch_bounds__(kWarps * 32, occupancy(HD, BITS, NT)) attn_pag
     }
     base += __shfl_sync(0xffffffffu, incl, 31);
   }
-  s = get_item(a, b, rep, ROWS, bad);
+  s = get_item<L::BLOCK>(a, b, rep, ROWS, bad);
 
   for (long long x = x0; x < x1;) {
     while (x >= base + (long long)s.blocks * s.tiles * a.Hkv) {
       base += (long long)s.blocks * s.tiles * a.Hkv;
-      s = get_item(a, ++b, rep, ROWS, bad);
+      s = get_item<L::BLOCK>(a, ++b, rep, ROWS, bad);
     }
     const int local = (int)((x - base) / s.blocks), blk0 = (int)((x - base) - (long long)local * s.blocks);
     const int g = local % a.Hkv, r0 = local / a.Hkv * ROWS;
@@ -162,37 +191,41 @@ __global__ void __launch_bounds__(kWarps * 32, occupancy(HD, BITS, NT)) attn_pag
     const int R = s.nq * rep, before = s.len - s.nq;  // positions that every row sees, less its own
     const int most = s.len == 0 ? 0 : before + min(R - 1, r0 + ROWS - 1) / rep + 1;  // positions that the tile's last row sees
     const int least = s.len == 0 ? 0 : before + r0 / rep + 1;                       // ... and its first
-    const int u0 = blk0 * kWarps + warp, c1 = min(most, blk1 * kBlock);
-    const int nu = u0 * kUnit < c1 ? ((c1 - u0 * kUnit + kUnit - 1) / kUnit + kWarps - 1) / kWarps : 0;  // this warp's units
+    const int u0 = blk0 * kWarps + warp, c1 = min(most, blk1 * L::BLOCK);
+    const int nu = u0 * L::UNIT < c1 ? ((c1 - u0 * L::UNIT + L::UNIT - 1) / L::UNIT + kWarps - 1) / kWarps : 0;  // this warp's units
 
-    // pages of 32 units: lane k has unit k's
-    int ids = 0;
-    auto load_ids = [&](int k) {
-      const int p = (u0 + kWarps * (k + lane)) * kUnit;
-      int id = p < c1 ? a.tables[(size_t)b * a.max_pages + (p >> a.shift)] : 0;
-      if (id < 0 || id >= a.n_pages) {
+    // the pool's first rows of 16 positions each: lane i has those of unit i / SUBS of the next 32 / SUBS (a pool has fewer
+    // than 2^32 rows: host check; what lies behind the last position is some row of it)
+    uint32_t rows = 0;
+    auto load_rows = [&](int k) {
+      const int p = (u0 + kWarps * (k + lane / L::SUBS)) * L::UNIT + lane % L::SUBS * kSub;
+      int id = a.tables[(size_t)b * a.max_pages + (min(p, c1 - 1) >> a.shift)];
+      if ((unsigned)id >= (unsigned)a.n_pages) {
         id = 0;
         atomicExch(&g_attn_paged_status, -1);
       }
-      ids = id;
+      rows = (((uint32_t)id * a.Hkv + g) << a.shift) + (p & (page - 1));
     };
     auto copy_unit = [&](int k, int stage) {
-      if (k % 32 == 0) load_ids(k);
-      const int id = __shfl_sync(0xffffffffu, ids, k % 32);
-      if (k < nu) {
-        const size_t row = (((size_t)id * a.Hkv + g) << a.shift) + ((u0 + kWarps * k) * kUnit & (page - 1));
-        uint8_t *st = ring + stage * L::STAGE;
+      constexpr int PER = 32 / L::SUBS;
+      if (k % PER == 0 && k < nu) load_rows(k);
+#pragma unroll
+      for (int u = 0; u < L::SUBS; ++u) {
+        const size_t row = __shfl_sync(0xffffffffu, rows, k % PER * L::SUBS + u);
+        if (k >= nu) continue;
+        const uint32_t st = ring_at + stage * L::STAGE + u * L::SUB;
         const uint8_t *ks = reinterpret_cast<const uint8_t *>(a.kc) + row * L::ROW + lane * 16;
         const uint8_t *vs = reinterpret_cast<const uint8_t *>(a.vc) + row * L::ROW + lane * 16;
 #pragma unroll
         for (int i = 0; i < L::COPIES; ++i) {
           const int p = (lane + 32 * i) / L::CHR, ch = (lane + 32 * i) % L::CHR;
           const int place = (p & 8) + 2 * (p & 3) + (p >> 2 & 1);
-          cp_async16(st + place * L::ROW + ((ch ^ L::k_swz(place)) << 4), ks + 512 * i);
-          cp_async16(st + (kUnit + p) * L::ROW + ((ch ^ L::v_swz(p)) << 4), vs + 512 * i);
+          copy16(st + place * L::ROW + ((ch ^ L::k_swz(place)) << 4), ks + 512 * i);
+          copy16(st + (kSub + p) * L::ROW + ((ch ^ L::v_swz(p)) << 4), vs + 512 * i);
         }
-        if constexpr (BITS != 16)
-          cp_async4(st + 2 * kUnit * L::ROW + lane * 4, (lane < 16 ? a.km : a.vm) + row + (lane & 15));
+        if constexpr (BITS != 16)  // scales and zero points of rows p and p + 8 beside each other
+          copy4(st + 2 * kSub * L::ROW + ((lane & 16) + 2 * (lane & 7) + (lane >> 3 & 1)) * 4,
+                    (lane < 16 ? a.km : a.vm) + row + (lane & 15));
       }
       cp_async_commit();
     };
@@ -251,43 +284,58 @@ __global__ void __launch_bounds__(kWarps * 32, occupancy(HD, BITS, NT)) attn_pag
       for (int e = 0; e < 2; ++e) m[n][e] = -INFINITY, l[n][e] = 0.f;
     }
 
-    int stage = 0, into = L::NS - 1;
-    for (int k = 0; k < nu; ++k) {
-      cp_async_wait_group<L::NS - 2>();
-      __syncwarp();
-      // (every lane has read what this stage held, the one before)
-      copy_unit(k + L::NS - 1, into);
-      into = into + 1 == L::NS ? 0 : into + 1;
-      const uint8_t *st = ring + stage * L::STAGE, *sv = st + kUnit * L::ROW;
-      stage = stage + 1 == L::NS ? 0 : stage + 1;
-      const int p0 = (u0 + kWarps * k) * kUnit;
-      const int pa = (gr >> 1) + 4 * (gr & 1);  // the lane's positions of the scores: pa and pa + 8
+    // what a score is less before 2^x: the rows' maxima (less kLift: p is 2^kLift times larger, so that small ones are normal
+    // numbers), 0 while there is none; a score above the limit raises them, so that p stays below 2^(8 + kLift)
+    constexpr float kLift = BITS == 16 ? 0.f : 6.f;
+    float base_m[NT][2], most_y[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) base_m[n][e] = -kLift, most_y[n][e] = -INFINITY;
+    const int pa = (gr >> 1) + 4 * (gr & 1);  // the lane's positions of the scores: pa and pa + 8 of 16
 
-      const uint32_t *meta = reinterpret_cast<const uint32_t *>(sv + kUnit * L::ROW);
-      float y[NT][4], y2[NT][4], sk[2];
-      {
+    auto highest = [](const float (&y)[L::SUBS][NT][4], int n, int e) {  // of the lane's scores of row e
+      float t = fmaxf(y[0][n][e], y[0][n][2 + e]);
+#pragma unroll
+      for (int u = 1; u < L::SUBS; ++u) t = fmaxf(t, fmaxf(y[u][n][e], y[u][n][2 + e]));
+      return t;
+    };
+    // One step's positions, from p0 on.  SOME: some row does not see them all, and behind the last position they may hold
+    // anything.
+    auto unit = [&](uint32_t st0, int p0, auto is_some) {
+      constexpr bool SOME = decltype(is_some)::value;
+      float y[L::SUBS][NT][4];
+      [[maybe_unused]] float rs[L::SUBS][2];
+#pragma unroll
+      for (int u = 0; u < L::SUBS; ++u) {
+        const uint32_t st = st0 + u * L::SUB;
         uint32_t ka[L::KI * L::KW], kb[L::KI * L::KW];
 #pragma unroll
         for (int i = 0; i < L::KI; ++i) {
           const int off = L::ROW >= 64 ? (((tc + 4 * i) ^ L::k_swz(gr)) << 4) : tc * 4 * L::KW;
-          load_words(*reinterpret_cast<uint32_t(*)[L::KW]>(&ka[L::KW * i]), st + gr * L::ROW + off);
-          load_words(*reinterpret_cast<uint32_t(*)[L::KW]>(&kb[L::KW * i]), st + (gr + 8) * L::ROW + off);
+          lds_words(*reinterpret_cast<uint32_t(*)[L::KW]>(&ka[L::KW * i]), st + gr * L::ROW + off);
+          lds_words(*reinterpret_cast<uint32_t(*)[L::KW]>(&kb[L::KW * i]), st + (gr + 8) * L::ROW + off);
         }
-        uint32_t za = 0, zb = 0;
+        uint32_t za = 0, zb = 0, za6 = 0, zb6 = 0;
+        float sk[2] = {1.f, 1.f}, lg[2] = {0.f, 0.f};
         if constexpr (BITS != 16) {
+          const uint32_t meta = st + 2 * kSub * L::ROW;
+          uint32_t mk[2], mv[2];
+          lds_words(mk, meta + 8 * pa);
+          lds_words(mv, meta + 64 + 8 * pa);
+          const uint32_t k1024 = 0x64006400u;
+          za = hadd2_u(__byte_perm(mk[0], 0, 0x3232), k1024), zb = hadd2_u(__byte_perm(mk[1], 0, 0x3232), k1024);
+          za6 = hsub2_u(za, 0x63806380u), zb6 = hsub2_u(zb, 0x63806380u);  // less 960: 64 + z, exact
+          sk[0] = half_of(mk[0]), sk[1] = half_of(mk[1]);
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const __half2 mk = *reinterpret_cast<const __half2 *>(meta + pa + 8 * i);
-            sk[i] = __low2float(mk);
-            const __half2 z = __hadd2(__high2half2(mk), __float2half2_rn(1024.f));
-            (i ? zb : za) = *reinterpret_cast<const uint32_t *>(&z);
+            // rows of zeros, those of a zero-filled cache too: code - z is 0, and the least scale does as well
+            const uint32_t m = i ? mv[1] : mv[0];
+            const float s = max_nan((int)m < 0 ? 0.f : half_of(m), kLeastScale);  // (kZeroRow: the one zero point below 0)
+            lg[i] = lg2(s);
+            rs[u][i] = rcp(s);
           }
         }
-        const uint32_t za6 = hsub2_u(za, 0x63806380u), zb6 = hsub2_u(zb, 0x63806380u);  // less 960: 64 + z, exact
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) y[n][e] = y2[n][e] = 0.f;
 #pragma unroll
         for (int ks = 0; ks < L::KS; ++ks) {
           uint32_t f[4];
@@ -295,66 +343,85 @@ __global__ void __launch_bounds__(kWarps * 32, occupancy(HD, BITS, NT)) attn_pag
           k_frag<HD, BITS>(kb, ks, zb, zb6, f[1], f[3]);
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
+            if (ks == 0)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) y[u][n][e] = 0.f;
             if constexpr (BITS == 16)
-              mma_bf16_16816(ks % 2 ? y2[n] : y[n], f, qb[n][ks][0], qb[n][ks][1]);
+              mma_bf16_16816(y[u][n], f, qb[n][ks][0], qb[n][ks][1]);
             else
-              mma_f16_16816(ks % 2 ? y2[n] : y[n], f, qb[n][ks][0], qb[n][ks][1]);
+              mma_f16_16816(y[u][n], f, qb[n][ks][0], qb[n][ks][1]);
           }
         }
-      }
-      // places that some row does not see: behind the last position they may hold anything
-      const bool some = p0 + kUnit > least;
-      float rs[2] = {1.f, 1.f};
-      uint32_t zv[2] = {0, 0};  // 1024 + z of rows tc and tc + 4, tc + 8 and tc + 12
-      if constexpr (BITS == 16) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) y[n][e] = (y[n][e] + y2[n][e]) * A[n][e % 2];
-      } else {
+          for (int e = 0; e < 4; ++e) {
+            y[u][n][e] = BITS == 16 ? y[u][n][e] * A[n][e % 2] : fmaf(y[u][n][e], A[n][e % 2] * sk[e / 2], lg[e / 2]);
+            if (SOME && p0 + kSub * u + pa + 8 * (e / 2) >= limit[n][e % 2]) y[u][n][e] = -INFINITY;
+          }
+      }
+      // ---- softmax
+      bool up = false;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          uint32_t mv = meta[16 + pa + 8 * i];
-          // rows of zeros, those of a zero-filled cache too: code - z is 0, and the least scale does as well
-          if ((mv & 0xffffu) == 0 || mv == kZeroRow) mv = 1u;
-          const float s = __half2float(__ushort_as_half((unsigned short)(mv & 0xffffu)));
-          const float lg = lg2(s);
-          rs[i] = rcp(s);
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
+        for (int e = 0; e < 2; ++e) {
+          up |= highest(y, n, e) > most_y[n][e];
+        }
+      if (__any_sync(0xffffffffu, up)) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
-              y[n][2 * i + e] = fmaf((y[n][2 * i + e] + y2[n][2 * i + e]) * A[n][e], sk[i], lg);
-          uint32_t z = __byte_perm(meta[16 + tc + 8 * i], meta[20 + tc + 8 * i], 0x7632);
-          if (some) z &= (p0 + tc + 8 * i < most ? 0xffffu : 0u) | (p0 + tc + 4 + 8 * i < most ? 0xffff0000u : 0u);
-          const __half2 zz = __hadd2(*reinterpret_cast<const __half2 *>(&z), __float2half2_rn(1024.f));
-          zv[i] = *reinterpret_cast<const uint32_t *>(&zz);
+        for (int n = 0; n < NT; ++n) {
+          float al[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float t = highest(y, n, e);
+#pragma unroll
+            for (int d = 4; d <= 16; d <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
+            t = fmaxf(t, m[n][e]);
+            al[e] = t == -INFINITY ? 1.f : ex2(m[n][e] - t);
+            m[n][e] = t;
+            base_m[n][e] = t == -INFINITY ? -kLift : t - kLift;
+            most_y[n][e] = t + 8.f;
+            l[n][e] *= al[e];
+          }
+#pragma unroll
+          for (int j = 0; j < L::NJ / 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[n][j][e] *= al[e % 2];
         }
       }
-      uint32_t vw[4][L::VI * L::VW];
 #pragma unroll
-      for (int v = 0; v < 4; ++v)
+      for (int u = 0; u < L::SUBS; ++u) {
+        const uint32_t sv = st0 + u * L::SUB + kSub * L::ROW;
+        const int q0 = p0 + kSub * u;
+        uint32_t vw[4][L::VI * L::VW];
 #pragma unroll
-        for (int i = 0; i < L::VI; ++i) {
-          const int off = L::ROW >= 128 ? (((gr + 8 * i) ^ L::v_swz(tc)) << 4)
-                                        : (((gr * 4 * L::VW >> 4) ^ L::v_swz(tc)) << 4) + (gr * 4 * L::VW & 15);
-          load_words(*reinterpret_cast<uint32_t(*)[L::VW]>(&vw[v][L::VW * i]), sv + (tc + 4 * v) * L::ROW + off);
+        for (int v = 0; v < 4; ++v)
+#pragma unroll
+          for (int i = 0; i < L::VI; ++i) {
+            const int off = L::ROW >= 128 ? (((gr + 8 * i) ^ L::v_swz(tc)) << 4)
+                                          : (((gr * 4 * L::VW >> 4) ^ L::v_swz(tc)) << 4) + (gr * 4 * L::VW & 15);
+            lds_words(*reinterpret_cast<uint32_t(*)[L::VW]>(&vw[v][L::VW * i]), sv + (tc + 4 * v) * L::ROW + off);
+          }
+        uint32_t zv[2] = {0, 0}, z6[2] = {0, 0};  // 1024 + z of rows tc and tc + 4, tc + 8 and tc + 12
+        if constexpr (BITS != 16) {
+          const uint32_t meta = sv + kSub * L::ROW + 64;
+          uint32_t x[2], w[2];
+          lds_words(x, meta + 8 * tc);
+          lds_words(w, meta + 8 * tc + 32);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            uint32_t z = __byte_perm(x[i], w[i], 0x7632);
+            if (SOME) z &= (q0 + tc + 8 * i < most ? 0xffffu : 0u) | (q0 + tc + 4 + 8 * i < most ? 0xffff0000u : 0u);
+            zv[i] = hadd2_u(z, 0x64006400u);
+            z6[i] = hsub2_u(zv[i], 0x63806380u);
+          }
         }
-      bool odd = false;
-      if (some) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int p = p0 + pa + 8 * i;
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-              if (p >= limit[n][e]) y[n][2 * i + e] = -INFINITY;
-        }
-        if constexpr (BITS == 16)
+        bool odd = false;
+        if (SOME && BITS == 16)
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
-            const bool behind = p0 + tc + 4 * v >= most;
+            const bool behind = q0 + tc + 4 * v >= most;
 #pragma unroll
             for (int i = 0; i < L::VI * L::VW; ++i) {
               uint32_t &w = vw[v][i];
@@ -364,84 +431,69 @@ __global__ void __launch_bounds__(kWarps * 32, occupancy(HD, BITS, NT)) attn_pag
               if ((w & 0x7f800000u) == 0x7f800000u) w &= 0xffffu, odd = true;
             }
           }
-      }
-      // ---- softmax: the maximum is raised when a score passes it by 2^8 (p stays below that times 2^kLift)
-      constexpr float kLift = BITS == 16 ? 0.f : 6.f;
-      bool up = false;
+        uint32_t pb[NT][2];
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) up |= fmaxf(y[n][e], y[n][2 + e]) > m[n][e] + 8.f;
-      if (__any_sync(0xffffffffu, up)) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          float al[2];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float t = fmaxf(y[n][e], y[n][2 + e]);
-#pragma unroll
-            for (int d = 4; d <= 16; d <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
-            t = fmaxf(t, m[n][e]);
-            al[e] = t == -INFINITY ? 1.f : ex2(m[n][e] - t);
-            m[n][e] = t;
-            l[n][e] *= al[e];
+          for (int i = 0; i < 2; ++i) {
+            const float p0 = ex2(y[u][n][2 * i] - base_m[n][0]), p1 = ex2(y[u][n][2 * i + 1] - base_m[n][1]);
+            pb[n][i] = transpose8(BITS == 16 ? pack_bf2(p0, p1) : pack_h2(p0, p1));
+            if constexpr (BITS == 16) {
+              l[n][0] += p0;
+              l[n][1] += p1;
+            } else {  // (a masked row's scale may be NaN)
+              if (!SOME || p0 != 0.f) l[n][0] = fmaf(p0, rs[u][i], l[n][0]);
+              if (!SOME || p1 != 0.f) l[n][1] = fmaf(p1, rs[u][i], l[n][1]);
+            }
           }
 #pragma unroll
-          for (int j = 0; j < L::NJ / 2; ++j)
+        for (int j = 0; j < L::NJ / 2; ++j) {
+          uint32_t f[4];
+          f[0] = v_frag<HD, BITS>(vw[0], vw[1], 2 * j, zv[0], z6[0]);
+          f[1] = v_frag<HD, BITS>(vw[0], vw[1], 2 * j + 1, zv[0], z6[0]);
+          f[2] = v_frag<HD, BITS>(vw[2], vw[3], 2 * j, zv[1], z6[1]);
+          f[3] = v_frag<HD, BITS>(vw[2], vw[3], 2 * j + 1, zv[1], z6[1]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[n][j][e] *= al[e % 2];
-        }
-      }
-      uint32_t pb[NT][2];
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          float p[2];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) p[e] = ex2(y[n][2 * i + e] - (m[n][e] == -INFINITY ? 0.f : m[n][e] - kLift));
-          const uint32_t w = BITS == 16 ? pack_bf2(p[0], p[1]) : pack_h2(p[0], p[1]);
-          if constexpr (BITS != 16) {
-            // (a masked row's scale may be NaN)
-            l[n][0] = some && p[0] == 0.f ? l[n][0] : fmaf(p[0], rs[i], l[n][0]);
-            l[n][1] = some && p[1] == 0.f ? l[n][1] : fmaf(p[1], rs[i], l[n][1]);
-          } else {
-            l[n][0] += p[0];
-            l[n][1] += p[1];
+          for (int n = 0; n < NT; ++n) {
+            if constexpr (BITS == 16)
+              mma_bf16_16816(o[n][j], f, pb[n][0], pb[n][1]);
+            else
+              mma_f16_16816(o[n][j], f, pb[n][0], pb[n][1]);
           }
-          pb[n][i] = transpose8(w);
         }
-      const uint32_t z6[2] = {hsub2_u(zv[0], 0x63806380u), hsub2_u(zv[1], 0x63806380u)};
+        if (SOME && BITS == 16 && __any_sync(0xffffffffu, odd)) {
+          for (int p = 0; p < kSub && q0 + p < most; ++p)
 #pragma unroll
-      for (int j = 0; j < L::NJ / 2; ++j) {
-        uint32_t f[4];
-        f[0] = v_frag<HD, BITS>(vw[0], vw[1], 2 * j, zv[0], z6[0]);
-        f[1] = v_frag<HD, BITS>(vw[0], vw[1], 2 * j + 1, zv[0], z6[0]);
-        f[2] = v_frag<HD, BITS>(vw[2], vw[3], 2 * j, zv[1], z6[1]);
-        f[3] = v_frag<HD, BITS>(vw[2], vw[3], 2 * j + 1, zv[1], z6[1]);
+            for (int j = 0; j < L::NJ; ++j) {
+              const int at = L::v_at(j, gr) * 2;
+              uint32_t w[1];
+              lds_words(w, sv + p * L::ROW + (((at >> 4) ^ L::v_swz(p)) << 4) + (at & 12));
+              const float f = at & 2 ? bf_hi(w[0]) : bf_lo(w[0]);
+              if (isfinite(f)) continue;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          if constexpr (BITS == 16)
-            mma_bf16_16816(o[n][j], f, pb[n][0], pb[n][1]);
-          else
-            mma_f16_16816(o[n][j], f, pb[n][0], pb[n][1]);
+              for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                  if (q0 + p < limit[n][e]) o[n][j / 2][2 * (j % 2) + e] += f;
+            }
         }
       }
-      if (BITS == 16 && __any_sync(0xffffffffu, odd)) {
-        for (int p = 0; p < kUnit && p0 + p < most; ++p)
-#pragma unroll
-          for (int j = 0; j < L::NJ; ++j) {
-            const int at = L::v_at(j, gr) * 2;
-            const float f = __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(
-                sv + p * L::ROW + (((at >> 4) ^ L::v_swz(p)) << 4) + (at & 15)));
-            if (isfinite(f)) continue;
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-              for (int e = 0; e < 2; ++e)
-                if (p0 + p < limit[n][e]) o[n][j / 2][2 * (j % 2) + e] += f;
-          }
-      }
+    };
+
+    int stage = 0, into = L::NS - 1;
+    for (int k = 0; k < nu; ++k) {
+      cp_async_wait_group<L::NS - 2>();
+      __syncwarp();
+      // (every lane has read what this stage held, the one before)
+      copy_unit(k + L::NS - 1, into);
+      into = into + 1 == L::NS ? 0 : into + 1;
+      const uint32_t st = ring_at + stage * L::STAGE;
+      stage = stage + 1 == L::NS ? 0 : stage + 1;
+      const int p0 = (u0 + kWarps * k) * L::UNIT;
+      if (p0 + L::UNIT > least)
+        unit(st, p0, std::true_type());
+      else
+        unit(st, p0, std::false_type());
     }
     cp_async_wait_all();
     __syncthreads();  // the rings are read to their end
@@ -570,7 +622,7 @@ cudaError_t launch_t(const AttnPagedArgs &a, int num_sms, cudaStream_t s) {
   }
   // as many CTAs as the SMs hold at once, and no more than blocks there can be
   const long long tiles = ((long long)a.m * (a.H / a.Hkv) + 8 * NT - 1) / (8 * NT) + a.batch;
-  const long long blocks = (((long long)a.max_pages << a.shift) + kBlock - 1) / kBlock;
+  const long long blocks = (((long long)a.max_pages << a.shift) + L::BLOCK - 1) / L::BLOCK;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;

@@ -45,6 +45,15 @@ struct RowLay {
   }
 };
 
+// The codes of MASK in x as binary16 1024 + code (64 + code in bits 4 to 7).  One instruction: a second constant would be
+// a second one, so 1024 is a register that the compiler does not know the value of.
+template <uint32_t MASK>
+__device__ __forceinline__ uint32_t plus1024(uint32_t x) {
+  uint32_t k, v;
+  asm("mov.b32 %0, 0x64006400;" : "=r"(k));
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(v) : "r"(x), "n"(MASK), "r"(k));  // (x & MASK) | k
+  return v;
+}
 // The fragments (b0, b1) of MMA step ks from a lane's words of one K row; zk: z
 // in both halves, as 1024 + z (8 bits, low), and 64 + z (4 bits, high).
 template <int HD, int BITS>
@@ -58,8 +67,8 @@ __device__ __forceinline__ void k_frag(const uint32_t (&w)[RowLay<HD, BITS>::KI 
     b1 = hsub2_u(__byte_perm(w[ks], 0x64646464u, 0x4342), z1024);
   } else {
     const uint32_t x = ks % 2 ? w[ks / 2] >> 8 : w[ks / 2];
-    b0 = hsub2_u((x & 0x000f000fu) | 0x64006400u, z1024);
-    b1 = hfma16_u((x & 0x00f000f0u) | 0x64006400u, z64);
+    b0 = hsub2_u(plus1024<0x000f000fu>(x), z1024);
+    b1 = hfma16_u(plus1024<0x00f000f0u>(x), z64);
   }
 }
 
@@ -79,7 +88,7 @@ __device__ __forceinline__ uint32_t v_frag(const uint32_t (&wa)[RowLay<HD, BITS>
     uint32_t x = __byte_perm(wa[j / 8], wb[j / 8], j % 2 ? 0x7632 : 0x5410);
     const int nib = j % 8 / 2;
     if (nib >= 2) x >>= 8;
-    return nib % 2 ? hfma16_u((x & 0x00f000f0u) | 0x64006400u, z64) : hsub2_u((x & 0x000f000fu) | 0x64006400u, z1024);
+    return nib % 2 ? hfma16_u(plus1024<0x00f000f0u>(x), z64) : hsub2_u(plus1024<0x000f000fu>(x), z1024);
   }
 }
 

@@ -24,7 +24,7 @@ __device__ int g_pages_status = 0;
 
 namespace {
 
-constexpr int kPlanThreads = 512;
+constexpr int kPlanThreads = 512, kPutThreads = 128;
 constexpr int kPagedReadThreads = 256;
 
 struct Sums {
@@ -172,55 +172,49 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PagePlanA
 //   A CTA takes a token.  HD / 16 lanes take a row, values 8 l .. and HD/2 + 8 l .., so that
 // a value and the one it is rotated with are one lane's.
 template <int HD, int BITS, bool F32>
-__global__ void __launch_bounds__(128, 4) qkv_paged_kernel(const QkvPagedArgs a) {
-  constexpr int THREADS = 128, LPR = HD / 16, GROUPS = THREADS / LPR, U = 2;  // lanes a row, rows a pass, passes in flight
+__global__ void __launch_bounds__(kPutThreads, 5) qkv_paged_kernel(const QkvPagedArgs a) {
+  constexpr int THREADS = kPutThreads, LPR = HD / 16, GROUPS = THREADS / LPR, U = 2;  // lanes a row, rows a pass, passes in flight
   __shared__ float red[THREADS / 32];
   pdl_wait();
   pdl_launch_dependents();
   const int tid = threadIdx.x, lane = tid % LPR, grp = tid / LPR;
-  const int heads = a.n_heads + 2 * a.n_kv;
+  const int heads = a.n_heads + 2 * a.n_kv, passes = (heads + GROUPS - 1) / GROUPS;
   const size_t tok = blockIdx.x;
   const int pos = a.positions ? a.positions[tok] : 0, slot = a.slots[tok];
+  uint4 raw[U][F32 ? 4 : 2];
+  auto fetch = [&](int pass, uint4 (&r)[F32 ? 4 : 2]) {
+    const int h = pass * GROUPS + grp;
+    if (h >= heads) return;
+    const size_t at = (tok * heads + h) * HD + 8 * lane;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if constexpr (F32) {
+        const uint4 *p = reinterpret_cast<const uint4 *>(reinterpret_cast<const float *>(a.qkv) + at + i * (HD / 2));
+        r[2 * i] = __ldcs(p), r[2 * i + 1] = __ldcs(p + 1);
+      } else {
+        r[i] = __ldcs(reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(a.qkv) + at + i * (HD / 2)));
+      }
+    }
+  };
+#pragma unroll
+  for (int u = 0; u < U; ++u) fetch(u, raw[u]);
   const bool bad = a.positions && (pos < 0 || pos >= a.n_pos), out = slot < -1 || (slot >> a.shift) >= a.n_pages;
   if (bad || out) {
     if (tid == 0) atomicExch(&g_pages_status, -1);
     if (bad) return;
   }
   const bool put = slot >= 0 && !out;
-  float v[U][16];
-  auto fetch = [&](int h0) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int h = h0 + u * GROUPS + grp;
-      if (h >= heads) continue;
-      const size_t at = (tok * heads + h) * HD + 8 * lane;
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        if constexpr (F32) {
-          const float4 *p = reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(a.qkv) + at + i * (HD / 2));
-          const float4 f = __ldcs(p), g = __ldcs(p + 1);
-          v[u][8 * i] = f.x, v[u][8 * i + 1] = f.y, v[u][8 * i + 2] = f.z, v[u][8 * i + 3] = f.w;
-          v[u][8 * i + 4] = g.x, v[u][8 * i + 5] = g.y, v[u][8 * i + 6] = g.z, v[u][8 * i + 7] = g.w;
-        } else {
-          const uint4 w = __ldcs(reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(a.qkv) + at + i * (HD / 2)));
-          const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[u][8 * i + 2 * e] = bf_lo(x[e]), v[u][8 * i + 2 * e + 1] = bf_hi(x[e]);
-        }
-      }
-    }
-  };
-  fetch(0);
-  float co[8], si[8];  // of the lane's eight angles
+  // (two values an instruction; each of its operations is rounded as by itself)
+  uint64_t co[4], si[4];  // of the lane's eight angles
   if (a.positions) {
     const float4 *tab = reinterpret_cast<const float4 *>(a.table + ((size_t)pos * (HD / 2) + 8 * lane) * 2);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float4 t = __ldg(tab + e);
-      co[2 * e] = t.x, si[2 * e] = t.y, co[2 * e + 1] = t.z, si[2 * e + 1] = t.w;
+      co[e] = pack_f32x2(t.x, t.z), si[e] = pack_f32x2(t.y, t.w);
     }
   }
-  float rs = 1.f;
+  uint64_t rs = 0;
   if (a.x) {
     float ss = 0.f;
     const uint4 *xs = reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(a.x) + tok * a.d);
@@ -240,107 +234,120 @@ __global__ void __launch_bounds__(128, 4) qkv_paged_kernel(const QkvPagedArgs a)
     float tot = 0.f;
 #pragma unroll
     for (int w = 0; w < THREADS / 32; ++w) tot += red[w];
-    rs = __fdiv_rn(1.f, __fsqrt_rn(__fadd_rn(__fdiv_rn(tot, (float)a.d), kRmsEps)));
+    const float r = __fdiv_rn(1.f, __fsqrt_rn(__fadd_rn(__fdiv_rn(tot, (float)a.d), kRmsEps)));
+    rs = pack_f32x2(r, r);
   }
-  for (int h0 = 0; h0 < heads; h0 += U * GROUPS) {
-    if (h0 > 0) fetch(h0);
+  auto work = [&](int pass, uint4 (&r)[F32 ? 4 : 2]) {
+    const int h = pass * GROUPS + grp;
+    const bool in = h < heads, is_q = h < a.n_heads, turns = h < a.n_heads + a.n_kv;
+    uint64_t w[8];  // values 8 l .., then HD/2 + 8 l ..
+    if constexpr (F32) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int h = h0 + u * GROUPS + grp;
-      if (h0 + u * GROUPS >= heads) break;  // uniform in the CTA
-      const bool in = h < heads, is_q = h < a.n_heads, turns = h < a.n_heads + a.n_kv;
-      float(&w)[16] = v[u];
-      if (!in)
+      for (int i = 0; i < 4; ++i)
+        w[2 * i] = in ? (uint64_t)r[i].y << 32 | r[i].x : 0, w[2 * i + 1] = in ? (uint64_t)r[i].w << 32 | r[i].z : 0;
+    } else {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) w[e] = 0.f;
-      if (a.x)
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t x[4] = {r[i].x, r[i].y, r[i].z, r[i].w};
 #pragma unroll
-        for (int e = 0; e < 16; ++e) w[e] = __fmul_rn(w[e], rs);
-      if (a.head_norm) {
-        float sq[8];
+        for (int e = 0; e < 4; ++e) w[4 * i + e] = in ? pack_f32x2(bf_lo(x[e]), bf_hi(x[e])) : 0;
+      }
+    }
+    fetch(pass + U, r);
+    if (a.x)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sq[e] = __fadd_rn(__fmul_rn(w[e], w[e]), __fmul_rn(w[8 + e], w[8 + e]));
+      for (int e = 0; e < 8; ++e) w[e] = mul_f32x2(w[e], rs);
+    // heads of a warp's rows ascend: whether any of them is Q or K, or K or V, is known to all its lanes
+    if (a.head_norm && __any_sync(0xffffffffu, in && turns)) {
+      uint64_t sq[4];
 #pragma unroll
-        for (int o = 4; o >= 1; o >>= 1)
+      for (int e = 0; e < 4; ++e) sq[e] = add_f32x2(mul_f32x2(w[e], w[e]), mul_f32x2(w[4 + e], w[4 + e]));
+      float s, s1;
+      unpack_f32x2(add_f32x2(add_f32x2(sq[0], sq[2]), add_f32x2(sq[1], sq[3])), s, s1);
+      s = __fadd_rn(s, s1);
 #pragma unroll
-          for (int e = 0; e < o; ++e) sq[e] = __fadd_rn(sq[e], sq[e + o]);
+      for (int o = LPR / 2; o >= 1; o >>= 1) s = __fadd_rn(s, __shfl_xor_sync(0xffffffffu, s, o));
+      const float hn = __fdiv_rn(1.f, __fsqrt_rn(__fadd_rn(__fmul_rn(s, 1.f / HD), kRmsEps)));
+      if (turns) {
+        const void *norm = is_q ? a.q_norm : a.k_norm;
+        const uint64_t hn2 = pack_f32x2(hn, hn);
 #pragma unroll
-        for (int o = LPR / 2; o >= 1; o >>= 1) sq[0] = __fadd_rn(sq[0], __shfl_xor_sync(0xffffffffu, sq[0], o));
-        const float hn = __fdiv_rn(1.f, __fsqrt_rn(__fadd_rn(__fmul_rn(sq[0], 1.f / HD), kRmsEps)));
-        if (turns) {
-          const void *norm = is_q ? a.q_norm : a.k_norm;
+        for (int e = 0; e < 8; ++e) w[e] = mul_f32x2(w[e], hn2);
+        if (norm) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) w[e] = __fmul_rn(w[e], hn);
-          if (norm) {
+          for (int i = 0; i < 2; ++i) {
+            const uint4 g = __ldg(reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(norm) + i * (HD / 2) + 8 * lane));
+            const uint32_t x[4] = {g.x, g.y, g.z, g.w};
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const uint4 g = __ldg(reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(norm) + i * (HD / 2) + 8 * lane));
-              const uint32_t x[4] = {g.x, g.y, g.z, g.w};
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                w[8 * i + 2 * e] = __fmul_rn(w[8 * i + 2 * e], bf_lo(x[e]));
-                w[8 * i + 2 * e + 1] = __fmul_rn(w[8 * i + 2 * e + 1], bf_hi(x[e]));
-              }
-            }
+            for (int e = 0; e < 4; ++e) w[4 * i + e] = mul_f32x2(w[4 * i + e], pack_f32x2(bf_lo(x[e]), bf_hi(x[e])));
           }
         }
       }
-      if (turns && a.positions)
+    }
+    if (turns && a.positions) {
+      const uint64_t minus = pack_f32x2(-1.f, -1.f);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float lo = w[e], hi = w[8 + e];
-          w[e] = __fsub_rn(__fmul_rn(lo, co[e]), __fmul_rn(hi, si[e]));
-          w[8 + e] = __fadd_rn(__fmul_rn(hi, co[e]), __fmul_rn(lo, si[e]));
-        }
-      auto rounded = [&](int i) {
-        return make_uint4(pack_bf2(w[8 * i], w[8 * i + 1]), pack_bf2(w[8 * i + 2], w[8 * i + 3]),
-                          pack_bf2(w[8 * i + 4], w[8 * i + 5]), pack_bf2(w[8 * i + 6], w[8 * i + 7]));
-      };
-      if (in && is_q) {
-        __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(a.q) + (tok * a.n_heads + h) * HD + 8 * lane;
-        *reinterpret_cast<uint4 *>(dst) = rounded(0);
-        *reinterpret_cast<uint4 *>(dst + HD / 2) = rounded(1);
-      }
-      // heads of a warp's rows ascend: whether any of them is K or V is known to all its lanes
-      if (!put || __all_sync(0xffffffffu, is_q || !in)) continue;
-      const int g = turns ? h - a.n_heads : h - a.n_heads - a.n_kv;
-      const bool mine = in && !is_q;
-      const size_t row = mine ? (((size_t)(slot >> a.shift) * a.n_kv + g) << a.shift) + (slot & ((1 << a.shift) - 1)) : 0;
-      uint8_t *dst = reinterpret_cast<uint8_t *>(turns ? a.kc : a.vc) + row * (HD * BITS / 8) + lane * BITS;
-      if constexpr (BITS == 16) {
-        if (!mine) continue;
-        *reinterpret_cast<uint4 *>(dst) = rounded(0);
-        *reinterpret_cast<uint4 *>(dst + HD) = rounded(1);
-      } else {
-        float mn = 0.f, mx = 0.f;
-        bool nan = false;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          mn = fminf(mn, w[e]);
-          mx = fmaxf(mx, w[e]);
-          nan |= w[e] != w[e];
-        }
-        if (nan) mx = __int_as_float(0x7fffffff);
-#pragma unroll
-        for (int o = LPR / 2; o >= 1; o >>= 1) {
-          const float x = __shfl_xor_sync(0xffffffffu, mn, o), y = __shfl_xor_sync(0xffffffffu, mx, o);
-          mn = fminf(mn, x);
-          mx = y > mx || y != y ? y : mx;
-        }
-        uint32_t c[8], p[BITS / 2];
-        const uint32_t meta = quantize16<BITS>(w, mn, mx, c);
-        if (!mine) continue;
-        pack_codes<BITS>(c, p);
-        if constexpr (BITS == 8) {
-          *reinterpret_cast<uint2 *>(dst) = make_uint2(p[0], p[1]);
-          *reinterpret_cast<uint2 *>(dst + HD / 2) = make_uint2(p[2], p[3]);
-        } else {
-          *reinterpret_cast<uint32_t *>(dst) = p[0];
-          *reinterpret_cast<uint32_t *>(dst + HD / 4) = p[1];
-        }
-        if (lane == 0) (turns ? a.km : a.vm)[row] = meta;
+      for (int e = 0; e < 4; ++e) {
+        const uint64_t lo = w[e], hi = w[4 + e];
+        w[e] = fma_f32x2(mul_f32x2(hi, si[e]), minus, mul_f32x2(lo, co[e]));  // (the product with -1 is exact)
+        w[4 + e] = add_f32x2(mul_f32x2(hi, co[e]), mul_f32x2(lo, si[e]));
       }
     }
+    float v[16];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) unpack_f32x2(w[e], v[2 * e], v[2 * e + 1]);
+    auto rounded = [&](int i) {
+      return make_uint4(pack_bf2(v[8 * i], v[8 * i + 1]), pack_bf2(v[8 * i + 2], v[8 * i + 3]), pack_bf2(v[8 * i + 4], v[8 * i + 5]),
+                        pack_bf2(v[8 * i + 6], v[8 * i + 7]));
+    };
+    if (in && is_q) {
+      __nv_bfloat16 *dst = reinterpret_cast<__nv_bfloat16 *>(a.q) + (tok * a.n_heads + h) * HD + 8 * lane;
+      *reinterpret_cast<uint4 *>(dst) = rounded(0);
+      *reinterpret_cast<uint4 *>(dst + HD / 2) = rounded(1);
+    }
+    if (!put || __all_sync(0xffffffffu, is_q || !in)) return;
+    const int g = turns ? h - a.n_heads : h - a.n_heads - a.n_kv;
+    const bool mine = in && !is_q;
+    const size_t row = mine ? (((size_t)(slot >> a.shift) * a.n_kv + g) << a.shift) + (slot & ((1 << a.shift) - 1)) : 0;
+    uint8_t *dst = reinterpret_cast<uint8_t *>(turns ? a.kc : a.vc) + row * (HD * BITS / 8) + lane * BITS;
+    if constexpr (BITS == 16) {
+      if (!mine) return;
+      *reinterpret_cast<uint4 *>(dst) = rounded(0);
+      *reinterpret_cast<uint4 *>(dst + HD) = rounded(1);
+    } else {
+      float mn = 0.f, mx = 0.f;
+      bool nan = false;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        mn = fminf(mn, v[e]);
+        mx = fmaxf(mx, v[e]);
+        nan |= v[e] != v[e];
+      }
+      if (nan) mx = __int_as_float(0x7fffffff);
+#pragma unroll
+      for (int o = LPR / 2; o >= 1; o >>= 1) {
+        const float x = __shfl_xor_sync(0xffffffffu, mn, o), y = __shfl_xor_sync(0xffffffffu, mx, o);
+        mn = fminf(mn, x);
+        mx = y > mx || y != y ? y : mx;
+      }
+      uint32_t c[8], p[BITS / 2];
+      const uint32_t meta = quantize16<BITS>(v, mn, mx, c);
+      if (!mine) return;
+      pack_codes<BITS>(c, p);
+      if constexpr (BITS == 8) {
+        *reinterpret_cast<uint2 *>(dst) = make_uint2(p[0], p[1]);
+        *reinterpret_cast<uint2 *>(dst + HD / 2) = make_uint2(p[2], p[3]);
+      } else {
+        *reinterpret_cast<uint32_t *>(dst) = p[0];
+        *reinterpret_cast<uint32_t *>(dst + HD / 4) = p[1];
+      }
+      if (lane == 0) (turns ? a.km : a.vm)[row] = meta;
+    }
+  };
+  for (int pass = 0; pass < passes; pass += U) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (pass + u < passes) work(pass + u, raw[u]);  // uniform in the CTA
   }
 }
 
@@ -389,8 +396,8 @@ cudaError_t launch_page_plan(const PagePlanArgs &a, cudaStream_t s) {
 cudaError_t launch_qkv_paged(const QkvPagedArgs &a, int m, int hd, int bits, bool f32, cudaStream_t s) {
 #define WQ_PAGED(HD, BITS)                                                              \
   if (hd == HD && bits == BITS)                                                         \
-    return f32 ? launch_pdl(qkv_paged_kernel<HD, BITS, true>, (unsigned)m, 128, s, a)   \
-               : launch_pdl(qkv_paged_kernel<HD, BITS, false>, (unsigned)m, 128, s, a);
+    return f32 ? launch_pdl(qkv_paged_kernel<HD, BITS, true>, (unsigned)m, kPutThreads, s, a)   \
+               : launch_pdl(qkv_paged_kernel<HD, BITS, false>, (unsigned)m, kPutThreads, s, a);
   WQ_PAGED(128, 16) WQ_PAGED(128, 8) WQ_PAGED(128, 4) WQ_PAGED(64, 16) WQ_PAGED(64, 8) WQ_PAGED(64, 4)
 #undef WQ_PAGED
   return cudaErrorInvalidValue;

@@ -7,15 +7,11 @@
 #include <cstdint>
 
 #include "wq_cvt.cuh"
+#include "wq_frag.cuh"
 #include "wq_ptx.cuh"
 
 namespace wq {
 
-__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
-  uint64_t v;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
-  return v;
-}
 // Barrier `id` over `count` threads: whether `v` holds for all of them.
 __device__ __forceinline__ bool barrier_and(int id, int count, bool v) {
   uint32_t r;
@@ -91,10 +87,10 @@ __device__ __forceinline__ uint4 convert8(const uint2 &c, uint32_t z1024) {
     // 64 + z from 1024 + z: exact (z <= 15)
     const uint32_t z64 = hsub2_u(z1024, 0x63806380u);  // 960
     const uint32_t x = c.x >> 8;
-    o.x = hsub2_u((c.x & 0x000f000fu) | 0x64006400u, z1024);
-    o.y = hfma16_u((c.x & 0x00f000f0u) | 0x64006400u, z64);
-    o.z = hsub2_u((x & 0x000f000fu) | 0x64006400u, z1024);
-    o.w = hfma16_u((x & 0x00f000f0u) | 0x64006400u, z64);
+    o.x = hsub2_u(plus1024<0x000f000fu>(c.x), z1024);
+    o.y = hfma16_u(plus1024<0x00f000f0u>(c.x), z64);
+    o.z = hsub2_u(plus1024<0x000f000fu>(x), z1024);
+    o.w = hfma16_u(plus1024<0x00f000f0u>(x), z64);
   }
   return o;
 }
