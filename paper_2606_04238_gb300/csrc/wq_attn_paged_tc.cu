@@ -108,6 +108,7 @@ struct Shared {
   // there are any
   uint32_t odd[4][8][16];
   float pm[2][2][kStream], pl[2][2][kStream];  // the halves' maxima and sums
+  int limit[2][kStream];                       // positions that a stream's rows see
 };
 
 // The line of tiles: sequences in order, in a sequence pairs of blocks, the kv head fastest.  A pair has C places, as many
@@ -622,17 +623,16 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
       if (!ok || !w.any) break;
       const int lr = w.split ? row : s * kStream + row;  // the block's row
       const bool in = lr < w.live, busy = lr - lane < w.live;
-      const int tok = (int)by_rep.divide(w.r0 + min(lr, w.live - 1));
-      const int limit = in && w.len > 0 ? w.before + tok + 1 : 0;  // positions that the row sees
+      auto token = [&]() { return (int)by_rep.divide(w.r0 + min(lr, w.live - 1)); };
+      sh.limit[s][row] = in && w.len > 0 ? w.before + token() + 1 : 0;  // (by both halves' threads, the same)
       const int first = w.split ? s : 0, step = w.split ? 2 : 1;
-      const int seen_by_all = w.least, n_tiles = w.n, t0 = w.t0;
       auto out_row = [&](int tok) {
         return reinterpret_cast<__nv_bfloat16 *>(a.o) + ((size_t)(w.q0 + tok) * a.H + w.g * rep + w.r0 + lr - tok * rep) * HD;
       };
       float m = -INFINITY, l = 0.f, c1 = 1.f;
       bool own = false;
-      for (int ti = first; ti < n_tiles; ti += step) {
-        const int ring = (T + ti) & 3, p0 = (t0 + ti) * kTile + 64 * h;
+      for (int ti = first; ti < w.n; ti += step) {
+        const int ring = (T + ti) & 3, p0 = (w.t0 + ti) * kTile + 64 * h;
         ok = wait(&sh.s_full[s], cs & 1);
         ++cs;
         if (!ok && lane == 0) sh.sfail[s] = 1;
@@ -642,7 +642,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
           own = !BF && __any_sync(0xffffffffu, c1 != 1.f);
         }
         // V's exponents of the half's four times 16 positions
-        const bool some = p0 + 64 > seen_by_all;
+        const bool some = p0 + 64 > w.least;
         bool plain = !some && !own;
         if constexpr (!BF) {
           const int4 te4 = *reinterpret_cast<const int4 *>(&sh.te[ring][4 * h]);
@@ -669,7 +669,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
 #pragma unroll
             for (int j = 0; j < 16; ++j) u[j] += sh.td[ring][64 * h + 16 * c + j];
           if (some) {
-            const int n = limit - p0 - 16 * c;
+            const int n = sh.limit[s][row] - p0 - 16 * c;
 #pragma unroll
             for (int j = 0; j < 16; ++j) u[j] = j < n ? u[j] : -INFINITY;
           }
@@ -762,6 +762,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
       }
 
       // ---- the rows' outputs, or their parts
+      const int tok = token();
       if (w.n == 0) {  // not served
         if (in && (s == 0 || !w.split))
 #pragma unroll 1
@@ -786,7 +787,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
       const int c0 = w.c0, cl = w.cl;
       float *pt = a.part + (((size_t)blockIdx.x * 2 + (w.t0 == 0)) * kBlockRows + s * kStream + row) * (HD + 4);
       if (has && busy) {
-        const int least = seen_by_all, first_odd = least / kTile * kTile;
+        const int least = w.least, first_odd = least / kTile * kTile, limit = sh.limit[s][row];
         uint32_t odd = 0;
         if ((w.t0 + w.n) * kTile > least)
 #pragma unroll 1

@@ -172,7 +172,7 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PagePlanA
 //   A CTA takes a token.  HD / 16 lanes take a row, values 8 l .. and HD/2 + 8 l .., so that
 // a value and the one it is rotated with are one lane's.
 template <int HD, int BITS, bool F32>
-__global__ void __launch_bounds__(kPutThreads, 5) qkv_paged_kernel(const QkvPagedArgs a) {
+__global__ void __launch_bounds__(kPutThreads, F32 && BITS != 16 ? 4 : 5) qkv_paged_kernel(const QkvPagedArgs a) {
   constexpr int THREADS = kPutThreads, LPR = HD / 16, GROUPS = THREADS / LPR, U = 2;  // lanes a row, rows a pass, passes in flight
   __shared__ float red[THREADS / 32];
   pdl_wait();
