@@ -328,58 +328,60 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
           if (!any) break;
         }
       if (!ok) sh.fail = 1;
-    } else if (warp == kMmaWarp && elect_one()) {
+    } else if (warp == kMmaWarp) {
+      const uint32_t lead = elect_one();
+      const uint32_t tm0 = __shfl_sync(0xffffffffu, tm, 0);
       bool ok = true;
       int T = 0, seg = 0, cs[2] = {0, 0};
-      auto scores = [&](const Run &w, int s, int t, bool last) {  // S of stream s and tile t
-        ok = mbar_wait(&sh.k_full[(T + t) & 1], (T + t) >> 1 & 1);
+      auto scores = [&](bool split, int s, int t, bool last) {  // S of stream s and tile t
+        ok = wait(&sh.k_full[(T + t) & 1], (T + t) >> 1 & 1);
         if (!ok) return;
         tc_fence_after();
-        const uint64_t q = qd + (uint64_t)(((w.split ? 0 : s) * C::KB) >> 4), k = kd + (uint64_t)((((T + t) & 1) * C::KB) >> 4);
+        const uint64_t q = qd + (uint64_t)(((split ? 0 : s) * C::KB) >> 4), k = kd + (uint64_t)((((T + t) & 1) * C::KB) >> 4);
 #pragma unroll
         for (int ks = 0; ks < HD / 16; ++ks) {
           const uint64_t off = (uint64_t)(((ks / 4) * kBlk + (ks % 4) * 32) >> 4);
-          umma_f16(tm + s * 128, q + off, k + off, idqk, ks > 0);
+          umma_ss_lead(lead, tm0 + s * 128, q + off, k + off, idqk, ks > 0);
         }
-        umma_commit(&sh.s_full[s]);
-        if (w.split || s == 1) umma_commit(&sh.k_empty[(T + t) & 1]);
-        if (last) umma_commit(&sh.q_empty);
+        umma_commit_lead(lead, &sh.s_full[s]);
+        if (split || s == 1) umma_commit_lead(lead, &sh.k_empty[(T + t) & 1]);
+        if (last) umma_commit_lead(lead, &sh.q_empty);
       };
       for (int turn = 0; ok; ++turn) {
         const Run &w = sh.run[turn & 3];
-        ok = mbar_wait(&sh.run_full[turn & 3], turn >> 2 & 1);
+        ok = wait(&sh.run_full[turn & 3], turn >> 2 & 1);
         if (!ok || !w.any) break;
-        const int step = w.split ? 2 : 1;
-        if (w.n > 0) ok = mbar_wait(&sh.q_full, seg & 1);
+        const int n = __shfl_sync(0xffffffffu, w.n, 0), split = __shfl_sync(0xffffffffu, (int)w.split, 0), step = split ? 2 : 1;
+        if (n > 0) ok = wait(&sh.q_full, seg & 1);
         for (int s = 0; s < 2 && ok; ++s) {
-          const int t = w.split ? s : 0;
-          if (t < w.n) scores(w, s, t, w.split ? t == w.n - 1 : s == 1 && w.n == 1);
+          const int t = split ? s : 0;
+          if (t < n) scores(split, s, t, split ? t == n - 1 : s == 1 && n == 1);
         }
-        for (int t = 0; t < w.n && ok; t += step)
+        for (int t = 0; t < n && ok; t += step)
           for (int s = 0; s < 2 && ok; ++s) {
-            const int mine = w.split ? t + s : t;
-            if (mine >= w.n) break;
+            const int mine = split ? t + s : t;
+            if (mine >= n) break;
             const int st = (T + mine) & 1;
-            ok = mbar_wait(&sh.v_full[st], (T + mine) >> 1 & 1) && mbar_wait(&sh.p_full[s], cs[s] & 1);
+            ok = wait(&sh.v_full[st], (T + mine) >> 1 & 1) && wait(&sh.p_full[s], cs[s] & 1);
             if (!ok) break;
             ++cs[s];
             tc_fence_after();
             const uint64_t v = vd + (uint64_t)((st * C::KB) >> 4);
 #pragma unroll
             for (int ks = 0; ks < kTile / 16; ++ks)
-              umma_ts(tm + 256 + s * HD, tm + s * 128 + 8 * ks + (ks < 4 ? 0 : 32), v + (uint64_t)((ks * 2048) >> 4), idpv, t > 0 || ks > 0);
-            if (w.split || s == 1) umma_commit(&sh.v_empty[st]);
+              umma_ts_lead(lead, tm0 + 256 + s * HD, tm0 + s * 128 + 8 * ks + (ks < 4 ? 0 : 32), v + (uint64_t)((ks * 2048) >> 4), idpv, t > 0 || ks > 0);
+            if (split || s == 1) umma_commit_lead(lead, &sh.v_empty[st]);
             const int nx = mine + step;
-            if (nx < w.n)
-              scores(w, s, nx, nx == w.n - 1 && (w.split || s == 1));
+            if (nx < n)
+              scores(split, s, nx, nx == n - 1 && (split || s == 1));
             else
-              umma_commit(&sh.o_full[s]);
+              umma_commit_lead(lead, &sh.o_full[s]);
           }
-        T += w.n;
-        seg += w.n > 0;
-        mbar_arrive(&sh.run_empty[turn & 3]);
+        T += n;
+        seg += n > 0;
+        done(turn);
       }
-      if (!ok) sh.fail = 1;
+      if (!ok && lane == 0) sh.fail = 1;
     }
     __syncwarp();
   } else if (warp >= kConvWarp) {
@@ -683,17 +685,17 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
           constexpr bool PLAIN = decltype(is_plain)::value;
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
-            float u[16];
-            float sum = 0.f, sum_l = 0.f;
-            uint32_t p[8];
-            tmem_ld16(ts + 64 * h + 16 * c, *reinterpret_cast<uint32_t(*)[16]>(&u));
-            tmem_ld_wait16(u);
             const int t = BF ? 0 : sh.te[ring][4 * h + c];
             const bool spread = !PLAIN && t == kOwn;
-            const float te = spread ? 0.f : (float)t, ms = m == -INFINITY ? 0.f : te - m;
-            exponents(u, c, ms, spread, PLAIN);
+            const float te = spread ? 0.f : (float)t;
+            uint32_t p[8];
+            float sum, sum_l;
 #pragma unroll 1
-            for (int again = 0; again < 2; ++again) {
+            for (bool raised = false;; raised = true) {
+              float u[16];
+              tmem_ld16(ts + 64 * h + 16 * c, *reinterpret_cast<uint32_t(*)[16]>(&u));
+              tmem_ld_wait16(u);
+              exponents(u, c, m == -INFINITY ? 0.f : te - m, spread, PLAIN);
               uint64_t s2[2] = {0, 0};
               sum_l = 0.f;
 #pragma unroll
@@ -708,18 +710,18 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
               unpack_f32x2(add_f32x2(s2[0], s2[1]), x, y);
               sum = x + y;
               const bool up = sum >= kMostSum || (m == -INFINITY && sum > 0.f);
-              if (again || !__any_sync(0xffffffffu, up)) break;
+              if (raised || !__any_sync(0xffffffffu, up)) break;
+              // (rare: the scores once more)
+              tmem_ld16(ts + 64 * h + 16 * c, *reinterpret_cast<uint32_t(*)[16]>(&u));
+              tmem_ld_wait16(u);
+              exponents(u, c, te, spread, false);
               float mx = -INFINITY;
 #pragma unroll
               for (int j = 0; j < 16; ++j) mx = fmaxf(mx, u[j]);
-              const float was = m == -INFINITY ? 0.f : te - m;
-              const float mn = up ? ceilf(mx - was + te) - C::LIFT : m, al = raise_factor(m, mn);
+              const float mn = up ? ceilf(mx) - C::LIFT : m, al = raise_factor(m, mn);
               if (c > 0) rescale_p<BF>(ts + 64 * h, c, al);
               part *= al;
               m = mn;
-              const float now = m == -INFINITY ? 0.f : te - m;
-#pragma unroll
-              for (int j = 0; j < 16; ++j) u[j] += now - was;
             }
             part = spread ? part + sum_l : BF ? part + sum : fmaf(sum, pow2i(-t), part);
             tmem_st8(ts + 64 * h + 8 * c, p);

@@ -346,6 +346,14 @@ def test_long(bits, nq):
 
 
 @pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("h,kv,hd", [(8, 4, 128), (6, 2, 64)])
+def test_many_tiles_a_run(h, kv, hd, bits):
+    """Runs of tens of tiles, over ends of blocks: short chunks (both streams with the same rows) and longer ones."""
+    nq = [9] * 24 + [200, 131, 60, 300]
+    run_attn(nq, [4001 + 37 * i for i in range(24)] + [5000, 3000, 4096, 2500], h, kv, hd, bits, 64, seed=3)
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
 @pytest.mark.parametrize("scale", [0.0, -0.2, 3.0, 1e-30])
 def test_scales(bits, scale):
     run_attn([1, 2, 90], [200, 300, 100], 8, 2, 64, bits, 16, scale=scale, seed=3)
