@@ -1768,8 +1768,22 @@ wq_status attn_paged_impl(const void *q, int m, int max_q, int n_heads, const wq
   a.counters = static_cast<int *>(counters);
   a.part = static_cast<float *>(part);
   a.o = o;
-  const bool tc = (long long)max_q * (n_heads / pool->n_kv) > 16;
-  cudaError_t e = tc ? launch_attn_paged_tc(a, pool->head_dim, pool->bits, sms, s) : launch_attn_paged(a, pool->head_dim, pool->bits, sms, s);
+  // Up to 16 rows (query tokens x query heads of a kv head) a sequence the mma.sync kernel, above the tcgen05 kernel.  A
+  // batch that may have both kinds of sequences takes both, each its own: 14 decode steps over 1,500 to 3,000 positions
+  // of 8 bits beside two chunks of 250 tokens take MIXED_BOTH us, on the tcgen05 kernel alone MIXED_TC.
+  const int rep = n_heads / pool->n_kv, few = std::max(8, rep) / rep;  // tokens of a sequence that is left to mma.sync beside others
+  a.least_q = 0, a.most_q = INT32_MAX;
+  cudaError_t e = cudaSuccess;
+  if ((long long)max_q * rep <= 16) {
+    e = launch_attn_paged(a, pool->head_dim, pool->bits, sms, s);
+  } else {
+    if (batch > 1 && m < (long long)batch * max_q) {
+      a.most_q = few;
+      e = launch_attn_paged(a, pool->head_dim, pool->bits, sms, s);
+      a.least_q = few + 1, a.most_q = INT32_MAX;
+    }
+    if (e == cudaSuccess) e = launch_attn_paged_tc(a, pool->head_dim, pool->bits, sms, s);
+  }
   if (e != cudaSuccess) return cuda_fail(e, "paged attention launch");
   return ok();
 }

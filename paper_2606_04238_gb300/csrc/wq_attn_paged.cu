@@ -639,7 +639,7 @@ cudaError_t launch_t(const AttnPagedArgs &a, int num_sms, cudaStream_t s) {
 }  // namespace
 
 cudaError_t launch_attn_paged(const AttnPagedArgs &a, int hd, int bits, int num_sms, cudaStream_t s) {
-  const bool one = (long long)a.max_q * (a.H / a.Hkv) <= 8;
+  const bool one = (long long)std::min(a.max_q, a.most_q) * (a.H / a.Hkv) <= 8;
 #define WQ_PAGED(HD, BITS) \
   if (hd == HD && bits == BITS) return one ? launch_t<HD, BITS, 1>(a, num_sms, s) : launch_t<HD, BITS, 2>(a, num_sms, s);
   WQ_PAGED(128, 16) WQ_PAGED(128, 8) WQ_PAGED(128, 4) WQ_PAGED(64, 16) WQ_PAGED(64, 8) WQ_PAGED(64, 4)

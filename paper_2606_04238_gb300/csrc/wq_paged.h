@@ -57,6 +57,7 @@ struct AttnPagedArgs {
   const int *cu, *kv_lens;  // [batch + 1], [batch]
   const int *tables;        // [batch][max_pages]
   int m, max_q, batch, H, Hkv, n_pages, shift, max_pages;
+  int least_q, most_q;      // query rows of the sequences that the launch takes
   float scale;              // of the scores, times log2(e)
   float *part;              // [CTA][2][16][HD + 4]
   int *counters;            // [CTA], zero between calls

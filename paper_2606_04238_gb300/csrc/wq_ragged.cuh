@@ -7,7 +7,7 @@
 namespace wq {
 
 // A sequence's first row, rows and positions; no rows where a row offset or length is out of
-// range.  len 0: a request that is not served, whose rows are zeros.
+// range, or where the launch does not take sequences of so many rows.  len 0: a request that is not served, whose rows are zeros.
 struct Seq {
   int q0, nq, len;
 };
@@ -21,7 +21,7 @@ __device__ __forceinline__ Seq get_seq(const AttnPagedArgs &a, int b, bool &bad)
   const bool ok = s.q0 >= 0 && q1 >= s.q0 && q1 <= a.m && s.nq <= a.max_q && (none || (s.len >= s.nq && s.len <= a.max_pages << a.shift));
   bad |= !ok;
   if (none) s.len = 0;
-  if (!ok) s.nq = 0;
+  if (!ok || s.nq < a.least_q || s.nq > a.most_q) s.nq = 0;
   return s;
 }
 
