@@ -11,9 +11,10 @@
 //               in shared memory as it lies in a page (MN-major).
 // The MMA warp issues P V of one stream and its next S while the other's softmax runs.  Up to
 // 128 rows (a block's rest, short chunks) both streams have the same rows and take the tiles
-// in turn; their results are added up at the end.  21 warps: 0-15 softmax, 16-17 K and
-// 18-19 V (codes through registers to binary16 in the 128-byte swizzled layout; a bf16 pool by
-// cp.async; all four the queries of the next block), 20 the MMAs.
+// in turn; their results are added up at the end.  28 warps: 0-15 softmax; 16-23 the block's
+// queries, then K and V, 16 positions of a tile each (codes through registers to binary16 in the
+// 128-byte swizzled layout; a bf16 pool by cp.async); 24 the MMAs; 25 the runs of tiles, four
+// ahead; 26-27 only hold the registers that the softmax warps take over.
 //
 // K's operands are code - z, exact, its scales factors of the scores; V's are (code - z) s 2^-t
 // rounded to binary16, t one for 16 positions, or, where their scales span more than 2^8, one for

@@ -435,6 +435,33 @@ def test_not_served_and_out_of_range():
             check(o[cu[b]:cu[b + 1]], ref[cu[b]:cu[b + 1]], bound[cu[b]:cu[b + 1]])
 
 
+def test_few_and_many_rows_in_a_batch():
+    """Sequences of few rows beside longer ones: each served once, those not served zeros, wrong ones left, rows behind the last left."""
+    h, kv, hd, page = 8, 2, 128, 16
+    nq = [1, 300, 0, 2, 3, 1, 40, 1, 90, 2, 130, 4]
+    lens = [70, 300, 5, 2, 200, -1, 41, 400, -1, 1, 129, 900]  # (the last three: shorter than their rows, twice; a long one)
+    for bits in (16, 8, 4):
+        cu, tables, n_pages = ragged(nq, [max(x, n, 1) for x, n in zip(lens, nq)], page, 3)
+        pool = a_pool(n_pages, kv, page, hd, bits)
+        q = randn(cu[-1] + 5, h, hd, seed=6, dtype=BF)
+        t2 = tables.clone()
+        t2[3, 0], t2[6, 1] = n_pages, -1  # pages that the pool does not have
+        o = torch.full_like(q, 7.0)
+        wq.attn_paged(q, i32(*cu), i32(*lens), t2, pool, max_q=300, o=o)
+        assert status() == -1 and status() == 0
+        good = [max(x, n) for x, n in zip(lens, nq)]
+        ref, bound = attn_ref(q[:cu[-1]], cu, good, tables, pool, hd ** -0.5)
+        for b, (n, length) in enumerate(zip(nq, lens)):
+            at = slice(cu[b], cu[b + 1])
+            if length < 0:
+                assert bool((o[at] == 0).all())
+            elif length < n:
+                assert bool((o[at] == 7).all())
+            elif b not in (3, 6):
+                check(o[at], ref[at], bound[at], f"{bits} {b}")
+        assert bool((o[cu[-1]:] == 7).all())
+
+
 def test_shared_pages_and_zero_rows():
     """Two requests over one prefix; a pool of zeros and rows of zeros among others."""
     h, kv, hd, page = 8, 2, 128, 16

@@ -1,7 +1,7 @@
-"""The order of waits of the tcgen05 paged-attention kernel (wq_attn_paged_tc.cu), as a model on the CPU: the MMA warp,
-the converting warps (as one) and the two softmax streams run their programs' waits and arrivals over every mix of blocks,
-in all orders that a scheduler may choose at random, and must come to their ends; a stage is only written when all that reads
-it is done.  Barriers are mbarriers: a wait names the parity of a phase.
+"""The order of waits of the tcgen05 paged-attention kernel (wq_attn_paged_tc.cu), as a model on the CPU: the warp that plans,
+the MMA warp, the converting warps (as one) and the two softmax streams run their programs' waits and arrivals over every mix
+of blocks, in orders that a scheduler may choose at random, and must come to their ends; a stage is only written when all that
+reads it is done.  Barriers are mbarriers: a wait names the parity of a phase.
 """
 import random
 
@@ -14,6 +14,7 @@ class Bar:
 
     def arrive(self):
         self.here += 1
+        assert self.here <= self.count
         if self.here == self.count:
             self.here = 0
             self.phase += 1
@@ -23,107 +24,151 @@ class Bar:
 
 
 def bars():
-    two = lambda n: [Bar(n), Bar(n)]  # noqa: E731
-    return dict(q_full=Bar(1), q_empty=Bar(1), k_full=two(1), k_empty=two(1), v_full=two(1), v_empty=two(1),
-                s_full=[two(1), two(1)], p_full=[two(1), two(1)], o_full=two(1))
+    ring = lambda k, n: [Bar(n) for _ in range(k)]  # noqa: E731
+    return dict(q_full=Bar(1), q_empty=Bar(1), k_full=ring(2, 1), k_empty=ring(2, 1), v_full=ring(2, 1), v_empty=ring(2, 1),
+                s_full=ring(2, 1), p_full=ring(2, 1), o_full=ring(2, 1), run_full=ring(4, 1), run_empty=ring(4, 4))
 
 
-def conv(runs, B, bf16, state):
+def plan(runs, B, state):
+    for turn in range(len(runs) + 1):
+        if turn >= 4:
+            yield B["run_empty"][turn & 3], (turn >> 2) + 1 & 1
+        state["run"][turn & 3] = runs[turn] if turn < len(runs) else None
+        B["run_full"][turn & 3].arrive()
+
+
+def each_run(B, state):
+    """The runs as a role reads them: (wait) or (None, run)."""
+    turn = 0
+    while True:
+        yield B["run_full"][turn & 3], turn >> 2 & 1
+        if state["run"][turn & 3] is None:
+            return
+        yield None, state["run"][turn & 3]
+        assert state["run"][turn & 3] is not None
+        B["run_empty"][turn & 3].arrive()
+        turn += 1
+
+
+def conv(B, bf16, state):
     T = seg = 0
-    for n, split in runs:
+    for got, run in each_run(B, state):
+        if got is not None:
+            yield got, run
+            continue
+        n, split = run
+        if n == 0:
+            continue
         if seg > 0:
             yield B["q_empty"], (seg - 1) & 1
+        assert state["q"] == 0, "queries overwritten"
+        state["q"] = n if split else 2 * n
         B["q_full"].arrive()
         for ti in range(n):
             st = (T + ti) & 1
-            if T + ti >= 2:
-                yield B["k_empty"][st], ((T + ti) >> 1) + 1 & 1
-            assert state["k"][st] == 0, "K overwritten"
-            state["k"][st] = 1 if split else 2
-            if bf16 and ti > 0:
-                B["v_full"][st ^ 1].arrive()
-            B["k_full"][st].arrive()
-            if T + ti >= 2:
-                yield B["v_empty"][st], ((T + ti) >> 1) + 1 & 1
-            assert state["v"][st] == 0, "V overwritten"
-            state["v"][st] = 1 if split else 2
-            if not bf16:
-                B["v_full"][st].arrive()
+            for x in "kv":
+                if T + ti >= 2:
+                    yield B[x + "_empty"][st], ((T + ti) >> 1) + 1 & 1
+                assert state[x][st] == 0, "a stage overwritten"
+                state[x][st] = 1 if split else 2
+                if not bf16:
+                    B[x + "_full"][st].arrive()
+                elif ti > 0:  # (the copies of the tile before have landed)
+                    B[x + "_full"][st ^ 1].arrive()
         if bf16:
+            B["k_full"][(T + n - 1) & 1].arrive()
             B["v_full"][(T + n - 1) & 1].arrive()
         T += n
         seg += 1
 
 
-def mma(runs, B, state):
+def mma(B, state):
     T, seg, cs = 0, 0, [0, 0]
-    for n, split in runs:
+
+    def scores(s, t, split, last):
+        st = (T + t) & 1
+        yield B["k_full"][st], (T + t) >> 1 & 1
+        assert state["k"][st] > 0 and state["s"][s] == 0
+        state["k"][st] -= 1
+        state["q"] -= 1
+        state["s"][s] = 1
+        B["s_full"][s].arrive()
+        if split or s == 1:
+            B["k_empty"][st].arrive()
+        if last:
+            B["q_empty"].arrive()
+
+    for got, run in each_run(B, state):
+        if got is not None:
+            yield got, run
+            continue
+        n, split = run
         step = 2 if split else 1
-
-        def scores(s, t, hh):
-            yield B["k_full"][(T + t) & 1], (T + t) >> 1 & 1
-            B["s_full"][s][hh].arrive()
-            if hh == 1:
-                state["k"][(T + t) & 1] -= 1
-            if hh == 1 and (split or s == 1):
-                B["k_empty"][(T + t) & 1].arrive()
-                if t == n - 1:
-                    B["q_empty"].arrive()
-
-        yield B["q_full"], seg & 1
-        for i in range(4):
-            s, hh = (i // 2, i % 2) if split else (i % 2, i // 2)
+        if n > 0:
+            yield B["q_full"], seg & 1
+        for s in range(2):
             t = s if split else 0
             if t < n:
-                yield from scores(s, t, hh)
+                yield from scores(s, t, split, t == n - 1 if split else s == 1 and n == 1)
         for t in range(0, n, step):
-            for i in range(4):
-                s, hh = (i // 2, i % 2) if split else (i % 2, i // 2)
+            for s in range(2):
                 mine = t + s if split else t
                 if mine >= n:
-                    continue
+                    break
                 st = (T + mine) & 1
                 yield B["v_full"][st], (T + mine) >> 1 & 1
-                yield B["p_full"][s][hh], cs[s] & 1
-                cs[s] += hh
-                if hh == 1:
-                    state["v"][st] -= 1
-                if hh == 1 and (split or s == 1):
+                yield B["p_full"][s], cs[s] & 1
+                cs[s] += 1
+                assert state["v"][st] > 0
+                state["v"][st] -= 1
+                if split or s == 1:
                     B["v_empty"][st].arrive()
-                if mine + step < n:
-                    yield from scores(s, mine + step, hh)
-                elif hh == 1:
+                nx = mine + step
+                if nx < n:
+                    yield from scores(s, nx, split, nx == n - 1 and (split or s == 1))
+                else:
                     B["o_full"][s].arrive()
         T += n
-        seg += 1
+        seg += n > 0
 
 
-def softmax(s, runs, B, meet):
-    cs = os = 0
-    for r, (n, split) in enumerate(runs):
-        for ti in range(s if split else 0, n, 2 if split else 1):
-            for hh in range(2):
-                yield B["s_full"][s][hh], cs & 1
-                cs += hh
-                B["p_full"][s][hh].arrive()
-        if (s if split else 0) < n:
+def softmax(s, B, state, meet):
+    cs = os = blocks = 0
+    for got, run in each_run(B, state):
+        if got is not None:
+            yield got, run
+            continue
+        n, split = run
+        if n == 0:
+            continue
+        first = s if split else 0
+        for _ in range(first, n, 2 if split else 1):
+            yield B["s_full"][s], cs & 1
+            cs += 1
+            assert state["s"][s] == 1
+            state["s"][s] = 0
+            B["p_full"][s].arrive()
+        if first < n:
             yield B["o_full"][s], os & 1
             os += 1
-        meet[s] = r + 1  # the barrier of both streams at a block's end
-        yield None, r + 1
+        blocks += 1
+        meet[s] = blocks  # the barrier of both streams at a block's end
+        yield None, blocks
 
 
 @pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("seed", range(40))
 def test_every_role_comes_to_its_end(bf16, seed):
     rng = random.Random(seed)
-    runs = [(rng.choice([1, 1, 2, 3, 4, 5, 6, 7, 12, 31]), rng.random() < 0.5) for _ in range(rng.choice([1, 2, 5, 12]))]
+    runs = [(rng.choice([0, 1, 1, 2, 3, 4, 5, 6, 7, 12, 31]), rng.random() < 0.5) for _ in range(rng.choice([1, 2, 5, 12]))]
     for _ in range(5):
-        B, meet, state = bars(), [0, 0], dict(k=[0, 0], v=[0, 0])
-        roles = [conv(runs, B, bf16, state), mma(runs, B, state), softmax(0, runs, B, meet), softmax(1, runs, B, meet)]
+        B, meet = bars(), [0, 0]
+        state = dict(q=0, k=[0, 0], v=[0, 0], s=[0, 0], run=[None] * 4)
+        roles = [plan(runs, B, state), conv(B, bf16, state), mma(B, state), softmax(0, B, state, meet), softmax(1, B, state, meet)]
         waits = {i: next(g, "end") for i, g in enumerate(roles)}
         while any(w != "end" for w in waits.values()):
             ready = [i for i, w in waits.items() if w != "end" and (min(meet) >= w[1] if w[0] is None else w[0].passed(w[1]))]
             assert ready, f"stuck: {runs}"
             i = rng.choice(ready)
             waits[i] = next(roles[i], "end")
+        assert state["q"] == 0 and state["k"] == [0, 0] and state["v"] == [0, 0] and state["s"] == [0, 0]
