@@ -557,7 +557,9 @@ wq_status wq_paged_read(const wq_kv_cache *pool, const int32_t *slots, int m, vo
  *   in the device status.
  *   n_heads / n_kv <= 16, batch <= 2048, m <= 2^18, max_pages page <= 2^31 - 1024.
  *   Roundings: each probability once to 16 bits (binary16 over a quantized pool, 2^-11 of
- *   its term at most; bf16 over a bf16 pool, 2^-8), and o.  Everything else is fp32.
+ *   its term at most; bf16 over a bf16 pool, 2^-8), and o; where max_q n_heads / n_kv > 16 also
+ *   the values of V of a quantized pool, times a power of two, to binary16 (2^-11).  Everything
+ *   else is fp32.
  * Workspace: wq_attn_paged_workspace_bytes for up to `batch` sequences and m rows, zero-filled
  * before first use (wq_workspace_init).
  */

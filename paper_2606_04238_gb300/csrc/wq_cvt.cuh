@@ -1,5 +1,5 @@
-// wq_cvt.cuh -- conversions between packed 16-bit halves and fp32, and the exponential of
-// base 2, as the attention and KV-cache kernels use them.
+// wq_cvt.cuh -- conversions between packed 16-bit halves and fp32, the exponential of base
+// 2, packed fp32 sums and waits for cp.async, as the attention and KV-cache kernels use them.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -19,6 +19,17 @@ __device__ __forceinline__ uint32_t pack_bf2(float a, float b) {
 __device__ __forceinline__ uint32_t pack_h2(float a, float b) {
   const __half2 v = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t *>(&v);
+}
+// Two fp32 values each of a and b, added.
+__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
+  uint64_t v;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+  return v;
+}
+// Waits until at most N of this thread's cp.async groups are in flight.
+template <int N>
+__device__ __forceinline__ void cp_async_wait_group() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 // Two binary16 operations on packed halves.
 __device__ __forceinline__ uint32_t hsub2_u(uint32_t a, uint32_t b) {
