@@ -69,6 +69,7 @@ constexpr int kTmemCols = 512;             // S / P of the streams 0.., 128..; O
 constexpr int kQueryShift = 7;
 constexpr int kSpread = 8;                 // exponents that V's scales of 16 positions may span with one power of two for all
 constexpr int kOwn = 1 << 16;
+constexpr int kRing = 8;
 constexpr float kMostSum = 32768.f;        // of 16 p; binary16 ends at 65504
 
 template <int HD, int BITS>
@@ -77,7 +78,9 @@ struct Cfg {
   static constexpr int KB = NB * kBlk;           // bytes of one operand tile
   static constexpr int CH = HD / 8;              // 16-byte chunks a row of 16-bit values
   static constexpr int ROW = HD * BITS / 8;
-  static constexpr int SMEM = 1024 + 6 * KB;     // Q of both streams, two stages of K and of V
+  // stages of K and V tiles: heads of 64 leave room for four (the next tiles' conversion then waits for no product)
+  static constexpr unsigned STAGES = HD == 64 ? 4 : 2;
+  static constexpr int SMEM = 1024 + (2 + 2 * (int)STAGES) * KB;  // Q of both streams, K and V
   // codes: 16-byte pieces a row, pieces of a row in one load of a warp, rows of it, loads a row, loads of a warp's 16 rows
   static constexpr int PPR = ROW / 16, PP = PPR < 4 ? PPR : 4, RPI = 32 / PP, SPR = PPR / PP, NI = 16 * PPR / 32;
   static_assert(RPI > 0 && SPR > 0 && NI > 0, "");
@@ -94,16 +97,16 @@ struct Run {
 };
 
 struct Shared {
-  uint64_t q_full, q_empty, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], o_full[2];
+  uint64_t q_full, q_empty, k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[2], p_full[2], o_full[2];
   uint64_t run_full[4], run_empty[4];
   Run run[4];
   uint32_t tmem;
   int fail, sfail[2], last;
-  // of a tile, four tiles deep (a tile's are written when S of the one two before is done, whose softmax has then
-  // ended for the tile four before): K's scales times the score scale and 2^-kQueryShift, V's exponents t
-  __align__(16) float sk[4][kTile];
-  __align__(16) int te[4][8];  // by 16 positions; kOwn: their rows have their own
-  __align__(16) float td[4][kTile], tw[4][kTile];
+  // of a tile, eight tiles deep (a tile's are written when S of the one STAGES tiles before is done, whose softmax has then
+  // ended for the tile two before that): K's scales times the score scale and 2^-kQueryShift, V's exponents t
+  __align__(16) float sk[kRing][kTile];
+  __align__(16) int te[kRing][8];  // by 16 positions; kOwn: their rows have their own
+  __align__(16) float td[kRing][kTile], tw[kRing][kTile];
   float qf[4][kBlockRows];         // what a row's own power of two differs from 2^kQueryShift
   // of a block, by converting warp: positions from its first masked tile on (384 at most) whose V is not finite, and whether
   // there are any
@@ -261,7 +264,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
   constexpr bool BF = BITS == 16;
   extern __shared__ uint8_t paged_dyn[];
   __shared__ Shared sh;
-  uint8_t *qbuf = paged_dyn + (1024 - (smem_addr(paged_dyn) & 1023)) % 1024, *kbuf = qbuf + 2 * C::KB, *vbuf = kbuf + 2 * C::KB;
+  uint8_t *qbuf = paged_dyn + (1024 - (smem_addr(paged_dyn) & 1023)) % 1024, *kbuf = qbuf + 2 * C::KB, *vbuf = kbuf + C::STAGES * C::KB;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int page = 1 << a.shift;
   if (warp == kMmaWarp) {
@@ -270,16 +273,16 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
       mbar_init(&sh.q_full, kConv / 32);
       mbar_init(&sh.q_empty, 1);
       for (int i = 0; i < 2; ++i) {
-        mbar_init(&sh.k_full[i], kConv / 32);
-        mbar_init(&sh.v_full[i], kConv / 32);
-        mbar_init(&sh.k_empty[i], 1);
-        mbar_init(&sh.v_empty[i], 1);
         mbar_init(&sh.s_full[i], 1);
         mbar_init(&sh.p_full[i], 8);
         mbar_init(&sh.o_full[i], 1);
         sh.sfail[i] = 0;
       }
       for (int i = 0; i < 4; ++i) {
+        mbar_init(&sh.k_full[i], kConv / 32);
+        mbar_init(&sh.v_full[i], kConv / 32);
+        mbar_init(&sh.k_empty[i], 1);
+        mbar_init(&sh.v_empty[i], 1);
         mbar_init(&sh.run_full[i], 1);
         mbar_init(&sh.run_empty[i], kMmaWarp + 1);
       }
@@ -333,19 +336,17 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
       const uint32_t lead = elect_one();
       const uint32_t tm0 = __shfl_sync(0xffffffffu, tm, 0);
       bool ok = true;
-      int T = 0, seg = 0, cs[2] = {0, 0};
+      int seg = 0, cs[2] = {0, 0};
+      unsigned T = 0;
       auto scores = [&](bool split, int s, int t, bool last) {  // S of stream s and tile t
-        ok = wait(&sh.k_full[(T + t) & 1], (T + t) >> 1 & 1);
-        if (!ok) return;
-        tc_fence_after();
-        const uint64_t q = qd + (uint64_t)(((split ? 0 : s) * C::KB) >> 4), k = kd + (uint64_t)((((T + t) & 1) * C::KB) >> 4);
+        const uint64_t q = qd + (uint64_t)(((split ? 0 : s) * C::KB) >> 4), k = kd + (uint64_t)(((T + t) % C::STAGES * C::KB) >> 4);
 #pragma unroll
         for (int ks = 0; ks < HD / 16; ++ks) {
           const uint64_t off = (uint64_t)(((ks / 4) * kBlk + (ks % 4) * 32) >> 4);
           umma_ss_lead(lead, tm0 + s * 128, q + off, k + off, idqk, ks > 0);
         }
         umma_commit_lead(lead, &sh.s_full[s]);
-        if (split || s == 1) umma_commit_lead(lead, &sh.k_empty[(T + t) & 1]);
+        if (split || s == 1) umma_commit_lead(lead, &sh.k_empty[(T + t) % C::STAGES]);
         if (last) umma_commit_lead(lead, &sh.q_empty);
       };
       for (int turn = 0; ok; ++turn) {
@@ -356,14 +357,21 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
         if (n > 0) ok = wait(&sh.q_full, seg & 1);
         for (int s = 0; s < 2 && ok; ++s) {
           const int t = split ? s : 0;
-          if (t < n) scores(split, s, t, split ? t == n - 1 : s == 1 && n == 1);
+          if (t >= n) break;
+          ok = wait(&sh.k_full[(T + t) % C::STAGES], (T + t) / C::STAGES & 1);
+          if (!ok) break;
+          tc_fence_after();
+          scores(split, s, t, split ? t == n - 1 : s == 1 && n == 1);
         }
         for (int t = 0; t < n && ok; t += step)
           for (int s = 0; s < 2 && ok; ++s) {
             const int mine = split ? t + s : t;
             if (mine >= n) break;
-            const int st = (T + mine) & 1;
-            ok = wait(&sh.v_full[st], (T + mine) >> 1 & 1) && wait(&sh.p_full[s], cs[s] & 1);
+            const unsigned st = (T + mine) % C::STAGES;
+            const int nx = mine + step;
+            // (of split blocks the converting warps may wait for this tile's products before they hand K over)
+            if (!split && nx < n) ok = wait(&sh.k_full[(T + nx) % C::STAGES], (T + nx) / C::STAGES & 1);
+            ok = ok && wait(&sh.v_full[st], (T + mine) / C::STAGES & 1) && wait(&sh.p_full[s], cs[s] & 1);
             if (!ok) break;
             ++cs[s];
             tc_fence_after();
@@ -372,7 +380,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
             for (int ks = 0; ks < kTile / 16; ++ks)
               umma_ts_lead(lead, tm0 + 256 + s * HD, tm0 + s * 128 + 8 * ks + (ks < 4 ? 0 : 32), v + (uint64_t)((ks * 2048) >> 4), idpv, t > 0 || ks > 0);
             if (split || s == 1) umma_commit_lead(lead, &sh.v_empty[st]);
-            const int nx = mine + step;
+            if (split && nx < n) {
+              ok = wait(&sh.k_full[(T + nx) % C::STAGES], (T + nx) / C::STAGES & 1);
+              if (!ok) break;
+              tc_fence_after();
+            }
             if (nx < n)
               scores(split, s, nx, nx == n - 1 && (split || s == 1));
             else
@@ -391,7 +403,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
     const int ct = tid - 32 * kConvWarp, cw = ct >> 5;
     const uint8_t *const kc = reinterpret_cast<const uint8_t *>(a.kc), *const vc = reinterpret_cast<const uint8_t *>(a.vc);
     bool ok = true;
-    int T = 0, seg = 0;
+    int seg = 0;
+    unsigned T = 0;
     for (int turn = 0; ok; ++turn) {
       const Run &w = sh.run[turn & 3];
       ok = wait(&sh.run_full[turn & 3], turn >> 2 & 1);
@@ -483,27 +496,27 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
           }
         };
         for (int ti = 0; ti < n; ++ti) {
-          const int st = (T + ti) & 1;
+          const unsigned st = (T + ti) % C::STAGES, last = (T + ti - 1) % C::STAGES;
           const uint32_t base = base_of(id0, ti);
           id0 = id1;
           id1 = load_id(ti + 2);
-          if (T + ti >= 2) ok = wait(&sh.k_empty[st], ((T + ti) >> 1) + 1 & 1);
+          if (T + ti >= C::STAGES) ok = wait(&sh.k_empty[st], (T + ti) / C::STAGES + 1 & 1);
           if (!ok) break;
           copy(kc, kbuf + st * C::KB, base, ti);
           if (ti > 0) {  // K of the tile before has landed, all but the last two groups have
             cp_async_wait_group<2>();
-            hand_over(&sh.k_full[st ^ 1]);
+            hand_over(&sh.k_full[last]);
           }
-          if (T + ti >= 2) ok = wait(&sh.v_empty[st], ((T + ti) >> 1) + 1 & 1);
+          if (T + ti >= C::STAGES) ok = wait(&sh.v_empty[st], (T + ti) / C::STAGES + 1 & 1);
           if (!ok) break;
           copy(vc, vbuf + st * C::KB, base, ti);
           if (ti > 0) {
             cp_async_wait_group<2>();
-            clean(vbuf + (st ^ 1) * C::KB, ti - 1);
-            hand_over(&sh.v_full[st ^ 1]);
+            clean(vbuf + last * C::KB, ti - 1);
+            hand_over(&sh.v_full[last]);
           }
         }
-        const int st = (T + n - 1) & 1;
+        const unsigned st = (T + n - 1) % C::STAGES;
         if (ok) {
           cp_async_wait_group<1>();
           hand_over(&sh.k_full[st]);
@@ -538,7 +551,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
         fetch(kc, rk, b1);
         fetch(vc, rv, b1);
         for (int ti = 0; ti < n; ++ti) {
-          const int st = (T + ti) & 1, ring = (T + ti) & 3, p0 = p1 + ti * kTile;
+          const unsigned st = (T + ti) % C::STAGES, ring = (T + ti) % kRing, p0 = p1 + ti * kTile;
           b1 = base_of(id1, ti + 1);
           const uint32_t m1 = fetch_meta(b1);
           id1 = load_id(ti + 2);
@@ -556,7 +569,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
           const float s0 = half_lo(m0);
           const __half2 z = __hadd2(__half2half2(__ushort_as_half((unsigned short)(in ? m0 >> 16 : 0u))), __float2half2_rn(1024.f));
           uint32_t zs = *reinterpret_cast<const uint32_t *>(&z);
-          if (T + ti >= 2) ok = wait(&sh.k_empty[st], ((T + ti) >> 1) + 1 & 1);
+          if (T + ti >= C::STAGES) ok = wait(&sh.k_empty[st], (T + ti) / C::STAGES + 1 & 1);
           if (!ok) break;
           if (lane < 16) {
             sh.sk[ring][16 * cw + pl] = s0 * qscale;
@@ -586,7 +599,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
           }
           hand_over(&sh.k_full[st]);
           fetch(kc, rk, b1);
-          if (T + ti >= 2) ok = wait(&sh.v_empty[st], ((T + ti) >> 1) + 1 & 1);
+          if (T + ti >= C::STAGES) ok = wait(&sh.v_empty[st], (T + ti) / C::STAGES + 1 & 1);
           if (!ok) break;
 #pragma unroll
           for (int k = 0; k < C::NI; ++k) {
@@ -616,7 +629,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
     const int s = warp / 8, h = warp / 4 % 2, row = tid % kStream;
     const uint32_t tw = tm + ((uint32_t)(warp % 4 * 32) << 16), ts = tw + s * 128, to = tw + 256 + s * HD;
     bool ok = true;
-    int T = 0, seg = 0, cs = 0, os = 0;
+    int seg = 0, cs = 0, os = 0;
+    unsigned T = 0;
     auto sync_stream = [&](bool v) { return barrier_and(1 + s, 256, v); };
     for (int turn = 0; ok; ++turn) {
       const Run &w = sh.run[turn & 3];
@@ -635,7 +649,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
       float m = -INFINITY, l = 0.f, c1 = 1.f;
       bool own = false;
       for (int ti = first; ti < w.n; ti += step) {
-        const int ring = (T + ti) & 3, p0 = (w.t0 + ti) * kTile + 64 * h;
+        const int ring = (T + ti) % kRing, p0 = (w.t0 + ti) * kTile + 64 * h;
         ok = wait(&sh.s_full[s], cs & 1);
         ++cs;
         if (!ok && lane == 0) sh.sfail[s] = 1;

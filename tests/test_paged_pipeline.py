@@ -23,10 +23,10 @@ class Bar:
         return self.phase & 1 != parity
 
 
-def bars():
+def bars(stages):
     ring = lambda k, n: [Bar(n) for _ in range(k)]  # noqa: E731
-    return dict(q_full=Bar(1), q_empty=Bar(1), k_full=ring(2, 1), k_empty=ring(2, 1), v_full=ring(2, 1), v_empty=ring(2, 1),
-                s_full=ring(2, 1), p_full=ring(2, 1), o_full=ring(2, 1), run_full=ring(4, 1), run_empty=ring(4, 4))
+    return dict(q_full=Bar(1), q_empty=Bar(1), k_full=ring(stages, 1), k_empty=ring(stages, 1),
+                v_full=ring(stages, 1), v_empty=ring(stages, 1), s_full=ring(2, 1), p_full=ring(2, 1), o_full=ring(2, 1), run_full=ring(4, 1), run_empty=ring(4, 4))
 
 
 def plan(runs, B, state):
@@ -50,7 +50,7 @@ def each_run(B, state):
         turn += 1
 
 
-def conv(B, bf16, state):
+def conv(B, bf16, stages, state):
     T = seg = 0
     for got, run in each_run(B, state):
         if got is not None:
@@ -65,29 +65,33 @@ def conv(B, bf16, state):
         state["q"] = n if split else 2 * n
         B["q_full"].arrive()
         for ti in range(n):
-            st = (T + ti) & 1
+            st, last = (T + ti) % stages, (T + ti - 1) % stages
             for x in "kv":
-                if T + ti >= 2:
-                    yield B[x + "_empty"][st], ((T + ti) >> 1) + 1 & 1
+                if T + ti >= stages:
+                    yield B[x + "_empty"][st], (T + ti) // stages + 1 & 1
                 assert state[x][st] == 0, "a stage overwritten"
                 state[x][st] = 1 if split else 2
+                state["scales"] = T + ti
                 if not bf16:
                     B[x + "_full"][st].arrive()
                 elif ti > 0:  # (the copies of the tile before have landed)
-                    B[x + "_full"][st ^ 1].arrive()
+                    B[x + "_full"][last].arrive()
         if bf16:
-            B["k_full"][(T + n - 1) & 1].arrive()
-            B["v_full"][(T + n - 1) & 1].arrive()
+            B["k_full"][(T + n - 1) % stages].arrive()
+            B["v_full"][(T + n - 1) % stages].arrive()
         T += n
         seg += 1
 
 
-def mma(B, state):
+def mma(B, stages, state):
     T, seg, cs = 0, 0, [0, 0]
 
+    def k_full(t):
+        return B["k_full"][(T + t) % stages], (T + t) // stages & 1
+
     def scores(s, t, split, last):
-        st = (T + t) & 1
-        yield B["k_full"][st], (T + t) >> 1 & 1
+        st = (T + t) % stages
+        assert B["k_full"][st].phase * stages + st > T + t, "K is not there"
         assert state["k"][st] > 0 and state["s"][s] == 0
         state["k"][st] -= 1
         state["q"] -= 1
@@ -109,23 +113,28 @@ def mma(B, state):
         for s in range(2):
             t = s if split else 0
             if t < n:
-                yield from scores(s, t, split, t == n - 1 if split else s == 1 and n == 1)
+                yield k_full(t)
+                scores(s, t, split, t == n - 1 if split else s == 1 and n == 1)
         for t in range(0, n, step):
             for s in range(2):
                 mine = t + s if split else t
                 if mine >= n:
                     break
-                st = (T + mine) & 1
-                yield B["v_full"][st], (T + mine) >> 1 & 1
+                st = (T + mine) % stages
+                nx = mine + step
+                if nx < n and not split:
+                    yield k_full(nx)
+                yield B["v_full"][st], (T + mine) // stages & 1
                 yield B["p_full"][s], cs[s] & 1
                 cs[s] += 1
                 assert state["v"][st] > 0
                 state["v"][st] -= 1
                 if split or s == 1:
                     B["v_empty"][st].arrive()
-                nx = mine + step
                 if nx < n:
-                    yield from scores(s, nx, split, nx == n - 1 and (split or s == 1))
+                    if split:
+                        yield k_full(nx)
+                    scores(s, nx, split, nx == n - 1 and (split or s == 1))
                 else:
                     B["o_full"][s].arrive()
         T += n
@@ -133,7 +142,7 @@ def mma(B, state):
 
 
 def softmax(s, B, state, meet):
-    cs = os = blocks = 0
+    cs = os = blocks = T = 0
     for got, run in each_run(B, state):
         if got is not None:
             yield got, run
@@ -142,33 +151,37 @@ def softmax(s, B, state, meet):
         if n == 0:
             continue
         first = s if split else 0
-        for _ in range(first, n, 2 if split else 1):
+        for ti in range(first, n, 2 if split else 1):
             yield B["s_full"][s], cs & 1
             cs += 1
             assert state["s"][s] == 1
+            assert state["scales"] < T + ti + 8  # (whose scales take the place of this tile's)
             state["s"][s] = 0
             B["p_full"][s].arrive()
         if first < n:
             yield B["o_full"][s], os & 1
             os += 1
+        T += n
         blocks += 1
         meet[s] = blocks  # the barrier of both streams at a block's end
         yield None, blocks
 
 
 @pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("stages", [2, 4])
 @pytest.mark.parametrize("seed", range(40))
-def test_every_role_comes_to_its_end(bf16, seed):
+def test_every_role_comes_to_its_end(bf16, stages, seed):
     rng = random.Random(seed)
     runs = [(rng.choice([0, 1, 1, 2, 3, 4, 5, 6, 7, 12, 31]), rng.random() < 0.5) for _ in range(rng.choice([1, 2, 5, 12]))]
     for _ in range(5):
-        B, meet = bars(), [0, 0]
-        state = dict(q=0, k=[0, 0], v=[0, 0], s=[0, 0], run=[None] * 4)
-        roles = [plan(runs, B, state), conv(B, bf16, state), mma(B, state), softmax(0, B, state, meet), softmax(1, B, state, meet)]
+        B, meet = bars(stages), [0, 0]
+        state = dict(q=0, k=[0] * stages, v=[0] * stages, s=[0, 0], scales=-1, run=[None] * 4)
+        roles = [plan(runs, B, state), conv(B, bf16, stages, state), mma(B, stages, state), softmax(0, B, state, meet),
+                 softmax(1, B, state, meet)]
         waits = {i: next(g, "end") for i, g in enumerate(roles)}
         while any(w != "end" for w in waits.values()):
             ready = [i for i, w in waits.items() if w != "end" and (min(meet) >= w[1] if w[0] is None else w[0].passed(w[1]))]
             assert ready, f"stuck: {runs}"
             i = rng.choice(ready)
             waits[i] = next(roles[i], "end")
-        assert state["q"] == 0 and state["k"] == [0, 0] and state["v"] == [0, 0] and state["s"] == [0, 0]
+        assert state["q"] == 0 and state["k"] == state["v"] == [0] * stages and state["s"] == [0, 0]
