@@ -63,7 +63,7 @@ constexpr int kThreads = kSoft + kConv + 128;  // the MMA warp, one that plans, 
 // registers a thread: the launch's 72 x 896 shared out as 80 x 512 + 64 x 256 + 56 x 128
 constexpr int kRegsSoftmax = 80, kRegsConv = 64, kRegsMma = 56;
 constexpr int kBlk = kTile * 128;          // bytes of a 64-value block of Q, K or V: [row][128 bytes], swizzled
-constexpr int kTmemCols = 512;             // S / P of the streams 0.., 128..; O 256.., 256 + HD..
+constexpr int kTmemCols = 512;             // S / P: a buffer each 128; O behind them, a stream each HD
 // Queries enter binary16 times 2^7, which keeps a row with its largest |q| in [2^-4, 2^8) whole
 // but for values below 2^-27 of that; other rows by a power of two of their own.
 constexpr int kQueryShift = 7;
@@ -84,6 +84,10 @@ struct Cfg {
   // codes: 16-byte pieces a row, pieces of a row in one load of a warp, rows of it, loads a row, loads of a warp's 16 rows
   static constexpr int PPR = ROW / 16, PP = PPR < 4 ? PPR : 4, RPI = 32 / PP, SPR = PPR / PP, NI = 16 * PPR / 32;
   static_assert(RPI > 0 && SPR > 0 && NI > 0, "");
+  // Steps (a tile of a stream each) take the S buffers in turn.  Heads of 64 leave room for three: the MMA warp is then
+  // three steps ahead, and S of a stream's next tile is there when its softmax comes to it.
+  static constexpr int BUFS = HD == 64 ? 3 : 2, O_AT = BUFS * kTile;
+  static_assert(O_AT + 2 * HD <= kTmemCols, "");
   static constexpr float LIFT = BITS == 16 ? 0.f : 6.f;  // of p: small ones are then normal numbers
 };
 
@@ -97,11 +101,12 @@ struct Run {
 };
 
 struct Shared {
-  uint64_t q_full, q_empty, k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[2], p_full[2], o_full[2];
+  uint64_t q_full, q_empty, k_full[4], k_empty[4], v_full[4], v_empty[4], s_full[3], p_full[3];
+  uint64_t o_full[2][2];  // by stream and parity of its tile (two of a stream's products may be under way)
   uint64_t run_full[4], run_empty[4];
   Run run[4];
   uint32_t tmem;
-  int fail, sfail[2], last;
+  int fail, last;
   // of a tile, eight tiles deep (a tile's are written when S of the one STAGES tiles before is done, whose softmax has then
   // ended for the tile two before that): K's scales times the score scale and 2^-kQueryShift, V's exponents t
   __align__(16) float sk[kRing][kTile];
@@ -273,10 +278,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
       mbar_init(&sh.q_full, kConv / 32);
       mbar_init(&sh.q_empty, 1);
       for (int i = 0; i < 2; ++i) {
+        mbar_init(&sh.o_full[i][0], 1);
+        mbar_init(&sh.o_full[i][1], 1);
+      }
+      for (int i = 0; i < 3; ++i) {
         mbar_init(&sh.s_full[i], 1);
         mbar_init(&sh.p_full[i], 8);
-        mbar_init(&sh.o_full[i], 1);
-        sh.sfail[i] = 0;
       }
       for (int i = 0; i < 4; ++i) {
         mbar_init(&sh.k_full[i], kConv / 32);
@@ -336,60 +343,60 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
       const uint32_t lead = elect_one();
       const uint32_t tm0 = __shfl_sync(0xffffffffu, tm, 0);
       bool ok = true;
-      int seg = 0, cs[2] = {0, 0};
-      unsigned T = 0;
-      auto scores = [&](bool split, int s, int t, bool last) {  // S of stream s and tile t
-        const uint64_t q = qd + (uint64_t)(((split ? 0 : s) * C::KB) >> 4), k = kd + (uint64_t)(((T + t) % C::STAGES * C::KB) >> 4);
-#pragma unroll
-        for (int ks = 0; ks < HD / 16; ++ks) {
-          const uint64_t off = (uint64_t)(((ks / 4) * kBlk + (ks % 4) * 32) >> 4);
-          umma_ss_lead(lead, tm0 + s * 128, q + off, k + off, idqk, ks > 0);
-        }
-        umma_commit_lead(lead, &sh.s_full[s]);
-        if (split || s == 1) umma_commit_lead(lead, &sh.k_empty[(T + t) % C::STAGES]);
-        if (last) umma_commit_lead(lead, &sh.q_empty);
-      };
+      int seg = 0;
+      unsigned T = 0, K = 0, odd = 0;  // K: steps of the runs before; bit s of odd: the parity of stream s's tiles
       for (int turn = 0; ok; ++turn) {
         const Run &w = sh.run[turn & 3];
         ok = wait(&sh.run_full[turn & 3], turn >> 2 & 1);
         if (!ok || !w.any) break;
-        const int n = __shfl_sync(0xffffffffu, w.n, 0), split = __shfl_sync(0xffffffffu, (int)w.split, 0), step = split ? 2 : 1;
+        const int n = __shfl_sync(0xffffffffu, w.n, 0), split = __shfl_sync(0xffffffffu, (int)w.split, 0);
+        const int steps = split ? n : 2 * n, ahead = split ? 2 : C::BUFS;
+        // step k is tile k of split blocks, tile k / 2 of others, stream k % 2
+        auto k_there = [&](int k) {
+          const unsigned x = T + (split ? k : k >> 1);
+          return wait(&sh.k_full[x % C::STAGES], x / C::STAGES & 1);
+        };
+        auto scores = [&](int k) {
+          const unsigned x = T + (split ? k : k >> 1), s = k & 1, buf = (K + k) % C::BUFS;
+          const uint64_t q = qd + (uint64_t)(((split ? 0 : s) * C::KB) >> 4), kt = kd + (uint64_t)((x % C::STAGES * C::KB) >> 4);
+#pragma unroll
+          for (int ks = 0; ks < HD / 16; ++ks) {
+            const uint64_t off = (uint64_t)(((ks / 4) * kBlk + (ks % 4) * 32) >> 4);
+            umma_ss_lead(lead, tm0 + buf * 128, q + off, kt + off, idqk, ks > 0);
+          }
+          umma_commit_lead(lead, &sh.s_full[buf]);
+          if (split || s == 1) umma_commit_lead(lead, &sh.k_empty[x % C::STAGES]);
+          if (k == steps - 1) umma_commit_lead(lead, &sh.q_empty);
+        };
         if (n > 0) ok = wait(&sh.q_full, seg & 1);
-        for (int s = 0; s < 2 && ok; ++s) {
-          const int t = split ? s : 0;
-          if (t >= n) break;
-          ok = wait(&sh.k_full[(T + t) % C::STAGES], (T + t) / C::STAGES & 1);
+        for (int k = 0; k < min(ahead, steps) && ok; ++k) {
+          ok = k_there(k);
+          tc_fence_after();
+          if (ok) scores(k);
+        }
+        for (int k = 0; k < steps && ok; ++k) {
+          const unsigned x = T + (split ? k : k >> 1), s = k & 1, st = x % C::STAGES, buf = (K + k) % C::BUFS;
+          // (of split blocks the converting warps may wait for this tile's products before they hand K over)
+          if (!split && k + ahead < steps) ok = k_there(k + ahead);
+          ok = ok && wait(&sh.v_full[st], x / C::STAGES & 1) && wait(&sh.p_full[buf], (K + k) / C::BUFS & 1);
           if (!ok) break;
           tc_fence_after();
-          scores(split, s, t, split ? t == n - 1 : s == 1 && n == 1);
-        }
-        for (int t = 0; t < n && ok; t += step)
-          for (int s = 0; s < 2 && ok; ++s) {
-            const int mine = split ? t + s : t;
-            if (mine >= n) break;
-            const unsigned st = (T + mine) % C::STAGES;
-            const int nx = mine + step;
-            // (of split blocks the converting warps may wait for this tile's products before they hand K over)
-            if (!split && nx < n) ok = wait(&sh.k_full[(T + nx) % C::STAGES], (T + nx) / C::STAGES & 1);
-            ok = ok && wait(&sh.v_full[st], (T + mine) / C::STAGES & 1) && wait(&sh.p_full[s], cs[s] & 1);
-            if (!ok) break;
-            ++cs[s];
-            tc_fence_after();
-            const uint64_t v = vd + (uint64_t)((st * C::KB) >> 4);
+          const uint64_t v = vd + (uint64_t)((st * C::KB) >> 4);
 #pragma unroll
-            for (int ks = 0; ks < kTile / 16; ++ks)
-              umma_ts_lead(lead, tm0 + 256 + s * HD, tm0 + s * 128 + 8 * ks + (ks < 4 ? 0 : 32), v + (uint64_t)((ks * 2048) >> 4), idpv, t > 0 || ks > 0);
-            if (split || s == 1) umma_commit_lead(lead, &sh.v_empty[st]);
-            if (split && nx < n) {
-              ok = wait(&sh.k_full[(T + nx) % C::STAGES], (T + nx) / C::STAGES & 1);
-              if (!ok) break;
+          for (int ks = 0; ks < kTile / 16; ++ks)
+            umma_ts_lead(lead, tm0 + C::O_AT + s * HD, tm0 + buf * 128 + 8 * ks + (ks < 4 ? 0 : 32), v + (uint64_t)((ks * 2048) >> 4), idpv, k > 1 || ks > 0);
+          if (C::BUFS > 2 || k + ahead >= steps) umma_commit_lead(lead, &sh.o_full[s][C::BUFS > 2 ? odd >> s & 1 : 0]);
+          odd ^= 1u << s;
+          if (split || s == 1) umma_commit_lead(lead, &sh.v_empty[st]);
+          if (k + ahead < steps) {
+            if (split) {
+              ok = k_there(k + ahead);
               tc_fence_after();
             }
-            if (nx < n)
-              scores(split, s, nx, nx == n - 1 && (split || s == 1));
-            else
-              umma_commit_lead(lead, &sh.o_full[s]);
+            if (ok) scores(k + ahead);
           }
+        }
+        K += steps;
         T += n;
         seg += n > 0;
         done(turn);
@@ -627,15 +634,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
     // ---- softmax: stream s, half h of a tile's positions, thread = row
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
     const int s = warp / 8, h = warp / 4 % 2, row = tid % kStream;
-    const uint32_t tw = tm + ((uint32_t)(warp % 4 * 32) << 16), ts = tw + s * 128, to = tw + 256 + s * HD;
+    const uint32_t tw = tm + ((uint32_t)(warp % 4 * 32) << 16), to = tw + C::O_AT + s * HD;
     bool ok = true;
-    int seg = 0, cs = 0, os = 0;
-    unsigned T = 0;
-    auto sync_stream = [&](bool v) { return barrier_and(1 + s, 256, v); };
+    int seg = 0, cs = 0, os = 0;  // cs: tiles of the stream, os: blocks
+    unsigned T = 0, K = 0;        // K: steps of the runs before
+    // the two warps of a row's halves
+    auto sync_pair = [&](bool v) { return barrier_and(4 + warp / 8 * 4 + warp % 4, 64, v); };
     for (int turn = 0; ok; ++turn) {
       const Run &w = sh.run[turn & 3];
       ok = wait(&sh.run_full[turn & 3], turn >> 2 & 1);
-      if (!ok) sh.sfail[0] = sh.sfail[1] = 1;
       ok = barrier_and(3, kSoft, ok);
       if (!ok || !w.any) break;
       const int lr = w.split ? row : s * kStream + row;  // the block's row
@@ -650,9 +657,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
       bool own = false;
       for (int ti = first; ti < w.n; ti += step) {
         const int ring = (T + ti) % kRing, p0 = (w.t0 + ti) * kTile + 64 * h;
-        ok = wait(&sh.s_full[s], cs & 1);
+        const unsigned k = K + (w.split ? ti : 2 * ti + s), buf = k % C::BUFS;
+        const uint32_t ts = tw + buf * 128;
+        ok = wait(&sh.s_full[buf], k / C::BUFS & 1);
         ++cs;
-        if (!ok && lane == 0) sh.sfail[s] = 1;
         tc_fence_after();
         if (ti == first) {
           c1 = BF ? a.scale : in ? sh.qf[seg & 3][lr] : 1.f;
@@ -749,13 +757,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
             probabilities(std::false_type());
         }
         // the halves of a row go by the larger maximum
-        if (!sync_stream(ok && m == m0)) {
-          if (sh.sfail[s]) {
-            ok = false;
-            break;
-          }
+        if (!sync_pair(ok && m == m0)) {
           sh.pm[s][h][row] = m;
-          sync_stream(true);
+          // O of the tiles before (S of this one may be older than their products)
+          if (C::BUFS > 2 && ti != first && !wait(&sh.o_full[s][cs & 1], (cs - 2) >> 1 & 1)) ok = false;
+          tc_fence_after();
+          ok = sync_pair(ok);
+          if (!ok) break;
           if (busy) {
             const float mn = fmaxf(m, sh.pm[s][h ^ 1][row]), al = raise_factor(m, mn), old = raise_factor(m0, mn);
             if (__any_sync(0xffffffffu, al != 1.f)) {
@@ -767,7 +775,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
             m = mn;
             l *= old;
           }
-          sync_stream(true);  // pm is read
+          sync_pair(true);  // pm is read
         }
         if (busy) {
           l += part;
@@ -775,7 +783,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&sh.p_full[s]);
+        if (lane == 0) mbar_arrive(&sh.p_full[buf]);
       }
 
       // ---- the rows' outputs, or their parts
@@ -790,7 +798,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
       }
       const bool has = first < w.n;
       if (has && ok) {
-        ok = wait(&sh.o_full[s], os & 1);
+        ok = C::BUFS > 2 ? wait(&sh.o_full[s][(cs - 1) & 1], (cs - 1) >> 1 & 1) : wait(&sh.o_full[s][0], os & 1);
         ++os;
         sh.pl[s][h][row] = l;
       }
@@ -923,6 +931,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
         }
       }
       T += w.n;
+      K += w.split ? w.n : 2 * w.n;
       ++seg;
       done(turn);
     }

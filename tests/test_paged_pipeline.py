@@ -26,7 +26,7 @@ class Bar:
 def bars(stages):
     ring = lambda k, n: [Bar(n) for _ in range(k)]  # noqa: E731
     return dict(q_full=Bar(1), q_empty=Bar(1), k_full=ring(stages, 1), k_empty=ring(stages, 1),
-                v_full=ring(stages, 1), v_empty=ring(stages, 1), s_full=ring(2, 1), p_full=ring(2, 1), o_full=ring(2, 1), run_full=ring(4, 1), run_empty=ring(4, 4))
+                v_full=ring(stages, 1), v_empty=ring(stages, 1), s_full=ring(3, 1), p_full=ring(3, 1), o_full=[ring(2, 1), ring(2, 1)], run_full=ring(4, 1), run_empty=ring(4, 4))
 
 
 def plan(runs, B, state):
@@ -83,23 +83,25 @@ def conv(B, bf16, stages, state):
         seg += 1
 
 
-def mma(B, stages, state):
-    T, seg, cs = 0, 0, [0, 0]
+def mma(B, stages, bufs, state):
+    T = seg = K = 0
 
-    def k_full(t):
-        return B["k_full"][(T + t) % stages], (T + t) // stages & 1
+    def k_full(k, split):
+        x = T + (k if split else k // 2)
+        return B["k_full"][x % stages], x // stages & 1
 
-    def scores(s, t, split, last):
-        st = (T + t) % stages
-        assert B["k_full"][st].phase * stages + st > T + t, "K is not there"
-        assert state["k"][st] > 0 and state["s"][s] == 0
+    def scores(k, steps, split):
+        x, s, buf = T + (k if split else k // 2), k % 2, (K + k) % bufs
+        st = x % stages
+        assert B["k_full"][st].phase * stages + st > x, "K is not there"
+        assert state["k"][st] > 0 and state["s"][buf] == state["p"][buf] == 0
         state["k"][st] -= 1
         state["q"] -= 1
-        state["s"][s] = 1
-        B["s_full"][s].arrive()
+        state["s"][buf] = 1
+        B["s_full"][buf].arrive()
         if split or s == 1:
             B["k_empty"][st].arrive()
-        if last:
+        if k == steps - 1:
             B["q_empty"].arrive()
 
     for got, run in each_run(B, state):
@@ -107,42 +109,38 @@ def mma(B, stages, state):
             yield got, run
             continue
         n, split = run
-        step = 2 if split else 1
+        steps, ahead = (n, 2) if split else (2 * n, bufs)
         if n > 0:
             yield B["q_full"], seg & 1
-        for s in range(2):
-            t = s if split else 0
-            if t < n:
-                yield k_full(t)
-                scores(s, t, split, t == n - 1 if split else s == 1 and n == 1)
-        for t in range(0, n, step):
-            for s in range(2):
-                mine = t + s if split else t
-                if mine >= n:
-                    break
-                st = (T + mine) % stages
-                nx = mine + step
-                if nx < n and not split:
-                    yield k_full(nx)
-                yield B["v_full"][st], (T + mine) // stages & 1
-                yield B["p_full"][s], cs[s] & 1
-                cs[s] += 1
-                assert state["v"][st] > 0
-                state["v"][st] -= 1
-                if split or s == 1:
-                    B["v_empty"][st].arrive()
-                if nx < n:
-                    if split:
-                        yield k_full(nx)
-                    scores(s, nx, split, nx == n - 1 and (split or s == 1))
-                else:
-                    B["o_full"][s].arrive()
+        for k in range(min(ahead, steps)):
+            yield k_full(k, split)
+            scores(k, steps, split)
+        for k in range(steps):
+            x, s, buf = T + (k if split else k // 2), k % 2, (K + k) % bufs
+            st = x % stages
+            if not split and k + ahead < steps:
+                yield k_full(k + ahead, split)
+            yield B["v_full"][st], x // stages & 1
+            yield B["p_full"][buf], (K + k) // bufs & 1
+            assert state["v"][st] > 0 and state["p"][buf] == 1
+            state["v"][st] -= 1
+            state["p"][buf] = 0
+            if bufs > 2 or k + ahead >= steps:
+                B["o_full"][s][state["o"][s] & 1 if bufs > 2 else 0].arrive()
+            state["o"][s] += 1
+            if split or s == 1:
+                B["v_empty"][st].arrive()
+            if k + ahead < steps:
+                if split:
+                    yield k_full(k + ahead, split)
+                scores(k + ahead, steps, split)
+        K += steps
         T += n
         seg += n > 0
 
 
-def softmax(s, B, state, meet):
-    cs = os = blocks = T = 0
+def softmax(s, B, bufs, state, meet, rng):
+    cs = os = K = T = blocks = 0
     for got, run in each_run(B, state):
         if got is not None:
             yield got, run
@@ -152,36 +150,44 @@ def softmax(s, B, state, meet):
             continue
         first = s if split else 0
         for ti in range(first, n, 2 if split else 1):
-            yield B["s_full"][s], cs & 1
+            k = K + (ti if split else 2 * ti + s)
+            buf = k % bufs
+            yield B["s_full"][buf], k // bufs & 1
             cs += 1
-            assert state["s"][s] == 1
+            assert state["s"][buf] == 1
+            if ti != first and rng.random() < 0.3:  # a maximum is raised: O of the tiles before is rescaled
+                if bufs > 2:
+                    yield B["o_full"][s][cs & 1], (cs - 2) >> 1 & 1
+                assert state["o"][s] == cs - 1
             assert state["scales"] < T + ti + 8  # (whose scales take the place of this tile's)
-            state["s"][s] = 0
-            B["p_full"][s].arrive()
+            state["s"][buf], state["p"][buf] = 0, 1
+            B["p_full"][buf].arrive()
         if first < n:
-            yield B["o_full"][s], os & 1
+            yield (B["o_full"][s][cs - 1 & 1], (cs - 1) >> 1 & 1) if bufs > 2 else (B["o_full"][s][0], os & 1)
+            assert state["o"][s] == cs
             os += 1
         T += n
+        K += n if split else 2 * n
         blocks += 1
         meet[s] = blocks  # the barrier of both streams at a block's end
         yield None, blocks
 
 
 @pytest.mark.parametrize("bf16", [False, True])
-@pytest.mark.parametrize("stages", [2, 4])
+@pytest.mark.parametrize("stages,bufs", [(2, 2), (4, 3)])
 @pytest.mark.parametrize("seed", range(40))
-def test_every_role_comes_to_its_end(bf16, stages, seed):
+def test_every_role_comes_to_its_end(bf16, stages, bufs, seed):
     rng = random.Random(seed)
     runs = [(rng.choice([0, 1, 1, 2, 3, 4, 5, 6, 7, 12, 31]), rng.random() < 0.5) for _ in range(rng.choice([1, 2, 5, 12]))]
     for _ in range(5):
         B, meet = bars(stages), [0, 0]
-        state = dict(q=0, k=[0] * stages, v=[0] * stages, s=[0, 0], scales=-1, run=[None] * 4)
-        roles = [plan(runs, B, state), conv(B, bf16, stages, state), mma(B, stages, state), softmax(0, B, state, meet),
-                 softmax(1, B, state, meet)]
+        state = dict(q=0, k=[0] * stages, v=[0] * stages, s=[0] * 3, p=[0] * 3, o=[0, 0], scales=-1, run=[None] * 4)
+        roles = [plan(runs, B, state), conv(B, bf16, stages, state), mma(B, stages, bufs, state),
+                 softmax(0, B, bufs, state, meet, rng), softmax(1, B, bufs, state, meet, rng)]
         waits = {i: next(g, "end") for i, g in enumerate(roles)}
         while any(w != "end" for w in waits.values()):
             ready = [i for i, w in waits.items() if w != "end" and (min(meet) >= w[1] if w[0] is None else w[0].passed(w[1]))]
             assert ready, f"stuck: {runs}"
             i = rng.choice(ready)
             waits[i] = next(roles[i], "end")
-        assert state["q"] == 0 and state["k"] == state["v"] == [0] * stages and state["s"] == [0, 0]
+        assert state["q"] == 0 and state["k"] == state["v"] == [0] * stages and state["s"] == state["p"] == [0] * 3
