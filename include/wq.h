@@ -479,7 +479,8 @@ wq_status wq_decoder_tree_forward(const void *x, int n_draft, const int32_t *len
  * `max_len` is the positions of a page: 16, 32, 64, 128 or 256, the pool's positions below
  * 2^31.  Position p of a request is place p % page of the page that entry p / page of its row
  * of a block table names (int32 [batch, max_pages]); slot s of the pool is place s % page of
- * page s / page.  Requests may share pages that none of them writes to.
+ * page s / page.  Requests may share pages that none of them writes to (wq_page_plan takes
+ * every page to be held once: of sharers one at most may give a page back).
  */
 
 /*
@@ -526,7 +527,7 @@ wq_status wq_page_plan(const int32_t *lens, const int32_t *keep, const int32_t *
  *   q_norm, k_norm: bf16 [head_dim] or NULL (ones).
  *   slots:     int32 [m], different from one another; -1: the token's K and V are not kept.
  *              Outside the pool: the same, recorded as WQ_ERR_ARG.
- *   q:         bf16 [m, n_heads, head_dim].
+ *   q:         bf16 [m, n_heads, head_dim], not over qkv.
  */
 wq_status wq_qkv_paged(const void *qkv, int qkv_dtype, const void *x, int m, int d, const int32_t *positions,
                        const float *table, int n_pos, const void *q_norm, const void *k_norm, int n_heads, unsigned flags,
@@ -546,7 +547,7 @@ wq_status wq_paged_read(const wq_kv_cache *pool, const int32_t *slots, int m, vo
  * positions, its new tokens' among them (wq_qkv_paged has written them).  Its row i sees the
  * first kv_lens[b] - nq + i + 1:
  *   o = bf16( softmax_j(scale q . K_j) V_j ).
- *   q, o:    bf16 [m, n_heads, head_dim].  Rows behind cu[batch] are left as they were.
+ *   q, o:    bf16 [m, n_heads, head_dim], memory of their own each.  Rows behind cu[batch] are left as they were.
  *   cu:      int32 [batch + 1], kv_lens: int32 [batch], tables: int32 [batch, max_pages], all
  *            on the device (wq_page_plan makes them).
  *   max_q:   the most rows of a sequence, 1 <= max_q <= m: a hint for which kernels run, and a bound.
@@ -561,7 +562,8 @@ wq_status wq_paged_read(const wq_kv_cache *pool, const int32_t *slots, int m, vo
  *   the values of V of a quantized pool, times a power of two, to binary16 (2^-11).  Everything
  *   else is fp32.
  * Workspace: wq_attn_paged_workspace_bytes for up to `batch` sequences and m rows, zero-filled
- * before first use (wq_workspace_init).
+ * before first use (wq_workspace_init) and after a call whose device status reads
+ * WQ_ERR_TIMEOUT; calls that share one must not overlap in time on the GPU.
  */
 size_t wq_attn_paged_workspace_bytes(int batch, int m, int n_heads, int n_kv, int head_dim);
 wq_status wq_attn_paged(const void *q, int m, int max_q, int n_heads, const wq_kv_cache *pool, int batch, const int32_t *cu,

@@ -46,6 +46,10 @@ wq_status cuda_fail(cudaError_t e, const char *what) {
 }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool share_bytes(const void *a, size_t na, const void *b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + nb && y < x + na;
+}
 
 bool group_ok(int g) { return g == 32 || g == 64 || g == 128; }
 
@@ -1759,6 +1763,8 @@ wq_status attn_paged_impl(const void *q, int m, int max_q, int n_heads, const wq
   if (max_q < 1 || max_q > m) return fail(WQ_ERR_ARG, "max_q %d of %d rows", max_q, m);
   if (!q || !cu || !kv_lens || !tables || !o || !counters) return fail(WQ_ERR_ARG, "null pointer");
   if (!aligned16(q) || !aligned16(o) || !aligned16(counters)) return fail(WQ_ERR_ALIGN, "q, o or workspace not 16-byte aligned");
+  const size_t bytes = (size_t)m * n_heads * pool->head_dim * 2;
+  if (share_bytes(q, bytes, o, bytes)) return fail(WQ_ERR_ARG, "o lies over q");
   const int sms = num_sms();
   if (sms <= 0) return fail(WQ_ERR_CUDA, "cannot query the current device");
   a.q = q, a.kc = pool->k, a.vc = pool->v, a.km = pool->k_meta, a.vm = pool->v_meta;
@@ -1829,6 +1835,9 @@ wq_status wq_qkv_paged(const void *qkv, int qkv_dtype, const void *x, int m, int
   const void *all[] = {qkv, x, positions ? table : nullptr, q_norm, k_norm, q};
   for (const void *p : all)
     if (!aligned16(p)) return fail(WQ_ERR_ALIGN, "qkv, x, table, q_norm, k_norm or q not 16-byte aligned");
+  const size_t row = (size_t)pool->head_dim * m;
+  if (share_bytes(qkv, row * (n_heads + 2 * (size_t)pool->n_kv) * (qkv_dtype == WQ_F32 ? 4 : 2), q, row * n_heads * 2))
+    return fail(WQ_ERR_ARG, "q lies over qkv");
   a.qkv = qkv, a.x = x, a.positions = positions, a.table = table, a.q_norm = q_norm, a.k_norm = k_norm, a.slots = slots;
   a.kc = pool->k, a.vc = pool->v, a.km = pool->k_meta, a.vm = pool->v_meta, a.q = q;
   a.d = d, a.n_heads = n_heads, a.n_kv = pool->n_kv, a.n_pos = n_pos, a.head_norm = (flags & WQ_HEAD_NORM) ? 1 : 0;

@@ -22,6 +22,12 @@
 // (item) that other CTAs share is left in the workspace, and the last of them to arrive adds
 // up all parts in their order.  A warp takes 16 positions (32 of 4 bits) at a time, 16 of which
 // always lie in one page, through a ring of its own that cp.async fills: no warp waits for another.
+// The maximum is only raised, and sums and O rescaled, where a score passes it by 8.
+//   64 tokens over 4k to 8k positions of 4 bits (8 kv heads of 128, 4 query heads each) take 91
+// to 94 us for 426 MB, 0.69 of the copy's rate: 311 instructions a warp for 16 positions at
+// 0.58 a clock and scheduler, with the three warps that 168 registers leave room for.  One
+// token over 500 positions of 8 bits takes 9, over 32,767 of 4 bits 19: the chain of one
+// launch and one block, and the sum of the parts.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>

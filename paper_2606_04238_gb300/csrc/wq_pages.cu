@@ -44,7 +44,8 @@ __device__ __forceinline__ int above(const int *sums, int n, int x) {
   return lo;
 }
 
-// Inclusive sums over the CTA's threads, on top of `carry`, which becomes the total.
+// Inclusive sums over the CTA's threads, on top of `carry`, which becomes the total.  (All
+// the tables' entries are fewer than 2^31: host check.)
 __device__ __forceinline__ int scan(int v, int *warps, int &carry) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
@@ -77,6 +78,8 @@ __device__ __forceinline__ int scan(int v, int *warps, int &carry) {
 // `have` on are written, and the stack is written above n_free and read below it.  The
 // cluster's barrier stands between the reads of lens and n_free and the writes of kv_lens
 // and n_free_out, which may be the same arrays.
+//   Bound by latency, not by its few kB: 32 requests of a token each take 4.1 us from launch
+// to launch, 256 requests with 20 new prompts among them 7.0.
 __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PagePlanArgs a) {
   extern __shared__ int plan_smem[];
   __shared__ int warps[kPlanThreads / 32];
@@ -170,7 +173,10 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PagePlanA
 // products and roundings are separate and in one order (a row's squares: its halves, a
 // lane's eight pairwise, the lanes pairwise), so that equal rows have equal codes.
 //   A CTA takes a token.  HD / 16 lanes take a row, values 8 l .. and HD/2 + 8 l .., so that
-// a value and the one it is rotated with are one lane's.
+// a value and the one it is rotated with are one lane's.  Bound by instructions and loads in
+// flight together: 4093 tokens of 40 + 16 bf16 heads of 128 to 4 bits take 26.7 us, 3.9 TB/s
+// (one value an instruction and without the next heads on their way 37); 16 tokens 4.0, a
+// launch's latency.
 template <int HD, int BITS, bool F32>
 __global__ void __launch_bounds__(kPutThreads, F32 && BITS != 16 ? 4 : 5) qkv_paged_kernel(const QkvPagedArgs a) {
   constexpr int THREADS = kPutThreads, LPR = HD / 16, GROUPS = THREADS / LPR, U = 2;  // lanes a row, rows a pass, passes in flight
@@ -352,7 +358,8 @@ __global__ void __launch_bounds__(kPutThreads, F32 && BITS != 16 ? 4 : 5) qkv_pa
 }
 
 // Rows at the slots, zeros where a slot is -1.  Place i of the launch: token and head, K's
-// before V's.
+// before V's.  Bound by memory: 20,000 tokens of 8 heads of 128 from 4 bits to bf16 take
+// 18.8 us, 104 MB at 5.5 TB/s.
 template <int HD, int BITS, bool F32>
 __global__ void __launch_bounds__(kPagedReadThreads) paged_read_kernel(const PagedReadArgs a, const Divisor by_kv) {
   constexpr int LPR = HD / 16;

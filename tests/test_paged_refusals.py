@@ -83,3 +83,11 @@ def test_workspaces_of_no_sizes(L):
 def test_a_layer_is_needed(L):
     assert L.wq_decoder_paged_forward(256, 1, 1, 1, 256, 256, 256, 256, None, None, None, pool(), 256, 4, 256, 8, 0, 256, 256, 1 << 30,
                                       None) == ARG
+
+
+def test_outputs_over_their_inputs(L):
+    row = 8 * 128 * 2  # bytes of q and o; of qkv 12 heads of fp32
+    for o in (1 << 16, (1 << 16) + 16, (1 << 16) + 4 * row - 16, (1 << 16) - 4 * row + 16):
+        assert attn(L, q=1 << 16, o=o) == ARG and b"over" in L.wq_last_error()
+    for q in (1 << 16, (1 << 16) + 3 * 12 * 128 * 4 - 16, (1 << 16) - 3 * row + 16):
+        assert put(L, qkv=1 << 16, h=8, q=q) == ARG and b"over" in L.wq_last_error()
