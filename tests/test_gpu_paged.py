@@ -359,6 +359,27 @@ def test_scales(bits, scale):
     run_attn([1, 2, 90], [200, 300, 100], 8, 2, 64, bits, 16, scale=scale, seed=3)
 
 
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("nq,down", [(1, False), (150, False), (150, True)])
+def test_scores_that_rise(nq, down, hd, bits):
+    """Scores that grow (or fall) by some 13 powers of two a tile: the maximum is raised, and O rescaled, in every one."""
+    h, kv, page, n = 8, 2, 32, 1100
+    cu, tables, n_pages = ragged([nq], [n], page, 5)
+    k, v = (randn(n_pages, kv, page, hd, seed=s) for s in (1, 2))
+    along = torch.sign(randn(hd, seed=3))
+    at = torch.arange(n, device="cuda").flip(0) if down else torch.arange(n, device="cuda")
+    ids = tables[0].long().repeat_interleave(page)[:n]
+    k[ids, :, torch.arange(n, device="cuda") % page] += (at / n * 80 / hd ** 0.5)[:, None, None] * along
+    pool = wq.kv_pool(n_pages, kv, page, hd, bits)
+    fill_pool(pool, k.to(BF), v.to(BF))
+    q = (randn(nq, h, hd, seed=5) + along).to(BF)
+    o = wq.attn_paged(q, i32(*cu), i32(n), tables, pool, max_q=nq)
+    ref, bound = attn_ref(q, cu, [n], tables, pool, hd ** -0.5)
+    check(o, ref, bound, f"{nq} {hd} {bits}")
+    assert status() == 0
+
+
 def test_max_q_is_a_bound_not_a_shape():
     """The kernels that a larger max_q takes give what the smaller one's do, within the bound."""
     for bits in (16, 8, 4):
