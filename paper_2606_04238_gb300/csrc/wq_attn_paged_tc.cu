@@ -453,25 +453,37 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
       {
         const int c = ct % C::CH;
         const __nv_bfloat16 *q0 = reinterpret_cast<const __nv_bfloat16 *>(a.q) + ((size_t)w.q0 * a.H + w.g * rep) * HD + c * 8;
-#pragma unroll 2
-        for (int r = ct / C::CH; r < (w.live + 31) / 32 * 32; r += kConv / C::CH) {
-          const int row = w.r0 + min(r, w.live - 1), tok = (int)by_rep.divide(row);
-          const uint4 v = __ldg(reinterpret_cast<const uint4 *>(q0 + ((size_t)tok * a.H + row - tok * rep) * HD));
-          uint4 *dst = reinterpret_cast<uint4 *>(qbuf + (r / kStream) * C::KB + (c / 8) * kBlk + r % kStream * 128 + (((c & 7) ^ (r & 7)) << 4));
-          if constexpr (BF) {
-            *dst = v;
-          } else {
-            uint32_t big = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
-            big = max(big & 0xffffu, big >> 16);  // the row's largest |q|, as bf16 bits
+        constexpr int STEP = kConv / C::CH, QU = 4;  // rows a pass, passes on their way
+        const int rows = (w.live + 31) / 32 * 32;
+#pragma unroll 1
+        for (int r0 = ct / C::CH; r0 < rows; r0 += QU * STEP) {
+          uint4 x[QU];
 #pragma unroll
-            for (int o = C::CH / 2; o >= 1; o >>= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, o));
-            const int e = (int)(big >> 7) - 127;
-            int mine = kQueryShift;
-            if (big != 0 && (e < -4 || e >= 8)) mine = max(min(min(126, 14 - e), kQueryShift + 126), -114);
-            const float f = pow2i(mine);
-            if (c == 0) sh.qf[seg & 3][r] = pow2i(kQueryShift - mine);
-            *dst = make_uint4(pack_h2(bf_lo(v.x) * f, bf_hi(v.x) * f), pack_h2(bf_lo(v.y) * f, bf_hi(v.y) * f),
-                              pack_h2(bf_lo(v.z) * f, bf_hi(v.z) * f), pack_h2(bf_lo(v.w) * f, bf_hi(v.w) * f));
+          for (int u = 0; u < QU; ++u) {
+            const int row = w.r0 + min(r0 + u * STEP, w.live - 1), tok = (int)by_rep.divide(row);
+            x[u] = __ldg(reinterpret_cast<const uint4 *>(q0 + ((size_t)tok * a.H + row - tok * rep) * HD));
+          }
+#pragma unroll
+          for (int u = 0; u < QU; ++u) {
+            const int r = r0 + u * STEP;
+            if (r >= rows) break;  // (a warp's lanes alike: rows is a multiple of 32)
+            const uint4 v = x[u];
+            uint4 *dst = reinterpret_cast<uint4 *>(qbuf + (r / kStream) * C::KB + (c / 8) * kBlk + r % kStream * 128 + (((c & 7) ^ (r & 7)) << 4));
+            if constexpr (BF) {
+              *dst = v;
+            } else {
+              uint32_t big = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+              big = max(big & 0xffffu, big >> 16);  // the row's largest |q|, as bf16 bits
+#pragma unroll
+              for (int o = C::CH / 2; o >= 1; o >>= 1) big = max(big, __shfl_xor_sync(0xffffffffu, big, o));
+              const int e = (int)(big >> 7) - 127;
+              int mine = kQueryShift;
+              if (big != 0 && (e < -4 || e >= 8)) mine = max(min(min(126, 14 - e), kQueryShift + 126), -114);
+              const float f = pow2i(mine);
+              if (c == 0) sh.qf[seg & 3][r] = pow2i(kQueryShift - mine);
+              *dst = make_uint4(pack_h2(bf_lo(v.x) * f, bf_hi(v.x) * f), pack_h2(bf_lo(v.y) * f, bf_hi(v.y) * f),
+                                pack_h2(bf_lo(v.z) * f, bf_hi(v.z) * f), pack_h2(bf_lo(v.w) * f, bf_hi(v.w) * f));
+            }
           }
         }
       }
@@ -898,45 +910,50 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
           // all parts of the block in their order: CTA c0 has its begin (in its place 1), the others their first blocks
           // (0); a split block's streams one after the other
           __threadfence();
-          constexpr int LPR = HD / 4, RU = 4, STEP = kSoft / LPR;  // lanes a row, rows of a thread in flight
-          const int e = 4 * (tid % LPR), subs = w.split ? 2 : 1, parts = (cl - c0 + 1) * subs;
+          constexpr int LPR = HD / 4, RU = 4, STEP = kSoft / LPR, ROW = HD + 4, PART = kBlockRows * ROW;  // lanes a row, rows of a thread in flight
+          // (the run's numbers by value: stores of results might otherwise be stores to them)
+          const int e = 4 * (tid % LPR), split = w.split, parts = (cl - c0 + 1) << split, live = w.live, r0 = w.r0, h0 = w.g * rep;
+          const float *const p0 = a.part + (size_t)c0 * 2 * PART;
+          __nv_bfloat16 *const o0 = reinterpret_cast<__nv_bfloat16 *>(a.o) + ((size_t)w.q0 * a.H + h0) * HD + e;
 #pragma unroll 1
-          for (int r = tid / LPR; r < w.live; r += RU * STEP) {
+          for (int r = tid / LPR; r < live; r += RU * STEP) {
             float M[RU], S[RU];
             float4 O[RU];
+            int at[RU];
 #pragma unroll
-            for (int j = 0; j < RU; ++j) M[j] = -INFINITY, S[j] = 0.f, O[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int j = 0; j < RU; ++j) {
+              M[j] = -INFINITY, S[j] = 0.f, O[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+              at[j] = min(r + j * STEP, live - 1) * ROW;
+            }
 #pragma unroll 1
             for (int k = 0; k < parts; ++k) {
-              const int cta = k / subs, sub = k % subs;
-              const float *ps = a.part + (((size_t)(c0 + cta) * 2 + (cta == 0)) * kBlockRows + sub * kStream + r) * (HD + 4);
+              const int cta = k >> split;
+              const float *const ps = p0 + (size_t)(cta == 0 ? 1 : 2 * cta) * PART + (k & split) * (kStream * ROW);
               float2 ml[RU];
               float4 ov[RU];
 #pragma unroll
               for (int j = 0; j < RU; ++j) {
-                const bool there = r + j * STEP < w.live;
-                ml[j] = there ? __ldcg(reinterpret_cast<const float2 *>(ps + (size_t)j * STEP * (HD + 4) + HD)) : make_float2(-INFINITY, 0.f);
-                ov[j] = there ? __ldcg(reinterpret_cast<const float4 *>(ps + (size_t)j * STEP * (HD + 4) + e)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                ml[j] = __ldcg(reinterpret_cast<const float2 *>(ps + at[j] + HD));
+                ov[j] = __ldcg(reinterpret_cast<const float4 *>(ps + at[j] + e));
               }
 #pragma unroll
               for (int j = 0; j < RU; ++j) {
-                if (ml[j].x == -INFINITY && ml[j].y == 0.f) continue;  // (its values were not written)
+                const bool none = ml[j].x == -INFINITY;  // (then its values were not written, or its sum alone counts)
                 const float mn = fmaxf(M[j], ml[j].x);
-                const float f0 = M[j] == -INFINITY ? 0.f : ex2(M[j] - mn);
-                const float f = ml[j].x == -INFINITY ? 0.f : ex2(ml[j].x - mn);  // (a NaN of a part stays NaN)
+                const float f0 = M[j] == -INFINITY ? 0.f : ex2(M[j] - mn), f = none ? 0.f : ex2(ml[j].x - mn);
+                S[j] = fmaf(S[j], M[j] == -INFINITY ? 1.f : f0, none ? ml[j].y : ml[j].y * f);  // (a NaN of a part stays NaN)
                 M[j] = mn;
-                S[j] = fmaf(ml[j].y, f, S[j] * f0);
-                O[j].x = fmaf(ov[j].x, f, O[j].x * f0), O[j].y = fmaf(ov[j].y, f, O[j].y * f0);
-                O[j].z = fmaf(ov[j].z, f, O[j].z * f0), O[j].w = fmaf(ov[j].w, f, O[j].w * f0);
+                O[j].x = fmaf(none ? 0.f : ov[j].x, f, O[j].x * f0), O[j].y = fmaf(none ? 0.f : ov[j].y, f, O[j].y * f0);
+                O[j].z = fmaf(none ? 0.f : ov[j].z, f, O[j].z * f0), O[j].w = fmaf(none ? 0.f : ov[j].w, f, O[j].w * f0);
               }
             }
 #pragma unroll
             for (int j = 0; j < RU; ++j) {
-              const int rr = w.r0 + r + j * STEP, t = (int)by_rep.divide(rr);
-              if (r + j * STEP >= w.live) break;
-              const bool nothing = M[j] == -INFINITY && S[j] == 0.f;
-              *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(a.o) + ((size_t)(w.q0 + t) * a.H + w.g * rep + rr - t * rep) * HD + e) =
-                  nothing ? make_uint2(0, 0) : make_uint2(pack_bf2(O[j].x / S[j], O[j].y / S[j]), pack_bf2(O[j].z / S[j], O[j].w / S[j]));
+              const int rr = r0 + r + j * STEP, t = (int)by_rep.divide(rr);
+              const float inv = M[j] == -INFINITY && S[j] == 0.f ? 0.f : 1.f / S[j];
+              if (r + j * STEP < live)
+                *reinterpret_cast<uint2 *>(o0 + ((ptrdiff_t)t * a.H + rr - t * rep) * HD) =
+                    make_uint2(pack_bf2(O[j].x * inv, O[j].y * inv), pack_bf2(O[j].z * inv, O[j].w * inv));
             }
           }
         }
