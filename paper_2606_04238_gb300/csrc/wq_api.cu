@@ -1776,7 +1776,7 @@ wq_status attn_paged_impl(const void *q, int m, int max_q, int n_heads, const wq
   a.o = o;
   // Up to 16 rows (query tokens x query heads of a kv head) a sequence the mma.sync kernel, above the tcgen05 kernel.  A
   // batch that may have both kinds of sequences takes both, each its own: 14 decode steps over 1,500 to 3,000 positions
-  // of 8 bits beside two chunks of 250 tokens take 110 us, on the tcgen05 kernel alone 114.
+  // of 8 bits beside two chunks of 250 tokens took 110 us, on the tcgen05 kernel alone 114.
   const int rep = n_heads / pool->n_kv, few = std::max(8, rep) / rep;  // tokens of a sequence that is left to mma.sync beside others
   a.least_q = 0, a.most_q = INT32_MAX;
   cudaError_t e = cudaSuccess;

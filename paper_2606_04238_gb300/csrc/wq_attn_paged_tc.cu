@@ -30,12 +30,12 @@
 //
 // Bound by the softmax warps' chains (scores from TMEM, 2^x, conversion, P to TMEM: four
 // times 16 columns a tile), which the other stream's and the products' round trip overlap in
-// part: 2000 tokens over 14,000 positions of 4 bits, 40 heads of 128, take 548 us, 0.51 of the
+// part: 2000 tokens over 14,000 positions of 4 bits, 40 heads of 128, take 534 us, 0.52 of the
 // measured dense rate for the products alone; a prompt of 4000 over a bf16 pool, 64 heads of
-// 64, takes 218, 0.31 (half as many products a 2^x).  Tried and slower: tiles of 64 positions
+// 64, takes 216, 0.32 (half as many products a 2^x).  Tried and slower: tiles of 64 positions
 // with S twice (718 us for 572), a row's 64 scores before any is stored (227 for 219), 32
 // columns at a time.  Short runs are bound by their ends: what 14 decode steps and two chunks
-// of 250 tokens take (99 us) is in the larger part Q's and the first tile's way in, and parts
+// of 250 tokens take (96 us) is in the larger part Q's and the first tile's way in, and parts
 // of 132 KB written and added up.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
