@@ -723,8 +723,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
           }
         };
         // The half row's p with maximum m, into the columns whose scores have been read, and their sum (p stands for 2^-t).
-        // 16 columns at a time: where those add up to kMostSum (or there is no maximum yet) m is raised first, to a whole
-        // number, so that what has been computed with the old one is rescaled by an exact power of two.
+        // 16 columns at a time: where those add up to kMostSum, or are the first that the row sees, m is raised first, to a whole
+        // number, so that what has been computed with the old one is rescaled by an exact power of two.  (The first maximum is
+        // the scores' own: powers of scores below -126 are zeros, and say nothing.)
         const float m0 = m;
         float part = 0.f;
         auto probabilities = [&](auto is_plain) {
@@ -755,7 +756,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
               float x, y;
               unpack_f32x2(add_f32x2(s2[0], s2[1]), x, y);
               sum = x + y;
-              const bool up = sum >= kMostSum || (m == -INFINITY && sum > 0.f);
+              const bool up = sum >= kMostSum || (m == -INFINITY && (!some || sh.limit[s][row] > p0 + 16 * c));
               if (raised || !__any_sync(0xffffffffu, up)) break;
               // (rare: the scores once more)
               tmem_ld16(ts + 64 * h + 16 * c, *reinterpret_cast<uint32_t(*)[16]>(&u));
@@ -764,7 +765,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
               float mx = -INFINITY;
 #pragma unroll
               for (int j = 0; j < 16; ++j) mx = fmaxf(mx, u[j]);
-              const float mn = up ? ceilf(mx) - C::LIFT : m, al = raise_factor(m, mn);
+              const float mn = up ? ceilf(mx) - C::LIFT : m, al = raise_factor(m, mn);  // (all scores -inf: no maximum yet)
               if (c > 0) rescale_p<BF>(ts + 64 * h, c, al);
               part *= al;
               m = mn;
