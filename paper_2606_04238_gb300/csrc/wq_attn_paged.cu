@@ -538,10 +538,10 @@ __global__ void __launch_bounds__(kWarps * 32, occupancy(HD, BITS, NT)) attn_pag
           O1 = fmaf(so[w][r][e + 1], f, O1);
         }
         if (all) {
-          const bool none = M == -INFINITY && Ls == 0.f;
+          if (Ls == 0.f) Ls = NAN;  // scores that are all -inf have no softmax
           *reinterpret_cast<uint32_t *>(reinterpret_cast<__nv_bfloat16 *>(a.o) +
                                         ((size_t)(s.q0 + row / rep) * a.H + g * rep + row % rep) * HD + e) =
-              none ? 0u : pack_bf2(O0 / Ls, O1 / Ls);
+              s.len == 0 ? 0u : pack_bf2(O0 / Ls, O1 / Ls);  // (not served: zeros)
         } else {
           float *pt = part + (size_t)r * PS;
           *reinterpret_cast<float2 *>(pt + e) = make_float2(O0, O1);

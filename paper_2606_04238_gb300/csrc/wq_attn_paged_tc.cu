@@ -730,6 +730,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
         float part = 0.f;
         auto probabilities = [&](auto is_plain) {
           constexpr bool PLAIN = decltype(is_plain)::value;
+          const int sees = PLAIN || !some ? 64 : sh.limit[s][row] - p0;  // of the half's columns
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             const int t = BF ? 0 : sh.te[ring][4 * h + c];
@@ -756,7 +757,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
               float x, y;
               unpack_f32x2(add_f32x2(s2[0], s2[1]), x, y);
               sum = x + y;
-              const bool up = sum >= kMostSum || (m == -INFINITY && (!some || sh.limit[s][row] > p0 + 16 * c));
+              const bool up = sum >= kMostSum || (m == -INFINITY && sees > 16 * c);
               if (raised || !__any_sync(0xffffffffu, up)) break;
               // (rare: the scores once more)
               tmem_ld16(ts + 64 * h + 16 * c, *reinterpret_cast<uint32_t(*)[16]>(&u));
