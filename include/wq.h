@@ -551,7 +551,8 @@ wq_status wq_paged_read(const wq_kv_cache *pool, const int32_t *slots, int m, vo
  *   cu:      int32 [batch + 1], kv_lens: int32 [batch], tables: int32 [batch, max_pages], all
  *            on the device (wq_page_plan makes them).
  *   max_q:   the most rows of a sequence, 1 <= max_q <= m: a hint for which kernels run, and a bound.
- *   What positions hold that a row does not see, infinities and NaN too, does not reach it.
+ *   What positions hold that a row does not see, infinities and NaN too, does not reach it.  Where all scores
+ *   that a row sees are -inf (infinite keys of a bf16 pool) it is NaN, as its softmax is.
  *   kv_lens[b] == -1: the sequence's rows are zeros.  Offsets that do not ascend within m, more
  *   than max_q rows, or a length below nq or above max_pages page skip the sequence (o
  *   unwritten); a page outside the pool is read as page 0.  All are recorded as WQ_ERR_ARG

@@ -832,8 +832,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
       tc_fence_after();
       const float L = has ? sh.pl[s][0][row] + sh.pl[s][1][row] : 0.f;
       const bool alone = w.whole && !w.split;
-      const bool none = m == -INFINITY && L == 0.f;  // (all scores NaN: L is NaN)
-      const float inv = alone ? (none ? 0.f : 1.f / L) : 1.f;
+      // (every row of a block with tiles sees a position: a sum of 0 is that of scores that are all -inf, which have no softmax)
+      const float inv = !alone ? 1.f : L == 0.f ? NAN : 1.f / L;
       const int c0 = w.c0, cl = w.cl;
       float *pt = a.part + (((size_t)blockIdx.x * 2 + (w.t0 == 0)) * kBlockRows + s * kStream + row) * (HD + 4);
       if (has && busy) {
@@ -869,9 +869,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
             uint4 v[4];
 #pragma unroll
             for (int e = 0; e < 32; e += 8)
-              v[e / 8] = none ? make_uint4(0, 0, 0, 0)
-                              : make_uint4(pack_bf2(o[e] * inv, o[e + 1] * inv), pack_bf2(o[e + 2] * inv, o[e + 3] * inv),
-                                           pack_bf2(o[e + 4] * inv, o[e + 5] * inv), pack_bf2(o[e + 6] * inv, o[e + 7] * inv));
+              v[e / 8] = make_uint4(pack_bf2(o[e] * inv, o[e + 1] * inv), pack_bf2(o[e + 2] * inv, o[e + 3] * inv),
+                                    pack_bf2(o[e + 4] * inv, o[e + 5] * inv), pack_bf2(o[e + 6] * inv, o[e + 7] * inv));
             transpose4(v, at);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -952,7 +951,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const AttnPa
 #pragma unroll
             for (int j = 0; j < RU; ++j) {
               const int rr = r0 + r + j * STEP, t = (int)by_rep.divide(rr);
-              const float inv = M[j] == -INFINITY && S[j] == 0.f ? 0.f : 1.f / S[j];
+              const float inv = S[j] == 0.f ? NAN : 1.f / S[j];
               if (r + j * STEP < live)
                 *reinterpret_cast<uint2 *>(o0 + ((ptrdiff_t)t * a.H + rr - t * rep) * HD) =
                     make_uint2(pack_bf2(O[j].x * inv, O[j].y * inv), pack_bf2(O[j].z * inv, O[j].w * inv));
