@@ -576,8 +576,11 @@ wq_status wq_attn_paged(const void *q, int m, int max_q, int n_heads, const wq_k
  *   qkv = x deq(Wqkv)^T (fp32), q and the pages' rows by wq_qkv_paged(..., WQ_HEAD_NORM),
  *   o = wq_attn_paged(..., scale 1/sqrt(head_dim)), then the output projection and the MLP block as in
  *   wq_decoder_layer_forward (flags likewise).
- * x, y: bf16 [m, d].  The y of rows behind cu[batch] means nothing.  The layer's rope_theta
- * is not used (the angles are the table's).  m <= 16384.
+ * x, y: bf16 [m, d].  The y of rows behind cu[batch] means nothing, nor does that of a sequence that
+ * the attention skips.  A token whose position is outside the table (WQ_ERR_ARG in the device status)
+ * has zeros for q, K and V, in its slot too; one whose slot is outside the pool leaves no row, and the y
+ * of tokens that see its place means nothing.  The layer's rope_theta is not used (the angles are
+ * the table's).  m <= 16384.
  * Workspace: wq_decoder_paged_workspace_bytes, zero-filled before first use (wq_workspace_init).
  */
 size_t wq_decoder_paged_workspace_bytes(int batch, int m, const wq_decoder_layer *layer);

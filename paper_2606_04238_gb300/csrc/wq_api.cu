@@ -1744,6 +1744,36 @@ wq_status check_group(int n_heads, int n_kv) {
   return WQ_OK;
 }
 
+// bad_zeros: a token whose position is not in the table has rows of zeros, where it is else skipped.
+wq_status qkv_paged_impl(const void *qkv, int qkv_dtype, const void *x, int m, int d, const int32_t *positions,
+                         const float *table, int n_pos, const void *q_norm, const void *k_norm, int n_heads, unsigned flags,
+                         const wq_kv_cache *pool, const int32_t *slots, void *q, bool bad_zeros, cudaStream_t s) {
+  wq_status st;
+  QkvPagedArgs a{};
+  if ((st = check_pool(pool, &a.shift)) != WQ_OK || (st = check_dtype(qkv_dtype)) != WQ_OK) return st;
+  if (m < 0) return fail(WQ_ERR_ARG, "m %d", m);
+  if (flags & ~WQ_HEAD_NORM) return fail(WQ_ERR_ARG, "unknown flags 0x%x", flags);
+  if ((q_norm || k_norm) && !(flags & WQ_HEAD_NORM)) return fail(WQ_ERR_ARG, "weights of a head norm without WQ_HEAD_NORM");
+  if (n_heads <= 0 || (long long)n_heads + 2ll * pool->n_kv > 1 << 16) return fail(WQ_ERR_SHAPE, "heads %d/%d", n_heads, pool->n_kv);
+  if (x && (d <= 0 || d % 8 != 0)) return fail(WQ_ERR_SHAPE, "d %d (a positive multiple of 8)", d);
+  if (positions && n_pos <= 0) return fail(WQ_ERR_SHAPE, "a table of %d positions", n_pos);
+  if (m == 0) return ok();
+  if (!qkv || !slots || !q || (positions && !table)) return fail(WQ_ERR_ARG, "null pointer");
+  const void *all[] = {qkv, x, positions ? table : nullptr, q_norm, k_norm, q};
+  for (const void *p : all)
+    if (!aligned16(p)) return fail(WQ_ERR_ALIGN, "qkv, x, table, q_norm, k_norm or q not 16-byte aligned");
+  const size_t row = (size_t)pool->head_dim * m;
+  if (share_bytes(qkv, row * (n_heads + 2 * (size_t)pool->n_kv) * (qkv_dtype == WQ_F32 ? 4 : 2), q, row * n_heads * 2))
+    return fail(WQ_ERR_ARG, "q lies over qkv");
+  a.qkv = qkv, a.x = x, a.positions = positions, a.table = table, a.q_norm = q_norm, a.k_norm = k_norm, a.slots = slots;
+  a.kc = pool->k, a.vc = pool->v, a.km = pool->k_meta, a.vm = pool->v_meta, a.q = q;
+  a.d = d, a.n_heads = n_heads, a.n_kv = pool->n_kv, a.n_pos = n_pos, a.head_norm = (flags & WQ_HEAD_NORM) ? 1 : 0;
+  a.n_pages = pool->batch, a.bad_zeros = bad_zeros;
+  cudaError_t e = launch_qkv_paged(a, m, pool->head_dim, pool->bits, qkv_dtype == WQ_F32, s);
+  if (e != cudaSuccess) return cuda_fail(e, "paged projection launch");
+  return ok();
+}
+
 // The arrival counters, at the workspace's start, and the partial results behind them.
 size_t paged_counter_bytes(int sms) { return up256(sizeof(int) * (size_t)attn_paged_ctas(sms)); }
 size_t paged_part_bytes(int hd, int sms) {
@@ -1821,30 +1851,8 @@ wq_status wq_page_plan(const int32_t *lens, const int32_t *keep, const int32_t *
 wq_status wq_qkv_paged(const void *qkv, int qkv_dtype, const void *x, int m, int d, const int32_t *positions,
                        const float *table, int n_pos, const void *q_norm, const void *k_norm, int n_heads, unsigned flags,
                        const wq_kv_cache *pool, const int32_t *slots, void *q, void *stream) {
-  wq_status st;
-  QkvPagedArgs a{};
-  if ((st = check_pool(pool, &a.shift)) != WQ_OK || (st = check_dtype(qkv_dtype)) != WQ_OK) return st;
-  if (m < 0) return fail(WQ_ERR_ARG, "m %d", m);
-  if (flags & ~WQ_HEAD_NORM) return fail(WQ_ERR_ARG, "unknown flags 0x%x", flags);
-  if ((q_norm || k_norm) && !(flags & WQ_HEAD_NORM)) return fail(WQ_ERR_ARG, "weights of a head norm without WQ_HEAD_NORM");
-  if (n_heads <= 0 || (long long)n_heads + 2ll * pool->n_kv > 1 << 16) return fail(WQ_ERR_SHAPE, "heads %d/%d", n_heads, pool->n_kv);
-  if (x && (d <= 0 || d % 8 != 0)) return fail(WQ_ERR_SHAPE, "d %d (a positive multiple of 8)", d);
-  if (positions && n_pos <= 0) return fail(WQ_ERR_SHAPE, "a table of %d positions", n_pos);
-  if (m == 0) return ok();
-  if (!qkv || !slots || !q || (positions && !table)) return fail(WQ_ERR_ARG, "null pointer");
-  const void *all[] = {qkv, x, positions ? table : nullptr, q_norm, k_norm, q};
-  for (const void *p : all)
-    if (!aligned16(p)) return fail(WQ_ERR_ALIGN, "qkv, x, table, q_norm, k_norm or q not 16-byte aligned");
-  const size_t row = (size_t)pool->head_dim * m;
-  if (share_bytes(qkv, row * (n_heads + 2 * (size_t)pool->n_kv) * (qkv_dtype == WQ_F32 ? 4 : 2), q, row * n_heads * 2))
-    return fail(WQ_ERR_ARG, "q lies over qkv");
-  a.qkv = qkv, a.x = x, a.positions = positions, a.table = table, a.q_norm = q_norm, a.k_norm = k_norm, a.slots = slots;
-  a.kc = pool->k, a.vc = pool->v, a.km = pool->k_meta, a.vm = pool->v_meta, a.q = q;
-  a.d = d, a.n_heads = n_heads, a.n_kv = pool->n_kv, a.n_pos = n_pos, a.head_norm = (flags & WQ_HEAD_NORM) ? 1 : 0;
-  a.n_pages = pool->batch;
-  cudaError_t e = launch_qkv_paged(a, m, pool->head_dim, pool->bits, qkv_dtype == WQ_F32, static_cast<cudaStream_t>(stream));
-  if (e != cudaSuccess) return cuda_fail(e, "paged projection launch");
-  return ok();
+  return qkv_paged_impl(qkv, qkv_dtype, x, m, d, positions, table, n_pos, q_norm, k_norm, n_heads, flags, pool, slots, q, false,
+                        static_cast<cudaStream_t>(stream));
 }
 
 wq_status wq_paged_read(const wq_kv_cache *pool, const int32_t *slots, int m, void *k, void *v, int dtype, void *stream) {
@@ -1924,8 +1932,9 @@ wq_status wq_decoder_paged_forward(const void *x, int m, int max_q, int batch, c
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if ((st = decoder_projection("qkv", x, m, &Ly.qkv, nullptr, w8 + W.qkv, WQ_F32, W.b_qkv, W.cnt_qkv, W.proj_qkv, w8, s)) != WQ_OK)
     return st;
-  if ((st = wq_qkv_paged(w8 + W.qkv, WQ_F32, x, m, d, positions, table, n_pos, q_norm, k_norm, H, WQ_HEAD_NORM, pool, slots,
-                         w8 + W.q, stream)) != WQ_OK)
+  // (rows of a token without a position must not be what an earlier call left in the workspace and in the pages)
+  if ((st = qkv_paged_impl(w8 + W.qkv, WQ_F32, x, m, d, positions, table, n_pos, q_norm, k_norm, H, WQ_HEAD_NORM, pool, slots,
+                           w8 + W.q, true, s)) != WQ_OK)
     return fail(st, "projections to pages: %s", g_last_error.c_str());
   if ((st = attn_paged_impl(w8 + W.q, m, max_q, H, pool, batch, cu, kv_lens, tables, max_pages, 1.f / std::sqrt((float)hd),
                             w8 + W.o, w8 + W.cnt_attn, w8 + W.attn, s)) != WQ_OK)

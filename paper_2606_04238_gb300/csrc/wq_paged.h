@@ -36,6 +36,7 @@ struct QkvPagedArgs {
   uint32_t *km, *vm;
   void *q;  // bf16 [m][n_heads][HD]
   int d, n_heads, n_kv, n_pos, head_norm, n_pages, shift;
+  int bad_zeros;  // rows of a token whose position is not in the table: 1 zeros, 0 not written
 };
 cudaError_t launch_qkv_paged(const QkvPagedArgs &a, int m, int hd, int bits, bool f32, cudaStream_t s);
 

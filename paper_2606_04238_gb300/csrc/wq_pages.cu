@@ -207,13 +207,13 @@ __global__ void __launch_bounds__(kPutThreads, F32 && BITS != 16 ? 4 : 5) qkv_pa
   const bool bad = a.positions && (pos < 0 || pos >= a.n_pos), out = slot < -1 || (slot >> a.shift) >= a.n_pages;
   if (bad || out) {
     if (tid == 0) atomicExch(&g_pages_status, -1);
-    if (bad) return;
+    if (bad && !a.bad_zeros) return;
   }
   const bool put = slot >= 0 && !out;
   // (two values an instruction; each of its operations is rounded as by itself)
   uint64_t co[4], si[4];  // of the lane's eight angles
   if (a.positions) {
-    const float4 *tab = reinterpret_cast<const float4 *>(a.table + ((size_t)pos * (HD / 2) + 8 * lane) * 2);
+    const float4 *tab = reinterpret_cast<const float4 *>(a.table + ((size_t)(bad ? 0 : pos) * (HD / 2) + 8 * lane) * 2);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float4 t = __ldg(tab + e);
@@ -241,22 +241,22 @@ __global__ void __launch_bounds__(kPutThreads, F32 && BITS != 16 ? 4 : 5) qkv_pa
 #pragma unroll
     for (int w = 0; w < THREADS / 32; ++w) tot += red[w];
     const float r = __fdiv_rn(1.f, __fsqrt_rn(__fadd_rn(__fdiv_rn(tot, (float)a.d), kRmsEps)));
-    rs = pack_f32x2(r, r);
+    rs = bad ? 0 : pack_f32x2(r, r);  // (x may hold anything there)
   }
   auto work = [&](int pass, uint4 (&r)[F32 ? 4 : 2]) {
     const int h = pass * GROUPS + grp;
-    const bool in = h < heads, is_q = h < a.n_heads, turns = h < a.n_heads + a.n_kv;
+    const bool in = h < heads, is_q = h < a.n_heads, turns = h < a.n_heads + a.n_kv, has = in && !bad;
     uint64_t w[8];  // values 8 l .., then HD/2 + 8 l ..
     if constexpr (F32) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        w[2 * i] = in ? (uint64_t)r[i].y << 32 | r[i].x : 0, w[2 * i + 1] = in ? (uint64_t)r[i].w << 32 | r[i].z : 0;
+        w[2 * i] = has ? (uint64_t)r[i].y << 32 | r[i].x : 0, w[2 * i + 1] = has ? (uint64_t)r[i].w << 32 | r[i].z : 0;
     } else {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const uint32_t x[4] = {r[i].x, r[i].y, r[i].z, r[i].w};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[4 * i + e] = in ? pack_f32x2(bf_lo(x[e]), bf_hi(x[e])) : 0;
+        for (int e = 0; e < 4; ++e) w[4 * i + e] = has ? pack_f32x2(bf_lo(x[e]), bf_hi(x[e])) : 0;
       }
     }
     fetch(pass + U, r);
