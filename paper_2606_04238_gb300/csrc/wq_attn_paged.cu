@@ -204,8 +204,9 @@ __global__ void __launch_bounds__(kWarps * 32, occupancy(HD, BITS, NT)) attn_pag
     // than 2^32 rows: host check; what lies behind the last position is some row of it)
     uint32_t rows = 0;
     auto load_rows = [&](int k) {
-      const int p = (u0 + kWarps * (k + lane / L::SUBS)) * L::UNIT + lane % L::SUBS * kSub;
-      int id = a.tables[(size_t)b * a.max_pages + (min(p, c1 - 1) >> a.shift)];
+      // (lanes ahead of the last position may be 2016 past it: above 2^31 where it is the largest that tables may have)
+      const uint32_t p = (uint32_t)(u0 + kWarps * (k + lane / L::SUBS)) * L::UNIT + lane % L::SUBS * kSub;
+      int id = a.tables[(size_t)b * a.max_pages + (min(p, (uint32_t)c1 - 1) >> a.shift)];
       if ((unsigned)id >= (unsigned)a.n_pages) {
         id = 0;
         atomicExch(&g_attn_paged_status, -1);
