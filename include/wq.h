@@ -494,7 +494,8 @@ wq_status wq_decoder_tree_forward(const void *x, int n_draft, const int32_t *len
  *   tables:     int32 [batch, max_pages], in place: only entries from ceil(lens[b] / page)
  *               on are written (what a request gives back stays in its row, out of use).
  *   free_pages: int32 [n_pages], in place: a stack of n_free[0] pages; written from there on.
- *   n_free, n_free_out: int32 [1], and what is left.  n_free_out may be n_free.
+ *   n_free, n_free_out: int32 [1], and what is left.  n_free_out may be n_free.  No two of the arrays written may lie over
+ *               one another.
  *   cu:         int32 [batch + 1]: request b's tokens are rows cu[b] .. cu[b + 1] - 1 of the
  *               step (at most m).
  *   kv_lens:    int32 [batch]: keep[b] + n_new[b], the next step's lens; may be lens.  -1:
@@ -527,7 +528,7 @@ wq_status wq_page_plan(const int32_t *lens, const int32_t *keep, const int32_t *
  *   q_norm, k_norm: bf16 [head_dim] or NULL (ones).
  *   slots:     int32 [m], different from one another; -1: the token's K and V are not kept.
  *              Outside the pool: the same, recorded as WQ_ERR_ARG.
- *   q:         bf16 [m, n_heads, head_dim], not over qkv.
+ *   q:         bf16 [m, n_heads, head_dim], over none of the inputs and not over the pool.
  */
 wq_status wq_qkv_paged(const void *qkv, int qkv_dtype, const void *x, int m, int d, const int32_t *positions,
                        const float *table, int n_pos, const void *q_norm, const void *k_norm, int n_heads, unsigned flags,
@@ -536,7 +537,8 @@ wq_status wq_qkv_paged(const void *qkv, int qkv_dtype, const void *x, int m, int
 /*
  * Reads the rows at m slots back: k, v of `dtype` [m, n_kv, head_dim], exact (WQ_F32) or
  * rounded once (WQ_BF16); zeros where a slot is -1.  A slot outside the pool is recorded as
- * WQ_ERR_ARG and its rows are left unwritten.  m n_kv < 2^29.
+ * WQ_ERR_ARG and its rows are left unwritten.  k, v, the slots and the pool are memory of their own each.
+ * m n_kv < 2^29.
  */
 wq_status wq_paged_read(const wq_kv_cache *pool, const int32_t *slots, int m, void *k, void *v, int dtype, void *stream);
 
@@ -547,7 +549,7 @@ wq_status wq_paged_read(const wq_kv_cache *pool, const int32_t *slots, int m, vo
  * positions, its new tokens' among them (wq_qkv_paged has written them).  Its row i sees the
  * first kv_lens[b] - nq + i + 1:
  *   o = bf16( softmax_j(scale q . K_j) V_j ).
- *   q, o:    bf16 [m, n_heads, head_dim], memory of their own each.  Rows behind cu[batch] are left as they were.
+ *   q, o:    bf16 [m, n_heads, head_dim]; o and the workspace are memory of their own each.  Rows behind cu[batch] are left as they were.
  *   cu:      int32 [batch + 1], kv_lens: int32 [batch], tables: int32 [batch, max_pages], all
  *            on the device (wq_page_plan makes them).
  *   max_q:   the most rows of a sequence, 1 <= max_q <= m: a hint for which kernels run, and a bound.

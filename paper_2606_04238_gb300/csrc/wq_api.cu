@@ -8,6 +8,7 @@
 #include <cstring>
 #include <algorithm>
 #include <array>
+#include <initializer_list>
 #include <map>
 #include <mutex>
 #include <string>
@@ -1730,6 +1731,20 @@ wq_status check_pool(const wq_kv_cache *c, int *shift) {
     return fail(WQ_ERR_SHAPE, "a pool of %d pages of %d positions of %d heads", c->batch, c->max_len, c->n_kv);
   return WQ_OK;
 }
+// An array of a call, and whether an output lies over any of others (NULL: not given).
+struct Span {
+  const void *at;
+  size_t bytes;
+};
+bool lies_over(const Span &out, std::initializer_list<Span> others) {
+  for (const Span &o : others)
+    if (out.at && o.at && out.bytes && o.bytes && share_bytes(out.at, out.bytes, o.at, o.bytes)) return true;
+  return false;
+}
+bool lies_over_pool(const Span &out, const wq_kv_cache &c) {
+  const size_t rows = (size_t)c.batch * c.n_kv * c.max_len, held = rows * (c.head_dim * c.bits / 8), meta = c.bits == 16 ? 0 : rows * 4;
+  return lies_over(out, {{c.k, held}, {c.v, held}, {c.k_meta, meta}, {c.v_meta, meta}});
+}
 // A ragged batch: its sequences, rows and the width of its tables.
 wq_status check_ragged(int batch, int m, int max_pages, int page) {
   if (batch < 0 || batch > kMaxRequests) return fail(batch < 0 ? WQ_ERR_ARG : WQ_ERR_SHAPE, "%d requests, at most %d", batch, kMaxRequests);
@@ -1762,9 +1777,14 @@ wq_status qkv_paged_impl(const void *qkv, int qkv_dtype, const void *x, int m, i
   const void *all[] = {qkv, x, positions ? table : nullptr, q_norm, k_norm, q};
   for (const void *p : all)
     if (!aligned16(p)) return fail(WQ_ERR_ALIGN, "qkv, x, table, q_norm, k_norm or q not 16-byte aligned");
-  const size_t row = (size_t)pool->head_dim * m;
-  if (share_bytes(qkv, row * (n_heads + 2 * (size_t)pool->n_kv) * (qkv_dtype == WQ_F32 ? 4 : 2), q, row * n_heads * 2))
-    return fail(WQ_ERR_ARG, "q lies over qkv");
+  const size_t row = (size_t)pool->head_dim * m, norm = 2 * (size_t)pool->head_dim;
+  const Span out{q, row * n_heads * 2};
+  if (lies_over(out, {{qkv, row * (n_heads + 2 * (size_t)pool->n_kv) * (qkv_dtype == WQ_F32 ? 4 : 2)}, {x, 2 * (size_t)m * d}}))
+    return fail(WQ_ERR_ARG, "q lies over qkv or x");
+  if (lies_over_pool(out, *pool) ||
+      lies_over(out, {{slots, 4 * (size_t)m}, {positions, 4 * (size_t)m}, {q_norm, norm}, {k_norm, norm},
+                      {positions ? table : nullptr, 4 * (size_t)n_pos * pool->head_dim}}))
+    return fail(WQ_ERR_ARG, "q lies over the pool, slots, positions, table, q_norm or k_norm");
   a.qkv = qkv, a.x = x, a.positions = positions, a.table = table, a.q_norm = q_norm, a.k_norm = k_norm, a.slots = slots;
   a.kc = pool->k, a.vc = pool->v, a.km = pool->k_meta, a.vm = pool->v_meta, a.q = q;
   a.d = d, a.n_heads = n_heads, a.n_kv = pool->n_kv, a.n_pos = n_pos, a.head_norm = (flags & WQ_HEAD_NORM) ? 1 : 0;
@@ -1780,9 +1800,10 @@ size_t paged_part_bytes(int hd, int sms) {
   return up256(4 * std::max(attn_paged_part_floats(hd, sms), attn_paged_tc_part_floats(hd, sms)));
 }
 
+// (ws: the whole of the workspace)
 wq_status attn_paged_impl(const void *q, int m, int max_q, int n_heads, const wq_kv_cache *pool, int batch, const int32_t *cu,
                           const int32_t *kv_lens, const int32_t *tables, int max_pages, float scale, void *o, void *counters,
-                          void *part, cudaStream_t s) {
+                          void *part, const Span &ws, cudaStream_t s) {
   wq_status st;
   AttnPagedArgs a{};
   if ((st = check_pool(pool, &a.shift)) != WQ_OK || (st = check_ragged(batch, m, max_pages, pool->max_len)) != WQ_OK ||
@@ -1793,8 +1814,11 @@ wq_status attn_paged_impl(const void *q, int m, int max_q, int n_heads, const wq
   if (max_q < 1 || max_q > m) return fail(WQ_ERR_ARG, "max_q %d of %d rows", max_q, m);
   if (!q || !cu || !kv_lens || !tables || !o || !counters) return fail(WQ_ERR_ARG, "null pointer");
   if (!aligned16(q) || !aligned16(o) || !aligned16(counters)) return fail(WQ_ERR_ALIGN, "q, o or workspace not 16-byte aligned");
-  const size_t bytes = (size_t)m * n_heads * pool->head_dim * 2;
-  if (share_bytes(q, bytes, o, bytes)) return fail(WQ_ERR_ARG, "o lies over q");
+  const Span out{o, (size_t)m * n_heads * pool->head_dim * 2};
+  if (lies_over(out, {{q, out.bytes}})) return fail(WQ_ERR_ARG, "o lies over q");
+  if (lies_over_pool(out, *pool) || lies_over(out, {{cu, 4 * ((size_t)batch + 1)}, {kv_lens, 4 * (size_t)batch}, {tables, 4 * (size_t)batch * max_pages}}))
+    return fail(WQ_ERR_ARG, "o lies over the pool, cu, kv_lens or tables");
+  if (lies_over(ws, {{q, out.bytes}, out})) return fail(WQ_ERR_ARG, "the workspace lies over q or o");
   const int sms = num_sms();
   if (sms <= 0) return fail(WQ_ERR_CUDA, "cannot query the current device");
   a.q = q, a.kc = pool->k, a.vc = pool->v, a.km = pool->k_meta, a.vm = pool->v_meta;
@@ -1839,6 +1863,13 @@ wq_status wq_page_plan(const int32_t *lens, const int32_t *keep, const int32_t *
   if (batch == 0) return ok();
   if (!lens || !n_new || !tables || !free_pages || !n_free || !n_free_out || !cu || !kv_lens || (m > 0 && (!positions || !slots)))
     return fail(WQ_ERR_ARG, "null pointer");
+  // (lens, keep, n_new and n_free are read before anything is written)
+  const Span out[] = {{tables, 4 * (size_t)batch * max_pages}, {free_pages, 4 * (size_t)n_pages}, {cu, 4 * ((size_t)batch + 1)},
+                      {kv_lens, 4 * (size_t)batch}, {positions, 4 * (size_t)m}, {slots, 4 * (size_t)m}, {n_free_out, 4}};
+  for (const Span &p : out)
+    for (const Span *o = out; o != &p; ++o)
+      if (lies_over(p, {*o}))
+        return fail(WQ_ERR_ARG, "one of tables, free_pages, n_free_out, cu, kv_lens, positions and slots lies over another");
   a.lens = lens, a.keep = keep, a.n_new = n_new, a.tables = tables, a.free_pages = free_pages;
   a.n_free = n_free, a.n_free_out = n_free_out;
   a.batch = batch, a.max_pages = max_pages, a.n_pages = n_pages, a.m = m;
@@ -1864,6 +1895,11 @@ wq_status wq_paged_read(const wq_kv_cache *pool, const int32_t *slots, int m, vo
   if (m == 0) return ok();
   if (!slots || !k || !v) return fail(WQ_ERR_ARG, "null pointer");
   if (!aligned16(k) || !aligned16(v)) return fail(WQ_ERR_ALIGN, "k or v not 16-byte aligned");
+  const size_t bytes = (size_t)m * pool->n_kv * pool->head_dim * (dtype == WQ_F32 ? 4 : 2);
+  if (lies_over({k, bytes}, {{v, bytes}})) return fail(WQ_ERR_ARG, "k lies over v");
+  for (const void *p : {k, v})
+    if (lies_over_pool({p, bytes}, *pool) || lies_over({p, bytes}, {{slots, 4 * (size_t)m}}))
+      return fail(WQ_ERR_ARG, "k or v lies over the pool or slots");
   a.kc = pool->k, a.vc = pool->v, a.km = pool->k_meta, a.vm = pool->v_meta, a.slots = slots, a.k = k, a.v = v;
   a.m = m, a.n_kv = pool->n_kv, a.n_pages = pool->batch;
   cudaError_t e = launch_paged_read(a, pool->head_dim, pool->bits, dtype == WQ_F32, static_cast<cudaStream_t>(stream));
@@ -1880,16 +1916,17 @@ size_t wq_attn_paged_workspace_bytes(int batch, int m, int n_heads, int n_kv, in
 wq_status wq_attn_paged(const void *q, int m, int max_q, int n_heads, const wq_kv_cache *pool, int batch, const int32_t *cu,
                         const int32_t *kv_lens, const int32_t *tables, int max_pages, float scale, void *o, void *ws,
                         size_t ws_bytes, void *stream) {
-  size_t at = 0;
+  size_t at = 0, used = 0;
   if (pool && batch > 0 && m > 0 && ws) {
     const int sms = num_sms();
     const size_t need = wq_attn_paged_workspace_bytes(batch, m, n_heads, pool->n_kv, pool->head_dim);
     // (sizes without a workspace are refused below)
     if (need && ws_bytes < need) return fail(WQ_ERR_WORKSPACE, "attention workspace of %zu bytes, %zu needed", ws_bytes, need);
     if (need) at = paged_counter_bytes(sms);
+    used = need;
   }
   return attn_paged_impl(q, m, max_q, n_heads, pool, batch, cu, kv_lens, tables, max_pages, scale, o, ws,
-                         static_cast<uint8_t *>(ws) + at, static_cast<cudaStream_t>(stream));
+                         static_cast<uint8_t *>(ws) + at, {ws, used}, static_cast<cudaStream_t>(stream));
 }
 
 size_t wq_decoder_paged_workspace_bytes(int batch, int m, const wq_decoder_layer *layer) {
@@ -1937,7 +1974,7 @@ wq_status wq_decoder_paged_forward(const void *x, int m, int max_q, int batch, c
                            w8 + W.q, true, s)) != WQ_OK)
     return fail(st, "projections to pages: %s", g_last_error.c_str());
   if ((st = attn_paged_impl(w8 + W.q, m, max_q, H, pool, batch, cu, kv_lens, tables, max_pages, 1.f / std::sqrt((float)hd),
-                            w8 + W.o, w8 + W.cnt_attn, w8 + W.attn, s)) != WQ_OK)
+                            w8 + W.o, w8 + W.cnt_attn, w8 + W.attn, {w8 + W.attn, W.n_attn}, s)) != WQ_OK)
     return fail(st, "attention: %s", g_last_error.c_str());
   return decoder_after_attention(x, m, Ly, flags, y, W, w8, s);
 }
