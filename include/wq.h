@@ -560,10 +560,12 @@ wq_status wq_paged_read(const wq_kv_cache *pool, const int32_t *slots, int m, vo
  *   unwritten); a page outside the pool is read as page 0.  All are recorded as WQ_ERR_ARG
  *   in the device status.
  *   n_heads / n_kv <= 16, batch <= 2048, m <= 2^18, max_pages page <= 2^31 - 1024.
- *   Roundings: each probability once to 16 bits (binary16 over a quantized pool, 2^-11 of
- *   its term at most; bf16 over a bf16 pool, 2^-8), and o; where max_q n_heads / n_kv > 16 also
- *   the values of V of a quantized pool, times a power of two, to binary16 (2^-11).  Everything
- *   else is fp32.
+ *   Roundings: each probability once to 16 bits, and o.  Over a bf16 pool to bf16, 2^-8 of its term; over
+ *   a quantized pool to binary16, 2^-11 of its term, and where the probability times V's scale is below
+ *   2^-19 of the row's largest such product, up to 2^-29 of that largest a code's step.  Where
+ *   max_q n_heads / n_kv > 16 also the values of V of a quantized pool, times a power of two, to
+ *   binary16 (2^-11).  Everything else is fp32.  Scores (times log2 e) are below 2^24 in size: fp32 does
+ *   not tell larger ones apart by less than a factor of 2 in the probability, and their rows mean nothing.
  * Workspace: wq_attn_paged_workspace_bytes for up to `batch` sequences and m rows, zero-filled
  * before first use (wq_workspace_init) and after a call whose device status reads
  * WQ_ERR_TIMEOUT; calls that share one must not overlap in time on the GPU.

@@ -1828,9 +1828,12 @@ wq_status attn_paged_impl(const void *q, int m, int max_q, int n_heads, const wq
   a.counters = static_cast<int *>(counters);
   a.part = static_cast<float *>(part);
   a.o = o;
-  // Up to 16 rows (query tokens x query heads of a kv head) a sequence the mma.sync kernel, above the tcgen05 kernel.  A
-  // batch that may have both kinds of sequences takes both, each its own: 14 decode steps over 1,500 to 3,000 positions
-  // of 8 bits beside two chunks of 250 tokens took 110 us, on the tcgen05 kernel alone 114.
+  // Up to 16 rows (query tokens x query heads of a kv head) a sequence the mma.sync kernel, which holds no more, above them
+  // the tcgen05 kernel.  At 16 rows, 8 kv heads of 128: 64 sequences over 2000 to 4000 positions of 4 bits take 95 us, on
+  // tcgen05 174, of bf16 135 and 177; one over 8000 of 4 bits 35 and 41; but 16 over 250 to 500 of bf16 35 and 26.
+  // A batch that may have both kinds of sequences takes both, each its own: 32 decode steps over 2000 to 4000 positions
+  // of 4 bits beside a chunk of 512 tokens take 107 us, on the tcgen05 kernel alone 163; 14 over 1,500 to 3,000 of 8 bits
+  // beside two chunks of 250 103 and 105.
   const int rep = n_heads / pool->n_kv, few = std::max(8, rep) / rep;  // tokens of a sequence that is left to mma.sync beside others
   a.least_q = 0, a.most_q = INT32_MAX;
   cudaError_t e = cudaSuccess;

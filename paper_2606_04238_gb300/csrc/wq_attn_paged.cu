@@ -14,8 +14,9 @@
 // subnormal numbers code 2^-24, and the zero points could come off the sums: a third of the
 // instructions less.  But the tensor cores add products of subnormal numbers with 2^-14 of
 // their size lost, a 4-bit column's error then 2^-14 of its codes and not of their difference.)
-// p_j is rounded to binary16 (2^-11 of its term at most; 2^6 larger than above, so that small
-// ones are normal numbers) or over a bf16 cache to bf16 (2^-8); everything else is fp32.
+// p_j is rounded to binary16 (2^6 larger than above, so that it is a normal number, off by 2^-11
+// of its term at most, down to 2^-20 of the largest; below that by 2^-31 of the largest) or over a bf16
+// cache to bf16 (2^-8); everything else is fp32.
 //
 // The blocks of 64 positions (128 of 4 bits) of all (sequence, row tile, kv head) are laid end to end and
 // every CTA takes an equal run of them, found from the lengths themselves; what it has of an
@@ -111,8 +112,8 @@ struct Lay : RowLay<HD, BITS> {
   static __device__ __forceinline__ int v_swz(int row) { return ROW >= 128 ? 2 * (row & 3) : ROW == 64 ? 2 * (row / 2 & 1) : 0; }
 };
 
-// CTAs an SM holds: 168 registers a thread (with 128 and four CTAs 64 tokens over 4k to 8k positions of 4 bits take 117 us
-// for 110, over 2k to 4k of a bf16 pool 82 for 72); a bf16 ring of heads of 128 takes 96 KB.
+// CTAs an SM holds: 168 registers a thread (with 128 and four CTAs 64 tokens over 4k to 8k positions of 4 bits take 100 us
+// for 92, over 2k to 4k of a bf16 pool, heads of 64, 78 for 68); a bf16 ring of heads of 128 takes 96 KB.
 constexpr int occupancy(int hd, int bits, int nt) { return bits == 16 && hd == 128 ? 2 : kCtasPerSm; }
 
 // A sequence; the blocks of positions of each of its items, and its tiles of rows.

@@ -19,9 +19,10 @@
 //
 // K's operands are code - z, exact, its scales factors of the scores; V's are (code - z) s 2^-t
 // rounded to binary16, t one for 16 positions, or, where their scales span more than 2^8, one for
-// each, taken into the score.  The maximum is not searched in every tile: p is taken
-// with the maximum that the row has, which is raised, and what was computed with it rescaled in
-// TMEM by a power of two, only where 16 p add up to 2^15 (p is 2^6 at most where it is raised).
+// each, taken into the score.  The maximum is not searched in every tile: a row's first is that
+// of the first 16 scores that it sees; from there on p is taken with the maximum that the row has,
+// which is raised, and what was computed with it rescaled in TMEM by a power of two, only where
+// 16 p add up to 2^15 (p is 2^6 at most where it is raised).
 //
 // The tiles of all blocks are laid end to end and every CTA takes an equal run, found from the
 // lengths themselves; blocks are paired, the first with the last and so on inward, so that
@@ -30,9 +31,9 @@
 //
 // Bound by the softmax warps' chains (scores from TMEM, 2^x, conversion, P to TMEM: four
 // times 16 columns a tile), which the other stream's and the products' round trip overlap in
-// part: 2000 tokens over 14,000 positions of 4 bits, 40 heads of 128, take 534 us, 0.52 of the
+// part: 2000 tokens over 14,000 positions of 4 bits, 40 heads of 128, take 529 us, 0.53 of the
 // measured dense rate for the products alone; a prompt of 4000 over a bf16 pool, 64 heads of
-// 64, takes 216, 0.32 (half as many products a 2^x).  Tried and slower: tiles of 64 positions
+// 64, takes 213, 0.32 (half as many products a 2^x).  Tried and slower: tiles of 64 positions
 // with S twice (718 us for 572), a row's 64 scores before any is stored (227 for 219), 32
 // columns at a time.  Short runs are bound by their ends: what 14 decode steps and two chunks
 // of 250 tokens take (96 us) is in the larger part Q's and the first tile's way in, and parts

@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from paged_util import attn_ref, check, fill_pool, i32, status
+from paged_util import attn_ref, check, fill_pool, i32, pool_values, status
 from paper_2606_04238_gb300 import wq
 from test_gpu_paged import BF, ragged, randn
 
@@ -87,3 +87,18 @@ def test_low_scores_beside_others(level):
         q = q.to(BF)
         o = wq.attn_paged(q, i32(*cu), i32(*lens), tables, pool, max_q=200)
         check(o, *attn_ref(q, cu, lens, tables, pool, hd ** -0.5), f"{bits}")
+
+
+@pytest.mark.parametrize("bits", [16, 8, 4])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("nq", [3, 150])
+@pytest.mark.parametrize("level", [1e5, 1e6, 1e7, -1e7])
+def test_scores_of_millions(level, nq, hd, bits):
+    """Up to 2^24 (times log2 e) fp32's steps make a mean of what is seen: no infinity, no NaN, nothing beyond the largest V."""
+    n = 300
+    q, cu, tables, pool = shifted(nq, n, hd, bits, level / 16, seed=nq)
+    q[..., 3] *= 16
+    o = wq.attn_paged(q, i32(*cu), i32(n), tables, pool, max_q=nq).double()
+    kind = 2.0 ** -8 if bits == 16 else 2.0 ** -10  # roundings of p and V, and the store's
+    V = pool_values(pool)[1][tables[0].long()].transpose(1, 2).reshape(-1, 2, hd)[:n].abs().amax(0).repeat_interleave(4, 0)
+    assert bool((o.abs() <= V * (1 + kind) * (1 + 2.0 ** -8)).all()) and status() == 0
