@@ -1952,8 +1952,9 @@ wq_status wq_decoder_paged_forward(const void *x, int m, int max_q, int batch, c
   const int d = Ly.mlp.gate.k, H = Ly.n_heads, Hkv = Ly.n_kv, hd = Ly.head_dim;
   wq_status st;
   int shift;
+  // (what the parts would refuse is refused before the first of them has written to the pages)
   if ((st = check_decoder_layer(Ly)) != WQ_OK || (st = check_pool(pool, &shift)) != WQ_OK ||
-      (st = check_ragged(batch, m, max_pages, pool->max_len)) != WQ_OK)
+      (st = check_ragged(batch, m, max_pages, pool->max_len)) != WQ_OK || (st = check_group(H, Hkv)) != WQ_OK)
     return st;
   if (pool->n_kv != Hkv || pool->head_dim != hd)
     return fail(WQ_ERR_SHAPE, "pool of %d heads of %d, layer of %d of %d", pool->n_kv, pool->head_dim, Hkv, hd);
@@ -1961,6 +1962,7 @@ wq_status wq_decoder_paged_forward(const void *x, int m, int max_q, int batch, c
   if (m > kMaxGemmTokens) return fail(WQ_ERR_SHAPE, "%d rows, at most %d", m, kMaxGemmTokens);
   if (batch == 0 || m == 0) return ok();
   if (max_q < 1 || max_q > m) return fail(WQ_ERR_ARG, "max_q %d of %d rows", max_q, m);
+  if (n_pos <= 0) return fail(WQ_ERR_SHAPE, "a table of %d positions", n_pos);
   if (!x || !cu || !kv_lens || !positions || !slots || !tables || !table || !y) return fail(WQ_ERR_ARG, "null pointer");
   const int sms = num_sms();
   if (sms <= 0) return fail(WQ_ERR_CUDA, "cannot query the current device");
